@@ -1,0 +1,252 @@
+// C-ABI entry points of the block-scaled 8-bit operators: argument checks,
+// workspace layout.
+#include <algorithm>
+#include <cmath>
+
+#include "scaled.h"
+
+using namespace moe;
+
+namespace {
+
+bool width_ok(int32_t v) { return v > 0 && v % kDimAlign == 0 && v <= kMaxWidth; }
+bool type_ok(int32_t t) { return t == MOE_BF16 || t == MOE_FP32; }
+bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+// 16-byte loads and stores of tensors, 4-byte ones of scale rows.
+moe_status check_tensor(const char *fn, const char *name, const void *p, uintptr_t a = 16) {
+    if (!p) return fail(MOE_ERR_INVALID, "%s: %s is NULL", fn, name);
+    if (!aligned(p, a))
+        return fail(MOE_ERR_INVALID, "%s: %s is not %d-byte aligned", fn, name, (int)a);
+    return MOE_OK;
+}
+moe_status check_pair(const char *fn, const char *name, const void *q, const void *s) {
+    MOE_TRY(check_tensor(fn, name, q));
+    return check_tensor(fn, "a scale tensor", s, 4);
+}
+
+// Products of `rows` rows in `experts` groups: the kernels count rows and
+// tiles in 32 bits.
+moe_status check_product(const char *fn, int64_t rows, int64_t experts, int32_t n, int32_t k) {
+    if (!width_ok(n) || !width_ok(k))
+        return fail(MOE_ERR_INVALID, "%s: widths %d, %d not multiples of %d up to 2^20", fn, n, k,
+                    kDimAlign);
+    if (rows >= (int64_t(1) << 31))
+        return fail(MOE_ERR_UNSUPPORTED, "%s: 2^31 rows or more", fn);
+    if ((rows / 32 + experts + 1) * ((int64_t)n / 128 + 1) >= (int64_t(1) << 31))
+        return fail(MOE_ERR_UNSUPPORTED, "%s: %lld rows of %d columns are too many tiles", fn,
+                    (long long)rows, n);
+    return MOE_OK;
+}
+
+int64_t row_cap(const moe_dims *d) {
+    return d->tokens * std::min<int64_t>(d->top_k, d->local_count);
+}
+
+// Grouped calls' common arguments.
+moe_status check_group(const char *fn, const moe_dims *d, int32_t e_first, int32_t e_count,
+                       const int32_t *offsets, const int32_t *sorted_slot, int32_t k) {
+    if (e_first < 0 || e_count < 0 || e_first > d->local_count - e_count)
+        return fail(MOE_ERR_INVALID, "%s: expert range outside [0, local_count)", fn);
+    if (d->tokens == 0 || e_count == 0) return MOE_OK;
+    if (!offsets) return fail(MOE_ERR_INVALID, "%s: offsets is NULL", fn);
+    if (sorted_slot && (uint64_t)d->tokens * (uint64_t)k >= kMaxOffset)
+        return fail(MOE_ERR_UNSUPPORTED, "%s: a gathered token matrix of 4 GiB or more", fn);
+    return MOE_OK;
+}
+
+// The load a launch over these experts can expect under uniform routing.
+ScaledLoad expected_load(const moe_dims &d, int e_count) {
+    ScaledLoad l;
+    const double p = (double)d.top_k / d.experts;
+    l.max_rows = d.tokens;
+    l.rows = (double)d.tokens * p * e_count;
+    l.active = e_count * (1.0 - std::pow(1.0 - p, (double)d.tokens));
+    return l;
+}
+
+struct FfnWs {
+    size_t act, act_s, total;
+};
+FfnWs ffn_ws(const moe_dims *d) {
+    FfnWs w;
+    auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
+    const size_t rows = (size_t)row_cap(d);
+    w.act = 0;
+    w.act_s = up(rows * d->inter);
+    w.total = w.act_s + up(rows * scale_pitch(d->inter));
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t moe_scale_pitch(int32_t k) { return width_ok(k) ? (size_t)scale_pitch(k) : 0; }
+
+moe_status moe_quant_rows(int64_t rows, int32_t cols, const void *x, int32_t x_type, moe_e4m3 *q,
+                          moe_scale *scales, void *stream) {
+    const char *fn = "moe_quant_rows";
+    if (rows < 0) return fail(MOE_ERR_INVALID, "%s: rows < 0", fn);
+    if (!width_ok(cols))
+        return fail(MOE_ERR_INVALID, "%s: cols %d not a multiple of %d up to 2^20", fn, cols,
+                    kDimAlign);
+    if (!type_ok(x_type)) return fail(MOE_ERR_INVALID, "%s: x_type %d", fn, x_type);
+    if (rows == 0) return MOE_OK;
+    MOE_TRY(check_tensor(fn, "x", x));
+    MOE_TRY(check_pair(fn, "q", q, scales));
+    MOE_HIP(launch_norm_quant(rows, cols, x, x_type, nullptr, false, nullptr, 0.f, nullptr,
+                              nullptr, q, scales, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_quant_weights(int32_t experts, int32_t n, int32_t k, const moe_bf16 *w,
+                             moe_e4m3 *q, moe_scale *scales, void *stream) {
+    const char *fn = "moe_quant_weights";
+    if (experts < 0) return fail(MOE_ERR_INVALID, "%s: experts < 0", fn);
+    if (experts > kMaxExperts)
+        return fail(MOE_ERR_UNSUPPORTED, "%s: experts %d > %d", fn, experts, kMaxExperts);
+    if (!width_ok(n) || !width_ok(k))
+        return fail(MOE_ERR_INVALID, "%s: widths %d, %d not multiples of %d up to 2^20", fn, n, k,
+                    kDimAlign);
+    if (experts == 0) return MOE_OK;
+    MOE_TRY(check_tensor(fn, "w", w));
+    MOE_TRY(check_pair(fn, "q", q, scales));
+    MOE_HIP(launch_quant_weights(experts, n, k, w, q, scales, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_norm_quant(int64_t rows, int32_t hidden, const void *x, int32_t x_type,
+                          const moe_bf16 *residual, const moe_bf16 *weight, float eps,
+                          moe_bf16 *total, moe_bf16 *y, moe_e4m3 *q, moe_scale *scales,
+                          void *stream) {
+    const char *fn = "moe_norm_quant";
+    if (rows < 0) return fail(MOE_ERR_INVALID, "%s: rows < 0", fn);
+    if (!width_ok(hidden))
+        return fail(MOE_ERR_INVALID, "%s: hidden %d not a multiple of %d up to 2^20", fn, hidden,
+                    kDimAlign);
+    if (!type_ok(x_type)) return fail(MOE_ERR_INVALID, "%s: x_type %d", fn, x_type);
+    if (!(eps >= 0.f) || std::isinf(eps))
+        return fail(MOE_ERR_INVALID, "%s: eps is negative or not finite", fn);
+    if (!y && !q) return fail(MOE_ERR_INVALID, "%s: neither y nor q is given", fn);
+    if ((q == nullptr) != (scales == nullptr))
+        return fail(MOE_ERR_INVALID, "%s: q and scales go together", fn);
+    if (rows == 0) return MOE_OK;
+    MOE_TRY(check_tensor(fn, "x", x));
+    if (residual) MOE_TRY(check_tensor(fn, "residual", residual));
+    if (weight) MOE_TRY(check_tensor(fn, "weight", weight));
+    if (total) MOE_TRY(check_tensor(fn, "total", total));
+    if (y) MOE_TRY(check_tensor(fn, "y", y));
+    if (q) MOE_TRY(check_pair(fn, "q", q, scales));
+    MOE_HIP(launch_norm_quant(rows, hidden, x, x_type, residual, true, weight, eps, total, y, q,
+                              scales, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_gemm_scaled(int64_t rows, int32_t n, int32_t k, const moe_e4m3 *x,
+                           const moe_scale *x_scales, const moe_e4m3 *w,
+                           const moe_scale *w_scales, void *y, int32_t y_type, void *stream) {
+    const char *fn = "moe_gemm_scaled";
+    if (rows < 0) return fail(MOE_ERR_INVALID, "%s: rows < 0", fn);
+    MOE_TRY(check_product(fn, rows, 1, n, k));
+    if (!type_ok(y_type)) return fail(MOE_ERR_INVALID, "%s: y_type %d", fn, y_type);
+    if (rows == 0) return MOE_OK;
+    MOE_TRY(check_pair(fn, "x", x, x_scales));
+    MOE_TRY(check_pair(fn, "w", w, w_scales));
+    MOE_TRY(check_tensor(fn, "y", y));
+    ScaledGemm g{};
+    g.e_count = 1;
+    g.rows_one = rows;
+    g.x = x, g.xs = x_scales;
+    g.slot_div = 1;
+    g.w0 = w, g.s0 = w_scales;
+    g.N = n, g.K = k;
+    g.out = y;
+    MOE_HIP(launch_scaled_gemm(g, y_type, ScaledLoad{rows, (double)rows, 1.0},
+                               (hipStream_t)stream));
+    return MOE_OK;
+}
+
+moe_status moe_gemm_group_scaled(const moe_dims *dims, int32_t e_first, int32_t e_count,
+                                 const int32_t *offsets, const int32_t *sorted_slot, int32_t n,
+                                 int32_t k, const moe_e4m3 *x, const moe_scale *x_scales,
+                                 const moe_e4m3 *w, const moe_scale *w_scales, void *y,
+                                 int32_t y_type, void *stream) {
+    const char *fn = "moe_gemm_group_scaled";
+    MOE_TRY(check_dims(dims));
+    MOE_TRY(check_product(fn, row_cap(dims), dims->local_count, n, k));
+    if (!type_ok(y_type)) return fail(MOE_ERR_INVALID, "%s: y_type %d", fn, y_type);
+    MOE_TRY(check_group(fn, dims, e_first, e_count, offsets, sorted_slot, k));
+    if (dims->tokens == 0 || e_count == 0) return MOE_OK;
+    MOE_TRY(check_pair(fn, "x", x, x_scales));
+    MOE_TRY(check_pair(fn, "w", w, w_scales));
+    MOE_TRY(check_tensor(fn, "y", y));
+    ScaledGemm g{};
+    g.offsets = offsets;
+    g.e_first = e_first, g.e_count = e_count;
+    g.x = x, g.xs = x_scales;
+    g.row_map = sorted_slot;
+    g.slot_div = dims->top_k;
+    g.w0 = w, g.s0 = w_scales;
+    g.N = n, g.K = k;
+    g.out = y;
+    MOE_HIP(launch_scaled_gemm(g, y_type, expected_load(*dims, e_count), (hipStream_t)stream));
+    return MOE_OK;
+}
+
+size_t moe_scaled_workspace_bytes(const moe_dims *dims) {
+    if (check_dims(dims) != MOE_OK) return 0;
+    return std::max<size_t>(ffn_ws(dims).total, 256);
+}
+
+moe_status moe_ffn_group_scaled(const moe_dims *dims, int32_t e_first, int32_t e_count,
+                                const int32_t *offsets, const int32_t *sorted_slot,
+                                const moe_e4m3 *x, const moe_scale *x_scales,
+                                const moe_e4m3 *w_gate, const moe_scale *gate_scales,
+                                const moe_e4m3 *w_up, const moe_scale *up_scales,
+                                const moe_e4m3 *w_down, const moe_scale *down_scales,
+                                void *y_perm, int32_t y_type, void *ws, size_t ws_bytes,
+                                void *stream) {
+    const char *fn = "moe_ffn_group_scaled";
+    MOE_TRY(check_dims(dims));
+    MOE_TRY(check_product(fn, row_cap(dims), dims->local_count,
+                          std::max(dims->hidden, dims->inter), kDimAlign));
+    if (!type_ok(y_type)) return fail(MOE_ERR_INVALID, "%s: y_type %d", fn, y_type);
+    MOE_TRY(check_group(fn, dims, e_first, e_count, offsets, sorted_slot, dims->hidden));
+    if (dims->tokens == 0 || e_count == 0) return MOE_OK;
+    MOE_TRY(check_pair(fn, "x", x, x_scales));
+    MOE_TRY(check_pair(fn, "w_gate", w_gate, gate_scales));
+    MOE_TRY(check_pair(fn, "w_up", w_up, up_scales));
+    MOE_TRY(check_pair(fn, "w_down", w_down, down_scales));
+    MOE_TRY(check_tensor(fn, "y_perm", y_perm));
+    const FfnWs L = ffn_ws(dims);
+    if (!ws || ws_bytes < L.total)
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, L.total);
+    MOE_TRY(check_tensor(fn, "ws", ws));
+    uint8_t *base = (uint8_t *)ws;
+    const ScaledLoad load = expected_load(*dims, e_count);
+    hipStream_t s = (hipStream_t)stream;
+    ScaledGemm g{};
+    g.offsets = offsets;
+    g.e_first = e_first, g.e_count = e_count;
+    g.x = x, g.xs = x_scales;
+    g.row_map = sorted_slot;
+    g.slot_div = dims->top_k;
+    g.w0 = w_gate, g.s0 = gate_scales;
+    g.w1 = w_up, g.s1 = up_scales;
+    g.N = dims->inter, g.K = dims->hidden;
+    g.out = base + L.act, g.out_s = base + L.act_s;
+    MOE_HIP(launch_scaled_swiglu(g, load, s));
+    ScaledGemm h{};
+    h.offsets = offsets;
+    h.e_first = e_first, h.e_count = e_count;
+    h.x = base + L.act, h.xs = base + L.act_s;
+    h.slot_div = 1;
+    h.w0 = w_down, h.s0 = down_scales;
+    h.N = dims->hidden, h.K = dims->inter;
+    h.out = y_perm;
+    MOE_HIP(launch_scaled_gemm(h, y_type, load, s));
+    return MOE_OK;
+}
+
+}  // extern "C"

@@ -16,6 +16,7 @@ import torch
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmoe.so")
 
+BF16, FP32 = 0, 1
 GEMM_AUTO, GEMM_GROUP, GEMM_DENSE = 0, 1, 2
 CHUNK_EXPERTS, CHUNK_TOKENS = 0, 1
 FLAG_TIMING, FLAG_TIMING_GEMM, FLAG_EXACT_ORDER, FLAG_SERIAL = 1, 2, 4, 8
@@ -25,7 +26,9 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_guards", "moe_route", "moe_perm
            "moe_ffn_dense", "moe_combine", "moe_ffn_forward", "moe_ffn_forward_noalloc",
            "moe_last_timing",
            "moe_gemm_plan", "moe_pipeline_plan", "moe_choose_pipeline_n", "moe_status_string",
-           "moe_last_error")
+           "moe_last_error", "moe_scale_pitch", "moe_quant_rows", "moe_quant_weights",
+           "moe_norm_quant", "moe_gemm_scaled", "moe_gemm_group_scaled",
+           "moe_scaled_workspace_bytes", "moe_ffn_group_scaled")
 
 
 class MoEError(RuntimeError):
@@ -101,12 +104,24 @@ def lib():
                                 ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
     L.moe_choose_pipeline_n.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, I32,
                                         ctypes.POINTER(I32), ctypes.POINTER(ctypes.c_double)]
+    L.moe_scale_pitch.argtypes = [I32]
+    L.moe_scale_pitch.restype = SZ
+    L.moe_quant_rows.argtypes = [I64, I32, P, I32, P, P, P]
+    L.moe_quant_weights.argtypes = [I32, I32, I32, P, P, P, P]
+    L.moe_norm_quant.argtypes = [I64, I32, P, I32, P, P, ctypes.c_float, P, P, P, P, P]
+    L.moe_gemm_scaled.argtypes = [I64, I32, I32, P, P, P, P, P, I32, P]
+    L.moe_gemm_group_scaled.argtypes = [D, I32, I32, P, P, I32, I32, P, P, P, P, P, I32, P]
+    L.moe_scaled_workspace_bytes.argtypes = [D]
+    L.moe_scaled_workspace_bytes.restype = SZ
+    L.moe_ffn_group_scaled.argtypes = [D, I32, I32] + [P] * 11 + [I32, P, SZ, P]
     L.moe_status_string.argtypes = [I32]
     L.moe_status_string.restype = ctypes.c_char_p
     L.moe_last_error.restype = ctypes.c_char_p
     for name in ("moe_route", "moe_permute", "moe_gather", "moe_ffn_group", "moe_ffn_dense",
                  "moe_combine", "moe_ffn_forward", "moe_ffn_forward_noalloc", "moe_last_timing",
-                 "moe_choose_pipeline_n", "moe_gemm_plan", "moe_pipeline_plan"):
+                 "moe_choose_pipeline_n", "moe_gemm_plan", "moe_pipeline_plan", "moe_quant_rows",
+                 "moe_quant_weights", "moe_norm_quant", "moe_gemm_scaled",
+                 "moe_gemm_group_scaled", "moe_ffn_group_scaled"):
         getattr(L, name).restype = I32
     _lib = L
     return L
@@ -272,6 +287,152 @@ def gemm_plan(d: Dims, o: Optional[Opts], rows):
                                tiles.ctypes.data_as(ctypes.c_void_p), ctypes.byref(gus),
                                ctypes.byref(dus)))
     return bool(dense.value), tiles.tolist(), gus.value, dus.value
+
+
+# ---- block-scaled 8-bit operators -----------------------------------------
+# Quantised values are float8_e4m3fn tensors (or their uint8 bits), scales
+# uint8 (or float8_e8m0fnu).
+
+_E4M3 = (torch.float8_e4m3fn, torch.uint8)
+_SCALE = (torch.uint8, torch.float8_e8m0fnu)
+_REAL = {torch.bfloat16: BF16, torch.float32: FP32}
+_I32 = (torch.int32,)
+_BF16 = (torch.bfloat16,)
+
+
+def _real(name, t):
+    """The element type's code."""
+    if t.dtype not in _REAL:
+        raise ValueError(f"{name} must be bfloat16 or float32, not {t.dtype}")
+    return _REAL[t.dtype]
+
+
+def _arg(name, t, dtypes, shape):
+    """The address of a contiguous tensor of the current device with one of
+    the dtypes and the shape, or None for None."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor of shape {tuple(shape)} and "
+                         f"type {dtypes[0]}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    return t.data_ptr()
+
+
+def _rows(name, t, cols=None):
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name} must be 2-dimensional" +
+                         (f" with {cols} columns" if cols is not None else ""))
+    return t.shape
+
+
+def scale_pitch(k: int) -> int:
+    """Bytes of a scale row of a width k."""
+    n = lib().moe_scale_pitch(k)
+    if n == 0:
+        raise ValueError(f"width {k} is not a positive multiple of 64 up to 2^20")
+    return n
+
+
+def _pitch(k):
+    return 4 * -(-k // 512)
+
+
+def quant_rows(x, q, scales, stream=None):
+    """q, scales = Q(x): one scale per row and 128 columns."""
+    R, C = _rows("x", x)
+    _check(lib().moe_quant_rows(R, C, _arg("x", x, (x.dtype,), x.shape), _real("x", x),
+                                _arg("q", q, _E4M3, x.shape),
+                                _arg("scales", scales, _SCALE, (R, _pitch(C))), _s(stream)))
+
+
+def quant_weights(w, q, scales, stream=None):
+    """q, scales = Q(w) in 128 x 128 blocks; w [n, k] or [experts, n, k] bf16."""
+    if w.dim() not in (2, 3):
+        raise ValueError("w must be [n, k] or [experts, n, k]")
+    lead, (n, k) = w.shape[:-2], w.shape[-2:]
+    _check(lib().moe_quant_weights(lead[0] if lead else 1, n, k, _arg("w", w, _BF16, w.shape),
+                                   _arg("q", q, _E4M3, w.shape),
+                                   _arg("scales", scales, _SCALE,
+                                        lead + (-(-n // 128), _pitch(k))), _s(stream)))
+
+
+def norm_quant(x, residual, weight, eps, total, y, q, scales, stream=None):
+    """total = bf16(x + residual), y = bf16(v) and q, scales = Q(v) for the
+    RMS-normalised rows v = norm(x + residual) * weight.  residual, weight,
+    total, y and the pair q, scales may be None."""
+    shape = _rows("x", x)
+    R, H = shape
+    _check(lib().moe_norm_quant(R, H, _arg("x", x, (x.dtype,), shape), _real("x", x),
+                                _arg("residual", residual, _BF16, shape),
+                                _arg("weight", weight, _BF16, (H,)), eps,
+                                _arg("total", total, _BF16, shape), _arg("y", y, _BF16, shape),
+                                _arg("q", q, _E4M3, shape),
+                                _arg("scales", scales, _SCALE, (R, _pitch(H))), _s(stream)))
+
+
+def gemm_scaled(x, x_scales, w, w_scales, y, stream=None):
+    """y = x w^T over block-scaled x [rows, k] and w [n, k]; y bf16 or fp32."""
+    R, K = _rows("x", x)
+    N, _ = _rows("w", w, K)
+    _check(lib().moe_gemm_scaled(R, N, K, _arg("x", x, _E4M3, (R, K)),
+                                 _arg("x_scales", x_scales, _SCALE, (R, _pitch(K))),
+                                 _arg("w", w, _E4M3, (N, K)),
+                                 _arg("w_scales", w_scales, _SCALE, (-(-N // 128), _pitch(K))),
+                                 _arg("y", y, (y.dtype,), (R, N)), _real("y", y), _s(stream)))
+
+
+def _row_cap(d):
+    return d.tokens * min(d.top_k, d.local_count)
+
+
+def _group_args(d, offsets, sorted_slot, x, x_scales, k):
+    """Addresses of what the grouped calls share; x holds the tokens' rows
+    with sorted_slot, else the dispatched rows."""
+    cap = _row_cap(d)
+    rows = d.tokens if sorted_slot is not None else cap
+    return (_arg("offsets", offsets, _I32, (d.local_count + 1,)),
+            _arg("sorted_slot", sorted_slot, _I32, (cap,)), _arg("x", x, _E4M3, (rows, k)),
+            _arg("x_scales", x_scales, _SCALE, (rows, _pitch(k))))
+
+
+def _stack(name, d, w, s, n, k):
+    return (_arg(name, w, _E4M3, (d.local_count, n, k)),
+            _arg(name + " scales", s, _SCALE, (d.local_count, -(-n // 128), _pitch(k))))
+
+
+def gemm_group_scaled(d, e_first, e_count, offsets, sorted_slot, x, x_scales, w, w_scales, y,
+                      stream=None):
+    """gemm_scaled per local expert over the rows offsets gives each; with
+    sorted_slot the rows are gathered from the tokens' x."""
+    if w.dim() != 3:
+        raise ValueError("w must be [local_count, n, k]")
+    N, K = w.shape[1:]
+    off, slot, xp, xsp = _group_args(d, offsets, sorted_slot, x, x_scales, K)
+    wp, wsp = _stack("w", d, w, w_scales, N, K)
+    _check(lib().moe_gemm_group_scaled(ctypes.byref(d), e_first, e_count, off, slot, N, K, xp,
+                                       xsp, wp, wsp, _arg("y", y, (y.dtype,), (_row_cap(d), N)),
+                                       _real("y", y), _s(stream)))
+
+
+def scaled_workspace_bytes(d: Dims) -> int:
+    return lib().moe_scaled_workspace_bytes(ctypes.byref(d))
+
+
+def ffn_group_scaled(d, e_first, e_count, offsets, sorted_slot, x, x_scales, w_gate, gate_scales,
+                     w_up, up_scales, w_down, down_scales, y_perm, ws, stream=None):
+    """The experts' SwiGLU FFN in 8 bits; y_perm bf16 or fp32, ws of
+    scaled_workspace_bytes(d) bytes."""
+    H, I = d.hidden, d.inter
+    off, slot, xp, xsp = _group_args(d, offsets, sorted_slot, x, x_scales, H)
+    _check(lib().moe_ffn_group_scaled(
+        ctypes.byref(d), e_first, e_count, off, slot, xp, xsp,
+        *_stack("w_gate", d, w_gate, gate_scales, I, H),
+        *_stack("w_up", d, w_up, up_scales, I, H),
+        *_stack("w_down", d, w_down, down_scales, H, I),
+        _arg("y_perm", y_perm, (y_perm.dtype,), (_row_cap(d), H)), _real("y_perm", y_perm),
+        _arg("ws", ws, (ws.dtype,), ws.shape), ws.numel() * ws.element_size(), _s(stream)))
 
 
 class MoEBuffers:

@@ -1,0 +1,574 @@
+"""The block-scaled 8-bit operators through the Python binding: quantised rows
+and weights, the RMS norm in front of them, dense and grouped products and the
+experts' FFN against plain 64-bit implementations, and what the calls refuse."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import scaled_ref as ref
+from paper_2410_12247_amd import moe
+
+gpu = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def cuda(t):
+    return t.cuda()
+
+
+def same_stream_order():
+    torch.cuda.synchronize()
+
+
+# ---- refusals: host only --------------------------------------------------
+
+FAKE = ctypes.c_void_p(4096)  # never dereferenced
+ODD = ctypes.c_void_p(4096 + 2)
+
+
+def last():
+    return moe.lib().moe_last_error().decode()
+
+
+def test_scale_pitch():
+    L = moe.lib()
+    for k, n in ((64, 4), (128, 4), (512, 4), (576, 8), (1344, 12), (1 << 20, 8192)):
+        assert L.moe_scale_pitch(k) == n == ref.pitch(k) == moe.scale_pitch(k)
+    for k in (0, -64, 100, (1 << 20) + 64):
+        assert L.moe_scale_pitch(k) == 0
+        with pytest.raises(ValueError):
+            moe.scale_pitch(k)
+
+
+def test_quant_refusals():
+    L = moe.lib()
+    ok = dict(rows=4, cols=128, x=FAKE, t=0, q=FAKE, s=FAKE)
+
+    def call(**k):
+        a = {**ok, **k}
+        return L.moe_quant_rows(a["rows"], a["cols"], a["x"], a["t"], a["q"], a["s"], None)
+    for bad in (dict(rows=-1), dict(cols=0), dict(cols=100), dict(cols=(1 << 20) + 64), dict(t=2),
+                dict(t=-1), dict(x=None), dict(q=None), dict(s=None), dict(x=ODD), dict(q=ODD),
+                dict(s=ODD)):
+        assert call(**bad) == 1, (bad, last())
+        assert "moe_quant_rows" in last()
+    assert call(rows=0, x=None, q=None, s=None) == 0
+    assert L.moe_quant_weights(-1, 64, 64, FAKE, FAKE, FAKE, None) == 1
+    assert L.moe_quant_weights(257, 64, 64, FAKE, FAKE, FAKE, None) == 2
+    assert L.moe_quant_weights(1, 32, 64, FAKE, FAKE, FAKE, None) == 1
+    assert L.moe_quant_weights(1, 64, 65, FAKE, FAKE, FAKE, None) == 1
+    assert L.moe_quant_weights(1, 64, 64, None, FAKE, FAKE, None) == 1
+    assert L.moe_quant_weights(1, 64, 64, FAKE, FAKE, ODD, None) == 1
+    assert L.moe_quant_weights(0, 64, 64, None, None, None, None) == 0
+
+
+def test_norm_refusals():
+    L = moe.lib()
+    ok = dict(rows=4, h=128, x=FAKE, t=1, r=FAKE, w=FAKE, eps=1e-6, tot=FAKE, y=FAKE, q=FAKE,
+              s=FAKE)
+
+    def call(**k):
+        a = {**ok, **k}
+        return L.moe_norm_quant(a["rows"], a["h"], a["x"], a["t"], a["r"], a["w"], a["eps"],
+                                a["tot"], a["y"], a["q"], a["s"], None)
+    for bad in (dict(rows=-1), dict(h=96), dict(t=3), dict(eps=-1e-6), dict(eps=float("nan")),
+                dict(eps=float("inf")), dict(x=None), dict(y=None, q=None, s=None),
+                dict(q=None), dict(s=None), dict(x=ODD), dict(r=ODD), dict(w=ODD), dict(tot=ODD),
+                dict(y=ODD), dict(q=ODD), dict(s=ODD)):
+        assert call(**bad) == 1, (bad, last())
+    assert call(rows=0, x=None) == 0
+
+
+def test_product_refusals():
+    L = moe.lib()
+
+    def gemm(rows=4, n=64, k=64, x=FAKE, xs=FAKE, w=FAKE, ws=FAKE, y=FAKE, t=0):
+        return L.moe_gemm_scaled(rows, n, k, x, xs, w, ws, y, t, None)
+    for bad in (dict(rows=-1), dict(n=0), dict(n=100), dict(k=32), dict(k=(1 << 20) + 64),
+                dict(t=2), dict(x=None), dict(xs=None), dict(w=None), dict(ws=None), dict(y=None),
+                dict(x=ODD), dict(xs=ODD), dict(w=ODD), dict(ws=ODD), dict(y=ODD)):
+        assert gemm(**bad) == 1, (bad, last())
+    assert gemm(rows=1 << 31) == 2
+    assert gemm(rows=(1 << 31) - 1, n=1 << 20) == 2
+    assert gemm(rows=0, x=None) == 0
+    d = moe.dims(64, 256, 128, 8, 2)
+
+    def group(d=d, e0=0, ec=8, off=FAKE, slot=FAKE, n=64, k=64, x=FAKE, y=FAKE, t=0):
+        return L.moe_gemm_group_scaled(ctypes.byref(d), e0, ec, off, slot, n, k, x, FAKE, FAKE,
+                                       FAKE, y, t, None)
+    for bad in (dict(e0=-1), dict(ec=9), dict(e0=8, ec=1), dict(e0=2 ** 31 - 1), dict(ec=-1),
+                dict(off=None), dict(n=65), dict(k=0), dict(t=9), dict(x=None), dict(y=ODD)):
+        assert group(**bad) == 1, (bad, last())
+    assert group(ec=0, off=None) == 0
+    assert group(d=moe.dims(0, 256, 128, 8, 2), x=None) == 0
+    # a gathered token matrix of 4 GiB: refused; the same rows in order are not
+    big = moe.dims(1 << 16, 64, 64, 8, 2)
+    assert group(d=big, k=1 << 16) == 2 and "4 GiB" in last()
+    assert group(d=big, k=1 << 16, slot=None, y=None) == 1
+
+
+def test_ffn_refusals():
+    L = moe.lib()
+    d = moe.dims(64, 256, 128, 8, 2)
+    need = moe.scaled_workspace_bytes(d)
+    assert need >= 64 * 2 * (128 + 4)
+    assert moe.scaled_workspace_bytes(moe.dims(64, 100, 128, 8, 2)) == 0
+
+    def ffn(d=d, e0=0, ec=8, off=FAKE, slot=None, x=FAKE, wg=FAKE, gs=FAKE, y=FAKE, t=1, ws=FAKE,
+            n=need):
+        return L.moe_ffn_group_scaled(ctypes.byref(d), e0, ec, off, slot, x, FAKE, wg, gs, FAKE,
+                                      FAKE, FAKE, FAKE, y, t, ws, n, None)
+    for bad in (dict(e0=-1), dict(ec=9), dict(off=None), dict(x=None), dict(wg=None),
+                dict(gs=ODD), dict(y=None), dict(t=2), dict(ws=ODD)):
+        assert ffn(**bad) == 1, (bad, last())
+    assert ffn(n=need - 1) == 3 and ffn(ws=None) == 3
+    assert ffn(d=moe.dims(64, 100, 128, 8, 2)) == 1
+    assert ffn(d=moe.dims(0, 256, 128, 8, 2), x=None) == 0
+
+
+def test_binding_refuses_what_it_cannot_pass():
+    cpu = torch.zeros((4, 128), dtype=BF16)
+    with pytest.raises(ValueError, match="contiguous device tensor"):
+        moe.quant_rows(cpu, cpu, cpu)
+    with pytest.raises(ValueError):
+        moe.quant_rows(cpu.half(), cpu, cpu)
+    with pytest.raises(ValueError):
+        moe.quant_rows(cpu[0], cpu, cpu)
+
+
+# ---- quantising -----------------------------------------------------------
+
+WIDTHS = [64, 128, 192, 512, 576, 2048, 2112, 4160, 8192, 8256]
+
+
+def rows_of(g, R, C, dtype):
+    x = torch.randn((R, C), generator=g) * torch.exp(2 * torch.randn((R, 1), generator=g))
+    x[:, ::17] *= 30
+    if R > 2:
+        x[1] = 0  # blocks of zeros
+        x[2, :64] = 0
+    return x.to(dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C", WIDTHS)
+def test_quant_rows_has_the_oracles_bits(C, dtype):
+    for R in (1, 5, 67):
+        x = rows_of(gen(C + R), R, C, dtype)
+        q = torch.full((R + 1, C), 0x5A, dtype=torch.uint8, device="cuda")
+        s = torch.full((R + 1, ref.pitch(C)), 0x5A, dtype=torch.uint8, device="cuda")
+        moe.quant_rows(cuda(x), q[:R], s[:R])
+        torch.cuda.synchronize()
+        want, e = ref.quant(x.double(), 1)
+        assert torch.equal(ref.decode(q[:R]), want)
+        assert torch.equal(s[:R, :ref.blocks(C)].cpu().int() - 127, e.int())
+        # nothing behind the rows or the scales
+        assert bool((q[R] == 0x5A).all()) and bool((s[R] == 0x5A).all())
+        assert bool((s[:R, ref.blocks(C):] == 0x5A).all())
+
+
+@gpu
+def test_quant_rows_borders_and_values_that_are_no_numbers():
+    x = torch.zeros((12, 256))
+    x[0, 3] = 448.0
+    x[1, 3] = float(np.nextafter(np.float32(448), np.float32(1e9)))  # one step above: the next power
+    x[2, 200] = 2.0 ** -149  # the smallest fp32
+    x[3, 5] = 3.4e38
+    x[4, 7] = 2.0 ** -130
+    x[5, :128] = torch.linspace(-17, 17, 128)  # halves between e4m3 values
+    x[6, 1] = -448.0 * 2.0 ** 20
+    x[7, :128] = float("nan")
+    x[8, 1], x[8, 2] = float("inf"), 5.0
+    x[9, 1], x[9, 2] = -float("inf"), float("nan")
+    x[10, 130], x[10, 131] = float("nan"), 3.0
+    q = torch.empty((12, 256), dtype=torch.float8_e4m3fn, device="cuda")
+    s = torch.empty((12, 4), dtype=torch.uint8, device="cuda")
+    moe.quant_rows(cuda(x), q, s)
+    v, e = ref.decode(q), s.cpu().int() - 127
+    want, we = ref.quant(x[:7].double(), 1)
+    assert torch.equal(v[:7], want) and torch.equal(e[:7, :2], we.int())
+    assert e[0, 0] == 0 and e[1, 0] == 1 and e[2, 1] == -127 and e[3, 0] == 120
+    assert bool(v[7, :128].isnan().all()) and bool((v[7, 128:] == 0).all()) and e[7, 0] == 0
+    assert bool(v[8, 1].isnan()) and v[8, 2] == 0 and e[8, 0] == 120
+    assert bool(v[9, 1].isnan()) and bool(v[9, 2].isnan())
+    assert bool(v[10, 130].isnan()) and v[10, 131] == 384 and e[10, 1] == -7
+    assert bool((v[10, :128] == 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("E,n,k", [(1, 64, 64), (3, 192, 320), (2, 128, 1344), (1, 704, 128)])
+def test_quant_weights_has_the_oracles_bits(E, n, k):
+    w = (torch.randn((E, n, k), generator=gen(n + k)) * 0.02).to(BF16)
+    w[0, :64, :64] = 0
+    q = torch.empty((E, n, k), dtype=torch.float8_e4m3fn, device="cuda")
+    s = torch.full((E, ref.blocks(n), ref.pitch(k)), 0x5A, dtype=torch.uint8, device="cuda")
+    moe.quant_weights(cuda(w), q, s)
+    for i in range(E):
+        want, e = ref.quant(w[i].double(), 128)
+        assert torch.equal(ref.decode(q[i]), want)
+        assert torch.equal(s[i, :, :ref.blocks(k)].cpu().int() - 127, e.int())
+    assert bool((s[..., ref.blocks(k):] == 0x5A).all())
+    if E == 1:  # one matrix without the leading dimension
+        q2, s2 = torch.empty_like(q[0]), torch.full_like(s[0], 0x5A)
+        moe.quant_weights(cuda(w[0]), q2, s2)
+        assert torch.equal(q2.view(torch.uint8), q[0].view(torch.uint8)) and torch.equal(s2, s[0])
+
+
+def check_norm(x, res, w, eps, total, y, q, s):
+    R, C = x.shape
+    v = x.double() + (res.double() if res is not None else 0)
+    if total is not None:  # the fp32 sum, then bf16
+        off = (total.cpu().double() - v).abs()
+        assert bool((off <= (2.0 ** -8 + 2.0 ** -23) * v.abs() + 2.0 ** -134).all())
+    n = v * torch.rsqrt((v * v).mean(1, keepdim=True) + eps) * (w.double() if w is not None else 1)
+    # fp32: s, the squares' sum (a chain of at most 8 terms a pass and lane,
+    # then the tree), its root, three roundings of the products
+    chain = 8 * max(4, -(-C // 8192)) + 26
+    rel = (chain / 2 + 8) * 2.0 ** -24
+    if y is not None:
+        off = (y.cpu().double() - n).abs()
+        bad = off > (2.0 ** -8 + 2 * rel) * n.abs() + 2.0 ** -134
+        assert not bool(bad.any())
+    if q is None:
+        return
+    got_e = s[:, :ref.blocks(C)].cpu().int() - 127
+    top = ref.tiles(n.abs(), 1).amax((1, 3))
+    lo, hi = ref.exponent(top * (1 - rel)).int(), ref.exponent(top * (1 + rel)).int()
+    assert bool(((got_e == lo) | (got_e == hi)).all())
+    f = torch.ldexp(torch.ones((), dtype=torch.float64), got_e).repeat_interleave(128, 1)[:, :C]
+    got = ref.decode(q) * f
+    # half a step of e4m3 (2^-4 of the value, 2^-10 below the smallest normal)
+    assert bool(((got - n).abs() <= torch.maximum(2.0 ** -4 * n.abs(), 2.0 ** -10 * f)
+                 + 2 * rel * n.abs()).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C", WIDTHS)
+def test_norm_quant(C, dtype):
+    for R in (1, 6, 33):
+        g = gen(7 * C + R)
+        x, res = rows_of(g, R, C, dtype), torch.randn((R, C), generator=g).to(BF16)
+        w = (1 + 0.3 * torch.randn(C, generator=g)).to(BF16)
+        q = torch.empty((R, C), dtype=torch.uint8, device="cuda")
+        s = torch.empty((R, ref.pitch(C)), dtype=torch.uint8, device="cuda")
+        y, total = torch.empty((R, C), dtype=BF16, device="cuda"), cuda(res).clone()
+        xd = cuda(x)
+        moe.norm_quant(xd, total, cuda(w), 1e-5, total, y, q, s)  # total over the residual
+        check_norm(x, res, w, 1e-5, total, y, q, s)
+        # parts of the outputs, and without weight and residual
+        y2 = torch.empty_like(y)
+        moe.norm_quant(xd, None, None, 0.5, None, y2, None, None)
+        check_norm(x, None, None, 0.5, None, y2, None, None)
+        q2, s2 = torch.empty_like(q), torch.empty_like(s)
+        moe.norm_quant(xd, cuda(res), cuda(w), 1e-5, None, None, q2, s2)
+        assert torch.equal(q2, q)
+        assert torch.equal(s2[:, :ref.blocks(C)], s[:, :ref.blocks(C)])
+        if dtype == BF16:  # y over x
+            moe.norm_quant(xd, None, None, 0.5, None, xd, None, None)
+            assert torch.equal(xd, y2)
+
+
+@gpu
+def test_norm_rows_that_are_zero_or_no_numbers():
+    x = torch.zeros((4, 320), dtype=F32)
+    x[1, 5] = float("nan")
+    x[2, 5] = float("inf")
+    x[3] = 1.0
+    y = torch.empty((4, 320), dtype=BF16, device="cuda")
+    q = torch.empty((4, 320), dtype=torch.uint8, device="cuda")
+    s = torch.empty((4, 4), dtype=torch.uint8, device="cuda")
+    moe.norm_quant(cuda(x), None, None, 1e-6, None, y, q, s)
+    y, v = y.cpu(), ref.decode(q)
+    assert bool((y[0] == 0).all()) and bool((v[0] == 0).all())
+    assert bool(y[1].isnan().all()) and bool(v[1].isnan().all())
+    assert bool(y[2, 5].isnan()) and bool((y[2, :5] == 0).all())
+    assert bool((y[3] == 1).all())
+
+
+# ---- products -------------------------------------------------------------
+
+def product(x, w, dtype):
+    """(result, bound) in fp64."""
+    y = x @ w.T
+    b = ref.group_bound(x, w)
+    return y, b + HALF(dtype) * (y.abs() + b) + 2.0 ** -134
+
+
+def HALF(dtype):
+    return ref.HALF[dtype]
+
+
+def run_gemm(xq, xs, wq, ws, dtype):
+    R, N = xq.shape[0], wq.shape[0]
+    y = torch.full((R + 2, N), 77.0, dtype=dtype, device="cuda")
+    moe.gemm_scaled(cuda(xq), cuda(xs), cuda(wq), cuda(ws), y[:R])
+    torch.cuda.synchronize()
+    assert bool((y[R:] == 77).all())
+    return y[:R].cpu()
+
+
+GEMMS = [(1, 64, 64), (1, 256, 128), (2, 320, 192), (7, 128, 576), (16, 192, 1344), (17, 64, 320),
+         (31, 448, 704), (33, 256, 1024), (65, 320, 128), (100, 1344, 640), (129, 576, 448),
+         (255, 256, 256), (300, 704, 1088)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("R,N,K", GEMMS)
+def test_gemm_of_small_integers_is_exact(R, N, K, dtype):
+    g = gen(R + N + K)
+    xq, wq = ref.small_integers(g, R, K), ref.small_integers(g, N, K)
+    xs, ws = ref.scale_bytes(g, R, K), ref.scale_bytes(g, ref.blocks(N), K)
+    want = ref.widen(xq, xs, 1) @ ref.widen(wq, ws, 128).T
+    got = run_gemm(xq, xs, wq, ws, dtype)
+    assert torch.equal(got, want.to(F32).to(dtype))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("R,N,K", GEMMS[1::2])
+def test_gemm_of_any_values(R, N, K, dtype):
+    g = gen(2 * R + N + K)
+    xq, wq = ref.e4m3_random(g, R, K), ref.e4m3_random(g, N, K)
+    xs, ws = ref.scale_bytes(g, R, K, -20, 10), ref.scale_bytes(g, ref.blocks(N), K, -20, 10)
+    want, bound = product(ref.widen(xq, xs, 1), ref.widen(wq, ws, 128), dtype)
+    got = run_gemm(xq, xs, wq, ws, dtype).double()
+    assert bool(((got - want).abs() <= bound).all())
+
+
+@gpu
+@pytest.mark.parametrize("R", [3, 90, 400])
+def test_gemm_keeps_a_nan_in_its_row_and_column(R):
+    g = gen(R)
+    N, K = 192, 320
+    xq, wq = ref.small_integers(g, R, K), ref.small_integers(g, N, K)
+    xs, ws = ref.scale_bytes(g, R, K), ref.scale_bytes(g, ref.blocks(N), K)
+    clean = ref.widen(xq, xs, 1) @ ref.widen(wq, ws, 128).T
+    xq[R - 1, 5] = 0x7F
+    wq[N - 1, K - 1] = 0xFF
+    got = run_gemm(xq, xs, wq, ws, F32).double()
+    assert bool(got[R - 1].isnan().all()) and bool(got[:, N - 1].isnan().all())
+    assert torch.equal(got[:R - 1, :N - 1], clean[:R - 1, :N - 1])
+
+
+def dispatch(g, T, E, k, e0, EL, weights=None):
+    """Distinct experts per token; (offsets, sorted_slot) as moe.permute."""
+    p = torch.rand((T, E), generator=g) if weights is None else \
+        torch.rand((T, E), generator=g) ** (1 / torch.as_tensor(weights).clamp(min=1e-9))
+    ids = p.topk(k, 1).indices
+    slots = [[t * k + j for t in range(T) for j in range(k) if ids[t, j] == e0 + e]
+             for e in range(EL)]
+    off = torch.tensor([0] + [len(s) for s in slots]).cumsum(0).int()
+    flat = torch.tensor([v for s in slots for v in s], dtype=torch.int32)
+    cap = T * min(k, EL)
+    slot = torch.full((cap,), -(1 << 30), dtype=torch.int32)  # never read behind the rows
+    slot[:len(flat)] = flat
+    return off, slot, cap
+
+
+GROUPS = [
+    # T, E, k, e0, EL, N, K, popularity
+    (1, 8, 2, 0, 8, 128, 256, None),
+    (5, 8, 2, 2, 4, 192, 576, None),
+    (40, 4, 1, 0, 4, 320, 128, [1, 0, 0, 0]),  # one expert has every row
+    (64, 16, 4, 0, 16, 448, 320, None),
+    (150, 8, 2, 6, 2, 256, 704, None),
+    (333, 6, 3, 0, 6, 576, 192, [8, 1, 0.2, 4, 0, 1]),
+    (700, 2, 2, 0, 2, 128, 128, None),
+]
+
+
+@gpu
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("case", GROUPS, ids=str)
+def test_group_gemm_of_small_integers_is_exact(case, gather):
+    T, E, k, e0, EL, N, K, pop = case
+    g = gen(T + N + K)
+    off, slot, cap = dispatch(g, T, E, k, e0, EL, pop)
+    d = moe.dims(T, 64, 64, E, k, e0, EL)
+    n = T if gather else cap
+    xq, xs = ref.small_integers(g, n, K), ref.scale_bytes(g, n, K)
+    wq = ref.small_integers(g, EL, N, K)
+    ws = torch.stack([ref.scale_bytes(g, ref.blocks(N), K) for _ in range(EL)])
+    x = ref.widen(xq, xs, 1)
+    dev = [cuda(t) for t in (off, slot, xq, xs, wq, ws)]
+    for first, count in ((0, EL), (EL // 2, EL - EL // 2), (0, max(1, EL // 3))):
+        for dtype in (F32, BF16):
+            y = torch.full((cap, N), 55.0, dtype=dtype, device="cuda")
+            moe.gemm_group_scaled(d, first, count, dev[0], dev[1] if gather else None, dev[2],
+                                  dev[3], dev[4], dev[5], y)
+            want = torch.full((cap, N), 55.0, dtype=torch.float64)
+            for e in range(first, first + count):
+                lo, hi = int(off[e]), int(off[e + 1])
+                rows = (slot[lo:hi] // k).long() if gather else slice(lo, hi)
+                want[lo:hi] = x[rows] @ ref.widen(wq[e], ws[e], 128).T
+            assert torch.equal(y.cpu(), want.to(F32).to(dtype))
+
+
+FFNS = [
+    # T, E, k, e0, EL, H, I, popularity
+    (1, 8, 2, 0, 8, 256, 192, None),
+    (13, 4, 2, 1, 2, 192, 320, None),
+    (70, 8, 2, 0, 8, 320, 128, [1, 1, 0, 0, 5, 1, 1, 1]),
+    (200, 3, 2, 0, 3, 128, 448, None),
+    (290, 2, 1, 0, 2, 576, 64, [1, 0]),
+]
+
+
+def ffn_inputs(g, T, H, I, EL):
+    x = torch.randn((T, H), generator=g) * torch.exp(0.5 * torch.randn((T, 1), generator=g))
+    q = torch.empty((T, H), dtype=torch.float8_e4m3fn, device="cuda")
+    s = torch.empty((T, ref.pitch(H)), dtype=torch.uint8, device="cuda")
+    moe.quant_rows(cuda(x), q, s)
+    out = [q, s]
+    for n, k in ((I, H), (I, H), (H, I)):
+        w = (torch.randn((EL, n, k), generator=g) * 0.05).to(BF16)
+        wq = torch.empty((EL, n, k), dtype=torch.float8_e4m3fn, device="cuda")
+        ws = torch.empty((EL, ref.blocks(n), ref.pitch(k)), dtype=torch.uint8, device="cuda")
+        moe.quant_weights(cuda(w), wq, ws)
+        out += [wq, ws]
+    return out
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("case", FFNS, ids=str)
+def test_ffn_group(case, dtype):
+    T, E, k, e0, EL, H, I, pop = case
+    g = gen(T + H + I)
+    off, slot, cap = dispatch(g, T, E, k, e0, EL, pop)
+    d = moe.dims(T, H, I, E, k, e0, EL)
+    t = ffn_inputs(g, T, H, I, EL)
+    need = moe.scaled_workspace_bytes(d)
+    ws = torch.full((need + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    y = torch.full((cap, H), 33.0, dtype=dtype, device="cuda")
+    first, count = (0, EL) if T % 2 else (EL - 2, 2)
+    moe.ffn_group_scaled(d, first, count, cuda(off), cuda(slot), *t, y, ws[:need])
+    torch.cuda.synchronize()
+    assert bool((ws[need:] == 0xA5).all())
+    x = ref.widen(t[0], t[1], 1)
+    got = y.cpu().double()
+    for e in range(EL):
+        lo, hi = int(off[e]), int(off[e + 1])
+        if not first <= e < first + count:
+            assert bool((got[lo:hi] == 33).all())
+            continue
+        if lo == hi:
+            continue
+        w = [ref.widen(t[i][e], t[i + 1][e], 128) for i in (2, 4, 6)]
+        want, bound = ref.ffn_rows(x[(slot[lo:hi] // k).long()], *w)
+        off_by = (got[lo:hi] - want).abs()
+        assert bool((off_by <= bound + HALF(dtype) * (want.abs() + bound)).all())
+        # the bound lets every value next to a rounding border flip; few do
+        assert float(off_by.norm() / want.norm()) < 0.02
+    assert bool((got[int(off[EL]):] == 33).all())
+    # rows in dispatch order give the same as rows gathered on the way
+    rows = cuda((slot[:int(off[EL])] // k).long())
+    xp = torch.zeros((cap, H), dtype=torch.uint8, device="cuda")
+    sp = torch.zeros((cap, ref.pitch(H)), dtype=torch.uint8, device="cuda")
+    xp[:len(rows)], sp[:len(rows)] = t[0].view(torch.uint8)[rows], t[1][rows]
+    y2 = torch.full((cap, H), 33.0, dtype=dtype, device="cuda")
+    moe.ffn_group_scaled(d, first, count, cuda(off), None, xp, sp, *t[2:], y2, ws[:need])
+    assert torch.equal(y2, y)
+
+
+@gpu
+def test_other_stream_and_graph_replays():
+    T, E, k, H, I = 48, 8, 2, 256, 192
+    g = gen(3)
+    off, slot, cap = dispatch(g, T, E, k, 0, E, None)
+    d = moe.dims(T, H, I, E, k)
+    t = ffn_inputs(g, T, H, I, E)
+    off, slot = cuda(off), cuda(slot)
+    ws = torch.empty(moe.scaled_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    x = torch.randn((T, H), generator=g).cuda()
+    y0 = torch.zeros((cap, H), device="cuda")
+
+    def step(y, st=None):
+        moe.quant_rows(x, t[0], t[1], stream=st)
+        moe.ffn_group_scaled(d, 0, E, off, slot, *t, y, ws, stream=st)
+    step(y0)
+    torch.cuda.synchronize()
+    y1 = torch.zeros_like(y0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(y1, side)
+    side.synchronize()
+    assert torch.equal(y0, y1)
+    y2 = torch.zeros_like(y0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(y2)
+    for i in range(3):
+        x.copy_(torch.randn((T, H), generator=g))
+        step(y0)  # eager work between the replays
+        y2.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y0, y2), i
+
+
+@gpu
+def test_runs_are_the_same_bit_for_bit():
+    for T in (3, 300):
+        g = gen(T)
+        off, slot, cap = dispatch(g, T, 4, 2, 0, 4, None)
+        d = moe.dims(T, 576, 320, 4, 2)
+        t = ffn_inputs(g, T, 576, 320, 4)
+        ws = torch.empty(moe.scaled_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+        ys = []
+        for i in range(3):
+            ws.fill_(i)
+            ys.append(torch.zeros((cap, 576), device="cuda"))
+            moe.ffn_group_scaled(d, 0, 4, cuda(off), cuda(slot), *t, ys[-1], ws)
+        assert torch.equal(ys[0], ys[1]) and torch.equal(ys[0], ys[2])
+
+
+@gpu
+def test_norm_route_dispatch_ffn_combine():
+    """The operators in a row, as a layer uses them."""
+    T, E, k, H, I = 77, 8, 2, 256, 192
+    g = gen(11)
+    moe_out = torch.randn((T, H), generator=g)
+    res = torch.randn((T, H), generator=g).to(BF16)
+    norm_w = (1 + 0.1 * torch.randn(H, generator=g)).to(BF16)
+    router = (torch.randn((E, H), generator=g) * 0.05).cuda()
+    t = ffn_inputs(g, T, H, I, E)
+    d = moe.dims(T, H, I, E, k)
+    dev = dict(device="cuda")
+    total, y = torch.empty((T, H), dtype=BF16, **dev), torch.empty((T, H), dtype=BF16, **dev)
+    moe.norm_quant(cuda(moe_out), cuda(res), cuda(norm_w), 1e-6, total, y, t[0], t[1])
+    ids, w = torch.empty((T, k), dtype=torch.int32, **dev), torch.empty((T, k), **dev)
+    moe.route(d, y, router, None, ids, w)
+    counts, off = torch.empty(E, dtype=torch.int32, **dev), torch.empty(E + 1, dtype=torch.int32,
+                                                                        **dev)
+    slot, slot_row = (torch.empty(T * k, dtype=torch.int32, **dev) for _ in range(2))
+    pws = torch.empty(moe.workspace_bytes(d), dtype=torch.uint8, **dev)
+    moe.permute(d, ids, None, counts, off, slot, slot_row, None, pws)
+    y_perm = torch.empty((T * k, H), **dev)
+    ws = torch.empty(moe.scaled_workspace_bytes(d), dtype=torch.uint8, **dev)
+    moe.ffn_group_scaled(d, 0, E, off, slot, *t, y_perm, ws)
+    out = torch.empty((T, H), **dev)
+    moe.combine(d, 0, E, y_perm, ids, slot_row, w, out, False)
+    torch.cuda.synchronize()
+    x = ref.widen(t[0], t[1], 1)
+    want, bound = torch.zeros((T, H), dtype=torch.float64), torch.zeros((T, H),
+                                                                       dtype=torch.float64)
+    ids, w = ids.cpu(), w.cpu().double()
+    for e in range(E):
+        tok, j = (ids == e).nonzero(as_tuple=True)
+        if len(tok) == 0:
+            continue
+        ww = [ref.widen(t[i][e], t[i + 1][e], 128) for i in (2, 4, 6)]
+        ye, be = ref.ffn_rows(x[tok], *ww)
+        want.index_add_(0, tok, w[tok, j, None] * ye)
+        bound.index_add_(0, tok, w[tok, j, None] * (be + (k + 1) * 2.0 ** -23 * ye.abs()))
+    assert bool(((out.cpu().double() - want).abs() <= bound).all())
