@@ -33,6 +33,14 @@ __device__ __forceinline__ void buf16_to_lds(const u32x4 &rsrc, uint32_t voff, u
                  : "v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds_addr)
                  : "memory");
 }
+// The same of 4 bytes per lane (lane l's go to lds_addr + 4 l).
+__device__ __forceinline__ void buf4_to_lds(const u32x4 &rsrc, uint32_t voff, uint32_t soff,
+                                            uint32_t lds_addr) {
+    asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, %2 offen lds"
+                 :
+                 : "v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds_addr)
+                 : "memory");
+}
 __device__ __forceinline__ u32x4 buf_rsrc(const void *p) {
     const uint64_t b = (uint64_t)(uintptr_t)p;
     return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b),

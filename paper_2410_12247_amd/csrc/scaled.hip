@@ -1,6 +1,7 @@
 // Products over block-scaled 8-bit tensors on the gfx950 matrix cores.
 #include <algorithm>
 
+#include "lds_dma.h"
 #include "scaled.h"
 
 namespace moe {
@@ -26,18 +27,37 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
 }
 
+// ---------------------------------------------------------------------------
+// Tile of 256 weight rows x BM token rows, four waves (one per SIMD) in a 2 x 2
+// arrangement, each with a 128 x BM/2 accumulator block of 32 x 32 MFMAs.
+// K advances 64 per stage through a ring of LDS stages filled by LDS-DMA.
+// ---------------------------------------------------------------------------
 template <int MODE, int BM_>
 struct Cfg {
     static constexpr int BM = BM_;
-    static constexpr int BN = 256;                          // weight rows of the tile
+    static constexpr int BN = 256;                            // weight rows of the tile
     static constexpr int BNOUT = MODE == SWIGLU ? 128 : 256;  // output columns
     static constexpr int THREADS = 256;
+    static constexpr int BK = 64, NS = 4;  // bytes of a row per stage, stages of the ring
     static constexpr int WTN = 128, WTM = BM / 2;
     static constexpr int TN = WTN / 32, TM = WTM / 32;
+    static constexpr int WI = BN / 16 / 4, XI = BM / 16 / 4;  // LDS-DMA requests per wave, stage
+    static constexpr int LPS = WI + XI;
+    static constexpr int STAGE_W = BN * BK, STAGE = (BN + BM) * BK;
     static constexpr int ES = MODE == OUT_F32 ? 4 : 2;
-    static constexpr int OUT_ROW = 128 * ES + 16;  // scratch row of the epilogue
-    static constexpr int LDS_BYTES =
-        MODE == SWIGLU ? BM * 128 + 2 * BM * 4 : 4 * 32 * OUT_ROW;
+    // LDS: ring | token scales [SG][256] words | row indices [2][256] |
+    // epilogue scratch | expert offsets
+    static constexpr int SG = 8;
+    static constexpr int SCALES = NS * STAGE;
+    static constexpr int IDX = SCALES + SG * 1024;
+    static constexpr int SCRATCH = IDX + 2 * 1024;
+    static constexpr int SC_COLS = MODE == OUT_F32 ? 32 : 64;  // columns of a scratch block
+    static constexpr int SC_ROW = (MODE == SWIGLU ? 64 : SC_COLS * ES) + 16;
+    static constexpr int SC_WAVE = 32 * SC_ROW;
+    static constexpr int SMAX = SCRATCH + 4 * SC_WAVE;
+    static constexpr int INTS = SMAX + (MODE == SWIGLU ? 2 * BM * 4 : 0);
+    static constexpr int LDS_BYTES = INTS + 2 * (kMaxExperts + 1) * 4;
+    static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
 };
 
 struct Tile {
@@ -96,129 +116,275 @@ struct Walk {
     }
 };
 
-template <int MODE, int BM_>
-__global__ __launch_bounds__(256) void scaled_kernel(ScaledGemm g) {
-    using C = Cfg<MODE, BM_>;
-    __shared__ __attribute__((aligned(16))) char smem[C::LDS_BYTES];
-    __shared__ int s_int[2 * (kMaxExperts + 1)];
-    const Walk<C> walk(g, s_int);
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wn = wave & 1, wm = wave >> 1;
-    const int K = g.K, SK = scale_pitch(K);
+typedef const __attribute__((address_space(4))) uint32_t *scalar_words;
 
-    for (int tau = blockIdx.x; tau < walk.total; tau += gridDim.x) {
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <int MODE, int BM_>
+struct TileLoop {
+    using C = Cfg<MODE, BM_>;
+    struct Frags {
+        u32x4 a[C::TN][2], b[C::TM][2];
+    };
+
+    const ScaledGemm &g;
+    const Walk<C> &walk;
+    char *smem;
+    uint32_t lds0;
+    int lane, wave, wn, wm, K, SK, nk, G;
+
+    // load side: the tile whose stages are being requested
+    int l_tau, l_ks, l_slot, l_group, l_idx;
+    u32x4 wres, xres, sres;
+    uint32_t woff[C::WI], xoff[C::XI], soff;
+
+    // compute side
+    int c_slot, c_group, c_byte;
+    floatx16 acc[C::TN][C::TM];
+    int sx[C::TM], sxn[C::TM];
+
+    __device__ __forceinline__ TileLoop(const ScaledGemm &g_, const Walk<C> &w_, char *sm)
+        : g(g_), walk(w_), smem(sm) {
+        lds0 = (uint32_t)(uintptr_t)(lds_void_t *)sm;
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wn = wave & 1, wm = wave >> 1;
+        K = g.K, SK = scale_pitch(K), nk = K / C::BK;
+        G = gridDim.x;
+    }
+
+    // The row indices of tile tau, one request per wave (behind the last row:
+    // the last one's).
+    __device__ __forceinline__ void request_idx(int tau, int which) {
+        if (!g.row_map || tau >= walk.total) return;
         const Tile t = walk.tile(g, tau);
-        // operand rows of this lane
-        const uint8_t *wrow[C::TN], *xrow[C::TM], *wsc[C::TN], *xsc[C::TM];
-        const int64_t we = (int64_t)(g.e_first + t.e) * g.N;
-        const int64_t se = (int64_t)(g.e_first + t.e) * scale_blocks(g.N);
+        const uint32_t r = (uint32_t)min(wave * 64 + lane, t.m_valid - 1) * 4u;
+        buf4_to_lds(buf_rsrc(g.row_map + t.r0), r, 0,
+                    lds0 + C::IDX + which * 1024 + wave * 256);
+    }
+
+    // Operand addresses of tile l_tau.
+    __device__ __forceinline__ void bind() {
+        const Tile t = walk.tile(g, l_tau);
+        const int64_t we = (int64_t)(g.e_first + t.e) * g.N + t.n0;
+        const bool up = MODE == SWIGLU && wave >= 2;
+        const int wrow0 = MODE == SWIGLU ? (wave & 1) * 64 : wave * 64;
+        wres = buf_rsrc((up ? g.w1 : g.w0) + we * K);
+        int ln = threadIdx.x & 63;  // opaque: its products are not kept over the K loop
+        asm volatile("" : "+v"(ln));
+        const int drow = ln >> 2;
+        const uint32_t chunk = (uint32_t)((ln & 3) ^ ((ln >> 3) & 3)) * 16u;
 #pragma unroll
-        for (int i = 0; i < C::TN; ++i) {
-            const bool up = MODE == SWIGLU && i >= C::TN / 2;
-            const int r = MODE == SWIGLU ? wn * 64 + (i % 2) * 32 : wn * 128 + i * 32;
-            const int64_t row = t.n0 + min(r + (lane & 31), t.n_valid - 1);
-            wrow[i] = (up ? g.w1 : g.w0) + (we + row) * K;
-            wsc[i] = (up ? g.s1 : g.s0) + (se + row / kScaleBlock) * SK;
-        }
+        for (int i = 0; i < C::WI; ++i)
+            woff[i] = (uint32_t)(min(wrow0 + i * 16 + drow, t.n_valid - 1) * K) + chunk;
+        const int srow = min(wave * 64 + ln, t.m_valid - 1);
+        if (g.row_map) {
+            const int *idx = reinterpret_cast<const int *>(smem + C::IDX + l_idx * 1024);
+            xres = buf_rsrc(g.x);
+            sres = buf_rsrc(g.xs);
 #pragma unroll
-        for (int j = 0; j < C::TM; ++j) {
-            const int64_t r = t.r0 + min(wm * C::WTM + j * 32 + (lane & 31), t.m_valid - 1);
-            const int64_t src = g.row_map ? g.row_map[r] / g.slot_div : r;
-            xrow[j] = g.x + src * K;
-            xsc[j] = g.xs + src * SK;
+            for (int i = 0; i < C::XI; ++i)
+                xoff[i] = (uint32_t)(idx[(wave * C::XI + i) * 16 + drow] / g.slot_div) *
+                              (uint32_t)K + chunk;
+            soff = (uint32_t)(idx[srow] / g.slot_div) * (uint32_t)SK;
+        } else {
+            xres = buf_rsrc(g.x + t.r0 * K);
+            sres = buf_rsrc(g.xs + t.r0 * SK);
+#pragma unroll
+            for (int i = 0; i < C::XI; ++i)
+                xoff[i] = (uint32_t)(min((wave * C::XI + i) * 16 + drow, t.m_valid - 1) * K) +
+                          chunk;
+            soff = (uint32_t)(srow * SK);
         }
-        floatx16 acc[C::TN][C::TM];
+        l_ks = 0;
+    }
+    // Behind a stage's requests: the next tile's first stage follows the last
+    // one (behind the last tile: its last stage again, which nothing reads).
+    __device__ __forceinline__ void advance() {
+        l_slot = l_slot == C::NS - 1 ? 0 : l_slot + 1;
+        if (++l_ks < nk) return;
+        if (l_tau + G >= walk.total) {
+            l_ks = nk - 1;
+            return;
+        }
+        l_tau += G;
+        if (g.row_map) {
+            l_idx ^= 1;
+            if (nk <= C::NS) {  // its indices may still be on their way
+                wait_vmcnt<0>();
+                __builtin_amdgcn_s_barrier();
+            }
+        }
+        bind();
+        request_idx(l_tau + G, l_idx ^ 1);
+    }
+    __device__ __forceinline__ void request_scales() {
+        if (l_ks & 7) return;
+        buf4_to_lds(sres, soff, (uint32_t)(l_ks >> 3) * 4u,
+                    lds0 + C::SCALES + l_group * 1024 + wave * 256);
+        l_group = (l_group + 1) & (C::SG - 1);
+    }
+    // request i of the stage's LPS
+    __device__ __forceinline__ void request(int i) {
+        const uint32_t kb = (uint32_t)l_ks * C::BK;
+        const uint32_t base = lds0 + (uint32_t)l_slot * C::STAGE;
+        if (i < C::WI)
+            buf16_to_lds(wres, woff[i], kb, base + (wave * C::WI + i) * 1024);
+        else
+            buf16_to_lds(xres, xoff[i - C::WI], kb,
+                         base + C::STAGE_W + (wave * C::XI + i - C::WI) * 1024);
+    }
+    __device__ __forceinline__ void request_stage() {
+        request_scales();
+#pragma unroll
+        for (int i = 0; i < C::LPS; ++i) request(i);
+        advance();
+    }
+
+    // read r of the next stage's 2 (TN + TM): 16 bytes of a fragment
+    __device__ __forceinline__ void read(Frags &f, int r) {
+        const int row = lane & 31, h = r & 1;
+        const int chunk = ((((lane >> 5) * 2 + h) ^ ((row >> 1) & 3))) * 16;
+        const char *st = smem + c_slot * C::STAGE;
+        if (r < 2 * C::TN) {
+            const int i = r >> 1;
+            const int w0 = MODE == SWIGLU ? (i >= 2 ? 128 : 0) + wn * 64 + (i & 1) * 32
+                                          : wn * 128 + i * 32;
+            f.a[i][h] = *reinterpret_cast<const u32x4 *>(st + (w0 + row) * C::BK + chunk);
+        } else {
+            const int j = (r >> 1) - C::TN;
+            f.b[j][h] = *reinterpret_cast<const u32x4 *>(
+                st + C::STAGE_W + (wm * C::WTM + j * 32 + row) * C::BK + chunk);
+        }
+    }
+    __device__ __forceinline__ void read_scales(int (&s)[C::TM]) {
+        const uint8_t *p = reinterpret_cast<const uint8_t *>(smem) + C::SCALES +
+                           c_group * 1024 + c_byte;
+#pragma unroll
+        for (int j = 0; j < C::TM; ++j) s[j] = p[(wm * C::WTM + j * 32 + (lane & 31)) * 4];
+    }
+    __device__ __forceinline__ static v8i whole(const u32x4 (&v)[2]) {
+        return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3],
+                   (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
+    }
+
+    // One stage: its MFMAs, with the next stage's fragment reads and the
+    // requests of the stage NS ahead between them.  Behind it the stage after
+    // the next has landed for every wave.
+    __device__ __forceinline__ void body(const Frags &cur, Frags &nxt, int sw0, int sw1) {
+        constexpr int NM = C::TN * C::TM, NR = 2 * (C::TN + C::TM);
+        constexpr int RM = NM * 3 / 4;  // reads go behind the first three quarters
+        c_slot = c_slot == C::NS - 1 ? 0 : c_slot + 1;
+        request_scales();
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            const int i = m / C::TM, j = m % C::TM;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                whole(cur.a[i]), whole(cur.b[j]), acc[i][j], 0, 0, 0,
+                MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
+            if (m < RM) {
+#pragma unroll
+                for (int r = m * NR / RM; r < (m + 1) * NR / RM; ++r) read(nxt, r);
+            }
+#pragma unroll
+            for (int q = m * C::LPS / NM; q < (m + 1) * C::LPS / NM; ++q) request(q);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // (the sums count as used here: the compiler would move their MFMAs
+        // behind the branches that follow, away from the requests and reads)
 #pragma unroll
         for (int i = 0; i < C::TN; ++i)
 #pragma unroll
-            for (int j = 0; j < C::TM; ++j)
+            for (int j = 0; j < C::TM; ++j) asm volatile("" : "+a"(acc[i][j]));
+        advance();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wait_vmcnt<2 * C::LPS>();
+        __builtin_amdgcn_s_barrier();
+    }
+};
+
+// Between the steps of an epilogue block: a wave's LDS accesses stay in order,
+// and no later block's accumulators are taken up early.
+__device__ __forceinline__ void block_end() {
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int MODE, int BM_, class L>
+__device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &loop, char *smem) {
+    using C = Cfg<MODE, BM_>;
+    int lane = threadIdx.x & 63;  // opaque: its products are not kept over the K loop
+    asm volatile("" : "+v"(lane));
+    const int wave = loop.wave, wn = loop.wn, wm = loop.wm, half = lane >> 5;
+    auto &acc = loop.acc;
+    // The lane holds, of token row wm WTM + 32 j + lane % 32, the weight rows
+    // 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4.
+    char *sc = smem + C::SCRATCH + wave * C::SC_WAVE;
+    if constexpr (MODE == SWIGLU) {
+        float *smax = reinterpret_cast<float *>(smem + C::SMAX);  // [2][BM]
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        for (int k = 0; k < K; k += 64) {
-            const int at = k + (lane >> 5) * 32;
-            v8i a[C::TN], b[C::TM];
-            int sa[C::TN], sb[C::TM];
-            auto load = [&](const uint8_t *p) {
-                const u32x4 lo = *reinterpret_cast<const u32x4 *>(p + at);
-                const u32x4 hi = *reinterpret_cast<const u32x4 *>(p + at + 16);
-                return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
-                           (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-            };
+        for (int j = 0; j < C::TM; ++j) {
+            float m = 0.f;
 #pragma unroll
-            for (int i = 0; i < C::TN; ++i) a[i] = load(wrow[i]), sa[i] = wsc[i][k / kScaleBlock];
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < C::TM; ++j) b[j] = load(xrow[j]), sb[j] = xsc[j][k / kScaleBlock];
-#pragma unroll
-            for (int i = 0; i < C::TN; ++i)
-#pragma unroll
-                for (int j = 0; j < C::TM; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                        a[i], b[j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
+                for (int r = 0; r < 16; ++r) {
+                    const float h = wn * 64 + i * 32 < t.n_valid
+                                        ? silu_mul(acc[i][j][r], acc[i + 2][j][r])
+                                        : 0.f;
+                    acc[i][j][r] = h;
+                    m = fmaxf(m, fabsf(h));
+                }
+            m = fmaxf(m, __shfl_xor(m, 32));
+            if (half == 0) smax[wn * C::BM + wm * C::WTM + j * 32 + lane] = m;
+            __builtin_amdgcn_sched_barrier(0);
         }
-        // The lane holds, of token row wm WTM + 32 j + lane % 32, the weight
-        // rows 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4.
-        const int half = lane >> 5;
-        __syncthreads();
-        if constexpr (MODE == SWIGLU) {
-            float *smax = reinterpret_cast<float *>(smem + C::BM * 128);  // [2][BM]
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
 #pragma unroll
-            for (int j = 0; j < C::TM; ++j) {
-                float m = 0.f;
+        for (int j = 0; j < C::TM; ++j) {
+            const int row = wm * C::WTM + j * 32 + (lane & 31);
+            const int e = scale_exponent(fmaxf(smax[row], smax[C::BM + row]));
+            const float inv = scale_inverse(e);
+            if (wn == 0 && half == 0 && row < t.m_valid)
+                g.out_s[(t.r0 + row) * scale_pitch(g.N) + t.n0 / kScaleBlock] = scale_byte(e);
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float h = wn * 64 + i * 32 < t.n_valid
-                                            ? silu_mul(acc[i][j][r], acc[i + 2][j][r])
-                                            : 0.f;
-                        acc[i][j][r] = h;
-                        m = fmaxf(m, fabsf(h));
-                    }
-                m = fmaxf(m, __shfl_xor(m, 32));
-                if (half == 0) smax[wn * C::BM + wm * C::WTM + j * 32 + lane] = m;
+                for (int r = 0; r < 4; ++r)
+                    *reinterpret_cast<uint32_t *>(sc + (lane & 31) * C::SC_ROW + i * 32 + r * 8 +
+                                                  half * 4) =
+                        pack_e4m3(acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2],
+                                  acc[i][j][4 * r + 3], inv);
+            block_end();
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int rr = q * 16 + (lane >> 2), chunk = lane & 3;
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(sc + rr * C::SC_ROW + chunk * 16);
+                const int orow = wm * C::WTM + j * 32 + rr;
+                if (orow < t.m_valid && wn * 64 < t.n_valid)
+                    *reinterpret_cast<u32x4 *>((uint8_t *)g.out + (t.r0 + orow) * g.N + t.n0 +
+                                               wn * 64 + chunk * 16) = v;
             }
-            __syncthreads();
+            block_end();
+        }
+        // (the next tile's maxima are written many barriers from here)
+    } else {
+        constexpr int IB = C::SC_COLS / 32;                  // fragments of a scratch block
+        constexpr int CPR = C::SC_COLS * C::ES / 16, RPI = 64 / CPR;  // chunks per row, rows a pass
 #pragma unroll
-            for (int j = 0; j < C::TM; ++j) {
-                const int row = wm * C::WTM + j * 32 + (lane & 31);
-                const int e = scale_exponent(fmaxf(smax[row], smax[C::BM + row]));
-                const float inv = scale_inverse(e);
-                if (wn == 0 && half == 0 && row < t.m_valid)
-                    g.out_s[(t.r0 + row) * scale_pitch(g.N) + t.n0 / kScaleBlock] = scale_byte(e);
+        for (int j = 0; j < C::TM; ++j)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+            for (int ib = 0; ib < C::TN; ib += IB) {
+#pragma unroll
+                for (int i = 0; i < IB; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int col = wn * 64 + i * 32 + r * 8 + half * 4;
-                        // 16-byte chunks swizzled by the row
-                        char *p = smem + row * 128 + (((col >> 4) ^ (row & 7)) << 4) + (col & 15);
-                        *reinterpret_cast<uint32_t *>(p) =
-                            pack_e4m3(acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2],
-                                      acc[i][j][4 * r + 3], inv);
-                    }
-            }
-            __syncthreads();
-            for (int c = threadIdx.x; c < C::BM * 8; c += C::THREADS) {
-                const int row = c >> 3, chunk = c & 7;
-                if (row < t.m_valid && chunk * 16 < t.n_valid)
-                    *reinterpret_cast<u32x4 *>((uint8_t *)g.out + (t.r0 + row) * g.N + t.n0 +
-                                               chunk * 16) =
-                        *reinterpret_cast<const u32x4 *>(smem + row * 128 +
-                                                         ((chunk ^ (row & 7)) << 4));
-            }
-        } else {
-            char *sc = smem + wave * 32 * C::OUT_ROW;
-            constexpr int CPR = 128 * C::ES / 16, RPI = 64 / CPR;  // chunks per row, rows per pass
-#pragma unroll
-            for (int j = 0; j < C::TM; ++j) {
-#pragma unroll
-                for (int i = 0; i < C::TN; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const floatx16 &v = acc[i][j];
-                        char *p = sc + (lane & 31) * C::OUT_ROW +
-                                  (i * 32 + r * 8 + half * 4) * C::ES;
+                        const floatx16 &v = acc[ib + i][j];
+                        char *p = sc + (lane & 31) * C::SC_ROW + (i * 32 + r * 8 + half * 4) * C::ES;
                         if (MODE == OUT_F32) {
                             *reinterpret_cast<floatx4 *>(p) =
                                 floatx4{v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]};
@@ -229,26 +395,117 @@ __global__ __launch_bounds__(256) void scaled_kernel(ScaledGemm g) {
                             *reinterpret_cast<uint2 *>(p) = u;
                         }
                     }
-                __builtin_amdgcn_wave_barrier();
+                block_end();
+#pragma unroll
                 for (int q = 0; q < 32 / RPI; ++q) {
                     const int rr = q * RPI + lane / CPR, chunk = lane % CPR;
                     const int row = wm * C::WTM + j * 32 + rr;
-                    const int col = wn * 128 + chunk * (16 / C::ES);
+                    const int col = wn * 128 + ib * 32 + chunk * (16 / C::ES);
                     const u32x4 v =
-                        *reinterpret_cast<const u32x4 *>(sc + rr * C::OUT_ROW + chunk * 16);
+                        *reinterpret_cast<const u32x4 *>(sc + rr * C::SC_ROW + chunk * 16);
                     if (row < t.m_valid && col < t.n_valid)
                         *reinterpret_cast<u32x4 *>((char *)g.out +
                                                    ((t.r0 + row) * g.N + t.n0 + col) * C::ES) = v;
                 }
-                __builtin_amdgcn_wave_barrier();
+                block_end();
             }
-        }
     }
 }
 
+template <int MODE, int BM_>
+__global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
+    using C = Cfg<MODE, BM_>;
+    using L = TileLoop<MODE, BM_>;
+    __shared__ __attribute__((aligned(16))) char smem[C::LDS_BYTES];
+    const Walk<C> walk(g, reinterpret_cast<int *>(smem + C::INTS));
+    const int slot = (blockIdx.x % NXCD) * (gridDim.x / NXCD) + blockIdx.x / NXCD;
+    if (slot >= walk.total) return;
+
+    L t(g, walk, smem);
+    t.l_tau = slot;
+    t.l_slot = t.l_group = t.l_idx = 0;
+    t.request_idx(slot, 0);
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    t.bind();
+    t.request_idx(slot + t.G, 1);
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) t.request_stage();
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    typename L::Frags f0, f1;
+    t.c_slot = t.c_group = t.c_byte = 0;
+#pragma unroll
+    for (int r = 0; r < 2 * (C::TN + C::TM); ++r) t.read(f0, r);
+    t.read_scales(t.sx);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+
+    for (int tau = slot; tau < walk.total; tau += t.G) {
+        const Tile tile = walk.tile(g, tau);
+        const int64_t nb = (int64_t)(g.e_first + tile.e) * scale_blocks(g.N) +
+                           min((int)(tile.n0 / kScaleBlock) + (MODE == SWIGLU ? 0 : t.wn),
+                               scale_blocks(g.N) - 1);
+        auto words = [&](const uint8_t *s) {
+            const uint64_t a = (uint64_t)(uintptr_t)(s + nb * t.SK);
+            return (scalar_words)(uintptr_t)(
+                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a) |
+                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32);
+        };
+        const scalar_words ws0 = words(g.s0), ws1 = MODE == SWIGLU ? words(g.s1) : nullptr;
+        uint32_t w0 = ws0[0], w1 = MODE == SWIGLU ? ws1[0] : 0;
+#pragma unroll
+        for (int i = 0; i < C::TN; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TM; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) t.acc[i][j][r] = 0.f;
+        // behind the last stage of a block of 128: the next block's scales
+        auto next_scales = [&](int k) {
+            const bool last = k + 1 >= t.nk;
+            if (last || t.c_byte == 3) {
+                t.c_byte = 0;
+                t.c_group = (t.c_group + 1) & (C::SG - 1);
+            } else {
+                t.c_byte += 1;
+            }
+            t.read_scales(t.sxn);
+        };
+        auto next_words = [&](int k) {
+            w0 >>= 8, w1 >>= 8;
+            if ((k & 7) == 7 && k + 1 < t.nk) {
+                w0 = ws0[(k + 1) >> 3];
+                if (MODE == SWIGLU) w1 = ws1[(k + 1) >> 3];
+            }
+#pragma unroll
+            for (int j = 0; j < C::TM; ++j) t.sx[j] = t.sxn[j];
+        };
+        int k = 0;
+        for (; k + 1 < t.nk; k += 2) {
+            const int s0 = w0 & 255, s1 = w1 & 255;
+            t.body(f0, f1, s0, s1);
+            next_scales(k + 1);
+            t.body(f1, f0, s0, s1);
+            next_words(k + 1);
+        }
+        if (k < t.nk) {
+            next_scales(k);
+            t.body(f0, f1, w0 & 255, w1 & 255);
+            next_words(k);
+            f0 = f1;
+        }
+        epilogue<MODE, BM_>(g, tile, t, smem);
+    }
+    wait_vmcnt<0>();  // requests behind the last stage
+}
+
 template <int MODE>
-hipError_t go(const ScaledGemm &g, const ScaledLoad &, hipStream_t s) {
-    scaled_kernel<MODE, 128><<<(unsigned)device_cu_count(), 256, 0, s>>>(g);
+hipError_t go(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
+    const unsigned grid = (unsigned)std::max(NXCD, device_cu_count() / NXCD * NXCD);
+    if (load.rows / load.active > 128)
+        tile_kernel<MODE, 256><<<grid, 256, 0, s>>>(g);
+    else
+        tile_kernel<MODE, 128><<<grid, 256, 0, s>>>(g);
     return hipGetLastError();
 }
 
