@@ -30,7 +30,8 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
 // ---------------------------------------------------------------------------
 // Tile of 256 weight rows x BM token rows, four waves (one per SIMD) in a 2 x 2
 // arrangement, each with a 128 x BM/2 accumulator block of 32 x 32 MFMAs.
-// K advances 64 per stage through a ring of LDS stages filled by LDS-DMA.
+// K advances by pairs of 64 (one MFMA's K, so a pair is a scale block) through
+// two LDS buffers filled by LDS-DMA with whole 128-byte lines of the rows.
 // ---------------------------------------------------------------------------
 template <int MODE, int BM_>
 struct Cfg {
@@ -38,16 +39,16 @@ struct Cfg {
     static constexpr int BN = 256;                            // weight rows of the tile
     static constexpr int BNOUT = MODE == SWIGLU ? 128 : 256;  // output columns
     static constexpr int THREADS = 256;
-    static constexpr int BK = 64, NS = 4;  // bytes of a row per stage, stages of the ring
+    static constexpr int BK = 128, NS = 2;  // bytes of a row per pair, LDS buffers
     static constexpr int WTN = 128, WTM = BM / 2;
     static constexpr int TN = WTN / 32, TM = WTM / 32;
-    static constexpr int WI = BN / 16 / 4, XI = BM / 16 / 4;  // LDS-DMA requests per wave, stage
+    static constexpr int WI = BN / 8 / 4, XI = BM / 8 / 4;  // LDS-DMA requests per wave and pair
     static constexpr int LPS = WI + XI;
     static constexpr int STAGE_W = BN * BK, STAGE = (BN + BM) * BK;
     static constexpr int ES = MODE == OUT_F32 ? 4 : 2;
     // LDS: ring | token scales [SG][256] words | row indices [2][256] |
     // epilogue scratch | expert offsets
-    static constexpr int SG = 8;
+    static constexpr int SG = 4;
     static constexpr int SCALES = NS * STAGE;
     static constexpr int IDX = SCALES + SG * 1024;
     static constexpr int SCRATCH = IDX + 2 * 1024;
@@ -134,12 +135,12 @@ struct TileLoop {
     const Walk<C> &walk;
     char *smem;
     uint32_t lds0;
-    int lane, wave, wn, wm, K, SK, nk, G;
+    int lane, wave, wn, wm, K, SK, np, G;
 
-    // load side: the tile whose stages are being requested
-    int l_tau, l_ks, l_slot, l_group, l_idx;
+    // load side: the tile whose pairs are being requested
+    int l_tau, l_kp, l_slot, l_group, l_idx;
     u32x4 wres, xres, sres;
-    uint32_t woff[C::WI], xoff[C::XI], soff;
+    uint32_t woff[C::WI], xoff[C::XI], soff, upper;
 
     // compute side
     int c_slot, c_group, c_byte;
@@ -152,8 +153,10 @@ struct TileLoop {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wn = wave & 1, wm = wave >> 1;
-        K = g.K, SK = scale_pitch(K), nk = K / C::BK;
+        K = g.K, SK = scale_pitch(K), np = scale_blocks(K);
         G = gridDim.x;
+        l_slot = l_group = l_idx = 0;
+        c_slot = c_group = c_byte = 0;
     }
 
     // The row indices of tile tau, one request per wave (behind the last row:
@@ -166,7 +169,9 @@ struct TileLoop {
                     lds0 + C::IDX + which * 1024 + wave * 256);
     }
 
-    // Operand addresses of tile l_tau.
+    // Operand addresses of tile l_tau.  A request copies 8 rows of 128 bytes;
+    // the 16-byte chunks of LDS row r are stored at chunk ^ (r / 2 % 8), so
+    // the 16 lanes of a fragment read that are served together find all banks.
     __device__ __forceinline__ void bind() {
         const Tile t = walk.tile(g, l_tau);
         const int64_t we = (int64_t)(g.e_first + t.e) * g.N + t.n0;
@@ -175,11 +180,16 @@ struct TileLoop {
         wres = buf_rsrc((up ? g.w1 : g.w0) + we * K);
         int ln = threadIdx.x & 63;  // opaque: its products are not kept over the K loop
         asm volatile("" : "+v"(ln));
-        const int drow = ln >> 2;
-        const uint32_t chunk = (uint32_t)((ln & 3) ^ ((ln >> 3) & 3)) * 16u;
+        const int drow = ln >> 3;
+        // LDS rows 8 i + drow: r / 2 % 8 is drow / 2 + 4 (i % 2)
+        const uint32_t c0 = (uint32_t)((ln & 7) ^ (drow >> 1)), c1 = c0 ^ 4u;
 #pragma unroll
         for (int i = 0; i < C::WI; ++i)
-            woff[i] = (uint32_t)(min(wrow0 + i * 16 + drow, t.n_valid - 1) * K) + chunk;
+            woff[i] = (uint32_t)(min(wrow0 + i * 8 + drow, t.n_valid - 1) * K) +
+                      (i & 1 ? c1 : c0) * 16u;
+        // where K ends inside a pair: how far a chunk of the missing half is
+        // moved back (one of the two chunks c0, c1 always is)
+        upper = c0 & 4u;
         const int srow = min(wave * 64 + ln, t.m_valid - 1);
         if (g.row_map) {
             const int *idx = reinterpret_cast<const int *>(smem + C::IDX + l_idx * 1024);
@@ -187,67 +197,71 @@ struct TileLoop {
             sres = buf_rsrc(g.xs);
 #pragma unroll
             for (int i = 0; i < C::XI; ++i)
-                xoff[i] = (uint32_t)(idx[(wave * C::XI + i) * 16 + drow] / g.slot_div) *
-                              (uint32_t)K + chunk;
+                xoff[i] = (uint32_t)(idx[(wave * C::XI + i) * 8 + drow] / g.slot_div) *
+                              (uint32_t)K + (i & 1 ? c1 : c0) * 16u;
             soff = (uint32_t)(idx[srow] / g.slot_div) * (uint32_t)SK;
         } else {
             xres = buf_rsrc(g.x + t.r0 * K);
             sres = buf_rsrc(g.xs + t.r0 * SK);
 #pragma unroll
             for (int i = 0; i < C::XI; ++i)
-                xoff[i] = (uint32_t)(min((wave * C::XI + i) * 16 + drow, t.m_valid - 1) * K) +
-                          chunk;
+                xoff[i] = (uint32_t)(min((wave * C::XI + i) * 8 + drow, t.m_valid - 1) * K) +
+                          (i & 1 ? c1 : c0) * 16u;
             soff = (uint32_t)(srow * SK);
         }
-        l_ks = 0;
+        l_kp = 0;
     }
-    // Behind a stage's requests: the next tile's first stage follows the last
-    // one (behind the last tile: its last stage again, which nothing reads).
+    // Behind a pair's requests: the next tile's first pair follows the last one
+    // (behind the last tile: its last pair again, which nothing reads).
     __device__ __forceinline__ void advance() {
-        l_slot = l_slot == C::NS - 1 ? 0 : l_slot + 1;
-        if (++l_ks < nk) return;
+        l_slot ^= 1;
+        if (++l_kp < np) return;
         if (l_tau + G >= walk.total) {
-            l_ks = nk - 1;
+            l_kp = np - 1;
             return;
         }
         l_tau += G;
-        if (g.row_map) {
-            l_idx ^= 1;
-            if (nk <= C::NS) {  // its indices may still be on their way
-                wait_vmcnt<0>();
-                __builtin_amdgcn_s_barrier();
-            }
-        }
+        l_idx ^= 1;
         bind();
         request_idx(l_tau + G, l_idx ^ 1);
     }
     __device__ __forceinline__ void request_scales() {
-        if (l_ks & 7) return;
-        buf4_to_lds(sres, soff, (uint32_t)(l_ks >> 3) * 4u,
+        if (l_kp & 3) return;
+        buf4_to_lds(sres, soff, (uint32_t)l_kp,
                     lds0 + C::SCALES + l_group * 1024 + wave * 256);
         l_group = (l_group + 1) & (C::SG - 1);
     }
-    // request i of the stage's LPS
-    __device__ __forceinline__ void request(int i) {
-        const uint32_t kb = (uint32_t)l_ks * C::BK;
+    // request i of the pair's LPS; back: 64 where the pair has one half only
+    __device__ __forceinline__ void request(int i, uint32_t back0, uint32_t back1) {
+        const uint32_t kb = (uint32_t)l_kp * C::BK;
         const uint32_t base = lds0 + (uint32_t)l_slot * C::STAGE;
         if (i < C::WI)
-            buf16_to_lds(wres, woff[i], kb, base + (wave * C::WI + i) * 1024);
+            buf16_to_lds(wres, woff[i] - (i & 1 ? back1 : back0), kb,
+                         base + (wave * C::WI + i) * 1024);
         else
-            buf16_to_lds(xres, xoff[i - C::WI], kb,
+            buf16_to_lds(xres, xoff[i - C::WI] - (i & 1 ? back1 : back0), kb,
                          base + C::STAGE_W + (wave * C::XI + i - C::WI) * 1024);
     }
-    __device__ __forceinline__ void request_stage() {
+    // The missing half's chunks read the half that is there (nothing uses them).
+    __device__ __forceinline__ void backs(uint32_t &back0, uint32_t &back1) const {
+        const bool half = (l_kp + 1) * C::BK > K;
+        back0 = half ? upper * 16u : 0u;
+        back1 = half ? (upper ^ 4u) * 16u : 0u;
+    }
+    __device__ __forceinline__ void request_pair() {
         request_scales();
+        uint32_t b0, b1;
+        backs(b0, b1);
 #pragma unroll
-        for (int i = 0; i < C::LPS; ++i) request(i);
+        for (int i = 0; i < C::LPS; ++i) request(i, b0, b1);
         advance();
     }
 
-    // read r of the next stage's 2 (TN + TM): 16 bytes of a fragment
-    __device__ __forceinline__ void read(Frags &f, int r) {
+    // read r of a fragment set's 2 (TN + TM): 16 bytes of half `hf` of the pair
+    // in c_slot
+    __device__ __forceinline__ void read(Frags &f, int r, int hf) {
         const int row = lane & 31, h = r & 1;
-        const int chunk = ((((lane >> 5) * 2 + h) ^ ((row >> 1) & 3))) * 16;
+        const int chunk = ((hf * 4 + (lane >> 5) * 2 + h) ^ ((row >> 1) & 7)) * 16;
         const char *st = smem + c_slot * C::STAGE;
         if (r < 2 * C::TN) {
             const int i = r >> 1;
@@ -271,26 +285,37 @@ struct TileLoop {
                    (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
     }
 
-    // One stage: its MFMAs, with the next stage's fragment reads and the
-    // requests of the stage NS ahead between them.  Behind it the stage after
-    // the next has landed for every wave.
+    // Half a pair's MFMAs, with the next half's fragment reads between them.
+    // FIRST half: the next fragments are the pair's other half's; behind it no
+    // wave needs the pair's buffer any more and the next pair has landed for
+    // every wave.  Second half: they are the next pair's, and the pair after it
+    // is requested into the buffer that has become free.
+    template <bool FIRST>
     __device__ __forceinline__ void body(const Frags &cur, Frags &nxt, int sw0, int sw1) {
         constexpr int NM = C::TN * C::TM, NR = 2 * (C::TN + C::TM);
         constexpr int RM = NM * 3 / 4;  // reads go behind the first three quarters
-        c_slot = c_slot == C::NS - 1 ? 0 : c_slot + 1;
-        request_scales();
+        constexpr int QM = NM / 2;      // requests behind the first half
+        uint32_t back0 = 0, back1 = 0;
+        if (!FIRST) {
+            c_slot ^= 1;
+            request_scales();
+            backs(back0, back1);
+        }
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
             const int i = m / C::TM, j = m % C::TM;
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
                 whole(cur.a[i]), whole(cur.b[j]), acc[i][j], 0, 0, 0,
                 MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
+            if (!FIRST && m < QM) {
+#pragma unroll
+                for (int q = m * C::LPS / QM; q < (m + 1) * C::LPS / QM; ++q)
+                    request(q, back0, back1);
+            }
             if (m < RM) {
 #pragma unroll
-                for (int r = m * NR / RM; r < (m + 1) * NR / RM; ++r) read(nxt, r);
+                for (int r = m * NR / RM; r < (m + 1) * NR / RM; ++r) read(nxt, r, FIRST ? 1 : 0);
             }
-#pragma unroll
-            for (int q = m * C::LPS / NM; q < (m + 1) * C::LPS / NM; ++q) request(q);
             __builtin_amdgcn_sched_barrier(0);
         }
         // (the sums count as used here: the compiler would move their MFMAs
@@ -299,9 +324,13 @@ struct TileLoop {
         for (int i = 0; i < C::TN; ++i)
 #pragma unroll
             for (int j = 0; j < C::TM; ++j) asm volatile("" : "+a"(acc[i][j]));
-        advance();
+        if (!FIRST) advance();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        wait_vmcnt<2 * C::LPS>();
+        if (FIRST) landed();
+    }
+    // Every wave's requests so far have landed, and its reads are done.
+    __device__ __forceinline__ void landed() {
+        wait_vmcnt<0>();
         __builtin_amdgcn_s_barrier();
     }
 };
@@ -312,6 +341,10 @@ __device__ __forceinline__ void block_end() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_sched_barrier(0);
 }
+
+// Keeps an accumulator in the matrix cores' registers up to here: the ones of
+// all blocks do not fit the others beside the next tile's fragments.
+__device__ __forceinline__ void in_place(floatx16 &v) { asm volatile("" : "+a"(v)); }
 
 template <int MODE, int BM_, class L>
 __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &loop, char *smem) {
@@ -329,7 +362,9 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
         for (int j = 0; j < C::TM; ++j) {
             float m = 0.f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i) {
+                in_place(acc[i][j]);
+                in_place(acc[i + 2][j]);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float h = wn * 64 + i * 32 < t.n_valid
@@ -338,6 +373,8 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
                     acc[i][j][r] = h;
                     m = fmaxf(m, fabsf(h));
                 }
+                in_place(acc[i][j]);
+            }
             m = fmaxf(m, __shfl_xor(m, 32));
             if (half == 0) smax[wn * C::BM + wm * C::WTM + j * 32 + lane] = m;
             __builtin_amdgcn_sched_barrier(0);
@@ -352,13 +389,15 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
             if (wn == 0 && half == 0 && row < t.m_valid)
                 g.out_s[(t.r0 + row) * scale_pitch(g.N) + t.n0 / kScaleBlock] = scale_byte(e);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i) {
+                in_place(acc[i][j]);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     *reinterpret_cast<uint32_t *>(sc + (lane & 31) * C::SC_ROW + i * 32 + r * 8 +
                                                   half * 4) =
                         pack_e4m3(acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2],
                                   acc[i][j][4 * r + 3], inv);
+            }
             block_end();
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
@@ -380,7 +419,8 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
 #pragma unroll
             for (int ib = 0; ib < C::TN; ib += IB) {
 #pragma unroll
-                for (int i = 0; i < IB; ++i)
+                for (int i = 0; i < IB; ++i) {
+                    in_place(acc[ib + i][j]);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const floatx16 &v = acc[ib + i][j];
@@ -395,6 +435,7 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
                             *reinterpret_cast<uint2 *>(p) = u;
                         }
                     }
+                }
                 block_end();
 #pragma unroll
                 for (int q = 0; q < 32 / RPI; ++q) {
@@ -423,23 +464,18 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
 
     L t(g, walk, smem);
     t.l_tau = slot;
-    t.l_slot = t.l_group = t.l_idx = 0;
     t.request_idx(slot, 0);
-    wait_vmcnt<0>();
-    __builtin_amdgcn_s_barrier();
+    t.landed();
     t.bind();
     t.request_idx(slot + t.G, 1);
-#pragma unroll
-    for (int s = 0; s < C::NS; ++s) t.request_stage();
-    wait_vmcnt<0>();
-    __builtin_amdgcn_s_barrier();
+    t.request_pair();
+    t.landed();  // (a tile of one pair: the next one's indices)
+    t.request_pair();
+    t.landed();
     typename L::Frags f0, f1;
-    t.c_slot = t.c_group = t.c_byte = 0;
 #pragma unroll
-    for (int r = 0; r < 2 * (C::TN + C::TM); ++r) t.read(f0, r);
+    for (int r = 0; r < 2 * (C::TN + C::TM); ++r) t.read(f0, r, 0);
     t.read_scales(t.sx);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
 
     for (int tau = slot; tau < walk.total; tau += t.G) {
         const Tile tile = walk.tile(g, tau);
@@ -460,10 +496,9 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
             for (int j = 0; j < C::TM; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) t.acc[i][j][r] = 0.f;
-        // behind the last stage of a block of 128: the next block's scales
-        auto next_scales = [&](int k) {
-            const bool last = k + 1 >= t.nk;
-            if (last || t.c_byte == 3) {
+        // the next pair's scales of the tokens, and behind the pair of the weights
+        auto next_scales = [&](int p) {
+            if (p + 1 >= t.np || t.c_byte == 3) {
                 t.c_byte = 0;
                 t.c_group = (t.c_group + 1) & (C::SG - 1);
             } else {
@@ -471,27 +506,28 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
             }
             t.read_scales(t.sxn);
         };
-        auto next_words = [&](int k) {
+        auto next_words = [&](int p) {
             w0 >>= 8, w1 >>= 8;
-            if ((k & 7) == 7 && k + 1 < t.nk) {
-                w0 = ws0[(k + 1) >> 3];
-                if (MODE == SWIGLU) w1 = ws1[(k + 1) >> 3];
+            if ((p & 3) == 3 && p + 1 < t.np) {
+                w0 = ws0[(p + 1) >> 2];
+                if (MODE == SWIGLU) w1 = ws1[(p + 1) >> 2];
             }
 #pragma unroll
             for (int j = 0; j < C::TM; ++j) t.sx[j] = t.sxn[j];
         };
-        int k = 0;
-        for (; k + 1 < t.nk; k += 2) {
+        const int whole = t.K / C::BK;
+        for (int p = 0; p < whole; ++p) {
             const int s0 = w0 & 255, s1 = w1 & 255;
-            t.body(f0, f1, s0, s1);
-            next_scales(k + 1);
-            t.body(f1, f0, s0, s1);
-            next_words(k + 1);
+            t.template body<true>(f0, f1, s0, s1);
+            next_scales(p);
+            t.template body<false>(f1, f0, s0, s1);
+            next_words(p);
         }
-        if (k < t.nk) {
-            next_scales(k);
-            t.body(f0, f1, w0 & 255, w1 & 255);
-            next_words(k);
+        if (whole < t.np) {  // half a pair: its fragments are in registers already
+            t.landed();
+            next_scales(whole);
+            t.template body<false>(f0, f1, w0 & 255, w1 & 255);
+            next_words(whole);
             f0 = f1;
         }
         epilogue<MODE, BM_>(g, tile, t, smem);
