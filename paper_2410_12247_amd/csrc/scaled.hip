@@ -10,6 +10,8 @@ namespace {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
+// buffer resource word 3 for raw (untyped, unswizzled) access on gfx9 parts
+constexpr int kBufferFlags = 0x00020000;
 constexpr int NXCD = 8;
 constexpr int GROUP_N = 8;  // n-tiles per super-column of the tile order
 
@@ -55,6 +57,8 @@ struct Cfg {
     static constexpr int SC_COLS = MODE == OUT_F32 ? 32 : 64;  // columns of a scratch block
     static constexpr int SC_ROW = (MODE == SWIGLU ? 64 : SC_COLS * ES) + 16;
     static constexpr int SC_WAVE = 32 * SC_ROW;
+    // 16-byte stores of a tile's epilogue per wave (all are issued, whatever is valid)
+    static constexpr int STORES = MODE == SWIGLU ? 2 * TM : TN * TM * (ES == 4 ? 4 : 2);
     static constexpr int SMAX = SCRATCH + 4 * SC_WAVE;
     static constexpr int INTS = SMAX + (MODE == SWIGLU ? 2 * BM * 4 : 0);
     static constexpr int LDS_BYTES = INTS + 2 * (kMaxExperts + 1) * 4;
@@ -127,8 +131,11 @@ __device__ __forceinline__ void wait_vmcnt() {
 template <int MODE, int BM_>
 struct TileLoop {
     using C = Cfg<MODE, BM_>;
-    struct Frags {
-        u32x4 a[C::TN][2], b[C::TM][2];
+    struct FragsA {
+        u32x4 v[C::TN][2];
+    };
+    struct FragsB {
+        u32x4 v[C::TM][2];
     };
 
     const ScaledGemm &g;
@@ -231,48 +238,53 @@ struct TileLoop {
                     lds0 + C::SCALES + l_group * 1024 + wave * 256);
         l_group = (l_group + 1) & (C::SG - 1);
     }
-    // request i of the pair's LPS; back: 64 where the pair has one half only
-    __device__ __forceinline__ void request(int i, uint32_t back0, uint32_t back1) {
-        const uint32_t kb = (uint32_t)l_kp * C::BK;
-        const uint32_t base = lds0 + (uint32_t)l_slot * C::STAGE;
-        if (i < C::WI)
-            buf16_to_lds(wres, woff[i] - (i & 1 ? back1 : back0), kb,
-                         base + (wave * C::WI + i) * 1024);
-        else
-            buf16_to_lds(xres, xoff[i - C::WI] - (i & 1 ? back1 : back0), kb,
-                         base + C::STAGE_W + (wave * C::XI + i - C::WI) * 1024);
-    }
-    // The missing half's chunks read the half that is there (nothing uses them).
+    // Where the pair has one half only, the other half's chunks read that one
+    // (nothing uses them): how far back, for even and odd requests.
     __device__ __forceinline__ void backs(uint32_t &back0, uint32_t &back1) const {
         const bool half = (l_kp + 1) * C::BK > K;
         back0 = half ? upper * 16u : 0u;
         back1 = half ? (upper ^ 4u) * 16u : 0u;
     }
-    __device__ __forceinline__ void request_pair() {
+    __device__ __forceinline__ void request_w(int i, uint32_t back0, uint32_t back1) {
+        buf16_to_lds(wres, woff[i] - (i & 1 ? back1 : back0), (uint32_t)l_kp * C::BK,
+                     lds0 + (uint32_t)l_slot * C::STAGE + (wave * C::WI + i) * 1024);
+    }
+    __device__ __forceinline__ void request_x(int i, uint32_t back0, uint32_t back1) {
+        buf16_to_lds(xres, xoff[i] - (i & 1 ? back1 : back0), (uint32_t)l_kp * C::BK,
+                     lds0 + (uint32_t)l_slot * C::STAGE + C::STAGE_W +
+                         (wave * C::XI + i) * 1024);
+    }
+    __device__ __forceinline__ void request_all_x() {
         request_scales();
         uint32_t b0, b1;
         backs(b0, b1);
 #pragma unroll
-        for (int i = 0; i < C::LPS; ++i) request(i, b0, b1);
+        for (int i = 0; i < C::XI; ++i) request_x(i, b0, b1);
+    }
+    __device__ __forceinline__ void request_pair() {
+        request_all_x();
+        uint32_t b0, b1;
+        backs(b0, b1);
+#pragma unroll
+        for (int i = 0; i < C::WI; ++i) request_w(i, b0, b1);
         advance();
     }
 
-    // read r of a fragment set's 2 (TN + TM): 16 bytes of half `hf` of the pair
-    // in c_slot
-    __device__ __forceinline__ void read(Frags &f, int r, int hf) {
-        const int row = lane & 31, h = r & 1;
+    // 16 bytes (h of 2) of a fragment, half `hf` of the pair in c_slot
+    __device__ __forceinline__ u32x4 read(int lds_row, int h, int hf) const {
+        const int row = lane & 31;
         const int chunk = ((hf * 4 + (lane >> 5) * 2 + h) ^ ((row >> 1) & 7)) * 16;
-        const char *st = smem + c_slot * C::STAGE;
-        if (r < 2 * C::TN) {
-            const int i = r >> 1;
-            const int w0 = MODE == SWIGLU ? (i >= 2 ? 128 : 0) + wn * 64 + (i & 1) * 32
-                                          : wn * 128 + i * 32;
-            f.a[i][h] = *reinterpret_cast<const u32x4 *>(st + (w0 + row) * C::BK + chunk);
-        } else {
-            const int j = (r >> 1) - C::TN;
-            f.b[j][h] = *reinterpret_cast<const u32x4 *>(
-                st + C::STAGE_W + (wm * C::WTM + j * 32 + row) * C::BK + chunk);
-        }
+        return *reinterpret_cast<const u32x4 *>(smem + c_slot * C::STAGE +
+                                                (lds_row + row) * C::BK + chunk);
+    }
+    __device__ __forceinline__ void read_a(FragsA &f, int r, int hf) const {
+        const int i = r >> 1;
+        const int w0 = MODE == SWIGLU ? (i >= 2 ? 128 : 0) + wn * 64 + (i & 1) * 32
+                                      : wn * 128 + i * 32;
+        f.v[i][r & 1] = read(w0, r & 1, hf);
+    }
+    __device__ __forceinline__ void read_b(FragsB &f, int r, int hf) const {
+        f.v[r >> 1][r & 1] = read(C::BN + wm * C::WTM + (r >> 1) * 32, r & 1, hf);
     }
     __device__ __forceinline__ void read_scales(int (&s)[C::TM]) {
         const uint8_t *p = reinterpret_cast<const uint8_t *>(smem) + C::SCALES +
@@ -285,52 +297,86 @@ struct TileLoop {
                    (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
     }
 
-    // Half a pair's MFMAs, with the next half's fragment reads between them.
-    // FIRST half: the next fragments are the pair's other half's; behind it no
-    // wave needs the pair's buffer any more and the next pair has landed for
-    // every wave.  Second half: they are the next pair's, and the pair after it
-    // is requested into the buffer that has become free.
-    template <bool FIRST>
-    __device__ __forceinline__ void body(const Frags &cur, Frags &nxt, int sw0, int sw1) {
-        constexpr int NM = C::TN * C::TM, NR = 2 * (C::TN + C::TM);
-        constexpr int RM = NM * 3 / 4;  // reads go behind the first three quarters
-        constexpr int QM = NM / 2;      // requests behind the first half
-        uint32_t back0 = 0, back1 = 0;
-        if (!FIRST) {
-            c_slot ^= 1;
-            request_scales();
-            backs(back0, back1);
-        }
-#pragma unroll
-        for (int m = 0; m < NM; ++m) {
-            const int i = m / C::TM, j = m % C::TM;
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                whole(cur.a[i]), whole(cur.b[j]), acc[i][j], 0, 0, 0,
-                MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
-            if (!FIRST && m < QM) {
-#pragma unroll
-                for (int q = m * C::LPS / QM; q < (m + 1) * C::LPS / QM; ++q)
-                    request(q, back0, back1);
-            }
-            if (m < RM) {
-#pragma unroll
-                for (int r = m * NR / RM; r < (m + 1) * NR / RM; ++r) read(nxt, r, FIRST ? 1 : 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        // (the sums count as used here: the compiler would move their MFMAs
-        // behind the branches that follow, away from the requests and reads)
+    __device__ __forceinline__ void mfma(const FragsA &a, const FragsB &b, int m, int sw0,
+                                         int sw1) {
+        const int i = m / C::TM, j = m % C::TM;
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            whole(a.v[i]), whole(b.v[j]), acc[i][j], 0, 0, 0,
+            MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
+    }
+    // (the sums count as used here: the compiler would move their MFMAs behind
+    // the branches that follow, away from the requests and reads)
+    __device__ __forceinline__ void sums_used() {
 #pragma unroll
         for (int i = 0; i < C::TN; ++i)
 #pragma unroll
             for (int j = 0; j < C::TM; ++j) asm volatile("" : "+a"(acc[i][j]));
-        if (!FIRST) advance();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (FIRST) landed();
     }
-    // Every wave's requests so far have landed, and its reads are done.
+    static constexpr int NM = C::TN * C::TM;
+    static constexpr int RM = NM * 3 / 4;  // reads go behind the first three quarters
+    // N of something spread evenly behind the first M of a half's MFMAs
+    template <int N, int M, class F>
+    __device__ __forceinline__ static void behind(int m, F &&f) {
+        if (m >= M) return;
+#pragma unroll
+        for (int q = m * N / M; q < (m + 1) * N / M; ++q) f(q);
+    }
+
+    // The first half of a pair.  The token rows of its buffer are in registers
+    // (both halves' fragments), so those of the pair after the next are
+    // requested into it; the other half's weight fragments are read.  Behind
+    // it no wave needs the pair's buffer, and the next pair has landed for
+    // every wave.  stored: the epilogue's stores, younger than that pair's
+    // requests, may still be on their way.
+    __device__ __forceinline__ void first_half(const FragsA &a, const FragsB &b, FragsA &a2,
+                                               int sw0, int sw1, bool stored) {
+        request_scales();
+        uint32_t b0, b1;
+        backs(b0, b1);
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            mfma(a, b, m, sw0, sw1);
+            behind<2 * C::TN, RM>(m, [&](int r) { read_a(a2, r, 1); });
+            behind<C::XI, NM>(m, [&](int q) { request_x(q, b0, b1); });
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sums_used();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (stored)
+            wait_vmcnt<(C::XI + C::STORES < 63 ? C::XI + C::STORES : 63)>();
+        else
+            wait_vmcnt<C::XI>();
+        __builtin_amdgcn_s_barrier();
+    }
+    // The second half: the weights of the pair after the next are requested,
+    // and the next pair's token fragments read for both halves (b, b2) and its
+    // weights' for the first (a).  Behind it every wave has its token rows.
+    __device__ __forceinline__ void second_half(const FragsA &ca, const FragsB &cb, FragsA &a,
+                                                FragsB &b, FragsB &b2, int sw0, int sw1) {
+        uint32_t b0, b1;
+        backs(b0, b1);
+        c_slot ^= 1;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            mfma(ca, cb, m, sw0, sw1);
+            behind<2 * C::TN + 4 * C::TM, RM>(m, [&](int r) {
+                if (r < 4 * C::TM)
+                    read_b(r & 1 ? b2 : b, r >> 1, r & 1);
+                else
+                    read_a(a, r - 4 * C::TM, 0);
+            });
+            behind<C::WI, NM>(m, [&](int q) { request_w(q, b0, b1); });
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sums_used();
+        advance();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+    }
+    // Every wave's requests so far but the youngest N have landed.
+    template <int N>
     __device__ __forceinline__ void landed() {
-        wait_vmcnt<0>();
+        wait_vmcnt<N>();
         __builtin_amdgcn_s_barrier();
     }
 };
@@ -356,6 +402,15 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
     // The lane holds, of token row wm WTM + 32 j + lane % 32, the weight rows
     // 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4.
     char *sc = smem + C::SCRATCH + wave * C::SC_WAVE;
+    // every store is issued, since the waits count them: what is not valid gets
+    // an offset past the resource's range, which drops it
+    constexpr uint32_t RANGE = 0xFFFFFFF0u, DROP = 0xFFFFFFF8u;
+    const __amdgpu_buffer_rsrc_t ores = __builtin_amdgcn_make_buffer_rsrc(
+        (char *)g.out + (t.r0 * g.N + t.n0) * (MODE == SWIGLU ? 1 : C::ES), 0, (int)RANGE,
+        kBufferFlags);
+    auto store = [&](const u32x4 &v, bool valid, uint32_t off) {
+        __builtin_amdgcn_raw_buffer_store_b128(v, ores, valid ? off : DROP, 0, 0);
+    };
     if constexpr (MODE == SWIGLU) {
         float *smax = reinterpret_cast<float *>(smem + C::SMAX);  // [2][BM]
 #pragma unroll
@@ -404,9 +459,8 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
                 const int rr = q * 16 + (lane >> 2), chunk = lane & 3;
                 const u32x4 v = *reinterpret_cast<const u32x4 *>(sc + rr * C::SC_ROW + chunk * 16);
                 const int orow = wm * C::WTM + j * 32 + rr;
-                if (orow < t.m_valid && wn * 64 < t.n_valid)
-                    *reinterpret_cast<u32x4 *>((uint8_t *)g.out + (t.r0 + orow) * g.N + t.n0 +
-                                               wn * 64 + chunk * 16) = v;
+                store(v, orow < t.m_valid && wn * 64 < t.n_valid,
+                      (uint32_t)(orow * g.N + wn * 64 + chunk * 16));
             }
             block_end();
         }
@@ -444,9 +498,8 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
                     const int col = wn * 128 + ib * 32 + chunk * (16 / C::ES);
                     const u32x4 v =
                         *reinterpret_cast<const u32x4 *>(sc + rr * C::SC_ROW + chunk * 16);
-                    if (row < t.m_valid && col < t.n_valid)
-                        *reinterpret_cast<u32x4 *>((char *)g.out +
-                                                   ((t.r0 + row) * g.N + t.n0 + col) * C::ES) = v;
+                    store(v, row < t.m_valid && col < t.n_valid,
+                          (uint32_t)(row * g.N + col) * C::ES);
                 }
                 block_end();
             }
@@ -465,17 +518,25 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
     L t(g, walk, smem);
     t.l_tau = slot;
     t.request_idx(slot, 0);
-    t.landed();
+    t.template landed<0>();
     t.bind();
     t.request_idx(slot + t.G, 1);
     t.request_pair();
-    t.landed();  // (a tile of one pair: the next one's indices)
+    t.template landed<0>();  // (a tile of one pair: the next one's indices)
     t.request_pair();
-    t.landed();
-    typename L::Frags f0, f1;
+    t.template landed<0>();
+    typename L::FragsA a0, a1;
+    typename L::FragsB b0, b1, n1;
 #pragma unroll
-    for (int r = 0; r < 2 * (C::TN + C::TM); ++r) t.read(f0, r, 0);
+    for (int r = 0; r < 2 * C::TN; ++r) t.read_a(a0, r, 0);
+#pragma unroll
+    for (int r = 0; r < 2 * C::TM; ++r) {
+        t.read_b(b0, r, 0);
+        t.read_b(b1, r, 1);
+    }
     t.read_scales(t.sx);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
 
     for (int tau = slot; tau < walk.total; tau += t.G) {
         const Tile tile = walk.tile(g, tau);
@@ -515,20 +576,32 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
 #pragma unroll
             for (int j = 0; j < C::TM; ++j) t.sx[j] = t.sxn[j];
         };
-        const int whole = t.K / C::BK;
-        for (int p = 0; p < whole; ++p) {
+        // b1: the pair's second half's token fragments, n1: the next one's
+        auto pair = [&](int p, typename L::FragsB &b1, typename L::FragsB &n1) {
             const int s0 = w0 & 255, s1 = w1 & 255;
-            t.template body<true>(f0, f1, s0, s1);
+            t.first_half(a0, b0, a1, s0, s1, p == 0 && tau != slot);
             next_scales(p);
-            t.template body<false>(f1, f0, s0, s1);
+            t.second_half(a1, b1, a0, b0, n1, s0, s1);
             next_words(p);
+        };
+        const int whole = t.K / C::BK;
+        int p = 0;
+        for (; p + 1 < whole; p += 2) {
+            pair(p, b1, n1);
+            pair(p + 1, n1, b1);
         }
-        if (whole < t.np) {  // half a pair: its fragments are in registers already
-            t.landed();
+        if (p < whole) {
+            pair(p, b1, n1);
+            b1 = n1;
+        }
+        if (whole < t.np) {  // half a pair
+            t.request_all_x();
+            t.template landed<C::XI>();
             next_scales(whole);
-            t.template body<false>(f0, f1, w0 & 255, w1 & 255);
+            a1 = a0;
+            typename L::FragsB c0 = b0;
+            t.second_half(a1, c0, a0, b0, b1, w0 & 255, w1 & 255);
             next_words(whole);
-            f0 = f1;
         }
         epilogue<MODE, BM_>(g, tile, t, smem);
     }
