@@ -36,10 +36,9 @@ struct ScaledGemm {
     void *out;       // y [.][N], or the SwiGLU launch's e4m3 rows
     uint8_t *out_s;  // their scales
 };
-// Host bounds a launch's form is chosen by: the most rows an expert can have
-// and the rows expected in all.
+// What a launch's form is chosen by: the rows expected in all and the experts
+// expected to have any.
 struct ScaledLoad {
-    int64_t max_rows;
     double rows, active;
 };
 
@@ -48,6 +47,16 @@ hipError_t launch_scaled_gemm(const ScaledGemm &g, int y_type, const ScaledLoad 
                               hipStream_t s);
 // out = Q(silu(x w0^T) * x w1^T).
 hipError_t launch_scaled_swiglu(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s);
+
+// The same for few rows per expert (scaled_stream_fits).  The SwiGLU launch
+// leaves its rows in fp32 (out [.][N], out_s unused); the product behind it
+// takes them so (from_h: x is fp32) and quantises them as it reads them.
+// tiles_n: column tiles of the (first) tiled launch (scaled_tiles).
+bool scaled_stream_fits(int tiles_n, const ScaledLoad &load);
+constexpr int scaled_tiles(bool swiglu, int n) { return (n + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); }
+hipError_t launch_stream_scaled(const ScaledGemm &g, int y_type, bool from_h,
+                                const ScaledLoad &load, hipStream_t s);
+hipError_t launch_stream_swiglu(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s);
 
 // Rows quantised, with (norm) or without the residual addition and RMS norm.
 hipError_t launch_norm_quant(int64_t rows, int cols, const void *x, int x_type,

@@ -33,7 +33,7 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
 // Tile of 256 weight rows x BM token rows, four waves (one per SIMD) in a 2 x 2
 // arrangement, each with a 128 x BM/2 accumulator block of 32 x 32 MFMAs.
 // K advances by pairs of 64 (one MFMA's K, so a pair is a scale block) through
-// two LDS buffers filled by LDS-DMA with whole 128-byte lines of the rows.
+// two or three LDS buffers filled by LDS-DMA with whole 128-byte lines of the rows.
 // ---------------------------------------------------------------------------
 template <int MODE, int BM_>
 struct Cfg {
@@ -41,7 +41,7 @@ struct Cfg {
     static constexpr int BN = 256;                            // weight rows of the tile
     static constexpr int BNOUT = MODE == SWIGLU ? 128 : 256;  // output columns
     static constexpr int THREADS = 256;
-    static constexpr int BK = 128, NS = 2;  // bytes of a row per pair, LDS buffers
+    static constexpr int BK = 128, NS = BM_ >= 128 ? 2 : 3;  // bytes of a row per pair, LDS buffers
     static constexpr int WTN = 128, WTM = BM / 2;
     static constexpr int TN = WTN / 32, TM = WTM / 32;
     static constexpr int WI = BN / 8 / 4, XI = BM / 8 / 4;  // LDS-DMA requests per wave and pair
@@ -218,10 +218,13 @@ struct TileLoop {
         }
         l_kp = 0;
     }
+    __device__ __forceinline__ static int next(int slot) {
+        return slot == C::NS - 1 ? 0 : slot + 1;
+    }
     // Behind a pair's requests: the next tile's first pair follows the last one
     // (behind the last tile: its last pair again, which nothing reads).
     __device__ __forceinline__ void advance() {
-        l_slot ^= 1;
+        l_slot = next(l_slot);
         if (++l_kp < np) return;
         if (l_tau + G >= walk.total) {
             l_kp = np - 1;
@@ -229,6 +232,7 @@ struct TileLoop {
         }
         l_tau += G;
         l_idx ^= 1;
+        if (np < C::NS - 1 && g.row_map) landed<0>();  // its indices may be on their way
         bind();
         request_idx(l_tau + G, l_idx ^ 1);
     }
@@ -313,6 +317,8 @@ struct TileLoop {
             for (int j = 0; j < C::TM; ++j) asm volatile("" : "+a"(acc[i][j]));
     }
     static constexpr int NM = C::TN * C::TM;
+    // requests younger than the next pair's once a pair's token rows are requested
+    static constexpr int AHEAD = C::XI + (C::NS - 2) * C::LPS;
     static constexpr int RM = NM * 3 / 4;  // reads go behind the first three quarters
     // N of something spread evenly behind the first M of a half's MFMAs
     template <int N, int M, class F>
@@ -323,7 +329,7 @@ struct TileLoop {
     }
 
     // The first half of a pair.  The token rows of its buffer are in registers
-    // (both halves' fragments), so those of the pair after the next are
+    // (both halves' fragments), so those of the pair NS ahead are
     // requested into it; the other half's weight fragments are read.  Behind
     // it no wave needs the pair's buffer, and the next pair has landed for
     // every wave.  stored: the epilogue's stores, younger than that pair's
@@ -343,19 +349,19 @@ struct TileLoop {
         sums_used();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (stored)
-            wait_vmcnt<(C::XI + C::STORES < 63 ? C::XI + C::STORES : 63)>();
+            wait_vmcnt<(AHEAD + C::STORES < 63 ? AHEAD + C::STORES : 63)>();
         else
-            wait_vmcnt<C::XI>();
+            wait_vmcnt<AHEAD>();
         __builtin_amdgcn_s_barrier();
     }
-    // The second half: the weights of the pair after the next are requested,
+    // The second half: the weights of the pair NS ahead are requested,
     // and the next pair's token fragments read for both halves (b, b2) and its
     // weights' for the first (a).  Behind it every wave has its token rows.
     __device__ __forceinline__ void second_half(const FragsA &ca, const FragsB &cb, FragsA &a,
                                                 FragsB &b, FragsB &b2, int sw0, int sw1) {
         uint32_t b0, b1;
         backs(b0, b1);
-        c_slot ^= 1;
+        c_slot = next(c_slot);
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
             mfma(ca, cb, m, sw0, sw1);
@@ -521,10 +527,12 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
     t.template landed<0>();
     t.bind();
     t.request_idx(slot + t.G, 1);
-    t.request_pair();
-    t.template landed<0>();  // (a tile of one pair: the next one's indices)
-    t.request_pair();
-    t.template landed<0>();
+#pragma unroll
+    for (int i = 0; i < C::NS; ++i) {
+        t.request_pair();
+        // (a tile of few pairs: the next one's indices)
+        if (i == C::NS - 1 || (g.row_map && t.np < C::NS)) t.template landed<0>();
+    }
     typename L::FragsA a0, a1;
     typename L::FragsB b0, b1, n1;
 #pragma unroll
@@ -596,7 +604,7 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
         }
         if (whole < t.np) {  // half a pair
             t.request_all_x();
-            t.template landed<C::XI>();
+            t.template landed<L::AHEAD>();
             next_scales(whole);
             a1 = a0;
             typename L::FragsB c0 = b0;
@@ -613,6 +621,8 @@ hipError_t go(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
     const unsigned grid = (unsigned)std::max(NXCD, device_cu_count() / NXCD * NXCD);
     if (load.rows / load.active > 128)
         tile_kernel<MODE, 256><<<grid, 256, 0, s>>>(g);
+    else if (load.rows / load.active <= 64)
+        tile_kernel<MODE, 64><<<grid, 256, 0, s>>>(g);
     else
         tile_kernel<MODE, 128><<<grid, 256, 0, s>>>(g);
     return hipGetLastError();

@@ -55,26 +55,37 @@ moe_status check_group(const char *fn, const moe_dims *d, int32_t e_first, int32
     return MOE_OK;
 }
 
-// The load a launch over these experts can expect under uniform routing.
-ScaledLoad expected_load(const moe_dims &d, int e_count) {
+// The load of the local experts under uniform routing.  It picks the form of a
+// launch, over whatever range of them, so that a range has the bits of the
+// whole.
+ScaledLoad expected_load(const moe_dims &d) {
     ScaledLoad l;
     const double p = (double)d.top_k / d.experts;
-    l.max_rows = d.tokens;
-    l.rows = (double)d.tokens * p * e_count;
-    l.active = e_count * (1.0 - std::pow(1.0 - p, (double)d.tokens));
+    l.rows = (double)d.tokens * p * d.local_count;
+    l.active = d.local_count * (1.0 - std::pow(1.0 - p, (double)d.tokens));
     return l;
 }
 
+hipError_t product(const ScaledGemm &g, int y_type, const ScaledLoad &load, hipStream_t s) {
+    return scaled_stream_fits(scaled_tiles(false, g.N), load)
+               ? launch_stream_scaled(g, y_type, false, load, s)
+               : launch_scaled_gemm(g, y_type, load, s);
+}
+
+// The SwiGLU rows between the two products: quantised, or fp32 where the
+// launches of few rows run.
 struct FfnWs {
+    bool stream;
     size_t act, act_s, total;
 };
 FfnWs ffn_ws(const moe_dims *d) {
     FfnWs w;
     auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
     const size_t rows = (size_t)row_cap(d);
+    w.stream = rows > 0 && scaled_stream_fits(scaled_tiles(true, d->inter), expected_load(*d));
     w.act = 0;
-    w.act_s = up(rows * d->inter);
-    w.total = w.act_s + up(rows * scale_pitch(d->inter));
+    w.act_s = up(rows * d->inter * (w.stream ? sizeof(float) : 1));
+    w.total = w.act_s + (w.stream ? 0 : up(rows * scale_pitch(d->inter)));
     return w;
 }
 
@@ -162,8 +173,7 @@ moe_status moe_gemm_scaled(int64_t rows, int32_t n, int32_t k, const moe_e4m3 *x
     g.w0 = w, g.s0 = w_scales;
     g.N = n, g.K = k;
     g.out = y;
-    MOE_HIP(launch_scaled_gemm(g, y_type, ScaledLoad{rows, (double)rows, 1.0},
-                               (hipStream_t)stream));
+    MOE_HIP(product(g, y_type, ScaledLoad{(double)rows, 1.0}, (hipStream_t)stream));
     return MOE_OK;
 }
 
@@ -190,7 +200,7 @@ moe_status moe_gemm_group_scaled(const moe_dims *dims, int32_t e_first, int32_t 
     g.w0 = w, g.s0 = w_scales;
     g.N = n, g.K = k;
     g.out = y;
-    MOE_HIP(launch_scaled_gemm(g, y_type, expected_load(*dims, e_count), (hipStream_t)stream));
+    MOE_HIP(product(g, y_type, expected_load(*dims), (hipStream_t)stream));
     return MOE_OK;
 }
 
@@ -224,7 +234,7 @@ moe_status moe_ffn_group_scaled(const moe_dims *dims, int32_t e_first, int32_t e
         return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, L.total);
     MOE_TRY(check_tensor(fn, "ws", ws));
     uint8_t *base = (uint8_t *)ws;
-    const ScaledLoad load = expected_load(*dims, e_count);
+    const ScaledLoad load = expected_load(*dims);
     hipStream_t s = (hipStream_t)stream;
     ScaledGemm g{};
     g.offsets = offsets;
@@ -236,7 +246,7 @@ moe_status moe_ffn_group_scaled(const moe_dims *dims, int32_t e_first, int32_t e
     g.w1 = w_up, g.s1 = up_scales;
     g.N = dims->inter, g.K = dims->hidden;
     g.out = base + L.act, g.out_s = base + L.act_s;
-    MOE_HIP(launch_scaled_swiglu(g, load, s));
+    MOE_HIP(L.stream ? launch_stream_swiglu(g, load, s) : launch_scaled_swiglu(g, load, s));
     ScaledGemm h{};
     h.offsets = offsets;
     h.e_first = e_first, h.e_count = e_count;
@@ -245,7 +255,8 @@ moe_status moe_ffn_group_scaled(const moe_dims *dims, int32_t e_first, int32_t e
     h.w0 = w_down, h.s0 = down_scales;
     h.N = dims->hidden, h.K = dims->inter;
     h.out = y_perm;
-    MOE_HIP(launch_scaled_gemm(h, y_type, load, s));
+    MOE_HIP(L.stream ? launch_stream_scaled(h, y_type, true, load, s)
+                     : launch_scaled_gemm(h, y_type, load, s));
     return MOE_OK;
 }
 

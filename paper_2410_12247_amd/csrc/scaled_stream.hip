@@ -1,0 +1,252 @@
+// Block-scaled products of few rows per expert: one pass over the weights,
+// whose stream from memory is what the time goes to.
+#include <algorithm>
+#include <cmath>
+
+#include "scaled.h"
+
+namespace moe {
+namespace {
+
+constexpr int kRawFlags = 0x00020000;     // raw (untyped, unswizzled) buffer
+constexpr uint32_t kRange = 0xFFFFFFF0u;  // its size
+constexpr uint32_t kOutside = 0xFFFFFFF8u;  // an offset that reads as zero
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+enum { SWIGLU = 0, OUT_F32 = 1, OUT_BF16 = 2 };
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void *p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)kRange, kRawFlags);
+}
+// eight e4m3 values as bf16, exactly
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ float silu_mul(float g, float u) {
+    const float e = __builtin_amdgcn_exp2f(g * -1.44269504088896341f);
+    return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
+    const uint16_t ua = __builtin_bit_cast(uint16_t, static_cast<__bf16>(a));
+    const uint16_t ub = __builtin_bit_cast(uint16_t, static_cast<__bf16>(b));
+    return (uint32_t)ua | ((uint32_t)ub << 16);
+}
+
+// The workgroup owns 16 NT weight rows (of each matrix) of one expert over the
+// whole of K; its W waves take blocks of 128 k in turn and keep D of them in
+// flight, loaded straight into registers in the MFMA's operand layout.  The
+// e4m3 values are widened to bf16, where the matrix instruction's products and
+// sums are exact to fp32, and the scales applied to a block's fp32 sums: the
+// stream leaves the compute units idle most of the time, so this costs nothing
+// and the sums are exact to fp32 too.  The waves' sums meet in LDS and are
+// added in wave order.
+// FROM_H: the token rows are fp32 (the SwiGLU launch's) and quantised here,
+// block by block, as they are read.
+template <int MODE, bool FROM_H, int NT, int W, int D>
+__global__ __launch_bounds__(64 * W) void stream_kernel(ScaledGemm g) {
+    constexpr int NM = MODE == SWIGLU ? 2 : 1;  // matrices
+    constexpr int NTT = NT * NM;
+    __shared__ __attribute__((aligned(16))) floatx4 part[W][NTT][64];
+    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int e = blockIdx.y;
+    int row0 = 0, cnt = (int)g.rows_one;
+    if (g.offsets) {
+        row0 = __builtin_amdgcn_readfirstlane(g.offsets[g.e_first + e]);
+        cnt = __builtin_amdgcn_readfirstlane(g.offsets[g.e_first + e + 1]) - row0;
+    }
+    if (cnt <= 0) return;
+    const int K = g.K, SK = scale_pitch(K), nb = scale_blocks(K);
+    const int n0 = blockIdx.x * 16 * NT;
+    const int64_t we = (int64_t)(g.e_first + e) * g.N + n0;
+    const int64_t se = (int64_t)(g.e_first + e) * scale_blocks(g.N) + n0 / kScaleBlock;
+    __amdgpu_buffer_rsrc_t wr[NM], sr[NM];
+    wr[0] = rsrc(g.w0 + we * K);
+    sr[0] = rsrc(g.s0 + se * SK);
+    if (NM == 2) {
+        wr[NM - 1] = rsrc(g.w1 + we * K);
+        sr[NM - 1] = rsrc(g.s1 + se * SK);
+    }
+    uint32_t woff[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+        woff[i] = (uint32_t)(min(i * 16 + col, g.N - 1 - n0) * K + grp * 16);
+
+    for (int m0 = 0; m0 < cnt; m0 += 16) {
+        const uint8_t *xb = g.x;
+        const uint8_t *sb = g.xs;
+        const int64_t first = (int64_t)row0 + m0;
+        if (!g.row_map) {
+            xb += first * K * (FROM_H ? 4 : 1);
+            sb += first * SK;
+        }
+        const __amdgpu_buffer_rsrc_t xr = rsrc(xb), xsr = rsrc(sb);
+        const int r = min(col, cnt - 1 - m0);
+        const uint32_t src =
+            g.row_map ? (uint32_t)(g.row_map[first + r] / g.slot_div) : (uint32_t)r;
+        const uint32_t xoff = (src * (uint32_t)K + grp * 16) * (FROM_H ? 4u : 1u);
+        const uint32_t xsoff = src * (uint32_t)SK;
+        struct Step {
+            u32x4 a[NTT][2];
+            u32x4 b[FROM_H ? 8 : 2];
+            int sw[NM], sx;
+        };
+        // Block kb; nothing (zeros) behind K.  A lane takes 16 values of each
+        // half, so a request reads 64 bytes of a row in one piece.
+        auto load = [&](Step &s, int kb) {
+            const uint32_t k = (uint32_t)kb * kScaleBlock;
+            const bool in[2] = {kb * kScaleBlock < K, kb * kScaleBlock + 64 < K};
+#pragma unroll
+            for (int m = 0; m < NM; ++m) {
+                s.sw[m] = __builtin_amdgcn_raw_buffer_load_b8(sr[m], kb < nb ? kb : kOutside, 0, 0);
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        s.a[m * NT + i][h] = __builtin_bit_cast(
+                            u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                       wr[m], in[h] ? woff[i] + k + h * 64 : kOutside, 0, 0));
+            }
+            if (!FROM_H)
+                s.sx = __builtin_amdgcn_raw_buffer_load_b8(
+                    xsr, kb < nb ? xsoff + kb : kOutside, 0, 0);
+#pragma unroll
+            for (int h = 0; h < (FROM_H ? 8 : 2); ++h) {
+                const uint32_t at = FROM_H ? k * 4 + (h >> 2) * 256 + (h & 3) * 16 : k + h * 64;
+                s.b[h] = __builtin_bit_cast(
+                    u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                               xr, in[FROM_H ? h >> 2 : h] ? xoff + at : kOutside, 0, 0));
+            }
+        };
+        floatx4 acc[NTT];
+#pragma unroll
+        for (int i = 0; i < NTT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        auto compute = [&](const Step &s) {
+            bf16x8 b[4];
+            int ex;
+            if (FROM_H) {
+                float m = 0.f;
+#pragma unroll
+                for (int h = 0; h < 8; ++h)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) m = fmaxf(m, fabsf(__uint_as_float(s.b[h][q])));
+                m = fmaxf(m, __shfl_xor(m, 16));
+                m = fmaxf(m, __shfl_xor(m, 32));
+                ex = scale_exponent(m);
+                const float inv = scale_inverse(ex);
+                auto pack = [&](const u32x4 &v) {
+                    return pack_e4m3(__uint_as_float(v[0]), __uint_as_float(v[1]),
+                                     __uint_as_float(v[2]), __uint_as_float(v[3]), inv);
+                };
+#pragma unroll
+                for (int h = 0; h < 4; ++h) b[h] = widen(pack(s.b[2 * h]), pack(s.b[2 * h + 1]));
+            } else {
+                ex = s.sx - 127;
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    b[h] = widen(s.b[h >> 1][2 * (h & 1)], s.b[h >> 1][2 * (h & 1) + 1]);
+            }
+#pragma unroll
+            for (int i = 0; i < NTT; ++i) {
+                const int sw = s.sw[i / NT];
+                floatx4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        widen(s.a[i][h >> 1][2 * (h & 1)], s.a[i][h >> 1][2 * (h & 1) + 1]), b[h],
+                        p, 0, 0, 0);
+                // (scale byte 255 is NaN)
+                const float nan = sw == 255 || ex == 128 ? __builtin_nanf("") : 0.f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    acc[i][r] += __builtin_amdgcn_ldexpf(p[r] + nan, ex + sw - 127);
+            }
+        };
+        Step s[D];
+#pragma unroll
+        for (int d = 0; d < D; ++d) load(s[d], wave + W * d);
+        for (int kb = wave; kb < nb; kb += W * D) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                compute(s[d]);
+                load(s[d], kb + W * (d + D));
+            }
+        }
+        // The lane holds weight rows 4 (lane / 16) + r of token row lane % 16.
+#pragma unroll
+        for (int i = 0; i < NTT; ++i) part[wave][i][lane] = acc[i];
+        __syncthreads();
+        for (int i = wave; i < NT; i += W) {
+            floatx4 v = part[0][i][lane], u = NM == 2 ? part[0][NT * (NM - 1) + i][lane] : v;
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                v += part[w][i][lane];
+                if (NM == 2) u += part[w][NT * (NM - 1) + i][lane];
+            }
+            const int r = m0 + col, n = n0 + i * 16 + grp * 4;
+            if (r >= cnt || n >= g.N) continue;
+            const int64_t at = ((int64_t)row0 + r) * g.N + n;
+            if (MODE == SWIGLU) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] = silu_mul(v[x], u[x]);
+            }
+            if (MODE == OUT_BF16) {
+                uint2 p;
+                p.x = pack_bf16x2(v[0], v[1]);
+                p.y = pack_bf16x2(v[2], v[3]);
+                *reinterpret_cast<uint2 *>((bf16_t *)g.out + at) = p;
+            } else {
+                *reinterpret_cast<floatx4 *>((float *)g.out + at) = v;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <int MODE, bool FROM_H, int NT, int W, int D>
+hipError_t go(const ScaledGemm &g, hipStream_t s) {
+    const dim3 grid((unsigned)((g.N + 16 * NT - 1) / (16 * NT)), (unsigned)g.e_count);
+    stream_kernel<MODE, FROM_H, NT, W, D><<<grid, 64 * W, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+template <int MODE, bool FROM_H>
+hipError_t go_out(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
+    // Few blocks of K: four waves, so that each has several.
+    if (FROM_H)
+        return scale_blocks(g.K) <= 16 ? go<MODE, true, 2, 4, 2>(g, s)
+                                       : go<MODE, true, 2, 8, 2>(g, s);
+    // Two weight tiles per wave share the token rows' loads and widening, where
+    // that leaves more than half of the compute units a workgroup.
+    return g.N / 32 * load.active > device_cu_count() / 2
+               ? go<MODE, false, 2, 8, 2>(g, s)
+               : go<MODE, false, 1, 8, 2>(g, s);
+}
+
+}  // namespace
+
+// Up to 16 rows per expert a weight is read once; below half a tile per compute
+// unit the tiled launch leaves most of the chip idle.  Tiled -> this, us: FFN of
+// one token 4096 x 3584 (two experts, 56 tiles) 62 -> 26, 6144 x 1344 (four, 44)
+// 64 -> 33, eight tokens 5120 x 1536 (63) 60 -> 34; four tokens 6144 x 1344 (120
+// tiles) 81 and 81, 61 tokens 5120 x 1536 (216) 94 -> 105.
+bool scaled_stream_fits(int tiles_n, const ScaledLoad &load) {
+    return load.rows <= 16 * load.active && 2 * tiles_n * load.active < device_cu_count();
+}
+
+hipError_t launch_stream_scaled(const ScaledGemm &g, int y_type, bool from_h,
+                                const ScaledLoad &load, hipStream_t s) {
+    if (y_type == MOE_FP32)
+        return from_h ? go_out<OUT_F32, true>(g, load, s) : go_out<OUT_F32, false>(g, load, s);
+    return from_h ? go_out<OUT_BF16, true>(g, load, s) : go_out<OUT_BF16, false>(g, load, s);
+}
+hipError_t launch_stream_swiglu(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
+    return go<SWIGLU, false, 2, 8, 2>(g, s);
+}
+
+}  // namespace moe
