@@ -300,24 +300,47 @@ _I32 = (torch.int32,)
 _BF16 = (torch.bfloat16,)
 
 
+# (Small batches take a few microseconds on the GPU: these checks are kept to
+# tenths of one per tensor, and the stream is asked for without making a Stream
+# object, which takes 3.)
+
 def _real(name, t):
     """The element type's code."""
-    if t.dtype not in _REAL:
+    code = _REAL.get(t.dtype)
+    if code is None:
         raise ValueError(f"{name} must be bfloat16 or float32, not {t.dtype}")
-    return _REAL[t.dtype]
+    return code
 
 
-def _arg(name, t, dtypes, shape):
-    """The address of a contiguous tensor of the current device with one of
-    the dtypes and the shape, or None for None."""
+def _dev(name, t):
+    """The current device, which t has to be on."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a contiguous device tensor, not on {t.device}")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    return dev
+
+
+def _arg(dev, name, t, dtypes, shape):
+    """The address of a contiguous tensor on dev with one of the dtypes and the
+    shape, or None for None."""
     if t is None:
         return None
-    if t.dtype not in dtypes or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+    if t.get_device() != dev or t.dtype not in dtypes or t.shape != shape or \
+            not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous device tensor of shape {tuple(shape)} and "
-                         f"type {dtypes[0]}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
+                         f"type {dtypes[0]} on cuda:{dev}, not {tuple(t.shape)} of {t.dtype} on "
+                         f"{t.device}")
     return t.data_ptr()
+
+
+def _stream_on(dev, stream):
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"the stream is on cuda:{stream.device_index}, the tensors on cuda:{dev}")
+    return stream.cuda_stream
 
 
 def _rows(name, t, cols=None):
@@ -341,65 +364,73 @@ def _pitch(k):
 
 def quant_rows(x, q, scales, stream=None):
     """q, scales = Q(x): one scale per row and 128 columns."""
-    R, C = _rows("x", x)
-    _check(lib().moe_quant_rows(R, C, _arg("x", x, (x.dtype,), x.shape), _real("x", x),
-                                _arg("q", q, _E4M3, x.shape),
-                                _arg("scales", scales, _SCALE, (R, _pitch(C))), _s(stream)))
+    shape = R, C = _rows("x", x)
+    dev, code = _dev("x", x), _real("x", x)
+    _check(lib().moe_quant_rows(R, C, _arg(dev, "x", x, (x.dtype,), shape), code,
+                                _arg(dev, "q", q, _E4M3, shape),
+                                _arg(dev, "scales", scales, _SCALE, (R, _pitch(C))),
+                                _stream_on(dev, stream)))
 
 
 def quant_weights(w, q, scales, stream=None):
     """q, scales = Q(w) in 128 x 128 blocks; w [n, k] or [experts, n, k] bf16."""
     if w.dim() not in (2, 3):
         raise ValueError("w must be [n, k] or [experts, n, k]")
-    lead, (n, k) = w.shape[:-2], w.shape[-2:]
-    _check(lib().moe_quant_weights(lead[0] if lead else 1, n, k, _arg("w", w, _BF16, w.shape),
-                                   _arg("q", q, _E4M3, w.shape),
-                                   _arg("scales", scales, _SCALE,
-                                        lead + (-(-n // 128), _pitch(k))), _s(stream)))
+    lead, (n, k), dev = w.shape[:-2], w.shape[-2:], _dev("w", w)
+    _check(lib().moe_quant_weights(lead[0] if lead else 1, n, k,
+                                   _arg(dev, "w", w, _BF16, w.shape),
+                                   _arg(dev, "q", q, _E4M3, w.shape),
+                                   _arg(dev, "scales", scales, _SCALE,
+                                        lead + (-(-n // 128), _pitch(k))),
+                                   _stream_on(dev, stream)))
 
 
 def norm_quant(x, residual, weight, eps, total, y, q, scales, stream=None):
     """total = bf16(x + residual), y = bf16(v) and q, scales = Q(v) for the
     RMS-normalised rows v = norm(x + residual) * weight.  residual, weight,
     total, y and the pair q, scales may be None."""
-    shape = _rows("x", x)
-    R, H = shape
-    _check(lib().moe_norm_quant(R, H, _arg("x", x, (x.dtype,), shape), _real("x", x),
-                                _arg("residual", residual, _BF16, shape),
-                                _arg("weight", weight, _BF16, (H,)), eps,
-                                _arg("total", total, _BF16, shape), _arg("y", y, _BF16, shape),
-                                _arg("q", q, _E4M3, shape),
-                                _arg("scales", scales, _SCALE, (R, _pitch(H))), _s(stream)))
+    shape = R, H = _rows("x", x)
+    dev, code = _dev("x", x), _real("x", x)
+    _check(lib().moe_norm_quant(R, H, _arg(dev, "x", x, (x.dtype,), shape), code,
+                                _arg(dev, "residual", residual, _BF16, shape),
+                                _arg(dev, "weight", weight, _BF16, (H,)), eps,
+                                _arg(dev, "total", total, _BF16, shape),
+                                _arg(dev, "y", y, _BF16, shape), _arg(dev, "q", q, _E4M3, shape),
+                                _arg(dev, "scales", scales, _SCALE, (R, _pitch(H))),
+                                _stream_on(dev, stream)))
 
 
 def gemm_scaled(x, x_scales, w, w_scales, y, stream=None):
     """y = x w^T over block-scaled x [rows, k] and w [n, k]; y bf16 or fp32."""
     R, K = _rows("x", x)
     N, _ = _rows("w", w, K)
-    _check(lib().moe_gemm_scaled(R, N, K, _arg("x", x, _E4M3, (R, K)),
-                                 _arg("x_scales", x_scales, _SCALE, (R, _pitch(K))),
-                                 _arg("w", w, _E4M3, (N, K)),
-                                 _arg("w_scales", w_scales, _SCALE, (-(-N // 128), _pitch(K))),
-                                 _arg("y", y, (y.dtype,), (R, N)), _real("y", y), _s(stream)))
+    dev, code, P = _dev("x", x), _real("y", y), _pitch(K)
+    _check(lib().moe_gemm_scaled(R, N, K, _arg(dev, "x", x, _E4M3, (R, K)),
+                                 _arg(dev, "x_scales", x_scales, _SCALE, (R, P)),
+                                 _arg(dev, "w", w, _E4M3, (N, K)),
+                                 _arg(dev, "w_scales", w_scales, _SCALE, (-(-N // 128), P)),
+                                 _arg(dev, "y", y, (y.dtype,), (R, N)), code,
+                                 _stream_on(dev, stream)))
 
 
 def _row_cap(d):
     return d.tokens * min(d.top_k, d.local_count)
 
 
-def _group_args(d, offsets, sorted_slot, x, x_scales, k):
+def _group_args(dev, d, offsets, sorted_slot, x, x_scales, k):
     """Addresses of what the grouped calls share; x holds the tokens' rows
     with sorted_slot, else the dispatched rows."""
     cap = _row_cap(d)
     rows = d.tokens if sorted_slot is not None else cap
-    return (_arg("offsets", offsets, _I32, (d.local_count + 1,)),
-            _arg("sorted_slot", sorted_slot, _I32, (cap,)), _arg("x", x, _E4M3, (rows, k)),
-            _arg("x_scales", x_scales, _SCALE, (rows, _pitch(k))))
+    return (_arg(dev, "offsets", offsets, _I32, (d.local_count + 1,)),
+            _arg(dev, "sorted_slot", sorted_slot, _I32, (cap,)),
+            _arg(dev, "x", x, _E4M3, (rows, k)),
+            _arg(dev, "x_scales", x_scales, _SCALE, (rows, _pitch(k))))
 
 
-def _stack(name, d, w, s, n, k):
-    return (_arg(name, w, _E4M3, (d.local_count, n, k)),
-            _arg(name + " scales", s, _SCALE, (d.local_count, -(-n // 128), _pitch(k))))
+def _stack(dev, name, d, w, s, n, k):
+    return (_arg(dev, name, w, _E4M3, (d.local_count, n, k)),
+            _arg(dev, name + " scales", s, _SCALE, (d.local_count, -(-n // 128), _pitch(k))))
 
 
 def gemm_group_scaled(d, e_first, e_count, offsets, sorted_slot, x, x_scales, w, w_scales, y,
@@ -409,11 +440,13 @@ def gemm_group_scaled(d, e_first, e_count, offsets, sorted_slot, x, x_scales, w,
     if w.dim() != 3:
         raise ValueError("w must be [local_count, n, k]")
     N, K = w.shape[1:]
-    off, slot, xp, xsp = _group_args(d, offsets, sorted_slot, x, x_scales, K)
-    wp, wsp = _stack("w", d, w, w_scales, N, K)
+    dev, code = _dev("x", x), _real("y", y)
+    off, slot, xp, xsp = _group_args(dev, d, offsets, sorted_slot, x, x_scales, K)
+    wp, wsp = _stack(dev, "w", d, w, w_scales, N, K)
     _check(lib().moe_gemm_group_scaled(ctypes.byref(d), e_first, e_count, off, slot, N, K, xp,
-                                       xsp, wp, wsp, _arg("y", y, (y.dtype,), (_row_cap(d), N)),
-                                       _real("y", y), _s(stream)))
+                                       xsp, wp, wsp,
+                                       _arg(dev, "y", y, (y.dtype,), (_row_cap(d), N)), code,
+                                       _stream_on(dev, stream)))
 
 
 def scaled_workspace_bytes(d: Dims) -> int:
@@ -425,14 +458,16 @@ def ffn_group_scaled(d, e_first, e_count, offsets, sorted_slot, x, x_scales, w_g
     """The experts' SwiGLU FFN in 8 bits; y_perm bf16 or fp32, ws of
     scaled_workspace_bytes(d) bytes."""
     H, I = d.hidden, d.inter
-    off, slot, xp, xsp = _group_args(d, offsets, sorted_slot, x, x_scales, H)
+    dev, code = _dev("x", x), _real("y_perm", y_perm)
+    off, slot, xp, xsp = _group_args(dev, d, offsets, sorted_slot, x, x_scales, H)
     _check(lib().moe_ffn_group_scaled(
         ctypes.byref(d), e_first, e_count, off, slot, xp, xsp,
-        *_stack("w_gate", d, w_gate, gate_scales, I, H),
-        *_stack("w_up", d, w_up, up_scales, I, H),
-        *_stack("w_down", d, w_down, down_scales, H, I),
-        _arg("y_perm", y_perm, (y_perm.dtype,), (_row_cap(d), H)), _real("y_perm", y_perm),
-        _arg("ws", ws, (ws.dtype,), ws.shape), ws.numel() * ws.element_size(), _s(stream)))
+        *_stack(dev, "w_gate", d, w_gate, gate_scales, I, H),
+        *_stack(dev, "w_up", d, w_up, up_scales, I, H),
+        *_stack(dev, "w_down", d, w_down, down_scales, H, I),
+        _arg(dev, "y_perm", y_perm, (y_perm.dtype,), (_row_cap(d), H)), code,
+        _arg(dev, "ws", ws, (ws.dtype,), ws.shape), ws.numel() * ws.element_size(),
+        _stream_on(dev, stream)))
 
 
 class MoEBuffers:
