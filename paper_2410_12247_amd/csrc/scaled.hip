@@ -31,7 +31,9 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
 
 // ---------------------------------------------------------------------------
 // Tile of 256 weight rows x BM token rows, four waves (one per SIMD) in a 2 x 2
-// arrangement, each with a 128 x BM/2 accumulator block of 32 x 32 MFMAs.
+// arrangement, each with a 128 x BM/2 accumulator block of 32 x 32 MFMAs (the
+// blocks' token rows alternate by 32, so a tile of few rows keeps all waves
+// busy).
 // K advances by pairs of 64 (one MFMA's K, so a pair is a scale block) through
 // two or three LDS buffers filled by LDS-DMA with whole 128-byte lines of the rows.
 // ---------------------------------------------------------------------------
@@ -61,7 +63,7 @@ struct Cfg {
     static constexpr int STORES = MODE == SWIGLU ? 2 * TM : TN * TM * (ES == 4 ? 4 : 2);
     static constexpr int SMAX = SCRATCH + 4 * SC_WAVE;
     static constexpr int INTS = SMAX + (MODE == SWIGLU ? 2 * BM * 4 : 0);
-    static constexpr int LDS_BYTES = INTS + 2 * (kMaxExperts + 1) * 4;
+    static constexpr int LDS_BYTES = INTS + 3 * (kMaxExperts + 1) * 4;
     static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
 };
 
@@ -71,46 +73,86 @@ struct Tile {
     int m_valid, n_valid;
 };
 
-// Walks the tiles of all experts; s_off, s_pre: e_count + 1 ints each in LDS.
-template <class C>
+// The tiles of all experts, BM token rows high.  TAIL: in launches of at least
+// four tile rows per expert, an expert's last rows, where they fill at most half
+// a tile, are no tile of it but a tail; the tails run behind the tiles, as tiles
+// of half the height and a fraction of the time, and are dealt out from the first
+// workgroup that the tiles' last round leaves without one.  So the last round
+// is a short one instead of a whole one: DBRX gate of 8192 tokens (768 tiles, 54
+// tails, 256 workgroups) 288 -> 275 us.  With fewer tile rows reading the weights
+// again costs more than it saves: DeepSeekV2 FFN of 8192 tokens (a tile and a
+// tail per expert) 241 -> 256.
+template <class C, bool TAIL>
 struct Walk {
-    int *s_off, *s_pre;
-    int NT, total;
+    int *s_off, *s_tile, *s_tail;  // e_count + 1 ints each in LDS
+    int NT, tiles, tails, least;  // least: a last row of tiles has more rows than this
+    __device__ __forceinline__ int tile_rows(int cnt) const {
+        return cnt / C::BM + (cnt % C::BM > least);
+    }
     __device__ __forceinline__ Walk(const ScaledGemm &g, int *lds) {
         s_off = lds;
-        s_pre = lds + kMaxExperts + 1;
+        s_tile = lds + kMaxExperts + 1;
+        s_tail = lds + 2 * (kMaxExperts + 1);
         NT = (g.N + C::BNOUT - 1) / C::BNOUT;
-        const int tid = threadIdx.x;
+        least = TAIL ? C::BM / 2 : 0;
+        const int tid = threadIdx.x, lane = tid & 63;
         for (int i = tid; i <= g.e_count; i += C::THREADS)
             s_off[i] = g.offsets ? g.offsets[g.e_first + i] : (i == 0 ? 0 : (int)g.rows_one);
         __syncthreads();
-        if (tid == 0) {
-            int t = 0;
-            for (int e = 0; e < g.e_count; ++e) {
-                s_pre[e] = t;
-                t += (s_off[e + 1] - s_off[e] + C::BM - 1) / C::BM * NT;
-            }
-            s_pre[g.e_count] = t;
+        // inclusive prefix sums over the experts, one per thread
+        int f = 0, h = 0;
+        if (tid < g.e_count) {
+            const int cnt = s_off[tid + 1] - s_off[tid];
+            const int n = tile_rows(cnt);
+            f = n * NT;
+            h = ((cnt + C::BM - 1) / C::BM - n) * NT;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int uf = __shfl_up(f, d), uh = __shfl_up(h, d);
+            if (lane >= d) f += uf, h += uh;
+        }
+        s_tile[tid + 1] = f;
+        s_tail[tid + 1] = h;
+        if (tid == 0) s_tile[0] = s_tail[0] = 0;
+        if (g.e_count > 64) {
+            __syncthreads();
+            for (int w = 64; w <= tid - lane; w += 64) f += s_tile[w], h += s_tail[w];
+            __syncthreads();
+            s_tile[tid + 1] = f;
+            s_tail[tid + 1] = h;
         }
         __syncthreads();
-        total = __builtin_amdgcn_readfirstlane(s_pre[g.e_count]);
+        tiles = __builtin_amdgcn_readfirstlane(s_tile[g.e_count]);
+        tails = __builtin_amdgcn_readfirstlane(s_tail[g.e_count]);
+        if (TAIL && tails > 0 && tiles < 4 * NT * g.e_count) {  // tiles like the others
+            __syncthreads();
+            s_tile[tid + 1] += s_tail[tid + 1];
+            tiles += tails;
+            tails = 0;
+            least = 0;
+            __syncthreads();
+        }
     }
-    __device__ __forceinline__ Tile tile(const ScaledGemm &g, int tau) const {
+    // tile tau of the tiles (tail false) or of the tails
+    __device__ __forceinline__ Tile tile(const ScaledGemm &g, int tau, bool tail) const {
         auto lds = [](const int &v) { return __builtin_amdgcn_readfirstlane(v); };
-        int lo = 0, hi = g.e_count - 1;
+        const int *pre = tail ? s_tail : s_tile;
+        int lo = 0, hi = g.e_count - 1;  // the last expert with pre[e] <= tau
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (lds(s_pre[mid]) <= tau) lo = mid; else hi = mid - 1;
+            if (lds(pre[mid]) <= tau) lo = mid; else hi = mid - 1;
         }
         const int row0 = lds(s_off[lo]);
         const int cnt = lds(s_off[lo + 1]) - row0;
-        const int MT = (cnt + C::BM - 1) / C::BM;
-        const int r = tau - lds(s_pre[lo]);
-        const int per_sc = GROUP_N * MT;
-        const int sc = r / per_sc;
-        const int q = r - sc * per_sc;
-        const int width = min(GROUP_N, NT - sc * GROUP_N);
-        const int mt = q / width, nt = sc * GROUP_N + (q - mt * width);
+        int mt = cnt / C::BM, nt = tau - lds(pre[lo]);
+        if (!tail) {
+            const int MT = tile_rows(cnt), per_sc = GROUP_N * MT;
+            const int sc = nt / per_sc, q = nt - sc * per_sc;
+            const int width = min(GROUP_N, NT - sc * GROUP_N);
+            mt = q / width;
+            nt = sc * GROUP_N + (q - mt * width);
+        }
         Tile t;
         t.e = lo;
         t.r0 = (int64_t)row0 + (int64_t)mt * C::BM;
@@ -128,7 +170,8 @@ __device__ __forceinline__ void wait_vmcnt() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <int MODE, int BM_>
+// TAIL: the tiles are the walk's tails.
+template <int MODE, int BM_, bool TAIL, class W>
 struct TileLoop {
     using C = Cfg<MODE, BM_>;
     struct FragsA {
@@ -139,8 +182,9 @@ struct TileLoop {
     };
 
     const ScaledGemm &g;
-    const Walk<C> &walk;
+    const W &walk;
     char *smem;
+    const int total;
     uint32_t lds0;
     int lane, wave, wn, wm, K, SK, np, G;
 
@@ -154,8 +198,8 @@ struct TileLoop {
     floatx16 acc[C::TN][C::TM];
     int sx[C::TM], sxn[C::TM];
 
-    __device__ __forceinline__ TileLoop(const ScaledGemm &g_, const Walk<C> &w_, char *sm)
-        : g(g_), walk(w_), smem(sm) {
+    __device__ __forceinline__ TileLoop(const ScaledGemm &g_, const W &w_, char *sm)
+        : g(g_), walk(w_), smem(sm), total(TAIL ? w_.tails : w_.tiles) {
         lds0 = (uint32_t)(uintptr_t)(lds_void_t *)sm;
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -169,8 +213,8 @@ struct TileLoop {
     // The row indices of tile tau, one request per wave (behind the last row:
     // the last one's).
     __device__ __forceinline__ void request_idx(int tau, int which) {
-        if (!g.row_map || tau >= walk.total) return;
-        const Tile t = walk.tile(g, tau);
+        if (!g.row_map || tau >= total) return;
+        const Tile t = walk.tile(g, tau, TAIL);
         const uint32_t r = (uint32_t)min(wave * 64 + lane, t.m_valid - 1) * 4u;
         buf4_to_lds(buf_rsrc(g.row_map + t.r0), r, 0,
                     lds0 + C::IDX + which * 1024 + wave * 256);
@@ -180,7 +224,7 @@ struct TileLoop {
     // the 16-byte chunks of LDS row r are stored at chunk ^ (r / 2 % 8), so
     // the 16 lanes of a fragment read that are served together find all banks.
     __device__ __forceinline__ void bind() {
-        const Tile t = walk.tile(g, l_tau);
+        const Tile t = walk.tile(g, l_tau, TAIL);
         const int64_t we = (int64_t)(g.e_first + t.e) * g.N + t.n0;
         const bool up = MODE == SWIGLU && wave >= 2;
         const int wrow0 = MODE == SWIGLU ? (wave & 1) * 64 : wave * 64;
@@ -226,7 +270,7 @@ struct TileLoop {
     __device__ __forceinline__ void advance() {
         l_slot = next(l_slot);
         if (++l_kp < np) return;
-        if (l_tau + G >= walk.total) {
+        if (l_tau + G >= total) {
             l_kp = np - 1;
             return;
         }
@@ -274,6 +318,8 @@ struct TileLoop {
         advance();
     }
 
+    // first token row of the wave's fragment j
+    __device__ __forceinline__ int row0(int j) const { return (2 * j + wm) * 32; }
     // 16 bytes (h of 2) of a fragment, half `hf` of the pair in c_slot
     __device__ __forceinline__ u32x4 read(int lds_row, int h, int hf) const {
         const int row = lane & 31;
@@ -288,41 +334,45 @@ struct TileLoop {
         f.v[i][r & 1] = read(w0, r & 1, hf);
     }
     __device__ __forceinline__ void read_b(FragsB &f, int r, int hf) const {
-        f.v[r >> 1][r & 1] = read(C::BN + wm * C::WTM + (r >> 1) * 32, r & 1, hf);
+        f.v[r >> 1][r & 1] = read(C::BN + row0(r >> 1), r & 1, hf);
     }
     __device__ __forceinline__ void read_scales(int (&s)[C::TM]) {
         const uint8_t *p = reinterpret_cast<const uint8_t *>(smem) + C::SCALES +
                            c_group * 1024 + c_byte;
 #pragma unroll
-        for (int j = 0; j < C::TM; ++j) s[j] = p[(wm * C::WTM + j * 32 + (lane & 31)) * 4];
+        for (int j = 0; j < C::TM; ++j) s[j] = p[(row0(j) + (lane & 31)) * 4];
     }
     __device__ __forceinline__ static v8i whole(const u32x4 (&v)[2]) {
         return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3],
                    (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
     }
 
-    __device__ __forceinline__ void mfma(const FragsA &a, const FragsB &b, int m, int sw0,
-                                         int sw1) {
-        const int i = m / C::TM, j = m % C::TM;
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-            whole(a.v[i]), whole(b.v[j]), acc[i][j], 0, 0, 0,
-            MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
-    }
-    // (the sums count as used here: the compiler would move their MFMAs behind
-    // the branches that follow, away from the requests and reads)
-    __device__ __forceinline__ void sums_used() {
-#pragma unroll
-        for (int i = 0; i < C::TN; ++i)
-#pragma unroll
-            for (int j = 0; j < C::TM; ++j) asm volatile("" : "+a"(acc[i][j]));
-    }
+    // One half's MFMAs, and between them the parts f(m, n) of its reads and
+    // requests, m of n.  (The sums count as used behind them: the compiler would
+    // move the MFMAs behind branches that follow, away from those.)
     static constexpr int NM = C::TN * C::TM;
+    template <class F>
+    __device__ __forceinline__ void half(const FragsA &a, const FragsB &b, int sw0, int sw1,
+                                         F &&f) {
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            const int i = m / C::TM, j = m % C::TM;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                whole(a.v[i]), whole(b.v[j]), acc[i][j], 0, 0, 0,
+                MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
+            f(m);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int m = 0; m < NM; ++m) asm volatile("" : "+a"(acc[m / C::TM][m % C::TM]));
+    }
     // requests younger than the next pair's once a pair's token rows are requested
     static constexpr int AHEAD = C::XI + (C::NS - 2) * C::LPS;
-    static constexpr int RM = NM * 3 / 4;  // reads go behind the first three quarters
-    // N of something spread evenly behind the first M of a half's MFMAs
-    template <int N, int M, class F>
-    __device__ __forceinline__ static void behind(int m, F &&f) {
+    // Part m of NM of N things; EARLY: all of them in the first three quarters
+    // (the last MFMAs then hide the reads' latency).
+    template <int N, bool EARLY, class F>
+    __device__ __forceinline__ static void part(int m, F &&f) {
+        constexpr int M = EARLY ? NM * 3 / 4 : NM;
         if (m >= M) return;
 #pragma unroll
         for (int q = m * N / M; q < (m + 1) * N / M; ++q) f(q);
@@ -334,19 +384,15 @@ struct TileLoop {
     // it no wave needs the pair's buffer, and the next pair has landed for
     // every wave.  stored: the epilogue's stores, younger than that pair's
     // requests, may still be on their way.
-    __device__ __forceinline__ void first_half(const FragsA &a, const FragsB &b, FragsA &a2,
-                                               int sw0, int sw1, bool stored) {
+    __device__ __forceinline__ void first_half(const FragsA &a, const FragsB &b,
+                                               FragsA &a2, int sw0, int sw1, bool stored) {
         request_scales();
         uint32_t b0, b1;
         backs(b0, b1);
-#pragma unroll
-        for (int m = 0; m < NM; ++m) {
-            mfma(a, b, m, sw0, sw1);
-            behind<2 * C::TN, RM>(m, [&](int r) { read_a(a2, r, 1); });
-            behind<C::XI, NM>(m, [&](int q) { request_x(q, b0, b1); });
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        sums_used();
+        half(a, b, sw0, sw1, [&](int m) {
+            part<2 * C::TN, true>(m, [&](int r) { read_a(a2, r, 1); });
+            part<C::XI, false>(m, [&](int q) { request_x(q, b0, b1); });
+        });
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (stored)
             wait_vmcnt<(AHEAD + C::STORES < 63 ? AHEAD + C::STORES : 63)>();
@@ -357,24 +403,21 @@ struct TileLoop {
     // The second half: the weights of the pair NS ahead are requested,
     // and the next pair's token fragments read for both halves (b, b2) and its
     // weights' for the first (a).  Behind it every wave has its token rows.
-    __device__ __forceinline__ void second_half(const FragsA &ca, const FragsB &cb, FragsA &a,
-                                                FragsB &b, FragsB &b2, int sw0, int sw1) {
+    __device__ __forceinline__ void second_half(const FragsA &ca, const FragsB &cb,
+                                                FragsA &a, FragsB &b, FragsB &b2, int sw0,
+                                                int sw1) {
         uint32_t b0, b1;
         backs(b0, b1);
         c_slot = next(c_slot);
-#pragma unroll
-        for (int m = 0; m < NM; ++m) {
-            mfma(ca, cb, m, sw0, sw1);
-            behind<2 * C::TN + 4 * C::TM, RM>(m, [&](int r) {
+        half(ca, cb, sw0, sw1, [&](int m) {
+            part<2 * C::TN + 4 * C::TM, true>(m, [&](int r) {
                 if (r < 4 * C::TM)
                     read_b(r & 1 ? b2 : b, r >> 1, r & 1);
                 else
                     read_a(a, r - 4 * C::TM, 0);
             });
-            behind<C::WI, NM>(m, [&](int q) { request_w(q, b0, b1); });
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        sums_used();
+            part<C::WI, false>(m, [&](int q) { request_w(q, b0, b1); });
+        });
         advance();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -398,14 +441,14 @@ __device__ __forceinline__ void block_end() {
 // all blocks do not fit the others beside the next tile's fragments.
 __device__ __forceinline__ void in_place(floatx16 &v) { asm volatile("" : "+a"(v)); }
 
-template <int MODE, int BM_, class L>
+template <int MODE, class L>
 __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &loop, char *smem) {
-    using C = Cfg<MODE, BM_>;
+    using C = typename L::C;
     int lane = threadIdx.x & 63;  // opaque: its products are not kept over the K loop
     asm volatile("" : "+v"(lane));
-    const int wave = loop.wave, wn = loop.wn, wm = loop.wm, half = lane >> 5;
+    const int wave = loop.wave, wn = loop.wn, half = lane >> 5;
     auto &acc = loop.acc;
-    // The lane holds, of token row wm WTM + 32 j + lane % 32, the weight rows
+    // The lane holds, of token row row0(j) + lane % 32, the weight rows
     // 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4.
     char *sc = smem + C::SCRATCH + wave * C::SC_WAVE;
     // every store is issued, since the waits count them: what is not valid gets
@@ -437,14 +480,14 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
                 in_place(acc[i][j]);
             }
             m = fmaxf(m, __shfl_xor(m, 32));
-            if (half == 0) smax[wn * C::BM + wm * C::WTM + j * 32 + lane] = m;
+            if (half == 0) smax[wn * C::BM + loop.row0(j) + lane] = m;
             __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
 #pragma unroll
         for (int j = 0; j < C::TM; ++j) {
-            const int row = wm * C::WTM + j * 32 + (lane & 31);
+            const int row = loop.row0(j) + (lane & 31);
             const int e = scale_exponent(fmaxf(smax[row], smax[C::BM + row]));
             const float inv = scale_inverse(e);
             if (wn == 0 && half == 0 && row < t.m_valid)
@@ -464,7 +507,7 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
             for (int q = 0; q < 2; ++q) {
                 const int rr = q * 16 + (lane >> 2), chunk = lane & 3;
                 const u32x4 v = *reinterpret_cast<const u32x4 *>(sc + rr * C::SC_ROW + chunk * 16);
-                const int orow = wm * C::WTM + j * 32 + rr;
+                const int orow = loop.row0(j) + rr;
                 store(v, orow < t.m_valid && wn * 64 < t.n_valid,
                       (uint32_t)(orow * g.N + wn * 64 + chunk * 16));
             }
@@ -500,7 +543,7 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
 #pragma unroll
                 for (int q = 0; q < 32 / RPI; ++q) {
                     const int rr = q * RPI + lane / CPR, chunk = lane % CPR;
-                    const int row = wm * C::WTM + j * 32 + rr;
+                    const int row = loop.row0(j) + rr;
                     const int col = wn * 128 + ib * 32 + chunk * (16 / C::ES);
                     const u32x4 v =
                         *reinterpret_cast<const u32x4 *>(sc + rr * C::SC_ROW + chunk * 16);
@@ -512,21 +555,20 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
     }
 }
 
-template <int MODE, int BM_>
-__global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
-    using C = Cfg<MODE, BM_>;
-    using L = TileLoop<MODE, BM_>;
-    __shared__ __attribute__((aligned(16))) char smem[C::LDS_BYTES];
-    const Walk<C> walk(g, reinterpret_cast<int *>(smem + C::INTS));
-    const int slot = (blockIdx.x % NXCD) * (gridDim.x / NXCD) + blockIdx.x / NXCD;
-    if (slot >= walk.total) return;
-
+// The workgroup's share of the tiles, or of the tails: `first` and every
+// gridDim.x-th one behind it.
+template <int MODE, int BM_, bool TAIL, class W>
+__device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, int first,
+                                          char *smem) {
+    using L = TileLoop<MODE, BM_, TAIL, W>;
+    using C = typename L::C;
     L t(g, walk, smem);
-    t.l_tau = slot;
-    t.request_idx(slot, 0);
+    if (first >= t.total) return;
+    t.l_tau = first;
+    t.request_idx(first, 0);
     t.template landed<0>();
     t.bind();
-    t.request_idx(slot + t.G, 1);
+    t.request_idx(first + t.G, 1);
 #pragma unroll
     for (int i = 0; i < C::NS; ++i) {
         t.request_pair();
@@ -546,8 +588,8 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
 
-    for (int tau = slot; tau < walk.total; tau += t.G) {
-        const Tile tile = walk.tile(g, tau);
+    for (int tau = first; tau < t.total; tau += t.G) {
+        const Tile tile = walk.tile(g, tau, TAIL);
         const int64_t nb = (int64_t)(g.e_first + tile.e) * scale_blocks(g.N) +
                            min((int)(tile.n0 / kScaleBlock) + (MODE == SWIGLU ? 0 : t.wn),
                                scale_blocks(g.N) - 1);
@@ -587,7 +629,7 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
         // b1: the pair's second half's token fragments, n1: the next one's
         auto pair = [&](int p, typename L::FragsB &b1, typename L::FragsB &n1) {
             const int s0 = w0 & 255, s1 = w1 & 255;
-            t.first_half(a0, b0, a1, s0, s1, p == 0 && tau != slot);
+            t.first_half(a0, b0, a1, s0, s1, p == 0 && tau != first);
             next_scales(p);
             t.second_half(a1, b1, a0, b0, n1, s0, s1);
             next_words(p);
@@ -611,9 +653,30 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
             t.second_half(a1, c0, a0, b0, b1, w0 & 255, w1 & 255);
             next_words(whole);
         }
-        epilogue<MODE, BM_>(g, tile, t, smem);
+        epilogue<MODE>(g, tile, t, smem);
     }
-    wait_vmcnt<0>();  // requests behind the last stage
+    t.template landed<0>();  // requests behind the last pair
+}
+
+template <int MODE, int BM_>
+__global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
+    using C = Cfg<MODE, BM_>;
+    constexpr bool TAILS = BM_ == 256;
+    __shared__ __attribute__((aligned(16))) char smem[C::LDS_BYTES];
+    using W = Walk<C, TAILS>;
+    const W walk(g, reinterpret_cast<int *>(smem + C::INTS));
+    // neighbouring tiles on one XCD
+    const int G = gridDim.x;  // a multiple of NXCD
+    const int slot = (blockIdx.x % NXCD) * (G / NXCD) + blockIdx.x / NXCD;
+    run_tiles<MODE, BM_, false>(g, walk, slot, smem);
+    if constexpr (TAILS) {
+        static_assert(Cfg<MODE, 128>::INTS <= C::INTS, "the offsets lie behind both layouts");
+        if (walk.tails > 0) {
+            const int used = walk.tiles % G;
+            run_tiles<MODE, 128, true>(g, walk, slot >= used ? slot - used : slot + G - used,
+                                       smem);
+        }
+    }
 }
 
 template <int MODE>
