@@ -502,6 +502,53 @@ moe_status moe_ffn_group_scaled(const moe_dims *dims, int32_t e_first, int32_t e
                                 void *y_perm, int32_t y_type, void *ws, size_t ws_bytes,
                                 void *stream);
 
+/* moe_combine over rows of either type: y_perm [R][H] of y_type.  The terms,
+ * their order and y are moe_combine's (bf16 rows are widened exactly). */
+moe_status moe_combine_rows(const moe_dims *dims, int32_t e_first, int32_t e_count,
+                            const void *y_perm, int32_t y_type, const int32_t *topk_ids,
+                            const int32_t *slot_row, const float *topk_w, float *y,
+                            int32_t accumulate, void *stream);
+
+/* A layer's quantised weights (moe_quant_weights): experts gate, up [EL][I][H]
+ * and down [EL][H][I], shared gate, up [Is][H] and down [H][Is] (NULL without
+ * shared experts).  The struct is host memory; its pointers are device ones. */
+typedef struct {
+    const moe_e4m3 *gate;
+    const moe_scale *gate_scales;
+    const moe_e4m3 *up;
+    const moe_scale *up_scales;
+    const moe_e4m3 *down;
+    const moe_scale *down_scales;
+    const moe_e4m3 *shared_gate;
+    const moe_scale *shared_gate_scales;
+    const moe_e4m3 *shared_up;
+    const moe_scale *shared_up_scales;
+    const moe_e4m3 *shared_down;
+    const moe_scale *shared_down_scales;
+} moe_scaled_weights;
+
+/* Workspace of moe_forward_scaled.  Host-only; 0 for invalid dims. */
+size_t moe_forward_scaled_bytes(const moe_dims *dims);
+
+/* The MoE layer in 8 bits, from the block's input to its output:
+ *   moe_norm_quant (total = bf16(x + residual), the normalised rows in bf16
+ *   and quantised) -> moe_route on the bf16 rows -> dispatch -> the shared
+ *   experts (if any) and moe_ffn_group_scaled on the quantised rows, the
+ *   routed rows in bf16 -> combine into y [T][H] fp32.
+ * The next layer takes y and total as its x (MOE_FP32) and residual.
+ * norm_weight NULL: x is bf16 rows that are normalised already (moe_ffn_forward's
+ * input); then residual and total must be NULL and eps is not read.
+ * topk_ids, topk_w, counts: optional outputs.  ws: moe_forward_scaled_bytes(dims)
+ * bytes, 16-byte aligned.  Every step runs on `stream`; the call allocates
+ * nothing, never synchronises and can be captured; calls that may overlap on
+ * the GPU need a workspace each. */
+moe_status moe_forward_scaled(const moe_dims *dims, const void *x, int32_t x_type,
+                              const moe_bf16 *residual, const moe_bf16 *norm_weight, float eps,
+                              moe_bf16 *total, const float *w_router, const float *bias,
+                              const moe_scaled_weights *weights, float *y, int32_t *topk_ids,
+                              float *topk_w, int32_t *counts, void *ws, size_t ws_bytes,
+                              void *stream);
+
 const char *moe_status_string(moe_status s);
 const char *moe_last_error(void);
 

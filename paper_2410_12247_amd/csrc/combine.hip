@@ -24,15 +24,25 @@ __device__ __forceinline__ float4 load_stream(const float4 *p) {
     return __builtin_bit_cast(float4,
                               __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(p)));
 }
+// four consecutive values of a row, fp32 or bf16
+__device__ __forceinline__ float4 load_row(const float *row, int v) {
+    return load_stream(reinterpret_cast<const float4 *>(row) + v);
+}
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float4 load_row(const bf16_t *row, int v) {
+    const u32x2 u = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(row) + v);
+    return make_float4(__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u),
+                       __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xFFFF0000u));
+}
 __device__ __forceinline__ void store_stream(float4 *p, float4 v) {
     __builtin_nontemporal_store(__builtin_bit_cast(floatx4, v), reinterpret_cast<floatx4 *>(p));
 }
 
-template <int KS>
+template <int KS, class Y>
 __global__ __launch_bounds__(256) void combine_kernel(int64_t t_begin, int64_t t_end, int H,
                                                       int k, int e0,
                                                       int e_lo, int e_hi,
-                                                      const float *__restrict__ y_perm,
+                                                      const Y *__restrict__ y_perm,
                                                       const int32_t *__restrict__ ids,
                                                       const int32_t *__restrict__ slot_row,
                                                       const float *__restrict__ w,
@@ -106,11 +116,9 @@ __global__ __launch_bounds__(256) void combine_kernel(int64_t t_begin, int64_t t
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             if (j < n) {
-                const float4 *prow =
-                    reinterpret_cast<const float4 *>(y_perm + (int64_t)orow[j] * H);
+                const Y *prow = y_perm + (int64_t)orow[j] * H;
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    p[j][u] = load_stream(prow + min(v0 + 64 * u, vecs - 1));
+                for (int u = 0; u < 4; ++u) p[j][u] = load_row(prow, min(v0 + 64 * u, vecs - 1));
             }
         }
 #pragma unroll
@@ -134,10 +142,12 @@ __global__ __launch_bounds__(256) void combine_kernel(int64_t t_begin, int64_t t
 
 }  // namespace
 
-hipError_t launch_combine(const moe_dims &d, int e_first, int e_count, int64_t t_begin,
-                          int64_t t_end, const float *y_perm, const int32_t *ids,
-                          const int32_t *slot_row, const float *w, float *y, int accumulate,
-                          hipStream_t s) {
+namespace {
+
+template <class Y>
+hipError_t go(const moe_dims &d, int e_first, int e_count, int64_t t_begin, int64_t t_end,
+              const Y *y_perm, const int32_t *ids, const int32_t *slot_row, const float *w,
+              float *y, int accumulate, hipStream_t s) {
     if (t_end <= t_begin) return hipSuccess;
     const int64_t blocks = (t_end - t_begin + 3) / 4;
     // few tokens: each token's passes over the hidden dimension spread over
@@ -147,16 +157,31 @@ hipError_t launch_combine(const moe_dims &d, int e_first, int e_count, int64_t t
     const int split = blocks * passes <= 2 * (int64_t)device_cu_count() * 4 ? passes : 1;
     // a token has at most k rows in range
     const int ks = d.top_k;
-    auto go = [&](auto kernel) {
+    auto launch = [&](auto kernel) {
         kernel<<<dim3((unsigned)blocks, (unsigned)split), 256, 0, s>>>(
             t_begin, t_end, d.hidden, d.top_k, d.local_begin, e_first, e_first + e_count, y_perm,
             ids, slot_row, w, y, accumulate);
         return hipGetLastError();
     };
-    if (ks <= 1) return go(combine_kernel<1>);
-    if (ks <= 2) return go(combine_kernel<2>);
-    if (ks <= 4) return go(combine_kernel<4>);
-    return go(combine_kernel<kMaxTopK>);
+    if (ks <= 1) return launch(combine_kernel<1, Y>);
+    if (ks <= 2) return launch(combine_kernel<2, Y>);
+    if (ks <= 4) return launch(combine_kernel<4, Y>);
+    return launch(combine_kernel<kMaxTopK, Y>);
+}
+
+}  // namespace
+
+hipError_t launch_combine(const moe_dims &d, int e_first, int e_count, int64_t t_begin,
+                          int64_t t_end, const float *y_perm, const int32_t *ids,
+                          const int32_t *slot_row, const float *w, float *y, int accumulate,
+                          hipStream_t s) {
+    return go(d, e_first, e_count, t_begin, t_end, y_perm, ids, slot_row, w, y, accumulate, s);
+}
+hipError_t launch_combine(const moe_dims &d, int e_first, int e_count, int64_t t_begin,
+                          int64_t t_end, const bf16_t *y_perm, const int32_t *ids,
+                          const int32_t *slot_row, const float *w, float *y, int accumulate,
+                          hipStream_t s) {
+    return go(d, e_first, e_count, t_begin, t_end, y_perm, ids, slot_row, w, y, accumulate, s);
 }
 
 }  // namespace moe

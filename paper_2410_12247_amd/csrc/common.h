@@ -174,6 +174,10 @@ hipError_t launch_combine(const moe_dims &d, int e_first, int e_count, int64_t t
                           int64_t t_end, const float *y_perm, const int32_t *ids,
                           const int32_t *slot_row, const float *w, float *y, int accumulate,
                           hipStream_t s);
+hipError_t launch_combine(const moe_dims &d, int e_first, int e_count, int64_t t_begin,
+                          int64_t t_end, const bf16_t *y_perm, const int32_t *ids,
+                          const int32_t *slot_row, const float *w, float *y, int accumulate,
+                          hipStream_t s);
 // Grouped GEMMs over local experts [e_first, e_first+e_count) (rows from
 // device offsets).  Gate/up takes its token rows either contiguous
 // (row_map NULL: x_rows is x_perm) or straight from the token matrix

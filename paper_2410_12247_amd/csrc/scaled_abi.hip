@@ -1,5 +1,5 @@
 // C-ABI entry points of the block-scaled 8-bit operators: argument checks,
-// workspace layout.
+// workspace layout, and the layer that runs them one after another.
 #include <algorithm>
 #include <cmath>
 
@@ -72,20 +72,88 @@ hipError_t product(const ScaledGemm &g, int y_type, const ScaledLoad &load, hipS
                : launch_scaled_gemm(g, y_type, load, s);
 }
 
-// The SwiGLU rows between the two products: quantised, or fp32 where the
+size_t up(size_t v) { return (v + 255) & ~size_t(255); }
+
+// The SwiGLU rows between an FFN's two products: quantised, or fp32 where the
 // launches of few rows run.
 struct FfnWs {
     bool stream;
     size_t act, act_s, total;
 };
-FfnWs ffn_ws(const moe_dims *d) {
+FfnWs ffn_ws(int64_t rows, int32_t inter, const ScaledLoad &load) {
     FfnWs w;
-    auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
-    const size_t rows = (size_t)row_cap(d);
-    w.stream = rows > 0 && scaled_stream_fits(scaled_tiles(true, d->inter), expected_load(*d));
+    w.stream = rows > 0 && scaled_stream_fits(scaled_tiles(true, inter), load);
     w.act = 0;
-    w.act_s = up(rows * d->inter * (w.stream ? sizeof(float) : 1));
-    w.total = w.act_s + (w.stream ? 0 : up(rows * scale_pitch(d->inter)));
+    w.act_s = up((size_t)rows * inter * (w.stream ? sizeof(float) : 1));
+    w.total = w.act_s + (w.stream ? 0 : up((size_t)rows * scale_pitch(inter)));
+    return w;
+}
+FfnWs ffn_ws(const moe_dims *d) {
+    return ffn_ws(row_cap(d), d->inter, expected_load(*d));
+}
+
+struct Matrix {
+    const uint8_t *q, *s;
+};
+// Both products of an FFN; `rows` holds the rows of the first (offsets, x,
+// row_map, ..), weights of width `inter`.
+moe_status ffn(ScaledGemm rows, int32_t hidden, int32_t inter, Matrix gate, Matrix up_,
+               Matrix down, void *y, int32_t y_type, const FfnWs &L, char *ws,
+               const ScaledLoad &load, hipStream_t s) {
+    uint8_t *act = (uint8_t *)ws + L.act, *act_s = (uint8_t *)ws + L.act_s;
+    ScaledGemm g = rows;
+    g.w0 = gate.q, g.s0 = gate.s;
+    g.w1 = up_.q, g.s1 = up_.s;
+    g.N = inter, g.K = hidden;
+    g.out = act, g.out_s = act_s;
+    MOE_HIP(L.stream ? launch_stream_swiglu(g, load, s) : launch_scaled_swiglu(g, load, s));
+    ScaledGemm h = rows;
+    h.x = act, h.xs = act_s;
+    h.row_map = nullptr;
+    h.w0 = down.q, h.s0 = down.s;
+    h.N = hidden, h.K = inter;
+    h.out = y;
+    MOE_HIP(L.stream ? launch_stream_scaled(h, y_type, true, load, s)
+                     : launch_scaled_gemm(h, y_type, load, s));
+    return MOE_OK;
+}
+
+// Workspace of the whole layer.
+struct LayerWs {
+    WsLayout perm;  // the dispatch's own regions, at offset 0
+    FfnWs routed, shared;
+    size_t y, q, s, ids, weights, logits, counts, offsets, sorted_slot, slot_row, ffn, y_perm,
+        total;
+};
+LayerWs layer_ws(const moe_dims *d) {
+    LayerWs w;
+    w.perm = ws_layout(d, nullptr);
+    w.routed = ffn_ws(d);
+    w.shared = d->shared_inter > 0
+                   ? ffn_ws(d->tokens, d->shared_inter, ScaledLoad{(double)d->tokens, 1.0})
+                   : FfnWs{};
+    size_t o = up(w.perm.total);
+    auto take = [&](size_t bytes) {
+        const size_t at = o;
+        o += up(bytes);
+        return at;
+    };
+    const size_t T = (size_t)d->tokens, slots = T * d->top_k, H = (size_t)d->hidden;
+    w.y = take(T * H * sizeof(bf16_t));
+    w.q = take(T * H);
+    w.s = take(T * scale_pitch(d->hidden));
+    w.ids = take(slots * sizeof(int32_t));
+    w.weights = take(slots * sizeof(float));
+    w.logits = d->experts > 16 && d->tokens <= kRouteLogitsMaxTokens
+                   ? take(T * d->experts * sizeof(float))
+                   : 0;
+    w.counts = take(d->local_count * sizeof(int32_t));
+    w.offsets = take((d->local_count + 1) * sizeof(int32_t));
+    w.sorted_slot = take((size_t)row_cap(d) * sizeof(int32_t));
+    w.slot_row = take(slots * sizeof(int32_t));
+    w.ffn = take(std::max(w.routed.total, w.shared.total));  // one FFN after the other
+    w.y_perm = take((size_t)row_cap(d) * H * sizeof(bf16_t));
+    w.total = o;
     return w;
 }
 
@@ -233,30 +301,135 @@ moe_status moe_ffn_group_scaled(const moe_dims *dims, int32_t e_first, int32_t e
     if (!ws || ws_bytes < L.total)
         return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, L.total);
     MOE_TRY(check_tensor(fn, "ws", ws));
-    uint8_t *base = (uint8_t *)ws;
-    const ScaledLoad load = expected_load(*dims);
-    hipStream_t s = (hipStream_t)stream;
     ScaledGemm g{};
     g.offsets = offsets;
     g.e_first = e_first, g.e_count = e_count;
     g.x = x, g.xs = x_scales;
     g.row_map = sorted_slot;
     g.slot_div = dims->top_k;
-    g.w0 = w_gate, g.s0 = gate_scales;
-    g.w1 = w_up, g.s1 = up_scales;
-    g.N = dims->inter, g.K = dims->hidden;
-    g.out = base + L.act, g.out_s = base + L.act_s;
-    MOE_HIP(L.stream ? launch_stream_swiglu(g, load, s) : launch_scaled_swiglu(g, load, s));
-    ScaledGemm h{};
-    h.offsets = offsets;
-    h.e_first = e_first, h.e_count = e_count;
-    h.x = base + L.act, h.xs = base + L.act_s;
-    h.slot_div = 1;
-    h.w0 = w_down, h.s0 = down_scales;
-    h.N = dims->hidden, h.K = dims->inter;
-    h.out = y_perm;
-    MOE_HIP(L.stream ? launch_stream_scaled(h, y_type, true, load, s)
-                     : launch_scaled_gemm(h, y_type, load, s));
+    return ffn(g, dims->hidden, dims->inter, {w_gate, gate_scales}, {w_up, up_scales},
+               {w_down, down_scales}, y_perm, y_type, L, (char *)ws, expected_load(*dims),
+               (hipStream_t)stream);
+}
+
+moe_status moe_combine_rows(const moe_dims *dims, int32_t e_first, int32_t e_count,
+                            const void *y_perm, int32_t y_type, const int32_t *topk_ids,
+                            const int32_t *slot_row, const float *topk_w, float *y,
+                            int32_t accumulate, void *stream) {
+    const char *fn = "moe_combine_rows";
+    MOE_TRY(check_dims(dims));
+    if (!type_ok(y_type)) return fail(MOE_ERR_INVALID, "%s: y_type %d", fn, y_type);
+    if (y_type == MOE_FP32)
+        return moe_combine(dims, e_first, e_count, (const float *)y_perm, topk_ids, slot_row,
+                           topk_w, y, accumulate, stream);
+    if (e_first < 0 || e_count < 0 || e_first > dims->local_count - e_count)
+        return fail(MOE_ERR_INVALID, "%s: expert range outside [0, local_count)", fn);
+    if (accumulate != 0 && accumulate != 1)
+        return fail(MOE_ERR_INVALID, "%s: accumulate must be 0 or 1", fn);
+    if (dims->tokens == 0) return MOE_OK;
+    if (!topk_ids || !slot_row || !topk_w)
+        return fail(MOE_ERR_INVALID, "%s: NULL index tensor", fn);
+    MOE_TRY(check_tensor(fn, "y", y));
+    if (e_count > 0) MOE_TRY(check_tensor(fn, "y_perm", y_perm, 8));
+    MOE_HIP(launch_combine(*dims, e_first, e_count, 0, dims->tokens, (const bf16_t *)y_perm,
+                           topk_ids, slot_row, topk_w, y, accumulate, (hipStream_t)stream));
+    return MOE_OK;
+}
+
+size_t moe_forward_scaled_bytes(const moe_dims *dims) {
+    if (check_dims(dims) != MOE_OK) return 0;
+    return layer_ws(dims).total;
+}
+
+moe_status moe_forward_scaled(const moe_dims *dims, const void *x, int32_t x_type,
+                              const moe_bf16 *residual, const moe_bf16 *norm_weight, float eps,
+                              moe_bf16 *total, const float *w_router, const float *bias,
+                              const moe_scaled_weights *weights, float *y, int32_t *topk_ids,
+                              float *topk_w, int32_t *counts, void *ws, size_t ws_bytes,
+                              void *stream) {
+    const char *fn = "moe_forward_scaled";
+    MOE_TRY(check_dims(dims));
+    MOE_TRY(check_product(fn, row_cap(dims), dims->local_count,
+                          std::max({dims->hidden, dims->inter, dims->shared_inter}), kDimAlign));
+    if (!type_ok(x_type)) return fail(MOE_ERR_INVALID, "%s: x_type %d", fn, x_type);
+    if (!norm_weight && (x_type != MOE_BF16 || residual || total))
+        return fail(MOE_ERR_INVALID,
+                    "%s: without norm_weight x is bf16 rows normalised before, with no residual "
+                    "and no total",
+                    fn);
+    if (norm_weight && (!(eps >= 0.f) || std::isinf(eps)))
+        return fail(MOE_ERR_INVALID, "%s: eps is negative or not finite", fn);
+    if (!weights) return fail(MOE_ERR_INVALID, "%s: weights is NULL", fn);
+    if ((uint64_t)dims->tokens * (uint64_t)dims->hidden >= kMaxOffset)
+        return fail(MOE_ERR_UNSUPPORTED, "%s: a quantised token matrix of 4 GiB or more", fn);
+    if (dims->tokens == 0) return MOE_OK;
+    MOE_TRY(check_tensor(fn, "x", x));
+    if (residual) MOE_TRY(check_tensor(fn, "residual", residual));
+    if (norm_weight) MOE_TRY(check_tensor(fn, "norm_weight", norm_weight));
+    if (total) MOE_TRY(check_tensor(fn, "total", total));
+    if (!w_router) return fail(MOE_ERR_INVALID, "%s: w_router is NULL", fn);
+    const moe_scaled_weights &w = *weights;
+    MOE_TRY(check_pair(fn, "w_gate", w.gate, w.gate_scales));
+    MOE_TRY(check_pair(fn, "w_up", w.up, w.up_scales));
+    MOE_TRY(check_pair(fn, "w_down", w.down, w.down_scales));
+    if (dims->shared_inter > 0) {
+        MOE_TRY(check_pair(fn, "shared_gate", w.shared_gate, w.shared_gate_scales));
+        MOE_TRY(check_pair(fn, "shared_up", w.shared_up, w.shared_up_scales));
+        MOE_TRY(check_pair(fn, "shared_down", w.shared_down, w.shared_down_scales));
+    }
+    MOE_TRY(check_tensor(fn, "y", y));
+    const LayerWs L = layer_ws(dims);
+    if (!ws || ws_bytes < L.total)
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, L.total);
+    MOE_TRY(check_tensor(fn, "ws", ws));
+
+    const moe_dims &d = *dims;
+    char *base = (char *)ws;
+    hipStream_t s = (hipStream_t)stream;
+    uint8_t *q = (uint8_t *)base + L.q, *qs = (uint8_t *)base + L.s;
+    // rows: normalised ones go through the workspace to the router
+    const bf16_t *rows = (const bf16_t *)x;
+    if (norm_weight) {
+        bf16_t *yn = (bf16_t *)(base + L.y);
+        MOE_HIP(launch_norm_quant(d.tokens, d.hidden, x, x_type, residual, true, norm_weight, eps,
+                                  total, yn, q, qs, s));
+        rows = yn;
+    } else {
+        MOE_HIP(launch_norm_quant(d.tokens, d.hidden, x, x_type, nullptr, false, nullptr, 0.f,
+                                  nullptr, nullptr, q, qs, s));
+    }
+    // routing and dispatch indices
+    int32_t *ids = topk_ids ? topk_ids : (int32_t *)(base + L.ids);
+    float *wts = topk_w ? topk_w : (float *)(base + L.weights);
+    int32_t *cnt = counts ? counts : (int32_t *)(base + L.counts);
+    int32_t *off = (int32_t *)(base + L.offsets), *slot = (int32_t *)(base + L.sorted_slot);
+    int32_t *slot_row = (int32_t *)(base + L.slot_row);
+    float *logits = L.logits ? (float *)(base + L.logits) : nullptr;
+    const bool fused = route_dispatches(d, rows, logits);
+    const DispatchOut disp = dispatch_out(d, L.perm, 0, cnt, off, nullptr, slot, slot_row);
+    MOE_HIP(launch_route(d, rows, w_router, bias, ids, wts, logits, s, fused ? &disp : nullptr));
+    if (!fused)
+        MOE_HIP(launch_permute(d, ids, base, L.perm, 0, cnt, off, nullptr, slot, slot_row, s));
+    // the shared experts are one expert of all tokens and write y
+    ScaledGemm g{};
+    g.x = q, g.xs = qs;
+    g.slot_div = d.top_k;
+    if (d.shared_inter > 0) {
+        g.e_count = 1;
+        g.rows_one = d.tokens;
+        MOE_TRY(ffn(g, d.hidden, d.shared_inter, {w.shared_gate, w.shared_gate_scales},
+                    {w.shared_up, w.shared_up_scales}, {w.shared_down, w.shared_down_scales}, y,
+                    MOE_FP32, L.shared, base + L.ffn, ScaledLoad{(double)d.tokens, 1.0}, s));
+    }
+    g.offsets = off;
+    g.e_count = d.local_count;
+    g.row_map = slot;
+    bf16_t *y_perm = (bf16_t *)(base + L.y_perm);
+    MOE_TRY(ffn(g, d.hidden, d.inter, {w.gate, w.gate_scales}, {w.up, w.up_scales},
+                {w.down, w.down_scales}, y_perm, MOE_BF16, L.routed, base + L.ffn,
+                expected_load(d), s));
+    MOE_HIP(launch_combine(d, 0, d.local_count, 0, d.tokens, y_perm, ids, slot_row, wts, y,
+                           d.shared_inter > 0 ? 1 : 0, s));
     return MOE_OK;
 }
 

@@ -28,7 +28,8 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_guards", "moe_route", "moe_perm
            "moe_gemm_plan", "moe_pipeline_plan", "moe_choose_pipeline_n", "moe_status_string",
            "moe_last_error", "moe_scale_pitch", "moe_quant_rows", "moe_quant_weights",
            "moe_norm_quant", "moe_gemm_scaled", "moe_gemm_group_scaled",
-           "moe_scaled_workspace_bytes", "moe_ffn_group_scaled")
+           "moe_scaled_workspace_bytes", "moe_ffn_group_scaled", "moe_combine_rows",
+           "moe_forward_scaled", "moe_forward_scaled_bytes")
 
 
 class MoEError(RuntimeError):
@@ -62,6 +63,13 @@ class Timing(ctypes.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class ScaledWeights(ctypes.Structure):
+    """A layer's quantised weights (moe_scaled_weights); scaled_weights() fills it."""
+    _fields_ = [(n + s, ctypes.c_void_p)
+                for n in ("gate", "up", "down", "shared_gate", "shared_up", "shared_down")
+                for s in ("", "_scales")]
 
 
 class PipelineEval(ctypes.Structure):
@@ -114,6 +122,11 @@ def lib():
     L.moe_scaled_workspace_bytes.argtypes = [D]
     L.moe_scaled_workspace_bytes.restype = SZ
     L.moe_ffn_group_scaled.argtypes = [D, I32, I32] + [P] * 11 + [I32, P, SZ, P]
+    L.moe_combine_rows.argtypes = [D, I32, I32, P, I32, P, P, P, P, I32, P]
+    L.moe_forward_scaled_bytes.argtypes = [D]
+    L.moe_forward_scaled_bytes.restype = SZ
+    L.moe_forward_scaled.argtypes = [D, P, I32, P, P, ctypes.c_float, P, P, P,
+                                     ctypes.POINTER(ScaledWeights), P, P, P, P, P, SZ, P]
     L.moe_status_string.argtypes = [I32]
     L.moe_status_string.restype = ctypes.c_char_p
     L.moe_last_error.restype = ctypes.c_char_p
@@ -121,7 +134,8 @@ def lib():
                  "moe_combine", "moe_ffn_forward", "moe_ffn_forward_noalloc", "moe_last_timing",
                  "moe_choose_pipeline_n", "moe_gemm_plan", "moe_pipeline_plan", "moe_quant_rows",
                  "moe_quant_weights", "moe_norm_quant", "moe_gemm_scaled",
-                 "moe_gemm_group_scaled", "moe_ffn_group_scaled"):
+                 "moe_gemm_group_scaled", "moe_ffn_group_scaled", "moe_combine_rows",
+                 "moe_forward_scaled"):
         getattr(L, name).restype = I32
     _lib = L
     return L
@@ -298,6 +312,7 @@ _SCALE = (torch.uint8, torch.float8_e8m0fnu)
 _REAL = {torch.bfloat16: BF16, torch.float32: FP32}
 _I32 = (torch.int32,)
 _BF16 = (torch.bfloat16,)
+_F32 = (torch.float32,)
 
 
 # (Small batches take a few microseconds on the GPU: these checks are kept to
@@ -468,6 +483,69 @@ def ffn_group_scaled(d, e_first, e_count, offsets, sorted_slot, x, x_scales, w_g
         _arg(dev, "y_perm", y_perm, (y_perm.dtype,), (_row_cap(d), H)), code,
         _arg(dev, "ws", ws, (ws.dtype,), ws.shape), ws.numel() * ws.element_size(),
         _stream_on(dev, stream)))
+
+
+def combine_rows(d, e_first, e_count, y_perm, topk_ids, slot_row, topk_w, y, accumulate,
+                 stream=None):
+    """combine for y_perm of bf16 or fp32."""
+    dev, code = _dev("y_perm", y_perm), _real("y_perm", y_perm)
+    slots = (d.tokens, d.top_k)
+    _check(lib().moe_combine_rows(
+        ctypes.byref(d), e_first, e_count,
+        _arg(dev, "y_perm", y_perm, (y_perm.dtype,), (_row_cap(d), d.hidden)), code,
+        _arg(dev, "topk_ids", topk_ids, _I32, slots),
+        _arg(dev, "slot_row", slot_row.view(-1), _I32, (d.tokens * d.top_k,)),
+        _arg(dev, "topk_w", topk_w, _F32, slots),
+        _arg(dev, "y", y, _F32, (d.tokens, d.hidden)), int(accumulate), _stream_on(dev, stream)))
+
+
+def scaled_weights(d, gate, up, down, shared_gate=None, shared_up=None,
+                   shared_down=None) -> ScaledWeights:
+    """Checks and packs a layer's weights, each a pair (q, scales) of
+    quant_weights; made once and kept with the tensors."""
+    H, I, Is = d.hidden, d.inter, d.shared_inter
+    dev = _dev("gate", gate[0])
+    w = ScaledWeights()
+    w.keep = (gate, up, down, shared_gate, shared_up, shared_down)
+    for name, (q, s), n, k in (("gate", gate, I, H), ("up", up, I, H), ("down", down, H, I)):
+        a, b = _stack(dev, name, d, q, s, n, k)
+        setattr(w, name, a)
+        setattr(w, name + "_scales", b)
+    if Is:
+        for name, pair, n, k in (("shared_gate", shared_gate, Is, H),
+                                 ("shared_up", shared_up, Is, H),
+                                 ("shared_down", shared_down, H, Is)):
+            if pair is None:
+                raise ValueError(f"dims have shared experts: {name} is missing")
+            setattr(w, name, _arg(dev, name, pair[0], _E4M3, (n, k)))
+            setattr(w, name + "_scales", _arg(dev, name + " scales", pair[1], _SCALE,
+                                              (-(-n // 128), _pitch(k))))
+    return w
+
+
+def forward_scaled_bytes(d: Dims) -> int:
+    return lib().moe_forward_scaled_bytes(ctypes.byref(d))
+
+
+def forward_scaled(d, x, residual, norm_weight, eps, total, w_router, bias, weights, y, topk_ids,
+                   topk_w, counts, ws, stream=None):
+    """The MoE layer in 8 bits (moe_forward_scaled): norm, route, dispatch,
+    experts, combine.  weights: scaled_weights(); norm_weight None: x holds bf16
+    rows normalised before."""
+    T, H, k = d.tokens, d.hidden, d.top_k
+    dev, code = _dev("x", x), _real("x", x)
+    _check(lib().moe_forward_scaled(
+        ctypes.byref(d), _arg(dev, "x", x, (x.dtype,), (T, H)), code,
+        _arg(dev, "residual", residual, _BF16, (T, H)),
+        _arg(dev, "norm_weight", norm_weight, _BF16, (H,)), eps,
+        _arg(dev, "total", total, _BF16, (T, H)),
+        _arg(dev, "w_router", w_router, _F32, (d.experts, H)),
+        _arg(dev, "bias", bias, _F32, (d.experts,)), ctypes.byref(weights),
+        _arg(dev, "y", y, _F32, (T, H)), _arg(dev, "topk_ids", topk_ids, _I32, (T, k)),
+        _arg(dev, "topk_w", topk_w, _F32, (T, k)),
+        _arg(dev, "counts", counts, _I32, (d.local_count,)), _arg(dev, "ws", ws, (ws.dtype,),
+                                                                  ws.shape),
+        ws.numel() * ws.element_size(), _stream_on(dev, stream)))
 
 
 class MoEBuffers:

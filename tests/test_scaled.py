@@ -578,3 +578,234 @@ def test_norm_route_dispatch_ffn_combine():
         want.index_add_(0, tok, w[tok, j, None] * ye)
         bound.index_add_(0, tok, w[tok, j, None] * (be + (k + 1) * 2.0 ** -23 * ye.abs()))
     assert bool(((out.cpu().double() - want).abs() <= bound).all())
+
+
+# ---- the layer ------------------------------------------------------------
+
+def test_layer_refusals():
+    L = moe.lib()
+    d = moe.dims(64, 256, 128, 8, 2)
+    ds = moe.dims(64, 256, 128, 8, 2, shared_inter=192)
+    need = moe.forward_scaled_bytes(d)
+    assert need > moe.scaled_workspace_bytes(d) + 64 * 256 * (2 + 1) + 128 * 256 * 2
+    assert moe.forward_scaled_bytes(moe.dims(64, 100, 128, 8, 2)) == 0
+
+    def weights(**k):
+        w = moe.ScaledWeights()
+        for n, _ in w._fields_:
+            setattr(w, n, None if n.startswith("shared") else 4096)
+        for n, v in k.items():
+            setattr(w, n, v)
+        return w
+
+    def layer(d=d, x=FAKE, t=1, res=FAKE, nw=FAKE, eps=1e-6, tot=FAKE, wr=FAKE, w=weights(),
+              y=FAKE, ws=FAKE, n=need):
+        return L.moe_forward_scaled(ctypes.byref(d), x, t, res, nw, eps, tot, wr, None,
+                                    ctypes.byref(w) if w is not None else None, y, None, None,
+                                    None, ws, n, None)
+    for bad in (dict(t=2), dict(x=None), dict(x=ODD), dict(res=ODD), dict(nw=ODD), dict(tot=ODD),
+                dict(eps=-1.0), dict(eps=float("nan")), dict(wr=None), dict(w=None),
+                dict(w=weights(up=None)), dict(w=weights(down_scales=None)),
+                dict(w=weights(gate=4098)), dict(y=None), dict(ws=ODD),
+                # normalised x: bf16, without residual and total
+                dict(nw=None), dict(nw=None, t=0, tot=None), dict(nw=None, t=0, res=None),
+                dict(nw=None, t=1, res=None, tot=None),
+                dict(d=ds)):  # no shared weights
+        assert layer(**bad) == 1, (bad, last())
+    assert layer(n=need - 1) == 3 and layer(ws=None) == 3
+    assert layer(d=moe.dims(1 << 16, 1 << 16, 64, 8, 2)) == 2 and "4 GiB" in last()
+    assert layer(d=moe.dims(0, 256, 128, 8, 2), x=None) == 0
+
+    def combine(e0=0, ec=8, yp=FAKE, t=0, ids=FAKE, y=FAKE, acc=0):
+        return L.moe_combine_rows(ctypes.byref(d), e0, ec, yp, t, ids, FAKE, FAKE, y, acc, None)
+    for bad in (dict(e0=-1), dict(ec=9), dict(yp=None), dict(yp=ODD), dict(t=2), dict(ids=None),
+                dict(y=None), dict(acc=2), dict(t=1, yp=None)):
+        assert combine(**bad) == 1, (bad, last())
+
+
+@gpu
+@pytest.mark.parametrize("T,E,k,e0,EL,H", [(1, 8, 2, 0, 8, 64), (37, 16, 4, 4, 8, 320),
+                                           (300, 8, 8, 0, 8, 1088)])
+def test_combine_rows(T, E, k, e0, EL, H):
+    g = gen(T)
+    ids = torch.rand((T, E), generator=g).topk(k, 1).indices.int()
+    d = moe.dims(T, H, 64, E, k, e0, EL)
+    cap = T * min(k, EL)
+    off, slot, _ = torch.empty(EL + 1, dtype=torch.int32).cuda(), None, None
+    counts = torch.empty(EL, dtype=torch.int32).cuda()
+    slot = torch.empty(cap, dtype=torch.int32).cuda()
+    slot_row = torch.empty(T * k, dtype=torch.int32).cuda()
+    ws = torch.empty(moe.workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    idc = cuda(ids)
+    moe.permute(d, idc, None, counts, off, slot, slot_row, None, ws)
+    w = torch.rand((T, k), generator=g).cuda()
+    yp = torch.randn((cap, H), generator=g).to(BF16).cuda()
+    for first, count in ((0, EL), (1, EL // 2)):
+        for acc in (False, True):
+            base = torch.randn((T, H), generator=g).cuda()
+            a, b, c = base.clone(), base.clone(), base.clone()
+            moe.combine_rows(d, first, count, yp, idc, slot_row, w, a, acc)
+            moe.combine_rows(d, first, count, yp.float(), idc, slot_row, w, b, acc)
+            moe.combine(d, first, count, yp.float(), idc, slot_row, w, c, acc)
+            assert torch.equal(a, c) and torch.equal(b, c)
+
+
+class Layer:
+    def __init__(self, T, H, I, E, k, e0, EL, Is, seed, x_dtype=F32, normed=False):
+        g = gen(seed)
+        self.d = moe.dims(T, H, I, E, k, e0, EL, shared_inter=Is)
+        self.eps = 1e-5
+        self.x = torch.randn((T, H), generator=g).to(x_dtype)
+        self.res = None if normed else torch.randn((T, H), generator=g).to(BF16)
+        self.nw = None if normed else (1 + 0.1 * torch.randn(H, generator=g)).to(BF16)
+        self.router = torch.randn((E, H), generator=g) * 0.05
+        self.pairs = []
+        for shape in ((EL, I, H), (EL, I, H), (EL, H, I)) + (((Is, H), (Is, H), (H, Is)) if Is
+                                                             else ()):
+            w = (torch.randn(shape, generator=g) * 0.05).to(BF16)
+            q = torch.empty(shape, dtype=torch.float8_e4m3fn, device="cuda")
+            s = torch.empty(shape[:-2] + (ref.blocks(shape[-2]), ref.pitch(shape[-1])),
+                            dtype=torch.uint8, device="cuda")
+            moe.quant_weights(cuda(w), q, s)
+            self.pairs.append((q, s))
+        self.w = moe.scaled_weights(self.d, *self.pairs)
+        dev = dict(device="cuda")
+        self.xd, self.rd = cuda(self.x), None if normed else cuda(self.res)
+        self.nwd, self.routerd = None if normed else cuda(self.nw), cuda(self.router)
+        self.total = None if normed else torch.empty((T, H), dtype=BF16, **dev)
+        self.y = torch.full((T, H), float("nan"), **dev)
+        self.ids = torch.empty((T, k), dtype=torch.int32, **dev)
+        self.wts = torch.empty((T, k), **dev)
+        self.counts = torch.empty(EL, dtype=torch.int32, **dev)
+        n = moe.forward_scaled_bytes(self.d)
+        self.ws_all = torch.full((n + 256,), 0xA5, dtype=torch.uint8, **dev)
+        self.ws = self.ws_all[:n]
+
+    def run(self, outs=True, stream=None):
+        o = (self.ids, self.wts, self.counts) if outs else (None, None, None)
+        moe.forward_scaled(self.d, self.xd, self.rd, self.nwd, self.eps, self.total, self.routerd,
+                           None, self.w, self.y, *o, self.ws, stream)
+
+
+LAYERS = [
+    # T, H, I, E, k, e0, EL, Is
+    (1, 256, 192, 8, 2, 0, 8, 0),
+    (1, 192, 128, 32, 4, 8, 8, 320),
+    (29, 320, 192, 8, 2, 0, 8, 192),
+    (70, 128, 320, 40, 6, 10, 20, 64),
+    (260, 256, 128, 4, 2, 1, 2, 128),
+]
+
+
+@gpu
+@pytest.mark.parametrize("normed", [False, True])
+@pytest.mark.parametrize("case", LAYERS, ids=str)
+def test_layer(case, normed):
+    T, H, I, E, k, e0, EL, Is = case
+    L = Layer(*case, seed=T + H, x_dtype=BF16 if normed else F32, normed=normed)
+    L.run()
+    torch.cuda.synchronize()
+    assert bool((L.ws_all[len(L.ws):] == 0xA5).all())
+    # the first steps one by one have the same bits
+    q = torch.empty((T, H), dtype=torch.uint8, device="cuda")
+    s = torch.empty((T, ref.pitch(H)), dtype=torch.uint8, device="cuda")
+    yn = torch.empty((T, H), dtype=BF16, device="cuda")
+    if normed:
+        moe.quant_rows(L.xd, q, s)
+        yn = L.xd
+    else:
+        total = torch.empty_like(yn)
+        moe.norm_quant(L.xd, L.rd, L.nwd, L.eps, total, yn, q, s)
+        assert torch.equal(total, L.total)
+    ids, w = torch.empty_like(L.ids), torch.empty_like(L.wts)
+    moe.route(L.d, yn, L.routerd, None, ids, w)
+    assert torch.equal(ids, L.ids) and torch.equal(w, L.wts)
+    local = ids.cpu() - e0
+    assert torch.equal(L.counts.cpu(), torch.bincount(local[(local >= 0) & (local < EL)],
+                                                      minlength=EL)[:EL].int())
+    if not Is:  # and the rest
+        counts, off = torch.empty_like(L.counts), torch.empty(EL + 1, dtype=torch.int32).cuda()
+        slot = torch.empty(T * min(k, EL), dtype=torch.int32).cuda()
+        slot_row = torch.empty(T * k, dtype=torch.int32).cuda()
+        pws = torch.empty(moe.workspace_bytes(L.d), dtype=torch.uint8, device="cuda")
+        moe.permute(L.d, ids, None, counts, off, slot, slot_row, None, pws)
+        yp = torch.empty((len(slot), H), dtype=BF16, device="cuda")
+        fws = torch.empty(moe.scaled_workspace_bytes(L.d), dtype=torch.uint8, device="cuda")
+        moe.ffn_group_scaled(L.d, 0, EL, off, slot, q, s, *[t for p in L.pairs for t in p], yp,
+                             fws)
+        y = torch.empty_like(L.y)
+        moe.combine_rows(L.d, 0, EL, yp, ids, slot_row, w, y, False)
+        assert torch.equal(y, L.y)
+    # against 64 bits
+    x = ref.widen(q, s, 1)
+    want, bound = torch.zeros((T, H), dtype=torch.float64), torch.zeros((T, H),
+                                                                       dtype=torch.float64)
+    if Is:
+        want, bound = ref.ffn_rows(x, *[ref.widen(p[0], p[1], 128) for p in L.pairs[3:]])
+        bound = bound + 2.0 ** -23 * (want.abs() + bound)
+    w = w.cpu().double()
+    for e in range(EL):
+        tok, j = (local == e).nonzero(as_tuple=True)
+        if len(tok):
+            ye, be = ref.ffn_rows(x[tok], *[ref.widen(p[0][e], p[1][e], 128)
+                                            for p in L.pairs[:3]])
+            be = be + 2.0 ** -8 * (ye.abs() + be)  # the rows in bf16
+            want.index_add_(0, tok, w[tok, j, None] * ye)
+            bound.index_add_(0, tok, w[tok, j, None] * (be + (k + 2) * 2.0 ** -23 * ye.abs()))
+    assert bool(((L.y.cpu().double() - want).abs() <= bound).all())
+    # without the optional outputs: the same
+    y = L.y.clone()
+    L.y.fill_(float("nan"))
+    L.run(outs=False)
+    assert torch.equal(L.y, y)
+
+
+@gpu
+def test_layer_on_another_stream_and_in_graphs():
+    """Two graphs of one layer with a workspace each, replayed in turn and beside
+    each other, with eager work between."""
+    case = (24, 256, 192, 8, 2, 0, 8, 128)
+    A, B = Layer(*case, seed=1), Layer(*case, seed=2)
+    graphs = []
+    for L in (A, B):
+        L.run()
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            L.run()
+        graphs.append(gr)
+    g = gen(9)
+    side = torch.cuda.Stream()
+    for i in range(3):
+        for L in (A, B):
+            L.xd.copy_(torch.randn(L.x.shape, generator=g))
+        want = []
+        for L in (A, B):
+            L.run()
+            want.append(L.y.clone())
+            L.y.zero_()
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        with torch.cuda.stream(side):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(A.y, want[0]) and torch.equal(B.y, want[1]), i
+    B.y.zero_()
+    B.run(stream=side)
+    side.synchronize()
+    assert torch.equal(B.y, want[1])
+
+
+@gpu
+def test_layers_in_a_row():
+    """Two layers: the second takes the first one's output and residual stream."""
+    case = (19, 192, 128, 8, 2, 0, 8, 0)
+    A, B = Layer(*case, seed=5), Layer(*case, seed=6)
+    A.run()
+    B.xd, B.rd = A.y, A.total
+    B.run()
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(B.y).all())
+    s = A.y.cpu().double() + A.total.cpu().double()
+    off = (B.total.cpu().double() - s).abs()
+    assert bool((off <= (2.0 ** -8 + 2.0 ** -23) * s.abs()).all())
