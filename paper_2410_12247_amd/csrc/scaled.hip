@@ -50,12 +50,14 @@ struct Cfg {
     static constexpr int LPS = WI + XI;
     static constexpr int STAGE_W = BN * BK, STAGE = (BN + BM) * BK;
     static constexpr int ES = MODE == OUT_F32 ? 4 : 2;
-    // LDS: ring | token scales [SG][256] words | row indices [2][256] |
-    // epilogue scratch | expert offsets
+    // LDS: ring | token scales [SG][256] words | row indices [2][256] | tiles
+    // ahead [4 waves][PLAN][8] | epilogue scratch | expert offsets
     static constexpr int SG = 4;
     static constexpr int SCALES = NS * STAGE;
     static constexpr int IDX = SCALES + SG * 1024;
-    static constexpr int SCRATCH = IDX + 2 * 1024;
+    static constexpr int PLAN = 8;
+    static constexpr int PLANS = IDX + 2 * 1024;
+    static constexpr int SCRATCH = PLANS + 4 * PLAN * 32;
     static constexpr int SC_COLS = MODE == OUT_F32 ? 32 : 64;  // columns of a scratch block
     static constexpr int SC_ROW = (MODE == SWIGLU ? 64 : SC_COLS * ES) + 16;
     static constexpr int SC_WAVE = 32 * SC_ROW;
@@ -68,8 +70,8 @@ struct Cfg {
 };
 
 struct Tile {
-    int e;              // expert of the launch
-    int64_t r0, n0;     // first product row, first output column
+    int e;           // expert of the launch
+    int64_t r0, n0;  // first product row, first output column
     int m_valid, n_valid;
 };
 
@@ -188,8 +190,8 @@ struct TileLoop {
     uint32_t lds0;
     int lane, wave, wn, wm, K, SK, np, G;
 
-    // load side: the tile whose pairs are being requested
-    int l_tau, l_kp, l_slot, l_group, l_idx;
+    // load side: the tile whose pairs are being requested, and its number
+    int l_tau, l_n, l_kp, l_slot, l_group, l_idx;
     u32x4 wres, xres, sres;
     uint32_t woff[C::WI], xoff[C::XI], soff, upper;
 
@@ -210,21 +212,38 @@ struct TileLoop {
         c_slot = c_group = c_byte = 0;
     }
 
-    // The row indices of tile tau, one request per wave (behind the last row:
-    // the last one's).
-    __device__ __forceinline__ void request_idx(int tau, int which) {
-        if (!g.row_map || tau >= total) return;
+    // The workgroup's n-th tile is found once, ahead of its first request, and
+    // kept in LDS (each wave for itself: no barrier); the gather's row indices
+    // (behind the last row: the last one's) are requested with it.
+    __device__ __forceinline__ int *plan(int n) const {
+        return reinterpret_cast<int *>(smem + C::PLANS) +
+               (wave * C::PLAN + (n & (C::PLAN - 1))) * 8;
+    }
+    __device__ __forceinline__ void plan_tile(int tau, int n, int which) {
+        if (tau >= total) return;
         const Tile t = walk.tile(g, tau, TAIL);
+        int *p = plan(n);
+        p[0] = t.e;
+        p[1] = (int)t.r0;
+        p[2] = (int)t.n0;
+        p[3] = t.m_valid;
+        p[4] = t.n_valid;
+        if (!g.row_map) return;
         const uint32_t r = (uint32_t)min(wave * 64 + lane, t.m_valid - 1) * 4u;
         buf4_to_lds(buf_rsrc(g.row_map + t.r0), r, 0,
                     lds0 + C::IDX + which * 1024 + wave * 256);
+    }
+    __device__ __forceinline__ Tile planned(int n) const {
+        const int *p = plan(n);
+        auto at = [&](int i) { return __builtin_amdgcn_readfirstlane(p[i]); };
+        return Tile{at(0), at(1), at(2), at(3), at(4)};
     }
 
     // Operand addresses of tile l_tau.  A request copies 8 rows of 128 bytes;
     // the 16-byte chunks of LDS row r are stored at chunk ^ (r / 2 % 8), so
     // the 16 lanes of a fragment read that are served together find all banks.
     __device__ __forceinline__ void bind() {
-        const Tile t = walk.tile(g, l_tau, TAIL);
+        const Tile t = planned(l_n);
         const int64_t we = (int64_t)(g.e_first + t.e) * g.N + t.n0;
         const bool up = MODE == SWIGLU && wave >= 2;
         const int wrow0 = MODE == SWIGLU ? (wave & 1) * 64 : wave * 64;
@@ -275,10 +294,11 @@ struct TileLoop {
             return;
         }
         l_tau += G;
+        l_n += 1;
         l_idx ^= 1;
         if (np < C::NS - 1 && g.row_map) landed<0>();  // its indices may be on their way
         bind();
-        request_idx(l_tau + G, l_idx ^ 1);
+        plan_tile(l_tau + G, l_n + 1, l_idx ^ 1);
     }
     __device__ __forceinline__ void request_scales() {
         if (l_kp & 3) return;
@@ -565,10 +585,11 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
     L t(g, walk, smem);
     if (first >= t.total) return;
     t.l_tau = first;
-    t.request_idx(first, 0);
+    t.l_n = 0;
+    t.plan_tile(first, 0, 0);
     t.template landed<0>();
     t.bind();
-    t.request_idx(first + t.G, 1);
+    t.plan_tile(first + t.G, 1, 1);
 #pragma unroll
     for (int i = 0; i < C::NS; ++i) {
         t.request_pair();
@@ -588,8 +609,10 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
 
-    for (int tau = first; tau < t.total; tau += t.G) {
-        const Tile tile = walk.tile(g, tau, TAIL);
+    // a tile's weight scales, a word for four pairs, and the first words
+    scalar_words ws0, ws1 = nullptr;
+    uint32_t w0, w1 = 0;
+    auto first_words = [&](const Tile &tile) {
         const int64_t nb = (int64_t)(g.e_first + tile.e) * scale_blocks(g.N) +
                            min((int)(tile.n0 / kScaleBlock) + (MODE == SWIGLU ? 0 : t.wn),
                                scale_blocks(g.N) - 1);
@@ -599,14 +622,16 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
                 (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a) |
                 (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32);
         };
-        const scalar_words ws0 = words(g.s0), ws1 = MODE == SWIGLU ? words(g.s1) : nullptr;
-        uint32_t w0 = ws0[0], w1 = MODE == SWIGLU ? ws1[0] : 0;
-#pragma unroll
-        for (int i = 0; i < C::TN; ++i)
-#pragma unroll
-            for (int j = 0; j < C::TM; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) t.acc[i][j][r] = 0.f;
+        ws0 = words(g.s0);
+        w0 = ws0[0];
+        if (MODE == SWIGLU) {
+            ws1 = words(g.s1);
+            w1 = ws1[0];
+        }
+    };
+    first_words(t.planned(0));
+
+    for (int tau = first, n = 0; tau < t.total; tau += t.G, ++n) {
         // the next pair's scales of the tokens, and behind the pair of the weights
         auto next_scales = [&](int p) {
             if (p + 1 >= t.np || t.c_byte == 3) {
@@ -626,6 +651,12 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
 #pragma unroll
             for (int j = 0; j < C::TM; ++j) t.sx[j] = t.sxn[j];
         };
+#pragma unroll
+        for (int i = 0; i < C::TN; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TM; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) t.acc[i][j][r] = 0.f;
         // b1: the pair's second half's token fragments, n1: the next one's
         auto pair = [&](int p, typename L::FragsB &b1, typename L::FragsB &n1) {
             const int s0 = w0 & 255, s1 = w1 & 255;
@@ -653,6 +684,8 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
             t.second_half(a1, c0, a0, b0, b1, w0 & 255, w1 & 255);
             next_words(whole);
         }
+        const Tile tile = t.planned(n);
+        if (tau + t.G < t.total) first_words(t.planned(n + 1));  // (bound by now)
         epilogue<MODE>(g, tile, t, smem);
     }
     t.template landed<0>();  // requests behind the last pair
