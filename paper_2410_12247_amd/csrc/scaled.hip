@@ -75,28 +75,30 @@ struct Tile {
     int m_valid, n_valid;
 };
 
-// The tiles of all experts, BM token rows high.  TAIL: in launches of at least
-// four tile rows per expert, an expert's last rows, where they fill at most half
-// a tile, are no tile of it but a tail; the tails run behind the tiles, as tiles
-// of half the height and a fraction of the time, and are dealt out from the first
-// workgroup that the tiles' last round leaves without one.  So the last round
-// is a short one instead of a whole one: DBRX gate of 8192 tokens (768 tiles, 54
-// tails, 256 workgroups) 288 -> 275 us.  With fewer tile rows reading the weights
-// again costs more than it saves: DeepSeekV2 FFN of 8192 tokens (a tile and a
-// tail per expert) 241 -> 256.
+// The tiles of all experts, BM token rows high.  TAIL: an expert's last rows,
+// where they fill at most half a tile and are all it has or follow at least
+// four whole tiles, are no tile of it but a tail; the tails run behind the
+// tiles, as tiles of half the height and a fraction of the time, and are dealt
+// out from the first workgroup that the tiles' last round leaves without one.
+// So experts of few rows cost less, and the last round is a short one instead
+// of a whole one: DBRX gate of 8192 tokens (768 tiles, 54 tails, 256
+// workgroups) 288 -> 275 us.  Behind fewer tiles, reading the weights again
+// costs more than it saves: DeepSeekV2 FFN of 8192 tokens (a tile and some 50
+// rows per expert) 241 -> 256.
 template <class C, bool TAIL>
 struct Walk {
     int *s_off, *s_tile, *s_tail;  // e_count + 1 ints each in LDS
-    int NT, tiles, tails, least;  // least: a last row of tiles has more rows than this
-    __device__ __forceinline__ int tile_rows(int cnt) const {
-        return cnt / C::BM + (cnt % C::BM > least);
+    int NT, tiles, tails;
+    static __device__ __forceinline__ int tile_rows(int cnt) {
+        const int n = cnt / C::BM, rest = cnt % C::BM;
+        const bool tail = TAIL && rest <= C::BM / 2 && (n == 0 || n >= 4);
+        return n + (rest > 0 && !tail);
     }
     __device__ __forceinline__ Walk(const ScaledGemm &g, int *lds) {
         s_off = lds;
         s_tile = lds + kMaxExperts + 1;
         s_tail = lds + 2 * (kMaxExperts + 1);
         NT = (g.N + C::BNOUT - 1) / C::BNOUT;
-        least = TAIL ? C::BM / 2 : 0;
         const int tid = threadIdx.x, lane = tid & 63;
         for (int i = tid; i <= g.e_count; i += C::THREADS)
             s_off[i] = g.offsets ? g.offsets[g.e_first + i] : (i == 0 ? 0 : (int)g.rows_one);
@@ -127,14 +129,6 @@ struct Walk {
         __syncthreads();
         tiles = __builtin_amdgcn_readfirstlane(s_tile[g.e_count]);
         tails = __builtin_amdgcn_readfirstlane(s_tail[g.e_count]);
-        if (TAIL && tails > 0 && tiles < 4 * NT * g.e_count) {  // tiles like the others
-            __syncthreads();
-            s_tile[tid + 1] += s_tail[tid + 1];
-            tiles += tails;
-            tails = 0;
-            least = 0;
-            __syncthreads();
-        }
     }
     // tile tau of the tiles (tail false) or of the tails
     __device__ __forceinline__ Tile tile(const ScaledGemm &g, int tau, bool tail) const {
