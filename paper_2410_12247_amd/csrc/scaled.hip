@@ -9,6 +9,7 @@ namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // buffer resource word 3 for raw (untyped, unswizzled) access on gfx9 parts
 constexpr int kBufferFlags = 0x00020000;
@@ -361,24 +362,65 @@ struct TileLoop {
                    (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
     }
 
-    // One half's MFMAs, and between them the parts f(m, n) of its reads and
-    // requests, m of n.  (The sums count as used behind them: the compiler would
-    // move the MFMAs behind branches that follow, away from those.)
-    static constexpr int NM = C::TN * C::TM;
+    // The gate/up launch of few rows per expert (64-row tiles) is bound by the
+    // weight stream, so its products can be exact: e4m3 widened to bf16, in which
+    // products and sums are exact to fp32, at half the rate.  An error of 2e-5 of
+    // a sum, which the 8-bit instruction has, moves one quantised value in
+    // some thousands to its neighbour, which a row of few large values shows
+    // (DBRX FFN of 64 tokens: off by 1.9 to 3.7e-3 with it, 1.7e-3 without, all of
+    // that the output's bf16), at 3% of the time (93.8 -> 96.7 us); with more rows
+    // it is lost in the rest.
+    static constexpr bool EXACT = MODE == SWIGLU && BM_ == 64;
+    // e4m3 values of a lane's 32 bytes, 8 (part) to 8 (part) + 7, times scale
+    __device__ __forceinline__ static bf16x8 widen(const u32x4 (&v)[2], int part, float scale) {
+        const uint32_t lo = v[part >> 1][2 * (part & 1)], hi = v[part >> 1][2 * (part & 1) + 1];
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+        const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+        return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+    // The product of two scales as a float (a scale byte of 255 stays NaN).
+    __device__ __forceinline__ static float both(int s, int t) {
+        const int e = s == 255 || t == 255 ? 255 : min(max(s + t - 127, 1), 254);
+        return __uint_as_float((uint32_t)e << 23);
+    }
+    // One half's MFMAs, and between them the parts f(m) of NM of its reads and
+    // requests.  (The sums count as used behind them: the compiler would move the
+    // MFMAs behind branches that follow, away from those.)
+    static constexpr int NM = C::TN * C::TM * (EXACT ? 4 : 1);
     template <class F>
     __device__ __forceinline__ void half(const FragsA &a, const FragsB &b, int sw0, int sw1,
                                          F &&f) {
+        if constexpr (EXACT) {
+            static_assert(C::TM == 1, "one token fragment");
+            const float sg = both(sx[0], sw0), su = both(sx[0], sw1);
 #pragma unroll
-        for (int m = 0; m < NM; ++m) {
-            const int i = m / C::TM, j = m % C::TM;
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                whole(a.v[i]), whole(b.v[j]), acc[i][j], 0, 0, 0,
-                MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
-            f(m);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int h = 0; h < 4; ++h) {
+                const bf16x8 bg = widen(b.v[0], h, sg), bu = widen(b.v[0], h, su);
+#pragma unroll
+                for (int i = 0; i < C::TN; ++i) {
+                    acc[i][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        widen(a.v[i], h, 1.0f), i >= 2 ? bu : bg, acc[i][0], 0, 0, 0);
+                    f(h * C::TN + i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int m = 0; m < NM; ++m) {
+                const int i = m / C::TM, j = m % C::TM;
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                    whole(a.v[i]), whole(b.v[j]), acc[i][j], 0, 0, 0,
+                    MODE == SWIGLU && i >= 2 ? sw1 : sw0, 0, sx[j]);
+                f(m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
 #pragma unroll
-        for (int m = 0; m < NM; ++m) asm volatile("" : "+a"(acc[m / C::TM][m % C::TM]));
+        for (int i = 0; i < C::TN; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TM; ++j) asm volatile("" : "+a"(acc[i][j]));
     }
     // requests younger than the next pair's once a pair's token rows are requested
     static constexpr int AHEAD = C::XI + (C::NS - 2) * C::LPS;

@@ -359,6 +359,39 @@ def test_gemm_keeps_a_nan_in_its_row_and_column(R):
     assert torch.equal(got[:R - 1, :N - 1], clean[:R - 1, :N - 1])
 
 
+@gpu
+@pytest.mark.parametrize("R", [3, 30, 90, 400])
+def test_scale_byte_255_is_nan(R):
+    g = gen(R)
+    N, K = 192, 320
+    xq, wq = ref.small_integers(g, R, K), ref.small_integers(g, N, K)
+    xs, ws = ref.scale_bytes(g, R, K), ref.scale_bytes(g, ref.blocks(N), K)
+    clean = ref.widen(xq, xs, 1) @ ref.widen(wq, ws, 128).T
+    xs[R - 1, 2] = 255
+    ws[1, 1] = 255  # weight rows 128 to 191
+    got = run_gemm(xq, xs, wq, ws, F32).double()
+    assert bool(got[R - 1].isnan().all()) and bool(got[:, 128:].isnan().all())
+    assert torch.equal(got[:R - 1, :128], clean[:R - 1, :128])
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 40, 200])
+def test_ffn_keeps_a_nan_scale_in_its_token(T):
+    E, k, H, I = 4, 2, 192, 192
+    g = gen(T)
+    off, slot, cap = dispatch(g, T, E, k, 0, E, None)
+    d = moe.dims(T, H, I, E, k)
+    t = ffn_inputs(g, T, H, I, E)
+    ws = torch.empty(moe.scaled_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    y, z = torch.zeros((cap, H), device="cuda"), torch.zeros((cap, H), device="cuda")
+    moe.ffn_group_scaled(d, 0, E, cuda(off), cuda(slot), *t, y, ws)
+    t[1][T - 1, 1] = 255
+    moe.ffn_group_scaled(d, 0, E, cuda(off), cuda(slot), *t, z, ws)
+    mine = (slot[:int(off[E])] // k == T - 1).cuda()
+    assert int(mine.sum()) == k and bool(z[mine].isnan().all())
+    assert torch.equal(z[~mine], y[~mine])
+
+
 def dispatch(g, T, E, k, e0, EL, weights=None):
     """Distinct experts per token; (offsets, sorted_slot) as moe.permute."""
     p = torch.rand((T, E), generator=g) if weights is None else \
