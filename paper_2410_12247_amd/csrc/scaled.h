@@ -37,9 +37,11 @@ struct ScaledGemm {
     uint8_t *out_s;  // their scales
 };
 // What a launch's form is chosen by: the rows expected in all and the experts
-// expected to have any.
+// expected to have any, the most rows an expert can have and the experts.
 struct ScaledLoad {
     double rows, active;
+    int64_t max_rows;
+    int experts;
 };
 
 // y = x w^T, y_type MOE_FP32 or MOE_BF16.
@@ -57,6 +59,12 @@ constexpr int scaled_tiles(bool swiglu, int n) { return (n + (swiglu ? 127 : 255
 hipError_t launch_stream_scaled(const ScaledGemm &g, int y_type, bool from_h,
                                 const ScaledLoad &load, hipStream_t s);
 hipError_t launch_stream_swiglu(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s);
+
+// Products of a few dozen to some hundred rows; form: scaled_mid_form's, -1 where
+// the tiled launch is faster.
+int scaled_mid_form(int N, const ScaledLoad &load);
+hipError_t launch_mid_scaled(const ScaledGemm &g, int y_type, int form, int64_t max_rows,
+                             hipStream_t s);
 
 // Rows quantised, with (norm) or without the residual addition and RMS norm.
 hipError_t launch_norm_quant(int64_t rows, int cols, const void *x, int x_type,

@@ -63,13 +63,19 @@ ScaledLoad expected_load(const moe_dims &d) {
     const double p = (double)d.top_k / d.experts;
     l.rows = (double)d.tokens * p * d.local_count;
     l.active = d.local_count * (1.0 - std::pow(1.0 - p, (double)d.tokens));
+    l.max_rows = d.tokens;  // a token routes to an expert at most once
+    l.experts = d.local_count;
     return l;
 }
 
+ScaledLoad dense_load(int64_t rows) { return {(double)rows, 1.0, rows, 1}; }
+
 hipError_t product(const ScaledGemm &g, int y_type, const ScaledLoad &load, hipStream_t s) {
-    return scaled_stream_fits(scaled_tiles(false, g.N), load)
-               ? launch_stream_scaled(g, y_type, false, load, s)
-               : launch_scaled_gemm(g, y_type, load, s);
+    if (scaled_stream_fits(scaled_tiles(false, g.N), load))
+        return launch_stream_scaled(g, y_type, false, load, s);
+    const int mid = scaled_mid_form(g.N, load);
+    return mid >= 0 ? launch_mid_scaled(g, y_type, mid, load.max_rows, s)
+                    : launch_scaled_gemm(g, y_type, load, s);
 }
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
@@ -114,7 +120,7 @@ moe_status ffn(ScaledGemm rows, int32_t hidden, int32_t inter, Matrix gate, Matr
     h.N = hidden, h.K = inter;
     h.out = y;
     MOE_HIP(L.stream ? launch_stream_scaled(h, y_type, true, load, s)
-                     : launch_scaled_gemm(h, y_type, load, s));
+                     : product(h, y_type, load, s));
     return MOE_OK;
 }
 
@@ -130,7 +136,7 @@ LayerWs layer_ws(const moe_dims *d) {
     w.perm = ws_layout(d, nullptr);
     w.routed = ffn_ws(d);
     w.shared = d->shared_inter > 0
-                   ? ffn_ws(d->tokens, d->shared_inter, ScaledLoad{(double)d->tokens, 1.0})
+                   ? ffn_ws(d->tokens, d->shared_inter, dense_load(d->tokens))
                    : FfnWs{};
     size_t o = up(w.perm.total);
     auto take = [&](size_t bytes) {
@@ -241,7 +247,7 @@ moe_status moe_gemm_scaled(int64_t rows, int32_t n, int32_t k, const moe_e4m3 *x
     g.w0 = w, g.s0 = w_scales;
     g.N = n, g.K = k;
     g.out = y;
-    MOE_HIP(product(g, y_type, ScaledLoad{(double)rows, 1.0}, (hipStream_t)stream));
+    MOE_HIP(product(g, y_type, dense_load(rows), (hipStream_t)stream));
     return MOE_OK;
 }
 
@@ -419,7 +425,7 @@ moe_status moe_forward_scaled(const moe_dims *dims, const void *x, int32_t x_typ
         g.rows_one = d.tokens;
         MOE_TRY(ffn(g, d.hidden, d.shared_inter, {w.shared_gate, w.shared_gate_scales},
                     {w.shared_up, w.shared_up_scales}, {w.shared_down, w.shared_down_scales}, y,
-                    MOE_FP32, L.shared, base + L.ffn, ScaledLoad{(double)d.tokens, 1.0}, s));
+                    MOE_FP32, L.shared, base + L.ffn, dense_load(d.tokens), s));
     }
     g.offsets = off;
     g.e_count = d.local_count;
