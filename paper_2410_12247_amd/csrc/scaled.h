@@ -60,11 +60,10 @@ hipError_t launch_stream_scaled(const ScaledGemm &g, int y_type, bool from_h,
                                 const ScaledLoad &load, hipStream_t s);
 hipError_t launch_stream_swiglu(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s);
 
-// Products of a few dozen to some hundred rows; form: scaled_mid_form's, -1 where
-// the tiled launch is faster.
-int scaled_mid_form(int N, const ScaledLoad &load);
-hipError_t launch_mid_scaled(const ScaledGemm &g, int y_type, int form, int64_t max_rows,
-                             hipStream_t s);
+// Products of a few dozen to some hundred rows, where the tiled launch has too
+// few tiles (scaled_mid_fits).
+bool scaled_mid_fits(int N, const ScaledLoad &load);
+hipError_t launch_mid_scaled(const ScaledGemm &g, int y_type, int64_t max_rows, hipStream_t s);
 
 // Rows quantised, with (norm) or without the residual addition and RMS norm.
 hipError_t launch_norm_quant(int64_t rows, int cols, const void *x, int x_type,

@@ -31,21 +31,23 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
 }
 
 // ---------------------------------------------------------------------------
-// Tile of 256 weight rows x BM token rows, four waves (one per SIMD) in a 2 x 2
-// arrangement, each with a 128 x BM/2 accumulator block of 32 x 32 MFMAs (the
+// Tile of BN weight rows x BM token rows, four waves (one per SIMD) in a 2 x 2
+// arrangement, each with a BN/2 x BM/2 accumulator block of 32 x 32 MFMAs (the
 // blocks' token rows alternate by 32, so a tile of few rows keeps all waves
 // busy).
 // K advances by pairs of 64 (one MFMA's K, so a pair is a scale block) through
-// two or three LDS buffers filled by LDS-DMA with whole 128-byte lines of the rows.
+// two to four LDS buffers filled by LDS-DMA with whole 128-byte lines of the rows.
 // ---------------------------------------------------------------------------
-template <int MODE, int BM_>
+template <int MODE, int BM_, int BN_>
 struct Cfg {
-    static constexpr int BM = BM_;
-    static constexpr int BN = 256;                            // weight rows of the tile
-    static constexpr int BNOUT = MODE == SWIGLU ? 128 : 256;  // output columns
+    static constexpr int BM = BM_, BN = BN_;                 // token and weight rows of the tile
+    static constexpr int BNOUT = MODE == SWIGLU ? 128 : BN;  // output columns
+    static_assert(BN == 256 || (BN == 128 && MODE != SWIGLU), "whole scale blocks per tile");
     static constexpr int THREADS = 256;
-    static constexpr int BK = 128, NS = BM_ >= 128 ? 2 : 3;  // bytes of a row per pair, LDS buffers
-    static constexpr int WTN = 128, WTM = BM / 2;
+    static constexpr int BK = 128;  // bytes of a row per pair
+    // LDS buffers: 96 to 128 KB
+    static constexpr int NS = BM + BN > 320 ? 2 : BM + BN > 192 ? 3 : 4;
+    static constexpr int WTN = BN / 2, WTM = BM / 2;
     static constexpr int TN = WTN / 32, TM = WTM / 32;
     static constexpr int WI = BN / 8 / 4, XI = BM / 8 / 4;  // LDS-DMA requests per wave and pair
     static constexpr int LPS = WI + XI;
@@ -53,7 +55,7 @@ struct Cfg {
     static constexpr int ES = MODE == OUT_F32 ? 4 : 2;
     // LDS: ring | token scales [SG][256] words | row indices [2][256] | tiles
     // ahead [4 waves][PLAN][8] | epilogue scratch | expert offsets
-    static constexpr int SG = 4;
+    static constexpr int SG = NS < 4 ? 4 : 8;  // more than NS
     static constexpr int SCALES = NS * STAGE;
     static constexpr int IDX = SCALES + SG * 1024;
     static constexpr int PLAN = 8;
@@ -168,9 +170,9 @@ __device__ __forceinline__ void wait_vmcnt() {
 }
 
 // TAIL: the tiles are the walk's tails.
-template <int MODE, int BM_, bool TAIL, class W>
+template <int MODE, int BM_, int BN_, bool TAIL, class W>
 struct TileLoop {
-    using C = Cfg<MODE, BM_>;
+    using C = Cfg<MODE, BM_, BN_>;
     struct FragsA {
         u32x4 v[C::TN][2];
     };
@@ -241,7 +243,7 @@ struct TileLoop {
         const Tile t = planned(l_n);
         const int64_t we = (int64_t)(g.e_first + t.e) * g.N + t.n0;
         const bool up = MODE == SWIGLU && wave >= 2;
-        const int wrow0 = MODE == SWIGLU ? (wave & 1) * 64 : wave * 64;
+        const int wrow0 = (MODE == SWIGLU ? wave & 1 : wave) * (C::BN / 4);
         wres = buf_rsrc((up ? g.w1 : g.w0) + we * K);
         int ln = threadIdx.x & 63;  // opaque: its products are not kept over the K loop
         asm volatile("" : "+v"(ln));
@@ -345,7 +347,7 @@ struct TileLoop {
     __device__ __forceinline__ void read_a(FragsA &f, int r, int hf) const {
         const int i = r >> 1;
         const int w0 = MODE == SWIGLU ? (i >= 2 ? 128 : 0) + wn * 64 + (i & 1) * 32
-                                      : wn * 128 + i * 32;
+                                      : wn * C::WTN + i * 32;
         f.v[i][r & 1] = read(w0, r & 1, hf);
     }
     __device__ __forceinline__ void read_b(FragsB &f, int r, int hf) const {
@@ -600,7 +602,7 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
                 for (int q = 0; q < 32 / RPI; ++q) {
                     const int rr = q * RPI + lane / CPR, chunk = lane % CPR;
                     const int row = loop.row0(j) + rr;
-                    const int col = wn * 128 + ib * 32 + chunk * (16 / C::ES);
+                    const int col = wn * C::WTN + ib * 32 + chunk * (16 / C::ES);
                     const u32x4 v =
                         *reinterpret_cast<const u32x4 *>(sc + rr * C::SC_ROW + chunk * 16);
                     store(v, row < t.m_valid && col < t.n_valid,
@@ -613,10 +615,10 @@ __device__ __forceinline__ void epilogue(const ScaledGemm &g, const Tile &t, L &
 
 // The workgroup's share of the tiles, or of the tails: `first` and every
 // gridDim.x-th one behind it.
-template <int MODE, int BM_, bool TAIL, class W>
+template <int MODE, int BM_, int BN_, bool TAIL, class W>
 __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, int first,
                                           char *smem) {
-    using L = TileLoop<MODE, BM_, TAIL, W>;
+    using L = TileLoop<MODE, BM_, BN_, TAIL, W>;
     using C = typename L::C;
     L t(g, walk, smem);
     if (first >= t.total) return;
@@ -650,7 +652,7 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
     uint32_t w0, w1 = 0;
     auto first_words = [&](const Tile &tile) {
         const int64_t nb = (int64_t)(g.e_first + tile.e) * scale_blocks(g.N) +
-                           min((int)(tile.n0 / kScaleBlock) + (MODE == SWIGLU ? 0 : t.wn),
+                           min((int)(tile.n0 / kScaleBlock) + (C::WTN == 128 && MODE != SWIGLU ? t.wn : 0),
                                scale_blocks(g.N) - 1);
         auto words = [&](const uint8_t *s) {
             const uint64_t a = (uint64_t)(uintptr_t)(s + nb * t.SK);
@@ -727,9 +729,9 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
     t.template landed<0>();  // requests behind the last pair
 }
 
-template <int MODE, int BM_>
+template <int MODE, int BM_, int BN_>
 __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
-    using C = Cfg<MODE, BM_>;
+    using C = Cfg<MODE, BM_, BN_>;
     constexpr bool TAILS = BM_ == 256;
     __shared__ __attribute__((aligned(16))) char smem[C::LDS_BYTES];
     using W = Walk<C, TAILS>;
@@ -737,37 +739,96 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
     // neighbouring tiles on one XCD
     const int G = gridDim.x;  // a multiple of NXCD
     const int slot = (blockIdx.x % NXCD) * (G / NXCD) + blockIdx.x / NXCD;
-    run_tiles<MODE, BM_, false>(g, walk, slot, smem);
+    run_tiles<MODE, BM_, BN_, false>(g, walk, slot, smem);
     if constexpr (TAILS) {
-        static_assert(Cfg<MODE, 128>::INTS <= C::INTS, "the offsets lie behind both layouts");
+        static_assert(Cfg<MODE, 128, BN_>::INTS <= C::INTS, "the offsets lie behind both layouts");
         if (walk.tails > 0) {
             const int used = walk.tiles % G;
-            run_tiles<MODE, 128, true>(g, walk, slot >= used ? slot - used : slot + G - used,
+            run_tiles<MODE, 128, BN_, true>(g, walk, slot >= used ? slot - used : slot + G - used,
                                        smem);
         }
     }
 }
 
-template <int MODE>
-hipError_t go(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
-    const unsigned grid = (unsigned)std::max(NXCD, device_cu_count() / NXCD * NXCD);
-    if (load.rows / load.active > 128)
-        tile_kernel<MODE, 256><<<grid, 256, 0, s>>>(g);
-    else if (load.rows / load.active <= 64)
-        tile_kernel<MODE, 64><<<grid, 256, 0, s>>>(g);
-    else
-        tile_kernel<MODE, 128><<<grid, 256, 0, s>>>(g);
+// Tile rows of all experts at a height of bm, expected under uniform routing: an
+// expert's rows are then about normal with the mean m and the variance v.
+double expected_tile_rows(const ScaledLoad &l, int bm) {
+    if (l.rows <= 0) return 0;
+    const double m = l.rows / l.experts, p = std::min(1.0, m / (double)l.max_rows);
+    const double v = m * (1 - p);
+    if (v < 1e-9 || m > 64.0 * bm)
+        return l.experts * (v < 1e-9 ? std::ceil(m / bm) : m / bm + 0.5);
+    double rows = l.active / l.experts;  // P(any)
+    for (int j = 1; j * (double)bm < m + 6 * std::sqrt(v) + 1; ++j)  // + P(more than j bm)
+        rows += 0.5 * std::erfc((j * (double)bm + 0.5 - m) / std::sqrt(2 * v));
+    return l.experts * rows;
+}
+
+// The tile of a launch: the one whose rounds over the chip are expected to take
+// least, from the measured us per pair of K (a round of full tiles) and per tile.
+// 256 x 256 (weight x token rows) does 1.0 of the work per time, 256 x 128 0.8,
+// 128 x 128 0.7 and 128 x 64 0.5, but more and smaller tiles fill the chip:
+// 1500 x 4096 x 4096 (96, 192, 384 and 768 tiles) 52.2, 33.0, 36.3 and 41.7 us,
+// 300 x 5120 x 1536 (40, 60, 120 and 200) 23.2, 15.8, 11.4 and 10.2.  A smaller
+// tile has to promise an eighth less: a large one's rounds take less than
+// counted where its rows are not all valid (DeepSeekV2 FFN of 8192 tokens, 307
+// rows per expert: 239 us, with 128-row tiles counted 7% less 261).
+struct Form {
+    int bm, bn;
+    double pair, tile;
+};
+int pick_form(const Form *forms, int count, const ScaledGemm &g, int columns,
+              const ScaledLoad &load, unsigned grid) {
+    int best = 0;
+    double least = 0;
+    for (int i = 0; i < count; ++i) {
+        const Form &f = forms[i];
+        const int nt = (g.N + (columns ? columns : f.bn) - 1) / (columns ? columns : f.bn);
+        const double tiles = expected_tile_rows(load, f.bm) * nt;
+        const double us = std::ceil(tiles / grid) * (scale_blocks(g.K) * f.pair + f.tile);
+        if (i == 0 || us < 0.875 * least) {
+            best = i;
+            least = us;
+        }
+    }
+    return best;
+}
+
+template <int MODE, int BM, int BN>
+hipError_t go(const ScaledGemm &g, unsigned grid, hipStream_t s) {
+    tile_kernel<MODE, BM, BN><<<grid, 256, 0, s>>>(g);
     return hipGetLastError();
+}
+unsigned tile_grid() { return (unsigned)std::max(NXCD, device_cu_count() / NXCD * NXCD); }
+
+template <int MODE>
+hipError_t go_out(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
+    static const Form forms[] = {
+        {256, 256, 1.48, 3.5}, {128, 256, 0.90, 3.0}, {128, 128, 0.55, 1.6}, {64, 128, 0.39, 1.6}};
+    const unsigned grid = tile_grid();
+    switch (pick_form(forms, 4, g, 0, load, grid)) {
+        case 0: return go<MODE, 256, 256>(g, grid, s);
+        case 1: return go<MODE, 128, 256>(g, grid, s);
+        case 2: return go<MODE, 128, 128>(g, grid, s);
+        default: return go<MODE, 64, 128>(g, grid, s);
+    }
 }
 
 }  // namespace
 
 hipError_t launch_scaled_gemm(const ScaledGemm &g, int y_type, const ScaledLoad &load,
                               hipStream_t s) {
-    return y_type == MOE_FP32 ? go<OUT_F32>(g, load, s) : go<OUT_BF16>(g, load, s);
+    return y_type == MOE_FP32 ? go_out<OUT_F32>(g, load, s) : go_out<OUT_BF16>(g, load, s);
 }
 hipError_t launch_scaled_swiglu(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
-    return go<SWIGLU>(g, load, s);
+    static const Form forms[] = {
+        {256, 256, 1.48, 4.5}, {128, 256, 0.90, 3.5}, {64, 256, 0.73, 3.0}};
+    const unsigned grid = tile_grid();
+    switch (pick_form(forms, 3, g, 128, load, grid)) {  // 128 gate and 128 up rows
+        case 0: return go<SWIGLU, 256, 256>(g, grid, s);
+        case 1: return go<SWIGLU, 128, 256>(g, grid, s);
+        default: return go<SWIGLU, 64, 256>(g, grid, s);
+    }
 }
 
 }  // namespace moe

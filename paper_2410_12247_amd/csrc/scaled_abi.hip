@@ -73,9 +73,8 @@ ScaledLoad dense_load(int64_t rows) { return {(double)rows, 1.0, rows, 1}; }
 hipError_t product(const ScaledGemm &g, int y_type, const ScaledLoad &load, hipStream_t s) {
     if (scaled_stream_fits(scaled_tiles(false, g.N), load))
         return launch_stream_scaled(g, y_type, false, load, s);
-    const int mid = scaled_mid_form(g.N, load);
-    return mid >= 0 ? launch_mid_scaled(g, y_type, mid, load.max_rows, s)
-                    : launch_scaled_gemm(g, y_type, load, s);
+    return scaled_mid_fits(g.N, load) ? launch_mid_scaled(g, y_type, load.max_rows, s)
+                                      : launch_scaled_gemm(g, y_type, load, s);
 }
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }

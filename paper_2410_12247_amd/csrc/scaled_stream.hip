@@ -211,21 +211,22 @@ __global__ __launch_bounds__(64 * W) void stream_kernel(ScaledGemm g) {
 
 // ---------------------------------------------------------------------------
 // Products of a few dozen to some hundred rows, where the tiled launch has too
-// few tiles for the chip.  A workgroup owns 16 NT weight rows x 16 MT token rows
+// few tiles for the chip.  A workgroup owns 32 weight rows x 32 token rows
 // over the whole of K; its eight waves take blocks of 128 k in turn, each
 // straight from memory into the scaled matrix instruction's operands, two
 // blocks in flight per wave, and their sums meet in LDS and are added in wave
-// order.  So the chain of a launch is an eighth of K long, and there are
-// (N / 16 NT) (rows / 16 MT) workgroups; every operand row is read once per
-// workgroup, from the L2.  Tiled -> this, GPU us, rows x N x K: 20 x 4096 x 4096
-// 20.7 -> 11.0, 128 x 4096 x 4096 27.8 -> 17.5, 300 x 1152 x 1024 17.0 -> 7.5,
-// 700 x 1024 x 4096 43.0 -> 23.9; 300 x 4096 x 4096 (320 workgroups of the largest
-// form) 45.9 -> 42.4, 1500 x 1152 x 1024 (432) 19.2 -> 19.8.
+// order.  So the chain of a launch is an eighth of K long; every operand row is
+// read once per workgroup, from the L2.  Tiles of 64 x 128 -> this, GPU us, rows
+// x N x K: 20 x 4096 x 4096 17.7 -> 10.9, 40 x 1024 x 4096 15.4 -> 12.0, 128 x 1152
+// x 1024 7.6 -> 5.7, 300 x 512 x 1024 7.2 -> 5.7.
+// (Tiles of 64 x 32 and 64 x 64 per workgroup serve more rows at once, but no
+// faster than the tiled launch: 700 x 1152 x 1024 10.7 against 8.4.)
 // ---------------------------------------------------------------------------
+constexpr int MNT = 2, MMT = 2;
 constexpr int MW = 8, MD = 2;
-template <int MODE, int NT, int MT>
+template <int MODE>
 __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
-    __shared__ __attribute__((aligned(16))) floatx4 part[MW][NT * MT][64];
+    __shared__ __attribute__((aligned(16))) floatx4 part[MW][MNT * MMT][64];
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int e = blockIdx.z;
@@ -234,22 +235,22 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
         row0 = __builtin_amdgcn_readfirstlane(g.offsets[g.e_first + e]);
         cnt = __builtin_amdgcn_readfirstlane(g.offsets[g.e_first + e + 1]) - row0;
     }
-    const int m0 = blockIdx.y * 16 * MT;
+    const int m0 = blockIdx.y * 16 * MMT;
     if (m0 >= cnt) return;
     const int K = g.K, SK = scale_pitch(K), nb = scale_blocks(K);
-    const int n0 = blockIdx.x * 16 * NT;
+    const int n0 = blockIdx.x * 16 * MNT;
     const int64_t we = (int64_t)(g.e_first + e) * g.N + n0;
     const int64_t se = (int64_t)(g.e_first + e) * scale_blocks(g.N) + n0 / kScaleBlock;
     const __amdgpu_buffer_rsrc_t wr = rsrc(g.w0 + we * K), sr = rsrc(g.s0 + se * SK);
     const int64_t first = (int64_t)row0 + m0;
     const __amdgpu_buffer_rsrc_t xr = rsrc(g.x + (g.row_map ? 0 : first * K));
     const __amdgpu_buffer_rsrc_t xsr = rsrc(g.xs + (g.row_map ? 0 : first * SK));
-    uint32_t woff[NT], xoff[MT], xsoff[MT];
+    uint32_t woff[MNT], xoff[MMT], xsoff[MMT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int i = 0; i < MNT; ++i)
         woff[i] = (uint32_t)(min(i * 16 + col, g.N - 1 - n0) * K + grp * 16);
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
+    for (int j = 0; j < MMT; ++j) {
         const int r = min(j * 16 + col, cnt - 1 - m0);
         const uint32_t src =
             g.row_map ? (uint32_t)(g.row_map[first + r] / g.slot_div) : (uint32_t)r;
@@ -257,8 +258,8 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
         xsoff[j] = src * (uint32_t)SK;
     }
     struct Step {
-        u32x4 a[NT][2], b[MT][2];
-        int sw, sx[MT];
+        u32x4 a[MNT][2], b[MMT][2];
+        int sw, sx[MMT];
     };
     auto load = [&](Step &s, int kb) {  // nothing (zeros) behind K
         const uint32_t k = (uint32_t)kb * kScaleBlock;
@@ -267,18 +268,18 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+            for (int i = 0; i < MNT; ++i)
                 s.a[i][h] = __builtin_bit_cast(
                     u32x4, __builtin_amdgcn_raw_buffer_load_b128(
                                wr, in[h] ? woff[i] + k + h * 64 : kOutside, 0, 0));
 #pragma unroll
-            for (int j = 0; j < MT; ++j)
+            for (int j = 0; j < MMT; ++j)
                 s.b[j][h] = __builtin_bit_cast(
                     u32x4, __builtin_amdgcn_raw_buffer_load_b128(
                                xr, in[h] ? xoff[j] + k + h * 64 : kOutside, 0, 0));
         }
 #pragma unroll
-        for (int j = 0; j < MT; ++j)
+        for (int j = 0; j < MMT; ++j)
             s.sx[j] =
                 __builtin_amdgcn_raw_buffer_load_b8(xsr, kb < nb ? xsoff[j] + kb : kOutside, 0, 0);
     };
@@ -286,11 +287,11 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
         return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3],
                    (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
     };
-    floatx4 acc[NT][MT];
+    floatx4 acc[MNT][MMT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int i = 0; i < MNT; ++i)
 #pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < MMT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     Step s[MD];
 #pragma unroll
     for (int d = 0; d < MD; ++d) load(s[d], wave + MW * d);
@@ -298,9 +299,9 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
 #pragma unroll
         for (int d = 0; d < MD; ++d) {
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+            for (int i = 0; i < MNT; ++i)
 #pragma unroll
-                for (int j = 0; j < MT; ++j)
+                for (int j = 0; j < MMT; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
                         whole(s[d].a[i]), whole(s[d].b[j]), acc[i][j], 0, 0, 0, s[d].sw, 0,
                         s[d].sx[j]);
@@ -308,15 +309,15 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
         }
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int i = 0; i < MNT; ++i)
 #pragma unroll
-        for (int j = 0; j < MT; ++j) part[wave][i * MT + j][lane] = acc[i][j];
+        for (int j = 0; j < MMT; ++j) part[wave][i * MMT + j][lane] = acc[i][j];
     __syncthreads();
-    for (int q = wave; q < NT * MT; q += MW) {
+    for (int q = wave; q < MNT * MMT; q += MW) {
         floatx4 v = part[0][q][lane];
 #pragma unroll
         for (int w = 1; w < MW; ++w) v += part[w][q][lane];
-        const int r = m0 + (q % MT) * 16 + col, n = n0 + q / MT * 16 + grp * 4;
+        const int r = m0 + (q % MMT) * 16 + col, n = n0 + q / MMT * 16 + grp * 4;
         if (r >= cnt || n >= g.N) continue;
         const int64_t at = ((int64_t)row0 + r) * g.N + n;
         if (MODE == OUT_BF16) {
@@ -330,11 +331,11 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
     }
 }
 
-template <int MODE, int NT, int MT>
+template <int MODE>
 hipError_t go_mid(const ScaledGemm &g, int64_t max_rows, hipStream_t s) {
-    const dim3 grid((unsigned)((g.N + 16 * NT - 1) / (16 * NT)),
-                    (unsigned)((max_rows + 16 * MT - 1) / (16 * MT)), (unsigned)g.e_count);
-    mid_kernel<MODE, NT, MT><<<grid, 64 * MW, 0, s>>>(g);
+    const dim3 grid((unsigned)((g.N + 16 * MNT - 1) / (16 * MNT)),
+                    (unsigned)((max_rows + 16 * MMT - 1) / (16 * MMT)), (unsigned)g.e_count);
+    mid_kernel<MODE><<<grid, 64 * MW, 0, s>>>(g);
     return hipGetLastError();
 }
 
@@ -369,29 +370,17 @@ bool scaled_stream_fits(int tiles_n, const ScaledLoad &load) {
     return load.rows <= 16 * load.active && 2 * tiles_n * load.active < device_cu_count();
 }
 
-// The smallest form (tile of 32 x 32, 64 x 32 or 64 x 64: 0, 1, 2) whose
-// workgroups the chip runs at once; -1: none, the tiled launch is faster.  Its
-// grid covers the most rows an expert can have, at no more than eight empty
-// workgroups for each that may run.
-int scaled_mid_form(int N, const ScaledLoad &load) {
-    if (load.rows <= 0) return -1;
-    const double cus = device_cu_count(), per = load.rows / load.active;
-    for (int f = 0; f < 3; ++f) {
-        const int n = f == 0 ? 32 : 64, m = f == 2 ? 64 : 32, cols = (N + n - 1) / n;
-        const double grid = (double)cols * load.experts * ((load.max_rows + m - 1) / m);
-        if (cols * load.active * std::ceil(per / m) <= cus && grid <= 9 * cus) return f;
-    }
-    return -1;
+// Where the chip runs the workgroups at once.  The grid covers the most rows an
+// expert can have, at no more than eight empty workgroups for each that may run.
+bool scaled_mid_fits(int N, const ScaledLoad &load) {
+    if (load.rows <= 0) return false;
+    const double cus = device_cu_count(), cols = (N + 16 * MNT - 1) / (16 * MNT);
+    const double grid = cols * load.experts * ((load.max_rows + 16 * MMT - 1) / (16 * MMT));
+    return cols * load.active * std::ceil(load.rows / load.active / (16 * MMT)) <= cus &&
+           grid <= 9 * cus;
 }
-hipError_t launch_mid_scaled(const ScaledGemm &g, int y_type, int form, int64_t max_rows,
-                             hipStream_t s) {
-    if (y_type == MOE_FP32)
-        return form == 0   ? go_mid<OUT_F32, 2, 2>(g, max_rows, s)
-               : form == 1 ? go_mid<OUT_F32, 4, 2>(g, max_rows, s)
-                           : go_mid<OUT_F32, 4, 4>(g, max_rows, s);
-    return form == 0   ? go_mid<OUT_BF16, 2, 2>(g, max_rows, s)
-           : form == 1 ? go_mid<OUT_BF16, 4, 2>(g, max_rows, s)
-                       : go_mid<OUT_BF16, 4, 4>(g, max_rows, s);
+hipError_t launch_mid_scaled(const ScaledGemm &g, int y_type, int64_t max_rows, hipStream_t s) {
+    return y_type == MOE_FP32 ? go_mid<OUT_F32>(g, max_rows, s) : go_mid<OUT_BF16>(g, max_rows, s);
 }
 hipError_t launch_stream_scaled(const ScaledGemm &g, int y_type, bool from_h,
                                 const ScaledLoad &load, hipStream_t s) {
