@@ -5,8 +5,7 @@
 // workgroup holds a row (or a wave holds one, for short rows) in registers
 // as fp32, so nothing is read twice and Q sees y before its rounding to
 // bf16.  A lane holds eight consecutive columns, so a block of 128 is one
-// DPP row of 16 lanes and its largest value needs no LDS.  Sum of squares in
-// fp32.
+// DPP row of 16 lanes and its largest value needs no LDS.
 #include <algorithm>
 
 #include "scaled.h"
@@ -68,10 +67,22 @@ __device__ __forceinline__ float row_max(float v) {
     v = fmaxf(v, dpp<0x122>(v));
     return fmaxf(v, dpp<0x121>(v));
 }
-__device__ __forceinline__ float wave_sum(float v) {
+__device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
     return v;
+}
+// The squares of eight columns, and 1 / sqrt(mean + eps) of the row's.  The
+// sum over the row is in 64 bits: an error of rstd moves every value of the
+// row the same way, and with some of them their rounding to 8 bits.
+__device__ __forceinline__ float squares(const float (&s)[VEC]) {
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v = __builtin_fmaf(s[i], s[i], v);
+    return v;
+}
+__device__ __forceinline__ float inverse_rms(double ss, int cols, float eps) {
+    return (float)(1.0 / sqrt(ss / cols + (double)eps));
 }
 
 // One pass' eight columns of every lane: quantised (all lanes take part; a
@@ -124,21 +135,19 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_quant_kern
                 for (int i = 0; i < VEC; ++i) s[p][i] += r[i];
             }
         }
-        float ss = 0.f;
+        double ss = 0.;
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) ss = __builtin_fmaf(s[p][i], s[p][i], ss);
+        for (int p = 0; p < PASSES; ++p) ss += squares(s[p]);
         ss = wave_sum(ss);
         if (WAVES > 1) {
-            __shared__ float part[WAVES];
+            __shared__ double part[WAVES];
             if ((tid & 63) == 0) part[tid >> 6] = ss;
             __syncthreads();
-            ss = 0.f;
+            ss = 0.;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) ss += part[w];
         }
-        const float rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+        const float rstd = inverse_rms(ss, a.cols, a.eps);
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const int col = (p * THREADS + tid) * VEC;
@@ -147,7 +156,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_quant_kern
             float w[VEC];
             if (a.weight) load8(a.weight + col, w);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s[p][i] *= a.weight ? rstd * w[i] : rstd;
+            for (int i = 0; i < VEC; ++i)
+                s[p][i] = a.weight ? s[p][i] * rstd * w[i] : s[p][i] * rstd;
             if (a.y) store8(a.y + row * a.cols + col, s[p]);
         }
     }
@@ -174,20 +184,19 @@ __global__ __launch_bounds__(1024) void norm_quant_long_kernel(NormArgs a) {
     };
     float rstd = 1.f;
     if (NORM) {
-        float ss = 0.f;
+        double ss = 0.;
         for (int col = tid * VEC; col < a.cols; col += 1024 * VEC) {
             float s[VEC];
             load(col, s);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) ss = __builtin_fmaf(s[i], s[i], ss);
+            ss += squares(s);
         }
         ss = wave_sum(ss);
-        __shared__ float part[16];
+        __shared__ double part[16];
         if ((tid & 63) == 0) part[tid >> 6] = ss;
         __syncthreads();
-        ss = 0.f;
+        ss = 0.;
         for (int w = 0; w < 16; ++w) ss += part[w];
-        rstd = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+        rstd = inverse_rms(ss, a.cols, a.eps);
     }
     for (int c0 = 0; c0 < a.cols; c0 += 1024 * VEC) {
         const int col = c0 + tid * VEC;
@@ -201,7 +210,8 @@ __global__ __launch_bounds__(1024) void norm_quant_long_kernel(NormArgs a) {
                 float w[VEC];
                 if (a.weight) load8(a.weight + col, w);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) s[i] *= a.weight ? rstd * w[i] : rstd;
+                for (int i = 0; i < VEC; ++i)
+                    s[i] = a.weight ? s[i] * rstd * w[i] : s[i] * rstd;
                 if (a.y) store8(a.y + row * a.cols + col, s);
             }
         }
