@@ -732,7 +732,7 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
 template <int MODE, int BM_, int BN_>
 __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
     using C = Cfg<MODE, BM_, BN_>;
-    constexpr bool TAILS = BM_ == 256;
+    constexpr bool TAILS = BM_ > 128;
     __shared__ __attribute__((aligned(16))) char smem[C::LDS_BYTES];
     using W = Walk<C, TAILS>;
     const W walk(g, reinterpret_cast<int *>(smem + C::INTS));
@@ -766,13 +766,20 @@ double expected_tile_rows(const ScaledLoad &l, int bm) {
 
 // The tile of a launch: the one whose rounds over the chip are expected to take
 // least, from the measured us per pair of K (a round of full tiles) and per tile.
-// 256 x 256 (weight x token rows) does 1.0 of the work per time, 256 x 128 0.8,
-// 128 x 128 0.7 and 128 x 64 0.5, but more and smaller tiles fill the chip:
+// 256 x 256 (weight x token rows) does 1.0 of the work per time, 256 x 192 0.95,
+// 256 x 128 0.8, 128 x 128 0.7 and 128 x 64 0.5, but more and smaller tiles fill
+// the chip:
 // 1500 x 4096 x 4096 (96, 192, 384 and 768 tiles) 52.2, 33.0, 36.3 and 41.7 us,
 // 300 x 5120 x 1536 (40, 60, 120 and 200) 23.2, 15.8, 11.4 and 10.2.  A smaller
 // tile has to promise an eighth less: a large one's rounds take less than
 // counted where its rows are not all valid (DeepSeekV2 FFN of 8192 tokens, 307
 // rows per expert: 239 us, with 128-row tiles counted 7% less 261).
+// 192 token rows are for one group of rows, whose number is known: 5000 x 2048 x
+// 2048 31.3 -> 25.8 us, 2500 x 4096 x 4096 53.4 -> 43.4, 1501 x 5120 x 1536 24.8 ->
+// 20.6.  Over experts they gain while the loads are even (DeepSeekV2 FFN of 8192
+// tokens 233 -> 215 us) and lose more where they are not, for the rounds that the
+// fuller experts add (the same with exponents of 0.3 and, 4099 tokens, 1.1: 236 ->
+// 266 and 213 -> 222).
 struct Form {
     int bm, bn;
     double pair, tile;
@@ -783,6 +790,7 @@ int pick_form(const Form *forms, int count, const ScaledGemm &g, int columns,
     double least = 0;
     for (int i = 0; i < count; ++i) {
         const Form &f = forms[i];
+        if (f.bm == 192 && load.experts > 1) continue;
         const int nt = (g.N + (columns ? columns : f.bn) - 1) / (columns ? columns : f.bn);
         const double tiles = expected_tile_rows(load, f.bm) * nt;
         const double us = std::ceil(tiles / grid) * (scale_blocks(g.K) * f.pair + f.tile);
@@ -804,12 +812,14 @@ unsigned tile_grid() { return (unsigned)std::max(NXCD, device_cu_count() / NXCD 
 template <int MODE>
 hipError_t go_out(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
     static const Form forms[] = {
-        {256, 256, 1.48, 3.5}, {128, 256, 0.90, 3.0}, {128, 128, 0.55, 1.6}, {64, 128, 0.39, 1.6}};
+        {256, 256, 1.48, 3.5}, {192, 256, 1.16, 3.3}, {128, 256, 0.90, 3.0},
+        {128, 128, 0.55, 1.6}, {64, 128, 0.39, 1.6}};
     const unsigned grid = tile_grid();
-    switch (pick_form(forms, 4, g, 0, load, grid)) {
+    switch (pick_form(forms, 5, g, 0, load, grid)) {
         case 0: return go<MODE, 256, 256>(g, grid, s);
-        case 1: return go<MODE, 128, 256>(g, grid, s);
-        case 2: return go<MODE, 128, 128>(g, grid, s);
+        case 1: return go<MODE, 192, 256>(g, grid, s);
+        case 2: return go<MODE, 128, 256>(g, grid, s);
+        case 3: return go<MODE, 128, 128>(g, grid, s);
         default: return go<MODE, 64, 128>(g, grid, s);
     }
 }

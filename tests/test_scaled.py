@@ -344,6 +344,22 @@ def test_gemm_of_any_values(R, N, K, dtype):
     assert bool(((got - want).abs() <= bound).all())
 
 
+# tiles of 64 x 128, 128 x 128, 128 x 256, 192 x 256 and 256 x 256 (token x weight
+# rows); 192 and 256 again with a tail behind them
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("R,N,K", [(700, 1024, 320), (1100, 1472, 192), (2000, 2112, 320),
+                                   (2500, 3904, 320), (2950, 4160, 192), (5000, 2048, 320),
+                                   (1030, 8256, 64)])
+def test_gemm_of_every_tile(R, N, K, dtype):
+    g = gen(R + N + K)
+    xq, wq = ref.small_integers(g, R, K), ref.small_integers(g, N, K)
+    xs, ws = ref.scale_bytes(g, R, K), ref.scale_bytes(g, ref.blocks(N), K)
+    want = ref.widen(xq, xs, 1) @ ref.widen(wq, ws, 128).T
+    got = run_gemm(xq, xs, wq, ws, dtype)
+    assert torch.equal(got, want.to(F32).to(dtype))
+
+
 @gpu
 @pytest.mark.parametrize("R", [3, 90, 400])
 def test_gemm_keeps_a_nan_in_its_row_and_column(R):
