@@ -54,6 +54,7 @@ hipError_t launch_scaled_swiglu(const ScaledGemm &g, const ScaledLoad &load, hip
 // leaves its rows in fp32 (out [.][N], out_s unused); the product behind it
 // takes them so (from_h: x is fp32) and quantises them as it reads them.
 // tiles_n: column tiles of the (first) tiled launch (scaled_tiles).
+constexpr int64_t kStreamRows = 16;  // per expert that has any
 bool scaled_stream_fits(int tiles_n, const ScaledLoad &load);
 constexpr int scaled_tiles(bool swiglu, int n) { return (n + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); }
 hipError_t launch_stream_scaled(const ScaledGemm &g, int y_type, bool from_h,

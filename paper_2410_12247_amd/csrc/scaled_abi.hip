@@ -80,21 +80,28 @@ hipError_t product(const ScaledGemm &g, int y_type, const ScaledLoad &load, hipS
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
 
 // The SwiGLU rows between an FFN's two products: quantised, or fp32 where the
-// launches of few rows run.
+// launches of few rows run.  few: the most rows that those can be chosen for.
+// A workspace holds either, so that one made for some tokens serves fewer.
 struct FfnWs {
     bool stream;
     size_t act, act_s, total;
 };
-FfnWs ffn_ws(int64_t rows, int32_t inter, const ScaledLoad &load) {
+FfnWs ffn_ws(int64_t rows, int64_t few, int32_t inter, const ScaledLoad &load) {
     FfnWs w;
     w.stream = rows > 0 && scaled_stream_fits(scaled_tiles(true, inter), load);
     w.act = 0;
-    w.act_s = up((size_t)rows * inter * (w.stream ? sizeof(float) : 1));
-    w.total = w.act_s + (w.stream ? 0 : up((size_t)rows * scale_pitch(inter)));
+    w.act_s = up((size_t)rows * inter);
+    w.total = std::max(w.act_s + up((size_t)rows * scale_pitch(inter)),
+                       up((size_t)std::min(rows, few) * inter * sizeof(float)));
     return w;
 }
 FfnWs ffn_ws(const moe_dims *d) {
-    return ffn_ws(row_cap(d), d->inter, expected_load(*d));
+    const int64_t few_tokens = kStreamRows * d->experts / d->top_k;
+    return ffn_ws(row_cap(d), few_tokens * std::min(d->top_k, d->local_count), d->inter,
+                  expected_load(*d));
+}
+FfnWs shared_ws(const moe_dims *d) {
+    return ffn_ws(d->tokens, kStreamRows, d->shared_inter, dense_load(d->tokens));
 }
 
 struct Matrix {
@@ -134,9 +141,7 @@ LayerWs layer_ws(const moe_dims *d) {
     LayerWs w;
     w.perm = ws_layout(d, nullptr);
     w.routed = ffn_ws(d);
-    w.shared = d->shared_inter > 0
-                   ? ffn_ws(d->tokens, d->shared_inter, dense_load(d->tokens))
-                   : FfnWs{};
+    w.shared = d->shared_inter > 0 ? shared_ws(d) : FfnWs{};
     size_t o = up(w.perm.total);
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -343,7 +348,10 @@ moe_status moe_combine_rows(const moe_dims *dims, int32_t e_first, int32_t e_cou
 
 size_t moe_forward_scaled_bytes(const moe_dims *dims) {
     if (check_dims(dims) != MOE_OK) return 0;
-    return layer_ws(dims).total;
+    // (more tokens than that need no router logits)
+    moe_dims few = *dims;
+    few.tokens = std::min(few.tokens, kRouteLogitsMaxTokens);
+    return std::max(layer_ws(dims).total, layer_ws(&few).total);
 }
 
 moe_status moe_forward_scaled(const moe_dims *dims, const void *x, int32_t x_type,

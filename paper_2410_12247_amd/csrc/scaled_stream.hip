@@ -367,7 +367,7 @@ hipError_t go_out(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
 // 64 -> 33, eight tokens 5120 x 1536 (63) 60 -> 34; four tokens 6144 x 1344 (120
 // tiles) 81 and 81, 61 tokens 5120 x 1536 (216) 94 -> 105.
 bool scaled_stream_fits(int tiles_n, const ScaledLoad &load) {
-    return load.rows <= 16 * load.active && 2 * tiles_n * load.active < device_cu_count();
+    return load.rows <= kStreamRows * load.active && 2 * tiles_n * load.active < device_cu_count();
 }
 
 // Where the chip runs the workgroups at once.  The grid covers the most rows an

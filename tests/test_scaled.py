@@ -672,6 +672,20 @@ def test_layer_refusals():
         assert combine(**bad) == 1, (bad, last())
 
 
+@pytest.mark.parametrize("H,I,E,k,e0,EL,Is", [(256, 128, 64, 8, 0, 64, 0), (512, 1344, 16, 4, 0, 16, 0),
+                                              (128, 64, 256, 1, 0, 256, 64),
+                                              (256, 320, 160, 6, 20, 20, 640),
+                                              (64, 704, 8, 2, 7, 1, 0), (64, 64, 1, 1, 0, 1, 64)])
+def test_a_workspace_serves_fewer_tokens(H, I, E, k, e0, EL, Is):
+    last_ffn = last_layer = 0
+    for T in sorted({*range(0, 70), *range(70, 600, 7), *range(600, 5000, 61), 4095, 4096, 4097,
+                     16384}):
+        d = moe.dims(T, H, I, E, k, e0, EL, shared_inter=Is)
+        ffn, layer = moe.scaled_workspace_bytes(d), moe.forward_scaled_bytes(d)
+        assert ffn >= last_ffn and layer >= last_layer, T
+        last_ffn, last_layer = ffn, layer
+
+
 @gpu
 @pytest.mark.parametrize("T,E,k,e0,EL,H", [(1, 8, 2, 0, 8, 64), (37, 16, 4, 4, 8, 320),
                                            (300, 8, 8, 0, 8, 1088)])
