@@ -382,10 +382,10 @@ struct TileLoop {
         const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
         return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
-    // The product of two scales as a float (a scale byte of 255 stays NaN).
-    __device__ __forceinline__ static float both(int s, int t) {
-        const int e = s == 255 || t == 255 ? 255 : min(max(s + t - 127, 1), 254);
-        return __uint_as_float((uint32_t)e << 23);
+    // A scale byte as the float whose exponent it is.  Both operands carry their
+    // own: as one factor the product of two could leave the exponent's range.
+    __device__ __forceinline__ static float scale(int s) {
+        return __uint_as_float((uint32_t)s << 23);
     }
     // One half's MFMAs, and between them the parts f(m) of NM of its reads and
     // requests.  (The sums count as used behind them: the compiler would move the
@@ -396,14 +396,14 @@ struct TileLoop {
                                          F &&f) {
         if constexpr (EXACT) {
             static_assert(C::TM == 1, "one token fragment");
-            const float sg = both(sx[0], sw0), su = both(sx[0], sw1);
+            const float st = scale(sx[0]), sg = scale(sw0), su = scale(sw1);
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                const bf16x8 bg = widen(b.v[0], h, sg), bu = widen(b.v[0], h, su);
+                const bf16x8 bt = widen(b.v[0], h, st);
 #pragma unroll
                 for (int i = 0; i < C::TN; ++i) {
                     acc[i][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        widen(a.v[i], h, 1.0f), i >= 2 ? bu : bg, acc[i][0], 0, 0, 0);
+                        widen(a.v[i], h, i >= 2 ? su : sg), bt, acc[i][0], 0, 0, 0);
                     f(h * C::TN + i);
                     __builtin_amdgcn_sched_barrier(0);
                 }

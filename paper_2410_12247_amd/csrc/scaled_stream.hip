@@ -235,99 +235,103 @@ __global__ __launch_bounds__(64 * MW) void mid_kernel(ScaledGemm g) {
         row0 = __builtin_amdgcn_readfirstlane(g.offsets[g.e_first + e]);
         cnt = __builtin_amdgcn_readfirstlane(g.offsets[g.e_first + e + 1]) - row0;
     }
-    const int m0 = blockIdx.y * 16 * MMT;
-    if (m0 >= cnt) return;
     const int K = g.K, SK = scale_pitch(K), nb = scale_blocks(K);
     const int n0 = blockIdx.x * 16 * MNT;
     const int64_t we = (int64_t)(g.e_first + e) * g.N + n0;
     const int64_t se = (int64_t)(g.e_first + e) * scale_blocks(g.N) + n0 / kScaleBlock;
     const __amdgpu_buffer_rsrc_t wr = rsrc(g.w0 + we * K), sr = rsrc(g.s0 + se * SK);
-    const int64_t first = (int64_t)row0 + m0;
-    const __amdgpu_buffer_rsrc_t xr = rsrc(g.x + (g.row_map ? 0 : first * K));
-    const __amdgpu_buffer_rsrc_t xsr = rsrc(g.xs + (g.row_map ? 0 : first * SK));
-    uint32_t woff[MNT], xoff[MMT], xsoff[MMT];
+    uint32_t woff[MNT];
 #pragma unroll
     for (int i = 0; i < MNT; ++i)
         woff[i] = (uint32_t)(min(i * 16 + col, g.N - 1 - n0) * K + grp * 16);
+    // (more than once only where tokens name an expert twice: the grid covers one
+    // row of every token)
+    for (int m0 = blockIdx.y * 16 * MMT; m0 < cnt; m0 += gridDim.y * 16 * MMT) {
+        const int64_t first = (int64_t)row0 + m0;
+        const __amdgpu_buffer_rsrc_t xr = rsrc(g.x + (g.row_map ? 0 : first * K));
+        const __amdgpu_buffer_rsrc_t xsr = rsrc(g.xs + (g.row_map ? 0 : first * SK));
+        uint32_t xoff[MMT], xsoff[MMT];
 #pragma unroll
-    for (int j = 0; j < MMT; ++j) {
-        const int r = min(j * 16 + col, cnt - 1 - m0);
-        const uint32_t src =
-            g.row_map ? (uint32_t)(g.row_map[first + r] / g.slot_div) : (uint32_t)r;
-        xoff[j] = src * (uint32_t)K + grp * 16;
-        xsoff[j] = src * (uint32_t)SK;
-    }
-    struct Step {
-        u32x4 a[MNT][2], b[MMT][2];
-        int sw, sx[MMT];
-    };
-    auto load = [&](Step &s, int kb) {  // nothing (zeros) behind K
-        const uint32_t k = (uint32_t)kb * kScaleBlock;
-        const bool in[2] = {kb * kScaleBlock < K, kb * kScaleBlock + 64 < K};
-        s.sw = __builtin_amdgcn_raw_buffer_load_b8(sr, kb < nb ? kb : kOutside, 0, 0);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int i = 0; i < MNT; ++i)
-                s.a[i][h] = __builtin_bit_cast(
-                    u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                               wr, in[h] ? woff[i] + k + h * 64 : kOutside, 0, 0));
-#pragma unroll
-            for (int j = 0; j < MMT; ++j)
-                s.b[j][h] = __builtin_bit_cast(
-                    u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                               xr, in[h] ? xoff[j] + k + h * 64 : kOutside, 0, 0));
+        for (int j = 0; j < MMT; ++j) {
+            const int r = min(j * 16 + col, cnt - 1 - m0);
+            const uint32_t src =
+                g.row_map ? (uint32_t)(g.row_map[first + r] / g.slot_div) : (uint32_t)r;
+            xoff[j] = src * (uint32_t)K + grp * 16;
+            xsoff[j] = src * (uint32_t)SK;
         }
+        struct Step {
+            u32x4 a[MNT][2], b[MMT][2];
+            int sw, sx[MMT];
+        };
+        auto load = [&](Step &s, int kb) {  // nothing (zeros) behind K
+            const uint32_t k = (uint32_t)kb * kScaleBlock;
+            const bool in[2] = {kb * kScaleBlock < K, kb * kScaleBlock + 64 < K};
+            s.sw = __builtin_amdgcn_raw_buffer_load_b8(sr, kb < nb ? kb : kOutside, 0, 0);
 #pragma unroll
-        for (int j = 0; j < MMT; ++j)
-            s.sx[j] =
-                __builtin_amdgcn_raw_buffer_load_b8(xsr, kb < nb ? xsoff[j] + kb : kOutside, 0, 0);
-    };
-    auto whole = [](const u32x4 (&v)[2]) {
-        return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3],
-                   (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
-    };
-    floatx4 acc[MNT][MMT];
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int i = 0; i < MNT; ++i)
-#pragma unroll
-        for (int j = 0; j < MMT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    Step s[MD];
-#pragma unroll
-    for (int d = 0; d < MD; ++d) load(s[d], wave + MW * d);
-    for (int kb = wave; kb < nb; kb += MW * MD) {
-#pragma unroll
-        for (int d = 0; d < MD; ++d) {
-#pragma unroll
-            for (int i = 0; i < MNT; ++i)
+                for (int i = 0; i < MNT; ++i)
+                    s.a[i][h] = __builtin_bit_cast(
+                        u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                   wr, in[h] ? woff[i] + k + h * 64 : kOutside, 0, 0));
 #pragma unroll
                 for (int j = 0; j < MMT; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        whole(s[d].a[i]), whole(s[d].b[j]), acc[i][j], 0, 0, 0, s[d].sw, 0,
-                        s[d].sx[j]);
-            load(s[d], kb + MW * (d + MD));
+                    s.b[j][h] = __builtin_bit_cast(
+                        u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                   xr, in[h] ? xoff[j] + k + h * 64 : kOutside, 0, 0));
+            }
+#pragma unroll
+            for (int j = 0; j < MMT; ++j)
+                s.sx[j] =
+                    __builtin_amdgcn_raw_buffer_load_b8(xsr, kb < nb ? xsoff[j] + kb : kOutside, 0, 0);
+        };
+        auto whole = [](const u32x4 (&v)[2]) {
+            return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3],
+                       (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
+        };
+        floatx4 acc[MNT][MMT];
+#pragma unroll
+        for (int i = 0; i < MNT; ++i)
+#pragma unroll
+            for (int j = 0; j < MMT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        Step s[MD];
+#pragma unroll
+        for (int d = 0; d < MD; ++d) load(s[d], wave + MW * d);
+        for (int kb = wave; kb < nb; kb += MW * MD) {
+#pragma unroll
+            for (int d = 0; d < MD; ++d) {
+#pragma unroll
+                for (int i = 0; i < MNT; ++i)
+#pragma unroll
+                    for (int j = 0; j < MMT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                            whole(s[d].a[i]), whole(s[d].b[j]), acc[i][j], 0, 0, 0, s[d].sw, 0,
+                            s[d].sx[j]);
+                load(s[d], kb + MW * (d + MD));
+            }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < MNT; ++i)
+        for (int i = 0; i < MNT; ++i)
 #pragma unroll
-        for (int j = 0; j < MMT; ++j) part[wave][i * MMT + j][lane] = acc[i][j];
-    __syncthreads();
-    for (int q = wave; q < MNT * MMT; q += MW) {
-        floatx4 v = part[0][q][lane];
+            for (int j = 0; j < MMT; ++j) part[wave][i * MMT + j][lane] = acc[i][j];
+        __syncthreads();
+        for (int q = wave; q < MNT * MMT; q += MW) {
+            floatx4 v = part[0][q][lane];
 #pragma unroll
-        for (int w = 1; w < MW; ++w) v += part[w][q][lane];
-        const int r = m0 + (q % MMT) * 16 + col, n = n0 + q / MMT * 16 + grp * 4;
-        if (r >= cnt || n >= g.N) continue;
-        const int64_t at = ((int64_t)row0 + r) * g.N + n;
-        if (MODE == OUT_BF16) {
-            uint2 p;
-            p.x = pack_bf16x2(v[0], v[1]);
-            p.y = pack_bf16x2(v[2], v[3]);
-            *reinterpret_cast<uint2 *>((bf16_t *)g.out + at) = p;
-        } else {
-            *reinterpret_cast<floatx4 *>((float *)g.out + at) = v;
+            for (int w = 1; w < MW; ++w) v += part[w][q][lane];
+            const int r = m0 + (q % MMT) * 16 + col, n = n0 + q / MMT * 16 + grp * 4;
+            if (r >= cnt || n >= g.N) continue;
+            const int64_t at = ((int64_t)row0 + r) * g.N + n;
+            if (MODE == OUT_BF16) {
+                uint2 p;
+                p.x = pack_bf16x2(v[0], v[1]);
+                p.y = pack_bf16x2(v[2], v[3]);
+                *reinterpret_cast<uint2 *>((bf16_t *)g.out + at) = p;
+            } else {
+                *reinterpret_cast<floatx4 *>((float *)g.out + at) = v;
+            }
         }
+        __syncthreads();
     }
 }
 

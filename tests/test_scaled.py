@@ -390,6 +390,70 @@ def test_scale_byte_255_is_nan(R):
     assert torch.equal(got[:R - 1, :128], clean[:R - 1, :128])
 
 
+# values of 128 to 448: products of at least 2^14, so that none is below the normal
+# range of fp32 beside scales whose product is
+def large_values(g, *shape):
+    sign = torch.randint(0, 2, shape, generator=g) * 128
+    return (torch.randint(0x70, 0x7F, shape, generator=g) + sign).to(torch.uint8)
+
+
+@gpu
+@pytest.mark.parametrize("ex,ew", [(-67, -66), (45, 40)])
+@pytest.mark.parametrize("R", [3, 30, 90, 400])
+def test_gemm_of_extreme_scales(R, ex, ew):
+    g = gen(R)
+    N, K = 192, 320
+    xq, wq = large_values(g, R, K), large_values(g, N, K)
+    xs, ws = ref.scale_bytes(g, R, K, ex, ex + 1), ref.scale_bytes(g, ref.blocks(N), K, ew, ew + 1)
+    want, bound = product(ref.widen(xq, xs, 1), ref.widen(wq, ws, 128), F32)
+    got = run_gemm(xq, xs, wq, ws, F32).double()
+    assert bool(((got - want).abs() <= bound).all())
+
+
+@gpu
+@pytest.mark.parametrize("T,I", [(1, 192), (40, 192), (200, 192), (1100, 1024)])
+def test_ffn_of_extreme_scales(T, I):
+    E, k, H = 4, 2, 192
+    g = gen(T)
+    off, slot, cap = dispatch(g, T, E, k, 0, E, None)
+    d = moe.dims(T, H, I, E, k)
+    x, xs = large_values(g, T, H), ref.scale_bytes(g, T, H, -67, -66)
+    stacks = []
+    for n, kk, e in ((I, H, -66), (I, H, 100), (H, I, -8)):
+        stacks += [large_values(g, E, n, kk),
+                   torch.stack([ref.scale_bytes(g, ref.blocks(n), kk, e, e + 1)
+                                for _ in range(E)])]
+    ws = torch.empty(moe.scaled_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    y = torch.zeros((cap, H), device="cuda")
+    moe.ffn_group_scaled(d, 0, E, cuda(off), cuda(slot), *map(cuda, (x, xs, *stacks)), y, ws)
+    got, xw = y.cpu().double(), ref.widen(x, xs, 1)
+    for e in range(E):
+        lo, hi = int(off[e]), int(off[e + 1])
+        if lo == hi:
+            continue
+        w = [ref.widen(stacks[i][e], stacks[i + 1][e], 128) for i in (0, 2, 4)]
+        want, bound = ref.ffn_rows(xw[(slot[lo:hi] // k).long()], *w)
+        assert bool(((got[lo:hi] - want).abs() <= bound + HALF(F32) * (want.abs() + bound)).all())
+
+
+@gpu
+@pytest.mark.parametrize("T", [3, 40, 200])
+def test_group_gemm_of_tokens_that_name_an_expert_twice(T):
+    """Offsets that give an expert more rows than there are tokens."""
+    E, k, N, K = 4, 2, 192, 320
+    g = gen(T)
+    slot = torch.arange(T * k, dtype=torch.int32)
+    off = torch.tensor([0, T * k, T * k, T * k, T * k], dtype=torch.int32)
+    d = moe.dims(T, 64, 64, E, k)
+    xq, xs = ref.small_integers(g, T, K), ref.scale_bytes(g, T, K)
+    wq = ref.small_integers(g, E, N, K)
+    ws = torch.stack([ref.scale_bytes(g, ref.blocks(N), K) for _ in range(E)])
+    want = ref.widen(xq, xs, 1) @ ref.widen(wq[0], ws[0], 128).T
+    y = torch.full((T * k, N), 55.0, device="cuda")
+    moe.gemm_group_scaled(d, 0, E, *map(cuda, (off, slot, xq, xs, wq, ws)), y)
+    assert torch.equal(y.cpu(), want[(slot // k).long()].to(F32))
+
+
 @gpu
 @pytest.mark.parametrize("T", [1, 40, 200])
 def test_ffn_keeps_a_nan_scale_in_its_token(T):
@@ -437,6 +501,9 @@ GROUPS = [
     (2100, 2, 1, 0, 2, 320, 192, None),
     (2600, 3, 1, 0, 2, 192, 64, [1, 1, 0.05]),
     (4352, 4, 4, 0, 4, 64, 128, None),
+    # tiles of 128 x 256 and of 256 x 256 with tails
+    (1000, 4, 2, 0, 4, 2112, 192, None),
+    (2101, 4, 2, 0, 4, 2112, 192, [1, 0.6, 1, 0.8]),
 ]
 
 
@@ -475,6 +542,9 @@ FFNS = [
     (200, 3, 2, 0, 3, 128, 448, None),
     (290, 2, 1, 0, 2, 576, 64, [1, 0]),
     (1101, 1, 1, 0, 1, 192, 192, None),  # tails in both products
+    # tiles of 128 rows, and of 256 with tails
+    (1001, 4, 2, 0, 4, 192, 1024, None),
+    (2101, 4, 2, 0, 4, 192, 1024, [1, 0.6, 1, 0.8]),
 ]
 
 
