@@ -499,6 +499,10 @@ def combine_rows(d, e_first, e_count, y_perm, topk_ids, slot_row, topk_w, y, acc
         _arg(dev, "y", y, _F32, (d.tokens, d.hidden)), int(accumulate), _stream_on(dev, stream)))
 
 
+def _layer_shape(d):
+    return d.hidden, d.inter, d.shared_inter, d.local_count
+
+
 def scaled_weights(d, gate, up, down, shared_gate=None, shared_up=None,
                    shared_down=None) -> ScaledWeights:
     """Checks and packs a layer's weights, each a pair (q, scales) of
@@ -507,6 +511,7 @@ def scaled_weights(d, gate, up, down, shared_gate=None, shared_up=None,
     dev = _dev("gate", gate[0])
     w = ScaledWeights()
     w.keep = (gate, up, down, shared_gate, shared_up, shared_down)
+    w.made_for = _layer_shape(d), dev
     for name, (q, s), n, k in (("gate", gate, I, H), ("up", up, I, H), ("down", down, H, I)):
         a, b = _stack(dev, name, d, q, s, n, k)
         setattr(w, name, a)
@@ -534,6 +539,8 @@ def forward_scaled(d, x, residual, norm_weight, eps, total, w_router, bias, weig
     rows normalised before."""
     T, H, k = d.tokens, d.hidden, d.top_k
     dev, code = _dev("x", x), _real("x", x)
+    if getattr(weights, "made_for", None) != (_layer_shape(d), dev):
+        raise ValueError("weights are not scaled_weights() of these dims on this device")
     _check(lib().moe_forward_scaled(
         ctypes.byref(d), _arg(dev, "x", x, (x.dtype,), (T, H)), code,
         _arg(dev, "residual", residual, _BF16, (T, H)),

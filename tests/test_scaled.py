@@ -827,6 +827,7 @@ LAYERS = [
     (29, 320, 192, 8, 2, 0, 8, 192),
     (70, 128, 320, 40, 6, 10, 20, 64),
     (260, 256, 128, 4, 2, 1, 2, 128),
+    (4200, 128, 64, 32, 4, 0, 32, 64),  # more tokens than the router's logits are kept for
 ]
 
 
@@ -942,3 +943,15 @@ def test_layers_in_a_row():
     s = A.y.cpu().double() + A.total.cpu().double()
     off = (B.total.cpu().double() - s).abs()
     assert bool((off <= (2.0 ** -8 + 2.0 ** -23) * s.abs()).all())
+
+
+@gpu
+def test_layer_refuses_weights_of_other_dims():
+    A, B = (Layer(5, 192, I, 8, 2, 0, 8, 0, seed=I) for I in (128, 192))
+    A.w, B.w = B.w, A.w
+    for L in (A, B):
+        with pytest.raises(ValueError, match="of these dims"):
+            L.run()
+    A.w = moe.ScaledWeights()
+    with pytest.raises(ValueError, match="of these dims"):
+        A.run()
