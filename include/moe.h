@@ -417,12 +417,16 @@ moe_status moe_choose_pipeline_n(double c_ms, double k_ms, double b_ms, int32_t 
  * infinity becomes one; beside an infinity (e = 120) a block's other values
  * are rounded to zero, or nearly.
  *
- * The products run on the matrix cores with the scales applied by the matrix
- * instruction and fp32 accumulators.  Inside an instruction the products of
+ * The products run on the matrix cores with fp32 accumulators and the scales
+ * applied on the way.  Inside an 8-bit matrix instruction the products of
  * eight consecutive k are added as one group, each cut to 13 bits below the
  * group's largest exponent, so a sum's error is at most 2^-10 times the sum
  * over groups of the group's largest |product| (1.5e-5 of the result's norm
- * on Gaussian data), whatever the output type.
+ * on Gaussian data), whatever the output type.  Launches of few rows, which the
+ * weights' stream bounds, widen the values to bf16 instead and are exact to
+ * fp32.  Which form a launch takes depends on its dims and widths alone: not on
+ * the data, the expert range or the device's state, so results have the same
+ * bits from run to run and from a range as from the whole.
  *
  * Tensors must be 16-byte aligned, scale tensors 4-byte aligned, else
  * MOE_ERR_INVALID, and belong to the current device.  Rows behind the last
@@ -447,11 +451,13 @@ moe_status moe_quant_weights(int32_t experts, int32_t n, int32_t k, const moe_bf
 
 /* The normalisation in front of an MoE layer, with the residual's addition
  * and the quantised rows the products take:
- *   s = x + residual             (fp32; residual NULL: s = x)
- *   total = bf16(s)              the residual stream behind the addition
- *   v = s * rsqrt(mean(s^2) + eps) * weight   (fp32; weight NULL: ones)
+ *   s = x + residual             (residual NULL: s = x)
+ *   total = bf16(s)              the residual stream behind the addition (s
+ *                                rounded to fp32 first)
+ *   v = s * rsqrt(mean(s^2) + eps) * weight   (weight NULL: ones)
  *   y = bf16(v)                  what the router reads
  *   q, scales = Q(v)             from v before its rounding to bf16
+ * v is computed in 64 bits.
  * x [rows][hidden] of x_type (MOE_FP32 is what moe_combine writes); residual,
  * total, y [rows][hidden] bf16; weight [hidden] bf16.  total, y and the pair
  * q, scales may each be NULL; y or q has to be given.  total may be the
@@ -480,8 +486,8 @@ moe_status moe_gemm_group_scaled(const moe_dims *dims, int32_t e_first, int32_t 
                                  const moe_e4m3 *w, const moe_scale *w_scales, void *y,
                                  int32_t y_type, void *stream);
 
-/* Workspace of moe_ffn_group_scaled: the quantised activations between its
- * two products.  Host-only; 0 for invalid dims. */
+/* Workspace of moe_ffn_group_scaled: the activations between its two products.
+ * One for some tokens serves fewer too.  Host-only; 0 for invalid dims. */
 size_t moe_scaled_workspace_bytes(const moe_dims *dims);
 
 /* moe_ffn_group in 8 bits, for the rows of local experts [e_first, e_first +
@@ -527,7 +533,8 @@ typedef struct {
     const moe_scale *shared_down_scales;
 } moe_scaled_weights;
 
-/* Workspace of moe_forward_scaled.  Host-only; 0 for invalid dims. */
+/* Workspace of moe_forward_scaled; one for some tokens serves fewer too.
+ * Host-only; 0 for invalid dims. */
 size_t moe_forward_scaled_bytes(const moe_dims *dims);
 
 /* The MoE layer in 8 bits, from the block's input to its output:

@@ -1,11 +1,20 @@
 // Rows and weights into block-scaled 8 bits.
 //
-// norm_quant: s = x + residual, total = bf16(s), y = s rsqrt(mean s^2 + eps) w,
-// and Q(y) with one scale per 128 columns, in one pass over the row: a
-// workgroup holds a row (or a wave holds one, for short rows) in registers
-// as fp32, so nothing is read twice and Q sees y before its rounding to
-// bf16.  A lane holds eight consecutive columns, so a block of 128 is one
-// DPP row of 16 lanes and its largest value needs no LDS.
+// norm_quant: s = x + residual, total = bf16(s), v = s rsqrt(mean s^2 + eps) w,
+// y = bf16(v) and Q(v) with one scale per 128 columns, in one pass over the row:
+// a workgroup holds a row (or a wave holds one, for short rows) in registers, so
+// nothing is read twice and Q sees v before its rounding to bf16.  A lane holds
+// eight consecutive columns, so a block of 128 is one DPP row of 16 lanes and
+// its largest value needs no LDS.
+//
+// It is bound by memory: 16384 x 5120 (fp32 x, bf16 residual, total and y) moves
+// 923 MB in 171 us, 5.4 TB/s; 16384 x 8192 5.7 TB/s; the quantisation alone of
+// bf16 rows 16384 x 5120, 254 MB, in 45 us, 5.6 TB/s.  One row of 4096 takes 3.2
+// us, a launch's latency and a chain of loads, sum, reciprocal root and stores.
+// So the arithmetic between the loads and the two roundings is in 64 bits, under
+// the memory's time: in fp32 some 50 of those 84 million values are rounded to
+// the neighbour of the definition's, here none (166 us in fp32).  Eight waves a
+// row: four with twice the passes take 179 us and 3.7 (one row), sixteen 198.
 #include <algorithm>
 
 #include "scaled.h"
@@ -23,6 +32,7 @@ struct NormArgs {
     float eps;
     bf16_t *total, *y;
     uint8_t *q, *scales;
+    double one_col;  // 1 / cols
 };
 
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
@@ -72,17 +82,42 @@ __device__ __forceinline__ double wave_sum(double v) {
     for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
-// The squares of eight columns, and 1 / sqrt(mean + eps) of the row's.  The
-// sum over the row is in 64 bits: an error of rstd moves every value of the
-// row the same way, and with some of them their rounding to 8 bits.
-__device__ __forceinline__ float squares(const float (&s)[VEC]) {
-    float v = 0.f;
+// Eight columns of x + residual, exactly: two fp32 numbers whose sum has 64
+// bits' room.
+struct Sum8 {
+    float x[VEC], r[VEC];
+    __device__ __forceinline__ double operator[](int i) const { return (double)x[i] + (double)r[i]; }
+    __device__ __forceinline__ void rounded(float (&s)[VEC]) const {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v = __builtin_fmaf(s[i], s[i], v);
-    return v;
+        for (int i = 0; i < VEC; ++i) s[i] = x[i] + r[i];
+    }
+    __device__ __forceinline__ double squares(double v) const {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const double s = (*this)[i];
+            v = __builtin_fma(s, s, v);
+        }
+        return v;
+    }
+};
+__device__ __forceinline__ double inverse_rms(double ss, const NormArgs &a) {
+    return rsqrt(__builtin_fma(ss, a.one_col, (double)a.eps));
 }
-__device__ __forceinline__ float inverse_rms(double ss, int cols, float eps) {
-    return (float)(1.0 / sqrt(ss / cols + (double)eps));
+// To fp32 with the last bit set where bits behind it are: what is rounded from
+// this to fewer bits (bf16, e4m3) is rounded as if from v itself.
+__device__ __forceinline__ float to_odd(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const uint32_t lo = (uint32_t)u;
+    const uint32_t cut = (lo & 0xE0000000u) | ((lo & 0x1FFFFFFFu) ? 0x20000000u : 0u);
+    return (float)__longlong_as_double((long long)((u & 0xFFFFFFFF00000000ull) | cut));
+}
+// (x + residual) rstd weight
+__device__ __forceinline__ void normalise(const Sum8 &s, double rstd, const bf16_t *weight,
+                                          float (&v)[VEC]) {
+    float w[VEC];
+    if (weight) load8(weight, w);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = to_odd(weight ? s[i] * rstd * (double)w[i] : s[i] * rstd);
 }
 
 // One pass' eight columns of every lane: quantised (all lanes take part; a
@@ -112,32 +147,21 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_quant_kern
         WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
     if (row >= a.rows) return;
     const X *x = reinterpret_cast<const X *>(a.x) + row * a.cols;
-    float s[PASSES][VEC];
+    Sum8 s[PASSES];
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int col = (p * THREADS + tid) * VEC;
-        if (col < a.cols) {
-            load8(x + col, s[p]);
-        } else {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s[p][i] = 0.f;
-        }
+        for (int i = 0; i < VEC; ++i) s[p].x[i] = 0.f, s[p].r[i] = -0.f;  // x + -0 is x, signs too
+        if (col >= a.cols) continue;
+        load8(x + col, s[p].x);
+        if (NORM && a.residual) load8(a.residual + row * a.cols + col, s[p].r);
     }
+    double rstd = 1.;
     if (NORM) {
-        if (a.residual) {
-#pragma unroll
-            for (int p = 0; p < PASSES; ++p) {
-                const int col = (p * THREADS + tid) * VEC;
-                if (col >= a.cols) continue;
-                float r[VEC];
-                load8(a.residual + row * a.cols + col, r);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) s[p][i] += r[i];
-            }
-        }
         double ss = 0.;
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) ss += squares(s[p]);
+        for (int p = 0; p < PASSES; ++p) ss = s[p].squares(ss);
         ss = wave_sum(ss);
         if (WAVES > 1) {
             __shared__ double part[WAVES];
@@ -147,23 +171,23 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_quant_kern
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) ss += part[w];
         }
-        const float rstd = inverse_rms(ss, a.cols, a.eps);
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int col = (p * THREADS + tid) * VEC;
-            if (col >= a.cols) continue;
-            if (a.total) store8(a.total + row * a.cols + col, s[p]);
-            float w[VEC];
-            if (a.weight) load8(a.weight + col, w);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                s[p][i] = a.weight ? s[p][i] * rstd * w[i] : s[p][i] * rstd;
-            if (a.y) store8(a.y + row * a.cols + col, s[p]);
-        }
+        rstd = inverse_rms(ss, a);
     }
-    if (a.q) {
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) quant8(a, row, (p * THREADS + tid) * VEC, s[p]);
+    for (int p = 0; p < PASSES; ++p) {
+        const int col = (p * THREADS + tid) * VEC;
+        float v[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = s[p].x[i];
+        if (NORM && col < a.cols) {
+            if (a.total) {
+                s[p].rounded(v);
+                store8(a.total + row * a.cols + col, v);
+            }
+            normalise(s[p], rstd, a.weight ? a.weight + col : nullptr, v);
+            if (a.y) store8(a.y + row * a.cols + col, v);
+        }
+        if (a.q) quant8(a, row, col, v);
     }
 }
 
@@ -173,22 +197,19 @@ __global__ __launch_bounds__(1024) void norm_quant_long_kernel(NormArgs a) {
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
     const X *x = reinterpret_cast<const X *>(a.x) + row * a.cols;
-    auto load = [&](int col, float (&s)[VEC]) {
-        load8(x + col, s);
-        if (NORM && a.residual) {
-            float r[VEC];
-            load8(a.residual + row * a.cols + col, r);
+    auto load = [&](int col, Sum8 &s) {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s[i] += r[i];
-        }
+        for (int i = 0; i < VEC; ++i) s.r[i] = -0.f;
+        load8(x + col, s.x);
+        if (NORM && a.residual) load8(a.residual + row * a.cols + col, s.r);
     };
-    float rstd = 1.f;
+    double rstd = 1.;
     if (NORM) {
         double ss = 0.;
         for (int col = tid * VEC; col < a.cols; col += 1024 * VEC) {
-            float s[VEC];
+            Sum8 s;
             load(col, s);
-            ss += squares(s);
+            ss = s.squares(ss);
         }
         ss = wave_sum(ss);
         __shared__ double part[16];
@@ -196,26 +217,28 @@ __global__ __launch_bounds__(1024) void norm_quant_long_kernel(NormArgs a) {
         __syncthreads();
         ss = 0.;
         for (int w = 0; w < 16; ++w) ss += part[w];
-        rstd = inverse_rms(ss, a.cols, a.eps);
+        rstd = inverse_rms(ss, a);
     }
     for (int c0 = 0; c0 < a.cols; c0 += 1024 * VEC) {
         const int col = c0 + tid * VEC;
-        float s[VEC] = {};
+        float v[VEC] = {};
         if (col < a.cols) {
+            Sum8 s;
             load(col, s);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = s.x[i];
             if (NORM) {
                 // (a lane reads its columns of the residual before it writes
                 // them: total may be the residual itself)
-                if (a.total) store8(a.total + row * a.cols + col, s);
-                float w[VEC];
-                if (a.weight) load8(a.weight + col, w);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    s[i] = a.weight ? s[i] * rstd * w[i] : s[i] * rstd;
-                if (a.y) store8(a.y + row * a.cols + col, s);
+                if (a.total) {
+                    s.rounded(v);
+                    store8(a.total + row * a.cols + col, v);
+                }
+                normalise(s, rstd, a.weight ? a.weight + col : nullptr, v);
+                if (a.y) store8(a.y + row * a.cols + col, v);
             }
         }
-        if (a.q) quant8(a, row, col, s);
+        if (a.q) quant8(a, row, col, v);
     }
 }
 
@@ -279,9 +302,9 @@ hipError_t go_norm(NormArgs a, hipStream_t s) {
         else if (a.cols <= 2048)
             norm_quant_kernel<X, NORM, 4, 1><<<rows, 256, 0, s>>>(a);
         else if (a.cols <= 4096)
-            norm_quant_kernel<X, NORM, 4, 2><<<rows, 256, 0, s>>>(a);
+            norm_quant_kernel<X, NORM, 8, 1><<<rows, 512, 0, s>>>(a);
         else if (a.cols <= 8192)
-            norm_quant_kernel<X, NORM, 4, 4><<<rows, 256, 0, s>>>(a);
+            norm_quant_kernel<X, NORM, 8, 2><<<rows, 512, 0, s>>>(a);
         else
             norm_quant_long_kernel<X, NORM><<<rows, 1024, 0, s>>>(a);
         const hipError_t err = hipGetLastError();
@@ -302,7 +325,8 @@ hipError_t launch_norm_quant(int64_t rows, int cols, const void *x, int x_type,
                              const bf16_t *residual, bool norm, const bf16_t *weight, float eps,
                              bf16_t *total, bf16_t *y, uint8_t *q, uint8_t *scales,
                              hipStream_t s) {
-    const NormArgs a{rows, cols, x, residual, weight, eps, total, y, q, scales};
+    const NormArgs a{rows, cols, x, residual, weight, eps, total, y, q, scales,
+                     1.0 / cols};
     if (x_type == MOE_FP32)
         return norm ? go_norm<float, true>(a, s) : go_norm<float, false>(a, s);
     return norm ? go_norm<bf16_t, true>(a, s) : go_norm<bf16_t, false>(a, s);

@@ -277,6 +277,25 @@ def test_norm_quant(C, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("R,C", [(1500, 320), (400, 1344), (300, 4096), (300, 5120), (60, 8320)])
+def test_norm_quant_rounds_as_64_bits_do(R, C, dtype):
+    """The kernel's v is exact to 2^-50: a value would have to lie that close to
+    a rounding border to differ (half a million of them: once in 10^9 runs)."""
+    g = gen(R + C)
+    x, res = rows_of(g, R, C, dtype), torch.randn((R, C), generator=g).to(BF16)
+    w = (1 + 0.3 * torch.randn(C, generator=g)).to(BF16)
+    q = torch.empty((R, C), dtype=torch.uint8, device="cuda")
+    s = torch.zeros((R, ref.pitch(C)), dtype=torch.uint8, device="cuda")
+    moe.norm_quant(cuda(x), cuda(res), cuda(w), 1e-5, None, None, q, s)
+    v = x.double() + res.double()
+    v = v / torch.sqrt((v * v).mean(1, keepdim=True) + float(torch.tensor(1e-5))) * w.double()
+    want, e = ref.quant(v, 1)
+    assert torch.equal(s[:, :ref.blocks(C)].cpu().int() - 127, e.int())
+    assert torch.equal(ref.decode(q), want)
+
+
+@gpu
 def test_norm_rows_that_are_zero_or_no_numbers():
     x = torch.zeros((4, 320), dtype=F32)
     x[1, 5] = float("nan")
