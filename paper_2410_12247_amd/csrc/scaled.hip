@@ -1,4 +1,21 @@
-// Products over block-scaled 8-bit tensors on the gfx950 matrix cores.
+// Products over block-scaled 8-bit tensors on the gfx950 matrix cores:
+//   y[r][n] = sum over blocks b of 128 k of
+//             2^(sx[r][b] + sw[n/128][b] - 254) sum_{k in b} x[r][k] w[n][k],
+// or Q(silu(g) u) of two such products.  The scaled matrix instruction takes
+// both scale bytes as operands, so a block's scaling costs nothing: the token
+// row's scale is a lane's own byte, the weight's one for all.  Weights are its A
+// operand and tokens its B, so a lane holds runs of four output columns of one
+// token row.
+//
+// Large launches are bound by the matrix cores, and those by the board's power:
+// the chip runs at 1.85 to 1.9 GHz under them.  16384 x 5120 x 4096 takes 265 us,
+// 2.59 PFLOP/s (a library's 8-bit product of 8192^3 2.71), the cores busy in 66%
+// of the cycles; the Mixtral FFN of 16384 tokens 1.20 ms, 2.41 PFLOP/s; DBRX gate
+// of 8192 tokens 272 us, 1.99 (N is 5.25 tiles of 256: 15% of the products are
+// padding).  Few rows are bound by the weights' stream: DBRX FFN of 64 tokens 91
+// us, 4.4 TB/s; DeepSeekV2 down product of 4099 tokens with a Zipf load 68 to 75
+// us, 3.9 TB/s and 1.2 PFLOP/s, between the two, its second round of tiles part
+// full.
 #include <algorithm>
 
 #include "lds_dma.h"
@@ -37,6 +54,8 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
 // busy).
 // K advances by pairs of 64 (one MFMA's K, so a pair is a scale block) through
 // two to four LDS buffers filled by LDS-DMA with whole 128-byte lines of the rows.
+// One workgroup per CU stays for the whole launch, and the next tile's requests
+// are on their way under a tile's epilogue.
 // ---------------------------------------------------------------------------
 template <int MODE, int BM_, int BN_>
 struct Cfg {
@@ -371,7 +390,8 @@ struct TileLoop {
     // some thousands to its neighbour, which a row of few large values shows
     // (DBRX FFN of 64 tokens: off by 1.9 to 3.7e-3 with it, 1.7e-3 without, all of
     // that the output's bf16), at 3% of the time (93.8 -> 96.7 us); with more rows
-    // it is lost in the rest.
+    // the matrix cores are the bound, and the 8-bit products stay (the FFN's rows are
+    // off by 2.0 to 2.5e-3 then).
     static constexpr bool EXACT = MODE == SWIGLU && BM_ == 64;
     // e4m3 values of a lane's 32 bytes, 8 (part) to 8 (part) + 7, times scale
     __device__ __forceinline__ static bf16x8 widen(const u32x4 (&v)[2], int part, float scale) {
