@@ -11,7 +11,7 @@
 // the chip runs at 1.85 to 1.9 GHz under them.  16384 x 5120 x 4096 takes 265 us,
 // 2.59 PFLOP/s (a library's 8-bit product of 8192^3 2.71), the cores busy in 66%
 // of the cycles; the Mixtral FFN of 16384 tokens 1.20 ms, 2.41 PFLOP/s; DBRX gate
-// of 8192 tokens 272 us, 1.99 (N is 5.25 tiles of 256: 15% of the products are
+// of 8192 tokens 253 us, 2.14 (N is 5.25 tiles of 256: 15% of the products are
 // padding).  Few rows are bound by the weights' stream: DBRX FFN of 64 tokens 91
 // us, 4.4 TB/s; DeepSeekV2 down product of 4099 tokens with a Zipf load 68 to 75
 // us, 3.9 TB/s and 1.2 PFLOP/s, between the two, its second round of tiles part
@@ -152,7 +152,19 @@ struct Walk {
         tiles = __builtin_amdgcn_readfirstlane(s_tile[g.e_count]);
         tails = __builtin_amdgcn_readfirstlane(s_tail[g.e_count]);
     }
-    // tile tau of the tiles (tail false) or of the tails
+    // Tails of 128 columns instead of BNOUT.
+    __device__ __forceinline__ int narrow_tails(const ScaledGemm &g) const {
+        return tails / NT * ((g.N + 127) / 128);
+    }
+    __device__ __forceinline__ void narrow(const ScaledGemm &g) {
+        const int n = (g.N + 127) / 128;
+        __syncthreads();
+        for (int i = threadIdx.x; i <= g.e_count; i += C::THREADS) s_tail[i] = s_tail[i] / NT * n;
+        __syncthreads();
+        tails = tails / NT * n;
+    }
+    // tile tau of the tiles (tail false) or of the tails, of BN columns
+    template <int BN>
     __device__ __forceinline__ Tile tile(const ScaledGemm &g, int tau, bool tail) const {
         auto lds = [](const int &v) { return __builtin_amdgcn_readfirstlane(v); };
         const int *pre = tail ? s_tail : s_tile;
@@ -174,9 +186,9 @@ struct Walk {
         Tile t;
         t.e = lo;
         t.r0 = (int64_t)row0 + (int64_t)mt * C::BM;
-        t.n0 = (int64_t)nt * C::BNOUT;
+        t.n0 = (int64_t)nt * BN;
         t.m_valid = min(C::BM, cnt - mt * C::BM);
-        t.n_valid = min(C::BNOUT, (int)(g.N - t.n0));
+        t.n_valid = min(BN, (int)(g.N - t.n0));
         return t;
     }
 };
@@ -237,7 +249,7 @@ struct TileLoop {
     }
     __device__ __forceinline__ void plan_tile(int tau, int n, int which) {
         if (tau >= total) return;
-        const Tile t = walk.tile(g, tau, TAIL);
+        const Tile t = walk.template tile<C::BNOUT>(g, tau, TAIL);
         int *p = plan(n);
         p[0] = t.e;
         p[1] = (int)t.r0;
@@ -755,18 +767,29 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(ScaledGemm g) {
     constexpr bool TAILS = BM_ > 128;
     __shared__ __attribute__((aligned(16))) char smem[C::LDS_BYTES];
     using W = Walk<C, TAILS>;
-    const W walk(g, reinterpret_cast<int *>(smem + C::INTS));
+    W walk(g, reinterpret_cast<int *>(smem + C::INTS));
     // neighbouring tiles on one XCD
     const int G = gridDim.x;  // a multiple of NXCD
     const int slot = (blockIdx.x % NXCD) * (G / NXCD) + blockIdx.x / NXCD;
     run_tiles<MODE, BM_, BN_, false>(g, walk, slot, smem);
     if constexpr (TAILS) {
-        static_assert(Cfg<MODE, 128, BN_>::INTS <= C::INTS, "the offsets lie behind both layouts");
-        if (walk.tails > 0) {
-            const int used = walk.tiles % G;
-            run_tiles<MODE, 128, BN_, true>(g, walk, slot >= used ? slot - used : slot + G - used,
-                                       smem);
+        static_assert(Cfg<MODE, 128, BN_>::INTS <= C::INTS, "the offsets lie behind every layout");
+        if (walk.tails == 0) return;
+        const int used = walk.tiles % G, left = used ? G - used : 0;
+        const int from = slot >= used ? slot - used : slot + G - used;
+        // Where the tails need a round of their own, ones of half the columns that
+        // fit into it shorten it (DBRX gate of 8192 tokens 270 -> 253 us).  Where
+        // they do not fit, or run beside the last tiles, whole ones do less work.
+        // (The SwiGLU tile's columns are one scale block: it has no half.)
+        if constexpr (MODE != SWIGLU && BM_ == 256) {
+            static_assert(Cfg<MODE, 128, 128>::INTS <= C::INTS, "and this one");
+            if (walk.tails > left && walk.narrow_tails(g) <= G + left) {
+                walk.narrow(g);
+                run_tiles<MODE, 128, 128, true>(g, walk, from, smem);
+                return;
+            }
         }
+        run_tiles<MODE, 128, BN_, true>(g, walk, from, smem);
     }
 }
 

@@ -364,12 +364,12 @@ def test_gemm_of_any_values(R, N, K, dtype):
 
 
 # tiles of 64 x 128, 128 x 128, 128 x 256, 192 x 256 and 256 x 256 (token x weight
-# rows); 192 and 256 again with a tail behind them
+# rows); 192 and 256 again with a tail behind them, and 256 with narrow tails
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("R,N,K", [(700, 1024, 320), (1100, 1472, 192), (2000, 2112, 320),
                                    (2500, 3904, 320), (2950, 4160, 192), (5000, 2048, 320),
-                                   (1030, 8256, 64)])
+                                   (1030, 8256, 64), (2068, 8192, 64)])
 def test_gemm_of_every_tile(R, N, K, dtype):
     g = gen(R + N + K)
     xq, wq = ref.small_integers(g, R, K), ref.small_integers(g, N, K)
@@ -523,6 +523,8 @@ GROUPS = [
     # tiles of 128 x 256 and of 256 x 256 with tails
     (1000, 4, 2, 0, 4, 2112, 192, None),
     (2101, 4, 2, 0, 4, 2112, 192, [1, 0.6, 1, 0.8]),
+    # tails in a round of their own
+    (2068, 2, 2, 0, 2, 4096, 64, None),
 ]
 
 
