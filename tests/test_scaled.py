@@ -416,6 +416,91 @@ def large_values(g, *shape):
     return (torch.randint(0x70, 0x7F, shape, generator=g) + sign).to(torch.uint8)
 
 
+def ones(*shape):
+    """Scale bytes of 2^0."""
+    return torch.full(shape, 127, dtype=torch.uint8, device="cuda")
+
+
+@gpu
+@pytest.mark.parametrize("R,N,K", [(1130000, 64, 4096), (300000, 8192, 64)])
+def test_gemm_past_offsets_of_32_bits(R, N, K):
+    """x, or y, of more than 4 GiB; all rows but the last are zeros."""
+    g = gen(R)
+    last = ref.small_integers(g, 300, K)
+    w = ref.small_integers(g, N, K)
+    w[:, 256:] = 0  # sums below 2^24
+    x = torch.zeros((R, K), dtype=torch.uint8, device="cuda")
+    x[-300:] = cuda(last)
+    y = torch.full((R, N), 3.0, dtype=BF16, device="cuda")
+    moe.gemm_scaled(x, ones(R, ref.pitch(K)), cuda(w), ones(ref.blocks(N), ref.pitch(K)), y)
+    want = (ref.decode(last) @ ref.decode(w).T).to(F32).to(BF16)
+    assert torch.equal(y[-300:].cpu(), want)
+    assert not bool(y[:-300].any())
+
+
+@gpu
+@pytest.mark.parametrize("T,N,K", [(20, 1024, 1 << 20), (200, 1024, 1 << 20), (200, 32768, 32768)])
+def test_group_gemm_past_offsets_of_32_bits(T, N, K):
+    """The last expert's weights begin 4 GiB behind the first's."""
+    E = 5
+    g = gen(T + N)
+    x, w = ref.small_integers(g, T, 256), ref.small_integers(g, N, 256)
+    xd = torch.zeros((T, K), dtype=torch.uint8, device="cuda")
+    wd = torch.zeros((E, N, K), dtype=torch.uint8, device="cuda")
+    xd[:, -256:], wd[E - 1, :, -256:] = cuda(x), cuda(w)
+    off = torch.tensor([0, 1, 2, 2, 3, T], dtype=torch.int32)
+    y = torch.empty((T, N), device="cuda")
+    moe.gemm_group_scaled(moe.dims(T, 64, 64, E, 1), 0, E, cuda(off), None, xd,
+                          ones(T, ref.pitch(K)), wd, ones(E, ref.blocks(N), ref.pitch(K)), y)
+    want = (ref.decode(x) @ ref.decode(w).T).to(F32)
+    assert torch.equal(y[3:].cpu(), want[3:]) and not bool(y[:3].any())
+
+
+@gpu
+@pytest.mark.parametrize("T,E,EL,K,rows", [((1 << 20) - 1, 2, 2, 4096, 200),
+                                           (4095, 256, 4, 1 << 20, 16)])
+def test_gather_from_almost_4_gib(T, E, EL, K, rows):
+    """The last tokens of the largest matrix that can be gathered from."""
+    g = gen(T)
+    N, n = 64, EL * rows
+    x, w = ref.small_integers(g, n, 256), ref.small_integers(g, N, 256)
+    xd = torch.zeros((T, K), dtype=torch.uint8, device="cuda")
+    wd = torch.zeros((EL, N, K), dtype=torch.uint8, device="cuda")
+    xd[-n:, -256:], wd[:, :, -256:] = cuda(x), cuda(w)
+    slot = torch.zeros(T, dtype=torch.int32)
+    slot[:n] = torch.arange(T - 1, T - 1 - n, -1)
+    off = torch.arange(EL + 1, dtype=torch.int32) * rows
+    y = torch.full((T, N), 5.0, device="cuda")
+    moe.gemm_group_scaled(moe.dims(T, 64, 64, E, 1, 0, EL), 0, EL, cuda(off), cuda(slot), xd,
+                          ones(T, ref.pitch(K)), wd, ones(EL, 1, ref.pitch(K)), y)
+    want = (ref.decode(x) @ ref.decode(w).T).to(F32).flip(0)
+    assert torch.equal(y[:n].cpu(), want) and bool((y[n:] == 5).all())
+
+
+@gpu
+def test_rows_past_offsets_of_32_bits():
+    """Quantised and normalised rows of more than 4 GiB, in launches of 2^21 rows."""
+    R, C = (1 << 21) + 70, 2112
+    g = gen(C)
+    last = torch.randn((90, C), generator=g).to(BF16)
+    x = torch.zeros((R, C), dtype=BF16, device="cuda")
+    x[-90:] = cuda(last)
+    q = torch.full((R, C), 9, dtype=torch.uint8, device="cuda")
+    s = torch.zeros((R, ref.pitch(C)), dtype=torch.uint8, device="cuda")
+    y = torch.empty_like(x)
+    small = [torch.zeros((90, C), dtype=torch.uint8, device="cuda"),
+             torch.zeros((90, ref.pitch(C)), dtype=torch.uint8, device="cuda")]
+    moe.quant_rows(x, q, s)
+    moe.quant_rows(x[-90:].contiguous(), *small)
+    assert torch.equal(q[-90:], small[0]) and torch.equal(s[-90:], small[1])
+    assert not bool(q[:-90].any())
+    moe.norm_quant(x, None, None, 1e-5, None, y, q, s)
+    z = torch.empty((90, C), dtype=BF16, device="cuda")
+    moe.norm_quant(x[-90:].contiguous(), None, None, 1e-5, None, z, *small)
+    assert torch.equal(q[-90:], small[0]) and torch.equal(y[-90:], z)
+    assert not bool(y[:-90].any())
+
+
 @gpu
 @pytest.mark.parametrize("ex,ew", [(-67, -66), (45, 40)])
 @pytest.mark.parametrize("R", [3, 30, 90, 400])
@@ -474,6 +559,22 @@ def test_group_gemm_of_tokens_that_name_an_expert_twice(T):
 
 
 @gpu
+@pytest.mark.parametrize("T", [1, 40, 300, 4100])
+def test_no_token_for_any_expert(T):
+    E, H, I = 4, 192, 1024
+    g = gen(T)
+    d = moe.dims(T, H, I, E, 2)
+    off = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    slot = torch.full((2 * T,), -(1 << 30), dtype=torch.int32, device="cuda")
+    t = ffn_inputs(g, T, H, I, E)
+    ws = torch.full((moe.scaled_workspace_bytes(d),), 0xA5, dtype=torch.uint8, device="cuda")
+    y, z = torch.full((2 * T, H), 7.0, device="cuda"), torch.full((2 * T, I), 7.0, device="cuda")
+    moe.ffn_group_scaled(d, 0, E, off, slot, *t, y, ws)
+    moe.gemm_group_scaled(d, 0, E, off, slot, t[0], t[1], t[2], t[3], z)
+    assert bool((y == 7).all()) and bool((z == 7).all()) and bool((ws == 0xA5).all())
+
+
+@gpu
 @pytest.mark.parametrize("T", [1, 40, 200])
 def test_ffn_keeps_a_nan_scale_in_its_token(T):
     E, k, H, I = 4, 2, 192, 192
@@ -525,6 +626,8 @@ GROUPS = [
     (2101, 4, 2, 0, 4, 2112, 192, [1, 0.6, 1, 0.8]),
     # tails in a round of their own
     (2068, 2, 2, 0, 2, 4096, 64, None),
+    (1500, 256, 4, 0, 256, 64, 64, None),  # the most experts
+    (9, 256, 2, 0, 256, 128, 192, None),
 ]
 
 
