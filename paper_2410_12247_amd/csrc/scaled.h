@@ -56,6 +56,7 @@ hipError_t launch_scaled_swiglu(const ScaledGemm &g, const ScaledLoad &load, hip
 // tiles_n: column tiles of the (first) tiled launch (scaled_tiles).
 constexpr int64_t kStreamRows = 16;  // per expert that has any
 bool scaled_stream_fits(int tiles_n, const ScaledLoad &load);
+bool scaled_stream_product_fits(int n, int k, const ScaledLoad &load);  // of one product
 constexpr int scaled_tiles(bool swiglu, int n) { return (n + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); }
 hipError_t launch_stream_scaled(const ScaledGemm &g, int y_type, bool from_h,
                                 const ScaledLoad &load, hipStream_t s);

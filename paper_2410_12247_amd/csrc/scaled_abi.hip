@@ -71,7 +71,7 @@ ScaledLoad expected_load(const moe_dims &d) {
 ScaledLoad dense_load(int64_t rows) { return {(double)rows, 1.0, rows, 1}; }
 
 hipError_t product(const ScaledGemm &g, int y_type, const ScaledLoad &load, hipStream_t s) {
-    if (scaled_stream_fits(scaled_tiles(false, g.N), load))
+    if (scaled_stream_product_fits(g.N, g.K, load))
         return launch_stream_scaled(g, y_type, false, load, s);
     return scaled_mid_fits(g.N, load) ? launch_mid_scaled(g, y_type, load.max_rows, s)
                                       : launch_scaled_gemm(g, y_type, load, s);

@@ -376,6 +376,20 @@ hipError_t go_out(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
 bool scaled_stream_fits(int tiles_n, const ScaledLoad &load) {
     return load.rows <= kStreamRows * load.active && 2 * tiles_n * load.active < device_cu_count();
 }
+// A product of 32 blocks of K and more, four and more for each wave, goes this way
+// up to eight tiles per compute unit: over few rounds the last one is part full.
+// Tiled -> this, us: four tokens 14336 x 4096 (5.5 experts, 306 tiles) 71 -> 58, 60
+// tokens 5120 x 4096 (360 tiles) 87 -> 76, 32 tokens 14336 x 4096 (1790) 410 -> 356,
+// 8 rows x 65536 x 4096 (256) 73 -> 60, 16 x 32768 x 8192 (128) 63.5 -> 65.7; 100 tokens
+// 14336 x 4096 (3580) 785 -> 859; of 16 blocks, 60 tokens 5120 x 2048 39.5 -> 46,
+// of 12, 61 tokens 5120 x 1536 31.7 -> 40.6.  (Not an FFN as a whole: its gate and up
+// product has twice the operands in flight, and its down product quantises as it reads;
+// four tokens 4096 x 3584 61 -> 69.)
+bool scaled_stream_product_fits(int n, int k, const ScaledLoad &load) {
+    return scaled_stream_fits(scaled_tiles(false, n), load) ||
+           (load.rows <= kStreamRows * load.active && scale_blocks(k) >= 32 &&
+            scaled_tiles(false, n) * load.active <= 8.0 * device_cu_count());
+}
 
 // Where the chip runs the workgroups at once.  The grid covers the most rows an
 // expert can have, at no more than eight empty workgroups for each that may run.

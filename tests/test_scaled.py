@@ -439,6 +439,21 @@ def test_gemm_past_offsets_of_32_bits(R, N, K):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("R", [1, 5, 16])
+def test_gemm_of_few_rows_and_many_columns(R, dtype):
+    N, K = 33024, 4096
+    g = gen(R)
+    x, v = ref.small_integers(g, R, K), ref.small_integers(g, N, 256)
+    w = torch.zeros((N, K), dtype=torch.uint8, device="cuda")
+    w[:, 5::16] = cuda(v)
+    y = torch.empty((R, N), dtype=dtype, device="cuda")
+    moe.gemm_scaled(cuda(x), ones(R, ref.pitch(K)), w, ones(ref.blocks(N), ref.pitch(K)), y)
+    want = ref.decode(x)[:, 5::16] @ ref.decode(v).T
+    assert torch.equal(y.cpu(), want.to(F32).to(dtype))
+
+
+@gpu
 @pytest.mark.parametrize("T,N,K", [(20, 1024, 1 << 20), (200, 1024, 1 << 20), (200, 32768, 32768)])
 def test_group_gemm_past_offsets_of_32_bits(T, N, K):
     """The last expert's weights begin 4 GiB behind the first's."""
