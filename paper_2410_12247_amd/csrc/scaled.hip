@@ -324,7 +324,10 @@ struct TileLoop {
         l_tau += G;
         l_n += 1;
         l_idx ^= 1;
-        if (np < C::NS - 1 && g.row_map) landed<0>();  // its indices may be on their way
+        // Its indices were requested at the last crossing, np pairs ago; the waits in
+        // between let AHEAD requests stay on their way, those of NS - 2 pairs and a
+        // token tile.  So they cover the indices only where np >= NS - 1.
+        if (np < C::NS - 1 && g.row_map) landed<0>();
         bind();
         plan_tile(l_tau + G, l_n + 1, l_idx ^ 1);
     }
@@ -512,9 +515,11 @@ struct TileLoop {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
     }
-    // Every wave's requests so far but the youngest N have landed.
+    // Every wave's requests so far but the youngest N have landed, and its LDS
+    // reads are done.
     template <int N>
     __device__ __forceinline__ void landed() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         wait_vmcnt<N>();
         __builtin_amdgcn_s_barrier();
     }
@@ -656,14 +661,19 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
     if (first >= t.total) return;
     t.l_tau = first;
     t.l_n = 0;
+    // Where a tile has at most NS pairs, the first requests reach the second tile
+    // and those behind it.  So the second tile's indices are waited for with the
+    // first one's; the third tile's, which take the first one's place, are requested
+    // once every wave has read those; and a wait behind each pair covers the ones
+    // requested on the way.
     t.plan_tile(first, 0, 0);
+    t.plan_tile(first + t.G, 1, 1);
     t.template landed<0>();
     t.bind();
-    t.plan_tile(first + t.G, 1, 1);
+    if (g.row_map && t.np <= C::NS) t.template landed<0>();
 #pragma unroll
     for (int i = 0; i < C::NS; ++i) {
         t.request_pair();
-        // (a tile of few pairs: the next one's indices)
         if (i == C::NS - 1 || (g.row_map && t.np < C::NS)) t.template landed<0>();
     }
     typename L::FragsA a0, a1;
