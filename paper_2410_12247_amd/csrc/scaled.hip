@@ -422,6 +422,55 @@ struct TileLoop {
     __device__ __forceinline__ static float scale(int s) {
         return __uint_as_float((uint32_t)s << 23);
     }
+    // e4m3 values are 2^-9 to 448, so with bytes of 10 to 246 they are normal bf16
+    // numbers.  Rows that meet another byte in a tile (a block whose largest value is
+    // below 2^-108 or above 2^119; far: their lanes) get sums taken from memory again,
+    // the scales applied to each block's fp32 sums as the few rows' kernels do.
+    // Watching for them costs 1%.  (Scaling every block's sums in the loop, or a branch
+    // there to the 8-bit instruction, moves the accumulators about in every half: DBRX
+    // FFN of 64 tokens 89 -> 121 to 127 us.)
+    uint64_t far;
+    __device__ __forceinline__ void note_far(int sw0, int sw1) {
+        auto out = [](int s) { return (uint32_t)(s - 10) > 236u; };
+        far |= __builtin_amdgcn_ballot_w64(out(sx[0]) || out(sw0) || out(sw1));
+    }
+    __device__ __forceinline__ void sums_of_far(const Tile &t) {
+        const int row = min(row0(0) + (lane & 31), t.m_valid - 1);
+        const int64_t src = g.row_map ? g.row_map[t.r0 + row] / g.slot_div : t.r0 + row;
+        const int64_t we = (int64_t)(g.e_first + t.e) * g.N + t.n0;
+        const int64_t se = (int64_t)(g.e_first + t.e) * scale_blocks(g.N) + t.n0 / kScaleBlock;
+        const uint8_t *xp = g.x + src * K + (lane >> 5) * 32;
+        const bool mine = far >> lane & 1;
+#pragma unroll
+        for (int i = 0; i < C::TN; ++i) {
+            const int wrow = min(wn * 64 + (i & 1) * 32 + (lane & 31), t.n_valid - 1);
+            const uint8_t *wp = (i >= 2 ? g.w1 : g.w0) + (we + wrow) * K + (lane >> 5) * 32;
+            floatx16 sum;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+            for (int kb = 0; kb < np; ++kb) {
+                const int st = g.xs[src * SK + kb], sw = (i >= 2 ? g.s1 : g.s0)[se * SK + kb];
+                floatx16 p;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = 0.f;
+                for (int k = kb * C::BK; k < min(K, (kb + 1) * C::BK); k += 64) {
+                    const u32x4 *a = reinterpret_cast<const u32x4 *>(wp + k);
+                    const u32x4 *b = reinterpret_cast<const u32x4 *>(xp + k);
+                    const u32x4 av[2] = {a[0], a[1]}, bv[2] = {b[0], b[1]};
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            widen(av, h, 1.f), widen(bv, h, 1.f), p, 0, 0, 0);
+                }
+                const float nan = sw == 255 || st == 255 ? __builtin_nanf("") : 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    sum[r] += __builtin_amdgcn_ldexpf(p[r] + nan, st + sw - 254);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][0][r] = mine ? sum[r] : acc[i][0][r];
+        }
+    }
     // One half's MFMAs, and between them the parts f(m) of NM of its reads and
     // requests.  (The sums count as used behind them: the compiler would move the
     // MFMAs behind branches that follow, away from those.)
@@ -501,6 +550,7 @@ struct TileLoop {
                                                 int sw1) {
         uint32_t b0, b1;
         backs(b0, b1);
+        if constexpr (EXACT) note_far(sw0, sw1);
         c_slot = next(c_slot);
         half(ca, cb, sw0, sw1, [&](int m) {
             part<2 * C::TN + 4 * C::TM, true>(m, [&](int r) {
@@ -737,6 +787,7 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
             for (int j = 0; j < C::TM; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) t.acc[i][j][r] = 0.f;
+        t.far = 0;
         // b1: the pair's second half's token fragments, n1: the next one's
         auto pair = [&](int p, typename L::FragsB &b1, typename L::FragsB &n1) {
             const int s0 = w0 & 255, s1 = w1 & 255;
@@ -766,6 +817,8 @@ __device__ __forceinline__ void run_tiles(const ScaledGemm &g, const W &walk, in
         }
         const Tile tile = t.planned(n);
         if (tau + t.G < t.total) first_words(t.planned(n + 1));  // (bound by now)
+        if constexpr (L::EXACT)
+            if (t.far) t.sums_of_far(tile);
         epilogue<MODE>(g, tile, t, smem);
     }
     t.template landed<0>();  // requests behind the last pair
