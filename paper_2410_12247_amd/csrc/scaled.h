@@ -54,7 +54,8 @@ hipError_t launch_scaled_swiglu(const ScaledGemm &g, const ScaledLoad &load, hip
 // leaves its rows in fp32 (out [.][N], out_s unused); the product behind it
 // takes them so (from_h: x is fp32) and quantises them as it reads them.
 // tiles_n: column tiles of the (first) tiled launch (scaled_tiles).
-constexpr int64_t kStreamRows = 16;  // per expert that has any
+constexpr int64_t kStreamRows = 16;    // expected per expert that has any
+constexpr int64_t kStreamTokens = 48;  // the most rows of an expert, in an FFN
 bool scaled_stream_fits(int tiles_n, const ScaledLoad &load);
 bool scaled_stream_product_fits(int n, int k, const ScaledLoad &load);  // of one product
 constexpr int scaled_tiles(bool swiglu, int n) { return (n + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); }

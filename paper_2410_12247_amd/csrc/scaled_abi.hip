@@ -96,7 +96,7 @@ FfnWs ffn_ws(int64_t rows, int64_t few, int32_t inter, const ScaledLoad &load) {
     return w;
 }
 FfnWs ffn_ws(const moe_dims *d) {
-    const int64_t few_tokens = kStreamRows * d->experts / d->top_k;
+    const int64_t few_tokens = std::min(kStreamTokens, kStreamRows * d->experts / d->top_k);
     return ffn_ws(row_cap(d), few_tokens * std::min(d->top_k, d->local_count), d->inter,
                   expected_load(*d));
 }

@@ -368,27 +368,43 @@ hipError_t go_out(const ScaledGemm &g, const ScaledLoad &load, hipStream_t s) {
 
 }  // namespace
 
-// Up to 16 rows per expert a weight is read once; below half a tile per compute
-// unit the tiled launch leaves most of the chip idle.  Tiled -> this, us: FFN of
-// one token 4096 x 3584 (two experts, 56 tiles) 62 -> 26, 6144 x 1344 (four, 44)
-// 64 -> 33, eight tokens 5120 x 1536 (63) 60 -> 34; four tokens 6144 x 1344 (120
-// tiles) 81 and 81, 61 tokens 5120 x 1536 (216) 94 -> 105.
+// The kernel reads an expert's weights once for every 16 of its rows, one workgroup
+// after the other's steps, so it is for launches in which no expert can have many,
+// however uneven the routing: up to 16 tokens for one product, up to 48 for an FFN,
+// whose tiled launches of few tiles (below half a tile per compute unit) leave most
+// of the chip idle twice.  Tiled -> this, us, from weights that no cache holds, even
+// loads and ones with exponents of 1.2:
+//   product 1024 x 2048, 16 experts, top 4: 16 tokens 12.7 -> 10.7 and 12.6 -> 10.9;
+//     32 tokens 12.7 -> 11.0 and 12.7 -> 14.0; 48 tokens 12.8 -> 13.5 and 12.9 -> 18.0
+//   product 1536 x 5120, 20 of 160 experts, top 6: 16 tokens 26.3 -> 24.2 and 22.3 ->
+//     18.4; 61 tokens 31.2 -> 36.5 and 30.0 -> 45.9; 420 tokens 34 -> 65 and 48 -> 222
+//   FFN 2048 x 512, 64 experts, top 8: 32 tokens 31.9 -> 15.6 and 31.2 -> 25.5; 48
+//     tokens 32.0 -> 16.0 and 31.8 -> 35.4; 60 tokens 32 -> 16 and 32 -> 45
+//   FFN 2048 x 768, 20 of 160: 48 tokens 39.9 -> 32.1 and 38.1 -> 38.1; 420 tokens
+//     42 -> 57 and 43 -> 254
+//   FFN of one token 4096 x 3584 (two experts, 56 tiles) 62 -> 26; of four 61 -> 69
 bool scaled_stream_fits(int tiles_n, const ScaledLoad &load) {
-    return load.rows <= kStreamRows * load.active && 2 * tiles_n * load.active < device_cu_count();
+    return load.max_rows <= kStreamTokens && load.rows <= kStreamRows * load.active &&
+           2 * tiles_n * load.active < device_cu_count();
 }
 // A product of 32 blocks of K and more, four and more for each wave, goes this way
 // up to eight tiles per compute unit: over few rounds the last one is part full.
-// Tiled -> this, us: four tokens 14336 x 4096 (5.5 experts, 306 tiles) 71 -> 58, 60
-// tokens 5120 x 4096 (360 tiles) 87 -> 76, 32 tokens 14336 x 4096 (1790) 410 -> 356,
-// 8 rows x 65536 x 4096 (256) 73 -> 60, 16 x 32768 x 8192 (128) 63.5 -> 65.7; 100 tokens
-// 14336 x 4096 (3580) 785 -> 859; of 16 blocks, 60 tokens 5120 x 2048 39.5 -> 46,
-// of 12, 61 tokens 5120 x 1536 31.7 -> 40.6.  (Not an FFN as a whole: its gate and up
-// product has twice the operands in flight, and its down product quantises as it reads;
-// four tokens 4096 x 3584 61 -> 69.)
+// Tiled -> this, us: four tokens 14336 x 4096 (5.5 experts, 306 tiles) 71 -> 58, 12
+// tokens 3584 x 4096 of eight experts 30.6 -> 29.4, 8 rows x 65536 x 4096 (256) 73 ->
+// 60, 16 x 32768 x 8192 (128) 63.5 -> 65.7.  (Not an FFN as a whole: its gate and up
+// product has twice the operands in flight, and its down product quantises as it reads.)
+// Over more than one round that holds for 32 tokens too: 14336 x 4096 of eight experts
+// 118 -> 99, with an exponent of 1.2 119 -> 106; 8192 x 6144 of 16 158 -> 159 and 153 ->
+// 162, 17 tokens 160 -> 146 and 158 -> 135; of a round 4096 x 14336 86 -> 96 and 87 ->
+// 110.  (Of 160 experts with 20 here, 16384 x 5120, 17 tokens 152 -> 166, 24 with 1.2
+// 119 -> 151, 32 256 -> 231.)
 bool scaled_stream_product_fits(int n, int k, const ScaledLoad &load) {
-    return scaled_stream_fits(scaled_tiles(false, n), load) ||
-           (load.rows <= kStreamRows * load.active && scale_blocks(k) >= 32 &&
-            scaled_tiles(false, n) * load.active <= 8.0 * device_cu_count());
+    const double tiles = scaled_tiles(false, n) * load.active, cus = device_cu_count();
+    const bool wide = scale_blocks(k) >= 32 && tiles <= 8 * cus;
+    if (load.max_rows > kStreamRows)
+        return load.max_rows <= 2 * kStreamRows && load.rows <= kStreamRows * load.active &&
+               wide && tiles > cus;
+    return wide || scaled_stream_fits(scaled_tiles(false, n), load);
 }
 
 // Where the chip runs the workgroups at once.  The grid covers the most rows an
