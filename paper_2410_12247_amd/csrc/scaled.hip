@@ -426,7 +426,8 @@ struct TileLoop {
     // numbers.  Rows that meet another byte in a tile (a block whose largest value is
     // below 2^-108 or above 2^119; far: their lanes) get sums taken from memory again,
     // the scales applied to each block's fp32 sums as the few rows' kernels do.
-    // Watching for them costs 1%.  (Scaling every block's sums in the loop, or a branch
+    // Watching for them costs 1%, a few such rows 80% (DBRX FFN of 64 tokens 103 -> 187
+    // us; a byte of every row 245): a chain of loads as long as K.  (Scaling every block's sums in the loop, or a branch
     // there to the 8-bit instruction, moves the accumulators about in every half: DBRX
     // FFN of 64 tokens 89 -> 121 to 127 us.)
     uint64_t far;
@@ -440,36 +441,52 @@ struct TileLoop {
         const int64_t we = (int64_t)(g.e_first + t.e) * g.N + t.n0;
         const int64_t se = (int64_t)(g.e_first + t.e) * scale_blocks(g.N) + t.n0 / kScaleBlock;
         const uint8_t *xp = g.x + src * K + (lane >> 5) * 32;
-        const bool mine = far >> lane & 1;
+        const uint8_t *wp[C::TN];
+        floatx16 sum[C::TN];
 #pragma unroll
         for (int i = 0; i < C::TN; ++i) {
             const int wrow = min(wn * 64 + (i & 1) * 32 + (lane & 31), t.n_valid - 1);
-            const uint8_t *wp = (i >= 2 ? g.w1 : g.w0) + (we + wrow) * K + (lane >> 5) * 32;
-            floatx16 sum;
+            wp[i] = (i >= 2 ? g.w1 : g.w0) + (we + wrow) * K + (lane >> 5) * 32;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum[r] = 0.f;
-            for (int kb = 0; kb < np; ++kb) {
-                const int st = g.xs[src * SK + kb], sw = (i >= 2 ? g.s1 : g.s0)[se * SK + kb];
+            for (int r = 0; r < 16; ++r) sum[i][r] = 0.f;
+        }
+        for (int kb = 0; kb < np; ++kb) {
+            const int st = g.xs[src * SK + kb];
+            const int k[2] = {kb * C::BK, min(kb * C::BK + 64, K - 64)};
+            const bool one = k[0] == k[1];  // half a block: its one half again, unused
+            u32x4 b[2][2], a[C::TN][2][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    b[h][c] = reinterpret_cast<const u32x4 *>(xp + k[h])[c];
+#pragma unroll
+                    for (int i = 0; i < C::TN; ++i)
+                        a[i][h][c] = reinterpret_cast<const u32x4 *>(wp[i] + k[h])[c];
+                }
+#pragma unroll
+            for (int i = 0; i < C::TN; ++i) {
+                const int sw = (i >= 2 ? g.s1 : g.s0)[se * SK + kb];
                 floatx16 p;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) p[r] = 0.f;
-                for (int k = kb * C::BK; k < min(K, (kb + 1) * C::BK); k += 64) {
-                    const u32x4 *a = reinterpret_cast<const u32x4 *>(wp + k);
-                    const u32x4 *b = reinterpret_cast<const u32x4 *>(xp + k);
-                    const u32x4 av[2] = {a[0], a[1]}, bv[2] = {b[0], b[1]};
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
+                for (int h = 0; h < 8; ++h)
+                    if (h < 4 || !one)
                         p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            widen(av, h, 1.f), widen(bv, h, 1.f), p, 0, 0, 0);
-                }
+                            widen(a[i][h >> 2], h & 3, 1.f), widen(b[h >> 2], h & 3, 1.f), p, 0, 0,
+                            0);
                 const float nan = sw == 255 || st == 255 ? __builtin_nanf("") : 0.f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    sum[r] += __builtin_amdgcn_ldexpf(p[r] + nan, st + sw - 254);
+                    sum[i][r] += __builtin_amdgcn_ldexpf(p[r] + nan, st + sw - 254);
             }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][0][r] = mine ? sum[r] : acc[i][0][r];
         }
+        const bool mine = far >> lane & 1;
+#pragma unroll
+        for (int i = 0; i < C::TN; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][0][r] = mine ? sum[i][r] : acc[i][0][r];
     }
     // One half's MFMAs, and between them the parts f(m) of NM of its reads and
     // requests.  (The sums count as used behind them: the compiler would move the
