@@ -8,14 +8,15 @@
 // token row.
 //
 // Large launches are bound by the matrix cores, and those by the board's power:
-// the chip runs at 1.85 to 1.9 GHz under them.  16384 x 5120 x 4096 takes 265 us,
-// 2.59 PFLOP/s (a library's 8-bit product of 8192^3 2.71), the cores busy in 66%
-// of the cycles; the Mixtral FFN of 16384 tokens 1.20 ms, 2.41 PFLOP/s; DBRX gate
-// of 8192 tokens 253 us, 2.14 (N is 5.25 tiles of 256: 15% of the products are
+// the chip runs at 1.55 to 1.9 GHz under them, and a launch's time depends on what
+// ran before it.  16384 x 5120 x 4096 takes 263 us, 2.61 PFLOP/s (a library's 8-bit
+// product of 8192^3 2.71), the cores busy in 65% of the cycles; the Mixtral FFN of
+// 16384 tokens 1.22 ms, 2.36 PFLOP/s (1.34 under launches of its own only); DBRX gate
+// of 8192 tokens 253 to 259 us, 2.1 (N is 5.25 tiles of 256: 15% of the products are
 // padding).  Few rows are bound by the weights' stream: DBRX FFN of 64 tokens 91
-// us, 4.4 TB/s; DeepSeekV2 down product of 4099 tokens with a Zipf load 68 to 75
-// us, 3.9 TB/s and 1.2 PFLOP/s, between the two, its second round of tiles part
-// full.
+// us, 4.4 TB/s; DeepSeekV2 gate product of 61 tokens (20 experts, 157 MB) 31 us, 5.1
+// TB/s; its down product of 4099 tokens with a Zipf load 66 to 75 us, 4.0 TB/s and 1.2
+// PFLOP/s, between the two, its second round of tiles part full.
 #include <algorithm>
 
 #include "lds_dma.h"

@@ -631,8 +631,7 @@ GROUPS = [
     (150, 8, 2, 6, 2, 256, 704, None),
     (333, 6, 3, 0, 6, 576, 192, [8, 1, 0.2, 4, 0, 1]),
     (700, 2, 2, 0, 2, 128, 128, None),
-    # four tile rows per expert and more: experts whose last rows are a tail, a
-    # whole tile, and nothing
+    # experts of several tiles of 128 x 128, the last one part full, whole, and none
     (2100, 2, 1, 0, 2, 320, 192, None),
     (2600, 3, 1, 0, 2, 192, 64, [1, 1, 0.05]),
     (4352, 4, 4, 0, 4, 64, 128, None),
@@ -680,7 +679,7 @@ FFNS = [
     (70, 8, 2, 0, 8, 320, 128, [1, 1, 0, 0, 5, 1, 1, 1]),
     (200, 3, 2, 0, 3, 128, 448, None),
     (290, 2, 1, 0, 2, 576, 64, [1, 0]),
-    (1101, 1, 1, 0, 1, 192, 192, None),  # tails in both products
+    (1101, 1, 1, 0, 1, 192, 192, None),  # tiles of 64 rows, and of 32 x 32
     # tiles of 128 rows, and of 256 with tails
     (1001, 4, 2, 0, 4, 192, 1024, None),
     (2101, 4, 2, 0, 4, 192, 1024, [1, 0.6, 1, 0.8]),
