@@ -560,6 +560,118 @@ moe_status moe_forward_scaled(const moe_dims *dims, const void *x, int32_t x_typ
                               float *topk_w, int32_t *counts, void *ws, size_t ws_bytes,
                               void *stream);
 
+/* ---- Routing by scores ---------------------------------------------------
+ * moe_route's softmax top-k with the rules that larger layers are trained with:
+ * sigmoid scores, a bias that balances the experts' load, experts in groups.
+ * The router's product comes from moe_route_logits or elsewhere. */
+
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+enum { MOE_GROUP_MAX = 0, MOE_GROUP_TOP_TWO = 1 };
+/* Host memory. */
+typedef struct {
+    int32_t score;       /* MOE_SCORE_SOFTMAX (over all experts) or _SIGMOID */
+    int32_t groups;      /* G, dividing the experts; group g holds experts
+                            [g E/G, (g + 1) E/G).  1: no groups */
+    int32_t top_groups;  /* groups kept, 1 .. G; they have to hold top_k experts */
+    int32_t group_score; /* a group's value: its best choice (MOE_GROUP_MAX) or the
+                            sum of its two best (MOE_GROUP_TOP_TWO) */
+    float scale;         /* factor of the weights, finite */
+} moe_routing;
+
+/* The router's logits z[t][e], moe_route's chain without a bias: x [T][H] bf16,
+ * 16-byte aligned; w_router [E][H] fp32; logits [T][E] fp32. */
+moe_status moe_route_logits(const moe_dims *dims, const moe_bf16 *x, const float *w_router,
+                            float *logits, void *stream);
+
+/* Experts and weights from logits [T][E] of logits_type (MOE_FP32 or MOE_BF16).
+ * For each token, with bias [E] fp32 or NULL:
+ *   s[e] = softmax(z)[e] over all experts, or 1 / (1 + exp(-z[e]))
+ *   c[e] = s[e] + bias[e]             the choice (without a bias its order is z's)
+ *   groups: the top_groups largest values (descending; ties: the lower group)
+ *   topk_ids[t][0..k)  the k largest c of the groups kept, by (c descending, e
+ *                      ascending)
+ *   topk_w[t][j] = scale * s[id_j], with dims->renormalize scale * s[id_j] / sum
+ *                  of the chosen s
+ * Choices and group values are compared in 64 bits, weights computed in 64 bits
+ * and rounded to fp32; choices nearer to each other than 2^-50 may come in either
+ * order.  An expert is switched off by a logit of -inf, or by a choice of -inf or
+ * NaN (its bias'); it is never chosen.  Where fewer than k are left, the last ids
+ * are -1 with weight 0 (moe_permute and moe_combine pass over them).  A token with
+ * a NaN logit, or with +inf under softmax, has NaN weights, and its experts are
+ * the k largest logits of all groups, a NaN as the largest.
+ * dims gives tokens, experts, top_k and renormalize; the rest is not used. */
+moe_status moe_route_scores(const moe_dims *dims, const moe_routing *routing, const void *logits,
+                            int32_t logits_type, const float *bias, int32_t *topk_ids,
+                            float *topk_w, void *stream);
+
+/* Its gradient: dlogits [T][E] (of logits_type, every element written) from the
+ * chosen topk_ids and dtopk_w [T][k], the gradient of topk_w.  The choice itself
+ * has none, nor has the bias.  An id outside [0, E) takes no part; one that is
+ * named twice has the sum of both.  With dims->renormalize or sigmoid scores the
+ * logits of experts that were not chosen are not read and get 0. */
+moe_status moe_route_scores_backward(const moe_dims *dims, const moe_routing *routing,
+                                     const void *logits, int32_t logits_type,
+                                     const int32_t *topk_ids, const float *dtopk_w, void *dlogits,
+                                     void *stream);
+
+/* ---- Low-rank adapters ---------------------------------------------------
+ * A batch holds rows of several requests, each with an adapter of its own beside
+ * a projection y = x W^T that all share.  An adapter is a pair A [rank][k],
+ * B [n][rank] and a scale.  Rows are ordered by adapter as tokens are by expert:
+ * moe_permute with tokens = rows, experts = count, top_k = 1 and the rows'
+ * adapters as topk_ids (-1: none) gives offsets, sorted_slot and slot_row, once
+ * for all projections of a batch.
+ * Tensors must be 16-byte aligned, scale and index tensors 4-byte aligned.  The
+ * calls allocate nothing, never synchronise and can be captured; a workspace
+ * (16-byte aligned) serves one call at a time, and one for some rows serves fewer
+ * too.  Results are deterministic; their bits depend on rows and count (which
+ * pick the tiles), not on the other rows' adapters.  Offsets outside [0, rows] are
+ * cut to it, and entries of sorted_slot outside [0, rows) are passed over. */
+
+/* Host memory; its pointers are device ones. */
+typedef struct {
+    int32_t count;      /* adapters, 1 .. 256 */
+    int32_t rank;       /* a multiple of 8 up to 256; adapters of a smaller rank are
+                           padded with zeros */
+    int32_t n, k;       /* widths of the projection's output and input, multiples of
+                           64 up to 2^20 */
+    const moe_bf16 *a;  /* [count][rank][k] */
+    const moe_bf16 *b;  /* [count][n][rank] */
+    const float *scale; /* [count], or NULL for 1 */
+} moe_adapters;
+
+/* Workspace of moe_adapter_rows.  Host-only; 0 for invalid arguments. */
+size_t moe_adapter_workspace_bytes(int64_t rows, const moe_adapters *adapters);
+
+/* y[r] = base[r] + scale[e] * B[e] (A[e] x[r]) for every row r with an adapter e,
+ * y[r] = base[r] for the others.  x [rows][k] bf16; base and y [rows][n] of y_type
+ * (MOE_BF16 or MOE_FP32).  base may be y itself (the projection's output; rows
+ * without an adapter are then not touched and slot_row may be NULL), or NULL for
+ * zeros.  A x is held in fp32. */
+moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const int32_t *offsets,
+                            const int32_t *sorted_slot, const int32_t *slot_row,
+                            const moe_bf16 *x, const void *base, void *y, int32_t y_type, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/* Workspace of moe_adapter_backward.  Host-only; 0 for invalid arguments. */
+size_t moe_adapter_backward_bytes(int64_t rows, const moe_adapters *adapters);
+
+/* Its gradient from dy [rows][n] bf16, the gradient of y (base's is dy itself):
+ *   dx[r] = dx_base[r] + scale[e] * A[e]^T (B[e]^T dy[r])
+ *   da[e] (+)= scale[e] * sum over e's rows of (B[e]^T dy[r]) x[r]^T
+ *   db[e] (+)= scale[e] * sum over e's rows of dy[r] (A[e] x[r])^T
+ * dx, dx_base [rows][k] of dx_type; dx_base (what the projection's own gradient
+ * left) may be dx itself or NULL, as base above.  da [count][rank][k], db
+ * [count][n][rank] fp32, added to what they hold with accumulate = 1; else
+ * adapters without rows get zeros.  dx, or da and db together, may be NULL;
+ * without da and db x is not read. */
+moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
+                                const int32_t *offsets, const int32_t *sorted_slot,
+                                const int32_t *slot_row, const moe_bf16 *x, const moe_bf16 *dy,
+                                const void *dx_base, void *dx, int32_t dx_type, float *da,
+                                float *db, int32_t accumulate, void *ws, size_t ws_bytes,
+                                void *stream);
+
 const char *moe_status_string(moe_status s);
 const char *moe_last_error(void);
 

@@ -332,15 +332,21 @@ hipError_t launch_mfma(const moe_dims &d, const bf16_t *x, const float *wr, cons
 }
 
 template <int TT, int TE, int TW, int EW, int NS>
-hipError_t launch_mfma_z(const moe_dims &d, const bf16_t *x, const float *wr, const float *bias,
-                         int32_t *ids, float *w, float *z, hipStream_t s,
-                         const DispatchOut *disp) {
+hipError_t launch_mfma_logits(const moe_dims &d, const bf16_t *x, const float *wr,
+                              const float *bias, float *z, hipStream_t s) {
     using C = mfma::Cfg<TT, TE, TW, EW, NS>;
     const dim3 grid((unsigned)((d.tokens + C::TOK - 1) / C::TOK),
                     (unsigned)((d.experts + C::EP - 1) / C::EP));
     route_mfma_kernel<TT, TE, TW, EW, NS, true><<<grid, 64 * C::WAVES, 0, s>>>(
-        x, wr, bias, d.tokens, d.hidden, d.experts, d.top_k, d.renormalize, ids, w, z);
-    const hipError_t e = hipGetLastError();
+        x, wr, bias, d.tokens, d.hidden, d.experts, d.top_k, d.renormalize, nullptr, nullptr, z);
+    return hipGetLastError();
+}
+
+template <int TT, int TE, int TW, int EW, int NS>
+hipError_t launch_mfma_z(const moe_dims &d, const bf16_t *x, const float *wr, const float *bias,
+                         int32_t *ids, float *w, float *z, hipStream_t s,
+                         const DispatchOut *disp) {
+    const hipError_t e = launch_mfma_logits<TT, TE, TW, EW, NS>(d, x, wr, bias, z, s);
     if (e != hipSuccess) return e;
     return launch_route_select(d, z, ids, w, s, disp);
 }
@@ -419,6 +425,17 @@ bool mfma_router_selects_apart(const moe_dims &d, const float *logits) {
     const double cz = (double)((tile_waves(d) + simds - 1) / simds) * 20.0 + 10.0;
     return cz <= std::min(mfma_cost(d.tokens, 16, (eb + 3) / 4),
                           mfma_cost(d.tokens, 32, blocks_per_wave(eb)));
+}
+
+// One tile of a wave while the SIMDs take them at once, then more tokens and
+// experts per workgroup, which read fewer operands.
+hipError_t launch_route_logits(const moe_dims &d, const bf16_t *x, const float *wr, float *z,
+                               hipStream_t s) {
+    const int64_t simds = 4 * (int64_t)device_cu_count();
+    if (tile_waves(d) <= simds) return launch_mfma_logits<1, 1, 1, 1, 6>(d, x, wr, nullptr, z, s);
+    if (expert_blocks(d) <= 2 || tile_waves(d) <= 4 * simds)
+        return launch_mfma_logits<1, 1, 2, 2, 3>(d, x, wr, nullptr, z, s);
+    return launch_mfma_logits<2, 4, 4, 2, 3>(d, x, wr, nullptr, z, s);
 }
 
 extern "C" int32_t moe_router_shape_for_tests(const moe_dims *d, int32_t *blocks) {

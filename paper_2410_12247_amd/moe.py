@@ -19,6 +19,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmoe.so")
 BF16, FP32 = 0, 1
 GEMM_AUTO, GEMM_GROUP, GEMM_DENSE = 0, 1, 2
 CHUNK_EXPERTS, CHUNK_TOKENS = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_TOP_TWO = 0, 1
 FLAG_TIMING, FLAG_TIMING_GEMM, FLAG_EXACT_ORDER, FLAG_SERIAL = 1, 2, 4, 8
 
 # the entry points include/moe.h declares
@@ -29,7 +31,10 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_guards", "moe_route", "moe_perm
            "moe_last_error", "moe_scale_pitch", "moe_quant_rows", "moe_quant_weights",
            "moe_norm_quant", "moe_gemm_scaled", "moe_gemm_group_scaled",
            "moe_scaled_workspace_bytes", "moe_ffn_group_scaled", "moe_combine_rows",
-           "moe_forward_scaled", "moe_forward_scaled_bytes")
+           "moe_forward_scaled", "moe_forward_scaled_bytes",
+           "moe_route_logits", "moe_route_scores", "moe_route_scores_backward",
+           "moe_adapter_workspace_bytes", "moe_adapter_rows", "moe_adapter_backward_bytes",
+           "moe_adapter_backward")
 
 
 class MoEError(RuntimeError):
@@ -70,6 +75,17 @@ class ScaledWeights(ctypes.Structure):
     _fields_ = [(n + s, ctypes.c_void_p)
                 for n in ("gate", "up", "down", "shared_gate", "shared_up", "shared_down")
                 for s in ("", "_scales")]
+
+
+class Routing(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "groups", "top_groups", "group_score")] + \
+               [("scale", ctypes.c_float)]
+
+
+class Adapters(ctypes.Structure):
+    """The low-rank adapters of a projection (moe_adapters); adapters() fills it."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("count", "rank", "n", "k")] + \
+               [(n, ctypes.c_void_p) for n in ("a", "b", "scale")]
 
 
 class PipelineEval(ctypes.Structure):
@@ -127,6 +143,15 @@ def lib():
     L.moe_forward_scaled_bytes.restype = SZ
     L.moe_forward_scaled.argtypes = [D, P, I32, P, P, ctypes.c_float, P, P, P,
                                      ctypes.POINTER(ScaledWeights), P, P, P, P, P, SZ, P]
+    R, A = ctypes.POINTER(Routing), ctypes.POINTER(Adapters)
+    L.moe_route_logits.argtypes = [D, P, P, P, P]
+    L.moe_route_scores.argtypes = [D, R, P, I32, P, P, P, P]
+    L.moe_route_scores_backward.argtypes = [D, R, P, I32, P, P, P, P]
+    for name in ("moe_adapter_workspace_bytes", "moe_adapter_backward_bytes"):
+        getattr(L, name).argtypes = [I64, A]
+        getattr(L, name).restype = SZ
+    L.moe_adapter_rows.argtypes = [I64, A] + [P] * 6 + [I32, P, SZ, P]
+    L.moe_adapter_backward.argtypes = [I64, A] + [P] * 7 + [I32, P, P, I32, P, SZ, P]
     L.moe_status_string.argtypes = [I32]
     L.moe_status_string.restype = ctypes.c_char_p
     L.moe_last_error.restype = ctypes.c_char_p
@@ -135,7 +160,8 @@ def lib():
                  "moe_choose_pipeline_n", "moe_gemm_plan", "moe_pipeline_plan", "moe_quant_rows",
                  "moe_quant_weights", "moe_norm_quant", "moe_gemm_scaled",
                  "moe_gemm_group_scaled", "moe_ffn_group_scaled", "moe_combine_rows",
-                 "moe_forward_scaled"):
+                 "moe_forward_scaled", "moe_route_logits", "moe_route_scores",
+                 "moe_route_scores_backward", "moe_adapter_rows", "moe_adapter_backward"):
         getattr(L, name).restype = I32
     _lib = L
     return L
@@ -553,6 +579,115 @@ def forward_scaled(d, x, residual, norm_weight, eps, total, w_router, bias, weig
         _arg(dev, "counts", counts, _I32, (d.local_count,)), _arg(dev, "ws", ws, (ws.dtype,),
                                                                   ws.shape),
         ws.numel() * ws.element_size(), _stream_on(dev, stream)))
+
+
+# ---- routing by scores ------------------------------------------------------
+
+
+def routing(score=SCORE_SOFTMAX, groups=1, top_groups=1, group_score=GROUP_MAX,
+            scale=1.0) -> Routing:
+    return Routing(int(score), int(groups), int(top_groups), int(group_score), float(scale))
+
+
+def route_logits(d, x, w_router, logits, stream=None):
+    """logits = x w_router^T, as route computes them (no bias)."""
+    dev = _dev("x", x)
+    _check(lib().moe_route_logits(ctypes.byref(d), _arg(dev, "x", x, _BF16, (d.tokens, d.hidden)),
+                                  _arg(dev, "w_router", w_router, _F32, (d.experts, d.hidden)),
+                                  _arg(dev, "logits", logits, _F32, (d.tokens, d.experts)),
+                                  _stream_on(dev, stream)))
+
+
+def route_scores(d, r, logits, bias, topk_ids, topk_w, stream=None):
+    """Experts and weights of logits fp32 or bf16 by the rules of r (routing()).
+    bias may be None; ids are -1 where no expert is left."""
+    dev, code = _dev("logits", logits), _real("logits", logits)
+    slots = (d.tokens, d.top_k)
+    _check(lib().moe_route_scores(
+        ctypes.byref(d), ctypes.byref(r),
+        _arg(dev, "logits", logits, (logits.dtype,), (d.tokens, d.experts)), code,
+        _arg(dev, "bias", bias, _F32, (d.experts,)),
+        _arg(dev, "topk_ids", topk_ids, _I32, slots), _arg(dev, "topk_w", topk_w, _F32, slots),
+        _stream_on(dev, stream)))
+
+
+def route_scores_backward(d, r, logits, topk_ids, dtopk_w, dlogits, stream=None):
+    """dlogits (of logits' type) from dtopk_w, the gradient of route_scores' topk_w."""
+    dev, code = _dev("logits", logits), _real("logits", logits)
+    shape, slots = (d.tokens, d.experts), (d.tokens, d.top_k)
+    _check(lib().moe_route_scores_backward(
+        ctypes.byref(d), ctypes.byref(r), _arg(dev, "logits", logits, (logits.dtype,), shape),
+        code, _arg(dev, "topk_ids", topk_ids, _I32, slots),
+        _arg(dev, "dtopk_w", dtopk_w, _F32, slots),
+        _arg(dev, "dlogits", dlogits, (logits.dtype,), shape), _stream_on(dev, stream)))
+
+
+# ---- low-rank adapters ------------------------------------------------------
+
+
+def adapters(a, b, scale=None) -> Adapters:
+    """Checks and packs a projection's adapters: a [count, rank, k], b [count, n,
+    rank] bf16, scale [count] fp32 or None; made once and kept with the tensors."""
+    if a.dim() != 3 or b.dim() != 3:
+        raise ValueError("a must be [count, rank, k] and b [count, n, rank]")
+    (C, r, K), N, dev = a.shape, b.shape[1], _dev("a", a)
+    ad = Adapters(C, r, N, K, _arg(dev, "a", a, _BF16, (C, r, K)),
+                  _arg(dev, "b", b, _BF16, (C, N, r)), _arg(dev, "scale", scale, _F32, (C,)))
+    ad.keep = (a, b, scale)
+    ad.device = dev
+    return ad
+
+
+def adapter_workspace_bytes(rows: int, ad: Adapters) -> int:
+    return lib().moe_adapter_workspace_bytes(rows, ctypes.byref(ad))
+
+
+def adapter_backward_bytes(rows: int, ad: Adapters) -> int:
+    return lib().moe_adapter_backward_bytes(rows, ctypes.byref(ad))
+
+
+def _adapter_args(ad, dev, R, offsets, sorted_slot, slot_row):
+    """The handle and addresses of the rows' order (permute's outputs)."""
+    if ad.device != dev:
+        raise ValueError(f"the adapters are on cuda:{ad.device}, the rows on cuda:{dev}")
+    if slot_row is not None:
+        slot_row = slot_row.view(-1)
+    return (ctypes.byref(ad), _arg(dev, "offsets", offsets, _I32, (ad.count + 1,)),
+            _arg(dev, "sorted_slot", sorted_slot, _I32, (R,)),
+            _arg(dev, "slot_row", slot_row, _I32, (R,)))
+
+
+def adapter_rows(ad, offsets, sorted_slot, slot_row, x, base, y, ws, stream=None):
+    """y = base + scale (x A^T) B^T, each row by its adapter; base may be y or
+    None, ws of adapter_workspace_bytes bytes.  The order is permute's of the
+    rows' adapters (top_k 1); slot_row may be None where base is y."""
+    R, _ = _rows("x", x, ad.k)
+    dev, code = _dev("x", x), _real("y", y)
+    shape = (R, ad.n)
+    _check(lib().moe_adapter_rows(
+        R, *_adapter_args(ad, dev, R, offsets, sorted_slot, slot_row),
+        _arg(dev, "x", x, _BF16, (R, ad.k)), _arg(dev, "base", base, (y.dtype,), shape),
+        _arg(dev, "y", y, (y.dtype,), shape), code, _arg(dev, "ws", ws, (ws.dtype,), ws.shape),
+        ws.numel() * ws.element_size(), _stream_on(dev, stream)))
+
+
+def adapter_backward(ad, offsets, sorted_slot, slot_row, x, dy, dx_base, dx, da, db, ws,
+                     accumulate=False, stream=None):
+    """adapter_rows' gradients: dx = dx_base + .., and da, db fp32 (added to what
+    they hold with accumulate).  dx, or da and db, may be None; ws of
+    adapter_backward_bytes bytes."""
+    R, _ = _rows("dy", dy, ad.n)
+    dev = _dev("dy", dy)
+    wide = (dx.dtype,) if dx is not None else _F32
+    _check(lib().moe_adapter_backward(
+        R, *_adapter_args(ad, dev, R, offsets, sorted_slot, slot_row),
+        _arg(dev, "x", x, _BF16, (R, ad.k)), _arg(dev, "dy", dy, _BF16, (R, ad.n)),
+        _arg(dev, "dx_base", dx_base, wide, (R, ad.k)), _arg(dev, "dx", dx, wide, (R, ad.k)),
+        _real("dx", dx) if dx is not None else FP32,
+        _arg(dev, "da", da, _F32, (ad.count, ad.rank, ad.k)),
+        _arg(dev, "db", db, _F32, (ad.count, ad.n, ad.rank)), int(accumulate),
+        _arg(dev, "ws", ws, (ws.dtype,), ws.shape), ws.numel() * ws.element_size(),
+        _stream_on(dev, stream)))
 
 
 class MoEBuffers:
