@@ -9,34 +9,47 @@ constexpr int kMaxRank = 256;
 constexpr int kRankAlign = 8;  // a 16-byte load of an adapter row
 
 // The rows of a launch, ordered by adapter (moe_permute's outputs): places
-// [offsets[e], offsets[e + 1]) belong to adapter e, place p is row order[p].
+// [offsets[e], offsets[e + 1]) belong to adapter e, place p is row order[p];
+// place[row] < 0 for a row of no adapter.
 struct AdapterRows {
-    const int32_t *offsets, *order;
+    const int32_t *offsets, *order, *place;
     int64_t rows;
     int count;
 };
 
-// p[split][place][rank] = partial sums over K of w[e] x_row (w [count][rank][K]):
-// split s of `splits` takes its share of K.
-hipError_t launch_adapter_shrink(const AdapterRows &o, int rank, int K, const bf16_t *x,
-                                 const bf16_t *w, float *p, int splits, hipStream_t s);
-// y[row] = base[row] + scale[e] * w[e] (sum over splits of p[.][place]) (w [count][N][rank]);
-// rows of no adapter (place[row] < 0) get base's row, unless base is y.
-hipError_t launch_adapter_expand(const AdapterRows &o, int rank, int N, const float *p, int splits,
-                                 const bf16_t *w, const float *scale, const int32_t *place,
-                                 const void *base, void *y, int y_type, hipStream_t s);
-// out[e] (+)= scale[e] * sum over the adapter's rows of p[place]^T q_row: out
-// [count][rank][C], or transposed [count][C][rank].  parts: adapter_outer_slots()
-// buffers of rank * C floats.
-hipError_t launch_adapter_outer(const AdapterRows &o, int rank, int C, const float *p, int splits,
-                                const bf16_t *q, const float *scale, float *parts, bool transposed,
-                                bool accumulate, float *out, hipStream_t s);
-// wt[e] = w[e]^T for the adapters that have rows; w [count][m][n].
-hipError_t launch_adapter_transpose(const AdapterRows &o, int m, int n, const bf16_t *w,
-                                    bf16_t *wt, hipStream_t s);
+// Sums over K of rows times a low-rank matrix, in fp32: [tile][split][rank][rows of
+// a tile], tiles as the device numbers them, a split a share of K.
+struct AdapterSums {
+    float *p;
+    int splits;
+};
+// Shares of K that the sums of these rows are cut into, and their bytes (no fewer
+// than any fewer rows need).
+int adapter_splits(int64_t rows, int count, int K, int rank);
+size_t adapter_sums_bytes(int64_t rows, int count, int rank);
 
-// Shares of K that a shrink of these rows is cut into.
-int adapter_splits(int64_t rows, int count, int K);
-int64_t adapter_outer_slots(int64_t rows);
+// Bytes of the buffer of the outer products' parts over C columns (likewise).
+size_t adapter_parts_bytes(int64_t rows, int rank, int C);
+
+// The forward pass: y[row] = base[row] + scale[e] * b[e] (a[e] x_row).
+hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, const bf16_t *x,
+                               const void *base, void *y, int y_type, const AdapterSums &u,
+                               hipStream_t s);
+
+// Its gradient; dx, or da and db, may be NULL.  at, bt: room for the transposed
+// matrices; pa, pb: the parts of da and db.
+struct AdapterBack {
+    const bf16_t *x, *dy;
+    const void *base;
+    void *dx;
+    int dx_type;
+    float *da, *db;
+    bool accumulate;
+    AdapterSums u, v;
+    bf16_t *at, *bt;
+    float *pa, *pb;
+};
+hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
+                                   const AdapterBack &k, hipStream_t s);
 
 }  // namespace moe

@@ -49,13 +49,12 @@ moe_status check_rows(const char *fn, const int32_t *offsets, const int32_t *sor
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
 
-// A shrink's sums: no more than `rows` or fewer rows need.
-size_t sums_bytes(int64_t rows, int32_t rank) {
-    return up((size_t)std::max(rows, std::min<int64_t>(16 * rows, 65536)) * rank * sizeof(float));
+size_t sums_bytes(int64_t rows, const moe_adapters *ad) {
+    return up(adapter_sums_bytes(rows, ad->count, ad->rank));
 }
 
 struct BackWs {
-    size_t u, v, at, bt, parts, total;
+    size_t u, v, at, bt, pa, pb, total;
 };
 BackWs back_ws(int64_t rows, const moe_adapters *ad) {
     BackWs w;
@@ -65,12 +64,13 @@ BackWs back_ws(int64_t rows, const moe_adapters *ad) {
         o += up(bytes);
         return at;
     };
-    const size_t r = ad->rank, c = ad->count;
-    w.u = take(sums_bytes(rows, ad->rank));
-    w.v = take(sums_bytes(rows, ad->rank));
-    w.at = take(c * r * ad->k * sizeof(bf16_t));
-    w.bt = take(c * r * ad->n * sizeof(bf16_t));
-    w.parts = take((size_t)adapter_outer_slots(rows) * r * std::max(ad->n, ad->k) * sizeof(float));
+    const size_t weights = (size_t)ad->count * ad->rank * sizeof(bf16_t);
+    w.u = take(sums_bytes(rows, ad));
+    w.v = take(sums_bytes(rows, ad));
+    w.at = take(weights * ad->k);
+    w.bt = take(weights * ad->n);
+    w.pa = take(adapter_parts_bytes(rows, ad->rank, ad->k));
+    w.pb = take(adapter_parts_bytes(rows, ad->rank, ad->n));
     w.total = o;
     return w;
 }
@@ -81,7 +81,7 @@ extern "C" {
 
 size_t moe_adapter_workspace_bytes(int64_t rows, const moe_adapters *adapters) {
     if (check_adapters("moe_adapter_workspace_bytes", rows, adapters) != MOE_OK) return 0;
-    return std::max<size_t>(sums_bytes(rows, adapters->rank), 256);
+    return std::max<size_t>(sums_bytes(rows, adapters), 256);
 }
 
 moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const int32_t *offsets,
@@ -100,16 +100,14 @@ moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const in
     MOE_TRY(check_at(fn, "y", y));
     if (base != y) MOE_TRY(check_at(fn, "slot_row", slot_row, 4));
     const moe_adapters &ad = *adapters;
-    const size_t need = sums_bytes(rows, ad.rank);
+    const size_t need = sums_bytes(rows, &ad);
     if (!ws || ws_bytes < need)
         return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, need);
     MOE_TRY(check_at(fn, "ws", ws));
-    hipStream_t s = (hipStream_t)stream;
-    const AdapterRows o{offsets, sorted_slot, rows, ad.count};
-    const int splits = adapter_splits(rows, ad.count, ad.k);
-    MOE_HIP(launch_adapter_shrink(o, ad.rank, ad.k, x, ad.a, (float *)ws, splits, s));
-    MOE_HIP(launch_adapter_expand(o, ad.rank, ad.n, (const float *)ws, splits, ad.b, ad.scale,
-                                  slot_row, base, y, y_type, s));
+    const AdapterRows o{offsets, sorted_slot, slot_row, rows, ad.count};
+    MOE_HIP(launch_adapter_rows(o, ad, x, base, y, y_type,
+                                {(float *)ws, adapter_splits(rows, ad.count, ad.k, ad.rank)},
+                                (hipStream_t)stream));
     return MOE_OK;
 }
 
@@ -139,15 +137,13 @@ moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
         MOE_TRY(check_at(fn, "db", db));
     }
     const moe_adapters &ad = *adapters;
-    hipStream_t s = (hipStream_t)stream;
-    const AdapterRows o{offsets, sorted_slot, rows, ad.count};
+    const AdapterRows o{offsets, sorted_slot, slot_row, rows, ad.count};
+    AdapterBack k{};
+    k.x = x, k.dy = dy;
+    k.base = dx_base, k.dx = dx, k.dx_type = dx_type;
+    k.da = da, k.db = db, k.accumulate = accumulate != 0;
     if (rows == 0) {  // gradients of nothing are zeros
-        if (da) {
-            MOE_HIP(launch_adapter_outer(o, ad.rank, ad.k, nullptr, 1, nullptr, nullptr, nullptr,
-                                         false, accumulate, da, s));
-            MOE_HIP(launch_adapter_outer(o, ad.rank, ad.n, nullptr, 1, nullptr, nullptr, nullptr,
-                                         true, accumulate, db, s));
-        }
+        MOE_HIP(launch_adapter_backward(o, ad, k, (hipStream_t)stream));
         return MOE_OK;
     }
     MOE_TRY(check_weights(fn, adapters));
@@ -164,26 +160,11 @@ moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
         return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, L.total);
     MOE_TRY(check_at(fn, "ws", ws));
     char *base = (char *)ws;
-    float *u = (float *)(base + L.u), *v = (float *)(base + L.v);
-    float *parts = (float *)(base + L.parts);
-    bf16_t *at = (bf16_t *)(base + L.at), *bt = (bf16_t *)(base + L.bt);
-    // v = dy B
-    const int vs = adapter_splits(rows, ad.count, ad.n);
-    MOE_HIP(launch_adapter_transpose(o, ad.n, ad.rank, ad.b, bt, s));
-    MOE_HIP(launch_adapter_shrink(o, ad.rank, ad.n, dy, bt, v, vs, s));
-    if (da) {
-        const int us = adapter_splits(rows, ad.count, ad.k);
-        MOE_HIP(launch_adapter_shrink(o, ad.rank, ad.k, x, ad.a, u, us, s));
-        MOE_HIP(launch_adapter_outer(o, ad.rank, ad.n, u, us, dy, ad.scale, parts, true,
-                                     accumulate, db, s));
-        MOE_HIP(launch_adapter_outer(o, ad.rank, ad.k, v, vs, x, ad.scale, parts, false,
-                                     accumulate, da, s));
-    }
-    if (dx) {
-        MOE_HIP(launch_adapter_transpose(o, ad.rank, ad.k, ad.a, at, s));
-        MOE_HIP(launch_adapter_expand(o, ad.rank, ad.k, v, vs, at, ad.scale, slot_row, dx_base, dx,
-                                      dx_type, s));
-    }
+    k.u = {(float *)(base + L.u), adapter_splits(rows, ad.count, ad.k, ad.rank)};
+    k.v = {(float *)(base + L.v), adapter_splits(rows, ad.count, ad.n, ad.rank)};
+    k.at = (bf16_t *)(base + L.at), k.bt = (bf16_t *)(base + L.bt);
+    k.pa = (float *)(base + L.pa), k.pb = (float *)(base + L.pb);
+    MOE_HIP(launch_adapter_backward(o, ad, k, (hipStream_t)stream));
     return MOE_OK;
 }
 

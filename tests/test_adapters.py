@@ -292,6 +292,12 @@ def test_bad_indices_are_passed_over():
     forward(p, got, BF16, y=got)
     da, db, dx = (torch.empty(s, device="cuda") for s in ((4, 16, 64), (4, 128, 16), (100, 64)))
     backward(p, None, dx, da, db)
+    zigzag = torch.tensor([0, 100, 0, 100, 0], dtype=torch.int32, device="cuda")
+    for o, order in ((wild, slot), (zigzag, slot), (off, worse)):
+        p.order = (o, order, row)
+        backward(p, None, dx, da, db)
+        forward(p, got, BF16, y=got)
+    torch.cuda.synchronize()
 
 
 @gpu
