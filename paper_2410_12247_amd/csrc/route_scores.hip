@@ -2,17 +2,29 @@
 // groups of experts, the k best and their weights; and its gradient.
 #include <cmath>
 
+#include "dispatch.h"
 #include "route_common.h"
 
 namespace moe {
 namespace {
 
-constexpr int kTokens = 4;  // of a workgroup: one a wave
+constexpr int kWaves = 4;  // of a workgroup
 
 __device__ __forceinline__ float logit_at(const float *z, int64_t i) { return z[i]; }
 __device__ __forceinline__ float logit_at(const bf16_t *z, int64_t i) {
     return __uint_as_float((uint32_t)z[i] << 16);
 }
+
+struct Rules {
+    int64_t T;
+    int E, k, sigmoid, renorm, G, top_groups, pair;
+    float scale;
+    int per;          // experts of a lane (16 lanes a token)
+    uint32_t div_E;   // i / E = i * div_E >> 20 for i < 4 E
+    uint32_t div_per; // i / per = i * div_per >> 16 for i < E
+};
+
+// ---- one token by one wave, choices in 64 bits -------------------------------
 
 // Order-preserving bits of a choice; 0 (below every number's) for one that
 // cannot be chosen: -inf or NaN.
@@ -27,59 +39,73 @@ __device__ __forceinline__ uint64_t logit_choice_key(float z) {
     return z > -INFINITY ? (logit_key(z, 0) >> 32) << 32 : 0;
 }
 
-// fp64 exp of the argument, 0 for -inf.
-__device__ __forceinline__ double exp64(double v) { return exp(v); }
+__device__ __forceinline__ uint32_t ord32(float v) { return (uint32_t)(logit_key(v, 0) >> 32); }
+__device__ __forceinline__ float from_ord32(uint32_t k) { return key_logit((uint64_t)k << 32); }
 
-// The weights of a token's chosen experts, by lanes 0 .. k - 1 (e < 0: no
-// expert); z_at the lane's chosen logit, zmax and sum the softmax's over all.
+// Sums and maxima over the lanes of a token: its 16-lane row, or the wave.
+template <bool ROW>
+__device__ __forceinline__ double sum_f64(double v) {
+    if constexpr (!ROW) return wave_sum_f64(v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = v + dpp_f64(v, i);
+    return v;
+}
+template <bool ROW>
+__device__ __forceinline__ uint32_t max_u32(uint32_t v) {
+    if constexpr (!ROW) return wave_max_u32(v);
+    v = max(v, dpp32<0xB1>(v));
+    v = max(v, dpp32<0x4E>(v));
+    v = max(v, dpp32<0x141>(v));
+    return max(v, dpp32<0x140>(v));
+}
+
+// The weight of a lane's chosen expert of logit z_at, before the factor, among the
+// lanes of its token (0 where there is none); zmax and sum the softmax's over all.
+template <bool ROW>
 __device__ __forceinline__ double chosen_weight(bool sigmoid, bool renorm, bool there, float z_at,
                                                 float zmax, double sum) {
     if (!renorm) {
         if (!there) return 0.0;
-        return sigmoid ? 1.0 / (1.0 + exp64(-(double)z_at)) : exp64((double)z_at - zmax) / sum;
+        return sigmoid ? 1.0 / (1.0 + exp(-(double)z_at)) : exp((double)z_at - zmax) / sum;
     }
     // relative to the largest, so that no sum is 0
     const float v = sigmoid ? fminf(z_at, 0.f) : z_at;
-    const uint32_t key = there ? (uint32_t)(logit_key(v, 0) >> 32) : 0u;
-    const uint32_t top = wave_max_u32(key);
-    const float m = key_logit((uint64_t)top << 32);
+    const float m = from_ord32(max_u32<ROW>(there ? ord32(v) : 0u));
     double s = 0.0;
     if (there) {
-        s = exp64((double)v - m);
-        if (sigmoid) s /= 1.0 + exp64(-fabs((double)z_at));
+        s = exp((double)v - m);
+        if (sigmoid) s /= 1.0 + exp(-fabs((double)z_at));
     }
-    const double S = wave_sum_f64(s);
+    const double S = sum_f64<ROW>(s);
     return there ? s / S : 0.0;
 }
 
-// One wave a token; lane l has experts l, l + 64, l + 128, l + 192.
+// Token t, lane l with experts l, l + 64, l + 128, l + 192; cs, gs: room for E and G
+// doubles in LDS, this wave's.
 template <class Z>
-__global__ __launch_bounds__(64 * kTokens) void scores_kernel(
-    const Z *__restrict__ z, const float *__restrict__ bias, int64_t T, int E, int k, int sigmoid,
-    int renorm, int G, int top_groups, int pair, float scale, int32_t *__restrict__ ids,
-    float *__restrict__ w) {
-    __shared__ double cs[kTokens][kMaxExperts], gs[kTokens][kMaxExperts];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t = (int64_t)blockIdx.x * kTokens + wave;
-    const bool live = t < T;
+__device__ __forceinline__ void exact_token(const Rules &r, int64_t t, const Z *__restrict__ z,
+                                            const float *__restrict__ bias,
+                                            int32_t *__restrict__ ids, float *__restrict__ w,
+                                            double *cs, double *gs) {
+    const int lane = threadIdx.x & 63, E = r.E, G = r.G;
     float zl[4];
     uint32_t top = 0;
     bool bad = false;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int e = lane + 64 * q;
-        zl[q] = live && e < E ? logit_at(z, t * E + e) : -INFINITY;
-        bad |= zl[q] != zl[q] || (!sigmoid && zl[q] == INFINITY);
-        top = max(top, (uint32_t)(logit_key(zl[q], 0) >> 32));
+        zl[q] = e < E ? logit_at(z, t * E + e) : -INFINITY;
+        bad |= zl[q] != zl[q] || (!r.sigmoid && zl[q] == INFINITY);
+        top = max(top, ord32(zl[q]));
     }
     const bool broken = __ballot(bad) != 0;
-    const float zmax = key_logit((uint64_t)wave_max_u32(top) << 32);
+    const float zmax = from_ord32(wave_max_u32(top));
     double s[4], sum = 0.0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         s[q] = zl[q] == -INFINITY ? 0.0
-               : sigmoid          ? 1.0 / (1.0 + exp64(-(double)zl[q]))
-                                  : exp64((double)zl[q] - zmax);
+               : r.sigmoid        ? 1.0 / (1.0 + exp(-(double)zl[q]))
+                                  : exp((double)zl[q] - zmax);
         sum += s[q];
     }
     sum = wave_sum_f64(sum);
@@ -87,10 +113,10 @@ __global__ __launch_bounds__(64 * kTokens) void scores_kernel(
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int e = lane + 64 * q;
-        double c = sigmoid ? s[q] : s[q] / sum;
+        double c = r.sigmoid ? s[q] : s[q] / sum;
         if (bias && e < E) c += (double)bias[e];
         if (zl[q] == -INFINITY || c != c) c = -INFINITY;
-        if (e < E) cs[wave][e] = c;
+        if (e < E) cs[e] = c;
         // a token with a NaN: by the logits, a NaN as the largest
         key[q] = broken ? logit_choice_key(zl[q] != zl[q] ? INFINITY : zl[q])
                  : bias ? choice_key(c)
@@ -98,38 +124,39 @@ __global__ __launch_bounds__(64 * kTokens) void scores_kernel(
     }
     if (G > 1) {
         const int size = E / G;
-        __syncthreads();
+        wave_sync();
         for (int g = lane; g < G; g += 64) {
             double a = -INFINITY, b = -INFINITY;
             for (int i = 0; i < size; ++i) {
-                const double c = cs[wave][g * size + i];
+                const double c = cs[g * size + i];
                 if (c > a) b = a, a = c;
                 else if (c > b) b = c;
             }
-            gs[wave][g] = pair && b > -INFINITY ? a + b : a;
+            gs[g] = r.pair && b > -INFINITY ? a + b : a;
         }
-        __syncthreads();
+        wave_sync();
         if (!broken) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int e = lane + 64 * q;
                 if (e >= E) continue;
                 const int g = e / size;
-                const double v = gs[wave][g];
+                const double v = gs[g];
                 int better = 0;
                 for (int i = 0; i < G; ++i) {
-                    const double o = gs[wave][i];
+                    const double o = gs[i];
                     better += o > v || (o == v && i < g);
                 }
-                if (better >= top_groups) key[q] = 0;
+                if (better >= r.top_groups) key[q] = 0;
             }
         }
+        wave_sync();
     }
     float my_z = 0.f;
     int my_e = -1;
-    for (int j = 0; j < k; ++j) {
-        const uint64_t best = wave_max_u64(
-            max_u64(max_u64(key[0], key[1]), max_u64(key[2], key[3])));
+    for (int j = 0; j < r.k; ++j) {
+        const uint64_t best =
+            wave_max_u64(max_u64(max_u64(key[0], key[1]), max_u64(key[2], key[3])));
         if (best == 0) break;
         int e = -1;
 #pragma unroll
@@ -146,86 +173,568 @@ __global__ __launch_bounds__(64 * kTokens) void scores_kernel(
         }
         if (lane == j) my_e = e;
     }
-    double v = chosen_weight(sigmoid, renorm, my_e >= 0, my_z, zmax, sum) * scale;
+    double v = chosen_weight<false>(r.sigmoid, r.renorm, my_e >= 0, my_z, zmax, sum) * r.scale;
     if (broken) v = NAN;
-    if (live && lane < k) {
-        ids[t * k + lane] = my_e;
-        w[t * k + lane] = (float)v;
+    if (lane < r.k) {
+        ids[t * r.k + lane] = my_e;
+        w[t * r.k + lane] = (float)v;
     }
 }
 
-__device__ __forceinline__ void store_logit(float *z, int64_t i, float v) { z[i] = v; }
-__device__ __forceinline__ void store_logit(bf16_t *z, int64_t i, float v) {
-    z[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
+template <class Z>
+__global__ __launch_bounds__(64 * kWaves) void exact_kernel(Rules r, const Z *__restrict__ z,
+                                                            const float *__restrict__ bias,
+                                                            int32_t *__restrict__ ids,
+                                                            float *__restrict__ w) {
+    __shared__ double cs[kWaves][kMaxExperts], gs[kWaves][kMaxExperts];
+    const int wave = threadIdx.x >> 6;
+    const int64_t t = (int64_t)blockIdx.x * kWaves + wave;
+    if (t < r.T) exact_token(r, t, z, bias, ids, w, cs[wave], gs[wave]);
 }
 
-// dz of a token, by one wave.  Lane j < k works out the chosen expert j's part:
+// ---- four tokens by one wave -------------------------------------------------
+// A token has 16 lanes, a lane `per` experts next to each other (at most NV).  The
+// rows come in as whole cache lines and change places through LDS, where a lane's
+// experts are a chunk of NV + 4 floats (16-byte reads of different banks).
+
+constexpr int kQuad = 4;
+
+template <int NV>
+struct alignas(16) Quad {
+    static constexpr int PITCH = NV + 4;
+    float v[64 * PITCH];
+};
+
+// The place in LDS of element i of the quad's 4 E.
+template <int NV>
+__device__ __forceinline__ int quad_at(const Rules &r, uint32_t i) {
+    const uint32_t t = i * r.div_E >> 20, e = i - t * r.E, c = e * r.div_per >> 16;
+    return (t * 16 + c) * Quad<NV>::PITCH + (e - c * r.per);
+}
+
+__device__ __forceinline__ void load4(const float *p, float (&v)[4]) {
+    const floatx4 u = *reinterpret_cast<const floatx4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = u[i];
+}
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void load4(const bf16_t *p, float (&v)[4]) {
+    const u32x2 u = *reinterpret_cast<const u32x2 *>(p);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ uint32_t bits16(float v) {
+    return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+__device__ __forceinline__ void store4(float *p, const float (&v)[4]) {
+    *reinterpret_cast<floatx4 *>(p) = floatx4{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store4(bf16_t *p, const float (&v)[4]) {
+    *reinterpret_cast<u32x2 *>(p) =
+        u32x2{bits16(v[0]) | bits16(v[1]) << 16, bits16(v[2]) | bits16(v[3]) << 16};
+}
+__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store1(bf16_t *p, float v) { *p = (uint16_t)bits16(v); }
+
+// The quad's n logits (from src, four at a time where ALIGNED) to LDS.
+template <int NV, class Z, bool ALIGNED>
+__device__ __forceinline__ void quad_in(const Rules &r, const Z *__restrict__ src, int n,
+                                        Quad<NV> &q) {
+    const int lane = threadIdx.x & 63;
+    float v[NV / 4 + (NV < 4 ? 1 : 0) + (NV % 4 != 0 && NV > 4 ? 1 : 0)][4];
+    constexpr int IT = sizeof(v) / sizeof(v[0]);
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+        const int i = 4 * (lane + 64 * it);
+        if (ALIGNED && i + 4 <= n) {
+            load4(src + i, v[it]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[it][j] = i + j < n ? logit_at(src, i + j) : 0.f;
+        }
+    }
+    if (r.per % 4 == 0 && r.E % 4 == 0) {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const int i = 4 * (lane + 64 * it);
+            if (i < n)
+                *reinterpret_cast<floatx4 *>(&q.v[quad_at<NV>(r, i)]) =
+                    floatx4{v[it][0], v[it][1], v[it][2], v[it][3]};
+        }
+    } else {
+#pragma unroll
+        for (int it = 0; it < IT; ++it)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = 4 * (lane + 64 * it) + j;
+                if (i < n) q.v[quad_at<NV>(r, i)] = v[it][j];
+            }
+    }
+}
+
+// A lane's chunk; experts it does not have get `fill`.
+template <int NV>
+__device__ __forceinline__ void quad_get(const Rules &r, const Quad<NV> &q, int n, float fill,
+                                         float (&v)[NV]) {
+    const int lane = threadIdx.x & 63, l = lane & 15;
+    const float *p = q.v + lane * Quad<NV>::PITCH;
+    const int mine = min(r.per, (n > (lane >> 4) * r.E ? r.E : 0) - l * r.per);
+    if constexpr (NV % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < NV; i += 4) {
+            const floatx4 u = *reinterpret_cast<const floatx4 *>(p + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i + j] = u[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = i < mine ? v[i] : fill;
+}
+
+__device__ __forceinline__ float dpp_f32(float v, int which) {
+    const uint32_t b = __float_as_uint(v);
+    switch (which) {
+        case 0: return __uint_as_float(dpp32<0xB1>(b));
+        case 1: return __uint_as_float(dpp32<0x4E>(b));
+        case 2: return __uint_as_float(dpp32<0x141>(b));
+        default: return __uint_as_float(dpp32<0x140>(b));
+    }
+}
+__device__ __forceinline__ float row_max(float v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = fmaxf(v, dpp_f32(v, i));
+    return v;
+}
+__device__ __forceinline__ float row_min(float v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = fminf(v, dpp_f32(v, i));
+    return v;
+}
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = v + dpp_f32(v, i);
+    return v;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// exp of d <= 0 to some 2^-37: 2^n times a Taylor sum to the ninth power over
+// |x| <= ln 2 / 2 (the next term is below 2^-37).
+__device__ __forceinline__ double exp_near(double d) {
+    d = fmax(d, -1000.0);
+    const double n = __builtin_rint(d * 1.4426950408889634);
+    const double x = fma(n, -0.6931471805599453, d);
+    double s = 1.0 / 362880;
+    s = fma(s, x, 1.0 / 40320);
+    s = fma(s, x, 1.0 / 5040);
+    s = fma(s, x, 1.0 / 720);
+    s = fma(s, x, 1.0 / 120);
+    s = fma(s, x, 1.0 / 24);
+    s = fma(s, x, 1.0 / 6);
+    s = fma(s, x, 0.5);
+    s = fma(s, x, 1.0);
+    s = fma(s, x, 1.0);
+    return __builtin_amdgcn_ldexp(s, (int)n);
+}
+
+// Keys: 24 bits of the choice above 255 - expert, so that all differ and ties go to
+// the lowest expert; 0 for an expert that cannot be chosen.
+__device__ __forceinline__ void order(uint32_t &a, uint32_t &b) {
+    const uint32_t hi = max(a, b), lo = min(a, b);
+    a = hi;
+    b = lo;
+}
+__device__ __forceinline__ void sort8(uint32_t (&a)[8]) {  // odd-even merge sort, descending
+    order(a[0], a[1]), order(a[2], a[3]), order(a[4], a[5]), order(a[6], a[7]);
+    order(a[0], a[2]), order(a[1], a[3]), order(a[4], a[6]), order(a[5], a[7]);
+    order(a[1], a[2]), order(a[5], a[6]);
+    order(a[0], a[4]), order(a[1], a[5]), order(a[2], a[6]), order(a[3], a[7]);
+    order(a[2], a[4]), order(a[3], a[5]);
+    order(a[1], a[2]), order(a[3], a[4]), order(a[5], a[6]);
+}
+// a: the eight largest of both sorted lists, sorted; ninth: the largest left out.
+__device__ __forceinline__ void merge8(uint32_t (&a)[8], const uint32_t (&b)[8], uint32_t &ninth) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t hi = max(a[i], b[7 - i]);
+        ninth = max(ninth, min(a[i], b[7 - i]));
+        a[i] = hi;
+    }
+#pragma unroll
+    for (int d = 4; d >= 1; d /= 2)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(i & d)) order(a[i], a[i + d]);
+}
+template <int CTRL>
+__device__ __forceinline__ void merge_lanes(uint32_t (&a)[8], uint32_t &ninth) {
+    uint32_t b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = dpp32<CTRL>(a[i]);
+    ninth = max(ninth, dpp32<CTRL>(ninth));
+    merge8(a, b, ninth);
+}
+
+// The eight largest of a row's keys, and the ninth.
+template <int NV>
+__device__ __forceinline__ void row_top8(const uint32_t (&key)[NV], uint32_t (&a)[8],
+                                         uint32_t &ninth) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = i < NV ? key[i < NV ? i : 0] : 0u;
+    ninth = 0;
+    sort8(a);
+    if constexpr (NV > 8) {
+        uint32_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = 8 + i < NV ? key[8 + i < NV ? 8 + i : 0] : 0u;
+        sort8(b);
+        merge8(a, b, ninth);
+    }
+    merge_lanes<0xB1>(a, ninth);
+    merge_lanes<0x4E>(a, ninth);
+    merge_lanes<0x141>(a, ninth);
+    merge_lanes<0x140>(a, ninth);
+}
+
+template <int CTRL>
+__device__ __forceinline__ int lanes_above(float v) {
+    return __uint_as_float(dpp32<CTRL>(__float_as_uint(v))) > v ? 1 : 0;
+}
+// Lanes of the row with a larger value.
+__device__ __forceinline__ int row_rank(float v) {
+    return lanes_above<0x121>(v) + lanes_above<0x122>(v) + lanes_above<0x123>(v) +
+           lanes_above<0x124>(v) + lanes_above<0x125>(v) + lanes_above<0x126>(v) +
+           lanes_above<0x127>(v) + lanes_above<0x128>(v) + lanes_above<0x129>(v) +
+           lanes_above<0x12A>(v) + lanes_above<0x12B>(v) + lanes_above<0x12C>(v) +
+           lanes_above<0x12D>(v) + lanes_above<0x12E>(v) + lanes_above<0x12F>(v);
+}
+
+// Lanes of the row where it is true.
+__device__ __forceinline__ int row_count(bool b) {
+    return __popc((uint32_t)(__ballot(b) >> (threadIdx.x & 48)) & 0xFFFFu);
+}
+
+// Choices in fp32 with their error's bound: a token whose choice could come out
+// otherwise in 64 bits (a gap below the bound, a NaN, values out of range) is done
+// again by exact_token.  Bounds, for |c| <= 4: sigmoid within 2^-22 (exponent, sum
+// and reciprocal together below 4 * 2^-24), softmax within 2^-19.4 (a sum of 16 terms
+// by 16 lanes: 20 roundings of 2^-24, and the terms' own), the bias' addition 2^-22,
+// the key's step 2^-23.
+// Groups are whole runs of lanes: G divides 16, and 16 the experts.
+template <int NV, class Z, bool ALIGNED>
+__global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *__restrict__ z,
+                                                             const float *__restrict__ bias,
+                                                             int32_t *__restrict__ ids,
+                                                             float *__restrict__ w) {
+    __shared__ Quad<NV> quads[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15;
+    const int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * kQuad;
+    if (t0 >= r.T) return;
+    Quad<NV> &q = quads[wave];
+    const int n = (int)min((int64_t)kQuad, r.T - t0) * r.E;
+    const int64_t t = t0 + (lane >> 4);
+    quad_in<NV, Z, ALIGNED>(r, z + t0 * r.E, n, q);
+    float b[NV];
+    if (bias) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            b[i] = i < r.per && l * r.per + i < r.E ? bias[l * r.per + i] : 0.f;
+    }
+    wave_sync();
+    float v[NV];  // logits, then what the choice is by
+    quad_get(r, q, n, -INFINITY, v);
+    bool bad = false;
+    float zmax = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        bad |= !(v[i] < INFINITY);
+        zmax = fmaxf(zmax, v[i]);
+    }
+    zmax = row_max(zmax);
+    bad |= !(zmax > -INFINITY);  // (a NaN beside -inf alone; no expert at all)
+    const bool groups = r.G > 1, raw = r.sigmoid || r.renorm;
+    double sum = 1.0;
+    // scores: where the choice or the groups are by them
+    if (bias || (groups && r.pair)) {
+        float s[NV];
+        if (r.sigmoid) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                s[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v[i]));
+        } else {
+            float total = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(kLog2e * (v[i] - zmax));
+                total += s[i];
+            }
+            const float f = __builtin_amdgcn_rcpf(row_sum(total));
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s[i] *= f;
+        }
+        if (!raw) {
+            sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) sum += exp_near((double)v[i] - zmax);
+            sum = sum_f64<true>(sum);
+        }
+        float cmax = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const float c = bias ? s[i] + b[i] : s[i];
+            s[i] = v[i] > -INFINITY && c > -INFINITY ? c : -INFINITY;
+            cmax = fmaxf(cmax, s[i] > -INFINITY ? fabsf(s[i]) : 0.f);
+        }
+        bad |= !(cmax <= 4.f);  // out of the bounds' range
+        if (groups) {
+            float x = -INFINITY, y = -INFINITY;  // the two largest
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                y = fmaxf(y, fminf(x, s[i]));
+                x = fmaxf(x, s[i]);
+            }
+            const int run = 16 / r.G;  // lanes of a group
+            if (run >= 2) {
+                const float x2 = dpp_f32(x, 0), y2 = dpp_f32(y, 0);
+                y = fmaxf(fminf(x, x2), fmaxf(y, y2)), x = fmaxf(x, x2);
+            }
+            if (run >= 4) {
+                const float x2 = dpp_f32(x, 1), y2 = dpp_f32(y, 1);
+                y = fmaxf(fminf(x, x2), fmaxf(y, y2)), x = fmaxf(x, x2);
+            }
+            if (run >= 8) {
+                const float x2 = dpp_f32(x, 2), y2 = dpp_f32(y, 2);
+                y = fmaxf(fminf(x, x2), fmaxf(y, y2)), x = fmaxf(x, x2);
+            }
+            if (r.pair && y > -INFINITY) x += y;
+            const bool keep = x > -INFINITY && row_rank(x) < r.top_groups * run;
+            const float in = row_min(keep ? x : INFINITY), out = row_max(keep ? -INFINITY : x);
+            // a value is within 2^-18 (two choices and their sum)
+            bad |= out > -INFINITY && !(in - out > 0x1p-17f);
+            bad |= row_count(keep) > r.top_groups * run;  // equal ones
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (bias) v[i] = s[i];
+                if (!keep) v[i] = -INFINITY;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = s[i];
+        }
+    } else {
+        if (!raw) {
+            sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) sum += exp_near((double)v[i] - zmax);
+            sum = sum_f64<true>(sum);
+        }
+        if (groups) {  // by the largest logit: exact
+            float x = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) x = fmaxf(x, v[i]);
+            const int run = 16 / r.G;
+            if (run >= 2) x = fmaxf(x, dpp_f32(x, 0));
+            if (run >= 4) x = fmaxf(x, dpp_f32(x, 1));
+            if (run >= 8) x = fmaxf(x, dpp_f32(x, 2));
+            const bool keep = x > -INFINITY && row_rank(x) < r.top_groups * run;
+            const float in = row_min(keep ? x : INFINITY), out = row_max(keep ? -INFINITY : x);
+            bad |= out > -INFINITY && !(in > out);
+            bad |= row_count(keep) > r.top_groups * run;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (!keep) v[i] = -INFINITY;
+        }
+    }
+    // keys: steps below the largest, of 2^-23 for choices; of 2^-19 for logits, whose
+    // differences are within 2^-19 up to 32; bf16 logits keep their own bits
+    const bool bits = !bias && sizeof(Z) == 2;
+    uint32_t key[NV];
+    if (bits) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            key[i] = v[i] > -INFINITY ? ord32(v[i]) >> 16 << 8 : 0u;
+    } else {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) top = fmaxf(top, v[i]);
+        top = row_max(top);
+        const float step = bias ? 0x1p23f : 0x1p19f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const float d = fminf((top - v[i]) * step, 16777214.f);
+            key[i] = v[i] > -INFINITY ? (16777215u - (uint32_t)d) << 8 : 0u;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (key[i]) key[i] |= 255u - (uint32_t)(l * r.per + i);
+    uint32_t a[8], ninth;
+    row_top8(key, a, ninth);
+    if (!bits) {
+        const uint32_t gap = bias ? (r.sigmoid ? 16u : 48u) : 4u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t next = i < 7 ? a[i < 7 ? i + 1 : 7] : ninth;
+            if (i < r.k) bad |= next && (a[i] >> 8) - (next >> 8) < gap;
+        }
+    }
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine = l == i ? a[i] : mine;
+    const bool there = l < r.k && mine != 0;
+    const uint32_t e = there ? 255u - (mine & 255u) : 0u;
+    const float z_at = q.v[quad_at<NV>(r, (lane >> 4) * r.E + e)];
+    const double weight =
+        chosen_weight<true>(r.sigmoid, r.renorm, there, z_at, zmax, sum) * r.scale;
+    const uint64_t redo = __ballot(bad && t < r.T);
+    if (t < r.T && l < r.k && !(redo >> (lane & 48) & 0xFFFF)) {
+        ids[t * r.k + l] = there ? (int32_t)e : -1;
+        w[t * r.k + l] = (float)weight;
+    }
+    if (!redo) return;
+    wave_sync();
+#pragma unroll 1
+    for (int i = 0; i < kQuad; ++i)
+        if (redo >> (16 * i) & 0xFFFF)
+            exact_token(r, t0 + i, z, bias, ids, w, reinterpret_cast<double *>(q.v),
+                        reinterpret_cast<double *>(q.v) + r.E);
+}
+
+// ---- gradient ---------------------------------------------------------------
+
+template <int I>
+__device__ __forceinline__ uint32_t row_lane(uint32_t v) {  // lane I of the row
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x150 + I, 0xF, 0xF, false);
+}
+// Sum of c over the row's first eight lanes with the same id.
+__device__ __forceinline__ float same_id_sum(int id, float c) {
+    float s = 0.f;
+    auto add = [&](uint32_t other, uint32_t value) {
+        s += (int)other == id ? __uint_as_float(value) : 0.f;
+    };
+    const uint32_t i = (uint32_t)id, v = __float_as_uint(c);
+    add(row_lane<0>(i), row_lane<0>(v));
+    add(row_lane<1>(i), row_lane<1>(v));
+    add(row_lane<2>(i), row_lane<2>(v));
+    add(row_lane<3>(i), row_lane<3>(v));
+    add(row_lane<4>(i), row_lane<4>(v));
+    add(row_lane<5>(i), row_lane<5>(v));
+    add(row_lane<6>(i), row_lane<6>(v));
+    add(row_lane<7>(i), row_lane<7>(v));
+    return s;
+}
+
+// dz of four tokens.  Lane j < k of a token works out the chosen expert j's part:
 //   softmax over all     dz_e = s_e (sum over j with id e of G_j - D), D = sum G_j s_j
 //   softmax, renormalised dz_j = p_j (G_j - sum G p)      p: softmax over the chosen
 //   sigmoid              dz_j = G_j s (1 - s)
 //   sigmoid, renormalised dz_j = q_j (1 - s_j) (G_j - sum G q)   q: s over their sum
-// with G = scale dw.
-template <class Z>
-__global__ __launch_bounds__(64 * kTokens) void scores_back_kernel(
-    const Z *__restrict__ z, const int32_t *__restrict__ ids, const float *__restrict__ dw,
-    int64_t T, int E, int k, int sigmoid, int renorm, float scale, Z *__restrict__ dz) {
-    const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * kTokens + (threadIdx.x >> 6);
-    if (t >= T) return;
-    const bool all = !sigmoid && !renorm;
-    float zl[4] = {};
-    double s[4] = {}, sum = 1.0;
-    float zmax = 0.f;
-    if (all) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int e = lane + 64 * q;
-            zl[q] = e < E ? logit_at(z, t * E + e) : -INFINITY;
-            top = max(top, (uint32_t)(logit_key(zl[q], 0) >> 32));
-        }
-        zmax = key_logit((uint64_t)wave_max_u32(top) << 32);
-        double part = 0.0;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            s[q] = zl[q] == -INFINITY ? 0.0 : exp64((double)zl[q] - zmax);
-            part += s[q];
-        }
-        sum = wave_sum_f64(part);
-        if (sum == 0.0) sum = 1.0;  // every expert switched off: all s are 0
-    }
-    int id = lane < k ? ids[t * k + lane] : -1;
-    if (id >= E) id = -1;
+// with G = scale dw, in 64 bits; the other experts' -s_e D in fp32.
+template <int NV, class Z, bool ALIGNED>
+__global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
+    Rules r, const Z *__restrict__ z, const int32_t *__restrict__ ids,
+    const float *__restrict__ dw, Z *__restrict__ dz) {
+    __shared__ Quad<NV> quads[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15;
+    const int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * kQuad;
+    if (t0 >= r.T) return;
+    Quad<NV> &q = quads[wave];
+    const int n = (int)min((int64_t)kQuad, r.T - t0) * r.E;
+    const int64_t t = t0 + (lane >> 4);
+    const bool slot = t < r.T && l < r.k;
+    int id = slot ? ids[t * r.k + l] : -1;
+    if (id >= r.E || id < 0) id = -1;
     const bool there = id >= 0;
-    const double G = there ? (double)dw[t * k + lane] * scale : 0.0;
-    const float zj = there ? logit_at(z, t * E + id) : 0.f;
-    double p = chosen_weight(sigmoid, renorm, there, zj, zmax, sum), c;
-    if (sigmoid) {
-        const double rest = 1.0 / (1.0 + exp64((double)zj));  // 1 - s
-        c = renorm ? p * rest * (G - wave_sum_f64(G * p)) : G * p * rest;
-    } else {
-        const double D = wave_sum_f64(G * p);
-        c = renorm ? p * (G - D) : G * p;
-        if (all) {
+    const double G = there ? (double)dw[t * r.k + l] * r.scale : 0.0;
+    const float zj = there ? logit_at(z, t * r.E + id) : 0.f;
+    const bool all = !r.sigmoid && !r.renorm;
+    float *mine = q.v + lane * Quad<NV>::PITCH;
+    float s[NV];
+    float zmax = 0.f;
+    double sum = 1.0;
+    if (all) {
+        quad_in<NV, Z, ALIGNED>(r, z + t0 * r.E, n, q);
+        wave_sync();
+        quad_get(r, q, n, -INFINITY, s);
+        zmax = -INFINITY;
+        bool nan = false;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s[q] = -(s[q] / sum) * D;
+        for (int i = 0; i < NV; ++i) {
+            zmax = fmaxf(zmax, s[i]);
+            nan |= s[i] != s[i];
+        }
+        zmax = row_max(zmax);
+        const uint64_t has = __ballot(nan);
+        if (has >> (lane & 48) & 0xFFFF) zmax = NAN;
+        if (zmax == -INFINITY) zmax = 0.f;  // every expert switched off: all s are 0
+        float total = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(kLog2e * (s[i] - zmax));
+            total += s[i];
+        }
+        total = row_sum(total);
+        sum = total > 0.f ? (double)total : total == 0.f ? 1.0 : (double)NAN;
+    }
+    const double p = chosen_weight<true>(r.sigmoid, r.renorm, there, zj, zmax, sum);
+    const double D = sum_f64<true>(G * p);
+    double c;
+    if (r.sigmoid) {
+        const double rest = 1.0 / (1.0 + exp((double)zj));  // 1 - s
+        c = r.renorm ? p * rest * (G - D) : G * p * rest;
+    } else {
+        c = r.renorm ? p * (G - D) : G * p;
+    }
+    const float add = same_id_sum(id, there ? (float)c : 0.f);
+    const float f = all ? (float)(-D / sum) : 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) s[i] = all ? s[i] * f : 0.f;
+    if constexpr (NV % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < NV; i += 4)
+            *reinterpret_cast<floatx4 *>(mine + i) = floatx4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) mine[i] = s[i];
+    }
+    wave_sync();
+    if (there) {  // (lanes of one id write the same value)
+        const int at = quad_at<NV>(r, (lane >> 4) * r.E + id);
+        const float was = q.v[at];
+        wave_sync();
+        q.v[at] = was + add;
+    }
+    wave_sync();
+    Z *dst = dz + t0 * r.E;
+    constexpr int IT = (NV + 3) / 4;
+    const bool whole = r.per % 4 == 0 && r.E % 4 == 0;
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+        const int i = 4 * (lane + 64 * it);
+        if (i >= n) continue;
+        float o[4];
+        if (whole) {
+            const floatx4 u = *reinterpret_cast<const floatx4 *>(&q.v[quad_at<NV>(r, i)]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = u[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = i + j < n ? q.v[quad_at<NV>(r, i + j)] : 0.f;
+        }
+        if (ALIGNED && i + 4 <= n) {
+            store4(dst + i, o);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i + j < n) store1(dst + i + j, o[j]);
         }
     }
-    if (!there) c = 0.0;
-    double v[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = all ? s[q] : 0.0;
-    for (int j = 0; j < k; ++j) {
-        const int e = __builtin_amdgcn_readlane(id, j);
-        const double cj =
-            __builtin_bit_cast(double, readlane64(__builtin_bit_cast(uint64_t, c), j));
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (e == lane + 64 * q) v[q] += cj;
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        if (lane + 64 * q < E) store_logit(dz, t * E + lane + 64 * q, (float)v[q]);
 }
 
 moe_status check_routing(const char *fn, const moe_dims *d, const moe_routing *r, int32_t type) {
@@ -256,7 +765,62 @@ moe_status check_at(const char *fn, const char *name, const void *p, uintptr_t a
     return MOE_OK;
 }
 
-unsigned blocks(int64_t tokens) { return (unsigned)((tokens + kTokens - 1) / kTokens); }
+Rules rules(const moe_dims &d, const moe_routing &r) {
+    Rules q{};
+    q.T = d.tokens;
+    q.E = d.experts, q.k = d.top_k;
+    q.sigmoid = r.score == MOE_SCORE_SIGMOID, q.renorm = d.renormalize;
+    q.G = r.groups, q.top_groups = r.top_groups, q.pair = r.group_score == MOE_GROUP_TOP_TWO;
+    q.scale = r.scale;
+    q.per = (q.E + 15) / 16;
+    q.div_E = ((1u << 20) + q.E - 1) / q.E;
+    q.div_per = ((1u << 16) + q.per - 1) / q.per;
+    return q;
+}
+
+// fn(the most experts of a lane, whether four elements load at once).
+template <class F>
+hipError_t by_size(const Rules &r, bool aligned, F fn) {
+    auto go = [&](auto nv) {
+        return aligned ? fn(nv, std::true_type()) : fn(nv, std::false_type());
+    };
+    if (r.per <= 1) return go(std::integral_constant<int, 1>());
+    if (r.per <= 4) return go(std::integral_constant<int, 4>());
+    if (r.per <= 8) return go(std::integral_constant<int, 8>());
+    if (r.per <= 10) return go(std::integral_constant<int, 10>());
+    return go(std::integral_constant<int, 16>());
+}
+
+template <class Z>
+bool aligned4(const Z *p) { return (uintptr_t)p % (4 * sizeof(Z)) == 0; }
+
+unsigned quad_blocks(const Rules &r) {
+    return (unsigned)((r.T + kWaves * kQuad - 1) / (kWaves * kQuad));
+}
+
+template <class Z>
+hipError_t launch_scores(const Rules &r, const Z *z, const float *bias, int32_t *ids, float *w,
+                         hipStream_t s) {
+    if (r.G > 1 && (16 % r.G || r.E % 16)) {  // groups that are no runs of lanes
+        exact_kernel<Z><<<(unsigned)((r.T + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(r, z, bias,
+                                                                                       ids, w);
+        return hipGetLastError();
+    }
+    return by_size(r, aligned4(z), [&](auto nv, auto al) {
+        scores_kernel<nv(), Z, al()><<<quad_blocks(r), 64 * kWaves, 0, s>>>(r, z, bias, ids, w);
+        return hipGetLastError();
+    });
+}
+
+template <class Z>
+hipError_t launch_back(const Rules &r, const Z *z, const int32_t *ids, const float *dw, Z *dz,
+                       hipStream_t s) {
+    return by_size(r, aligned4(z) && aligned4(dz), [&](auto nv, auto al) {
+        scores_back_kernel<nv(), Z, al()><<<quad_blocks(r), 64 * kWaves, 0, s>>>(r, z, ids, dw,
+                                                                                 dz);
+        return hipGetLastError();
+    });
+}
 
 }  // namespace
 }  // namespace moe
@@ -287,19 +851,11 @@ moe_status moe_route_scores(const moe_dims *dims, const moe_routing *routing, co
     if (bias) MOE_TRY(check_at(fn, "bias", bias, 4));
     MOE_TRY(check_at(fn, "topk_ids", topk_ids, 4));
     MOE_TRY(check_at(fn, "topk_w", topk_w, 4));
-    const moe_dims &d = *dims;
-    const moe_routing &r = *routing;
+    const Rules r = rules(*dims, *routing);
     hipStream_t s = (hipStream_t)stream;
-    const int sigmoid = r.score == MOE_SCORE_SIGMOID, pair = r.group_score == MOE_GROUP_TOP_TWO;
-    if (logits_type == MOE_FP32)
-        scores_kernel<float><<<blocks(d.tokens), 64 * kTokens, 0, s>>>(
-            (const float *)logits, bias, d.tokens, d.experts, d.top_k, sigmoid, d.renormalize,
-            r.groups, r.top_groups, pair, r.scale, topk_ids, topk_w);
-    else
-        scores_kernel<bf16_t><<<blocks(d.tokens), 64 * kTokens, 0, s>>>(
-            (const bf16_t *)logits, bias, d.tokens, d.experts, d.top_k, sigmoid, d.renormalize,
-            r.groups, r.top_groups, pair, r.scale, topk_ids, topk_w);
-    MOE_HIP(hipGetLastError());
+    MOE_HIP(logits_type == MOE_FP32
+                ? launch_scores(r, (const float *)logits, bias, topk_ids, topk_w, s)
+                : launch_scores(r, (const bf16_t *)logits, bias, topk_ids, topk_w, s));
     return MOE_OK;
 }
 
@@ -315,18 +871,12 @@ moe_status moe_route_scores_backward(const moe_dims *dims, const moe_routing *ro
     MOE_TRY(check_at(fn, "topk_ids", topk_ids, 4));
     MOE_TRY(check_at(fn, "dtopk_w", dtopk_w, 4));
     MOE_TRY(check_at(fn, "dlogits", dlogits, a));
-    const moe_dims &d = *dims;
+    const Rules r = rules(*dims, *routing);
     hipStream_t s = (hipStream_t)stream;
-    const int sigmoid = routing->score == MOE_SCORE_SIGMOID;
-    if (logits_type == MOE_FP32)
-        scores_back_kernel<float><<<blocks(d.tokens), 64 * kTokens, 0, s>>>(
-            (const float *)logits, topk_ids, dtopk_w, d.tokens, d.experts, d.top_k, sigmoid,
-            d.renormalize, routing->scale, (float *)dlogits);
-    else
-        scores_back_kernel<bf16_t><<<blocks(d.tokens), 64 * kTokens, 0, s>>>(
-            (const bf16_t *)logits, topk_ids, dtopk_w, d.tokens, d.experts, d.top_k, sigmoid,
-            d.renormalize, routing->scale, (bf16_t *)dlogits);
-    MOE_HIP(hipGetLastError());
+    MOE_HIP(logits_type == MOE_FP32 ? launch_back(r, (const float *)logits, topk_ids, dtopk_w,
+                                                  (float *)dlogits, s)
+                                    : launch_back(r, (const bf16_t *)logits, topk_ids, dtopk_w,
+                                                  (bf16_t *)dlogits, s));
     return MOE_OK;
 }
 
