@@ -64,20 +64,15 @@ __device__ __forceinline__ uint32_t max_u32(uint32_t v) {
 template <bool ROW>
 __device__ __forceinline__ double chosen_weight(bool sigmoid, bool renorm, bool there, float z_at,
                                                 float zmax, double sum) {
-    if (!renorm) {
-        if (!there) return 0.0;
-        return sigmoid ? 1.0 / (1.0 + exp(-(double)z_at)) : exp((double)z_at - zmax) / sum;
-    }
-    // relative to the largest, so that no sum is 0
-    const float v = sigmoid ? fminf(z_at, 0.f) : z_at;
-    const float m = from_ord32(max_u32<ROW>(there ? ord32(v) : 0u));
-    double s = 0.0;
-    if (there) {
-        s = exp((double)v - m);
-        if (sigmoid) s /= 1.0 + exp(-fabs((double)z_at));
-    }
-    const double S = sum_f64<ROW>(s);
-    return there ? s / S : 0.0;
+    // sigmoids far below 1 are exponentials: taken relative to the largest, so that
+    // their sum is not 0
+    const float top = renorm ? from_ord32(max_u32<ROW>(there ? ord32(z_at) : 0u)) : zmax;
+    const bool far = !sigmoid || (renorm && top < -80.f);
+    const double x = exp(far ? (double)z_at - top : -(double)z_at);
+    double s = there ? far ? x : 1.0 / (1.0 + x) : 0.0;
+    if (renorm) sum = sum_f64<ROW>(s);
+    if (renorm || !sigmoid) s = s / sum;
+    return there ? s : 0.0;
 }
 
 // Token t, lane l with experts l, l + 64, l + 128, l + 192; cs, gs: room for E and G
@@ -246,15 +241,15 @@ __device__ __forceinline__ void quad_in(const Rules &r, const Z *__restrict__ sr
     const int lane = threadIdx.x & 63;
     float v[NV / 4 + (NV < 4 ? 1 : 0) + (NV % 4 != 0 && NV > 4 ? 1 : 0)][4];
     constexpr int IT = sizeof(v) / sizeof(v[0]);
+    if (ALIGNED && n % 4 == 0) {  // (behind the end: the last ones again)
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-        const int i = 4 * (lane + 64 * it);
-        if (ALIGNED && i + 4 <= n) {
-            load4(src + i, v[it]);
-        } else {
+        for (int it = 0; it < IT; ++it) load4(src + min(4 * (lane + 64 * it), n - 4), v[it]);
+    } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[it][j] = i + j < n ? logit_at(src, i + j) : 0.f;
-        }
+        for (int it = 0; it < IT; ++it)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v[it][j] = logit_at(src, min(4 * (lane + 64 * it) + j, n - 1));
     }
     if (r.per % 4 == 0 && r.E % 4 == 0) {
 #pragma unroll
@@ -293,33 +288,9 @@ __device__ __forceinline__ void quad_get(const Rules &r, const Quad<NV> &q, int 
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = p[i];
     }
+    if (r.E == 16 * NV && n == kQuad * r.E) return;
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i] = i < mine ? v[i] : fill;
-}
-
-__device__ __forceinline__ float dpp_f32(float v, int which) {
-    const uint32_t b = __float_as_uint(v);
-    switch (which) {
-        case 0: return __uint_as_float(dpp32<0xB1>(b));
-        case 1: return __uint_as_float(dpp32<0x4E>(b));
-        case 2: return __uint_as_float(dpp32<0x141>(b));
-        default: return __uint_as_float(dpp32<0x140>(b));
-    }
-}
-__device__ __forceinline__ float row_max(float v) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v = fmaxf(v, dpp_f32(v, i));
-    return v;
-}
-__device__ __forceinline__ float row_min(float v) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v = fminf(v, dpp_f32(v, i));
-    return v;
-}
-__device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v = v + dpp_f32(v, i);
-    return v;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -343,14 +314,51 @@ __device__ __forceinline__ double exp_near(double d) {
     return __builtin_amdgcn_ldexp(s, (int)n);
 }
 
-// Keys: 24 bits of the choice above 255 - expert, so that all differ and ties go to
-// the lowest expert; 0 for an expert that cannot be chosen.
-__device__ __forceinline__ void order(uint32_t &a, uint32_t &b) {
-    const uint32_t hi = max(a, b), lo = min(a, b);
-    a = hi;
-    b = lo;
+// Keys: 24 bits that fall with the choice above the expert, so that all differ, the
+// smallest is the best and ties go to the lowest expert.  kNone and above: an expert
+// that cannot be chosen.
+constexpr uint32_t kNone = 0xFFFFFF00u;
+
+// Another lane's value (no lane is off).
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane32(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
 }
-__device__ __forceinline__ void sort8(uint32_t (&a)[8]) {  // odd-even merge sort, descending
+template <int CTRL>
+__device__ __forceinline__ float lane_f32(float v) {
+    return __uint_as_float(lane32<CTRL>(__float_as_uint(v)));
+}
+
+__device__ __forceinline__ float dpp_f32(float v, int which) {
+    switch (which) {
+        case 0: return lane_f32<0xB1>(v);
+        case 1: return lane_f32<0x4E>(v);
+        case 2: return lane_f32<0x141>(v);
+        default: return lane_f32<0x140>(v);
+    }
+}
+__device__ __forceinline__ float row_max(float v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = fmaxf(v, dpp_f32(v, i));
+    return v;
+}
+__device__ __forceinline__ float row_min(float v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = fminf(v, dpp_f32(v, i));
+    return v;
+}
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = v + dpp_f32(v, i);
+    return v;
+}
+
+__device__ __forceinline__ void order(uint32_t &a, uint32_t &b) {
+    const uint32_t lo = min(a, b), hi = max(a, b);
+    a = lo;
+    b = hi;
+}
+__device__ __forceinline__ void sort8(uint32_t (&a)[8]) {  // odd-even merge sort
     order(a[0], a[1]), order(a[2], a[3]), order(a[4], a[5]), order(a[6], a[7]);
     order(a[0], a[2]), order(a[1], a[3]), order(a[4], a[6]), order(a[5], a[7]);
     order(a[1], a[2]), order(a[5], a[6]);
@@ -358,13 +366,12 @@ __device__ __forceinline__ void sort8(uint32_t (&a)[8]) {  // odd-even merge sor
     order(a[2], a[4]), order(a[3], a[5]);
     order(a[1], a[2]), order(a[3], a[4]), order(a[5], a[6]);
 }
-// a: the eight largest of both sorted lists, sorted; ninth: the largest left out.
+// a: the eight smallest of both sorted lists, sorted; ninth: the smallest left out.
 __device__ __forceinline__ void merge8(uint32_t (&a)[8], const uint32_t (&b)[8], uint32_t &ninth) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t hi = max(a[i], b[7 - i]);
-        ninth = max(ninth, min(a[i], b[7 - i]));
-        a[i] = hi;
+        ninth = min(ninth, max(a[i], b[7 - i]));
+        a[i] = min(a[i], b[7 - i]);
     }
 #pragma unroll
     for (int d = 4; d >= 1; d /= 2)
@@ -376,23 +383,23 @@ template <int CTRL>
 __device__ __forceinline__ void merge_lanes(uint32_t (&a)[8], uint32_t &ninth) {
     uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = dpp32<CTRL>(a[i]);
-    ninth = max(ninth, dpp32<CTRL>(ninth));
+    for (int i = 0; i < 8; ++i) b[i] = lane32<CTRL>(a[i]);
+    ninth = min(ninth, lane32<CTRL>(ninth));
     merge8(a, b, ninth);
 }
 
-// The eight largest of a row's keys, and the ninth.
+// The eight smallest of a row's keys, and the ninth.
 template <int NV>
-__device__ __forceinline__ void row_top8(const uint32_t (&key)[NV], uint32_t (&a)[8],
-                                         uint32_t &ninth) {
+__device__ __forceinline__ void row_best8(const uint32_t (&key)[NV], uint32_t (&a)[8],
+                                          uint32_t &ninth) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = i < NV ? key[i < NV ? i : 0] : 0u;
-    ninth = 0;
+    for (int i = 0; i < 8; ++i) a[i] = i < NV ? key[i < NV ? i : 0] : ~0u;
+    ninth = ~0u;
     sort8(a);
     if constexpr (NV > 8) {
         uint32_t b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = 8 + i < NV ? key[8 + i < NV ? 8 + i : 0] : 0u;
+        for (int i = 0; i < 8; ++i) b[i] = 8 + i < NV ? key[8 + i < NV ? 8 + i : 0] : ~0u;
         sort8(b);
         merge8(a, b, ninth);
     }
@@ -402,17 +409,19 @@ __device__ __forceinline__ void row_top8(const uint32_t (&key)[NV], uint32_t (&a
     merge_lanes<0x140>(a, ninth);
 }
 
-template <int CTRL>
-__device__ __forceinline__ int lanes_above(float v) {
-    return __uint_as_float(dpp32<CTRL>(__float_as_uint(v))) > v ? 1 : 0;
+template <int N>
+__device__ __forceinline__ int above(float v) {  // the lane N before has a larger value
+    return lane_f32<0x120 + N>(v) > v ? 1 : 0;
 }
-// Lanes of the row with a larger value.
-__device__ __forceinline__ int row_rank(float v) {
-    return lanes_above<0x121>(v) + lanes_above<0x122>(v) + lanes_above<0x123>(v) +
-           lanes_above<0x124>(v) + lanes_above<0x125>(v) + lanes_above<0x126>(v) +
-           lanes_above<0x127>(v) + lanes_above<0x128>(v) + lanes_above<0x129>(v) +
-           lanes_above<0x12A>(v) + lanes_above<0x12B>(v) + lanes_above<0x12C>(v) +
-           lanes_above<0x12D>(v) + lanes_above<0x12E>(v) + lanes_above<0x12F>(v);
+// Groups (runs of lanes that hold their value) of the row with a larger value.
+__device__ __forceinline__ int group_rank(float v, int run) {
+    int n = above<8>(v);
+    if (run <= 4) n += above<4>(v) + above<12>(v);
+    if (run <= 2) n += above<2>(v) + above<6>(v) + above<10>(v) + above<14>(v);
+    if (run <= 1)
+        n += above<1>(v) + above<3>(v) + above<5>(v) + above<7>(v) + above<9>(v) + above<11>(v) +
+             above<13>(v) + above<15>(v);
+    return n;
 }
 
 // Lanes of the row where it is true.
@@ -443,8 +452,7 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     float b[NV];
     if (bias) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            b[i] = i < r.per && l * r.per + i < r.E ? bias[l * r.per + i] : 0.f;
+        for (int i = 0; i < NV; ++i) b[i] = bias[min(l * r.per + i, r.E - 1)];
     }
     wave_sync();
     float v[NV];  // logits, then what the choice is by
@@ -513,7 +521,8 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
                 y = fmaxf(fminf(x, x2), fmaxf(y, y2)), x = fmaxf(x, x2);
             }
             if (r.pair && y > -INFINITY) x += y;
-            const bool keep = x > -INFINITY && row_rank(x) < r.top_groups * run;
+            const int rank = group_rank(x, run);  // (by every lane)
+            const bool keep = x > -INFINITY && rank < r.top_groups;
             const float in = row_min(keep ? x : INFINITY), out = row_max(keep ? -INFINITY : x);
             // a value is within 2^-18 (two choices and their sum)
             bad |= out > -INFINITY && !(in - out > 0x1p-17f);
@@ -542,7 +551,8 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
             if (run >= 2) x = fmaxf(x, dpp_f32(x, 0));
             if (run >= 4) x = fmaxf(x, dpp_f32(x, 1));
             if (run >= 8) x = fmaxf(x, dpp_f32(x, 2));
-            const bool keep = x > -INFINITY && row_rank(x) < r.top_groups * run;
+            const int rank = group_rank(x, run);  // (by every lane)
+            const bool keep = x > -INFINITY && rank < r.top_groups;
             const float in = row_min(keep ? x : INFINITY), out = row_max(keep ? -INFINITY : x);
             bad |= out > -INFINITY && !(in > out);
             bad |= row_count(keep) > r.top_groups * run;
@@ -557,38 +567,34 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     uint32_t key[NV];
     if (bits) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            key[i] = v[i] > -INFINITY ? ord32(v[i]) >> 16 << 8 : 0u;
+        for (int i = 0; i < NV; ++i) key[i] = 0xFFFFu - (ord32(v[i]) >> 16);
     } else {
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NV; ++i) top = fmaxf(top, v[i]);
-        top = row_max(top);
         const float step = bias ? 0x1p23f : 0x1p19f;
+        top = row_max(top) * step;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const float d = fminf((top - v[i]) * step, 16777214.f);
-            key[i] = v[i] > -INFINITY ? (16777215u - (uint32_t)d) << 8 : 0u;
-        }
+        for (int i = 0; i < NV; ++i)
+            key[i] = (uint32_t)fminf(fmaf(v[i], -step, top), 16777214.f);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (key[i]) key[i] |= 255u - (uint32_t)(l * r.per + i);
+        key[i] = v[i] > -INFINITY ? (key[i] << 8) + (uint32_t)(l * r.per + i) : ~0u;
     uint32_t a[8], ninth;
-    row_top8(key, a, ninth);
+    row_best8(key, a, ninth);
     if (!bits) {
-        const uint32_t gap = bias ? (r.sigmoid ? 16u : 48u) : 4u;
+        // (a list that ends before the k-th is done again too)
+        const uint32_t gap = (bias ? (r.sigmoid ? 17u : 49u) : 5u) << 8;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t next = i < 7 ? a[i < 7 ? i + 1 : 7] : ninth;
-            if (i < r.k) bad |= next && (a[i] >> 8) - (next >> 8) < gap;
-        }
+        for (int i = 0; i < 8; ++i)
+            bad |= (i < 7 ? a[i < 7 ? i + 1 : 7] : ninth) - a[i] < (i < r.k ? gap : 0u);
     }
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) mine = l == i ? a[i] : mine;
-    const bool there = l < r.k && mine != 0;
-    const uint32_t e = there ? 255u - (mine & 255u) : 0u;
+    const bool there = l < r.k && mine < kNone;
+    const uint32_t e = there ? mine & 255u : 0u;
     const float z_at = q.v[quad_at<NV>(r, (lane >> 4) * r.E + e)];
     const double weight =
         chosen_weight<true>(r.sigmoid, r.renorm, there, z_at, zmax, sum) * r.scale;
