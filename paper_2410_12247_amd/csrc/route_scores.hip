@@ -9,6 +9,8 @@ namespace moe {
 namespace {
 
 constexpr int kWaves = 4;  // of a workgroup
+// From so many tokens on eight lanes have one.
+constexpr int64_t kManyTokens = 16384;
 
 __device__ __forceinline__ float logit_at(const float *z, int64_t i) { return z[i]; }
 __device__ __forceinline__ float logit_at(const bf16_t *z, int64_t i) {
@@ -19,8 +21,8 @@ struct Rules {
     int64_t T;
     int E, k, sigmoid, renorm, G, top_groups, pair;
     float scale;
-    int per;          // experts of a lane (16 lanes a token)
-    uint32_t div_E;   // i / E = i * div_E >> 20 for i < 4 E
+    int per;          // experts of a lane
+    uint32_t div_E;   // i / E = i * div_E >> 20 for i < 8 E
     uint32_t div_per; // i / per = i * div_per >> 16 for i < E
 };
 
@@ -42,35 +44,35 @@ __device__ __forceinline__ uint64_t logit_choice_key(float z) {
 __device__ __forceinline__ uint32_t ord32(float v) { return (uint32_t)(logit_key(v, 0) >> 32); }
 __device__ __forceinline__ float from_ord32(uint32_t k) { return key_logit((uint64_t)k << 32); }
 
-// Sums and maxima over the lanes of a token: its 16-lane row, or the wave.
-template <bool ROW>
+// Sums and maxima over the LT lanes of a token: 8, 16 or the wave.
+template <int LT>
 __device__ __forceinline__ double sum_f64(double v) {
-    if constexpr (!ROW) return wave_sum_f64(v);
+    if constexpr (LT == 64) return wave_sum_f64(v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v = v + dpp_f64(v, i);
+    for (int i = 0; i < (LT == 8 ? 3 : 4); ++i) v = v + dpp_f64(v, i);
     return v;
 }
-template <bool ROW>
+template <int LT>
 __device__ __forceinline__ uint32_t max_u32(uint32_t v) {
-    if constexpr (!ROW) return wave_max_u32(v);
+    if constexpr (LT == 64) return wave_max_u32(v);
     v = max(v, dpp32<0xB1>(v));
     v = max(v, dpp32<0x4E>(v));
     v = max(v, dpp32<0x141>(v));
-    return max(v, dpp32<0x140>(v));
+    return LT == 8 ? v : max(v, dpp32<0x140>(v));
 }
 
 // The weight of a lane's chosen expert of logit z_at, before the factor, among the
 // lanes of its token (0 where there is none); zmax and sum the softmax's over all.
-template <bool ROW>
+template <int LT>
 __device__ __forceinline__ double chosen_weight(bool sigmoid, bool renorm, bool there, float z_at,
                                                 float zmax, double sum) {
     // sigmoids far below 1 are exponentials: taken relative to the largest, so that
     // their sum is not 0
-    const float top = renorm ? from_ord32(max_u32<ROW>(there ? ord32(z_at) : 0u)) : zmax;
+    const float top = renorm ? from_ord32(max_u32<LT>(there ? ord32(z_at) : 0u)) : zmax;
     const bool far = !sigmoid || (renorm && top < -80.f);
     const double x = exp(far ? (double)z_at - top : -(double)z_at);
     double s = there ? far ? x : 1.0 / (1.0 + x) : 0.0;
-    if (renorm) sum = sum_f64<ROW>(s);
+    if (renorm) sum = sum_f64<LT>(s);
     if (renorm || !sigmoid) s = s / sum;
     return there ? s : 0.0;
 }
@@ -168,7 +170,7 @@ __device__ __forceinline__ void exact_token(const Rules &r, int64_t t, const Z *
         }
         if (lane == j) my_e = e;
     }
-    double v = chosen_weight<false>(r.sigmoid, r.renorm, my_e >= 0, my_z, zmax, sum) * r.scale;
+    double v = chosen_weight<64>(r.sigmoid, r.renorm, my_e >= 0, my_z, zmax, sum) * r.scale;
     if (broken) v = NAN;
     if (lane < r.k) {
         ids[t * r.k + lane] = my_e;
@@ -187,25 +189,22 @@ __global__ __launch_bounds__(64 * kWaves) void exact_kernel(Rules r, const Z *__
     if (t < r.T) exact_token(r, t, z, bias, ids, w, cs[wave], gs[wave]);
 }
 
-// ---- four tokens by one wave -------------------------------------------------
-// A token has 16 lanes, a lane `per` experts next to each other (at most NV).  The
-// rows come in as whole cache lines and change places through LDS, where a lane's
-// experts are a chunk of NV + 4 floats (16-byte reads of different banks).
+// ---- several tokens by one wave ------------------------------------------------
+// A token has LT lanes (16, or 8 where there are many tokens: fewer steps across
+// lanes, twice the work of one), a lane `per` experts next to each other (at most
+// NV).  The rows come in as whole cache lines and change places through LDS, where a
+// lane's experts are a chunk of NV + 4 floats (16-byte reads of different banks).
 
-constexpr int kQuad = 4;
-
-template <int NV>
-struct alignas(16) Quad {
-    static constexpr int PITCH = NV + 4;
+template <int LT, int NV>
+struct alignas(16) Tokens {
+    static constexpr int N = 64 / LT, PITCH = NV + 4;
     float v[64 * PITCH];
+    // The place of element i of the tokens' N E.
+    static __device__ __forceinline__ int at(const Rules &r, uint32_t i) {
+        const uint32_t t = i * r.div_E >> 20, e = i - t * r.E, c = e * r.div_per >> 16;
+        return (t * LT + c) * PITCH + (e - c * r.per);
+    }
 };
-
-// The place in LDS of element i of the quad's 4 E.
-template <int NV>
-__device__ __forceinline__ int quad_at(const Rules &r, uint32_t i) {
-    const uint32_t t = i * r.div_E >> 20, e = i - t * r.E, c = e * r.div_per >> 16;
-    return (t * 16 + c) * Quad<NV>::PITCH + (e - c * r.per);
-}
 
 __device__ __forceinline__ void load4(const float *p, float (&v)[4]) {
     const floatx4 u = *reinterpret_cast<const floatx4 *>(p);
@@ -234,13 +233,14 @@ __device__ __forceinline__ void store4(bf16_t *p, const float (&v)[4]) {
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store1(bf16_t *p, float v) { *p = (uint16_t)bits16(v); }
 
-// The quad's n logits (from src, four at a time where ALIGNED) to LDS.
-template <int NV, class Z, bool ALIGNED>
-__device__ __forceinline__ void quad_in(const Rules &r, const Z *__restrict__ src, int n,
-                                        Quad<NV> &q) {
+// n logits (from src, four at a time where ALIGNED) to LDS.
+template <int LT, int NV, class Z, bool ALIGNED>
+__device__ __forceinline__ void tokens_in(const Rules &r, const Z *__restrict__ src, int n,
+                                          Tokens<LT, NV> &q) {
+    using Q = Tokens<LT, NV>;
+    constexpr int IT = (NV + 3) / 4;
     const int lane = threadIdx.x & 63;
-    float v[NV / 4 + (NV < 4 ? 1 : 0) + (NV % 4 != 0 && NV > 4 ? 1 : 0)][4];
-    constexpr int IT = sizeof(v) / sizeof(v[0]);
+    float v[IT][4];
     if (ALIGNED && n % 4 == 0) {  // (behind the end: the last ones again)
 #pragma unroll
         for (int it = 0; it < IT; ++it) load4(src + min(4 * (lane + 64 * it), n - 4), v[it]);
@@ -256,7 +256,7 @@ __device__ __forceinline__ void quad_in(const Rules &r, const Z *__restrict__ sr
         for (int it = 0; it < IT; ++it) {
             const int i = 4 * (lane + 64 * it);
             if (i < n)
-                *reinterpret_cast<floatx4 *>(&q.v[quad_at<NV>(r, i)]) =
+                *reinterpret_cast<floatx4 *>(&q.v[Q::at(r, i)]) =
                     floatx4{v[it][0], v[it][1], v[it][2], v[it][3]};
         }
     } else {
@@ -265,18 +265,17 @@ __device__ __forceinline__ void quad_in(const Rules &r, const Z *__restrict__ sr
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int i = 4 * (lane + 64 * it) + j;
-                if (i < n) q.v[quad_at<NV>(r, i)] = v[it][j];
+                if (i < n) q.v[Q::at(r, i)] = v[it][j];
             }
     }
 }
 
 // A lane's chunk; experts it does not have get `fill`.
-template <int NV>
-__device__ __forceinline__ void quad_get(const Rules &r, const Quad<NV> &q, int n, float fill,
-                                         float (&v)[NV]) {
-    const int lane = threadIdx.x & 63, l = lane & 15;
-    const float *p = q.v + lane * Quad<NV>::PITCH;
-    const int mine = min(r.per, (n > (lane >> 4) * r.E ? r.E : 0) - l * r.per);
+template <int LT, int NV>
+__device__ __forceinline__ void tokens_get(const Rules &r, const Tokens<LT, NV> &q, int n,
+                                           float fill, float (&v)[NV]) {
+    const int lane = threadIdx.x & 63;
+    const float *p = q.v + lane * Tokens<LT, NV>::PITCH;
     if constexpr (NV % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < NV; i += 4) {
@@ -288,7 +287,8 @@ __device__ __forceinline__ void quad_get(const Rules &r, const Quad<NV> &q, int 
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = p[i];
     }
-    if (r.E == 16 * NV && n == kQuad * r.E) return;
+    if (r.E == LT * NV && n == Tokens<LT, NV>::N * r.E) return;
+    const int mine = min(r.per, (n > lane / LT * r.E ? r.E : 0) - lane % LT * r.per);
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i] = i < mine ? v[i] : fill;
 }
@@ -337,20 +337,22 @@ __device__ __forceinline__ float dpp_f32(float v, int which) {
         default: return lane_f32<0x140>(v);
     }
 }
-__device__ __forceinline__ float row_max(float v) {
+template <int LT>
+__device__ __forceinline__ float max_f32(float v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v = fmaxf(v, dpp_f32(v, i));
+    for (int i = 0; i < (LT == 8 ? 3 : 4); ++i) v = fmaxf(v, dpp_f32(v, i));
     return v;
 }
-__device__ __forceinline__ float row_min(float v) {
+template <int LT>
+__device__ __forceinline__ float sum_f32(float v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v = fminf(v, dpp_f32(v, i));
+    for (int i = 0; i < (LT == 8 ? 3 : 4); ++i) v = v + dpp_f32(v, i);
     return v;
 }
-__device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v = v + dpp_f32(v, i);
-    return v;
+// Whether it is true on any lane of the token, and on how many.
+template <int LT>
+__device__ __forceinline__ uint32_t lanes_true(bool b) {
+    return (uint32_t)(__ballot(b) >> (threadIdx.x & (64 - LT))) & ((1u << LT) - 1);
 }
 
 __device__ __forceinline__ void order(uint32_t &a, uint32_t &b) {
@@ -388,67 +390,76 @@ __device__ __forceinline__ void merge_lanes(uint32_t (&a)[8], uint32_t &ninth) {
     merge8(a, b, ninth);
 }
 
-// The eight smallest of a row's keys, and the ninth.
+// A lane's eight smallest keys, sorted, and the ninth.
 template <int NV>
-__device__ __forceinline__ void row_best8(const uint32_t (&key)[NV], uint32_t (&a)[8],
-                                          uint32_t &ninth) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = i < NV ? key[i < NV ? i : 0] : ~0u;
+__device__ __forceinline__ void lane_best8(const uint32_t (&key)[NV], uint32_t (&a)[8],
+                                           uint32_t &ninth) {
     ninth = ~0u;
-    sort8(a);
-    if constexpr (NV > 8) {
+#pragma unroll
+    for (int o = 0; o < NV; o += 8) {
         uint32_t b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = 8 + i < NV ? key[8 + i < NV ? 8 + i : 0] : ~0u;
+        for (int i = 0; i < 8; ++i) b[i] = o + i < NV ? key[o + i < NV ? o + i : 0] : ~0u;
         sort8(b);
-        merge8(a, b, ninth);
+        if (o == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = b[i];
+        } else {
+            merge8(a, b, ninth);
+        }
     }
-    merge_lanes<0xB1>(a, ninth);
-    merge_lanes<0x4E>(a, ninth);
-    merge_lanes<0x141>(a, ninth);
-    merge_lanes<0x140>(a, ninth);
 }
 
-template <int N>
-__device__ __forceinline__ int above(float v) {  // the lane N before has a larger value
-    return lane_f32<0x120 + N>(v) > v ? 1 : 0;
+template <int CTRL>
+__device__ __forceinline__ int above(float other, float v) {
+    return lane_f32<CTRL>(other) > v ? 1 : 0;
 }
-// Groups (runs of lanes that hold their value) of the row with a larger value.
-__device__ __forceinline__ int group_rank(float v, int run) {
-    int n = above<8>(v);
-    if (run <= 4) n += above<4>(v) + above<12>(v);
-    if (run <= 2) n += above<2>(v) + above<6>(v) + above<10>(v) + above<14>(v);
-    if (run <= 1)
-        n += above<1>(v) + above<3>(v) + above<5>(v) + above<7>(v) + above<9>(v) + above<11>(v) +
-             above<13>(v) + above<15>(v);
-    return n;
+// Lanes of the token with a larger value.
+template <int LT>
+__device__ __forceinline__ int lanes_above(float v) {
+    if constexpr (LT == 8) {
+        const float o = lane_f32<0x141>(v);  // the other four lanes, mirrored
+        return above<0x39>(v, v) + above<0x4E>(v, v) + above<0x93>(v, v) + (o > v ? 1 : 0) +
+               above<0x39>(o, v) + above<0x4E>(o, v) + above<0x93>(o, v);
+    }
+    return above<0x121>(v, v) + above<0x122>(v, v) + above<0x123>(v, v) + above<0x124>(v, v) +
+           above<0x125>(v, v) + above<0x126>(v, v) + above<0x127>(v, v) + above<0x128>(v, v) +
+           above<0x129>(v, v) + above<0x12A>(v, v) + above<0x12B>(v, v) + above<0x12C>(v, v) +
+           above<0x12D>(v, v) + above<0x12E>(v, v) + above<0x12F>(v, v);
 }
 
-// Lanes of the row where it is true.
-__device__ __forceinline__ int row_count(bool b) {
-    return __popc((uint32_t)(__ballot(b) >> (threadIdx.x & 48)) & 0xFFFFu);
+// The two largest of a run of lanes.
+__device__ __forceinline__ void run_top2(float &x, float &y, int run) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (run >= 2 << i) {
+            const float x2 = dpp_f32(x, i), y2 = dpp_f32(y, i);
+            y = fmaxf(fminf(x, x2), fmaxf(y, y2));
+            x = fmaxf(x, x2);
+        }
 }
 
 // Choices in fp32 with their error's bound: a token whose choice could come out
 // otherwise in 64 bits (a gap below the bound, a NaN, values out of range) is done
 // again by exact_token.  Bounds, for |c| <= 4: sigmoid within 2^-22 (exponent, sum
-// and reciprocal together below 4 * 2^-24), softmax within 2^-19.4 (a sum of 16 terms
-// by 16 lanes: 20 roundings of 2^-24, and the terms' own), the bias' addition 2^-22,
-// the key's step 2^-23.
-// Groups are whole runs of lanes: G divides 16, and 16 the experts.
-template <int NV, class Z, bool ALIGNED>
+// and reciprocal together below 4 * 2^-24), softmax within 2^-18.7 (a sum of NV terms
+// by LT lanes: 35 roundings of 2^-24 at most, and the terms' own), the bias' addition
+// 2^-22, the key's step 2^-23.
+// Groups are whole runs of lanes: G divides LT, and LT the experts.
+template <int LT, int NV, class Z, bool ALIGNED>
 __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *__restrict__ z,
                                                              const float *__restrict__ bias,
                                                              int32_t *__restrict__ ids,
                                                              float *__restrict__ w) {
-    __shared__ Quad<NV> quads[kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15;
-    const int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * kQuad;
+    using Q = Tokens<LT, NV>;
+    __shared__ Q quads[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane % LT;
+    const int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * Q::N;
     if (t0 >= r.T) return;
-    Quad<NV> &q = quads[wave];
-    const int n = (int)min((int64_t)kQuad, r.T - t0) * r.E;
-    const int64_t t = t0 + (lane >> 4);
-    quad_in<NV, Z, ALIGNED>(r, z + t0 * r.E, n, q);
+    Q &q = quads[wave];
+    const int n = (int)min((int64_t)Q::N, r.T - t0) * r.E;
+    const int64_t t = t0 + lane / LT;
+    tokens_in<LT, NV, Z, ALIGNED>(r, z + t0 * r.E, n, q);
     float b[NV];
     if (bias) {
 #pragma unroll
@@ -456,110 +467,93 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     }
     wave_sync();
     float v[NV];  // logits, then what the choice is by
-    quad_get(r, q, n, -INFINITY, v);
-    bool bad = false;
-    float zmax = -INFINITY;
+    tokens_get(r, q, n, -INFINITY, v);
+    // infinities and NaN: a sum of zeros, or not
+    float odd = 0.f, zmax = v[0];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        bad |= !(v[i] < INFINITY);
+        odd = fmaf(v[i], 0.f, odd);
         zmax = fmaxf(zmax, v[i]);
     }
-    zmax = row_max(zmax);
-    bad |= !(zmax > -INFINITY);  // (a NaN beside -inf alone; no expert at all)
-    const bool groups = r.G > 1, raw = r.sigmoid || r.renorm;
+    zmax = max_f32<LT>(zmax);
+    const bool masks = __ballot(odd != 0.f) != 0;
+    bool bad = !(zmax < INFINITY && zmax > -INFINITY);
+    if (masks) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) bad |= v[i] != v[i];
+    }
+    const bool groups = r.G > 1, by_score = bias || (groups && r.pair);
     double sum = 1.0;
-    // scores: where the choice or the groups are by them
-    if (bias || (groups && r.pair)) {
-        float s[NV];
+    if (!r.sigmoid && !r.renorm) {
+        sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) sum += exp_near((double)v[i] - zmax);
+        sum = sum_f64<LT>(sum);
+    }
+    float s[NV];
+    if (by_score) {
         if (r.sigmoid) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 s[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v[i]));
         } else {
             float total = 0.f;
+            const float far = -kLog2e * zmax;  // (its rounding is every term's)
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(kLog2e * (v[i] - zmax));
+                s[i] = __builtin_amdgcn_exp2f(fmaf(v[i], kLog2e, far));
                 total += s[i];
             }
-            const float f = __builtin_amdgcn_rcpf(row_sum(total));
+            const float f = __builtin_amdgcn_rcpf(sum_f32<LT>(total));
 #pragma unroll
             for (int i = 0; i < NV; ++i) s[i] *= f;
         }
-        if (!raw) {
-            sum = 0.0;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) sum += exp_near((double)v[i] - zmax);
-            sum = sum_f64<true>(sum);
-        }
-        float cmax = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const float c = bias ? s[i] + b[i] : s[i];
-            s[i] = v[i] > -INFINITY && c > -INFINITY ? c : -INFINITY;
-            cmax = fmaxf(cmax, s[i] > -INFINITY ? fabsf(s[i]) : 0.f);
-        }
-        bad |= !(cmax <= 4.f);  // out of the bounds' range
-        if (groups) {
-            float x = -INFINITY, y = -INFINITY;  // the two largest
+        if (bias) {
+            float out = 0.f, most = 0.f;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                y = fmaxf(y, fminf(x, s[i]));
+                s[i] += b[i];
+                out = fmaf(s[i], 0.f, out);
+                most = fmaxf(most, fabsf(s[i]));
+            }
+            // a bias that is no number, or out of the bounds' range; -inf is a mask
+            if (__ballot(out != 0.f || !(most <= 4.f))) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (!(s[i] > -INFINITY)) s[i] = -INFINITY;
+                    bad |= s[i] > 4.f || (s[i] < -4.f && s[i] > -INFINITY);
+                }
+            }
+        }
+        if (masks) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (v[i] == -INFINITY) s[i] = -INFINITY;
+        }
+    }
+    bool keep = true;
+    if (groups) {
+        const int run = LT / r.G;  // lanes of a group
+        float x = -INFINITY, y = -INFINITY;  // the two largest
+        if (by_score) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                y = __builtin_amdgcn_fmed3f(x, y, s[i]);
                 x = fmaxf(x, s[i]);
-            }
-            const int run = 16 / r.G;  // lanes of a group
-            if (run >= 2) {
-                const float x2 = dpp_f32(x, 0), y2 = dpp_f32(y, 0);
-                y = fmaxf(fminf(x, x2), fmaxf(y, y2)), x = fmaxf(x, x2);
-            }
-            if (run >= 4) {
-                const float x2 = dpp_f32(x, 1), y2 = dpp_f32(y, 1);
-                y = fmaxf(fminf(x, x2), fmaxf(y, y2)), x = fmaxf(x, x2);
-            }
-            if (run >= 8) {
-                const float x2 = dpp_f32(x, 2), y2 = dpp_f32(y, 2);
-                y = fmaxf(fminf(x, x2), fmaxf(y, y2)), x = fmaxf(x, x2);
-            }
-            if (r.pair && y > -INFINITY) x += y;
-            const int rank = group_rank(x, run);  // (by every lane)
-            const bool keep = x > -INFINITY && rank < r.top_groups;
-            const float in = row_min(keep ? x : INFINITY), out = row_max(keep ? -INFINITY : x);
-            // a value is within 2^-18 (two choices and their sum)
-            bad |= out > -INFINITY && !(in - out > 0x1p-17f);
-            bad |= row_count(keep) > r.top_groups * run;  // equal ones
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (bias) v[i] = s[i];
-                if (!keep) v[i] = -INFINITY;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = s[i];
-        }
-    } else {
-        if (!raw) {
-            sum = 0.0;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) sum += exp_near((double)v[i] - zmax);
-            sum = sum_f64<true>(sum);
-        }
-        if (groups) {  // by the largest logit: exact
-            float x = -INFINITY;
-#pragma unroll
             for (int i = 0; i < NV; ++i) x = fmaxf(x, v[i]);
-            const int run = 16 / r.G;
-            if (run >= 2) x = fmaxf(x, dpp_f32(x, 0));
-            if (run >= 4) x = fmaxf(x, dpp_f32(x, 1));
-            if (run >= 8) x = fmaxf(x, dpp_f32(x, 2));
-            const int rank = group_rank(x, run);  // (by every lane)
-            const bool keep = x > -INFINITY && rank < r.top_groups;
-            const float in = row_min(keep ? x : INFINITY), out = row_max(keep ? -INFINITY : x);
-            bad |= out > -INFINITY && !(in > out);
-            bad |= row_count(keep) > r.top_groups * run;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (!keep) v[i] = -INFINITY;
         }
+        run_top2(x, y, run);
+        if (r.pair && y > -INFINITY) x += y;
+        const int rank = lanes_above<LT>(x);  // (by every lane)
+        keep = x > -INFINITY && rank < r.top_groups * run;
+        const float in = -max_f32<LT>(keep ? -x : -INFINITY);
+        const float out = max_f32<LT>(keep ? -INFINITY : x);
+        // a group's value is within 2^-17.4 (two choices and their sum); logits are exact
+        bad |= out > -INFINITY && !(by_score ? in - out > 0x1p-16f : in > out);
+        bad |= __popc(lanes_true<LT>(keep)) > r.top_groups * run;  // equal ones
     }
     // keys: steps below the largest, of 2^-23 for choices; of 2^-19 for logits, whose
     // differences are within 2^-19 up to 32; bf16 logits keep their own bits
@@ -569,23 +563,43 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
 #pragma unroll
         for (int i = 0; i < NV; ++i) key[i] = 0xFFFFu - (ord32(v[i]) >> 16);
     } else {
-        float top = -INFINITY;
+        float top = zmax;
+        if (bias) {
+            top = s[0];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) top = fmaxf(top, v[i]);
+            for (int i = 0; i < NV; ++i) {
+                v[i] = s[i];
+                top = fmaxf(top, s[i]);
+            }
+            top = max_f32<LT>(top);
+        }
         const float step = bias ? 0x1p23f : 0x1p19f;
-        top = row_max(top) * step;
+        top *= step;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             key[i] = (uint32_t)fminf(fmaf(v[i], -step, top), 16777214.f);
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        key[i] = v[i] > -INFINITY ? (key[i] << 8) + (uint32_t)(l * r.per + i) : ~0u;
+    for (int i = 0; i < NV; ++i) key[i] = (key[i] << 8) + (uint32_t)(l * r.per) + i;
+    if (masks || bias) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (v[i] == -INFINITY) key[i] = ~0u;
+    }
     uint32_t a[8], ninth;
-    row_best8(key, a, ninth);
+    lane_best8(key, a, ninth);
+    if (groups) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = keep ? a[i] : ~0u;
+        ninth = keep ? ninth : ~0u;
+    }
+    merge_lanes<0xB1>(a, ninth);
+    merge_lanes<0x4E>(a, ninth);
+    merge_lanes<0x141>(a, ninth);
+    if constexpr (LT == 16) merge_lanes<0x140>(a, ninth);
     if (!bits) {
         // (a list that ends before the k-th is done again too)
-        const uint32_t gap = (bias ? (r.sigmoid ? 17u : 49u) : 5u) << 8;
+        const uint32_t gap = (bias ? (r.sigmoid ? 17u : 65u) : 5u) << 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             bad |= (i < 7 ? a[i < 7 ? i + 1 : 7] : ninth) - a[i] < (i < r.k ? gap : 0u);
@@ -595,19 +609,19 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     for (int i = 0; i < 8; ++i) mine = l == i ? a[i] : mine;
     const bool there = l < r.k && mine < kNone;
     const uint32_t e = there ? mine & 255u : 0u;
-    const float z_at = q.v[quad_at<NV>(r, (lane >> 4) * r.E + e)];
-    const double weight =
-        chosen_weight<true>(r.sigmoid, r.renorm, there, z_at, zmax, sum) * r.scale;
-    const uint64_t redo = __ballot(bad && t < r.T);
-    if (t < r.T && l < r.k && !(redo >> (lane & 48) & 0xFFFF)) {
+    const float z_at = q.v[Q::at(r, lane / LT * r.E + e)];
+    const double weight = chosen_weight<LT>(r.sigmoid, r.renorm, there, z_at, zmax, sum) * r.scale;
+    bad = lanes_true<LT>(bad && t < r.T) != 0;
+    if (t < r.T && l < r.k && !bad) {
         ids[t * r.k + l] = there ? (int32_t)e : -1;
         w[t * r.k + l] = (float)weight;
     }
+    const uint64_t redo = __ballot(bad);
     if (!redo) return;
     wave_sync();
 #pragma unroll 1
-    for (int i = 0; i < kQuad; ++i)
-        if (redo >> (16 * i) & 0xFFFF)
+    for (int i = 0; i < Q::N; ++i)
+        if (redo >> (LT * i) & 1)
             exact_token(r, t0 + i, z, bias, ids, w, reinterpret_cast<double *>(q.v),
                         reinterpret_cast<double *>(q.v) + r.E);
 }
@@ -646,12 +660,13 @@ template <int NV, class Z, bool ALIGNED>
 __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
     Rules r, const Z *__restrict__ z, const int32_t *__restrict__ ids,
     const float *__restrict__ dw, Z *__restrict__ dz) {
-    __shared__ Quad<NV> quads[kWaves];
+    using Q = Tokens<16, NV>;
+    __shared__ Q quads[kWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15;
-    const int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * kQuad;
+    const int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * Q::N;
     if (t0 >= r.T) return;
-    Quad<NV> &q = quads[wave];
-    const int n = (int)min((int64_t)kQuad, r.T - t0) * r.E;
+    Q &q = quads[wave];
+    const int n = (int)min((int64_t)Q::N, r.T - t0) * r.E;
     const int64_t t = t0 + (lane >> 4);
     const bool slot = t < r.T && l < r.k;
     int id = slot ? ids[t * r.k + l] : -1;
@@ -660,14 +675,14 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
     const double G = there ? (double)dw[t * r.k + l] * r.scale : 0.0;
     const float zj = there ? logit_at(z, t * r.E + id) : 0.f;
     const bool all = !r.sigmoid && !r.renorm;
-    float *mine = q.v + lane * Quad<NV>::PITCH;
+    float *mine = q.v + lane * Q::PITCH;
     float s[NV];
     float zmax = 0.f;
     double sum = 1.0;
     if (all) {
-        quad_in<NV, Z, ALIGNED>(r, z + t0 * r.E, n, q);
+        tokens_in<16, NV, Z, ALIGNED>(r, z + t0 * r.E, n, q);
         wave_sync();
-        quad_get(r, q, n, -INFINITY, s);
+        tokens_get(r, q, n, -INFINITY, s);
         zmax = -INFINITY;
         bool nan = false;
 #pragma unroll
@@ -675,9 +690,8 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
             zmax = fmaxf(zmax, s[i]);
             nan |= s[i] != s[i];
         }
-        zmax = row_max(zmax);
-        const uint64_t has = __ballot(nan);
-        if (has >> (lane & 48) & 0xFFFF) zmax = NAN;
+        zmax = max_f32<16>(zmax);
+        if (lanes_true<16>(nan)) zmax = NAN;
         if (zmax == -INFINITY) zmax = 0.f;  // every expert switched off: all s are 0
         float total = 0.f;
 #pragma unroll
@@ -685,11 +699,11 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
             s[i] = __builtin_amdgcn_exp2f(kLog2e * (s[i] - zmax));
             total += s[i];
         }
-        total = row_sum(total);
+        total = sum_f32<16>(total);
         sum = total > 0.f ? (double)total : total == 0.f ? 1.0 : (double)NAN;
     }
-    const double p = chosen_weight<true>(r.sigmoid, r.renorm, there, zj, zmax, sum);
-    const double D = sum_f64<true>(G * p);
+    const double p = chosen_weight<16>(r.sigmoid, r.renorm, there, zj, zmax, sum);
+    const double D = sum_f64<16>(G * p);
     double c;
     if (r.sigmoid) {
         const double rest = 1.0 / (1.0 + exp((double)zj));  // 1 - s
@@ -711,7 +725,7 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
     }
     wave_sync();
     if (there) {  // (lanes of one id write the same value)
-        const int at = quad_at<NV>(r, (lane >> 4) * r.E + id);
+        const int at = Q::at(r, (lane >> 4) * r.E + id);
         const float was = q.v[at];
         wave_sync();
         q.v[at] = was + add;
@@ -726,12 +740,12 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
         if (i >= n) continue;
         float o[4];
         if (whole) {
-            const floatx4 u = *reinterpret_cast<const floatx4 *>(&q.v[quad_at<NV>(r, i)]);
+            const floatx4 u = *reinterpret_cast<const floatx4 *>(&q.v[Q::at(r, i)]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[j] = u[j];
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = i + j < n ? q.v[quad_at<NV>(r, i + j)] : 0.f;
+            for (int j = 0; j < 4; ++j) o[j] = i + j < n ? q.v[Q::at(r, i + j)] : 0.f;
         }
         if (ALIGNED && i + 4 <= n) {
             store4(dst + i, o);
@@ -778,52 +792,70 @@ Rules rules(const moe_dims &d, const moe_routing &r) {
     q.sigmoid = r.score == MOE_SCORE_SIGMOID, q.renorm = d.renormalize;
     q.G = r.groups, q.top_groups = r.top_groups, q.pair = r.group_score == MOE_GROUP_TOP_TWO;
     q.scale = r.scale;
-    q.per = (q.E + 15) / 16;
-    q.div_E = ((1u << 20) + q.E - 1) / q.E;
-    q.div_per = ((1u << 16) + q.per - 1) / q.per;
     return q;
 }
+Rules with_lanes(Rules r, int lanes) {
+    r.per = (r.E + lanes - 1) / lanes;
+    r.div_E = ((1u << 20) + r.E - 1) / r.E;
+    r.div_per = ((1u << 16) + r.per - 1) / r.per;
+    return r;
+}
 
+template <int N>
+using Int = std::integral_constant<int, N>;
 // fn(the most experts of a lane, whether four elements load at once).
 template <class F>
 hipError_t by_size(const Rules &r, bool aligned, F fn) {
     auto go = [&](auto nv) {
         return aligned ? fn(nv, std::true_type()) : fn(nv, std::false_type());
     };
-    if (r.per <= 1) return go(std::integral_constant<int, 1>());
-    if (r.per <= 4) return go(std::integral_constant<int, 4>());
-    if (r.per <= 8) return go(std::integral_constant<int, 8>());
-    if (r.per <= 10) return go(std::integral_constant<int, 10>());
-    return go(std::integral_constant<int, 16>());
+    if (r.per <= 1) return go(Int<1>());
+    if (r.per <= 4) return go(Int<4>());
+    if (r.per <= 8) return go(Int<8>());
+    if (r.per <= 10) return go(Int<10>());
+    return go(Int<16>());
 }
 
 template <class Z>
 bool aligned4(const Z *p) { return (uintptr_t)p % (4 * sizeof(Z)) == 0; }
 
-unsigned quad_blocks(const Rules &r) {
-    return (unsigned)((r.T + kWaves * kQuad - 1) / (kWaves * kQuad));
+unsigned grid_of(const Rules &r, int tokens) {  // of a wave
+    return (unsigned)((r.T + kWaves * tokens - 1) / (kWaves * tokens));
 }
 
+// Whether G groups are runs of the lanes.
+bool runs(const Rules &r, int lanes) { return r.G == 1 || (lanes % r.G == 0 && r.E % lanes == 0); }
+
 template <class Z>
-hipError_t launch_scores(const Rules &r, const Z *z, const float *bias, int32_t *ids, float *w,
+hipError_t launch_scores(Rules r, const Z *z, const float *bias, int32_t *ids, float *w,
                          hipStream_t s) {
-    if (r.G > 1 && (16 % r.G || r.E % 16)) {  // groups that are no runs of lanes
-        exact_kernel<Z><<<(unsigned)((r.T + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(r, z, bias,
-                                                                                       ids, w);
-        return hipGetLastError();
+    if (r.T >= kManyTokens && r.E > 64 && runs(r, 8) && aligned4(z)) {
+        r = with_lanes(r, 8);
+        auto go = [&](auto nv) {
+            scores_kernel<8, nv(), Z, true><<<grid_of(r, 8), 64 * kWaves, 0, s>>>(r, z, bias, ids,
+                                                                                  w);
+            return hipGetLastError();
+        };
+        return r.per <= 16 ? go(Int<16>()) : r.per <= 20 ? go(Int<20>()) : go(Int<32>());
     }
-    return by_size(r, aligned4(z), [&](auto nv, auto al) {
-        scores_kernel<nv(), Z, al()><<<quad_blocks(r), 64 * kWaves, 0, s>>>(r, z, bias, ids, w);
-        return hipGetLastError();
-    });
+    if (runs(r, 16)) {
+        r = with_lanes(r, 16);
+        return by_size(r, aligned4(z), [&](auto nv, auto al) {
+            scores_kernel<16, nv(), Z, al()><<<grid_of(r, 4), 64 * kWaves, 0, s>>>(r, z, bias, ids,
+                                                                                   w);
+            return hipGetLastError();
+        });
+    }
+    exact_kernel<Z><<<grid_of(r, 1), 64 * kWaves, 0, s>>>(r, z, bias, ids, w);
+    return hipGetLastError();
 }
 
 template <class Z>
-hipError_t launch_back(const Rules &r, const Z *z, const int32_t *ids, const float *dw, Z *dz,
+hipError_t launch_back(Rules r, const Z *z, const int32_t *ids, const float *dw, Z *dz,
                        hipStream_t s) {
+    r = with_lanes(r, 16);
     return by_size(r, aligned4(z) && aligned4(dz), [&](auto nv, auto al) {
-        scores_back_kernel<nv(), Z, al()><<<quad_blocks(r), 64 * kWaves, 0, s>>>(r, z, ids, dw,
-                                                                                 dz);
+        scores_back_kernel<nv(), Z, al()><<<grid_of(r, 4), 64 * kWaves, 0, s>>>(r, z, ids, dw, dz);
         return hipGetLastError();
     });
 }

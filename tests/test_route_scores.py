@@ -261,6 +261,34 @@ def test_many_tokens(T):
 
 
 @gpu
+@pytest.mark.parametrize("E,k,G,top", [(65, 5, 1, 1), (100, 8, 1, 1), (128, 8, 4, 2), (160, 6, 8, 3),
+                                       (161, 5, 7, 3), (200, 3, 1, 1), (256, 8, 8, 4),
+                                       (256, 7, 2, 1), (256, 8, 16, 5)])
+def test_rules_over_many_tokens(E, k, G, top):
+    T = 16387
+    b = torch.randn(E, generator=torch.Generator().manual_seed(2)).mul(0.1).cuda()
+    b[E // 2], b[3] = -math.inf, math.nan
+    at = torch.cat([torch.arange(0, T, 211), torch.arange(T - 9, T)]).cuda()
+    for i, (sigmoid, bias, pair, renorm, dtype, masked) in enumerate([
+            (True, b, True, True, F32, 0), (False, None, False, False, F32, 0),
+            (False, b, True, False, F32, 5), (True, None, True, False, BF16, 0),
+            (False, None, True, True, BF16, 9), (True, b, False, False, BF16, 0)]):
+        z = make(E + i, T, E, dtype, masked, sigmoid)
+        z[211 * 3, 7], z[211 * 5] = math.nan, -math.inf
+        z[T - 2, :9] = 1.5  # ties
+        rules = dict(sigmoid=sigmoid, groups=G, top_groups=top, pair=pair, renorm=renorm, scale=1.5)
+        ids, w = run(z, bias, k, **rules)
+        rid, rw = ref.route(z[at].double().cpu().numpy(),
+                            None if bias is None else b.double().cpu().numpy(), k, **rules)
+        np.testing.assert_array_equal(ids[at].cpu().numpy(), rid)
+        np.testing.assert_allclose(w[at].cpu().numpy(), rw, rtol=2.0 ** -23, atol=2.0 ** -150)
+        # the tokens in parts of few: the same
+        ids2, w2 = run(z[:5000], bias, k, **rules)
+        assert torch.equal(ids[:5000], ids2)
+        assert torch.equal(w[:5000].view(torch.int32), w2.view(torch.int32))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_any_address(dtype):
     """Logits and outputs at any address of their type, the bytes around untouched."""
