@@ -428,6 +428,28 @@ __device__ __forceinline__ int lanes_above(float v) {
            above<0x12D>(v, v) + above<0x12E>(v, v) + above<0x12F>(v, v);
 }
 
+// How many of a token's other first eight lanes are chosen before this one, by
+// (c descending, id ascending); lanes behind them keep their own number.
+template <int CTRL>
+__device__ __forceinline__ int before(double c, int id, double mc, int mid) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, c);
+    const double oc = __builtin_bit_cast(
+        double, (uint64_t)lane32<CTRL>((uint32_t)(b >> 32)) << 32 | lane32<CTRL>((uint32_t)b));
+    const int oid = (int)lane32<CTRL>((uint32_t)id);
+    return oc > mc || (oc == mc && oid < mid) ? 1 : 0;
+}
+__device__ __forceinline__ int eight_rank(double c, int id, int l) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, c);
+    const double o = __builtin_bit_cast(  // the other four, mirrored
+        double, (uint64_t)lane32<0x141>((uint32_t)(b >> 32)) << 32 | lane32<0x141>((uint32_t)b));
+    const int oid = (int)lane32<0x141>((uint32_t)id);
+    const int n = before<0x39>(c, id, c, id) + before<0x4E>(c, id, c, id) +
+                  before<0x93>(c, id, c, id) + before<0x39>(o, oid, c, id) +
+                  before<0x4E>(o, oid, c, id) + before<0x93>(o, oid, c, id) +
+                  (o > c || (o == c && oid < id) ? 1 : 0);
+    return l < 8 ? n : l;
+}
+
 // The two largest of a run of lanes.
 __device__ __forceinline__ void run_top2(float &x, float &y, int run) {
 #pragma unroll
@@ -477,7 +499,7 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     }
     zmax = max_f32<LT>(zmax);
     const bool masks = __ballot(odd != 0.f) != 0;
-    bool bad = !(zmax < INFINITY && zmax > -INFINITY);
+    bool bad = !(fabsf(zmax) < 0x1p100f);  // infinite, or far enough to overflow
     if (masks) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) bad |= v[i] != v[i];
@@ -551,12 +573,14 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
         keep = x > -INFINITY && rank < r.top_groups * run;
         const float in = -max_f32<LT>(keep ? -x : -INFINITY);
         const float out = max_f32<LT>(keep ? -INFINITY : x);
-        // a group's value is within 2^-17.4 (two choices and their sum); logits are exact
-        bad |= out > -INFINITY && !(by_score ? in - out > 0x1p-16f : in > out);
+        // a group's value (two choices and their sum) is within 2^-17.5, of sigmoids
+        // 2^-19.6; logits are exact
+        const float gap = r.sigmoid ? 0x1p-18f : 0x1p-16f;
+        bad |= out > -INFINITY && !(by_score ? in - out > gap : in > out);
         bad |= __popc(lanes_true<LT>(keep)) > r.top_groups * run;  // equal ones
     }
-    // keys: steps below the largest, of 2^-23 for choices; of 2^-19 for logits, whose
-    // differences are within 2^-19 up to 32; bf16 logits keep their own bits
+    // keys: steps below the largest, of 2^-23 for choices, of 2^-21 for logits, whose
+    // differences are within half a step; bf16 logits keep their own bits
     const bool bits = !bias && sizeof(Z) == 2;
     uint32_t key[NV];
     if (bits) {
@@ -573,7 +597,7 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
             }
             top = max_f32<LT>(top);
         }
-        const float step = bias ? 0x1p23f : 0x1p19f;
+        const float step = bias ? 0x1p23f : 0x1p21f;
         top *= step;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -597,24 +621,40 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     merge_lanes<0x4E>(a, ninth);
     merge_lanes<0x141>(a, ninth);
     if constexpr (LT == 16) merge_lanes<0x140>(a, ninth);
-    if (!bits) {
-        // (a list that ends before the k-th is done again too)
-        const uint32_t gap = (bias ? (r.sigmoid ? 17u : 65u) : 5u) << 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            bad |= (i < 7 ? a[i < 7 ? i + 1 : 7] : ninth) - a[i] < (i < r.k ? gap : 0u);
-    }
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) mine = l == i ? a[i] : mine;
-    const bool there = l < r.k && mine < kNone;
-    const uint32_t e = there ? mine & 255u : 0u;
+    const bool found = l < 8 && mine < kNone;
+    const uint32_t e = found ? mine & 255u : 0u;
     const float z_at = q.v[Q::at(r, lane / LT * r.E + e)];
+    int rank = l;
+    if (!bits) {
+        const uint32_t gap = (bias ? (r.sigmoid ? 12u : 65u) : 4u) << 8;
+        bool near = false;  // among the eight
+#pragma unroll
+        for (int i = 0; i < 7; ++i) near |= a[i + 1] - a[i] < (i < r.k && a[i + 1] < kNone ? gap : 0u);
+        // the ninth may be one of the k: by itself, or by a chain of near ones
+        uint32_t kth = a[7];
+#pragma unroll
+        for (int i = 0; i < 7; ++i) kth = r.k == i + 1 ? a[i] : kth;
+        bad |= ninth < kNone && ninth - a[7] < gap && a[7] - kth < 8 * gap;
+        bad |= kth >= kNone;  // fewer than k: rare, not looked into here
+        if (bias && !r.sigmoid) {
+            bad |= near;
+        } else if (__ballot(near)) {  // the eight in 64 bits
+            double c = z_at;
+            if (bias) c = 1.0 / (1.0 + exp(-(double)z_at)) + (double)bias[e];
+            if (!found) c = -INFINITY;
+            const int id = found ? (int)e : 256 + l;
+            rank = eight_rank(c, id, l);
+        }
+    }
+    const bool there = found && rank < r.k;
     const double weight = chosen_weight<LT>(r.sigmoid, r.renorm, there, z_at, zmax, sum) * r.scale;
     bad = lanes_true<LT>(bad && t < r.T) != 0;
-    if (t < r.T && l < r.k && !bad) {
-        ids[t * r.k + l] = there ? (int32_t)e : -1;
-        w[t * r.k + l] = (float)weight;
+    if (t < r.T && l < 8 && rank < r.k && !bad) {
+        ids[t * r.k + rank] = there ? (int32_t)e : -1;
+        w[t * r.k + rank] = (float)weight;
     }
     const uint64_t redo = __ballot(bad);
     if (!redo) return;
