@@ -18,14 +18,15 @@ struct AdapterRows {
 };
 
 // Sums over K of rows times a low-rank matrix, in fp32: [tile][split][rank][rows of
-// a tile], tiles as the device numbers them, a split a share of K.
+// a tile], tiles as the device numbers them, a split a share of K; for many rows also
+// scaled and cut into bf16 parts, as operands (e, q).
 struct AdapterSums {
     float *p;
     int splits;
+    bf16_t *e, *q;
 };
-// Shares of K that the sums of these rows are cut into, and their bytes (no fewer
-// than any fewer rows need).
-int adapter_splits(int64_t rows, int count, int K, int rank);
+// Their layout at an address, and its bytes (no fewer than any fewer rows need).
+AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, void *at);
 size_t adapter_sums_bytes(int64_t rows, int count, int rank);
 
 // Bytes of the buffer of the outer products' parts over C columns (likewise).

@@ -11,14 +11,22 @@
 #include "adapters.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dispatch.h"
 
 namespace moe {
 namespace {
 
-constexpr int kWaves = 4;        // of the kernels but shrink
-constexpr int kShrinkWaves = 4;  // which share K
+constexpr int kWaves = 4;       // of expand over short tiles
+constexpr int expand_waves(int RB) { return RB == 1 ? kWaves : RB; }
+constexpr int kExpandSpan = 8;  // blocks of 64 columns of its workgroups over tall tiles
+constexpr int kOuterWaves = 8;  // of outer: four column blocks, two halves of the rows
+
+// Row blocks of 16 of a tile -> rows of it, as a power of two.
+constexpr int tile_shift_of(int RB) { return RB == 8 ? 7 : RB == 4 ? 6 : 4; }
+// The waves of shrink: they share K, and the rows of the tallest tiles.
+constexpr int shrink_waves(int RB) { return 4; }
 
 __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -91,8 +99,9 @@ __device__ __forceinline__ int row_at(const AdapterRows &o, int64_t place) {
 // ---- x A^T ---------------------------------------------------------------
 
 // Sums of `rows` times w [count][rank][K].  The matrix instruction's M is the
-// rows, its N the rank; an operand load is 64 bytes of each of 16 rows.  The waves
-// (and `splits` workgroups) share K; a wave keeps DEP steps of 64 k in flight.
+// rows, its N the rank.  A wave has at most four row blocks; the waves with the same
+// ones (and `splits` workgroups) share K, each taking every so many-th 128 bytes of a
+// row, and keep DEP steps of them in flight.
 struct Shrink {
     const bf16_t *x, *w;
     AdapterSums out;
@@ -100,22 +109,28 @@ struct Shrink {
 };
 
 template <int RB, int NR>
+struct ShrinkCfg {
+    static constexpr int W = shrink_waves(RB), PB = RB < 4 ? RB : 4, RG = RB / PB, KG = W / RG;
+    static constexpr int DEP = PB + NR <= 3 ? 4 : PB + NR <= 5 && NR < 4 ? 3 : 2;
+};
+
+template <int RB, int NR>
 __device__ __forceinline__ void shrink(const AdapterRows &o, int rank, const Shrink &k, int tile,
-                                       int split, int r0, floatx4 (*lds)[RB * NR][64]) {
-    constexpr int DEP = RB + NR <= 3 ? 4 : RB + NR <= 5 ? 3 : 2, TM = 16 * RB;
-    const Tile t = find_tile(o, RB == 4 ? 6 : 4, tile);
+                                       int split, int r0, floatx4 *lds) {
+    using C = ShrinkCfg<RB, NR>;
+    constexpr int DEP = C::DEP, TM = 16 * RB, PB = C::PB;
+    const Tile t = find_tile(o, tile_shift_of(RB), tile);
     if (t.e < 0) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // a wave takes every parts-th 128 bytes of a row, so that a workgroup's loads are
-    // next to each other
-    const int parts = k.out.splits * kShrinkWaves, part = split * kShrinkWaves + wave;
+    const int rg = wave % C::RG, kg = wave / C::RG, b0 = rg * PB;
+    const int parts = k.out.splits * C::KG, part = split * C::KG + kg;
     const int n = (k.K / 64 - part + parts - 1) / parts;
-    uint64_t xo[RB];
+    uint64_t xo[PB];
     uint32_t wo[NR];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-        const int row = row_at(o, t.first + min(16 * b + m, t.rows - 1));
+    for (int b = 0; b < PB; ++b) {
+        const int row = row_at(o, t.first + min(16 * (b0 + b) + m, t.rows - 1));
         xo[b] = ((uint64_t)max(row, 0) * k.K + 8 * g) * 2;
     }
 #pragma unroll
@@ -123,13 +138,13 @@ __device__ __forceinline__ void shrink(const AdapterRows &o, int rank, const Shr
         wo[c] = ((uint32_t)min(r0 + 16 * c + m, rank - 1) * k.K + 8 * g) * 2;
     const char *xs = (const char *)(k.x + part * 64);
     const char *ws = (const char *)(k.w + (int64_t)t.e * rank * k.K + part * 64);
-    floatx4 acc[RB][NR] = {};
-    bf16x8 xv[DEP][RB][2], wv[DEP][NR][2];
+    floatx4 acc[PB][NR] = {};
+    bf16x8 xv[DEP][PB][2], wv[DEP][NR][2];
     // (both halves of a cache line one after the other: it may not stay)
     auto load = [&](int i, int s) {
         const int at = s * parts * 128;
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
+        for (int b = 0; b < PB; ++b)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 xv[i][b][h] = *reinterpret_cast<const bf16x8 *>(xs + at + xo[b] + 64 * h);
@@ -143,7 +158,7 @@ __device__ __forceinline__ void shrink(const AdapterRows &o, int rank, const Shr
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
+            for (int b = 0; b < PB; ++b)
 #pragma unroll
                 for (int c = 0; c < NR; ++c)
                     acc[b][c] = mfma(xv[i][b][h], wv[i][c][h], acc[b][c]);
@@ -163,32 +178,34 @@ __device__ __forceinline__ void shrink(const AdapterRows &o, int rank, const Shr
         for (int i = 0; i < DEP; ++i)
             if (s + i < n) use(i);
     }
-    // the waves' sums meet in LDS, half of the waves' at a time
+    // the sums of the waves that share K meet in LDS, half of them at a time
 #pragma unroll
-    for (int half = kShrinkWaves / 2; half >= 1; half /= 2) {
-        if (wave >= half && wave < 2 * half) {
+    for (int half = C::KG / 2; half >= 1; half /= 2) {
+        floatx4 *at = lds + ((kg % half) * C::RG + rg) * PB * NR * 64 + lane;
+        if (kg >= half && kg < 2 * half) {
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
+            for (int b = 0; b < PB; ++b)
 #pragma unroll
-                for (int c = 0; c < NR; ++c) lds[wave - half][b * NR + c][lane] = acc[b][c];
+                for (int c = 0; c < NR; ++c) at[(b * NR + c) * 64] = acc[b][c];
         }
         __syncthreads();
-        if (wave < half) {
+        if (kg < half) {
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
+            for (int b = 0; b < PB; ++b)
 #pragma unroll
-                for (int c = 0; c < NR; ++c) acc[b][c] += lds[wave][b * NR + c][lane];
+                for (int c = 0; c < NR; ++c) acc[b][c] += at[(b * NR + c) * 64];
         }
         __syncthreads();
     }
-    if (wave > 0) return;
+    if (kg > 0) return;
     float *p = k.out.p + ((int64_t)tile * k.out.splits + split) * rank * TM;
 #pragma unroll
-    for (int b = 0; b < RB; ++b)
+    for (int b = 0; b < PB; ++b)
 #pragma unroll
         for (int c = 0; c < NR; ++c) {
             const int r = r0 + 16 * c + m;
-            if (r < rank) *reinterpret_cast<floatx4 *>(p + r * TM + 16 * b + 4 * g) = acc[b][c];
+            if (r < rank)
+                *reinterpret_cast<floatx4 *>(p + r * TM + 16 * (b0 + b) + 4 * g) = acc[b][c];
         }
 }
 
@@ -234,17 +251,18 @@ __device__ __forceinline__ void transpose(const AdapterRows &o, const Transpose 
 
 // Blocks of the shrink, then of the transposes (of the gradient's first launch).
 template <int RB, int NR>
-__global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterRows o, int rank,
-                                                                   Shrink k, Transpose ta,
-                                                                   Transpose tb) {
+__global__ __launch_bounds__(64 * shrink_waves(RB), 2) void shrink_kernel(AdapterRows o, int rank,
+                                                                       Shrink k, Transpose ta,
+                                                                       Transpose tb) {
+    using C = ShrinkCfg<RB, NR>;
     __shared__ union {
-        floatx4 sums[kShrinkWaves / 2][RB * NR][64];
+        floatx4 sums[C::KG / 2 * C::RG * C::PB * NR * 64];
         uint16_t tile[64][66];
     } lds;
     int b = blockIdx.x;
     const int groups = (rank + 16 * NR - 1) / (16 * NR), mine = k.tiles * k.out.splits * groups;
     if (b < mine) {
-        shrink<RB, NR>(o, rank, k, b % k.tiles, b / k.tiles % k.out.splits,
+        shrink<RB, NR>(o, rank, k, b / k.out.splits % k.tiles, b % k.out.splits,
                        b / (k.tiles * k.out.splits) * 16 * NR, lds.sums);
         return;
     }
@@ -293,36 +311,98 @@ __device__ __forceinline__ void cut8(const float (&v)[8], bf16x8 (&part)[S]) {
     for (int q = 0; q < S; ++q) part[q] = __builtin_bit_cast(bf16x8, w[q]);
 }
 
-// A lane's 16 values of a row's 64 columns from c on: 16-byte pieces, the lane
-// groups' next to each other, so that a row's piece is 64 bytes.  column(): the
-// output column of the j-th instruction's m (a group has m = 4 g .. 4 g + 3).
-// S: bf16 parts of u, two for bf16 outputs (2^-15 of a value at worst, where the
-// output's rounding is 2^-8), three for fp32.
-template <class Y>
-struct Piece;
-template <>
-struct Piece<bf16_t> {
-    static constexpr int N = 2, W = 8, S = 2;
-    static __device__ __forceinline__ int column(int j, int m) {
-        return 32 * (j >> 1) + 8 * (m >> 2) + 4 * (j & 1) + (m & 3);
-    }
-    static __device__ __forceinline__ u32x4 add(u32x4 base, const floatx4 (&v)[4], int h) {
-        u32x4 u;
+// ---- sums, scaled and cut --------------------------------------------------
+// Of tall tiles: once a row, in a launch of its own, for the many workgroups behind
+// it.  e: S parts as operands of expand, [tile][row block][chunk][row][8] with the
+// chunks of Expand; q: three parts as operands of outer, [tile][part][rank][row].
+struct Cut {
+    AdapterSums u;
+    int S;  // parts of e; 0: none
+    bool q;
+};
+
+__device__ __forceinline__ int chunks_of(int rank, int S) { return (rank / 8 * S + 3) / 4 * 4; }
+
+template <int S>
+__device__ __forceinline__ void store_parts(const float (&v)[8], bf16x8 *e, int chunk0, int rc,
+                                            int kc, int row) {
+    bf16x8 part[S];
+    cut8<S>(v, part);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const floatx4 a = v[2 * h + (i >> 1)];
-            u[i] = pack2(__uint_as_float(base[i] << 16) + a[2 * (i & 1)],
-                         __uint_as_float(base[i] & 0xFFFF0000u) + a[2 * (i & 1) + 1]);
+    for (int s = 0; s < S; ++s) e[(chunk0 + s * rc + kc) * 16 + row] = part[s];
+}
+
+template <int RB>
+__device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const float *scale,
+                                         const Cut &k, const Tile &t, int tile) {
+    constexpr int TM = 16 * RB;
+    const int rc = rank / 8, chunks = k.S ? chunks_of(rank, k.S) : 0;
+    const float f = scale ? scale[t.e] : 1.f;
+    const float *p = k.u.p + (int64_t)tile * k.u.splits * rank * TM;
+    bf16x8 *e = reinterpret_cast<bf16x8 *>(k.u.e) + (int64_t)tile * chunks * TM;
+    uint16_t *q = k.u.q + (int64_t)tile * 3 * rank * TM;
+    for (int i = threadIdx.x; i < TM * rc; i += blockDim.x) {
+        const int row = i % TM, kc = i / TM;
+        float v[8] = {};
+        if (row < t.rows) {
+            for (int s = 0; s < k.u.splits; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += p[((int64_t)s * rank + 8 * kc + j) * TM + row];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= f;
         }
-        return u;
+        if (k.S == 2) store_parts<2>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
+        if (k.S == 3) store_parts<3>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
+        if (k.q) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t c[3];
+                cut<3>(v[j], c);
+#pragma unroll
+                for (int s = 0; s < 3; ++s)
+                    q[((int64_t)s * rank + 8 * kc + j) * TM + row] = (uint16_t)c[s];
+            }
+        }
+    }
+    // the padding behind the last part
+    const int pad = chunks - rc * k.S;
+    for (int i = threadIdx.x; i < TM * pad; i += blockDim.x) {
+        const int row = i % TM, c = rc * k.S + i / TM;
+        e[((row >> 4) * chunks + c) * 16 + (row & 15)] = bf16x8{};
+    }
+}
+
+template <int RB>
+__global__ __launch_bounds__(512) void cut_kernel(AdapterRows o, int rank, const float *scale,
+                                                  Cut a, Cut b, int tiles) {
+    const int tile = blockIdx.x % tiles;
+    const Tile t = find_tile(o, tile_shift_of(RB), tile);
+    if (t.e < 0) return;
+    cut_tile<RB>(o, rank, scale, (int)blockIdx.x < tiles ? a : b, t, tile);
+}
+
+// A lane's four columns of a row, next to each other (the lanes of a group have 64
+// between them).  S: bf16 parts of u, two for bf16 outputs (2^-15 of a value at worst,
+// where the output's rounding is 2^-8), three for fp32.
+template <class Y>
+struct Four;
+template <>
+struct Four<bf16_t> {
+    typedef uint32_t V __attribute__((ext_vector_type(2)));
+    static constexpr int S = 2;
+    static __device__ __forceinline__ V add(V base, floatx4 a) {
+        return V{pack2(__uint_as_float(base[0] << 16) + a[0],
+                       __uint_as_float(base[0] & 0xFFFF0000u) + a[1]),
+                 pack2(__uint_as_float(base[1] << 16) + a[2],
+                       __uint_as_float(base[1] & 0xFFFF0000u) + a[3])};
     }
 };
 template <>
-struct Piece<float> {
-    static constexpr int N = 4, W = 4, S = 3;
-    static __device__ __forceinline__ int column(int j, int m) { return 16 * j + m; }
-    static __device__ __forceinline__ u32x4 add(u32x4 base, const floatx4 (&v)[4], int h) {
-        return __builtin_bit_cast(u32x4, __builtin_bit_cast(floatx4, base) + v[h]);
+struct Four<float> {
+    typedef u32x4 V;
+    static constexpr int S = 3;
+    static __device__ __forceinline__ V add(V base, floatx4 a) {
+        return __builtin_bit_cast(u32x4, __builtin_bit_cast(floatx4, base) + a);
     }
 };
 
@@ -347,7 +427,7 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
     const int64_t mine = (int64_t)block * 64 + lane;
     uint64_t none = __ballot(mine < o.rows && o.place[min(mine, o.rows - 1)] < 0);
     for (int i = 0; none; ++i, none &= none - 1) {
-        if (i % kWaves != wave) continue;
+        if (i % (int)(blockDim.x >> 6) != wave) continue;
         const int64_t at = ((int64_t)block * 64 + __builtin_ctzll(none)) * k.N;
         for (int c = c0 + lane * V; c < c1; c += 64 * V) {
             u32x4 v = {};
@@ -360,137 +440,204 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
 // The contraction runs over S * rank positions: the S parts of u one behind the
 // other, against B's columns as many times.  Chunk c (8 positions) is part
 // c / (rank / 8) of u; chunks are padded to whole instructions of four.  Where
-// rank is a multiple of 32 an operand of B serves all parts.  M is the output
-// column, N the rows.  What does not depend on u (base's rows, the first operands
-// of B) is on its way before u is cut.
+// rank is a multiple of 32 an operand of B serves all parts.  M is the rows, N the
+// output columns: the j-th of four instructions has columns 4 n + j, so that a lane
+// ends with four columns of four rows, and a group's loads and stores are 64 columns
+// of a row (lanes side by side on one row: the cache takes a lane's 16 bytes of a row
+// of its own as slowly as 64 of a shared one).
+//
+// Tall tiles: the waves have a row block each and the same columns.  B
+// comes in as whole lines, by all of them, and lies in LDS as operands
+// [j][chunk][n][8], two blocks of 64 columns in turn.  Short tiles: the waves have
+// columns of their own and take B's operands from memory.
+constexpr int kPitch = 17;  // operands of a chunk and one: writes of different banks
+
 template <int RB, class Y>
 __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Expand<Y> &k,
                                        int block, char *lds) {
-    using P = Piece<Y>;
+    using P = Four<Y>;
+    using V = typename P::V;
     constexpr int S = P::S, TM = 16 * RB;
-    constexpr int WB = RB < 2 ? RB : 2, WR = RB / WB, WC = kWaves / WR;  // a wave's row blocks
+    constexpr bool SHARED = RB > 1;
+    constexpr int TH = 64 * expand_waves(RB), WC = SHARED ? 1 : kWaves;
     const int tile = block / k.ranges;
     const int c0 = block % k.ranges * k.span * 64, c1 = min(k.N, c0 + k.span * 64);
     if (tile >= k.tiles) {
         copy_rows(o, k, tile - k.tiles, c0, c1);
         return;
     }
-    const Tile t = find_tile(o, RB == 4 ? 6 : 4, tile);
+    const Tile t = find_tile(o, tile_shift_of(RB), tile);
     if (t.e < 0) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b0 = wave % WR * WB;
-    const int rc = rank / 8, chunks = (rc * S + 3) / 4 * 4;
-    const float *pt = k.u.p + (int64_t)tile * k.u.splits * rank * TM;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b0 = SHARED ? wave : 0;
+    const int rc = rank / 8, chunks = chunks_of(rank, S);
+    const bool whole = rank % 32 == 0;
+    const int steps = whole ? rc / 4 : chunks / 4;  // of B's operands
     const bf16_t *we = k.w + (int64_t)t.e * k.N * rank;
-    uint32_t wo[4];
+    int64_t at[4];
+    bool there[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) wo[j] = (uint32_t)P::column(j, m) * rank * 2;
-    const int step = 4 % rc, ch0 = g % rc;
-    int64_t at[WB];
-#pragma unroll
-    for (int b = 0; b < WB; ++b) {
-        const int i = 16 * (b0 + b) + m, row = i < t.rows ? row_at(o, t.first + i) : -1;
-        at[b] = row < 0 ? -1 : (int64_t)row * k.N + P::W * g;
+    for (int i = 0; i < 4; ++i) {  // (a place of no row: row 0's, not stored)
+        const int p = 16 * b0 + 4 * g + i, row = p < t.rows ? row_at(o, t.first + p) : -1;
+        there[i] = row >= 0;
+        at[i] = (int64_t)max(row, 0) * k.N + 4 * m;
     }
-    u32x4 old[WB][P::N];
-    bf16x8 wv[4];
-    auto load_block = [&](int c) {
+    bf16x8 *u = reinterpret_cast<bf16x8 *>(lds);
+    V old[4];
+    auto load_base = [&](V(&v)[4], int c) {
         if (k.base) {
 #pragma unroll
-            for (int b = 0; b < WB; ++b)
-#pragma unroll
-                for (int h = 0; h < P::N; ++h)  // (a place of no row: row 0's, not stored)
-                    old[b][h] = *reinterpret_cast<const u32x4 *>(
-                        k.base + max(at[b], (int64_t)(P::W * g)) + c + 4 * P::W * h);
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const V *>(k.base + at[i] + c);
         } else {
 #pragma unroll
-            for (int b = 0; b < WB; ++b)
-#pragma unroll
-                for (int h = 0; h < P::N; ++h) old[b][h] = u32x4{};
+            for (int i = 0; i < 4; ++i) v[i] = V{};
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) wv[j] = load8(we + (int64_t)c * rank, wo[j] + 16 * ch0);
     };
-    int c = c0 + wave / WR * 64;
-    if (c < c1) load_block(c);
-    // u, scaled and cut, in LDS: [row block][chunk][row][8]
-    bf16x8 *u = reinterpret_cast<bf16x8 *>(lds);
-    const float f = k.scale ? k.scale[t.e] : 1.f;
-    for (int i = threadIdx.x; i < TM * (chunks - rc * (S - 1)); i += 64 * kWaves) {
-        const int row = i % TM, kc = i / TM;
-        bf16x8 part[S] = {};
-        if (row < t.rows && kc < rc) {
-            float v[8] = {};
-            for (int q = 0; q < k.u.splits; ++q)
+    floatx4 acc[4];
+    auto clear = [&] {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += pt[((int64_t)q * rank + 8 * kc + j) * TM + row];
+        for (int j = 0; j < 4; ++j) acc[j] = floatx4{};
+    };
+    auto product = [&](const bf16x8(&wv)[4], int st) {
+        if (whole) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= f;
-            cut8<S>(v, part);
-        }
-        // chunks behind the last part's are the padding
+            for (int q = 0; q < S; ++q) {
+                const bf16x8 uv = u[(b0 * chunks + q * rc + 4 * st + g) * 16 + m];
 #pragma unroll
-        for (int q = 0; q < S; ++q)
-            if (kc < rc || q + 1 == S)
-                u[((row >> 4) * chunks + q * rc + kc) * 16 + (row & 15)] = part[q];
-    }
-    __syncthreads();
-    while (c < c1) {
-        const bf16_t *wc = we + (int64_t)c * rank;
-        floatx4 acc[WB][4] = {};
-        if (rank % 32 == 0) {
-            for (int s = 0; s < rc; s += 4) {
-                bf16x8 cur[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) cur[j] = wv[j];
-                if (s + 4 < rc) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) wv[j] = load8(wc, wo[j] + 16 * (s + 4 + g));
-                }
-#pragma unroll
-                for (int q = 0; q < S; ++q)
-#pragma unroll
-                    for (int b = 0; b < WB; ++b) {
-                        const bf16x8 uv = u[((b0 + b) * chunks + q * rc + s + g) * 16 + m];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[b][j] = mfma(cur[j], uv, acc[b][j]);
-                    }
+                for (int j = 0; j < 4; ++j) acc[j] = mfma(uv, wv[j], acc[j]);
             }
         } else {
-            int ch = ch0;
-            for (int s = 0; s < chunks; s += 4) {
-                bf16x8 cur[4];
+            const bool pad = 4 * st + g >= rc * S;  // zeros against u's zeros: B may hold inf
+            const bf16x8 uv = u[(b0 * chunks + 4 * st + g) * 16 + m];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) cur[j] = s + g < rc * S ? wv[j] : bf16x8{};
-                ch += step;
-                if (ch >= rc) ch -= rc;
-                if (s + 4 < chunks) {
+            for (int j = 0; j < 4; ++j) acc[j] = mfma(uv, pad ? bf16x8{} : wv[j], acc[j]);
+        }
+    };
+    auto store = [&](const V(&v)[4], int c) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) wv[j] = load8(wc, wo[j] + 16 * ch);
+        for (int i = 0; i < 4; ++i)
+            if (there[i])
+                *reinterpret_cast<V *>(k.y + at[i] + c) =
+                    P::add(v[i], floatx4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]});
+    };
+    auto chunk_of = [&](int st) { return whole ? 4 * st + g : (4 * st + g) % rc; };
+
+    if constexpr (SHARED) {
+        bf16x8 *wl = u + RB * chunks * 16;  // two blocks of B
+        const int size = 4 * rc * kPitch, items = 64 * rc;
+        auto run = [&](auto its) {
+            constexpr int IT = its();
+            bf16x8 w[IT];
+            int from[IT], to[IT];  // a thread's operands of 64 columns, as they lie
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int i = min((int)threadIdx.x + TH * it, items - 1), col = i / rc;
+                from[it] = 8 * i;
+                to[it] = ((col & 3) * rc + i % rc) * kPitch + (col >> 2);
+            }
+            auto load_w = [&](int c) {
+#pragma unroll
+                for (int it = 0; it < IT; ++it) w[it] = load8(we + (int64_t)c * rank + from[it]);
+            };
+            auto write_w = [&](bf16x8 *p) {  // (behind the last: the last again)
+#pragma unroll
+                for (int it = 0; it < IT; ++it) p[to[it]] = w[it];
+            };
+            auto block_product = [&](const bf16x8 *from) {
+                clear();
+                for (int st = 0; st < steps; ++st) {
+                    const int ch = chunk_of(st);
+                    bf16x8 wv[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) wv[j] = from[(j * rc + ch) * kPitch + m];
+                    product(wv, st);
                 }
+            };
+            load_base(old, c0);
+            load_w(c0);
+            const bf16x8 *src =
+                reinterpret_cast<const bf16x8 *>(k.u.e) + (int64_t)tile * chunks * TM;
+            for (int i = threadIdx.x; i < chunks * TM; i += TH) u[i] = src[i];
+            write_w(wl);
+            __syncthreads();
+            int c = c0, buf = 0;
+            // The next block's loads are on their way while this one's products run.
+            for (; c + 64 < c1; c += 64, buf ^= 1) {
+                V then[4];
+                load_base(then, c + 64);
+                load_w(c + 64);
+                block_product(wl + buf * size);
+                store(old, c);
+                write_w(wl + (buf ^ 1) * size);
+                __syncthreads();
 #pragma unroll
-                for (int b = 0; b < WB; ++b) {
-                    const bf16x8 uv = u[((b0 + b) * chunks + s + g) * 16 + m];
+                for (int i = 0; i < 4; ++i) old[i] = then[i];
+            }
+            block_product(wl + buf * size);
+            store(old, c);
+        };
+        if (items <= TH)
+            run(std::integral_constant<int, 1>());
+        else if (items <= 2 * TH)
+            run(std::integral_constant<int, 2>());
+        else
+            run(std::integral_constant<int, 4>());
+    } else {
+        int c = c0 + wave * 64;
+        bf16x8 first[4];
+        auto load_w = [&](bf16x8(&wv)[4], int c, int st) {
+            const int ch = chunk_of(st);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[b][j] = mfma(cur[j], uv, acc[b][j]);
-                }
+            for (int j = 0; j < 4; ++j)
+                wv[j] = load8(we + (int64_t)(c + j) * rank, (uint32_t)(4 * m * rank + 8 * ch) * 2);
+        };
+        // what does not depend on u is on its way before it is cut
+        if (c < c1) {
+            load_base(old, c);
+            load_w(first, c, 0);
+        }
+        // u, scaled and cut, in LDS: [chunk][row][8]
+        const float f = k.scale ? k.scale[t.e] : 1.f;
+        const float *pt = k.u.p + (int64_t)tile * k.u.splits * rank * TM;
+        for (int i = threadIdx.x; i < TM * (chunks - rc * (S - 1)); i += TH) {
+            const int row = i % TM, kc = i / TM;
+            bf16x8 part[S] = {};
+            if (row < t.rows && kc < rc) {
+                float v[8] = {};
+                for (int q = 0; q < k.u.splits; ++q)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        v[j] += pt[((int64_t)q * rank + 8 * kc + j) * TM + row];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= f;
+                cut8<S>(v, part);
+            }
+            // chunks behind the last part's are the padding
+#pragma unroll
+            for (int q = 0; q < S; ++q)
+                if (kc < rc || q + 1 == S) u[(q * rc + kc) * 16 + row] = part[q];
+        }
+        __syncthreads();
+        while (c < c1) {
+            clear();
+            product(first, 0);
+            for (int st = 1; st < steps; ++st) {
+                bf16x8 wv[4];
+                load_w(wv, c, st);
+                product(wv, st);
+            }
+            store(old, c);
+            c += WC * 64;
+            if (c < c1) {
+                load_base(old, c);
+                load_w(first, c, 0);
             }
         }
-#pragma unroll
-        for (int b = 0; b < WB; ++b)
-            if (at[b] >= 0) {
-#pragma unroll
-                for (int h = 0; h < P::N; ++h)
-                    *reinterpret_cast<u32x4 *>(k.y + at[b] + c + 4 * P::W * h) =
-                        P::add(old[b][h], acc[b], h);
-            }
-        c += WC * 64;
-        if (c < c1) load_block(c);
     }
 }
 
 template <int RB, class Y>
-__global__ __launch_bounds__(64 * kWaves) void expand_kernel(AdapterRows o, int rank,
+__global__ __launch_bounds__(64 * expand_waves(RB), 4) void expand_kernel(AdapterRows o, int rank,
                                                              Expand<Y> k) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     expand<RB, Y>(o, rank, k, blockIdx.x, lds);
@@ -520,7 +667,7 @@ struct Outer {
     AdapterSums p;
     const bf16_t *q;
     float *parts, *out;
-    int C, transposed, cb, blocks;  // cb: blocks of 128 columns
+    int C, transposed, cb, blocks;  // cb: blocks of 512 columns
 };
 
 // Tiles of 2^sh rows before adapter e.
@@ -533,150 +680,155 @@ __device__ __forceinline__ int tiles_before(const AdapterRows &o, int sh, int e)
 
 // The contraction runs over rows, 32 an instruction.  A lane loads 8 rows x 8
 // columns of q and turns them in registers: the operands of eight instructions,
-// the j-th of which has column 8 (lane % 16) + j.  M is the rank.  The waves take
-// steps of 32 rows in turn and join in LDS.  p in three parts: the sums are as
-// exact as fp32's.
+// the j-th of which has column 8 (lane % 16) + j.  M is the rank.  Four waves stand
+// side by side, 128 columns each, and read the same of p; two such rows of waves take
+// steps of 32 rows in turn and join in LDS.  p in three parts: the sums are as exact
+// as fp32's.
 template <int RB, int NR>
 __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const float *scale, int sh,
                                       int slots, bool accumulate, const Outer &k, int block,
                                       char *lds) {
-    constexpr int TSH = RB == 4 ? 6 : 4, TM = 16 * RB;
-    floatx4(*sums)[NR * 8][64] = reinterpret_cast<floatx4(*)[NR * 8][64]>(lds);
+    constexpr int TSH = tile_shift_of(RB), TM = 16 * RB, KR = kOuterWaves / 4;
+    floatx4 *sums = reinterpret_cast<floatx4 *>(lds);
     int *rows = reinterpret_cast<int *>(lds);  // before the sums
     const Tile t = find_tile(o, sh, block / k.cb);
     if (t.e < 0 || (t.tiles > 1 && t.several + t.index >= slots)) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = block % k.cb * 128 + 8 * m, qc = min(col, k.C - 8);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cw = wave % 4, rw = wave / 4;
+    const int col = (block % k.cb * 4 + cw) * 128 + 8 * m, qc = min(col, k.C - 8);
     const int groups = (rank + 16 * NR - 1) / (16 * NR);
-    for (int i = threadIdx.x; i < t.rows; i += 64 * kWaves) rows[i] = max(row_at(o, t.first + i), 0);
     const int64_t pt = tiles_before(o, TSH, t.e) + ((int64_t)t.index << (sh - TSH));
     // (offsets out of order may count more tiles than there are sums of)
     if (pt + ((t.rows + TM - 1) >> TSH) > (o.rows >> TSH) + min((int64_t)o.count, o.rows)) return;
     const float f = scale ? scale[t.e] : 1.f;
-    __syncthreads();
     const bf16_t *qr = k.q + qc;
     for (int grp = 0; grp < groups; ++grp) {
         const int r0 = grp * 16 * NR;
+        for (int i = threadIdx.x; i < t.rows; i += 64 * kOuterWaves)
+            rows[i] = max(row_at(o, t.first + i), 0);
+        __syncthreads();
         floatx4 acc[NR][8] = {};
         u32x4 raw[8];
-        floatx4 pv[NR][2];
-        auto load = [&](int k0) {
+        auto load_q = [&](int k0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int64_t row = rows[min(k0 + 8 * g + i, t.rows - 1)];
                 raw[i] = *reinterpret_cast<const u32x4 *>(qr + row * k.C);
             }
-            // (rows behind the last: of no tile's, cut off below)
+        };
+        constexpr bool AHEAD = NR < 4;  // (registers for two steps' rows)
+        if (AHEAD && 32 * rw < t.rows) load_q(32 * rw);
+        for (int k0 = 32 * rw; k0 < t.rows; k0 += 32 * KR) {
+            if (!AHEAD) load_q(k0);
+            // p of 8 rows, in parts; behind the last row zeros
             const int at = min(k0 + 8 * g, (t.rows - 1) & ~7);
-            const float *src =
-                k.p.p + ((pt + (at >> TSH)) * k.p.splits * rank + r0) * TM + (at & (TM - 1));
+            const int64_t tile = pt + (at >> TSH);
+            floatx4 pv[NR][RB == 1 ? 2 : 3];
 #pragma unroll
             for (int b = 0; b < NR; ++b) {
                 // (a rank value behind the last: another's, not stored)
-                const int r = min(16 * b + m, rank - 1 - r0);
-                pv[b][0] = pv[b][1] = floatx4{};
-                for (int s = 0; s < k.p.splits; ++s)
+                const int r = min(r0 + 16 * b + m, rank - 1);
+                if constexpr (RB == 1) {
+                    const float *src =
+                        k.p.p + (tile * k.p.splits * rank + r) * TM + (at & (TM - 1));
+                    pv[b][0] = pv[b][1] = floatx4{};
+                    for (int s = 0; s < k.p.splits; ++s)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        pv[b][h] += *reinterpret_cast<const floatx4 *>(
-                            src + ((int64_t)s * rank + r) * TM + 4 * h);
+                        for (int h = 0; h < 2; ++h)
+                            pv[b][h] += *reinterpret_cast<const floatx4 *>(
+                                src + (int64_t)s * rank * TM + 4 * h);
+                } else {
+                    const bf16_t *src = k.p.q + (tile * 3 * rank + r) * TM + (at & (TM - 1));
+#pragma unroll
+                    for (int s = 0; s < 3; ++s)
+                        pv[b][s] = *reinterpret_cast<const floatx4 *>(src + s * rank * TM);
+                }
             }
-        };
-        if (32 * wave < t.rows) load(32 * wave);
-        for (int k0 = 32 * wave; k0 < t.rows; k0 += 32 * kWaves) {
-            bf16x8 qv[8], part[NR][3];
+            bf16x8 qv[8];
             transpose8(raw, qv);
+            if (AHEAD && k0 + 32 * KR < t.rows) load_q(k0 + 32 * KR);
+            const bool tail = k0 + 32 > t.rows;
 #pragma unroll
             for (int b = 0; b < NR; ++b) {
-                float v[8];
+                bf16x8 part[3];
+                if constexpr (RB == 1) {
+                    float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    v[i] = k0 + 8 * g + i < t.rows ? pv[b][i / 4][i % 4] * f : 0.f;
-                cut8<3>(v, part[b]);
-            }
-            if (k0 + 32 * kWaves < t.rows) load(k0 + 32 * kWaves);
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = k0 + 8 * g + i < t.rows ? pv[b][i / 4][i % 4] * f : 0.f;
+                    cut8<3>(v, part);
+                } else {
+                    // (a tile's rows behind its last are zeros; eights behind that: no tile's)
 #pragma unroll
-            for (int b = 0; b < NR; ++b)
+                    for (int s = 0; s < 3; ++s) part[s] = __builtin_bit_cast(bf16x8, pv[b][s]);
+                    if (tail) {
+#pragma unroll
+                        for (int s = 0; s < 3; ++s)
+                            if (k0 + 8 * g >= t.rows) part[s] = bf16x8{};
+                    }
+                }
 #pragma unroll
                 for (int s = 0; s < 3; ++s)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[b][j] = mfma(part[b][s], qv[j], acc[b][j]);
+                    for (int j = 0; j < 8; ++j) acc[b][j] = mfma(part[s], qv[j], acc[b][j]);
+            }
         }
-        // (rows are read again for another group of rank values: kept behind the sums)
-        __syncthreads();
-        if (wave >= 2) {
+        __syncthreads();  // the rows' list has been read
+        floatx4 *mine = sums + cw * NR * 8 * 64 + lane;
+        if (rw == 1) {
 #pragma unroll
             for (int b = 0; b < NR; ++b)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sums[wave - 2][b * 8 + j][lane] = acc[b][j];
+                for (int j = 0; j < 8; ++j) mine[(b * 8 + j) * 64] = acc[b][j];
         }
         __syncthreads();
-        if (wave < 2) {
+        if (rw == 0 && col < k.C) {
 #pragma unroll
             for (int b = 0; b < NR; ++b)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sums[wave][b * 8 + j][lane] += acc[b][j];
-        }
-        __syncthreads();
-        const bool whole = t.tiles == 1, add = whole && accumulate;
-        float *to = whole ? k.out + (int64_t)t.e * rank * k.C
-                          : k.parts + (int64_t)(t.several + t.index) * rank * k.C;
-        if (col < k.C && k.transposed) {
-            // four rank values of a column: wave w has columns j = w, w + 4
-#pragma unroll
-            for (int b = 0; b < NR; ++b)
-#pragma unroll
-                for (int j = 0; j < 8; j += kWaves) {
-                    const int r = r0 + 16 * b + 4 * g;
-                    if (r >= rank) continue;
-                    const floatx4 v =
-                        sums[0][b * 8 + j + wave][lane] + sums[1][b * 8 + j + wave][lane];
-                    floatx4 *d =
-                        reinterpret_cast<floatx4 *>(to + (int64_t)(col + j + wave) * rank + r);
-                    *d = add ? *d + v : v;
-                }
-        } else if (col < k.C) {
-            // eight columns of a rank value: wave w has the w-th of a lane's four
-            const float *s0 = reinterpret_cast<const float *>(sums[0]) + lane * 4 + wave;
-            const float *s1 = reinterpret_cast<const float *>(sums[1]) + lane * 4 + wave;
+                for (int j = 0; j < 8; ++j) acc[b][j] += mine[(b * 8 + j) * 64];
+            const bool whole = t.tiles == 1, add = whole && accumulate;
+            float *to = whole ? k.out + (int64_t)t.e * rank * k.C
+                              : k.parts + (int64_t)(t.several + t.index) * rank * k.C;
 #pragma unroll
             for (int b = 0; b < NR; ++b) {
-                const int r = r0 + 16 * b + 4 * g + wave;
+                const int r = r0 + 16 * b + 4 * g;
                 if (r >= rank) continue;
+                if (k.transposed) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    floatx4 v;
+                    for (int j = 0; j < 8; ++j) {
+                        floatx4 *d =
+                            reinterpret_cast<floatx4 *>(to + (int64_t)(col + j) * rank + r);
+                        *d = add ? *d + acc[b][j] : acc[b][j];
+                    }
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        v[j] = s0[(b * 8 + 4 * h + j) * 256] + s1[(b * 8 + 4 * h + j) * 256];
-                    floatx4 *d = reinterpret_cast<floatx4 *>(to + (int64_t)r * k.C + col + 4 * h);
-                    *d = add ? *d + v : v;
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const floatx4 v = {acc[b][4 * h][i], acc[b][4 * h + 1][i],
+                                               acc[b][4 * h + 2][i], acc[b][4 * h + 3][i]};
+                            floatx4 *d = reinterpret_cast<floatx4 *>(
+                                to + (int64_t)(r + i) * k.C + col + 4 * h);
+                            *d = add ? *d + v : v;
+                        }
                 }
             }
         }
-        if (grp + 1 < groups) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < t.rows; i += 64 * kWaves)
-                rows[i] = max(row_at(o, t.first + i), 0);
-            __syncthreads();
-        }
+        __syncthreads();
     }
 }
 
-// The gradient's last products, one launch: blocks of db, of da, of dx.
-template <int RB, int NR, class Y>
-__global__ __launch_bounds__(64 * kWaves) void back_kernel(AdapterRows o, int rank,
-                                                           const float *scale, int sh, int slots,
-                                                           int accumulate, Outer kb, Outer ka,
-                                                           Expand<Y> kx) {
+// The gradient's products behind u and v: blocks of db, then of da.
+template <int RB, int NR>
+__global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(AdapterRows o, int rank,
+                                                                 const float *scale, int sh,
+                                                                 int slots, int accumulate,
+                                                                 Outer kb, Outer ka) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int b = blockIdx.x;
-    if (b < kb.blocks + ka.blocks)
-        outer<RB, NR>(o, rank, scale, sh, slots, accumulate, b < kb.blocks ? kb : ka,
-                      b < kb.blocks ? b : b - kb.blocks, lds);
-    else
-        expand<RB, Y>(o, rank, kx, b - kb.blocks - ka.blocks, lds);
+    const int b = blockIdx.x;
+    outer<RB, NR>(o, rank, scale, sh, slots, accumulate, b < kb.blocks ? kb : ka,
+                  b < kb.blocks ? b : b - kb.blocks, lds);
 }
 
 // Adapters of several tiles: their parts, added in order; adapters of no rows:
@@ -716,55 +868,56 @@ __global__ __launch_bounds__(256) void join_kernel(AdapterRows o, int sh, int sl
 int64_t tile_cap(int64_t rows, int count, int sh) {
     return (rows >> sh) + std::min<int64_t>(count, rows);
 }
-// Tiles of 64 rows, where they are many and the adapters' mean rows fill most of one.
-bool tall(int64_t rows, int count) { return rows >= 4096 && rows >= (int64_t)48 * count; }
-int tile_shift(int64_t rows, int count) { return tall(rows, count) ? 6 : 4; }
+// Row blocks of a tile.  Tall ones read the adapters' matrices less often; they are
+// for many rows, where the adapters' mean rows fill most of one.  u's parts of a tile
+// have to fit LDS.
+int row_blocks(int64_t rows, int count, int rank) {
+    if (rank > 128 || rows < 4096 || rows < (int64_t)48 * count) return 1;
+    return rows >= 8192 && rows >= (int64_t)96 * count ? 8 : 4;
+}
+int64_t tile_count(const AdapterRows &o, int rank) {
+    return tile_cap(o.rows, o.count, tile_shift_of(row_blocks(o.rows, o.count, rank)));
+}
 // Rows of a tile of the outer products, as a power of two: about 16 tiles, which with
-// some 60 column blocks fill the chip.
+// some 16 column blocks fill the chip.
 int outer_shift(int64_t rows) { return rows >= 4096 ? 9 : rows >= 2048 ? 8 : 7; }
 int64_t outer_slots(int64_t rows) { return 2 * (rows >> outer_shift(rows)) + 2; }
 
-template <int RB, int NR>
-hipError_t run_shrink(const AdapterRows &o, int rank, const Shrink &k, const Transpose &ta,
-                      const Transpose &tb, hipStream_t s) {
-    const unsigned groups = (rank + 16 * NR - 1) / (16 * NR);
-    const unsigned grid = (unsigned)k.tiles * k.out.splits * groups + ta.blocks + tb.blocks;
-    shrink_kernel<RB, NR><<<grid, 64 * kShrinkWaves, 0, s>>>(o, rank, k, ta, tb);
-    return hipGetLastError();
+template <int N>
+using Int = std::integral_constant<int, N>;
+// fn(row blocks of a tile, rank blocks of a wave) of this size.
+template <class F>
+hipError_t by_size(const AdapterRows &o, int rank, F fn) {
+    auto go = [&](auto rb) {
+        return rank <= 16 ? fn(rb, Int<1>()) : rank <= 32 ? fn(rb, Int<2>()) : fn(rb, Int<4>());
+    };
+    switch (row_blocks(o.rows, o.count, rank)) {
+        case 8: return go(Int<8>());
+        case 4: return go(Int<4>());
+        default: return go(Int<1>());
+    }
 }
 
 hipError_t launch_shrink(const AdapterRows &o, int rank, int K, const bf16_t *x, const bf16_t *w,
                          const AdapterSums &out, const Transpose &ta, const Transpose &tb,
                          hipStream_t s) {
-    const Shrink k{x, w, out, K,
-                   x ? (int)tile_cap(o.rows, o.count, tile_shift(o.rows, o.count)) : 0};
-    auto go = [&](auto fn) { return fn(o, rank, k, ta, tb, s); };
-    if (tall(o.rows, o.count))
-        return rank <= 16 ? go(run_shrink<4, 1>)
-                          : rank <= 32 ? go(run_shrink<4, 2>) : go(run_shrink<4, 4>);
-    return rank <= 16 ? go(run_shrink<1, 1>)
-                      : rank <= 32 ? go(run_shrink<1, 2>) : go(run_shrink<1, 4>);
+    const Shrink k{x, w, out, K, x ? (int)tile_count(o, rank) : 0};
+    return by_size(o, rank, [&](auto rb, auto nr) {
+        const unsigned groups = (rank + 16 * nr() - 1) / (16 * nr());
+        const unsigned grid = (unsigned)k.tiles * out.splits * groups + ta.blocks + tb.blocks;
+        shrink_kernel<rb(), nr()><<<grid, 64 * shrink_waves(rb()), 0, s>>>(o, rank, k, ta, tb);
+        return hipGetLastError();
+    });
 }
 
-template <class Y>
-Expand<Y> make_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u, const bf16_t *w,
-                      const float *scale, const void *base, void *y) {
-    Expand<Y> k{u, w, scale, (const Y *)base, (Y *)y, N, 0, 0, 0, 0};
-    if (!y) return k;
-    k.tiles = (int)tile_cap(o.rows, o.count, tile_shift(o.rows, o.count));
-    k.copies = base == y ? 0 : (int)((o.rows + 63) / 64);
-    // a block a wave; larger ranks take u's cutting further
-    k.span = kWaves * (rank <= 64 ? 1 : rank <= 128 ? 2 : 4);
-    k.ranges = (N / 64 + k.span - 1) / k.span;
-    return k;
-}
-template <class Y>
-size_t expand_lds(int64_t rows, int count, int rank) {
-    return (size_t)(tall(rows, count) ? 4 : 1) * ((rank / 8 * Piece<Y>::S + 3) / 4 * 4) * 256;
-}
-template <class Y>
-int64_t expand_blocks(const Expand<Y> &k) {
-    return (int64_t)(k.tiles + k.copies) * k.ranges;
+// Of tall tiles only.
+hipError_t launch_cut(const AdapterRows &o, int rank, const float *scale, const Cut &a,
+                      const Cut &b, bool both, hipStream_t s) {
+    const int rb = row_blocks(o.rows, o.count, rank), tiles = (int)tile_count(o, rank);
+    if (rb == 1) return hipSuccess;
+    const auto fn = rb == 8 ? cut_kernel<8> : cut_kernel<4>;
+    fn<<<(unsigned)tiles * (both ? 2 : 1), 512, 0, s>>>(o, rank, scale, a, b, tiles);
+    return hipGetLastError();
 }
 
 // More than 64 KB of LDS are asked for.
@@ -775,63 +928,106 @@ hipError_t allow_lds(const void *fn, size_t lds) {
 }
 
 template <class Y>
-hipError_t run_expand(const AdapterRows &o, int rank, const Expand<Y> &k, hipStream_t s) {
-    const size_t lds = expand_lds<Y>(o.rows, o.count, rank);
-    const unsigned grid = (unsigned)expand_blocks(k);
-    const auto fn = tall(o.rows, o.count) ? expand_kernel<4, Y> : expand_kernel<1, Y>;
+hipError_t launch_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u,
+                         const bf16_t *w, const float *scale, const void *base, void *y,
+                         hipStream_t s) {
+    Expand<Y> k{u, w, scale, (const Y *)base, (Y *)y, N, 0, 0, 0, 0};
+    const int rb = row_blocks(o.rows, o.count, rank);
+    k.tiles = (int)tile_count(o, rank);
+    k.copies = base == y ? 0 : (int)((o.rows + 63) / 64);
+    // a block a wave; larger ranks take u's cutting, tall tiles its parts further
+    k.span = rb > 1 ? kExpandSpan : kWaves * (rank <= 64 ? 1 : rank <= 128 ? 2 : 4);
+    k.ranges = (N / 64 + k.span - 1) / k.span;
+    size_t lds = (size_t)rb * ((rank / 8 * Four<Y>::S + 3) / 4 * 4) * 256;
+    if (rb > 1) lds += (size_t)2 * 4 * (rank / 8) * kPitch * 16;  // B's two blocks
+    const auto fn = rb == 8   ? expand_kernel<8, Y>
+                    : rb == 4 ? expand_kernel<4, Y>
+                              : expand_kernel<1, Y>;
     if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
-    fn<<<grid, 64 * kWaves, lds, s>>>(o, rank, k);
+    fn<<<(unsigned)((int64_t)(k.tiles + k.copies) * k.ranges), 64 * expand_waves(rb), lds, s>>>(
+        o, rank, k);
+    return hipGetLastError();
+}
+hipError_t launch_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u,
+                         const bf16_t *w, const float *scale, const void *base, void *y, int type,
+                         hipStream_t s) {
+    return type == MOE_FP32 ? launch_expand<float>(o, rank, N, u, w, scale, base, y, s)
+                            : launch_expand<bf16_t>(o, rank, N, u, w, scale, base, y, s);
+}
+
+hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool accumulate,
+                        Outer kb, Outer ka, hipStream_t s) {
+    const int sh = outer_shift(o.rows), slots = (int)outer_slots(o.rows);
+    if (o.rows) {
+        const int tiles = (int)tile_cap(o.rows, o.count, sh);
+        ka.blocks = tiles * ka.cb;
+        kb.blocks = tiles * kb.cb;
+        const hipError_t e = by_size(o, rank, [&](auto rb, auto nr) {
+            const auto fn = outer_kernel<rb(), nr()>;
+            const size_t lds = (size_t)4 * nr() * 8 * 64 * sizeof(floatx4);
+            if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
+            fn<<<(unsigned)(ka.blocks + kb.blocks), 64 * kOuterWaves, lds, s>>>(
+                o, rank, scale, sh, slots, accumulate, kb, ka);
+            return hipGetLastError();
+        });
+        if (e) return e;
+    }
+    const int64_t size = (int64_t)rank * std::max(ka.C, kb.C);
+    const unsigned bx = (unsigned)std::min<int64_t>((size + 1023) / 1024, 64);
+    join_kernel<<<dim3(bx, o.count, 2), 256, 0, s>>>(o, sh, slots, accumulate, ka, kb, rank);
     return hipGetLastError();
 }
 
-template <int RB, int NR, class Y>
-hipError_t run_back(const AdapterRows &o, int rank, const float *scale, bool accumulate,
-                    const Outer &kb, const Outer &ka, const Expand<Y> &kx, hipStream_t s) {
-    const int sh = outer_shift(o.rows);
-    size_t lds = kx.y ? expand_lds<Y>(o.rows, o.count, rank) : 0;
-    if (ka.blocks) lds = std::max(lds, (size_t)(kWaves / 2) * NR * 8 * 64 * sizeof(floatx4));
-    const unsigned grid = (unsigned)(kb.blocks + ka.blocks + expand_blocks(kx));
-    const auto fn = back_kernel<RB, NR, Y>;
-    if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
-    fn<<<grid, 64 * kWaves, lds, s>>>(o, rank, scale, sh, (int)outer_slots(o.rows), accumulate, kb,
-                                      ka, kx);
-    return hipGetLastError();
+// Shares of K that the sums of these rows are cut into: workgroups for every compute
+// unit at once, a step of 64 k for every wave.
+int splits_of(int64_t rows, int count, int K, int rank) {
+    const int rb = row_blocks(rows, count, rank);
+    const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift_of(rb)), 1);
+    const int64_t want = rb > 1 ? 512 / tiles : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
+    const int64_t most = std::max(1, K / 64 / (rb == 8 ? 2 : shrink_waves(rb)));
+    return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)(rb > 1 ? 8 : 16)}));
 }
 
-template <class Y>
-hipError_t launch_back(const AdapterRows &o, int rank, const float *scale, bool accumulate,
-                       const Outer &kb, const Outer &ka, const Expand<Y> &kx, hipStream_t s) {
-    auto go = [&](auto fn) { return fn(o, rank, scale, accumulate, kb, ka, kx, s); };
-    if (tall(o.rows, o.count))
-        return rank <= 16 ? go(run_back<4, 1, Y>)
-                          : rank <= 32 ? go(run_back<4, 2, Y>) : go(run_back<4, 4, Y>);
-    return rank <= 16 ? go(run_back<1, 1, Y>)
-                      : rank <= 32 ? go(run_back<1, 2, Y>) : go(run_back<1, 4, Y>);
+size_t up(size_t v) { return (v + 255) & ~size_t(255); }
+
+// Bytes of a shrink's sums and their parts (e, q), for these rows.
+struct SumsSize {
+    size_t p, e, q;
+};
+SumsSize sums_size(int64_t rows, int count, int rank) {
+    const int rb = row_blocks(rows, count, rank), sh = tile_shift_of(rb);
+    const int64_t tiles = tile_cap(rows, count, sh);
+    // no more than splits * tiles of any K
+    const int64_t sums = std::max(tiles, rb == 1 ? std::min<int64_t>(16 * tiles, 1024)
+                                                       : std::min<int64_t>(8 * tiles, 512));
+    SumsSize z{up((size_t)sums * rank * sizeof(float) << sh), 0, 0};
+    if (rb > 1) {
+        z.e = up((size_t)tiles * ((rank / 8 * 3 + 3) / 4 * 4) * 16 << sh);
+        z.q = up((size_t)tiles * 3 * rank * sizeof(bf16_t) << sh);
+    }
+    return z;
 }
 
 }  // namespace
 
-int adapter_splits(int64_t rows, int count, int K, int rank) {
-    // workgroups for every compute unit; a step of 64 k for every wave
-    const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift(rows, count)), 1);
-    const int64_t want = tall(rows, count) ? 1024 : 512;
-    const int64_t most = std::min(std::max(1, K / 64 / kShrinkWaves),
-                                  tall(rows, count) ? rank <= 32 ? 4 : 2 : 16);
-    return (int)std::max<int64_t>(1, std::min((want + tiles - 1) / tiles, most));
-}
-
 size_t adapter_sums_bytes(int64_t rows, int count, int rank) {
     auto bytes = [&](int64_t r) {
-        const int sh = tile_shift(r, count);
-        const int64_t tiles = tile_cap(r, count, sh);
-        // no more than splits * tiles of these rows or fewer
-        const int64_t sums = tall(r, count) ? std::max(tiles, std::min<int64_t>(4 * tiles, 2048))
-                                            : std::max(tiles, std::min<int64_t>(16 * tiles, 1024));
-        return (size_t)sums * rank * sizeof(float) << sh;
+        const SumsSize z = sums_size(r, count, rank);
+        return z.p + z.e + z.q;
     };
-    // (the tiles' height changes at one number of rows)
-    const int64_t edge = std::max<int64_t>(4096, (int64_t)48 * count);
-    return rows >= edge ? std::max(bytes(rows), bytes(edge - 1)) : bytes(rows);
+    size_t most = bytes(rows);
+    // (the last rows of each tile height)
+    for (int64_t edge : {std::max<int64_t>(4096, (int64_t)48 * count),
+                         std::max<int64_t>(8192, (int64_t)96 * count)})
+        if (rows >= edge) most = std::max(most, bytes(edge - 1));
+    return most;
+}
+
+AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, void *at) {
+    const SumsSize z = sums_size(rows, count, rank);
+    char *p = (char *)at;
+    return {(float *)p, splits_of(rows, count, K, rank), (bf16_t *)(p + z.p),
+            (bf16_t *)(p + z.p + z.e)};
 }
 
 size_t adapter_parts_bytes(int64_t rows, int rank, int C) {
@@ -846,22 +1042,13 @@ hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, con
                                hipStream_t s) {
     const Transpose none{};
     if (hipError_t e = launch_shrink(o, ad.rank, ad.k, x, ad.a, u, none, none, s)) return e;
-    if (y_type == MOE_FP32)
-        return run_expand(
-            o, ad.rank, make_expand<float>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y), s);
-    return run_expand(o, ad.rank,
-                      make_expand<bf16_t>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y), s);
+    const Cut cu{u, y_type == MOE_FP32 ? 3 : 2, false};
+    if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cu, cu, false, s)) return e;
+    return launch_expand(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y, y_type, s);
 }
 
 hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
                                    const AdapterBack &k, hipStream_t s) {
-    const int tiles = o.rows ? (int)tile_cap(o.rows, o.count, outer_shift(o.rows)) : 0;
-    Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 127) / 128, 0};
-    Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 127) / 128, 0};
-    if (k.da) {
-        ka.blocks = tiles * ka.cb;
-        kb.blocks = tiles * kb.cb;
-    }
     if (o.rows) {
         auto turn = [&](const bf16_t *w, bf16_t *wt, int m, int n) {
             const int bx = (n + 63) / 64;
@@ -876,25 +1063,18 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
         if (hipError_t e = launch_shrink(o, ad.rank, ad.n, k.dy, k.bt, k.v, Transpose{},
                                          Transpose{}, s))
             return e;
-        if (k.dx_type == MOE_FP32) {
-            const auto kx =
-                make_expand<float>(o, ad.rank, ad.k, k.v, k.at, ad.scale, k.base, k.dx);
-            if (hipError_t e = launch_back(o, ad.rank, ad.scale, k.accumulate, kb, ka, kx, s))
+        const Cut cv{k.v, !k.dx ? 0 : k.dx_type == MOE_FP32 ? 3 : 2, k.da != nullptr};
+        const Cut cu{k.u, 0, true};
+        if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cv, cu, k.da != nullptr, s)) return e;
+        if (k.dx)
+            if (hipError_t e = launch_expand(o, ad.rank, ad.k, k.v, k.at, ad.scale, k.base, k.dx,
+                                             k.dx_type, s))
                 return e;
-        } else {
-            const auto kx =
-                make_expand<bf16_t>(o, ad.rank, ad.k, k.v, k.at, ad.scale, k.base, k.dx);
-            if (hipError_t e = launch_back(o, ad.rank, ad.scale, k.accumulate, kb, ka, kx, s))
-                return e;
-        }
     }
     if (!k.da) return hipSuccess;
-    const int64_t size = (int64_t)ad.rank * std::max(ad.n, ad.k);
-    const unsigned bx = (unsigned)std::min<int64_t>((size + 1023) / 1024, 64);
-    join_kernel<<<dim3(bx, o.count, 2), 256, 0, s>>>(o, outer_shift(o.rows),
-                                                     (int)outer_slots(o.rows), k.accumulate, ka, kb,
-                                                     ad.rank);
-    return hipGetLastError();
+    const Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 511) / 512, 0};
+    const Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 511) / 512, 0};
+    return launch_outer(o, ad.rank, ad.scale, k.accumulate, kb, ka, s);
 }
 
 }  // namespace moe
