@@ -25,8 +25,9 @@ constexpr int kOuterWaves = 8;  // of outer: four column blocks, two halves of t
 
 // Row blocks of 16 of a tile -> rows of it, as a power of two.
 constexpr int tile_shift_of(int RB) { return RB == 8 ? 7 : RB == 4 ? 6 : 4; }
-// The waves of shrink: they share K, and the rows of the tallest tiles.
-constexpr int shrink_waves(int RB) { return 4; }
+// The waves of shrink.
+constexpr int shrink_waves(int RB) { return RB == 1 ? 4 : RB; }
+constexpr int kPitch = 17;  // operands of 16 rows and one: writes of different banks
 
 __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -99,55 +100,40 @@ __device__ __forceinline__ int row_at(const AdapterRows &o, int64_t place) {
 // ---- x A^T ---------------------------------------------------------------
 
 // Sums of `rows` times w [count][rank][K].  The matrix instruction's M is the
-// rows, its N the rank.  A wave has at most four row blocks; the waves with the same
-// ones (and `splits` workgroups) share K, each taking every so many-th 128 bytes of a
-// row, and keep DEP steps of them in flight.
+// rows, its N the rank.
 struct Shrink {
     const bf16_t *x, *w;
     AdapterSums out;
     int K, tiles;
 };
 
-template <int RB, int NR>
-struct ShrinkCfg {
-    static constexpr int W = shrink_waves(RB), PB = RB < 4 ? RB : 4, RG = RB / PB, KG = W / RG;
-    static constexpr int DEP = PB + NR <= 3 ? 4 : PB + NR <= 5 && NR < 4 ? 3 : 2;
-};
-
-template <int RB, int NR>
-__device__ __forceinline__ void shrink(const AdapterRows &o, int rank, const Shrink &k, int tile,
-                                       int split, int r0, floatx4 *lds) {
-    using C = ShrinkCfg<RB, NR>;
-    constexpr int DEP = C::DEP, TM = 16 * RB, PB = C::PB;
-    const Tile t = find_tile(o, tile_shift_of(RB), tile);
+// Short tiles: operands straight to registers, 64 bytes of each of 16 rows a load.
+// The four waves (and `splits` workgroups) share K, each taking every so many-th 128
+// bytes of a row, and keep DEP steps of them in flight.
+template <int NR>
+__device__ __forceinline__ void shrink_short(const AdapterRows &o, int rank, const Shrink &k,
+                                             int tile, int split, int r0, floatx4 *lds) {
+    constexpr int DEP = NR <= 2 ? 4 : 2, KG = shrink_waves(1);
+    const Tile t = find_tile(o, tile_shift_of(1), tile);
     if (t.e < 0) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rg = wave % C::RG, kg = wave / C::RG, b0 = rg * PB;
-    const int parts = k.out.splits * C::KG, part = split * C::KG + kg;
+    const int kg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int parts = k.out.splits * KG, part = split * KG + kg;
     const int n = (k.K / 64 - part + parts - 1) / parts;
-    uint64_t xo[PB];
+    const int row = row_at(o, t.first + min(m, t.rows - 1));
     uint32_t wo[NR];
-#pragma unroll
-    for (int b = 0; b < PB; ++b) {
-        const int row = row_at(o, t.first + min(16 * (b0 + b) + m, t.rows - 1));
-        xo[b] = ((uint64_t)max(row, 0) * k.K + 8 * g) * 2;
-    }
 #pragma unroll
     for (int c = 0; c < NR; ++c)  // behind the last rank value: the last again, not stored
         wo[c] = ((uint32_t)min(r0 + 16 * c + m, rank - 1) * k.K + 8 * g) * 2;
-    const char *xs = (const char *)(k.x + part * 64);
+    const char *xs = (const char *)(k.x + (int64_t)max(row, 0) * k.K + part * 64 + 8 * g);
     const char *ws = (const char *)(k.w + (int64_t)t.e * rank * k.K + part * 64);
-    floatx4 acc[PB][NR] = {};
-    bf16x8 xv[DEP][PB][2], wv[DEP][NR][2];
+    floatx4 acc[NR] = {};
+    bf16x8 xv[DEP][2], wv[DEP][NR][2];
     // (both halves of a cache line one after the other: it may not stay)
     auto load = [&](int i, int s) {
         const int at = s * parts * 128;
 #pragma unroll
-        for (int b = 0; b < PB; ++b)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                xv[i][b][h] = *reinterpret_cast<const bf16x8 *>(xs + at + xo[b] + 64 * h);
+        for (int h = 0; h < 2; ++h) xv[i][h] = *reinterpret_cast<const bf16x8 *>(xs + at + 64 * h);
 #pragma unroll
         for (int c = 0; c < NR; ++c)
 #pragma unroll
@@ -158,10 +144,7 @@ __device__ __forceinline__ void shrink(const AdapterRows &o, int rank, const Shr
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int b = 0; b < PB; ++b)
-#pragma unroll
-                for (int c = 0; c < NR; ++c)
-                    acc[b][c] = mfma(xv[i][b][h], wv[i][c][h], acc[b][c]);
+            for (int c = 0; c < NR; ++c) acc[c] = mfma(xv[i][h], wv[i][c][h], acc[c]);
     };
     if (n > 0) {
 #pragma unroll
@@ -178,35 +161,125 @@ __device__ __forceinline__ void shrink(const AdapterRows &o, int rank, const Shr
         for (int i = 0; i < DEP; ++i)
             if (s + i < n) use(i);
     }
-    // the sums of the waves that share K meet in LDS, half of them at a time
+    // the waves' sums meet in LDS, half of them at a time
 #pragma unroll
-    for (int half = C::KG / 2; half >= 1; half /= 2) {
-        floatx4 *at = lds + ((kg % half) * C::RG + rg) * PB * NR * 64 + lane;
+    for (int half = KG / 2; half >= 1; half /= 2) {
+        floatx4 *at = lds + (kg % half) * NR * 64 + lane;
         if (kg >= half && kg < 2 * half) {
 #pragma unroll
-            for (int b = 0; b < PB; ++b)
-#pragma unroll
-                for (int c = 0; c < NR; ++c) at[(b * NR + c) * 64] = acc[b][c];
+            for (int c = 0; c < NR; ++c) at[c * 64] = acc[c];
         }
         __syncthreads();
         if (kg < half) {
 #pragma unroll
-            for (int b = 0; b < PB; ++b)
-#pragma unroll
-                for (int c = 0; c < NR; ++c) acc[b][c] += at[(b * NR + c) * 64];
+            for (int c = 0; c < NR; ++c) acc[c] += at[c * 64];
         }
         __syncthreads();
     }
     if (kg > 0) return;
+    float *p = k.out.p + ((int64_t)tile * k.out.splits + split) * rank * 16;
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+        const int r = r0 + 16 * c + m;
+        if (r < rank) *reinterpret_cast<floatx4 *>(p + r * 16 + 4 * g) = acc[c];
+    }
+}
+
+// Tall tiles: a wave has a row block and all of the rank.  Rows and adapter come in as
+// whole lines (eight lanes to the 128 bytes of a row: the cache takes a lane's 16 bytes
+// of a row of its own as slowly as 64 of a shared one), AHEAD steps of 64 k in
+// registers, and lie in LDS as operands [block][chunk of 8 k][row][8], two steps in
+// turn.  `splits` workgroups share K.
+template <int RB, int NR>
+struct TallShrink {
+    static constexpr int TH = 64 * shrink_waves(RB), AHEAD = 3;
+    static constexpr int XI = 2, WI = (2 * NR + RB - 1) / RB;  // loads of a thread
+    static constexpr int XL = RB * 8 * kPitch, WL = NR * 8 * kPitch;
+    static constexpr size_t LDS = (size_t)2 * (XL + WL) * 16;
+};
+
+template <int RB, int NR>
+__device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, const Shrink &k,
+                                            int tile, int split, char *lds) {
+    using C = TallShrink<RB, NR>;
+    constexpr int TM = 16 * RB, D = C::AHEAD, XI = C::XI, WI = C::WI;
+    const Tile t = find_tile(o, tile_shift_of(RB), tile);
+    if (t.e < 0) return;
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int steps = k.K / 64, lo = (int)((int64_t)steps * split / k.out.splits);
+    const int n = (int)((int64_t)steps * (split + 1) / k.out.splits) - lo;
+    const bf16_t *xp[XI];
+    uint32_t wo[WI];
+    int xt[XI], wt[WI];  // places in LDS
+#pragma unroll
+    for (int i = 0; i < XI; ++i) {
+        const int item = threadIdx.x + C::TH * i, r = item / 8, ch = item % 8;
+        const int row = row_at(o, t.first + min(r, t.rows - 1));
+        xp[i] = k.x + (int64_t)max(row, 0) * k.K + lo * 64 + 8 * ch;
+        xt[i] = ((r >> 4) * 8 + ch) * kPitch + (r & 15);
+    }
+#pragma unroll
+    for (int i = 0; i < WI; ++i) {  // behind the last rank value: the last again, not stored
+        const int item = min((int)threadIdx.x + C::TH * i, 16 * NR * 8 - 1), r = item / 8;
+        wo[i] = ((uint32_t)min(r, rank - 1) * k.K + 8 * (item % 8)) * 2;
+        wt[i] = C::XL + ((r >> 4) * 8 + item % 8) * kPitch + (r & 15);
+    }
+    const bf16_t *we = k.w + (int64_t)t.e * rank * k.K + lo * 64;
+    bf16x8 xv[D][XI], wv[D][WI];
+    auto load = [&](int i, int s) {
+#pragma unroll
+        for (int j = 0; j < XI; ++j) xv[i][j] = load8(xp[j] + s * 64);
+#pragma unroll
+        for (int j = 0; j < WI; ++j) wv[i][j] = load8(we + s * 64, wo[j]);
+    };
+    floatx4 acc[NR] = {};
+    bf16x8 *buf = reinterpret_cast<bf16x8 *>(lds);
+    auto put = [&](int i, bf16x8 *to) {
+#pragma unroll
+        for (int j = 0; j < XI; ++j) to[xt[j]] = xv[i][j];
+#pragma unroll
+        for (int j = 0; j < WI; ++j) to[wt[j]] = wv[i][j];
+    };
+    auto use = [&](const bf16x8 *from) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bf16x8 a = from[(wave * 8 + 4 * h + g) * kPitch + m];
+#pragma unroll
+            for (int c = 0; c < NR; ++c)
+                acc[c] = mfma(a, from[C::XL + (c * 8 + 4 * h + g) * kPitch + m], acc[c]);
+        }
+    };
+    constexpr int SZ = C::XL + C::WL;
+    if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < D; ++i) load(i, min(i, n - 1));
+        // One barrier a step: who writes a buffer has passed the barrier behind which
+        // its last readers were done.
+        int s = 0, p = 0;
+        for (; s + D <= n; s += D) {
+#pragma unroll
+            for (int i = 0; i < D; ++i, p ^= 1) {
+                put(i, buf + p * SZ);
+                load(i, min(s + i + D, n - 1));
+                __syncthreads();
+                use(buf + p * SZ);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < D; ++i, p ^= 1)
+            if (s + i < n) {
+                put(i, buf + p * SZ);
+                __syncthreads();
+                use(buf + p * SZ);
+            }
+    }
     float *p = k.out.p + ((int64_t)tile * k.out.splits + split) * rank * TM;
 #pragma unroll
-    for (int b = 0; b < PB; ++b)
-#pragma unroll
-        for (int c = 0; c < NR; ++c) {
-            const int r = r0 + 16 * c + m;
-            if (r < rank)
-                *reinterpret_cast<floatx4 *>(p + r * TM + 16 * (b0 + b) + 4 * g) = acc[b][c];
-        }
+    for (int c = 0; c < NR; ++c) {
+        const int r = 16 * c + m;
+        if (r < rank) *reinterpret_cast<floatx4 *>(p + r * TM + 16 * wave + 4 * g) = acc[c];
+    }
 }
 
 // wt[e] = w[e]^T for the adapters that have rows, w [count][m][n]: 64 x 64 tiles
@@ -251,26 +324,27 @@ __device__ __forceinline__ void transpose(const AdapterRows &o, const Transpose 
 
 // Blocks of the shrink, then of the transposes (of the gradient's first launch).
 template <int RB, int NR>
-__global__ __launch_bounds__(64 * shrink_waves(RB), 2) void shrink_kernel(AdapterRows o, int rank,
-                                                                       Shrink k, Transpose ta,
-                                                                       Transpose tb) {
-    using C = ShrinkCfg<RB, NR>;
-    __shared__ union {
-        floatx4 sums[C::KG / 2 * C::RG * C::PB * NR * 64];
-        uint16_t tile[64][66];
-    } lds;
+__global__ __launch_bounds__(64 * shrink_waves(RB), RB == 1 ? 2 : 4) void shrink_kernel(
+    AdapterRows o, int rank, Shrink k, Transpose ta, Transpose tb) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     int b = blockIdx.x;
-    const int groups = (rank + 16 * NR - 1) / (16 * NR), mine = k.tiles * k.out.splits * groups;
+    const int groups = RB > 1 ? 1 : (rank + 16 * NR - 1) / (16 * NR);
+    const int mine = k.tiles * k.out.splits * groups;
     if (b < mine) {
-        shrink<RB, NR>(o, rank, k, b / k.out.splits % k.tiles, b % k.out.splits,
-                       b / (k.tiles * k.out.splits) * 16 * NR, lds.sums);
+        const int split = b % k.out.splits, tile = b / k.out.splits % k.tiles;
+        if constexpr (RB == 1)
+            shrink_short<NR>(o, rank, k, tile, split, b / (k.tiles * k.out.splits) * 16 * NR,
+                             reinterpret_cast<floatx4 *>(lds));
+        else
+            shrink_tall<RB, NR>(o, rank, k, tile, split, lds);
         return;
     }
     b -= mine;
+    uint16_t(*tile)[66] = reinterpret_cast<uint16_t(*)[66]>(lds);
     if (b < ta.blocks)
-        transpose(o, ta, b, lds.tile);
+        transpose(o, ta, b, tile);
     else
-        transpose(o, tb, b - ta.blocks, lds.tile);
+        transpose(o, tb, b - ta.blocks, tile);
 }
 
 // ---- + scale u B^T -------------------------------------------------------
@@ -450,8 +524,6 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
 // comes in as whole lines, by all of them, and lies in LDS as operands
 // [j][chunk][n][8], two blocks of 64 columns in turn.  Short tiles: the waves have
 // columns of their own and take B's operands from memory.
-constexpr int kPitch = 17;  // operands of a chunk and one: writes of different banks
-
 template <int RB, class Y>
 __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Expand<Y> &k,
                                        int block, char *lds) {
@@ -898,16 +970,32 @@ hipError_t by_size(const AdapterRows &o, int rank, F fn) {
     }
 }
 
+// More than 64 KB of LDS are asked for.
+hipError_t allow_lds(const void *fn, size_t lds) {
+    return lds > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)lds)
+                       : hipSuccess;
+}
+
 hipError_t launch_shrink(const AdapterRows &o, int rank, int K, const bf16_t *x, const bf16_t *w,
                          const AdapterSums &out, const Transpose &ta, const Transpose &tb,
                          hipStream_t s) {
     const Shrink k{x, w, out, K, x ? (int)tile_count(o, rank) : 0};
-    return by_size(o, rank, [&](auto rb, auto nr) {
-        const unsigned groups = (rank + 16 * nr() - 1) / (16 * nr());
+    auto go = [&](auto rb, auto nr) {
+        const unsigned groups = rb() > 1 ? 1 : (rank + 16 * nr() - 1) / (16 * nr());
         const unsigned grid = (unsigned)k.tiles * out.splits * groups + ta.blocks + tb.blocks;
-        shrink_kernel<rb(), nr()><<<grid, 64 * shrink_waves(rb()), 0, s>>>(o, rank, k, ta, tb);
+        size_t lds = rb() > 1 ? TallShrink<rb(), nr()>::LDS
+                              : (size_t)shrink_waves(1) / 2 * nr() * 64 * sizeof(floatx4);
+        lds = std::max(lds, (size_t)64 * 66 * sizeof(uint16_t));
+        const auto fn = shrink_kernel<rb(), nr()>;
+        if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
+        fn<<<grid, 64 * shrink_waves(rb()), lds, s>>>(o, rank, k, ta, tb);
         return hipGetLastError();
-    });
+    };
+    if (rank > 64 && row_blocks(o.rows, o.count, rank) > 1)  // one pass over the rows
+        return row_blocks(o.rows, o.count, rank) == 8 ? go(Int<8>(), Int<8>())
+                                                      : go(Int<4>(), Int<8>());
+    return by_size(o, rank, go);
 }
 
 // Of tall tiles only.
@@ -918,13 +1006,6 @@ hipError_t launch_cut(const AdapterRows &o, int rank, const float *scale, const 
     const auto fn = rb == 8 ? cut_kernel<8> : cut_kernel<4>;
     fn<<<(unsigned)tiles * (both ? 2 : 1), 512, 0, s>>>(o, rank, scale, a, b, tiles);
     return hipGetLastError();
-}
-
-// More than 64 KB of LDS are asked for.
-hipError_t allow_lds(const void *fn, size_t lds) {
-    return lds > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)lds)
-                       : hipSuccess;
 }
 
 template <class Y>
@@ -984,7 +1065,7 @@ int splits_of(int64_t rows, int count, int K, int rank) {
     const int rb = row_blocks(rows, count, rank);
     const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift_of(rb)), 1);
     const int64_t want = rb > 1 ? 512 / tiles : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
-    const int64_t most = std::max(1, K / 64 / (rb == 8 ? 2 : shrink_waves(rb)));
+    const int64_t most = std::max(1, K / 64 / 4);
     return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)(rb > 1 ? 8 : 16)}));
 }
 
