@@ -18,13 +18,12 @@
 namespace moe {
 namespace {
 
-constexpr int kWaves = 4;       // of expand over short tiles
-constexpr int expand_waves(int RB) { return RB == 1 ? kWaves : RB; }
-constexpr int kExpandSpan = 8;  // blocks of 64 columns of its workgroups over tall tiles
-constexpr int kOuterWaves = 8;  // of outer: four column blocks, two halves of the rows
+constexpr int kWaves = 8;  // of expand (tall tiles: a row block each; short: 64 columns) and
+                           // of outer (four column blocks, two halves of the rows)
+constexpr int kExpandSpan = 8;  // blocks of 64 columns of expand's workgroups
 
-// Row blocks of 16 of a tile -> rows of it, as a power of two.
-constexpr int tile_shift_of(int RB) { return RB == 8 ? 7 : RB == 4 ? 6 : 4; }
+// Row blocks of 16 of a tile (1 or 8) -> rows of it, as a power of two.
+constexpr int tile_shift_of(int RB) { return RB == 8 ? 7 : 4; }
 // The waves of shrink.
 constexpr int shrink_waves(int RB) { return RB == 1 ? 4 : RB; }
 constexpr int kPitch = 17;  // operands of 16 rows and one: writes of different banks
@@ -322,32 +321,29 @@ __device__ __forceinline__ void transpose(const AdapterRows &o, const Transpose 
     }
 }
 
-// Blocks of the shrink, then of the transposes (of the gradient's first launch).
+// Blocks of one shrink, then of another (of the gradient).
 template <int RB, int NR>
 __global__ __launch_bounds__(64 * shrink_waves(RB), RB == 1 ? 2 : 4) void shrink_kernel(
-    AdapterRows o, int rank, Shrink k, Transpose ta, Transpose tb) {
+    AdapterRows o, int rank, Shrink k0, Shrink k1, int blocks0) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int b = blockIdx.x;
-    const int groups = RB > 1 ? 1 : (rank + 16 * NR - 1) / (16 * NR);
-    const int mine = k.tiles * k.out.splits * groups;
-    if (b < mine) {
-        const int split = b % k.out.splits, tile = b / k.out.splits % k.tiles;
-        if constexpr (RB == 1)
-            shrink_short<NR>(o, rank, k, tile, split, b / (k.tiles * k.out.splits) * 16 * NR,
-                             reinterpret_cast<floatx4 *>(lds));
-        else
-            shrink_tall<RB, NR>(o, rank, k, tile, split, lds);
-        return;
-    }
-    b -= mine;
-    uint16_t(*tile)[66] = reinterpret_cast<uint16_t(*)[66]>(lds);
-    if (b < ta.blocks)
-        transpose(o, ta, b, tile);
+    const bool first = (int)blockIdx.x < blocks0;
+    const Shrink &k = first ? k0 : k1;
+    const int b = first ? blockIdx.x : blockIdx.x - blocks0;
+    const int split = b % k.out.splits, tile = b / k.out.splits % k.tiles;
+    if constexpr (RB == 1)
+        shrink_short<NR>(o, rank, k, tile, split, b / (k.tiles * k.out.splits) * 16 * NR,
+                         reinterpret_cast<floatx4 *>(lds));
     else
-        transpose(o, tb, b - ta.blocks, tile);
+        shrink_tall<RB, NR>(o, rank, k, tile, split, lds);
 }
 
-// ---- + scale u B^T -------------------------------------------------------
+// Both of an adapter's matrices.
+__global__ __launch_bounds__(256) void transpose_kernel(AdapterRows o, Transpose ta,
+                                                        Transpose tb) {
+    __shared__ uint16_t tile[64][66];
+    const int b = blockIdx.x;
+    transpose(o, b < ta.blocks ? ta : tb, b < ta.blocks ? b : b - ta.blocks, tile);
+}
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __bf16 x = (__bf16)a, y = (__bf16)b;
@@ -385,6 +381,26 @@ __device__ __forceinline__ void cut8(const float (&v)[8], bf16x8 (&part)[S]) {
     for (int q = 0; q < S; ++q) part[q] = __builtin_bit_cast(bf16x8, w[q]);
 }
 
+// v[j] += the sum over splits of p[split * pitch + j * TM], four splits' loads at once.
+template <int TM>
+__device__ __forceinline__ void sum_splits(float (&v)[8], const float *p, int pitch, int splits) {
+    int q = 0;
+    for (; q + 4 <= splits; q += 4) {
+        float w[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[i][j] = p[(q + i) * pitch + j * TM];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += w[i][j];
+    }
+    for (; q < splits; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += p[q * pitch + j * TM];
+}
+
 // ---- sums, scaled and cut --------------------------------------------------
 // Of tall tiles: once a row, in a launch of its own, for the many workgroups behind
 // it.  e: S parts as operands of expand, [tile][row block][chunk][row][8] with the
@@ -419,9 +435,7 @@ __device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const f
         const int row = i % TM, kc = i / TM;
         float v[8] = {};
         if (row < t.rows) {
-            for (int s = 0; s < k.u.splits; ++s)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += p[((int64_t)s * rank + 8 * kc + j) * TM + row];
+            sum_splits<TM>(v, p + 8 * kc * TM + row, rank * TM, k.u.splits);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= f;
         }
@@ -501,7 +515,7 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
     const int64_t mine = (int64_t)block * 64 + lane;
     uint64_t none = __ballot(mine < o.rows && o.place[min(mine, o.rows - 1)] < 0);
     for (int i = 0; none; ++i, none &= none - 1) {
-        if (i % (int)(blockDim.x >> 6) != wave) continue;
+        if (i % kWaves != wave) continue;
         const int64_t at = ((int64_t)block * 64 + __builtin_ctzll(none)) * k.N;
         for (int c = c0 + lane * V; c < c1; c += 64 * V) {
             u32x4 v = {};
@@ -531,7 +545,7 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
     using V = typename P::V;
     constexpr int S = P::S, TM = 16 * RB;
     constexpr bool SHARED = RB > 1;
-    constexpr int TH = 64 * expand_waves(RB), WC = SHARED ? 1 : kWaves;
+    constexpr int TH = 64 * kWaves, WC = SHARED ? 1 : kWaves;
     const int tile = block / k.ranges;
     const int c0 = block % k.ranges * k.span * 64, c1 = min(k.N, c0 + k.span * 64);
     if (tile >= k.tiles) {
@@ -676,10 +690,7 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
             bf16x8 part[S] = {};
             if (row < t.rows && kc < rc) {
                 float v[8] = {};
-                for (int q = 0; q < k.u.splits; ++q)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        v[j] += pt[((int64_t)q * rank + 8 * kc + j) * TM + row];
+                sum_splits<TM>(v, pt + 8 * kc * TM + row, rank * TM, k.u.splits);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= f;
                 cut8<S>(v, part);
@@ -709,7 +720,7 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
 }
 
 template <int RB, class Y>
-__global__ __launch_bounds__(64 * expand_waves(RB), 4) void expand_kernel(AdapterRows o, int rank,
+__global__ __launch_bounds__(64 * kWaves, 4) void expand_kernel(AdapterRows o, int rank,
                                                              Expand<Y> k) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     expand<RB, Y>(o, rank, k, blockIdx.x, lds);
@@ -760,7 +771,7 @@ template <int RB, int NR>
 __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const float *scale, int sh,
                                       int slots, bool accumulate, const Outer &k, int block,
                                       char *lds) {
-    constexpr int TSH = tile_shift_of(RB), TM = 16 * RB, KR = kOuterWaves / 4;
+    constexpr int TSH = tile_shift_of(RB), TM = 16 * RB, KR = kWaves / 4;
     floatx4 *sums = reinterpret_cast<floatx4 *>(lds);
     int *rows = reinterpret_cast<int *>(lds);  // before the sums
     const Tile t = find_tile(o, sh, block / k.cb);
@@ -776,7 +787,7 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
     const bf16_t *qr = k.q + qc;
     for (int grp = 0; grp < groups; ++grp) {
         const int r0 = grp * 16 * NR;
-        for (int i = threadIdx.x; i < t.rows; i += 64 * kOuterWaves)
+        for (int i = threadIdx.x; i < t.rows; i += 64 * kWaves)
             rows[i] = max(row_at(o, t.first + i), 0);
         __syncthreads();
         floatx4 acc[NR][8] = {};
@@ -788,7 +799,8 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                 raw[i] = *reinterpret_cast<const u32x4 *>(qr + row * k.C);
             }
         };
-        constexpr bool AHEAD = NR < 4;  // (registers for two steps' rows)
+        // (registers for two steps' rows; of few rows a wave has a step or two)
+        constexpr bool AHEAD = RB > 1 && NR < 4;
         if (AHEAD && 32 * rw < t.rows) load_q(32 * rw);
         for (int k0 = 32 * rw; k0 < t.rows; k0 += 32 * KR) {
             if (!AHEAD) load_q(k0);
@@ -893,7 +905,7 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
 
 // The gradient's products behind u and v: blocks of db, then of da.
 template <int RB, int NR>
-__global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(AdapterRows o, int rank,
+__global__ __launch_bounds__(64 * kWaves) void outer_kernel(AdapterRows o, int rank,
                                                                  const float *scale, int sh,
                                                                  int slots, int accumulate,
                                                                  Outer kb, Outer ka) {
@@ -901,6 +913,20 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(AdapterRows o, 
     const int b = blockIdx.x;
     outer<RB, NR>(o, rank, scale, sh, slots, accumulate, b < kb.blocks ? kb : ka,
                   b < kb.blocks ? b : b - kb.blocks, lds);
+}
+
+// Of few rows: those and the blocks of dx in one launch.
+template <int NR, class Y>
+__global__ __launch_bounds__(64 * kWaves, NR == 1 ? 4 : 2) void back_kernel(
+    AdapterRows o, int rank, const float *scale, int sh, int slots, int accumulate, Outer kb,
+    Outer ka, Expand<Y> kx) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int b = blockIdx.x;
+    if (b < kb.blocks + ka.blocks)
+        outer<1, NR>(o, rank, scale, sh, slots, accumulate, b < kb.blocks ? kb : ka,
+                     b < kb.blocks ? b : b - kb.blocks, lds);
+    else
+        expand<1, Y>(o, rank, kx, b - kb.blocks - ka.blocks, lds);
 }
 
 // Adapters of several tiles: their parts, added in order; adapters of no rows:
@@ -926,9 +952,18 @@ __global__ __launch_bounds__(256) void join_kernel(AdapterRows o, int sh, int sl
     n = min(n, slots - before);
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size;
          i += (int64_t)gridDim.x * 1024) {
+        const float *src = k.parts + before * size + i;
         floatx4 v = {};
-        for (int j = 0; j < n; ++j)
-            v += *reinterpret_cast<const floatx4 *>(k.parts + (int64_t)(before + j) * size + i);
+        int j = 0;
+        for (; j + 4 <= n; j += 4) {
+            floatx4 w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                w[q] = *reinterpret_cast<const floatx4 *>(src + (j + q) * size);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v += w[q];
+        }
+        for (; j < n; ++j) v += *reinterpret_cast<const floatx4 *>(src + j * size);
         floatx4 *d = reinterpret_cast<floatx4 *>(k.out + (int64_t)e * size + i);
         *d = accumulate ? *d + v : v;
     }
@@ -943,9 +978,9 @@ int64_t tile_cap(int64_t rows, int count, int sh) {
 // Row blocks of a tile.  Tall ones read the adapters' matrices less often; they are
 // for many rows, where the adapters' mean rows fill most of one.  u's parts of a tile
 // have to fit LDS.
+constexpr int64_t kTallRows = 4096;
 int row_blocks(int64_t rows, int count, int rank) {
-    if (rank > 128 || rows < 4096 || rows < (int64_t)48 * count) return 1;
-    return rows >= 8192 && rows >= (int64_t)96 * count ? 8 : 4;
+    return rank <= 128 && rows >= kTallRows && rows >= (int64_t)96 * count ? 8 : 1;
 }
 int64_t tile_count(const AdapterRows &o, int rank) {
     return tile_cap(o.rows, o.count, tile_shift_of(row_blocks(o.rows, o.count, rank)));
@@ -963,11 +998,7 @@ hipError_t by_size(const AdapterRows &o, int rank, F fn) {
     auto go = [&](auto rb) {
         return rank <= 16 ? fn(rb, Int<1>()) : rank <= 32 ? fn(rb, Int<2>()) : fn(rb, Int<4>());
     };
-    switch (row_blocks(o.rows, o.count, rank)) {
-        case 8: return go(Int<8>());
-        case 4: return go(Int<4>());
-        default: return go(Int<1>());
-    }
+    return row_blocks(o.rows, o.count, rank) == 8 ? go(Int<8>()) : go(Int<1>());
 }
 
 // More than 64 KB of LDS are asked for.
@@ -977,24 +1008,21 @@ hipError_t allow_lds(const void *fn, size_t lds) {
                        : hipSuccess;
 }
 
-hipError_t launch_shrink(const AdapterRows &o, int rank, int K, const bf16_t *x, const bf16_t *w,
-                         const AdapterSums &out, const Transpose &ta, const Transpose &tb,
+// a, and b unless it has no tiles.
+hipError_t launch_shrink(const AdapterRows &o, int rank, const Shrink &a, const Shrink &b,
                          hipStream_t s) {
-    const Shrink k{x, w, out, K, x ? (int)tile_count(o, rank) : 0};
     auto go = [&](auto rb, auto nr) {
-        const unsigned groups = rb() > 1 ? 1 : (rank + 16 * nr() - 1) / (16 * nr());
-        const unsigned grid = (unsigned)k.tiles * out.splits * groups + ta.blocks + tb.blocks;
-        size_t lds = rb() > 1 ? TallShrink<rb(), nr()>::LDS
-                              : (size_t)shrink_waves(1) / 2 * nr() * 64 * sizeof(floatx4);
-        lds = std::max(lds, (size_t)64 * 66 * sizeof(uint16_t));
+        const int groups = rb() > 1 ? 1 : (rank + 16 * nr() - 1) / (16 * nr());
+        const int na = a.tiles * a.out.splits * groups, nb = b.tiles * b.out.splits * groups;
+        const size_t lds = rb() > 1 ? TallShrink<rb(), nr()>::LDS
+                                    : (size_t)shrink_waves(1) / 2 * nr() * 64 * sizeof(floatx4);
         const auto fn = shrink_kernel<rb(), nr()>;
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
-        fn<<<grid, 64 * shrink_waves(rb()), lds, s>>>(o, rank, k, ta, tb);
+        fn<<<(unsigned)(na + nb), 64 * shrink_waves(rb()), lds, s>>>(o, rank, a, b, na);
         return hipGetLastError();
     };
     if (rank > 64 && row_blocks(o.rows, o.count, rank) > 1)  // one pass over the rows
-        return row_blocks(o.rows, o.count, rank) == 8 ? go(Int<8>(), Int<8>())
-                                                      : go(Int<4>(), Int<8>());
+        return go(Int<8>(), Int<8>());
     return by_size(o, rank, go);
 }
 
@@ -1003,59 +1031,91 @@ hipError_t launch_cut(const AdapterRows &o, int rank, const float *scale, const 
                       const Cut &b, bool both, hipStream_t s) {
     const int rb = row_blocks(o.rows, o.count, rank), tiles = (int)tile_count(o, rank);
     if (rb == 1) return hipSuccess;
-    const auto fn = rb == 8 ? cut_kernel<8> : cut_kernel<4>;
-    fn<<<(unsigned)tiles * (both ? 2 : 1), 512, 0, s>>>(o, rank, scale, a, b, tiles);
+    cut_kernel<8><<<(unsigned)tiles * (both ? 2 : 1), 512, 0, s>>>(o, rank, scale, a, b, tiles);
     return hipGetLastError();
 }
 
 template <class Y>
-hipError_t launch_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u,
-                         const bf16_t *w, const float *scale, const void *base, void *y,
-                         hipStream_t s) {
-    Expand<Y> k{u, w, scale, (const Y *)base, (Y *)y, N, 0, 0, 0, 0};
-    const int rb = row_blocks(o.rows, o.count, rank);
+Expand<Y> make_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u, const bf16_t *w,
+                      const float *scale, const void *base, void *y) {
+    Expand<Y> k{u, w, scale, (const Y *)base, (Y *)y, N, 0, 0, kExpandSpan, 0};
     k.tiles = (int)tile_count(o, rank);
     k.copies = base == y ? 0 : (int)((o.rows + 63) / 64);
-    // a block a wave; larger ranks take u's cutting, tall tiles its parts further
-    k.span = rb > 1 ? kExpandSpan : kWaves * (rank <= 64 ? 1 : rank <= 128 ? 2 : 4);
     k.ranges = (N / 64 + k.span - 1) / k.span;
-    size_t lds = (size_t)rb * ((rank / 8 * Four<Y>::S + 3) / 4 * 4) * 256;
-    if (rb > 1) lds += (size_t)2 * 4 * (rank / 8) * kPitch * 16;  // B's two blocks
-    const auto fn = rb == 8   ? expand_kernel<8, Y>
-                    : rb == 4 ? expand_kernel<4, Y>
-                              : expand_kernel<1, Y>;
+    return k;
+}
+template <class Y>
+size_t expand_lds(const AdapterRows &o, int rank) {
+    const int rb = row_blocks(o.rows, o.count, rank);
+    const size_t u = (size_t)rb * ((rank / 8 * Four<Y>::S + 3) / 4 * 4) * 256;
+    return rb > 1 ? u + (size_t)2 * 4 * (rank / 8) * kPitch * 16 : u;  // and B's two blocks
+}
+template <class Y>
+unsigned expand_blocks(const Expand<Y> &k) {
+    return (unsigned)((int64_t)(k.tiles + k.copies) * k.ranges);
+}
+
+template <class Y>
+hipError_t launch_expand(const AdapterRows &o, int rank, const Expand<Y> &k, hipStream_t s) {
+    const size_t lds = expand_lds<Y>(o, rank);
+    const auto fn = row_blocks(o.rows, o.count, rank) == 8 ? expand_kernel<8, Y>
+                                                           : expand_kernel<1, Y>;
     if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
-    fn<<<(unsigned)((int64_t)(k.tiles + k.copies) * k.ranges), 64 * expand_waves(rb), lds, s>>>(
-        o, rank, k);
+    fn<<<expand_blocks(k), 64 * kWaves, lds, s>>>(o, rank, k);
     return hipGetLastError();
 }
 hipError_t launch_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u,
                          const bf16_t *w, const float *scale, const void *base, void *y, int type,
                          hipStream_t s) {
-    return type == MOE_FP32 ? launch_expand<float>(o, rank, N, u, w, scale, base, y, s)
-                            : launch_expand<bf16_t>(o, rank, N, u, w, scale, base, y, s);
+    return type == MOE_FP32
+               ? launch_expand(o, rank, make_expand<float>(o, rank, N, u, w, scale, base, y), s)
+               : launch_expand(o, rank, make_expand<bf16_t>(o, rank, N, u, w, scale, base, y), s);
 }
+
+size_t outer_lds(int nr) { return (size_t)4 * nr * 8 * 64 * sizeof(floatx4); }
 
 hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool accumulate,
                         Outer kb, Outer ka, hipStream_t s) {
     const int sh = outer_shift(o.rows), slots = (int)outer_slots(o.rows);
-    if (o.rows) {
-        const int tiles = (int)tile_cap(o.rows, o.count, sh);
-        ka.blocks = tiles * ka.cb;
-        kb.blocks = tiles * kb.cb;
-        const hipError_t e = by_size(o, rank, [&](auto rb, auto nr) {
-            const auto fn = outer_kernel<rb(), nr()>;
-            const size_t lds = (size_t)4 * nr() * 8 * 64 * sizeof(floatx4);
-            if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
-            fn<<<(unsigned)(ka.blocks + kb.blocks), 64 * kOuterWaves, lds, s>>>(
-                o, rank, scale, sh, slots, accumulate, kb, ka);
-            return hipGetLastError();
-        });
-        if (e) return e;
-    }
+    const int tiles = (int)tile_cap(o.rows, o.count, sh);
+    ka.blocks = tiles * ka.cb;
+    kb.blocks = tiles * kb.cb;
+    return by_size(o, rank, [&](auto rb, auto nr) {
+        const auto fn = outer_kernel<rb(), nr()>;
+        const size_t lds = outer_lds(nr());
+        if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
+        fn<<<(unsigned)(ka.blocks + kb.blocks), 64 * kWaves, lds, s>>>(o, rank, scale, sh, slots,
+                                                                       accumulate, kb, ka);
+        return hipGetLastError();
+    });
+}
+
+template <class Y>
+hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const AdapterBack &k,
+                        Outer kb, Outer ka, hipStream_t s) {
+    const int sh = outer_shift(o.rows), slots = (int)outer_slots(o.rows);
+    const int tiles = (int)tile_cap(o.rows, o.count, sh), rank = ad.rank;
+    ka.blocks = tiles * ka.cb;
+    kb.blocks = tiles * kb.cb;
+    const auto kx = make_expand<Y>(o, rank, ad.k, k.v, k.at, ad.scale, k.base, k.dx);
+    auto go = [&](auto nr) {
+        const auto fn = back_kernel<nr(), Y>;
+        const size_t lds = std::max(outer_lds(nr()), expand_lds<Y>(o, rank));
+        if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
+        fn<<<ka.blocks + kb.blocks + expand_blocks(kx), 64 * kWaves, lds, s>>>(
+            o, rank, ad.scale, sh, slots, k.accumulate, kb, ka, kx);
+        return hipGetLastError();
+    };
+    return rank <= 16 ? go(Int<1>()) : rank <= 32 ? go(Int<2>()) : go(Int<4>());
+}
+
+hipError_t launch_join(const AdapterRows &o, int rank, bool accumulate, const Outer &ka,
+                       const Outer &kb, hipStream_t s) {
     const int64_t size = (int64_t)rank * std::max(ka.C, kb.C);
     const unsigned bx = (unsigned)std::min<int64_t>((size + 1023) / 1024, 64);
-    join_kernel<<<dim3(bx, o.count, 2), 256, 0, s>>>(o, sh, slots, accumulate, ka, kb, rank);
+    join_kernel<<<dim3(bx, o.count, 2), 256, 0, s>>>(o, outer_shift(o.rows),
+                                                     (int)outer_slots(o.rows), accumulate, ka, kb,
+                                                     rank);
     return hipGetLastError();
 }
 
@@ -1066,7 +1126,7 @@ int splits_of(int64_t rows, int count, int K, int rank) {
     const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift_of(rb)), 1);
     const int64_t want = rb > 1 ? 512 / tiles : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
     const int64_t most = std::max(1, K / 64 / 4);
-    return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)(rb > 1 ? 8 : 16)}));
+    return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)8}));
 }
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
@@ -1079,8 +1139,7 @@ SumsSize sums_size(int64_t rows, int count, int rank) {
     const int rb = row_blocks(rows, count, rank), sh = tile_shift_of(rb);
     const int64_t tiles = tile_cap(rows, count, sh);
     // no more than splits * tiles of any K
-    const int64_t sums = std::max(tiles, rb == 1 ? std::min<int64_t>(16 * tiles, 1024)
-                                                       : std::min<int64_t>(8 * tiles, 512));
+    const int64_t sums = std::max(tiles, std::min<int64_t>(8 * tiles, rb == 1 ? 1024 : 512));
     SumsSize z{up((size_t)sums * rank * sizeof(float) << sh), 0, 0};
     if (rb > 1) {
         z.e = up((size_t)tiles * ((rank / 8 * 3 + 3) / 4 * 4) * 16 << sh);
@@ -1096,12 +1155,9 @@ size_t adapter_sums_bytes(int64_t rows, int count, int rank) {
         const SumsSize z = sums_size(r, count, rank);
         return z.p + z.e + z.q;
     };
-    size_t most = bytes(rows);
-    // (the last rows of each tile height)
-    for (int64_t edge : {std::max<int64_t>(4096, (int64_t)48 * count),
-                         std::max<int64_t>(8192, (int64_t)96 * count)})
-        if (rows >= edge) most = std::max(most, bytes(edge - 1));
-    return most;
+    // (the tiles' height changes at one number of rows)
+    const int64_t edge = std::max<int64_t>(kTallRows, (int64_t)96 * count);
+    return rows >= edge ? std::max(bytes(rows), bytes(edge - 1)) : bytes(rows);
 }
 
 AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, void *at) {
@@ -1121,8 +1177,8 @@ size_t adapter_parts_bytes(int64_t rows, int rank, int C) {
 hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, const bf16_t *x,
                                const void *base, void *y, int y_type, const AdapterSums &u,
                                hipStream_t s) {
-    const Transpose none{};
-    if (hipError_t e = launch_shrink(o, ad.rank, ad.k, x, ad.a, u, none, none, s)) return e;
+    const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o, ad.rank)};
+    if (hipError_t e = launch_shrink(o, ad.rank, ku, Shrink{}, s)) return e;
     const Cut cu{u, y_type == MOE_FP32 ? 3 : 2, false};
     if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cu, cu, false, s)) return e;
     return launch_expand(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y, y_type, s);
@@ -1130,32 +1186,42 @@ hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, con
 
 hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
                                    const AdapterBack &k, hipStream_t s) {
+    const Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 511) / 512, 0};
+    const Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 511) / 512, 0};
     if (o.rows) {
         auto turn = [&](const bf16_t *w, bf16_t *wt, int m, int n) {
             const int bx = (n + 63) / 64;
             return Transpose{w, wt, m, n, bx, o.count * bx * ((m + 63) / 64)};
         };
-        // u = A x (for db), B^T, A^T (for dx)
-        if (hipError_t e = launch_shrink(o, ad.rank, ad.k, k.da ? k.x : nullptr, ad.a, k.u,
-                                         turn(ad.b, k.bt, ad.n, ad.rank),
-                                         k.dx ? turn(ad.a, k.at, ad.rank, ad.k) : Transpose{}, s))
-            return e;
-        // v = B^T dy
-        if (hipError_t e = launch_shrink(o, ad.rank, ad.n, k.dy, k.bt, k.v, Transpose{},
-                                         Transpose{}, s))
-            return e;
+        const Transpose tb = turn(ad.b, k.bt, ad.n, ad.rank);
+        const Transpose ta = k.dx ? turn(ad.a, k.at, ad.rank, ad.k) : Transpose{};
+        transpose_kernel<<<tb.blocks + ta.blocks, 256, 0, s>>>(o, tb, ta);
+        if (hipError_t e = hipGetLastError()) return e;
+        // v = B^T dy, and for db u = A x
+        const int tiles = (int)tile_count(o, ad.rank);
+        const Shrink kv{k.dy, k.bt, k.v, ad.n, tiles};
+        const Shrink ku = k.da ? Shrink{k.x, ad.a, k.u, ad.k, tiles} : Shrink{};
+        if (hipError_t e = launch_shrink(o, ad.rank, kv, ku, s)) return e;
         const Cut cv{k.v, !k.dx ? 0 : k.dx_type == MOE_FP32 ? 3 : 2, k.da != nullptr};
         const Cut cu{k.u, 0, true};
         if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cv, cu, k.da != nullptr, s)) return e;
-        if (k.dx)
-            if (hipError_t e = launch_expand(o, ad.rank, ad.k, k.v, k.at, ad.scale, k.base, k.dx,
-                                             k.dx_type, s))
+        if (k.dx && k.da && row_blocks(o.rows, o.count, ad.rank) == 1) {
+            // few rows: one launch for the three products
+            if (hipError_t e = k.dx_type == MOE_FP32
+                                   ? launch_short<float>(o, ad, k, kb, ka, s)
+                                   : launch_short<bf16_t>(o, ad, k, kb, ka, s))
                 return e;
+        } else {
+            if (k.dx)
+                if (hipError_t e = launch_expand(o, ad.rank, ad.k, k.v, k.at, ad.scale, k.base,
+                                                 k.dx, k.dx_type, s))
+                    return e;
+            if (k.da)
+                if (hipError_t e = launch_outer(o, ad.rank, ad.scale, k.accumulate, kb, ka, s))
+                    return e;
+        }
     }
-    if (!k.da) return hipSuccess;
-    const Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 511) / 512, 0};
-    const Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 511) / 512, 0};
-    return launch_outer(o, ad.rank, ad.scale, k.accumulate, kb, ka, s);
+    return k.da ? launch_join(o, ad.rank, k.accumulate, ka, kb, s) : hipSuccess;
 }
 
 }  // namespace moe
