@@ -978,9 +978,9 @@ int64_t tile_cap(int64_t rows, int count, int sh) {
 // Row blocks of a tile.  Tall ones read the adapters' matrices less often; they are
 // for many rows, where the adapters' mean rows fill most of one.  u's parts of a tile
 // have to fit LDS.
-constexpr int64_t kTallRows = 4096;
+constexpr int64_t kTallRows = 1536;
 int row_blocks(int64_t rows, int count, int rank) {
-    return rank <= 128 && rows >= kTallRows && rows >= (int64_t)96 * count ? 8 : 1;
+    return rank <= 128 && rows >= kTallRows && rows >= (int64_t)64 * count ? 8 : 1;
 }
 int64_t tile_count(const AdapterRows &o, int rank) {
     return tile_cap(o.rows, o.count, tile_shift_of(row_blocks(o.rows, o.count, rank)));
@@ -1080,7 +1080,7 @@ hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool
     const int tiles = (int)tile_cap(o.rows, o.count, sh);
     ka.blocks = tiles * ka.cb;
     kb.blocks = tiles * kb.cb;
-    return by_size(o, rank, [&](auto rb, auto nr) {
+    return by_size(o, std::min(rank, 32), [&](auto rb, auto nr) {
         const auto fn = outer_kernel<rb(), nr()>;
         const size_t lds = outer_lds(nr());
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
@@ -1106,7 +1106,7 @@ hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const Adap
             o, rank, ad.scale, sh, slots, k.accumulate, kb, ka, kx);
         return hipGetLastError();
     };
-    return rank <= 16 ? go(Int<1>()) : rank <= 32 ? go(Int<2>()) : go(Int<4>());
+    return rank <= 16 ? go(Int<1>()) : go(Int<2>());
 }
 
 hipError_t launch_join(const AdapterRows &o, int rank, bool accumulate, const Outer &ka,
@@ -1156,7 +1156,7 @@ size_t adapter_sums_bytes(int64_t rows, int count, int rank) {
         return z.p + z.e + z.q;
     };
     // (the tiles' height changes at one number of rows)
-    const int64_t edge = std::max<int64_t>(kTallRows, (int64_t)96 * count);
+    const int64_t edge = std::max<int64_t>(kTallRows, (int64_t)64 * count);
     return rows >= edge ? std::max(bytes(rows), bytes(edge - 1)) : bytes(rows);
 }
 
