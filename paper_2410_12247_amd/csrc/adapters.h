@@ -25,8 +25,8 @@ struct AdapterSums {
     int splits;
     bf16_t *e, *q;
 };
-// Their layout at an address, and its bytes (no fewer than any fewer rows need).
-AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, void *at);
+// Their layout at an address (together: how many sums share a launch), and its bytes (no fewer than any fewer rows need).
+AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, int together, void *at);
 size_t adapter_sums_bytes(int64_t rows, int count, int rank);
 
 // Bytes of the buffer of the outer products' parts over C columns (likewise).

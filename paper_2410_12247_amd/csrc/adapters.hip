@@ -384,21 +384,17 @@ __device__ __forceinline__ void cut8(const float (&v)[8], bf16x8 (&part)[S]) {
 // v[j] += the sum over splits of p[split * pitch + j * TM], four splits' loads at once.
 template <int TM>
 __device__ __forceinline__ void sum_splits(float (&v)[8], const float *p, int pitch, int splits) {
-    int q = 0;
-    for (; q + 4 <= splits; q += 4) {
+    for (int q = 0; q < splits; q += 4) {
         float w[4][8];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[i][j] = p[(q + i) * pitch + j * TM];
+            for (int j = 0; j < 8; ++j) w[i][j] = p[min(q + i, splits - 1) * pitch + j * TM];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += w[i][j];
+            for (int j = 0; j < 8; ++j) v[j] += q + i < splits ? w[i][j] : 0.f;
     }
-    for (; q < splits; ++q)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += p[q * pitch + j * TM];
 }
 
 // ---- sums, scaled and cut --------------------------------------------------
@@ -431,7 +427,7 @@ __device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const f
     const float *p = k.u.p + (int64_t)tile * k.u.splits * rank * TM;
     bf16x8 *e = reinterpret_cast<bf16x8 *>(k.u.e) + (int64_t)tile * chunks * TM;
     uint16_t *q = k.u.q + (int64_t)tile * 3 * rank * TM;
-    for (int i = threadIdx.x; i < TM * rc; i += blockDim.x) {
+    for (int i = threadIdx.x; i < TM * rc; i += 512) {
         const int row = i % TM, kc = i / TM;
         float v[8] = {};
         if (row < t.rows) {
@@ -454,7 +450,7 @@ __device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const f
     }
     // the padding behind the last part
     const int pad = chunks - rc * k.S;
-    for (int i = threadIdx.x; i < TM * pad; i += blockDim.x) {
+    for (int i = threadIdx.x; i < TM * pad; i += 512) {
         const int row = i % TM, c = rc * k.S + i / TM;
         e[((row >> 4) * chunks + c) * 16 + (row & 15)] = bf16x8{};
     }
@@ -799,8 +795,7 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                 raw[i] = *reinterpret_cast<const u32x4 *>(qr + row * k.C);
             }
         };
-        // (registers for two steps' rows; of few rows a wave has a step or two)
-        constexpr bool AHEAD = RB > 1 && NR < 4;
+        constexpr bool AHEAD = RB > 1;  // (of few rows a wave has a step or two)
         if (AHEAD && 32 * rw < t.rows) load_q(32 * rw);
         for (int k0 = 32 * rw; k0 < t.rows; k0 += 32 * KR) {
             if (!AHEAD) load_q(k0);
@@ -1080,14 +1075,17 @@ hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool
     const int tiles = (int)tile_cap(o.rows, o.count, sh);
     ka.blocks = tiles * ka.cb;
     kb.blocks = tiles * kb.cb;
-    return by_size(o, std::min(rank, 32), [&](auto rb, auto nr) {
+    auto go = [&](auto rb, auto nr) {
         const auto fn = outer_kernel<rb(), nr()>;
         const size_t lds = outer_lds(nr());
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
         fn<<<(unsigned)(ka.blocks + kb.blocks), 64 * kWaves, lds, s>>>(o, rank, scale, sh, slots,
                                                                        accumulate, kb, ka);
         return hipGetLastError();
-    });
+    };
+    if (row_blocks(o.rows, o.count, rank) == 8)
+        return rank <= 16 ? go(Int<8>(), Int<1>()) : go(Int<8>(), Int<2>());
+    return rank <= 16 ? go(Int<1>(), Int<1>()) : go(Int<1>(), Int<2>());
 }
 
 template <class Y>
@@ -1120,11 +1118,11 @@ hipError_t launch_join(const AdapterRows &o, int rank, bool accumulate, const Ou
 }
 
 // Shares of K that the sums of these rows are cut into: workgroups for every compute
-// unit at once, a step of 64 k for every wave.
-int splits_of(int64_t rows, int count, int K, int rank) {
+// unit at once, a step of 64 k for every wave.  together: sums in the same launch.
+int splits_of(int64_t rows, int count, int K, int rank, int together) {
     const int rb = row_blocks(rows, count, rank);
     const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift_of(rb)), 1);
-    const int64_t want = rb > 1 ? 512 / tiles : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
+    const int64_t want = rb > 1 ? 512 / tiles / together : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
     const int64_t most = std::max(1, K / 64 / 4);
     return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)8}));
 }
@@ -1160,10 +1158,10 @@ size_t adapter_sums_bytes(int64_t rows, int count, int rank) {
     return rows >= edge ? std::max(bytes(rows), bytes(edge - 1)) : bytes(rows);
 }
 
-AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, void *at) {
+AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, int together, void *at) {
     const SumsSize z = sums_size(rows, count, rank);
     char *p = (char *)at;
-    return {(float *)p, splits_of(rows, count, K, rank), (bf16_t *)(p + z.p),
+    return {(float *)p, splits_of(rows, count, K, rank, together), (bf16_t *)(p + z.p),
             (bf16_t *)(p + z.p + z.e)};
 }
 

@@ -106,7 +106,7 @@ moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const in
     MOE_TRY(check_at(fn, "ws", ws));
     const AdapterRows o{offsets, sorted_slot, slot_row, rows, ad.count};
     MOE_HIP(launch_adapter_rows(o, ad, x, base, y, y_type,
-                                adapter_sums(rows, ad.count, ad.rank, ad.k, ws),
+                                adapter_sums(rows, ad.count, ad.rank, ad.k, 1, ws),
                                 (hipStream_t)stream));
     return MOE_OK;
 }
@@ -160,8 +160,8 @@ moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
         return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, L.total);
     MOE_TRY(check_at(fn, "ws", ws));
     char *base = (char *)ws;
-    k.u = adapter_sums(rows, ad.count, ad.rank, ad.k, base + L.u);
-    k.v = adapter_sums(rows, ad.count, ad.rank, ad.n, base + L.v);
+    k.u = adapter_sums(rows, ad.count, ad.rank, ad.k, 2, base + L.u);
+    k.v = adapter_sums(rows, ad.count, ad.rank, ad.n, 2, base + L.v);
     k.at = (bf16_t *)(base + L.at), k.bt = (bf16_t *)(base + L.bt);
     k.pa = (float *)(base + L.pa), k.pb = (float *)(base + L.pb);
     MOE_HIP(launch_adapter_backward(o, ad, k, (hipStream_t)stream));
