@@ -24,6 +24,8 @@ struct Rules {
     int per;          // experts of a lane
     uint32_t div_E;   // i / E = i * div_E >> 20 for i < 8 E
     uint32_t div_per; // i / per = i * div_per >> 16 for i < E
+    uint32_t div_size;  // i / (E / G) likewise
+    int runs;           // groups are runs of lanes
 };
 
 // ---- one token by one wave, choices in 64 bits -------------------------------
@@ -77,14 +79,22 @@ __device__ __forceinline__ double chosen_weight(bool sigmoid, bool renorm, bool 
     return there ? s : 0.0;
 }
 
-// Token t, lane l with experts l, l + 64, l + 128, l + 192; cs, gs: room for E and G
-// doubles in LDS, this wave's.
+// By (value descending, number ascending); without a branch.
+__device__ __forceinline__ int comes_before(double o, int i, double v, int mine) {
+    return (int)(o > v) | ((int)(o == v) & (int)(i < mine));
+}
+
+// Bytes of exact_token's LDS.
+constexpr int exact_lds(int E) { return 8 * 2 * E; }
+
+// Token t, lane l with experts l, l + 64, l + 128, l + 192; lds: exact_lds(E) bytes.
 template <class Z>
 __device__ __forceinline__ void exact_token(const Rules &r, int64_t t, const Z *__restrict__ z,
                                             const float *__restrict__ bias,
                                             int32_t *__restrict__ ids, float *__restrict__ w,
-                                            double *cs, double *gs) {
+                                            void *lds) {
     const int lane = threadIdx.x & 63, E = r.E, G = r.G;
+    double *cs = static_cast<double *>(lds), *gs = cs + E;  // choices, groups' values
     float zl[4];
     uint32_t top = 0;
     bool bad = false;
@@ -178,17 +188,6 @@ __device__ __forceinline__ void exact_token(const Rules &r, int64_t t, const Z *
     }
 }
 
-template <class Z>
-__global__ __launch_bounds__(64 * kWaves) void exact_kernel(Rules r, const Z *__restrict__ z,
-                                                            const float *__restrict__ bias,
-                                                            int32_t *__restrict__ ids,
-                                                            float *__restrict__ w) {
-    __shared__ double cs[kWaves][kMaxExperts], gs[kWaves][kMaxExperts];
-    const int wave = threadIdx.x >> 6;
-    const int64_t t = (int64_t)blockIdx.x * kWaves + wave;
-    if (t < r.T) exact_token(r, t, z, bias, ids, w, cs[wave], gs[wave]);
-}
-
 // ---- several tokens by one wave ------------------------------------------------
 // A token has LT lanes (16, or 8 where there are many tokens: fewer steps across
 // lanes, twice the work of one), a lane `per` experts next to each other (at most
@@ -199,6 +198,7 @@ template <int LT, int NV>
 struct alignas(16) Tokens {
     static constexpr int N = 64 / LT, PITCH = NV + 4;
     float v[64 * PITCH];
+    static_assert(exact_lds(LT * NV) <= 4 * 64 * PITCH, "room for exact_token");
     // The place of element i of the tokens' N E.
     static __device__ __forceinline__ int at(const Rules &r, uint32_t i) {
         const uint32_t t = i * r.div_E >> 20, e = i - t * r.E, c = e * r.div_per >> 16;
@@ -436,7 +436,7 @@ __device__ __forceinline__ int before(double c, int id, double mc, int mid) {
     const double oc = __builtin_bit_cast(
         double, (uint64_t)lane32<CTRL>((uint32_t)(b >> 32)) << 32 | lane32<CTRL>((uint32_t)b));
     const int oid = (int)lane32<CTRL>((uint32_t)id);
-    return oc > mc || (oc == mc && oid < mid) ? 1 : 0;
+    return comes_before(oc, oid, mc, mid);
 }
 __device__ __forceinline__ int eight_rank(double c, int id, int l) {
     const uint64_t b = __builtin_bit_cast(uint64_t, c);
@@ -446,7 +446,7 @@ __device__ __forceinline__ int eight_rank(double c, int id, int l) {
     const int n = before<0x39>(c, id, c, id) + before<0x4E>(c, id, c, id) +
                   before<0x93>(c, id, c, id) + before<0x39>(o, oid, c, id) +
                   before<0x4E>(o, oid, c, id) + before<0x93>(o, oid, c, id) +
-                  (o > c || (o == c && oid < id) ? 1 : 0);
+                  comes_before(o, oid, c, id);
     return l < 8 ? n : l;
 }
 
@@ -467,9 +467,9 @@ __device__ __forceinline__ void run_top2(float &x, float &y, int run) {
 // and reciprocal together below 4 * 2^-24), softmax within 2^-18.7 (a sum of NV terms
 // by LT lanes: 35 roundings of 2^-24 at most, and the terms' own), the bias' addition
 // 2^-22, the key's step 2^-23.
-// Groups are whole runs of lanes: G divides LT, and LT the experts.
+// Groups are best as whole runs of lanes: G divides LT, and LT the experts.
 template <int LT, int NV, class Z, bool ALIGNED>
-__global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *__restrict__ z,
+__global__ __launch_bounds__(64 * kWaves, 4) void scores_kernel(Rules r, const Z *__restrict__ z,
                                                              const float *__restrict__ bias,
                                                              int32_t *__restrict__ ids,
                                                              float *__restrict__ w) {
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
         for (int i = 0; i < NV; ++i) sum += exp_near((double)v[i] - zmax);
         sum = sum_f64<LT>(sum);
     }
-    float s[NV];
+    float s[NV] = {};
     if (by_score) {
         if (r.sigmoid) {
 #pragma unroll
@@ -553,31 +553,86 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
                 if (v[i] == -INFINITY) s[i] = -INFINITY;
         }
     }
-    bool keep = true;
+    bool keep = true;  // all of a lane's experts
     if (groups) {
-        const int run = LT / r.G;  // lanes of a group
-        float x = -INFINITY, y = -INFINITY;  // the two largest
-        if (by_score) {
+        const int run = r.runs ? LT / r.G : 1;  // lanes of a group
+        float in, out;  // the worst group kept, the best one left out
+        int kept;
+        if (r.runs) {
+            float x = -INFINITY, y = -INFINITY;  // the two largest
+            if (by_score) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    y = __builtin_amdgcn_fmed3f(x, y, s[i]);
+                    x = fmaxf(x, s[i]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) x = fmaxf(x, v[i]);
+            }
+            run_top2(x, y, run);
+            if (r.pair && y > -INFINITY) x += y;
+            const int rank = lanes_above<LT>(x);  // (by every lane)
+            keep = x > -INFINITY && rank < r.top_groups * run;
+            in = -max_f32<LT>(keep ? -x : -INFINITY);
+            out = max_f32<LT>(keep ? -INFINITY : x);
+            kept = __popc(lanes_true<LT>(keep));
+        } else {
+            // any groups: through LDS, a lane takes every LT-th; a group's value, then
+            // whether it is kept, lies at its first expert
+            const int size = r.E / r.G, first = lane / LT * r.E;
+            float *own = q.v + lane * Q::PITCH;
+            if (by_score) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) own[i] = s[i];
+                wave_sync();
+            }
+            const int mine = (r.G - l + LT - 1) / LT;  // at most 32
+            float low = INFINITY, high = -INFINITY;
+            int n_kept = 0;
+            for (int j = 0; j < mine; ++j) {
+                const int at = first + (l + j * LT) * size;
+                float x = -INFINITY, y = -INFINITY;
+                for (int i = 0; i < size; ++i) {
+                    const float c = q.v[Q::at(r, at + i)];
+                    y = fmaxf(y, fminf(x, c));
+                    x = fmaxf(x, c);
+                }
+                if (r.pair && y > -INFINITY) x += y;
+                q.v[Q::at(r, at)] = x;
+            }
+            wave_sync();
+            uint32_t keeps = 0;  // bit j: the lane's j-th group
+            for (int j = 0; j < mine; ++j) {
+                const float x = q.v[Q::at(r, first + (l + j * LT) * size)];
+                int above = 0;
+                for (int g = 0; g < r.G; ++g) above += q.v[Q::at(r, first + g * size)] > x;
+                const bool k = x > -INFINITY && above < r.top_groups;
+                keeps |= (uint32_t)k << j;
+                n_kept += k;
+                low = fminf(low, k ? x : INFINITY);
+                high = fmaxf(high, k ? -INFINITY : x);
+            }
+            wave_sync();
+            for (int j = 0; j < mine; ++j)
+                q.v[Q::at(r, first + (l + j * LT) * size)] = keeps >> j & 1 ? 1.f : 0.f;
+            wave_sync();
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                y = __builtin_amdgcn_fmed3f(x, y, s[i]);
-                x = fmaxf(x, s[i]);
+                const uint32_t e = min(l * r.per + i, r.E - 1);
+                const float k = q.v[Q::at(r, first + (e * r.div_size >> 16) * size)];
+                v[i] = k != 0.f ? v[i] : -INFINITY;
+                s[i] = k != 0.f ? s[i] : -INFINITY;
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) x = fmaxf(x, v[i]);
+            in = -max_f32<LT>(-low);
+            out = max_f32<LT>(high);
+            kept = (int)sum_f32<LT>((float)n_kept);
         }
-        run_top2(x, y, run);
-        if (r.pair && y > -INFINITY) x += y;
-        const int rank = lanes_above<LT>(x);  // (by every lane)
-        keep = x > -INFINITY && rank < r.top_groups * run;
-        const float in = -max_f32<LT>(keep ? -x : -INFINITY);
-        const float out = max_f32<LT>(keep ? -INFINITY : x);
         // a group's value (two choices and their sum) is within 2^-17.5, of sigmoids
         // 2^-19.6; logits are exact
         const float gap = r.sigmoid ? 0x1p-18f : 0x1p-16f;
         bad |= out > -INFINITY && !(by_score ? in - out > gap : in > out);
-        bad |= __popc(lanes_true<LT>(keep)) > r.top_groups * run;  // equal ones
+        bad |= kept > r.top_groups * run;  // equal ones
     }
     // keys: steps below the largest, of 2^-23 for choices, of 2^-21 for logits, whose
     // differences are within half a step; bf16 logits keep their own bits
@@ -605,7 +660,7 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) key[i] = (key[i] << 8) + (uint32_t)(l * r.per) + i;
-    if (masks || bias) {
+    if (masks || bias || !r.runs) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (v[i] == -INFINITY) key[i] = ~0u;
@@ -626,7 +681,8 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
     for (int i = 0; i < 8; ++i) mine = l == i ? a[i] : mine;
     const bool found = l < 8 && mine < kNone;
     const uint32_t e = found ? mine & 255u : 0u;
-    const float z_at = q.v[Q::at(r, lane / LT * r.E + e)];
+    const float z_at = r.runs ? q.v[Q::at(r, lane / LT * r.E + e)]
+                              : logit_at(z, min(t, r.T - 1) * r.E + e);
     int rank = l;
     if (!bits) {
         const uint32_t gap = (bias ? (r.sigmoid ? 12u : 65u) : 4u) << 8;
@@ -662,8 +718,7 @@ __global__ __launch_bounds__(64 * kWaves) void scores_kernel(Rules r, const Z *_
 #pragma unroll 1
     for (int i = 0; i < Q::N; ++i)
         if (redo >> (LT * i) & 1)
-            exact_token(r, t0 + i, z, bias, ids, w, reinterpret_cast<double *>(q.v),
-                        reinterpret_cast<double *>(q.v) + r.E);
+            exact_token(r, t0 + i, z, bias, ids, w, q.v);
 }
 
 // ---- gradient ---------------------------------------------------------------
@@ -838,6 +893,9 @@ Rules with_lanes(Rules r, int lanes) {
     r.per = (r.E + lanes - 1) / lanes;
     r.div_E = ((1u << 20) + r.E - 1) / r.E;
     r.div_per = ((1u << 16) + r.per - 1) / r.per;
+    const int size = r.E / r.G;
+    r.div_size = ((1u << 16) + size - 1) / size;
+    r.runs = r.G == 1 || (lanes % r.G == 0 && r.E % lanes == 0);
     return r;
 }
 
@@ -863,13 +921,11 @@ unsigned grid_of(const Rules &r, int tokens) {  // of a wave
     return (unsigned)((r.T + kWaves * tokens - 1) / (kWaves * tokens));
 }
 
-// Whether G groups are runs of the lanes.
-bool runs(const Rules &r, int lanes) { return r.G == 1 || (lanes % r.G == 0 && r.E % lanes == 0); }
-
 template <class Z>
 hipError_t launch_scores(Rules r, const Z *z, const float *bias, int32_t *ids, float *w,
                          hipStream_t s) {
-    if (r.T >= kManyTokens && r.E > 64 && runs(r, 8) && aligned4(z)) {
+    const bool runs16 = with_lanes(r, 16).runs;
+    if (r.T >= kManyTokens && r.E > 64 && aligned4(z) && (with_lanes(r, 8).runs || !runs16)) {
         r = with_lanes(r, 8);
         auto go = [&](auto nv) {
             scores_kernel<8, nv(), Z, true><<<grid_of(r, 8), 64 * kWaves, 0, s>>>(r, z, bias, ids,
@@ -878,16 +934,11 @@ hipError_t launch_scores(Rules r, const Z *z, const float *bias, int32_t *ids, f
         };
         return r.per <= 16 ? go(Int<16>()) : r.per <= 20 ? go(Int<20>()) : go(Int<32>());
     }
-    if (runs(r, 16)) {
-        r = with_lanes(r, 16);
-        return by_size(r, aligned4(z), [&](auto nv, auto al) {
-            scores_kernel<16, nv(), Z, al()><<<grid_of(r, 4), 64 * kWaves, 0, s>>>(r, z, bias, ids,
-                                                                                   w);
-            return hipGetLastError();
-        });
-    }
-    exact_kernel<Z><<<grid_of(r, 1), 64 * kWaves, 0, s>>>(r, z, bias, ids, w);
-    return hipGetLastError();
+    r = with_lanes(r, 16);
+    return by_size(r, aligned4(z), [&](auto nv, auto al) {
+        scores_kernel<16, nv(), Z, al()><<<grid_of(r, 4), 64 * kWaves, 0, s>>>(r, z, bias, ids, w);
+        return hipGetLastError();
+    });
 }
 
 template <class Z>
