@@ -499,7 +499,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scores_kernel(Rules r, const Z
     }
     zmax = max_f32<LT>(zmax);
     const bool masks = __ballot(odd != 0.f) != 0;
-    bool bad = !(fabsf(zmax) < 0x1p100f);  // infinite, or far enough to overflow
+    // infinite, or so large that the exponent's rounding (of the size of zmax) overflows
+    bool bad = !(fabsf(zmax) < 0x1p24f);
     if (masks) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) bad |= v[i] != v[i];
@@ -632,6 +633,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scores_kernel(Rules r, const Z
         // 2^-19.6; logits are exact
         const float gap = r.sigmoid ? 0x1p-18f : 0x1p-16f;
         bad |= out > -INFINITY && !(by_score ? in - out > gap : in > out);
+        // (logits so far out that 64 bits hold the same score for several)
+        if (!by_score)
+            bad |= out > -INFINITY &&
+                   (r.sigmoid ? out > 20.f || in < -700.f : in < zmax - 700.f);
         bad |= kept > r.top_groups * run;  // equal ones
     }
     // keys: steps below the largest, of 2^-23 for choices, of 2^-21 for logits, whose
@@ -852,8 +857,16 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
     }
 }
 
-moe_status check_routing(const char *fn, const moe_dims *d, const moe_routing *r, int32_t type) {
+// Sixteen lanes a token, of 2^32 in a launch.
+moe_status check_tokens(const char *fn, const moe_dims *d) {
     MOE_TRY(check_dims(d));
+    return d->tokens < (int64_t(1) << 28)
+               ? MOE_OK
+               : fail(MOE_ERR_UNSUPPORTED, "%s: 2^28 tokens or more", fn);
+}
+
+moe_status check_routing(const char *fn, const moe_dims *d, const moe_routing *r, int32_t type) {
+    MOE_TRY(check_tokens(fn, d));
     if (!r) return fail(MOE_ERR_INVALID, "%s: routing is NULL", fn);
     if (r->score != MOE_SCORE_SOFTMAX && r->score != MOE_SCORE_SIGMOID)
         return fail(MOE_ERR_INVALID, "%s: score %d", fn, r->score);
@@ -961,7 +974,7 @@ extern "C" {
 moe_status moe_route_logits(const moe_dims *dims, const moe_bf16 *x, const float *w_router,
                             float *logits, void *stream) {
     const char *fn = "moe_route_logits";
-    MOE_TRY(check_dims(dims));
+    MOE_TRY(check_tokens(fn, dims));
     if (dims->tokens == 0) return MOE_OK;
     MOE_TRY(check_at(fn, "x", x, 16));
     MOE_TRY(check_at(fn, "w_router", w_router, 4));

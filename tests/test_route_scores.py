@@ -48,6 +48,7 @@ def test_refusals(backward):
         assert call(**b) == 1, (b, last())
     assert call(d=moe.dims(5, 64, 64, 257, 3)) == 2
     assert call(d=moe.dims(5, 64, 64, 12, 9)) == 2
+    assert call(d=moe.dims(1 << 28, 64, 64, 12, 3)) == 2
     assert call(d=moe.dims(0, 64, 64, 12, 3), z=None, ids=None, w=None, dz=None) == 0
 
 
@@ -219,6 +220,29 @@ def test_rows_with_little_left(sigmoid, renorm):
 
 @gpu
 @pytest.mark.parametrize("sigmoid", [False, True], ids=["softmax", "sigmoid"])
+def test_large_logits(sigmoid):
+    """Logits from 2^20 to 2^100, where a product with log2(e) is rounded by more than
+    the exponent's range."""
+    E, k = 96, 6
+    z = make(13, 81, E, F32).cpu()
+    z *= (2.0 ** torch.arange(20, 101)).float()[:, None]
+    z[::2, 1:] = make(14, 41, E - 1, F32).cpu()  # one large beside ordinary ones
+    z[::4, 0] = z[::4, 0].abs()
+    for T in (81, 81 * 203):
+        zt = z.repeat(T // 81, 1).cuda()
+        for dtype in (F32, BF16):
+            for bias in (None, torch.linspace(0.1, -0.1, E).cuda()):
+                for G, top, pair in ((1, 1, False), (8, 3, False), (8, 3, True)):
+                    rules = dict(sigmoid=sigmoid, groups=G, top_groups=top, pair=pair,
+                                 renorm=True, scale=1.0)
+                    ids, w = check(zt[:81].to(dtype), bias, k, **rules)
+                    ids2, w2 = run(zt.to(dtype), bias, k, **rules)
+                    assert torch.equal(ids2, ids.repeat(T // 81, 1))
+                    assert torch.equal(w2, w.repeat(T // 81, 1))
+
+
+@gpu
+@pytest.mark.parametrize("sigmoid", [False, True], ids=["softmax", "sigmoid"])
 def test_infinities_and_nan(sigmoid):
     E, k = 40, 3
     z = make(11, 8, E, F32).cpu()
@@ -311,6 +335,24 @@ def test_any_address(dtype):
                 assert (t[:off] == -9).all() and (t[off + 19 * k:] == -9).all()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_many_tokens_at_any_address(dtype):
+    """The same choices and weights where rows do not load four at a time."""
+    T, E, k = 16390, 160, 6
+    z = make(15, T, E, dtype)
+    flat = torch.zeros(T * E + 8, dtype=dtype, device="cuda")
+    zo = flat[1:1 + T * E].view(T, E)
+    zo.copy_(z)
+    for sigmoid, renorm in ((True, True), (False, False)):
+        rules = dict(sigmoid=sigmoid, groups=8, top_groups=3, pair=True, renorm=renorm, scale=2.0)
+        want, got = run(z, None, k, **rules), run(zo, None, k, **rules)
+        assert torch.equal(got[0], want[0])
+        assert ((got[1] - want[1]).abs() <= 2.0 ** -23 * want[1]).all()
+        rid, _ = ref.route(z[:40].double().cpu().numpy(), None, k, **rules)
+        np.testing.assert_array_equal(got[0][:40].cpu().numpy(), rid)
+
+
 # ---- gradient ---------------------------------------------------------------
 
 
@@ -388,6 +430,26 @@ def test_gradient_is_the_difference_quotient(sigmoid, renorm):
             q = (hi - lo) @ dw[t].double().cpu().numpy() / 2e-5
             # h^2 of the differences, 2^-52 / h of their rounding, 2^-20 |G| of the kernel
             assert abs(q - dz[t, e]) < 1e-9 + 2.0 ** -20 * 1.5 * float(dw[t].abs().max())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("renorm", [False, True], ids=["raw", "renorm"])
+def test_gradient_at_any_address(dtype, renorm):
+    """Logits and their gradient at any address of their type; the elements around stay."""
+    for E, k in ((7, 3), (64, 6), (161, 5), (256, 8)):
+        z = make(E, 19, E, dtype)
+        ids, _ = run(z, None, k, False, 1, 1, False, renorm, 1.0)
+        dw = torch.randn((19, k), generator=torch.Generator().manual_seed(E)).cuda()
+        want = back(z, ids, dw, False, renorm, 1.0)
+        d = moe.dims(19, 64, 64, E, k, renormalize=renorm)
+        for a, b in ((1, 0), (0, 3), (2, 1)):
+            flat = torch.full((2, 19 * E + 8), 5.0, dtype=dtype, device="cuda")
+            zo, dz = (flat[i, o:o + 19 * E].view(19, E) for i, o in ((0, a), (1, b)))
+            zo.copy_(z)
+            moe.route_scores_backward(d, moe.routing(), zo, ids, dw, dz)
+            assert torch.equal(dz, want)
+            assert (flat[1, :b] == 5).all() and (flat[1, b + 19 * E:] == 5).all()
 
 
 @gpu
