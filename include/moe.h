@@ -599,7 +599,8 @@ moe_status moe_route_logits(const moe_dims *dims, const moe_bf16 *x, const float
  * are -1 with weight 0 (moe_permute and moe_combine pass over them).  A token with
  * a NaN logit, or with +inf under softmax, has NaN weights, and its experts are
  * the k largest logits of all groups, a NaN as the largest.
- * dims gives tokens, experts, top_k and renormalize; the rest is not used. */
+ * dims gives tokens (fewer than 2^28), experts, top_k and renormalize; the rest is
+ * not used. */
 moe_status moe_route_scores(const moe_dims *dims, const moe_routing *routing, const void *logits,
                             int32_t logits_type, const float *bias, int32_t *topk_ids,
                             float *topk_w, void *stream);
@@ -624,9 +625,13 @@ moe_status moe_route_scores_backward(const moe_dims *dims, const moe_routing *ro
  * Tensors must be 16-byte aligned, scale and index tensors 4-byte aligned.  The
  * calls allocate nothing, never synchronise and can be captured; a workspace
  * (16-byte aligned) serves one call at a time, and one for some rows serves fewer
- * too.  Results are deterministic; their bits depend on rows and count (which
- * pick the tiles), not on the other rows' adapters.  Offsets outside [0, rows] are
- * cut to it, and entries of sorted_slot outside [0, rows) are passed over. */
+ * too.  Outputs overlap no input but base and dx_base as said below.  Results are
+ * deterministic; their bits depend on rows and count (which pick the tiles), not on
+ * the other rows' adapters.  An infinity stays in the outputs that its formula
+ * reaches, as an infinity or NaN.  Offsets outside [0, rows] are cut to it, and
+ * entries of sorted_slot outside [0, rows) are passed over: their rows take no part.
+ * Rows and widths that need 2^32 lanes in a launch (some 5 10^10 values of y) are
+ * MOE_ERR_UNSUPPORTED. */
 
 /* Host memory; its pointers are device ones. */
 typedef struct {

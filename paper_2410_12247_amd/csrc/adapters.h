@@ -25,9 +25,14 @@ struct AdapterSums {
     int splits;
     bf16_t *e, *q;
 };
-// Their layout at an address (together: how many sums share a launch), and its bytes (no fewer than any fewer rows need).
+// Their layout at an address (together: how many sums share a launch), and its bytes
+// (no fewer than any fewer rows need).
 AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, int together, void *at);
 size_t adapter_sums_bytes(int64_t rows, int count, int rank);
+
+// Whether every launch of these rows and widths (both directions') is one the device
+// takes.
+bool adapter_launches_fit(int64_t rows, const moe_adapters &ad);
 
 // Bytes of the buffer of the outer products' parts over C columns (likewise).
 size_t adapter_parts_bytes(int64_t rows, int rank, int C);

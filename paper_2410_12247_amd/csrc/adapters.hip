@@ -87,6 +87,7 @@ __device__ __forceinline__ Tile find_tile(const AdapterRows &o, int sh, int t) {
     r.tiles = (z - f + TM - 1) >> sh;
     r.first = f + ((int64_t)r.index << sh);
     r.rows = min(TM, (int)(z - r.first));
+    if (r.rows <= 0) r.e = -1;  // (offsets out of order over so many rows that sums wrapped)
     return r;
 }
 
@@ -430,7 +431,7 @@ __device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const f
     for (int i = threadIdx.x; i < TM * rc; i += 512) {
         const int row = i % TM, kc = i / TM;
         float v[8] = {};
-        if (row < t.rows) {
+        if (row < t.rows && row_at(o, t.first + row) >= 0) {
             sum_splits<TM>(v, p + 8 * kc * TM + row, rank * TM, k.u.splits);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= f;
@@ -783,15 +784,18 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
     const bf16_t *qr = k.q + qc;
     for (int grp = 0; grp < groups; ++grp) {
         const int r0 = grp * 16 * NR;
-        for (int i = threadIdx.x; i < t.rows; i += 64 * kWaves)
-            rows[i] = max(row_at(o, t.first + i), 0);
-        __syncthreads();
+        bool none = false;
+        for (int i = threadIdx.x; i < t.rows; i += 64 * kWaves) {
+            rows[i] = row_at(o, t.first + i);
+            none |= rows[i] < 0;
+        }
+        none = __syncthreads_or(none);
         floatx4 acc[NR][8] = {};
         u32x4 raw[8];
         auto load_q = [&](int k0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int64_t row = rows[min(k0 + 8 * g + i, t.rows - 1)];
+                const int64_t row = max(rows[min(k0 + 8 * g + i, t.rows - 1)], 0);
                 raw[i] = *reinterpret_cast<const u32x4 *>(qr + row * k.C);
             }
         };
@@ -823,6 +827,11 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                         pv[b][s] = *reinterpret_cast<const floatx4 *>(src + s * rank * TM);
                 }
             }
+            if (none) {  // (p has zeros for those: for an infinity of row 0's)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (rows[min(k0 + 8 * g + i, t.rows - 1)] < 0) raw[i] = u32x4{};
+            }
             bf16x8 qv[8];
             transpose8(raw, qv);
             if (AHEAD && k0 + 32 * KR < t.rows) load_q(k0 + 32 * KR);
@@ -834,7 +843,10 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                     float v[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        v[i] = k0 + 8 * g + i < t.rows ? pv[b][i / 4][i % 4] * f : 0.f;
+                        v[i] = k0 + 8 * g + i < t.rows &&
+                                       !(none && rows[k0 + 8 * g + i] < 0)
+                                   ? pv[b][i / 4][i % 4] * f
+                                   : 0.f;
                     cut8<3>(v, part);
                 } else {
                     // (a tile's rows behind its last are zeros; eights behind that: no tile's)
@@ -1122,9 +1134,19 @@ hipError_t launch_join(const AdapterRows &o, int rank, bool accumulate, const Ou
 int splits_of(int64_t rows, int count, int K, int rank, int together) {
     const int rb = row_blocks(rows, count, rank);
     const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift_of(rb)), 1);
-    const int64_t want = rb > 1 ? 512 / tiles / together : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
+    const int64_t want =
+        rb > 1 ? 512 / tiles / together : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
     const int64_t most = std::max(1, K / 64 / 4);
     return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)8}));
+}
+
+// Blocks of 512 threads at most that a launch of expand, or of outer over both
+// matrices, has.
+int64_t expand_cap(int64_t rows, int64_t tiles, int N) {
+    return (tiles + (rows + 63) / 64) * ((N / 64 + kExpandSpan - 1) / kExpandSpan);
+}
+int64_t outer_cap(int64_t rows, int count, int n, int k) {
+    return tile_cap(rows, count, outer_shift(rows)) * ((n + 511) / 512 + (k + 511) / 512);
 }
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
@@ -1147,6 +1169,18 @@ SumsSize sums_size(int64_t rows, int count, int rank) {
 }
 
 }  // namespace
+
+bool adapter_launches_fit(int64_t rows, const moe_adapters &ad) {
+    const int rb = row_blocks(rows, ad.count, ad.rank);
+    const int64_t tiles = tile_cap(rows, ad.count, tile_shift_of(rb));
+    // two sums' blocks, those of few tiles in several shares of K
+    const int64_t shrink = std::max<int64_t>(tiles, 1024) * 2 * ((ad.rank + 63) / 64);
+    const int64_t both = expand_cap(rows, tiles, std::max(ad.n, ad.k)) +
+                         outer_cap(rows, ad.count, ad.n, ad.k);
+    // (its workgroups have half the threads)
+    const int64_t turn = (int64_t)ad.count * ((ad.rank + 63) / 64) * (ad.n / 64 + ad.k / 64) / 2;
+    return std::max({shrink, both, turn}) * 64 * kWaves < int64_t(1) << 32;
+}
 
 size_t adapter_sums_bytes(int64_t rows, int count, int rank) {
     auto bytes = [&](int64_t r) {

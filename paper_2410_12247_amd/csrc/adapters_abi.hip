@@ -32,6 +32,9 @@ moe_status check_adapters(const char *fn, int64_t rows, const moe_adapters *ad) 
     if (!width_ok(ad->n) || !width_ok(ad->k))
         return fail(MOE_ERR_INVALID, "%s: widths %d, %d not multiples of %d up to 2^20", fn, ad->n,
                     ad->k, kDimAlign);
+    if (!adapter_launches_fit(rows, *ad))
+        return fail(MOE_ERR_UNSUPPORTED, "%s: %lld rows of %d and %d values need 2^32 lanes", fn,
+                    (long long)rows, ad->n, ad->k);
     return MOE_OK;
 }
 

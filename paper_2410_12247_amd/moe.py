@@ -635,7 +635,6 @@ def adapters(a, b, scale=None) -> Adapters:
                   _arg(dev, "b", b, _BF16, (C, N, r)), _arg(dev, "scale", scale, _F32, (C,)))
     ad.keep = (a, b, scale)
     ad.device = dev
-    ad.ref = ctypes.byref(ad)
     return ad
 
 
@@ -653,7 +652,7 @@ def _adapter_args(ad, dev, R, offsets, sorted_slot, slot_row):
         raise ValueError(f"the adapters are on cuda:{ad.device}, the rows on cuda:{dev}")
     if slot_row is not None and slot_row.dim() != 1:
         slot_row = slot_row.view(-1)
-    return (ad.ref, _arg(dev, "offsets", offsets, _I32, (ad.count + 1,)),
+    return (ctypes.byref(ad), _arg(dev, "offsets", offsets, _I32, (ad.count + 1,)),
             _arg(dev, "sorted_slot", sorted_slot, _I32, (R,)),
             _arg(dev, "slot_row", slot_row, _I32, (R,)))
 

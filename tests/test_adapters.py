@@ -2,6 +2,7 @@
 gradient, through the Python binding against 64 bits; what the calls refuse; a
 layer with adapters beside its products."""
 import ctypes
+import weakref
 
 import pytest
 import torch
@@ -66,6 +67,12 @@ def test_refusals():
               dict(y=ODD), dict(t=2), dict(t=-1), dict(ws=ODD), dict(base=None, place=None)):
         assert call(**b) == 1, (b, last())
     assert call(rows=1 << 31) == 2
+    # 2^32 lanes and more in a launch
+    wide = handle(rank=136, n=1 << 20, k=64)
+    assert call(rows=1 << 17, ad=wide) == 2 and call(rows=1 << 15, ad=wide) == 3
+    assert call(ad=handle(count=256, rank=256, n=1 << 20, k=1 << 20)) == 2
+    assert call(rows=1 << 29) == 2 and call(rows=(1 << 31) - 1, ad=handle(rank=8, n=64)) == 2
+    assert L.moe_adapter_workspace_bytes(1 << 17, ctypes.byref(wide)) == 0
     assert call(size=need - 1) == 3 and call(ws=None) == 3
     assert call(rows=0, off=None, order=None, x=None, y=None, ws=None) == 0
 
@@ -213,6 +220,33 @@ def test_rows(shape, dtype):
     z = forward(p, None, dtype)
     check_forward(p, z, None)
     # in place: the same bits, rows without an adapter as they were
+    w = base.clone()
+    forward(p, w, dtype, y=w, place=False)
+    assert torch.equal(w, y)
+
+
+# Many rows, in taller tiles: rows, n, k, rank, count, skewed (few adapters of many rows)
+MANY = [(1535, 192, 128, 32, 3, False), (1536, 64, 64, 8, 24, False), (1536, 128, 64, 16, 25, True),
+        (1537, 576, 320, 24, 24, True), (1663, 64, 448, 32, 1, True), (1792, 1344, 64, 40, 5, False),
+        (2047, 128, 576, 64, 7, True), (2048, 448, 1344, 72, 3, False), (2500, 704, 704, 128, 2, True),
+        (3001, 64, 1024, 136, 4, True), (4095, 512, 128, 16, 60, True), (4097, 128, 512, 120, 9, True),
+        (9000, 192, 192, 48, 1, False), (9001, 64, 4160, 64, 128, True)]
+
+
+def many(shape, seed=0):
+    R, n, k, rank, count, skew = shape
+    return Problem(R + seed, R, n, k, rank, count, pick(R, R, count, 0.1, skew))
+
+
+@gpu
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_many_rows(shape, dtype):
+    p = many(shape)
+    base = p.normal(1, p.n, dtype)
+    y = forward(p, base, dtype)
+    check_forward(p, y, base)
+    check_forward(p, forward(p, None, dtype), None)
     w = base.clone()
     forward(p, w, dtype, y=w, place=False)
     assert torch.equal(w, y)
@@ -407,6 +441,52 @@ def test_gradients(shape, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_gradients_of_tall_tiles(shape, dtype):
+    p = many(shape, 1)
+    base = p.normal(1, p.k, dtype)
+    dx, da, db = grads(p, dtype)
+    backward(p, base, dx, da, db)
+    check_backward(p, base, dx, da, db)
+    w = base.clone()
+    backward(p, w, w, None, None)
+    assert torch.equal(w, dx)
+    da2, db2 = torch.full_like(da, 9.0), torch.full_like(db, 9.0)
+    backward(p, None, None, da2, db2)
+    assert torch.equal(da, da2) and torch.equal(db, db2)
+    da0, db0 = torch.randn_like(da), torch.randn_like(db)
+    da2.copy_(da0), db2.copy_(db0)
+    backward(p, None, dx, da2, db2, accumulate=True)
+    check_backward(p, None, dx, da2, db2, da0, db0)
+
+
+@gpu
+@pytest.mark.parametrize("R", [90, 2100])
+def test_gradients_pass_over_bad_rows(R):
+    """Entries of sorted_slot outside the rows take no part in da and db, whatever
+    row 0 holds."""
+    p = Problem(17, R, 192, 128, 16, 3)
+    off, slot, row = p.order
+    bad = torch.arange(3, int((p.ids >= 0).sum()), 11, device="cuda")
+    worse = slot.clone()
+    worse[bad] = torch.tensor([-1, R, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32,
+                              device="cuda").repeat(len(bad))[:len(bad)]
+    keep = p.ids.clone()
+    keep[slot[bad].long()] = -1
+    if keep[0] >= 0:  # row 0 takes no part
+        worse[torch.nonzero(slot[:off[-1]] == 0)[0, 0]] = keep[0] = -1
+    for e in (float("nan"), 1.0):
+        p.x[0] = p.dy[0] = e
+        p.order = (off, worse, row)
+        da, db = grads(p, F32)[1:]
+        backward(p, None, None, da, db)
+        p.ids, was = keep, p.ids
+        check_backward(p, None, None, da, db)
+        p.ids = was
+
+
+@gpu
 @pytest.mark.parametrize("R,count", [(5000, 1), (4096, 3), (1537, 2)])
 def test_gradients_of_many_rows(R, count):
     """Adapters whose rows are cut into several sums, beside some with one or none."""
@@ -490,6 +570,65 @@ def test_other_stream_and_captured_graph():
         backward(p, None, dx2, da2, db2)
         torch.cuda.synchronize()
         assert torch.equal(dx, dx2) and torch.equal(da, da2) and torch.equal(db, db2)
+
+
+@gpu
+def test_many_rows_captured_and_beside_another_call():
+    """Two calls at once on streams and workspaces of their own; both captured."""
+    p, q = many((2300, 320, 576, 32, 7, True)), many((1700, 576, 320, 96, 2, False))
+    want = [forward(p, None, F32), *grads(p, BF16), forward(q, None, BF16), *grads(q, F32)]
+    backward(p, None, *want[1:4])
+    backward(q, None, *want[5:8])
+    got = [torch.full_like(t, 9.0) for t in want]
+    ws = [torch.full((moe.adapter_backward_bytes(t.R, t.ad),), 0xFF, dtype=torch.uint8,
+                     device="cuda") for t in (p, q)]
+
+    def run(stream=None):
+        forward(q, None, BF16, y=got[4], ws=ws[1], stream=stream)
+        backward(q, None, *got[5:8], ws=ws[1], stream=stream)
+        forward(p, None, F32, y=got[0], ws=ws[0], stream=torch.cuda.current_stream())
+        backward(p, None, *got[1:4], ws=ws[0], stream=torch.cuda.current_stream())
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    run(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        run(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for i in range(3):
+        for t in got:
+            t.fill_(float(i))
+        for w in ws:
+            w.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@gpu
+def test_adapters_are_let_go():
+    """A handle keeps its tensors while it lives, and no longer."""
+    a, b = (torch.zeros(s, dtype=BF16, device="cuda") for s in ((2, 8, 64), (2, 64, 8)))
+    ad, seen = moe.adapters(a, b), weakref.ref(a)
+    del a, b
+    assert seen() is not None
+    del ad
+    assert seen() is None
+
+
+@gpu
+def test_gradient_without_x():
+    p = Problem(24, 20, 128, 64, 16, 2)
+    dx = grads(p, BF16)[0]
+    backward(p, None, dx, None, None)
+    p.x, x = None, p.x
+    dx2 = torch.zeros_like(dx)
+    backward(p, None, dx2, None, None)
+    assert torch.equal(dx, dx2)
+    with pytest.raises(moe.MoEError):
+        backward(p, None, dx2, *grads(p, BF16)[1:])
 
 
 @gpu
