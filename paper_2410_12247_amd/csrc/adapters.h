@@ -42,8 +42,7 @@ hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, con
                                const void *base, void *y, int y_type, const AdapterSums &u,
                                hipStream_t s);
 
-// Its gradient; dx, or da and db, may be NULL.  at, bt: room for the transposed
-// matrices; pa, pb: the parts of da and db.
+// Its gradient; dx, or da and db, may be NULL.  pa, pb: the parts of da and db.
 struct AdapterBack {
     const bf16_t *x, *dy;
     const void *base;
@@ -52,7 +51,6 @@ struct AdapterBack {
     float *da, *db;
     bool accumulate;
     AdapterSums u, v;
-    bf16_t *at, *bt;
     float *pa, *pb;
 };
 hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,

@@ -39,6 +39,29 @@ __device__ __forceinline__ bf16x8 load8(const bf16_t *base, uint32_t off) {
     return *reinterpret_cast<const bf16x8 *>(reinterpret_cast<const char *>(base) + off);
 }
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) {
+    return __builtin_amdgcn_perm(b, a, 0x05040100u);
+}
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) {
+    return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+// Four values of each of two rows `pitch` apart.
+__device__ __forceinline__ bf16x8 load_pair(const bf16_t *p, int pitch) {
+    const u32x2 a = *reinterpret_cast<const u32x2 *>(p);
+    const u32x2 b = *reinterpret_cast<const u32x2 *>(p + pitch);
+    return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+}
+// The two of each column to word `at` of an operand in LDS, the next column's `step`
+// words behind.
+__device__ __forceinline__ void put_pair(bf16x8 *to, int at, int step, bf16x8 pair) {
+    const u32x4 u = __builtin_bit_cast(u32x4, pair);
+    uint32_t *p = reinterpret_cast<uint32_t *>(to) + at;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        p[q * step] = q & 1 ? high_halves(u[q / 2], u[2 + q / 2]) : low_halves(u[q / 2], u[2 + q / 2]);
+}
+
 // One tile: adapter e's places [first, first + rows), the tile's number among
 // the adapter's `tiles`, and the tiles of several-tile adapters before it.
 struct Tile {
@@ -99,8 +122,8 @@ __device__ __forceinline__ int row_at(const AdapterRows &o, int64_t place) {
 
 // ---- x A^T ---------------------------------------------------------------
 
-// Sums of `rows` times w [count][rank][K].  The matrix instruction's M is the
-// rows, its N the rank.
+// Sums of `rows` times w [count][rank][K], or where TURNED [count][K][rank] (the
+// gradient's).  The matrix instruction's M is the rows, its N the rank.
 struct Shrink {
     const bf16_t *x, *w;
     AdapterSums out;
@@ -109,11 +132,12 @@ struct Shrink {
 
 // Short tiles: operands straight to registers, 64 bytes of each of 16 rows a load.
 // The four waves (and `splits` workgroups) share K, each taking every so many-th 128
-// bytes of a row, and keep DEP steps of them in flight.
-template <int NR>
+// bytes of a row, and keep DEP steps of them in flight.  A turned w comes a value a
+// lane: a load has 16 rank values of four k, side by side where the rank is 16.
+template <int NR, bool TURNED>
 __device__ __forceinline__ void shrink_short(const AdapterRows &o, int rank, const Shrink &k,
                                              int tile, int split, int r0, floatx4 *lds) {
-    constexpr int DEP = NR <= 2 ? 4 : 2, KG = shrink_waves(1);
+    constexpr int DEP = NR == 1 || (NR == 2 && !TURNED) ? 4 : 2, KG = shrink_waves(1);
     const Tile t = find_tile(o, tile_shift_of(1), tile);
     if (t.e < 0) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
@@ -124,11 +148,15 @@ __device__ __forceinline__ void shrink_short(const AdapterRows &o, int rank, con
     uint32_t wo[NR];
 #pragma unroll
     for (int c = 0; c < NR; ++c)  // behind the last rank value: the last again, not stored
-        wo[c] = ((uint32_t)min(r0 + 16 * c + m, rank - 1) * k.K + 8 * g) * 2;
+        wo[c] = TURNED ? (uint32_t)(8 * g * rank + min(r0 + 16 * c + m, rank - 1)) * 2
+                       : ((uint32_t)min(r0 + 16 * c + m, rank - 1) * k.K + 8 * g) * 2;
     const char *xs = (const char *)(k.x + (int64_t)max(row, 0) * k.K + part * 64 + 8 * g);
-    const char *ws = (const char *)(k.w + (int64_t)t.e * rank * k.K + part * 64);
+    const char *ws =
+        (const char *)(k.w + (int64_t)t.e * rank * k.K + (int64_t)part * 64 * (TURNED ? rank : 1));
     floatx4 acc[NR] = {};
-    bf16x8 xv[DEP][2], wv[DEP][NR][2];
+    using W = std::conditional_t<TURNED, uint16_t[8], bf16x8>;
+    bf16x8 xv[DEP][2];
+    W wv[DEP][NR][2];
     // (both halves of a cache line one after the other: it may not stay)
     auto load = [&](int i, int s) {
         const int at = s * parts * 128;
@@ -137,14 +165,33 @@ __device__ __forceinline__ void shrink_short(const AdapterRows &o, int rank, con
 #pragma unroll
         for (int c = 0; c < NR; ++c)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                wv[i][c][h] = *reinterpret_cast<const bf16x8 *>(ws + at + wo[c] + 64 * h);
+            for (int h = 0; h < 2; ++h) {
+                if constexpr (TURNED) {
+                    const char *p = ws + (int64_t)at * rank + wo[c];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        wv[i][c][h][q] =
+                            *reinterpret_cast<const uint16_t *>(p + (32 * h + q) * rank * 2);
+                } else {
+                    wv[i][c][h] = *reinterpret_cast<const bf16x8 *>(ws + at + wo[c] + 64 * h);
+                }
+            }
+    };
+    auto operand = [&](const W &w) {
+        if constexpr (TURNED) {
+            u32x4 v;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = w[2 * q] | (uint32_t)w[2 * q + 1] << 16;
+            return __builtin_bit_cast(bf16x8, v);
+        } else {
+            return w;
+        }
     };
     auto use = [&](int i) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int c = 0; c < NR; ++c) acc[c] = mfma(xv[i][h], wv[i][c][h], acc[c]);
+            for (int c = 0; c < NR; ++c) acc[c] = mfma(xv[i][h], operand(wv[i][c][h]), acc[c]);
     };
     if (n > 0) {
 #pragma unroll
@@ -189,7 +236,8 @@ __device__ __forceinline__ void shrink_short(const AdapterRows &o, int rank, con
 // whole lines (eight lanes to the 128 bytes of a row: the cache takes a lane's 16 bytes
 // of a row of its own as slowly as 64 of a shared one), AHEAD steps of 64 k in
 // registers, and lie in LDS as operands [block][chunk of 8 k][row][8], two steps in
-// turn.  `splits` workgroups share K.
+// turn.  `splits` workgroups share K.  Of a turned w a thread takes four
+// rank values of two k.
 template <int RB, int NR>
 struct TallShrink {
     static constexpr int TH = 64 * shrink_waves(RB), AHEAD = 3;
@@ -198,7 +246,7 @@ struct TallShrink {
     static constexpr size_t LDS = (size_t)2 * (XL + WL) * 16;
 };
 
-template <int RB, int NR>
+template <int RB, int NR, bool TURNED>
 __device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, const Shrink &k,
                                             int tile, int split, char *lds) {
     using C = TallShrink<RB, NR>;
@@ -221,17 +269,29 @@ __device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, cons
     }
 #pragma unroll
     for (int i = 0; i < WI; ++i) {  // behind the last rank value: the last again, not stored
-        const int item = min((int)threadIdx.x + C::TH * i, 16 * NR * 8 - 1), r = item / 8;
-        wo[i] = ((uint32_t)min(r, rank - 1) * k.K + 8 * (item % 8)) * 2;
-        wt[i] = C::XL + ((r >> 4) * 8 + item % 8) * kPitch + (r & 15);
+        const int at = threadIdx.x + C::TH * i;
+        if constexpr (TURNED) {
+            const int item = min(at, 8 * rank - 1), kk = item / (rank / 4) * 2;
+            const int r = item % (rank / 4) * 4;
+            wo[i] = kk * rank + r;
+            wt[i] = (C::XL + ((r >> 4) * 8 + (kk >> 3)) * kPitch + (r & 15)) * 4 + (kk & 7) / 2;
+        } else {
+            const int item = min(at, 16 * NR * 8 - 1), r = item / 8;
+            wo[i] = ((uint32_t)min(r, rank - 1) * k.K + 8 * (item % 8)) * 2;
+            wt[i] = C::XL + ((r >> 4) * 8 + item % 8) * kPitch + (r & 15);
+        }
     }
-    const bf16_t *we = k.w + (int64_t)t.e * rank * k.K + lo * 64;
+    const int per_step = 64 * (TURNED ? rank : 1);
+    const bf16_t *we = k.w + (int64_t)t.e * rank * k.K + (int64_t)lo * per_step;
     bf16x8 xv[D][XI], wv[D][WI];
     auto load = [&](int i, int s) {
 #pragma unroll
         for (int j = 0; j < XI; ++j) xv[i][j] = load8(xp[j] + s * 64);
 #pragma unroll
-        for (int j = 0; j < WI; ++j) wv[i][j] = load8(we + s * 64, wo[j]);
+        for (int j = 0; j < WI; ++j) {
+            const bf16_t *p = we + (int64_t)s * per_step;
+            wv[i][j] = TURNED ? load_pair(p + wo[j], rank) : load8(p, wo[j]);
+        }
     };
     floatx4 acc[NR] = {};
     bf16x8 *buf = reinterpret_cast<bf16x8 *>(lds);
@@ -239,7 +299,12 @@ __device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, cons
 #pragma unroll
         for (int j = 0; j < XI; ++j) to[xt[j]] = xv[i][j];
 #pragma unroll
-        for (int j = 0; j < WI; ++j) to[wt[j]] = wv[i][j];
+        for (int j = 0; j < WI; ++j) {
+            if constexpr (TURNED)
+                put_pair(to, wt[j], 4, wv[i][j]);
+            else
+                to[wt[j]] = wv[i][j];
+        }
     };
     auto use = [&](const bf16x8 *from) {
 #pragma unroll
@@ -282,48 +347,8 @@ __device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, cons
     }
 }
 
-// wt[e] = w[e]^T for the adapters that have rows, w [count][m][n]: 64 x 64 tiles
-// through LDS, m and n any multiples of 8.
-struct Transpose {
-    const bf16_t *w;
-    bf16_t *wt;
-    int m, n, bx, blocks;  // tiles along n, and of all adapters
-};
-
-__device__ __forceinline__ void transpose(const AdapterRows &o, const Transpose &k, int block,
-                                          uint16_t (*tile)[66]) {
-    const int by = (k.m + 63) / 64, e = block / (k.bx * by), at = block % (k.bx * by);
-    if (offset_at(o, e + 1) <= offset_at(o, e)) return;
-    const int i0 = at / k.bx * 64, j0 = at % k.bx * 64;
-    const bf16_t *src = k.w + (int64_t)e * k.m * k.n;
-    bf16_t *dst = k.wt + (int64_t)e * k.m * k.n;
-    for (int v = threadIdx.x; v < 64 * 8; v += blockDim.x) {
-        const int i = v / 8, j = v % 8 * 8;
-        if (i0 + i < k.m && j0 + j < k.n) {
-            const u32x4 u =
-                *reinterpret_cast<const u32x4 *>(src + (int64_t)(i0 + i) * k.n + j0 + j);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                tile[i][j + 2 * q] = (uint16_t)u[q];
-                tile[i][j + 2 * q + 1] = (uint16_t)(u[q] >> 16);
-            }
-        }
-    }
-    __syncthreads();
-    for (int v = threadIdx.x; v < 64 * 8; v += blockDim.x) {
-        const int j = v / 8, i = v % 8 * 8;
-        if (i0 + i < k.m && j0 + j < k.n) {
-            u32x4 u;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                u[q] = tile[i + 2 * q][j] | ((uint32_t)tile[i + 2 * q + 1][j] << 16);
-            *reinterpret_cast<u32x4 *>(dst + (int64_t)(j0 + j) * k.m + i0 + i) = u;
-        }
-    }
-}
-
-// Blocks of one shrink, then of another (of the gradient).
-template <int RB, int NR>
+// Blocks of one shrink, then of another (of the gradient, whose first is turned).
+template <int RB, int NR, bool TURNED>
 __global__ __launch_bounds__(64 * shrink_waves(RB), RB == 1 ? 2 : 4) void shrink_kernel(
     AdapterRows o, int rank, Shrink k0, Shrink k1, int blocks0) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -331,19 +356,18 @@ __global__ __launch_bounds__(64 * shrink_waves(RB), RB == 1 ? 2 : 4) void shrink
     const Shrink &k = first ? k0 : k1;
     const int b = first ? blockIdx.x : blockIdx.x - blocks0;
     const int split = b % k.out.splits, tile = b / k.out.splits % k.tiles;
-    if constexpr (RB == 1)
-        shrink_short<NR>(o, rank, k, tile, split, b / (k.tiles * k.out.splits) * 16 * NR,
-                         reinterpret_cast<floatx4 *>(lds));
+    auto run = [&](auto turned) {
+        if constexpr (RB == 1)
+            shrink_short<NR, turned()>(o, rank, k, tile, split,
+                                       b / (k.tiles * k.out.splits) * 16 * NR,
+                                       reinterpret_cast<floatx4 *>(lds));
+        else
+            shrink_tall<RB, NR, turned()>(o, rank, k, tile, split, lds);
+    };
+    if (TURNED && first)
+        run(std::bool_constant<TURNED>());
     else
-        shrink_tall<RB, NR>(o, rank, k, tile, split, lds);
-}
-
-// Both of an adapter's matrices.
-__global__ __launch_bounds__(256) void transpose_kernel(AdapterRows o, Transpose ta,
-                                                        Transpose tb) {
-    __shared__ uint16_t tile[64][66];
-    const int b = blockIdx.x;
-    transpose(o, b < ta.blocks ? ta : tb, b < ta.blocks ? b : b - ta.blocks, tile);
+        run(std::false_type());
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -473,7 +497,7 @@ template <class Y>
 struct Four;
 template <>
 struct Four<bf16_t> {
-    typedef uint32_t V __attribute__((ext_vector_type(2)));
+    typedef u32x2 V;
     static constexpr int S = 2;
     static __device__ __forceinline__ V add(V base, floatx4 a) {
         return V{pack2(__uint_as_float(base[0] << 16) + a[0],
@@ -491,8 +515,9 @@ struct Four<float> {
     }
 };
 
-// y = base + scale w u over N columns, w [count][N][rank].  A workgroup has a tile
-// of rows and `span` blocks of 64 columns.
+// y = base + scale w u over N columns, w [count][N][rank], or where TURNED
+// [count][rank][N] (the gradient's).  A workgroup has a tile of rows and `span` blocks
+// of 64 columns.
 template <class Y>
 struct Expand {
     AdapterSums u;
@@ -535,7 +560,7 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
 // comes in as whole lines, by all of them, and lies in LDS as operands
 // [j][chunk][n][8], two blocks of 64 columns in turn.  Short tiles: the waves have
 // columns of their own and take B's operands from memory.
-template <int RB, class Y>
+template <int RB, class Y, bool TURNED>
 __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Expand<Y> &k,
                                        int block, char *lds) {
     using P = Four<Y>;
@@ -615,16 +640,29 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
                 const int i = min((int)threadIdx.x + TH * it, items - 1), col = i / rc;
-                from[it] = 8 * i;
-                to[it] = ((col & 3) * rc + i % rc) * kPitch + (col >> 2);
+                if constexpr (TURNED) {  // four columns of two rank values
+                    const int r = i / 16 * 2;
+                    from[it] = r * k.N + i % 16 * 4;
+                    to[it] = (r / 8 * kPitch + i % 16) * 4 + r % 8 / 2;
+                } else {
+                    from[it] = 8 * i;
+                    to[it] = ((col & 3) * rc + i % rc) * kPitch + (col >> 2);
+                }
             }
             auto load_w = [&](int c) {
+                const bf16_t *p = we + (TURNED ? c : (int64_t)c * rank);
 #pragma unroll
-                for (int it = 0; it < IT; ++it) w[it] = load8(we + (int64_t)c * rank + from[it]);
+                for (int it = 0; it < IT; ++it)
+                    w[it] = TURNED ? load_pair(p + from[it], k.N) : load8(p + from[it]);
             };
             auto write_w = [&](bf16x8 *p) {  // (behind the last: the last again)
 #pragma unroll
-                for (int it = 0; it < IT; ++it) p[to[it]] = w[it];
+                for (int it = 0; it < IT; ++it) {
+                    if constexpr (TURNED)
+                        put_pair(p, to[it], rc * kPitch * 4, w[it]);
+                    else
+                        p[to[it]] = w[it];
+                }
             };
             auto block_product = [&](const bf16x8 *from) {
                 clear();
@@ -670,9 +708,27 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
         bf16x8 first[4];
         auto load_w = [&](bf16x8(&wv)[4], int c, int st) {
             const int ch = chunk_of(st);
+            if constexpr (TURNED) {  // four columns of eight rank values, turned in registers
+                u32x2 v[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                wv[j] = load8(we + (int64_t)(c + j) * rank, (uint32_t)(4 * m * rank + 8 * ch) * 2);
+                for (int i = 0; i < 8; ++i)
+                    v[i] = *reinterpret_cast<const u32x2 *>(we + (int64_t)(8 * ch + i) * k.N + c +
+                                                            4 * m);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    u32x4 u;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        u[i] = j & 1 ? high_halves(v[2 * i][j / 2], v[2 * i + 1][j / 2])
+                                     : low_halves(v[2 * i][j / 2], v[2 * i + 1][j / 2]);
+                    wv[j] = __builtin_bit_cast(bf16x8, u);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    wv[j] =
+                        load8(we + (int64_t)(c + j) * rank, (uint32_t)(4 * m * rank + 8 * ch) * 2);
+            }
         };
         // what does not depend on u is on its way before it is cut
         if (c < c1) {
@@ -716,11 +772,11 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
     }
 }
 
-template <int RB, class Y>
+template <int RB, class Y, bool TURNED>
 __global__ __launch_bounds__(64 * kWaves, 4) void expand_kernel(AdapterRows o, int rank,
                                                              Expand<Y> k) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    expand<RB, Y>(o, rank, k, blockIdx.x, lds);
+    expand<RB, Y, TURNED>(o, rank, k, blockIdx.x, lds);
 }
 
 // ---- gradients of A and B ------------------------------------------------
@@ -732,8 +788,8 @@ __device__ __forceinline__ void transpose8(const u32x4 (&in)[8], bf16x8 (&out)[8
         u32x4 lo, hi;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            lo[i] = __builtin_amdgcn_perm(in[2 * i + 1][j], in[2 * i][j], 0x05040100u);
-            hi[i] = __builtin_amdgcn_perm(in[2 * i + 1][j], in[2 * i][j], 0x07060302u);
+            lo[i] = low_halves(in[2 * i][j], in[2 * i + 1][j]);
+            hi[i] = high_halves(in[2 * i][j], in[2 * i + 1][j]);
         }
         out[2 * j] = __builtin_bit_cast(bf16x8, lo);
         out[2 * j + 1] = __builtin_bit_cast(bf16x8, hi);
@@ -933,7 +989,7 @@ __global__ __launch_bounds__(64 * kWaves, NR == 1 ? 4 : 2) void back_kernel(
         outer<1, NR>(o, rank, scale, sh, slots, accumulate, b < kb.blocks ? kb : ka,
                      b < kb.blocks ? b : b - kb.blocks, lds);
     else
-        expand<1, Y>(o, rank, kx, b - kb.blocks - ka.blocks, lds);
+        expand<1, Y, true>(o, rank, kx, b - kb.blocks - ka.blocks, lds);
 }
 
 // Adapters of several tiles: their parts, added in order; adapters of no rows:
@@ -1015,7 +1071,8 @@ hipError_t allow_lds(const void *fn, size_t lds) {
                        : hipSuccess;
 }
 
-// a, and b unless it has no tiles.
+// a, and b unless it has no tiles; a's w is turned where TURNED.
+template <bool TURNED>
 hipError_t launch_shrink(const AdapterRows &o, int rank, const Shrink &a, const Shrink &b,
                          hipStream_t s) {
     auto go = [&](auto rb, auto nr) {
@@ -1023,7 +1080,7 @@ hipError_t launch_shrink(const AdapterRows &o, int rank, const Shrink &a, const 
         const int na = a.tiles * a.out.splits * groups, nb = b.tiles * b.out.splits * groups;
         const size_t lds = rb() > 1 ? TallShrink<rb(), nr()>::LDS
                                     : (size_t)shrink_waves(1) / 2 * nr() * 64 * sizeof(floatx4);
-        const auto fn = shrink_kernel<rb(), nr()>;
+        const auto fn = shrink_kernel<rb(), nr(), TURNED>;
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
         fn<<<(unsigned)(na + nb), 64 * shrink_waves(rb()), lds, s>>>(o, rank, a, b, na);
         return hipGetLastError();
@@ -1062,21 +1119,24 @@ unsigned expand_blocks(const Expand<Y> &k) {
     return (unsigned)((int64_t)(k.tiles + k.copies) * k.ranges);
 }
 
-template <class Y>
+template <bool TURNED, class Y>
 hipError_t launch_expand(const AdapterRows &o, int rank, const Expand<Y> &k, hipStream_t s) {
     const size_t lds = expand_lds<Y>(o, rank);
-    const auto fn = row_blocks(o.rows, o.count, rank) == 8 ? expand_kernel<8, Y>
-                                                           : expand_kernel<1, Y>;
+    const auto fn = row_blocks(o.rows, o.count, rank) == 8 ? expand_kernel<8, Y, TURNED>
+                                                           : expand_kernel<1, Y, TURNED>;
     if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
     fn<<<expand_blocks(k), 64 * kWaves, lds, s>>>(o, rank, k);
     return hipGetLastError();
 }
+template <bool TURNED>
 hipError_t launch_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u,
                          const bf16_t *w, const float *scale, const void *base, void *y, int type,
                          hipStream_t s) {
-    return type == MOE_FP32
-               ? launch_expand(o, rank, make_expand<float>(o, rank, N, u, w, scale, base, y), s)
-               : launch_expand(o, rank, make_expand<bf16_t>(o, rank, N, u, w, scale, base, y), s);
+    auto go = [&](auto zero) {
+        using Y = decltype(zero);
+        return launch_expand<TURNED>(o, rank, make_expand<Y>(o, rank, N, u, w, scale, base, y), s);
+    };
+    return type == MOE_FP32 ? go(float()) : go(bf16_t());
 }
 
 size_t outer_lds(int nr) { return (size_t)4 * nr * 8 * 64 * sizeof(floatx4); }
@@ -1107,7 +1167,7 @@ hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const Adap
     const int tiles = (int)tile_cap(o.rows, o.count, sh), rank = ad.rank;
     ka.blocks = tiles * ka.cb;
     kb.blocks = tiles * kb.cb;
-    const auto kx = make_expand<Y>(o, rank, ad.k, k.v, k.at, ad.scale, k.base, k.dx);
+    const auto kx = make_expand<Y>(o, rank, ad.k, k.v, ad.a, ad.scale, k.base, k.dx);
     auto go = [&](auto nr) {
         const auto fn = back_kernel<nr(), Y>;
         const size_t lds = std::max(outer_lds(nr()), expand_lds<Y>(o, rank));
@@ -1177,9 +1237,7 @@ bool adapter_launches_fit(int64_t rows, const moe_adapters &ad) {
     const int64_t shrink = std::max<int64_t>(tiles, 1024) * 2 * ((ad.rank + 63) / 64);
     const int64_t both = expand_cap(rows, tiles, std::max(ad.n, ad.k)) +
                          outer_cap(rows, ad.count, ad.n, ad.k);
-    // (its workgroups have half the threads)
-    const int64_t turn = (int64_t)ad.count * ((ad.rank + 63) / 64) * (ad.n / 64 + ad.k / 64) / 2;
-    return std::max({shrink, both, turn}) * 64 * kWaves < int64_t(1) << 32;
+    return std::max(shrink, both) * 64 * kWaves < int64_t(1) << 32;
 }
 
 size_t adapter_sums_bytes(int64_t rows, int count, int rank) {
@@ -1210,10 +1268,10 @@ hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, con
                                const void *base, void *y, int y_type, const AdapterSums &u,
                                hipStream_t s) {
     const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o, ad.rank)};
-    if (hipError_t e = launch_shrink(o, ad.rank, ku, Shrink{}, s)) return e;
+    if (hipError_t e = launch_shrink<false>(o, ad.rank, ku, Shrink{}, s)) return e;
     const Cut cu{u, y_type == MOE_FP32 ? 3 : 2, false};
     if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cu, cu, false, s)) return e;
-    return launch_expand(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y, y_type, s);
+    return launch_expand<false>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y, y_type, s);
 }
 
 hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
@@ -1221,19 +1279,11 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
     const Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 511) / 512, 0};
     const Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 511) / 512, 0};
     if (o.rows) {
-        auto turn = [&](const bf16_t *w, bf16_t *wt, int m, int n) {
-            const int bx = (n + 63) / 64;
-            return Transpose{w, wt, m, n, bx, o.count * bx * ((m + 63) / 64)};
-        };
-        const Transpose tb = turn(ad.b, k.bt, ad.n, ad.rank);
-        const Transpose ta = k.dx ? turn(ad.a, k.at, ad.rank, ad.k) : Transpose{};
-        transpose_kernel<<<tb.blocks + ta.blocks, 256, 0, s>>>(o, tb, ta);
-        if (hipError_t e = hipGetLastError()) return e;
         // v = B^T dy, and for db u = A x
         const int tiles = (int)tile_count(o, ad.rank);
-        const Shrink kv{k.dy, k.bt, k.v, ad.n, tiles};
+        const Shrink kv{k.dy, ad.b, k.v, ad.n, tiles};
         const Shrink ku = k.da ? Shrink{k.x, ad.a, k.u, ad.k, tiles} : Shrink{};
-        if (hipError_t e = launch_shrink(o, ad.rank, kv, ku, s)) return e;
+        if (hipError_t e = launch_shrink<true>(o, ad.rank, kv, ku, s)) return e;
         const Cut cv{k.v, !k.dx ? 0 : k.dx_type == MOE_FP32 ? 3 : 2, k.da != nullptr};
         const Cut cu{k.u, 0, true};
         if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cv, cu, k.da != nullptr, s)) return e;
@@ -1245,8 +1295,8 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
                 return e;
         } else {
             if (k.dx)
-                if (hipError_t e = launch_expand(o, ad.rank, ad.k, k.v, k.at, ad.scale, k.base,
-                                                 k.dx, k.dx_type, s))
+                if (hipError_t e = launch_expand<true>(o, ad.rank, ad.k, k.v, ad.a, ad.scale,
+                                                       k.base, k.dx, k.dx_type, s))
                     return e;
             if (k.da)
                 if (hipError_t e = launch_outer(o, ad.rank, ad.scale, k.accumulate, kb, ka, s))

@@ -57,7 +57,7 @@ size_t sums_bytes(int64_t rows, const moe_adapters *ad) {
 }
 
 struct BackWs {
-    size_t u, v, at, bt, pa, pb, total;
+    size_t u, v, pa, pb, total;
 };
 BackWs back_ws(int64_t rows, const moe_adapters *ad) {
     BackWs w;
@@ -67,11 +67,8 @@ BackWs back_ws(int64_t rows, const moe_adapters *ad) {
         o += up(bytes);
         return at;
     };
-    const size_t weights = (size_t)ad->count * ad->rank * sizeof(bf16_t);
     w.u = take(sums_bytes(rows, ad));
     w.v = take(sums_bytes(rows, ad));
-    w.at = take(weights * ad->k);
-    w.bt = take(weights * ad->n);
     w.pa = take(adapter_parts_bytes(rows, ad->rank, ad->k));
     w.pb = take(adapter_parts_bytes(rows, ad->rank, ad->n));
     w.total = o;
@@ -165,7 +162,6 @@ moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
     char *base = (char *)ws;
     k.u = adapter_sums(rows, ad.count, ad.rank, ad.k, 2, base + L.u);
     k.v = adapter_sums(rows, ad.count, ad.rank, ad.n, 2, base + L.v);
-    k.at = (bf16_t *)(base + L.at), k.bt = (bf16_t *)(base + L.bt);
     k.pa = (float *)(base + L.pa), k.pb = (float *)(base + L.pb);
     MOE_HIP(launch_adapter_backward(o, ad, k, (hipStream_t)stream));
     return MOE_OK;
