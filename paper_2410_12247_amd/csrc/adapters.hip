@@ -59,7 +59,8 @@ __device__ __forceinline__ void put_pair(bf16x8 *to, int at, int step, bf16x8 pa
     uint32_t *p = reinterpret_cast<uint32_t *>(to) + at;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        p[q * step] = q & 1 ? high_halves(u[q / 2], u[2 + q / 2]) : low_halves(u[q / 2], u[2 + q / 2]);
+        p[q * step] = q & 1 ? high_halves(u[q / 2], u[2 + q / 2])
+                            : low_halves(u[q / 2], u[2 + q / 2]);
 }
 
 // One tile: adapter e's places [first, first + rows), the tile's number among
@@ -120,6 +121,111 @@ __device__ __forceinline__ int row_at(const AdapterRows &o, int64_t place) {
     return (uint32_t)row < (uint64_t)o.rows ? row : -1;
 }
 
+// hi + mid (+ lo): the leading 8 bits by cutting, the last part rounded.
+template <int S>
+__device__ __forceinline__ void cut(float v, uint32_t (&part)[S]) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        const uint32_t u = __float_as_uint(v);
+        if (i + 1 < S) {
+            part[i] = u >> 16;
+            v = (u & 0x7F800000u) == 0x7F800000u ? 0.f : v - __uint_as_float(u & 0xFFFF0000u);
+        } else {
+            const bool special = (u & 0x7F800000u) == 0x7F800000u;
+            part[i] = (special ? u : u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+        }
+    }
+}
+// Eight values' parts, two to a word.
+template <int S>
+__device__ __forceinline__ void cut8(const float (&v)[8], bf16x8 (&part)[S]) {
+    u32x4 w[S] = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        uint32_t c[S];
+        cut<S>(v[j], c);
+#pragma unroll
+        for (int q = 0; q < S; ++q) w[q][j / 2] |= c[q] << (16 * (j & 1));
+    }
+#pragma unroll
+    for (int q = 0; q < S; ++q) part[q] = __builtin_bit_cast(bf16x8, w[q]);
+}
+
+// v[j] += the sum over splits of p[split * pitch + j * TM], four splits' loads at once.
+template <int TM>
+__device__ __forceinline__ void sum_splits(float (&v)[8], const float *p, int pitch, int splits) {
+    for (int q = 0; q < splits; q += 4) {
+        float w[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[i][j] = p[min(q + i, splits - 1) * pitch + j * TM];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += q + i < splits ? w[i][j] : 0.f;
+    }
+}
+
+// Sums of tall tiles, scaled and cut once a row for the many workgroups behind: by the
+// workgroup that has all of them, or where K is split by a launch of its own.  e: S
+// parts as operands of expand, [tile][row block][chunk][row][8] with the chunks of
+// Expand; q: three parts as operands of outer, [tile][part][rank][row].
+struct Cut {
+    int S;  // parts of e; 0: none
+    bool q;
+};
+
+__device__ __forceinline__ int chunks_of(int rank, int S) { return (rank / 8 * S + 3) / 4 * 4; }
+
+template <int S>
+__device__ __forceinline__ void store_parts(const float (&v)[8], bf16x8 *e, int chunk0, int rc,
+                                            int kc, int row) {
+    bf16x8 part[S];
+    cut8<S>(v, part);
+#pragma unroll
+    for (int s = 0; s < S; ++s) e[(chunk0 + s * rc + kc) * 16 + row] = part[s];
+}
+
+// p: [split][rank][row], PITCH values a rank value.
+template <int RB, int PITCH>
+__device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const float *scale,
+                                         const Cut &k, const AdapterSums &u, const Tile &t,
+                                         int tile, const float *p, int splits) {
+    constexpr int TM = 16 * RB;
+    const int rc = rank / 8, chunks = k.S ? chunks_of(rank, k.S) : 0;
+    const float f = scale ? scale[t.e] : 1.f;
+    bf16x8 *e = reinterpret_cast<bf16x8 *>(u.e) + (int64_t)tile * chunks * TM;
+    uint16_t *q = u.q + (int64_t)tile * 3 * rank * TM;
+    for (int i = threadIdx.x; i < TM * rc; i += 512) {
+        const int row = i % TM, kc = i / TM;
+        float v[8] = {};
+        if (row < t.rows && row_at(o, t.first + row) >= 0) {
+            sum_splits<PITCH>(v, p + 8 * kc * PITCH + row, rank * PITCH, splits);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= f;
+        }
+        if (k.S == 2) store_parts<2>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
+        if (k.S == 3) store_parts<3>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
+        if (k.q) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t c[3];
+                cut<3>(v[j], c);
+#pragma unroll
+                for (int s = 0; s < 3; ++s)
+                    q[((int64_t)s * rank + 8 * kc + j) * TM + row] = (uint16_t)c[s];
+            }
+        }
+    }
+    // the padding behind the last part
+    const int pad = chunks - rc * k.S;
+    for (int i = threadIdx.x; i < TM * pad; i += 512) {
+        const int row = i % TM, c = rc * k.S + i / TM;
+        e[((row >> 4) * chunks + c) * 16 + (row & 15)] = bf16x8{};
+    }
+}
+
 // ---- x A^T ---------------------------------------------------------------
 
 // Sums of `rows` times w [count][rank][K], or where TURNED [count][K][rank] (the
@@ -128,6 +234,7 @@ struct Shrink {
     const bf16_t *x, *w;
     AdapterSums out;
     int K, tiles;
+    Cut cut;  // of tall tiles
 };
 
 // Short tiles: operands straight to registers, 64 bytes of each of 16 rows a load.
@@ -248,7 +355,8 @@ struct TallShrink {
 
 template <int RB, int NR, bool TURNED>
 __device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, const Shrink &k,
-                                            int tile, int split, char *lds) {
+                                            const float *scale, int tile, int split,
+                                            char *lds) {
     using C = TallShrink<RB, NR>;
     constexpr int TM = 16 * RB, D = C::AHEAD, XI = C::XI, WI = C::WI;
     const Tile t = find_tile(o, tile_shift_of(RB), tile);
@@ -339,18 +447,28 @@ __device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, cons
                 use(buf + p * SZ);
             }
     }
-    float *p = k.out.p + ((int64_t)tile * k.out.splits + split) * rank * TM;
+    constexpr int PITCH = TM + 4;
+    static_assert((size_t)16 * NR * PITCH * 4 <= C::LDS, "room for the sums");
+    const bool whole = k.out.splits == 1;
+    float *p = whole ? reinterpret_cast<float *>(lds)
+                     : k.out.p + ((int64_t)tile * k.out.splits + split) * rank * TM;
+    const int pitch = whole ? PITCH : TM;
+    if (whole) __syncthreads();  // the operands have been read
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
         const int r = 16 * c + m;
-        if (r < rank) *reinterpret_cast<floatx4 *>(p + r * TM + 16 * wave + 4 * g) = acc[c];
+        if (r < rank) *reinterpret_cast<floatx4 *>(p + r * pitch + 16 * wave + 4 * g) = acc[c];
     }
+    if (!whole) return;
+    __syncthreads();
+    cut_tile<RB, PITCH>(o, rank, scale, k.cut, k.out, t, tile,
+                        reinterpret_cast<const float *>(lds), 1);
 }
 
 // Blocks of one shrink, then of another (of the gradient, whose first is turned).
 template <int RB, int NR, bool TURNED>
 __global__ __launch_bounds__(64 * shrink_waves(RB), RB == 1 ? 2 : 4) void shrink_kernel(
-    AdapterRows o, int rank, Shrink k0, Shrink k1, int blocks0) {
+    AdapterRows o, int rank, const float *scale, Shrink k0, Shrink k1, int blocks0) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const bool first = (int)blockIdx.x < blocks0;
     const Shrink &k = first ? k0 : k1;
@@ -362,7 +480,7 @@ __global__ __launch_bounds__(64 * shrink_waves(RB), RB == 1 ? 2 : 4) void shrink
                                        b / (k.tiles * k.out.splits) * 16 * NR,
                                        reinterpret_cast<floatx4 *>(lds));
         else
-            shrink_tall<RB, NR, turned()>(o, rank, k, tile, split, lds);
+            shrink_tall<RB, NR, turned()>(o, rank, k, scale, tile, split, lds);
     };
     if (TURNED && first)
         run(std::bool_constant<TURNED>());
@@ -376,118 +494,19 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
            ((uint32_t)__builtin_bit_cast(uint16_t, y) << 16);
 }
 
-// hi + mid (+ lo): the leading 8 bits by cutting, the last part rounded.
-template <int S>
-__device__ __forceinline__ void cut(float v, uint32_t (&part)[S]) {
-#pragma unroll
-    for (int i = 0; i < S; ++i) {
-        const uint32_t u = __float_as_uint(v);
-        if (i + 1 < S) {
-            part[i] = u >> 16;
-            v = (u & 0x7F800000u) == 0x7F800000u ? 0.f : v - __uint_as_float(u & 0xFFFF0000u);
-        } else {
-            const bool special = (u & 0x7F800000u) == 0x7F800000u;
-            part[i] = (special ? u : u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-        }
-    }
-}
-// Eight values' parts, two to a word.
-template <int S>
-__device__ __forceinline__ void cut8(const float (&v)[8], bf16x8 (&part)[S]) {
-    u32x4 w[S] = {};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t c[S];
-        cut<S>(v[j], c);
-#pragma unroll
-        for (int q = 0; q < S; ++q) w[q][j / 2] |= c[q] << (16 * (j & 1));
-    }
-#pragma unroll
-    for (int q = 0; q < S; ++q) part[q] = __builtin_bit_cast(bf16x8, w[q]);
-}
-
-// v[j] += the sum over splits of p[split * pitch + j * TM], four splits' loads at once.
-template <int TM>
-__device__ __forceinline__ void sum_splits(float (&v)[8], const float *p, int pitch, int splits) {
-    for (int q = 0; q < splits; q += 4) {
-        float w[4][8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[i][j] = p[min(q + i, splits - 1) * pitch + j * TM];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += q + i < splits ? w[i][j] : 0.f;
-    }
-}
-
-// ---- sums, scaled and cut --------------------------------------------------
-// Of tall tiles: once a row, in a launch of its own, for the many workgroups behind
-// it.  e: S parts as operands of expand, [tile][row block][chunk][row][8] with the
-// chunks of Expand; q: three parts as operands of outer, [tile][part][rank][row].
-struct Cut {
-    AdapterSums u;
-    int S;  // parts of e; 0: none
-    bool q;
-};
-
-__device__ __forceinline__ int chunks_of(int rank, int S) { return (rank / 8 * S + 3) / 4 * 4; }
-
-template <int S>
-__device__ __forceinline__ void store_parts(const float (&v)[8], bf16x8 *e, int chunk0, int rc,
-                                            int kc, int row) {
-    bf16x8 part[S];
-    cut8<S>(v, part);
-#pragma unroll
-    for (int s = 0; s < S; ++s) e[(chunk0 + s * rc + kc) * 16 + row] = part[s];
-}
-
-template <int RB>
-__device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const float *scale,
-                                         const Cut &k, const Tile &t, int tile) {
-    constexpr int TM = 16 * RB;
-    const int rc = rank / 8, chunks = k.S ? chunks_of(rank, k.S) : 0;
-    const float f = scale ? scale[t.e] : 1.f;
-    const float *p = k.u.p + (int64_t)tile * k.u.splits * rank * TM;
-    bf16x8 *e = reinterpret_cast<bf16x8 *>(k.u.e) + (int64_t)tile * chunks * TM;
-    uint16_t *q = k.u.q + (int64_t)tile * 3 * rank * TM;
-    for (int i = threadIdx.x; i < TM * rc; i += 512) {
-        const int row = i % TM, kc = i / TM;
-        float v[8] = {};
-        if (row < t.rows && row_at(o, t.first + row) >= 0) {
-            sum_splits<TM>(v, p + 8 * kc * TM + row, rank * TM, k.u.splits);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= f;
-        }
-        if (k.S == 2) store_parts<2>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
-        if (k.S == 3) store_parts<3>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
-        if (k.q) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint32_t c[3];
-                cut<3>(v[j], c);
-#pragma unroll
-                for (int s = 0; s < 3; ++s)
-                    q[((int64_t)s * rank + 8 * kc + j) * TM + row] = (uint16_t)c[s];
-            }
-        }
-    }
-    // the padding behind the last part
-    const int pad = chunks - rc * k.S;
-    for (int i = threadIdx.x; i < TM * pad; i += 512) {
-        const int row = i % TM, c = rc * k.S + i / TM;
-        e[((row >> 4) * chunks + c) * 16 + (row & 15)] = bf16x8{};
-    }
-}
-
+// Of one sum, then of another (of the gradient).
 template <int RB>
 __global__ __launch_bounds__(512) void cut_kernel(AdapterRows o, int rank, const float *scale,
-                                                  Cut a, Cut b, int tiles) {
-    const int tile = blockIdx.x % tiles;
+                                                  Shrink k0, Shrink k1) {
+    const bool first = (int)blockIdx.x < k0.tiles;
+    const Shrink &k = first ? k0 : k1;
+    const int tile = first ? blockIdx.x : blockIdx.x - k0.tiles, splits = k.out.splits;
+    if (splits == 1) return;
     const Tile t = find_tile(o, tile_shift_of(RB), tile);
     if (t.e < 0) return;
-    cut_tile<RB>(o, rank, scale, (int)blockIdx.x < tiles ? a : b, t, tile);
+    constexpr int TM = 16 * RB;
+    cut_tile<RB, TM>(o, rank, scale, k.cut, k.out, t, tile,
+                     k.out.p + (int64_t)tile * splits * rank * TM, splits);
 }
 
 // A lane's four columns of a row, next to each other (the lanes of a group have 64
@@ -1073,8 +1092,8 @@ hipError_t allow_lds(const void *fn, size_t lds) {
 
 // a, and b unless it has no tiles; a's w is turned where TURNED.
 template <bool TURNED>
-hipError_t launch_shrink(const AdapterRows &o, int rank, const Shrink &a, const Shrink &b,
-                         hipStream_t s) {
+hipError_t launch_shrink(const AdapterRows &o, int rank, const float *scale, const Shrink &a,
+                         const Shrink &b, hipStream_t s) {
     auto go = [&](auto rb, auto nr) {
         const int groups = rb() > 1 ? 1 : (rank + 16 * nr() - 1) / (16 * nr());
         const int na = a.tiles * a.out.splits * groups, nb = b.tiles * b.out.splits * groups;
@@ -1082,21 +1101,18 @@ hipError_t launch_shrink(const AdapterRows &o, int rank, const Shrink &a, const 
                                     : (size_t)shrink_waves(1) / 2 * nr() * 64 * sizeof(floatx4);
         const auto fn = shrink_kernel<rb(), nr(), TURNED>;
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
-        fn<<<(unsigned)(na + nb), 64 * shrink_waves(rb()), lds, s>>>(o, rank, a, b, na);
-        return hipGetLastError();
+        fn<<<(unsigned)(na + nb), 64 * shrink_waves(rb()), lds, s>>>(o, rank, scale, a, b,
+                                                                        na);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (rb() > 1 && std::max(a.out.splits, b.out.splits) > 1) {
+            cut_kernel<8><<<(unsigned)(a.tiles + b.tiles), 512, 0, s>>>(o, rank, scale, a, b);
+            return hipGetLastError();
+        }
+        return hipSuccess;
     };
     if (rank > 64 && row_blocks(o.rows, o.count, rank) > 1)  // one pass over the rows
         return go(Int<8>(), Int<8>());
     return by_size(o, rank, go);
-}
-
-// Of tall tiles only.
-hipError_t launch_cut(const AdapterRows &o, int rank, const float *scale, const Cut &a,
-                      const Cut &b, bool both, hipStream_t s) {
-    const int rb = row_blocks(o.rows, o.count, rank), tiles = (int)tile_count(o, rank);
-    if (rb == 1) return hipSuccess;
-    cut_kernel<8><<<(unsigned)tiles * (both ? 2 : 1), 512, 0, s>>>(o, rank, scale, a, b, tiles);
-    return hipGetLastError();
 }
 
 template <class Y>
@@ -1267,10 +1283,9 @@ size_t adapter_parts_bytes(int64_t rows, int rank, int C) {
 hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, const bf16_t *x,
                                const void *base, void *y, int y_type, const AdapterSums &u,
                                hipStream_t s) {
-    const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o, ad.rank)};
-    if (hipError_t e = launch_shrink<false>(o, ad.rank, ku, Shrink{}, s)) return e;
-    const Cut cu{u, y_type == MOE_FP32 ? 3 : 2, false};
-    if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cu, cu, false, s)) return e;
+    const Cut cut{y_type == MOE_FP32 ? 3 : 2, false};
+    const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o, ad.rank), cut};
+    if (hipError_t e = launch_shrink<false>(o, ad.rank, ad.scale, ku, Shrink{}, s)) return e;
     return launch_expand<false>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y, y_type, s);
 }
 
@@ -1281,12 +1296,10 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
     if (o.rows) {
         // v = B^T dy, and for db u = A x
         const int tiles = (int)tile_count(o, ad.rank);
-        const Shrink kv{k.dy, ad.b, k.v, ad.n, tiles};
-        const Shrink ku = k.da ? Shrink{k.x, ad.a, k.u, ad.k, tiles} : Shrink{};
-        if (hipError_t e = launch_shrink<true>(o, ad.rank, kv, ku, s)) return e;
-        const Cut cv{k.v, !k.dx ? 0 : k.dx_type == MOE_FP32 ? 3 : 2, k.da != nullptr};
-        const Cut cu{k.u, 0, true};
-        if (hipError_t e = launch_cut(o, ad.rank, ad.scale, cv, cu, k.da != nullptr, s)) return e;
+        const Cut cv{!k.dx ? 0 : k.dx_type == MOE_FP32 ? 3 : 2, k.da != nullptr};
+        const Shrink kv{k.dy, ad.b, k.v, ad.n, tiles, cv};
+        const Shrink ku = k.da ? Shrink{k.x, ad.a, k.u, ad.k, tiles, Cut{0, true}} : Shrink{};
+        if (hipError_t e = launch_shrink<true>(o, ad.rank, ad.scale, kv, ku, s)) return e;
         if (k.dx && k.da && row_blocks(o.rows, o.count, ad.rank) == 1) {
             // few rows: one launch for the three products
             if (hipError_t e = k.dx_type == MOE_FP32
