@@ -465,6 +465,84 @@ __device__ __forceinline__ void shrink_tall(const AdapterRows &o, int rank, cons
                         reinterpret_cast<const float *>(lds), 1);
 }
 
+// Few rows of few k: every workgroup of expand has its tile's sums itself, which saves
+// a launch.  A wave takes every eighth 64 k; rows and adapter come in as whole lines
+// and become operands through LDS of the wave's own, DEP steps in flight.  The waves'
+// sums lie at the end in lds, [wave][rank][row].
+template <int NR>
+struct OwnSums {
+    static constexpr int DEP = NR == 1 ? 8 : 4, OPERANDS = (1 + NR) * 8 * kPitch;  // a wave's
+    static constexpr size_t LDS = (size_t)kWaves * OPERANDS * 16;
+    static_assert(LDS >= (size_t)kWaves * 16 * NR * 16 * sizeof(float), "room for the sums");
+};
+
+template <int NR>
+__device__ __forceinline__ void own_sums(const AdapterRows &o, int rank, const Tile &t,
+                                         const bf16_t *x, const bf16_t *a, int K, char *lds) {
+    using C = OwnSums<NR>;
+    constexpr int DEP = C::DEP;
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, line = lane >> 3, ch = lane & 7;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = (K / 64 - wave + kWaves - 1) / kWaves;
+    bf16x8 *own = reinterpret_cast<bf16x8 *>(lds) + wave * C::OPERANDS;
+    const bf16_t *xp[2], *ap[2 * NR];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int row = row_at(o, t.first + min(8 * j + line, t.rows - 1));
+        xp[j] = x + (int64_t)max(row, 0) * K + wave * 64 + 8 * ch;
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * NR; ++j)  // behind the last rank value: the last again, not stored
+        ap[j] = a + ((int64_t)t.e * rank + min(8 * j + line, rank - 1)) * K + wave * 64 + 8 * ch;
+    bf16x8 xv[DEP][2], av[DEP][2 * NR];
+    auto load = [&](int i, int s) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) xv[i][j] = load8(xp[j] + s * kWaves * 64);
+#pragma unroll
+        for (int j = 0; j < 2 * NR; ++j) av[i][j] = load8(ap[j] + s * kWaves * 64);
+    };
+    floatx4 acc[NR] = {};
+    auto use = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) own[ch * kPitch + 8 * j + line] = xv[i][j];
+#pragma unroll
+        for (int j = 0; j < 2 * NR; ++j)
+            own[((1 + j / 2) * 8 + ch) * kPitch + 8 * (j & 1) + line] = av[i][j];
+        wave_sync();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bf16x8 v = own[(4 * h + g) * kPitch + m];
+#pragma unroll
+            for (int c = 0; c < NR; ++c)
+                acc[c] = mfma(v, own[((1 + c) * 8 + 4 * h + g) * kPitch + m], acc[c]);
+        }
+        wave_sync();
+    };
+    if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < DEP; ++i) load(i, min(i, n - 1));
+        int s = 0;
+        for (; s + DEP < n; s += DEP) {
+#pragma unroll
+            for (int i = 0; i < DEP; ++i) {
+                use(i);
+                load(i, min(s + i + DEP, n - 1));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < DEP; ++i)
+            if (s + i < n) use(i);
+    }
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(lds) + wave * rank * 16;
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+        const int r = 16 * c + m;
+        if (r < rank) *reinterpret_cast<floatx4 *>(sums + r * 16 + 4 * g) = acc[c];
+    }
+    __syncthreads();
+}
+
 // Blocks of one shrink, then of another (of the gradient, whose first is turned).
 template <int RB, int NR, bool TURNED>
 __global__ __launch_bounds__(64 * shrink_waves(RB), RB == 1 ? 2 : 4) void shrink_kernel(
@@ -545,6 +623,8 @@ struct Expand {
     const Y *base;
     Y *y;
     int N, tiles, copies, span, ranges;  // ranges: of span blocks
+    const bf16_t *x, *a;                 // for own_sums
+    int K;
 };
 
 // Rows of no adapter: base's row (zeros without one), 64 rows a workgroup.
@@ -579,7 +659,9 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
 // comes in as whole lines, by all of them, and lies in LDS as operands
 // [j][chunk][n][8], two blocks of 64 columns in turn.  Short tiles: the waves have
 // columns of their own and take B's operands from memory.
-template <int RB, class Y, bool TURNED>
+//
+// OWN: rank blocks of own_sums, 0 where the sums come from memory.
+template <int RB, class Y, bool TURNED, int OWN = 0>
 __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Expand<Y> &k,
                                        int block, char *lds) {
     using P = Four<Y>;
@@ -757,12 +839,18 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
         // u, scaled and cut, in LDS: [chunk][row][8]
         const float f = k.scale ? k.scale[t.e] : 1.f;
         const float *pt = k.u.p + (int64_t)tile * k.u.splits * rank * TM;
+        if constexpr (OWN > 0) {
+            char *at = lds + chunks * 256;
+            own_sums<OWN>(o, rank, t, k.x, k.a, k.K, at);
+            pt = reinterpret_cast<const float *>(at);
+        }
+        const int splits = OWN > 0 ? kWaves : k.u.splits;
         for (int i = threadIdx.x; i < TM * (chunks - rc * (S - 1)); i += TH) {
             const int row = i % TM, kc = i / TM;
             bf16x8 part[S] = {};
             if (row < t.rows && kc < rc) {
                 float v[8] = {};
-                sum_splits<TM>(v, pt + 8 * kc * TM + row, rank * TM, k.u.splits);
+                sum_splits<TM>(v, pt + 8 * kc * TM + row, rank * TM, splits);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= f;
                 cut8<S>(v, part);
@@ -796,6 +884,12 @@ __global__ __launch_bounds__(64 * kWaves, 4) void expand_kernel(AdapterRows o, i
                                                              Expand<Y> k) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     expand<RB, Y, TURNED>(o, rank, k, blockIdx.x, lds);
+}
+
+template <int OWN, class Y>
+__global__ __launch_bounds__(64 * kWaves, 2) void few_kernel(AdapterRows o, int rank, Expand<Y> k) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    expand<1, Y, false, OWN>(o, rank, k, blockIdx.x, lds);
 }
 
 // ---- gradients of A and B ------------------------------------------------
@@ -1061,6 +1155,11 @@ int64_t tile_cap(int64_t rows, int count, int sh) {
 // for many rows, where the adapters' mean rows fill most of one.  u's parts of a tile
 // have to fit LDS.
 constexpr int64_t kTallRows = 1536;
+// Values of x and A that every workgroup of expand reads itself (own_sums) rather than a
+// launch before it, at most: y of 4096 columns, rank 16, with and without it, us in a
+// graph: one row of 4096 k 8.4 and 8.8 (called one by one 8.5 and 11.0), of 8192 k 11.4
+// and 9.8; 100 rows of 1024 k 7.7 and 9.5.
+constexpr int64_t kFewValues = 98304;
 int row_blocks(int64_t rows, int count, int rank) {
     return rank <= 128 && rows >= kTallRows && rows >= (int64_t)64 * count ? 8 : 1;
 }
@@ -1118,7 +1217,9 @@ hipError_t launch_shrink(const AdapterRows &o, int rank, const float *scale, con
 template <class Y>
 Expand<Y> make_expand(const AdapterRows &o, int rank, int N, const AdapterSums &u, const bf16_t *w,
                       const float *scale, const void *base, void *y) {
-    Expand<Y> k{u, w, scale, (const Y *)base, (Y *)y, N, 0, 0, kExpandSpan, 0};
+    Expand<Y> k{};
+    k.u = u, k.w = w, k.scale = scale, k.base = (const Y *)base, k.y = (Y *)y;
+    k.N = N, k.span = kExpandSpan;
     k.tiles = (int)tile_count(o, rank);
     k.copies = base == y ? 0 : (int)((o.rows + 63) / 64);
     k.ranges = (N / 64 + k.span - 1) / k.span;
@@ -1153,6 +1254,29 @@ hipError_t launch_expand(const AdapterRows &o, int rank, int N, const AdapterSum
         return launch_expand<TURNED>(o, rank, make_expand<Y>(o, rank, N, u, w, scale, base, y), s);
     };
     return type == MOE_FP32 ? go(float()) : go(bf16_t());
+}
+
+// Whether every workgroup of expand has its sums itself: few values, and one workgroup a
+// compute unit.
+bool few_rows(const AdapterRows &o, const moe_adapters &ad) {
+    const int64_t tiles = tile_count(o, ad.rank);
+    const int64_t ranges = (ad.n / 64 + kExpandSpan - 1) / kExpandSpan;
+    return row_blocks(o.rows, o.count, ad.rank) == 1 && ad.rank <= 32 &&
+           (ad.rank + std::min<int64_t>(o.rows, 16)) * ad.k <= kFewValues && tiles * ranges <= 256;
+}
+template <class Y>
+hipError_t launch_few(const AdapterRows &o, const moe_adapters &ad, const bf16_t *x,
+                      const void *base, void *y, const AdapterSums &u, hipStream_t s) {
+    auto k = make_expand<Y>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y);
+    k.x = x, k.a = ad.a, k.K = ad.k;
+    auto go = [&](auto nr) {
+        const size_t lds = expand_lds<Y>(o, ad.rank) + OwnSums<nr()>::LDS;
+        const auto fn = few_kernel<nr(), Y>;
+        if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
+        fn<<<expand_blocks(k), 64 * kWaves, lds, s>>>(o, ad.rank, k);
+        return hipGetLastError();
+    };
+    return ad.rank <= 16 ? go(Int<1>()) : go(Int<2>());
 }
 
 size_t outer_lds(int nr) { return (size_t)4 * nr * 8 * 64 * sizeof(floatx4); }
@@ -1283,6 +1407,9 @@ size_t adapter_parts_bytes(int64_t rows, int rank, int C) {
 hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, const bf16_t *x,
                                const void *base, void *y, int y_type, const AdapterSums &u,
                                hipStream_t s) {
+    if (few_rows(o, ad))
+        return y_type == MOE_FP32 ? launch_few<float>(o, ad, x, base, y, u, s)
+                                  : launch_few<bf16_t>(o, ad, x, base, y, u, s);
     const Cut cut{y_type == MOE_FP32 ? 3 : 2, false};
     const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o, ad.rank), cut};
     if (hipError_t e = launch_shrink<false>(o, ad.rank, ad.scale, ku, Shrink{}, s)) return e;

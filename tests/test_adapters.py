@@ -205,7 +205,10 @@ SHAPES = [  # rows, n, k, rank, count
     (16, 192, 64, 8, 1), (17, 64, 320, 40, 1), (33, 320, 576, 16, 200), (63, 128, 64, 64, 1),
     (64, 64, 2048, 16, 64), (65, 448, 64, 72, 1), (130, 64, 64, 128, 2), (257, 1344, 448, 16, 5),
     (300, 64, 704, 200, 3), (256, 128, 128, 8, 256), (500, 192, 128, 256, 4),
-    (700, 256, 256, 64, 7), (1100, 704, 64, 32, 2), (3000, 64, 128, 8, 3)]
+    (700, 256, 256, 64, 7), (1100, 704, 64, 32, 2), (3000, 64, 128, 8, 3),
+    # either side of where a workgroup sums over k itself
+    (1, 128, 12288, 8, 2), (3, 64, 6208, 16, 2), (16, 192, 2048, 32, 1), (16, 128, 2112, 32, 3),
+    (90, 4096, 128, 16, 2), (200, 4160, 64, 24, 40), (1400, 1536, 128, 16, 7)]
 
 
 @gpu
