@@ -683,20 +683,20 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
     const bool whole = rank % 32 == 0;
     const int steps = whole ? rc / 4 : chunks / 4;  // of B's operands
     const bf16_t *we = k.w + (int64_t)t.e * k.N * rank;
-    int64_t at[4];
-    bool there[4];
+    int rows[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {  // (a place of no row: row 0's, not stored)
-        const int p = 16 * b0 + 4 * g + i, row = p < t.rows ? row_at(o, t.first + p) : -1;
-        there[i] = row >= 0;
-        at[i] = (int64_t)max(row, 0) * k.N + 4 * m;
+    for (int i = 0; i < 4; ++i) {
+        const int p = 16 * b0 + 4 * g + i;
+        rows[i] = p < t.rows ? row_at(o, t.first + p) : -1;
     }
+    // (a place of no row: row 0's, not stored)
+    auto at = [&](int i, int c) { return (int64_t)max(rows[i], 0) * k.N + 4 * m + c; };
     bf16x8 *u = reinterpret_cast<bf16x8 *>(lds);
     V old[4];
     auto load_base = [&](V(&v)[4], int c) {
         if (k.base) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const V *>(k.base + at[i] + c);
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const V *>(k.base + at(i, c));
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = V{};
@@ -725,8 +725,8 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
     auto store = [&](const V(&v)[4], int c) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (there[i])
-                *reinterpret_cast<V *>(k.y + at[i] + c) =
+            if (rows[i] >= 0)
+                *reinterpret_cast<V *>(k.y + at(i, c)) =
                     P::add(v[i], floatx4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]});
     };
     auto chunk_of = [&](int st) { return whole ? 4 * st + g : (4 * st + g) % rc; };
@@ -736,7 +736,8 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
         const int size = 4 * rc * kPitch, items = 64 * rc;
         auto run = [&](auto its) {
             constexpr int IT = its();
-            bf16x8 w[IT];
+            bf16x8 w[2][IT];
+            V hold[2][4];
             int from[IT], to[IT];  // a thread's operands of 64 columns, as they lie
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
@@ -750,19 +751,20 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
                     to[it] = ((col & 3) * rc + i % rc) * kPitch + (col >> 2);
                 }
             }
-            auto load_w = [&](int c) {
+            auto load_w = [&](bf16x8(&v)[IT], int c) {
                 const bf16_t *p = we + (TURNED ? c : (int64_t)c * rank);
 #pragma unroll
                 for (int it = 0; it < IT; ++it)
-                    w[it] = TURNED ? load_pair(p + from[it], k.N) : load8(p + from[it]);
+                    v[it] = TURNED ? load_pair(p + from[it], k.N) : load8(p + from[it]);
             };
-            auto write_w = [&](bf16x8 *p) {  // (behind the last: the last again)
+            // (behind the last: the last again)
+            auto write_w = [&](const bf16x8(&v)[IT], bf16x8 *p) {
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
                     if constexpr (TURNED)
-                        put_pair(p, to[it], rc * kPitch * 4, w[it]);
+                        put_pair(p, to[it], rc * kPitch * 4, v[it]);
                     else
-                        p[to[it]] = w[it];
+                        p[to[it]] = v[it];
                 }
             };
             auto block_product = [&](const bf16x8 *from) {
@@ -775,35 +777,54 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
                     product(wv, st);
                 }
             };
-            load_base(old, c0);
-            load_w(c0);
+            const int nb = (c1 - c0) / 64;  // blocks; two of them on their way
+            auto column = [&](int b) { return c0 + 64 * min(b, nb - 1); };
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                load_base(hold[i], column(i));
+                load_w(w[i], column(i));
+            }
             const bf16x8 *src =
                 reinterpret_cast<const bf16x8 *>(k.u.e) + (int64_t)tile * chunks * TM;
             for (int i = threadIdx.x; i < chunks * TM; i += TH) u[i] = src[i];
-            write_w(wl);
+            write_w(w[0], wl);
+            load_w(w[0], column(2));
             __syncthreads();
-            int c = c0, buf = 0;
-            // The next block's loads are on their way while this one's products run.
-            for (; c + 64 < c1; c += 64, buf ^= 1) {
-                V then[4];
-                load_base(then, c + 64);
-                load_w(c + 64);
-                block_product(wl + buf * size);
-                store(old, c);
-                write_w(wl + (buf ^ 1) * size);
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) old[i] = then[i];
+            // Block b, an even one where I is 0; after: 2 where two more come, 1 one more.
+            auto step = [&](auto slot, int b, auto after) {
+                constexpr int I = slot();
+                block_product(wl + I * size);
+                store(hold[I], column(b));
+                if constexpr (after() == 2) load_base(hold[I], column(b + 2));
+                if constexpr (after() > 0) {
+                    write_w(w[I ^ 1], wl + (I ^ 1) * size);
+                    if constexpr (after() == 2) load_w(w[I ^ 1], column(b + 3));
+                    __syncthreads();
+                }
+            };
+            constexpr std::integral_constant<int, 0> zero{};
+            constexpr std::integral_constant<int, 1> one{};
+            constexpr std::integral_constant<int, 2> two{};
+            int b = 0;
+            for (; b + 3 < nb; b += 2) {
+                step(zero, b, two);
+                step(one, b + 1, two);
             }
-            block_product(wl + buf * size);
-            store(old, c);
+            if (nb - b == 3) {
+                step(zero, b, two);
+                step(one, b + 1, one);
+                step(zero, b + 2, zero);
+            } else if (nb - b == 2) {
+                step(zero, b, one);
+                step(one, b + 1, zero);
+            } else {
+                step(zero, b, zero);
+            }
         };
         if (items <= TH)
             run(std::integral_constant<int, 1>());
-        else if (items <= 2 * TH)
-            run(std::integral_constant<int, 2>());
         else
-            run(std::integral_constant<int, 4>());
+            run(std::integral_constant<int, 2>());
     } else {
         int c = c0 + wave * 64;
         bf16x8 first[4];
