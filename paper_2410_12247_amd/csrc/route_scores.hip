@@ -134,28 +134,40 @@ __device__ __forceinline__ void exact_token(const Rules &r, int64_t t, const Z *
         wave_sync();
         for (int g = lane; g < G; g += 64) {
             double a = -INFINITY, b = -INFINITY;
-            for (int i = 0; i < size; ++i) {
-                const double c = cs[g * size + i];
-                if (c > a) b = a, a = c;
-                else if (c > b) b = c;
+            for (int i = 0; i < size; i += 8) {  // eight reads at once
+                double c[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) c[j] = cs[g * size + min(i + j, size - 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const double v = i + j < size ? c[j] : -INFINITY;
+                    b = v > a ? a : v > b ? v : b;
+                    a = v > a ? v : a;
+                }
             }
             gs[g] = r.pair && b > -INFINITY ? a + b : a;
         }
         wave_sync();
         if (!broken) {
+            double v[4];
+            int mine[4], better[4] = {};
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int e = lane + 64 * q;
-                if (e >= E) continue;
-                const int g = e / size;
-                const double v = gs[g];
-                int better = 0;
-                for (int i = 0; i < G; ++i) {
-                    const double o = gs[i];
-                    better += o > v || (o == v && i < g);
-                }
-                if (better >= r.top_groups) key[q] = 0;
+                mine[q] = min(lane + 64 * q, E - 1) / size;
+                v[q] = gs[mine[q]];
             }
+            for (int i = 0; i < G; i += 4) {
+                double o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = gs[min(i + j, G - 1)];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        better[q] += (int)(i + j < G) & comes_before(o[j], i + j, v[q], mine[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) key[q] = better[q] >= r.top_groups ? 0 : key[q];
         }
         wave_sync();
     }
