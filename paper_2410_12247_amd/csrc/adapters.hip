@@ -7,7 +7,9 @@
 // The sums over K of x A^T ("shrink") go through memory in fp32: rank values a
 // row, where the rows themselves have thousands.  The products behind it take
 // them cut into bf16 parts (hi + mid + lo hold all 24 bits), so that the matrix
-// cores multiply bf16 by bf16 without a rounding.
+// cores multiply bf16 by bf16 without a rounding.  All of it is bound by memory: the
+// matrix cores are busy 5 to 10% of the time.  Times below are of one call among
+// others on inputs of their own (4096 x 4096, bf16 y, where nothing else is said).
 #include "adapters.h"
 
 #include <algorithm>
@@ -170,7 +172,8 @@ __device__ __forceinline__ void sum_splits(float (&v)[8], const float *p, int pi
 // Sums of tall tiles, scaled and cut once a row for the many workgroups behind: by the
 // workgroup that has all of them, or where K is split by a launch of its own.  e: S
 // parts as operands of expand, [tile][row block][chunk][row][8] with the chunks of
-// Expand; q: three parts as operands of outer, [tile][part][rank][row].
+// Expand; q: three parts as operands of outer, [tile][part][rank][row].  16384 rows of
+// rank 64: 6.4 us, where every workgroup of expand cutting for itself cost 40.
 struct Cut {
     int S;  // parts of e; 0: none
     bool q;
@@ -241,6 +244,9 @@ struct Shrink {
 // The four waves (and `splits` workgroups) share K, each taking every so many-th 128
 // bytes of a row, and keep DEP steps of them in flight.  A turned w comes a value a
 // lane: a load has 16 rank values of four k, side by side where the rank is 16.
+// 64 rows of as many adapters, 6144 k, rank 32: 7.7 us, a launch's chain of latencies
+// (offsets, order, rows) and 15 MB; both sums of the gradient of 997 rows 10 us (with
+// the adapter transposed by a launch before it 11.2 + 3.8).
 template <int NR, bool TURNED>
 __device__ __forceinline__ void shrink_short(const AdapterRows &o, int rank, const Shrink &k,
                                              int tile, int split, int r0, floatx4 *lds) {
@@ -343,7 +349,9 @@ __device__ __forceinline__ void shrink_short(const AdapterRows &o, int rank, con
 // whole lines (eight lanes to the 128 bytes of a row: the cache takes a lane's 16 bytes
 // of a row of its own as slowly as 64 of a shared one), AHEAD steps of 64 k in
 // registers, and lie in LDS as operands [block][chunk of 8 k][row][8], two steps in
-// turn.  `splits` workgroups share K.  Of a turned w a thread takes four
+// turn.  `splits` workgroups share K.  16384 rows of rank 64: 45 us, of which reading
+// 134 MB of rows not in a cache takes some 40; 55 with lanes on rows of their own.  1, 2
+// or 4 to 8 splits in place of 3: 53, 60, 47 to 50.  Of a turned w a thread takes four
 // rank values of two k.
 template <int RB, int NR>
 struct TallShrink {
@@ -481,7 +489,8 @@ __device__ __forceinline__ void own_sums(const AdapterRows &o, int rank, const T
                                          const bf16_t *x, const bf16_t *a, int K, char *lds) {
     using C = OwnSums<NR>;
     constexpr int DEP = C::DEP;
-    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, line = lane >> 3, ch = lane & 7;
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int line = lane >> 3, ch = lane & 7;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = (K / 64 - wave + kWaves - 1) / kWaves;
     bf16x8 *own = reinterpret_cast<bf16x8 *>(lds) + wave * C::OPERANDS;
@@ -659,6 +668,9 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
 // comes in as whole lines, by all of them, and lies in LDS as operands
 // [j][chunk][n][8], two blocks of 64 columns in turn.  Short tiles: the waves have
 // columns of their own and take B's operands from memory.
+//
+// 16384 rows of rank 64: 74 us, 66 without the products; a linear copy of the base alone
+// takes 61 there.  Gradient of 8192 rows, rank 32, w turned: 40.
 //
 // OWN: rank blocks of own_sums, 0 where the sums come from memory.
 template <int RB, class Y, bool TURNED, int OWN = 0>
@@ -953,7 +965,8 @@ __device__ __forceinline__ int tiles_before(const AdapterRows &o, int sh, int e)
 // the j-th of which has column 8 (lane % 16) + j.  M is the rank.  Four waves stand
 // side by side, 128 columns each, and read the same of p; two such rows of waves take
 // steps of 32 rows in turn and join in LDS.  p in three parts: the sums are as exact
-// as fp32's.
+// as fp32's.  8192 rows, rank 32, both: 36 us for 134 MB of x and dy, 4.8 TB/s with
+// p and what it writes; twice the waves with half the registers spill (75 us).
 template <int RB, int NR>
 __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const float *scale, int sh,
                                       int slots, bool accumulate, const Outer &k, int block,
@@ -1127,7 +1140,8 @@ __global__ __launch_bounds__(64 * kWaves, NR == 1 ? 4 : 2) void back_kernel(
 }
 
 // Adapters of several tiles: their parts, added in order; adapters of no rows:
-// zeros (nothing where out accumulates).  blockIdx.z: da, db.
+// zeros (nothing where out accumulates).  blockIdx.z: da, db.  8192 rows, rank 32: 5.5 us,
+// 18 MB of parts; larger tiles have fewer of them and leave compute units idle.
 __global__ __launch_bounds__(256) void join_kernel(AdapterRows o, int sh, int slots, int accumulate,
                                                    Outer ka, Outer kb, int rank) {
     const Outer &k = blockIdx.z ? kb : ka;
@@ -1174,7 +1188,8 @@ int64_t tile_cap(int64_t rows, int count, int sh) {
 }
 // Row blocks of a tile.  Tall ones read the adapters' matrices less often; they are
 // for many rows, where the adapters' mean rows fill most of one.  u's parts of a tile
-// have to fit LDS.
+// have to fit LDS.  2048 rows of rank 64: 32 us against 45 in short ones, their gradient
+// 80 against 96.
 constexpr int64_t kTallRows = 1536;
 // Values of x and A that every workgroup of expand reads itself (own_sums) rather than a
 // launch before it, at most: y of 4096 columns, rank 16, with and without it, us in a

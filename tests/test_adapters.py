@@ -228,10 +228,12 @@ def test_rows(shape, dtype):
 
 
 # Many rows, in taller tiles: rows, n, k, rank, count, skewed (few adapters of many rows)
-MANY = [(1535, 192, 128, 32, 3, False), (1536, 64, 64, 8, 24, False), (1536, 128, 64, 16, 25, True),
-        (1537, 576, 320, 24, 24, True), (1663, 64, 448, 32, 1, True), (1792, 1344, 64, 40, 5, False),
-        (2047, 128, 576, 64, 7, True), (2048, 448, 1344, 72, 3, False), (2500, 704, 704, 128, 2, True),
-        (3001, 64, 1024, 136, 4, True), (4095, 512, 128, 16, 60, True), (4097, 128, 512, 120, 9, True),
+MANY = [(1535, 192, 128, 32, 3, False), (1536, 64, 64, 8, 24, False),
+        (1536, 128, 64, 16, 25, True), (1537, 576, 320, 24, 24, True),
+        (1663, 64, 448, 32, 1, True), (1792, 1344, 64, 40, 5, False),
+        (2047, 128, 576, 64, 7, True), (2048, 448, 1344, 72, 3, False),
+        (2500, 704, 704, 128, 2, True), (3001, 64, 1024, 136, 4, True),
+        (4095, 512, 128, 16, 60, True), (4097, 128, 512, 120, 9, True),
         (9000, 192, 192, 48, 1, False), (9001, 64, 4160, 64, 128, True)]
 
 

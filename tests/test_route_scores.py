@@ -285,9 +285,9 @@ def test_many_tokens(T):
 
 
 @gpu
-@pytest.mark.parametrize("E,k,G,top", [(65, 5, 1, 1), (100, 8, 1, 1), (128, 8, 4, 2), (160, 6, 8, 3),
-                                       (161, 5, 7, 3), (200, 3, 1, 1), (256, 8, 8, 4),
-                                       (256, 7, 2, 1), (256, 8, 16, 5)])
+@pytest.mark.parametrize("E,k,G,top", [(65, 5, 1, 1), (100, 8, 1, 1), (128, 8, 4, 2),
+                                       (160, 6, 8, 3), (161, 5, 7, 3), (200, 3, 1, 1),
+                                       (256, 8, 8, 4), (256, 7, 2, 1), (256, 8, 16, 5)])
 def test_rules_over_many_tokens(E, k, G, top):
     T = 16387
     b = torch.randn(E, generator=torch.Generator().manual_seed(2)).mul(0.1).cuda()
