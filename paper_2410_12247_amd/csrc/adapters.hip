@@ -973,7 +973,7 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                                       char *lds) {
     constexpr int TSH = tile_shift_of(RB), TM = 16 * RB, KR = kWaves / 4;
     floatx4 *sums = reinterpret_cast<floatx4 *>(lds);
-    int *rows = reinterpret_cast<int *>(lds);  // before the sums
+    int *rows = reinterpret_cast<int *>(sums + 4 * NR * 8 * 64);
     const Tile t = find_tile(o, sh, block / k.cb);
     if (t.e < 0 || (t.tiles > 1 && t.several + t.index >= slots)) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
@@ -985,14 +985,17 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
     if (pt + ((t.rows + TM - 1) >> TSH) > (o.rows >> TSH) + min((int64_t)o.count, o.rows)) return;
     const float f = scale ? scale[t.e] : 1.f;
     const bf16_t *qr = k.q + qc;
-    for (int grp = 0; grp < groups; ++grp) {
+    bool none = false;
+    for (int i = threadIdx.x; i < t.rows; i += 64 * kWaves) {
+        rows[i] = row_at(o, t.first + i);
+        none |= rows[i] < 0;
+    }
+    none = __syncthreads_or(none);
+    // Rows of one step: the halves take groups of the rank in turn, with nothing to join.
+    const bool one = RB == 1 && t.rows <= 32;
+    const int from = one ? 0 : 32 * rw;
+    for (int grp = one ? rw : 0; grp < groups; grp += one ? KR : 1) {
         const int r0 = grp * 16 * NR;
-        bool none = false;
-        for (int i = threadIdx.x; i < t.rows; i += 64 * kWaves) {
-            rows[i] = row_at(o, t.first + i);
-            none |= rows[i] < 0;
-        }
-        none = __syncthreads_or(none);
         floatx4 acc[NR][8] = {};
         u32x4 raw[8];
         auto load_q = [&](int k0) {
@@ -1003,8 +1006,8 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
             }
         };
         constexpr bool AHEAD = RB > 1;  // (of few rows a wave has a step or two)
-        if (AHEAD && 32 * rw < t.rows) load_q(32 * rw);
-        for (int k0 = 32 * rw; k0 < t.rows; k0 += 32 * KR) {
+        if (AHEAD && from < t.rows) load_q(from);
+        for (int k0 = from; k0 < t.rows; k0 += 32 * KR) {
             if (!AHEAD) load_q(k0);
             // p of 8 rows, in parts; behind the last row zeros
             const int at = min(k0 + 8 * g, (t.rows - 1) & ~7);
@@ -1067,20 +1070,24 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                     for (int j = 0; j < 8; ++j) acc[b][j] = mfma(part[s], qv[j], acc[b][j]);
             }
         }
-        __syncthreads();  // the rows' list has been read
-        floatx4 *mine = sums + cw * NR * 8 * 64 + lane;
-        if (rw == 1) {
+        if (!one) {
+            floatx4 *mine = sums + cw * NR * 8 * 64 + lane;
+            if (rw == 1) {
 #pragma unroll
-            for (int b = 0; b < NR; ++b)
+                for (int b = 0; b < NR; ++b)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) mine[(b * 8 + j) * 64] = acc[b][j];
+                    for (int j = 0; j < 8; ++j) mine[(b * 8 + j) * 64] = acc[b][j];
+            }
+            __syncthreads();
+            if (rw == 0) {
+#pragma unroll
+                for (int b = 0; b < NR; ++b)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[b][j] += mine[(b * 8 + j) * 64];
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        if (rw == 0 && col < k.C) {
-#pragma unroll
-            for (int b = 0; b < NR; ++b)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[b][j] += mine[(b * 8 + j) * 64];
+        if ((one || rw == 0) && col < k.C) {
             const bool whole = t.tiles == 1, add = whole && accumulate;
             float *to = whole ? k.out + (int64_t)t.e * rank * k.C
                               : k.parts + (int64_t)(t.several + t.index) * rank * k.C;
@@ -1109,7 +1116,6 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                 }
             }
         }
-        __syncthreads();
     }
 }
 
@@ -1211,9 +1217,11 @@ template <int N>
 using Int = std::integral_constant<int, N>;
 // fn(row blocks of a tile, rank blocks of a wave) of this size.
 template <class F>
-hipError_t by_size(const AdapterRows &o, int rank, F fn) {
+hipError_t by_size(const AdapterRows &o, int rank, int most, F fn) {
     auto go = [&](auto rb) {
-        return rank <= 16 ? fn(rb, Int<1>()) : rank <= 32 ? fn(rb, Int<2>()) : fn(rb, Int<4>());
+        return rank <= 16   ? fn(rb, Int<1>())
+               : rank <= most ? fn(rb, Int<2>())
+                              : fn(rb, Int<4>());
     };
     return row_blocks(o.rows, o.count, rank) == 8 ? go(Int<8>()) : go(Int<1>());
 }
@@ -1247,7 +1255,7 @@ hipError_t launch_shrink(const AdapterRows &o, int rank, const float *scale, con
     };
     if (rank > 64 && row_blocks(o.rows, o.count, rank) > 1)  // one pass over the rows
         return go(Int<8>(), Int<8>());
-    return by_size(o, rank, go);
+    return by_size(o, rank, TURNED && row_blocks(o.rows, o.count, rank) == 1 ? kMaxRank : 32, go);
 }
 
 template <class Y>
@@ -1315,7 +1323,8 @@ hipError_t launch_few(const AdapterRows &o, const moe_adapters &ad, const bf16_t
     return ad.rank <= 16 ? go(Int<1>()) : go(Int<2>());
 }
 
-size_t outer_lds(int nr) { return (size_t)4 * nr * 8 * 64 * sizeof(floatx4); }
+// The sums of half the waves, and the rows of a tile.
+size_t outer_lds(int nr) { return (size_t)4 * nr * 8 * 64 * sizeof(floatx4) + 512 * sizeof(int); }
 
 hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool accumulate,
                         Outer kb, Outer ka, hipStream_t s) {
