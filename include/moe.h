@@ -626,8 +626,8 @@ moe_status moe_route_scores_backward(const moe_dims *dims, const moe_routing *ro
  * calls allocate nothing, never synchronise and can be captured; a workspace
  * (16-byte aligned) serves one call at a time, and one for some rows serves fewer
  * too.  Outputs overlap no input but base and dx_base as said below.  Results are
- * deterministic; their bits depend on rows and count (which pick the tiles), not on
- * the other rows' adapters.  An infinity stays in the outputs that its formula
+ * deterministic; their bits depend on rows, count and widths (which pick the tiles),
+ * not on the other rows' adapters.  An infinity stays in the outputs that its formula
  * reaches, as an infinity or NaN.  Offsets outside [0, rows] are cut to it, and
  * entries of sorted_slot outside [0, rows) are passed over: their rows take no part.
  * Rows and widths that need 2^32 lanes in a launch (some 5 10^10 values of y) are

@@ -15,7 +15,10 @@ struct AdapterRows {
     const int32_t *offsets, *order, *place;
     int64_t rows;
     int count;
+    int blocks;  // of 16 rows of a tile, 1 or 8
 };
+// With the tiles' height, of the forward pass or the gradient.
+AdapterRows adapter_tiles(AdapterRows o, const moe_adapters &ad, bool back);
 
 // Sums over K of rows times a low-rank matrix, in fp32: [tile][split][rank][rows of
 // a tile], tiles as the device numbers them, a split a share of K; for many rows also
@@ -27,8 +30,8 @@ struct AdapterSums {
 };
 // Their layout at an address (together: how many sums share a launch), and its bytes
 // (no fewer than any fewer rows need).
-AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, int together, void *at);
-size_t adapter_sums_bytes(int64_t rows, int count, int rank);
+AdapterSums adapter_sums(const AdapterRows &o, int rank, int K, int together, void *at);
+size_t adapter_sums_bytes(int64_t rows, const moe_adapters &ad, bool back);
 
 // Whether every launch of these rows and widths (both directions') is one the device
 // takes.

@@ -13,6 +13,7 @@
 #include "adapters.h"
 
 #include <algorithm>
+#include <limits>
 #include <type_traits>
 
 #include "dispatch.h"
@@ -950,6 +951,7 @@ struct Outer {
     const bf16_t *q;
     float *parts, *out;
     int C, transposed, cb, blocks;  // cb: blocks of 512 columns
+    int shares;                     // workgroups that share the rank of a block
 };
 
 // Tiles of 2^sh rows before adapter e.
@@ -974,11 +976,12 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
     constexpr int TSH = tile_shift_of(RB), TM = 16 * RB, KR = kWaves / 4;
     floatx4 *sums = reinterpret_cast<floatx4 *>(lds);
     int *rows = reinterpret_cast<int *>(sums + 4 * NR * 8 * 64);
-    const Tile t = find_tile(o, sh, block / k.cb);
+    const int share = block % k.shares, at_cb = block / k.shares % k.cb;
+    const Tile t = find_tile(o, sh, block / k.shares / k.cb);
     if (t.e < 0 || (t.tiles > 1 && t.several + t.index >= slots)) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cw = wave % 4, rw = wave / 4;
-    const int col = (block % k.cb * 4 + cw) * 128 + 8 * m, qc = min(col, k.C - 8);
+    const int col = (at_cb * 4 + cw) * 128 + 8 * m, qc = min(col, k.C - 8);
     const int groups = (rank + 16 * NR - 1) / (16 * NR);
     const int64_t pt = tiles_before(o, TSH, t.e) + ((int64_t)t.index << (sh - TSH));
     // (offsets out of order may count more tiles than there are sums of)
@@ -994,7 +997,8 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
     // Rows of one step: the halves take groups of the rank in turn, with nothing to join.
     const bool one = RB == 1 && t.rows <= 32;
     const int from = one ? 0 : 32 * rw;
-    for (int grp = one ? rw : 0; grp < groups; grp += one ? KR : 1) {
+    for (int grp = share + (one ? rw * k.shares : 0); grp < groups;
+         grp += k.shares * (one ? KR : 1)) {
         const int r0 = grp * 16 * NR;
         floatx4 acc[NR][8] = {};
         u32x4 raw[8];
@@ -1192,21 +1196,31 @@ __global__ __launch_bounds__(256) void join_kernel(AdapterRows o, int sh, int sl
 int64_t tile_cap(int64_t rows, int count, int sh) {
     return (rows >> sh) + std::min<int64_t>(count, rows);
 }
-// Row blocks of a tile.  Tall ones read the adapters' matrices less often; they are
-// for many rows, where the adapters' mean rows fill most of one.  u's parts of a tile
-// have to fit LDS.  2048 rows of rank 64: 32 us against 45 in short ones, their gradient
-// 80 against 96.
-constexpr int64_t kTallRows = 1536;
+// Rows from which on tiles are tall.  Those read the adapters' matrices less often and
+// rows as whole lines, and take two launches more, some 12 us: worth it from so many
+// values of rows and outputs on, in the gradient the earlier the larger the rank, where
+// the adapters' mean rows fill half a tile and u's parts of a tile fit LDS.  us, short and
+// tall: rank 32, 4096 x 4096, 2100 rows 25.5 and 27.7, 3000 rows 37 and 29; 1024 x 2048, 4200
+// rows 19 and 26, 8200 rows 34 and 31.  The gradient: 4096 x 4096, rank 16, 3000 rows 47 and
+// 48, 6200 rows 72 and 67; rank 128, 1600 rows 117 and 107, 3000 rows 173 and 132.
+constexpr int64_t kTallValues = 18 << 20, kTallWork = 1 << 30;
+int64_t tall_from(const moe_adapters &ad, bool back) {
+    if (ad.rank > 128) return std::numeric_limits<int64_t>::max();
+    const int64_t width = (int64_t)ad.n + ad.k, work = width * (ad.rank + 24);
+    return std::max<int64_t>((int64_t)64 * ad.count, back ? (kTallWork + work - 1) / work
+                                                          : (kTallValues + width - 1) / width);
+}
+// Row blocks of 16 of a tile.
+int row_blocks(int64_t rows, const moe_adapters &ad, bool back) {
+    return rows >= tall_from(ad, back) ? 8 : 1;
+}
 // Values of x and A that every workgroup of expand reads itself (own_sums) rather than a
 // launch before it, at most: y of 4096 columns, rank 16, with and without it, us in a
 // graph: one row of 4096 k 8.4 and 8.8 (called one by one 8.5 and 11.0), of 8192 k 11.4
 // and 9.8; 100 rows of 1024 k 7.7 and 9.5.
 constexpr int64_t kFewValues = 98304;
-int row_blocks(int64_t rows, int count, int rank) {
-    return rank <= 128 && rows >= kTallRows && rows >= (int64_t)64 * count ? 8 : 1;
-}
-int64_t tile_count(const AdapterRows &o, int rank) {
-    return tile_cap(o.rows, o.count, tile_shift_of(row_blocks(o.rows, o.count, rank)));
+int64_t tile_count(const AdapterRows &o) {
+    return tile_cap(o.rows, o.count, tile_shift_of(o.blocks));
 }
 // Rows of a tile of the outer products, as a power of two: about 16 tiles, which with
 // some 16 column blocks fill the chip.
@@ -1223,7 +1237,7 @@ hipError_t by_size(const AdapterRows &o, int rank, int most, F fn) {
                : rank <= most ? fn(rb, Int<2>())
                               : fn(rb, Int<4>());
     };
-    return row_blocks(o.rows, o.count, rank) == 8 ? go(Int<8>()) : go(Int<1>());
+    return o.blocks == 8 ? go(Int<8>()) : go(Int<1>());
 }
 
 // More than 64 KB of LDS are asked for.
@@ -1253,9 +1267,9 @@ hipError_t launch_shrink(const AdapterRows &o, int rank, const float *scale, con
         }
         return hipSuccess;
     };
-    if (rank > 64 && row_blocks(o.rows, o.count, rank) > 1)  // one pass over the rows
+    if (rank > 64 && o.blocks > 1)  // one pass over the rows
         return go(Int<8>(), Int<8>());
-    return by_size(o, rank, TURNED && row_blocks(o.rows, o.count, rank) == 1 ? kMaxRank : 32, go);
+    return by_size(o, rank, TURNED && o.blocks == 1 ? kMaxRank : 32, go);
 }
 
 template <class Y>
@@ -1264,14 +1278,14 @@ Expand<Y> make_expand(const AdapterRows &o, int rank, int N, const AdapterSums &
     Expand<Y> k{};
     k.u = u, k.w = w, k.scale = scale, k.base = (const Y *)base, k.y = (Y *)y;
     k.N = N, k.span = kExpandSpan;
-    k.tiles = (int)tile_count(o, rank);
+    k.tiles = (int)tile_count(o);
     k.copies = base == y ? 0 : (int)((o.rows + 63) / 64);
     k.ranges = (N / 64 + k.span - 1) / k.span;
     return k;
 }
 template <class Y>
 size_t expand_lds(const AdapterRows &o, int rank) {
-    const int rb = row_blocks(o.rows, o.count, rank);
+    const int rb = o.blocks;
     const size_t u = (size_t)rb * ((rank / 8 * Four<Y>::S + 3) / 4 * 4) * 256;
     return rb > 1 ? u + (size_t)2 * 4 * (rank / 8) * kPitch * 16 : u;  // and B's two blocks
 }
@@ -1283,7 +1297,7 @@ unsigned expand_blocks(const Expand<Y> &k) {
 template <bool TURNED, class Y>
 hipError_t launch_expand(const AdapterRows &o, int rank, const Expand<Y> &k, hipStream_t s) {
     const size_t lds = expand_lds<Y>(o, rank);
-    const auto fn = row_blocks(o.rows, o.count, rank) == 8 ? expand_kernel<8, Y, TURNED>
+    const auto fn = o.blocks == 8 ? expand_kernel<8, Y, TURNED>
                                                            : expand_kernel<1, Y, TURNED>;
     if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
     fn<<<expand_blocks(k), 64 * kWaves, lds, s>>>(o, rank, k);
@@ -1303,9 +1317,9 @@ hipError_t launch_expand(const AdapterRows &o, int rank, int N, const AdapterSum
 // Whether every workgroup of expand has its sums itself: few values, and one workgroup a
 // compute unit.
 bool few_rows(const AdapterRows &o, const moe_adapters &ad) {
-    const int64_t tiles = tile_count(o, ad.rank);
+    const int64_t tiles = tile_count(o);
     const int64_t ranges = (ad.n / 64 + kExpandSpan - 1) / kExpandSpan;
-    return row_blocks(o.rows, o.count, ad.rank) == 1 && ad.rank <= 32 &&
+    return o.blocks == 1 && ad.rank <= 32 &&
            (ad.rank + std::min<int64_t>(o.rows, 16)) * ad.k <= kFewValues && tiles * ranges <= 256;
 }
 template <class Y>
@@ -1326,12 +1340,32 @@ hipError_t launch_few(const AdapterRows &o, const moe_adapters &ad, const bf16_t
 // The sums of half the waves, and the rows of a tile.
 size_t outer_lds(int nr) { return (size_t)4 * nr * 8 * 64 * sizeof(floatx4) + 512 * sizeof(int); }
 
+// Blocks of the outer products, which share the rank where they are few; returns the
+// rank blocks of a wave.  100 rows of one adapter, rank 128: the gradient 72 us where a
+// workgroup has all of the rank, 21 so; 64 adapters of them, rank 64: 78 with two rank
+// blocks a wave, 66 with one.
+constexpr int kOuterBlocks = 512;
+int size_outer(const AdapterRows &o, int rank, Outer &ka, Outer &kb) {
+    const int tiles = (int)tile_cap(o.rows, o.count, outer_shift(o.rows));
+    const int blocks = tiles * (ka.cb + kb.cb);
+    const int most = (rank + 15) / 16;
+    // one rank block a wave where that makes no more workgroups than are at home at once,
+    // or where adapters have a step of rows (more waves at a time)
+    const int nr =
+        most == 1 || (o.blocks == 1 && (blocks * most <= kOuterBlocks || o.rows <= 32 * o.count))
+            ? 1
+            : 2;
+    const int groups = (most + nr - 1) / nr;
+    ka.shares = kb.shares = std::max(1, std::min(groups, kOuterBlocks / blocks));
+    ka.blocks = tiles * ka.cb * ka.shares;
+    kb.blocks = tiles * kb.cb * kb.shares;
+    return nr;
+}
+
 hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool accumulate,
                         Outer kb, Outer ka, hipStream_t s) {
     const int sh = outer_shift(o.rows), slots = (int)outer_slots(o.rows);
-    const int tiles = (int)tile_cap(o.rows, o.count, sh);
-    ka.blocks = tiles * ka.cb;
-    kb.blocks = tiles * kb.cb;
+    const int nr = size_outer(o, rank, ka, kb);
     auto go = [&](auto rb, auto nr) {
         const auto fn = outer_kernel<rb(), nr()>;
         const size_t lds = outer_lds(nr());
@@ -1340,18 +1374,16 @@ hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool
                                                                        accumulate, kb, ka);
         return hipGetLastError();
     };
-    if (row_blocks(o.rows, o.count, rank) == 8)
-        return rank <= 16 ? go(Int<8>(), Int<1>()) : go(Int<8>(), Int<2>());
-    return rank <= 16 ? go(Int<1>(), Int<1>()) : go(Int<1>(), Int<2>());
+    if (o.blocks == 8)
+        return nr == 1 ? go(Int<8>(), Int<1>()) : go(Int<8>(), Int<2>());
+    return nr == 1 ? go(Int<1>(), Int<1>()) : go(Int<1>(), Int<2>());
 }
 
 template <class Y>
 hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const AdapterBack &k,
                         Outer kb, Outer ka, hipStream_t s) {
     const int sh = outer_shift(o.rows), slots = (int)outer_slots(o.rows);
-    const int tiles = (int)tile_cap(o.rows, o.count, sh), rank = ad.rank;
-    ka.blocks = tiles * ka.cb;
-    kb.blocks = tiles * kb.cb;
+    const int rank = ad.rank, nr = size_outer(o, rank, ka, kb);
     const auto kx = make_expand<Y>(o, rank, ad.k, k.v, ad.a, ad.scale, k.base, k.dx);
     auto go = [&](auto nr) {
         const auto fn = back_kernel<nr(), Y>;
@@ -1361,7 +1393,7 @@ hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const Adap
             o, rank, ad.scale, sh, slots, k.accumulate, kb, ka, kx);
         return hipGetLastError();
     };
-    return rank <= 16 ? go(Int<1>()) : go(Int<2>());
+    return nr == 1 ? go(Int<1>()) : go(Int<2>());
 }
 
 hipError_t launch_join(const AdapterRows &o, int rank, bool accumulate, const Outer &ka,
@@ -1376,8 +1408,7 @@ hipError_t launch_join(const AdapterRows &o, int rank, bool accumulate, const Ou
 
 // Shares of K that the sums of these rows are cut into: workgroups for every compute
 // unit at once, a step of 64 k for every wave.  together: sums in the same launch.
-int splits_of(int64_t rows, int count, int K, int rank, int together) {
-    const int rb = row_blocks(rows, count, rank);
+int splits_of(int64_t rows, int count, int K, int rb, int together) {
     const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift_of(rb)), 1);
     const int64_t want =
         rb > 1 ? 512 / tiles / together : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
@@ -1400,8 +1431,8 @@ size_t up(size_t v) { return (v + 255) & ~size_t(255); }
 struct SumsSize {
     size_t p, e, q;
 };
-SumsSize sums_size(int64_t rows, int count, int rank) {
-    const int rb = row_blocks(rows, count, rank), sh = tile_shift_of(rb);
+SumsSize sums_size(int64_t rows, int count, int rank, int rb) {
+    const int sh = tile_shift_of(rb);
     const int64_t tiles = tile_cap(rows, count, sh);
     // no more than splits * tiles of any K
     const int64_t sums = std::max(tiles, std::min<int64_t>(8 * tiles, rb == 1 ? 1024 : 512));
@@ -1416,29 +1447,33 @@ SumsSize sums_size(int64_t rows, int count, int rank) {
 }  // namespace
 
 bool adapter_launches_fit(int64_t rows, const moe_adapters &ad) {
-    const int rb = row_blocks(rows, ad.count, ad.rank);
+    const int rb = std::min(row_blocks(rows, ad, false), row_blocks(rows, ad, true));
     const int64_t tiles = tile_cap(rows, ad.count, tile_shift_of(rb));
     // two sums' blocks, those of few tiles in several shares of K
-    const int64_t shrink = std::max<int64_t>(tiles, 1024) * 2 * ((ad.rank + 63) / 64);
+    const int64_t shrink = std::max<int64_t>(tiles, 1024) * 2 * ((ad.rank + 31) / 32);
     const int64_t both = expand_cap(rows, tiles, std::max(ad.n, ad.k)) +
                          outer_cap(rows, ad.count, ad.n, ad.k);
     return std::max(shrink, both) * 64 * kWaves < int64_t(1) << 32;
 }
 
-size_t adapter_sums_bytes(int64_t rows, int count, int rank) {
-    auto bytes = [&](int64_t r) {
-        const SumsSize z = sums_size(r, count, rank);
-        return z.p + z.e + z.q;
-    };
-    // (the tiles' height changes at one number of rows)
-    const int64_t edge = std::max<int64_t>(kTallRows, (int64_t)64 * count);
-    return rows >= edge ? std::max(bytes(rows), bytes(edge - 1)) : bytes(rows);
+AdapterRows adapter_tiles(AdapterRows o, const moe_adapters &ad, bool back) {
+    o.blocks = row_blocks(o.rows, ad, back);
+    return o;
 }
 
-AdapterSums adapter_sums(int64_t rows, int count, int rank, int K, int together, void *at) {
-    const SumsSize z = sums_size(rows, count, rank);
+size_t adapter_sums_bytes(int64_t rows, const moe_adapters &ad, bool back) {
+    auto bytes = [&](int64_t r, int rb) {
+        const SumsSize z = sums_size(r, ad.count, ad.rank, rb);
+        return z.p + z.e + z.q;
+    };
+    const int64_t edge = tall_from(ad, back);
+    return rows >= edge ? std::max(bytes(rows, 8), bytes(edge - 1, 1)) : bytes(rows, 1);
+}
+
+AdapterSums adapter_sums(const AdapterRows &o, int rank, int K, int together, void *at) {
+    const SumsSize z = sums_size(o.rows, o.count, rank, o.blocks);
     char *p = (char *)at;
-    return {(float *)p, splits_of(rows, count, K, rank, together), (bf16_t *)(p + z.p),
+    return {(float *)p, splits_of(o.rows, o.count, K, o.blocks, together), (bf16_t *)(p + z.p),
             (bf16_t *)(p + z.p + z.e)};
 }
 
@@ -1456,23 +1491,23 @@ hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, con
         return y_type == MOE_FP32 ? launch_few<float>(o, ad, x, base, y, u, s)
                                   : launch_few<bf16_t>(o, ad, x, base, y, u, s);
     const Cut cut{y_type == MOE_FP32 ? 3 : 2, false};
-    const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o, ad.rank), cut};
+    const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o), cut};
     if (hipError_t e = launch_shrink<false>(o, ad.rank, ad.scale, ku, Shrink{}, s)) return e;
     return launch_expand<false>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y, y_type, s);
 }
 
 hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
                                    const AdapterBack &k, hipStream_t s) {
-    const Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 511) / 512, 0};
-    const Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 511) / 512, 0};
+    const Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 511) / 512, 0, 1};
+    const Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 511) / 512, 0, 1};
     if (o.rows) {
         // v = B^T dy, and for db u = A x
-        const int tiles = (int)tile_count(o, ad.rank);
+        const int tiles = (int)tile_count(o);
         const Cut cv{!k.dx ? 0 : k.dx_type == MOE_FP32 ? 3 : 2, k.da != nullptr};
         const Shrink kv{k.dy, ad.b, k.v, ad.n, tiles, cv};
         const Shrink ku = k.da ? Shrink{k.x, ad.a, k.u, ad.k, tiles, Cut{0, true}} : Shrink{};
         if (hipError_t e = launch_shrink<true>(o, ad.rank, ad.scale, kv, ku, s)) return e;
-        if (k.dx && k.da && row_blocks(o.rows, o.count, ad.rank) == 1) {
+        if (k.dx && k.da && o.blocks == 1) {
             // few rows: one launch for the three products
             if (hipError_t e = k.dx_type == MOE_FP32
                                    ? launch_short<float>(o, ad, k, kb, ka, s)

@@ -52,8 +52,8 @@ moe_status check_rows(const char *fn, const int32_t *offsets, const int32_t *sor
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
 
-size_t sums_bytes(int64_t rows, const moe_adapters *ad) {
-    return up(adapter_sums_bytes(rows, ad->count, ad->rank));
+size_t sums_bytes(int64_t rows, const moe_adapters *ad, bool back) {
+    return up(adapter_sums_bytes(rows, *ad, back));
 }
 
 struct BackWs {
@@ -67,8 +67,8 @@ BackWs back_ws(int64_t rows, const moe_adapters *ad) {
         o += up(bytes);
         return at;
     };
-    w.u = take(sums_bytes(rows, ad));
-    w.v = take(sums_bytes(rows, ad));
+    w.u = take(sums_bytes(rows, ad, true));
+    w.v = take(sums_bytes(rows, ad, true));
     w.pa = take(adapter_parts_bytes(rows, ad->rank, ad->k));
     w.pb = take(adapter_parts_bytes(rows, ad->rank, ad->n));
     w.total = o;
@@ -81,7 +81,7 @@ extern "C" {
 
 size_t moe_adapter_workspace_bytes(int64_t rows, const moe_adapters *adapters) {
     if (check_adapters("moe_adapter_workspace_bytes", rows, adapters) != MOE_OK) return 0;
-    return std::max<size_t>(sums_bytes(rows, adapters), 256);
+    return std::max<size_t>(sums_bytes(rows, adapters, false), 256);
 }
 
 moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const int32_t *offsets,
@@ -100,13 +100,13 @@ moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const in
     MOE_TRY(check_at(fn, "y", y));
     if (base != y) MOE_TRY(check_at(fn, "slot_row", slot_row, 4));
     const moe_adapters &ad = *adapters;
-    const size_t need = sums_bytes(rows, &ad);
+    const size_t need = sums_bytes(rows, &ad, false);
     if (!ws || ws_bytes < need)
         return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, need);
     MOE_TRY(check_at(fn, "ws", ws));
-    const AdapterRows o{offsets, sorted_slot, slot_row, rows, ad.count};
-    MOE_HIP(launch_adapter_rows(o, ad, x, base, y, y_type,
-                                adapter_sums(rows, ad.count, ad.rank, ad.k, 1, ws),
+    const AdapterRows o =
+        adapter_tiles({offsets, sorted_slot, slot_row, rows, ad.count, 0}, ad, false);
+    MOE_HIP(launch_adapter_rows(o, ad, x, base, y, y_type, adapter_sums(o, ad.rank, ad.k, 1, ws),
                                 (hipStream_t)stream));
     return MOE_OK;
 }
@@ -137,7 +137,8 @@ moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
         MOE_TRY(check_at(fn, "db", db));
     }
     const moe_adapters &ad = *adapters;
-    const AdapterRows o{offsets, sorted_slot, slot_row, rows, ad.count};
+    const AdapterRows o =
+        adapter_tiles({offsets, sorted_slot, slot_row, rows, ad.count, 0}, ad, true);
     AdapterBack k{};
     k.x = x, k.dy = dy;
     k.base = dx_base, k.dx = dx, k.dx_type = dx_type;
@@ -160,8 +161,8 @@ moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
         return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, ws_bytes, L.total);
     MOE_TRY(check_at(fn, "ws", ws));
     char *base = (char *)ws;
-    k.u = adapter_sums(rows, ad.count, ad.rank, ad.k, 2, base + L.u);
-    k.v = adapter_sums(rows, ad.count, ad.rank, ad.n, 2, base + L.v);
+    k.u = adapter_sums(o, ad.rank, ad.k, 2, base + L.u);
+    k.v = adapter_sums(o, ad.rank, ad.n, 2, base + L.v);
     k.pa = (float *)(base + L.pa), k.pb = (float *)(base + L.pb);
     MOE_HIP(launch_adapter_backward(o, ad, k, (hipStream_t)stream));
     return MOE_OK;

@@ -43,9 +43,12 @@ def test_bad_adapters(change, status):
 
 
 def test_workspaces():
-    L, ad = moe.lib(), handle(rank=64, n=4096, k=2048)
-    rows = [0, 1, 2, 17, 64, 100, 511, 512, 1000, 4096, 5000, 40000, 70000, 1 << 20]
-    for fn in (L.moe_adapter_workspace_bytes, L.moe_adapter_backward_bytes):
+    L = moe.lib()
+    rows = [0, 1, 2, 17, 64, 100, 511, 512, 1000, 1985, 1986, 2299, 2300, 4096, 5000, 40000,
+            70000, 1 << 20]
+    for fn, ad in ((f, handle(rank=r, n=4096, k=2048))
+                   for f in (L.moe_adapter_workspace_bytes, L.moe_adapter_backward_bytes)
+                   for r in (8, 64, 128, 256)):
         need = [fn(r, ctypes.byref(ad)) for r in rows]
         assert need == sorted(need) and need[0] > 0  # one for some rows serves fewer
         assert fn(-1, ctypes.byref(ad)) == 0 and fn(1 << 31, ctypes.byref(ad)) == 0
@@ -227,14 +230,19 @@ def test_rows(shape, dtype):
     assert torch.equal(w, y)
 
 
-# Many rows, in taller tiles: rows, n, k, rank, count, skewed (few adapters of many rows)
-MANY = [(1535, 192, 128, 32, 3, False), (1536, 64, 64, 8, 24, False),
-        (1536, 128, 64, 16, 25, True), (1537, 576, 320, 24, 24, True),
-        (1663, 64, 448, 32, 1, True), (1792, 1344, 64, 40, 5, False),
-        (2047, 128, 576, 64, 7, True), (2048, 448, 1344, 72, 3, False),
-        (2500, 704, 704, 128, 2, True), (3001, 64, 1024, 136, 4, True),
-        (4095, 512, 128, 16, 60, True), (4097, 128, 512, 120, 9, True),
-        (9000, 192, 192, 48, 1, False), (9001, 64, 4160, 64, 128, True)]
+# Many rows: rows, n, k, rank, count, skewed (few adapters of many rows); the latter ones in
+# tall tiles: from 18 * 2^20 values of (n + k) rows on, the gradient from 2^30 of
+# (n + k) (rank + 24) rows on, and 64 rows an adapter
+MANY = [(1536, 64, 64, 8, 24, False), (1537, 576, 320, 24, 24, True), (1663, 64, 448, 32, 1, True),
+        (2047, 128, 576, 64, 7, True), (2500, 704, 704, 128, 2, True), (3001, 64, 1024, 136, 4, True),
+        (4097, 128, 512, 120, 9, True), (9000, 192, 192, 48, 1, False),
+        (4600, 64, 7936, 8, 24, False), (4300, 6080, 2112, 16, 25, True),
+        (3001, 320, 8000, 24, 24, True), (2403, 7872, 448, 32, 1, True),
+        (2500, 64, 8192, 40, 5, False), (3100, 4096, 2112, 64, 7, True),
+        (2800, 1344, 5440, 72, 3, False), (2600, 5696, 1728, 128, 2, True),
+        (4097, 4160, 512, 120, 60, True), (9200, 192, 2048, 48, 1, False),
+        (16500, 64, 1088, 64, 128, True), (2303, 4096, 4096, 16, 36, False),
+        (2304, 4096, 4096, 16, 36, False), (2304, 4096, 4096, 16, 37, False)]
 
 
 def many(shape, seed=0):
@@ -466,11 +474,11 @@ def test_gradients_of_tall_tiles(shape, dtype):
 
 
 @gpu
-@pytest.mark.parametrize("R", [90, 2100])
-def test_gradients_pass_over_bad_rows(R):
+@pytest.mark.parametrize("R,n", [(90, 192), (2100, 192), (5000, 5696)])
+def test_gradients_pass_over_bad_rows(R, n):
     """Entries of sorted_slot outside the rows take no part in da and db, whatever
     row 0 holds."""
-    p = Problem(17, R, 192, 128, 16, 3)
+    p = Problem(17, R, n, 128, 16, 3)
     off, slot, row = p.order
     bad = torch.arange(3, int((p.ids >= 0).sum()), 11, device="cuda")
     worse = slot.clone()
@@ -577,9 +585,10 @@ def test_other_stream_and_captured_graph():
 
 
 @gpu
-def test_many_rows_captured_and_beside_another_call():
+@pytest.mark.parametrize("rows,width", [(1700, 576), (2300, 8192)])
+def test_many_rows_captured_and_beside_another_call(rows, width):
     """Two calls at once on streams and workspaces of their own; both captured."""
-    p, q = many((2300, 320, 576, 32, 7, True)), many((1700, 576, 320, 96, 2, False))
+    p, q = many((rows + 10, 320, width, 32, 7, True)), many((rows, width, 320, 96, 2, False))
     want = [forward(p, None, F32), *grads(p, BF16), forward(q, None, BF16), *grads(q, F32)]
     backward(p, None, *want[1:4])
     backward(q, None, *want[5:8])
