@@ -78,7 +78,8 @@ __device__ __forceinline__ int offset_at(const AdapterRows &o, int e) {
     return (int)min((int64_t)max(o.offsets[e], 0), o.rows);
 }
 
-// Tile t of all adapters' tiles of 2^sh rows; e < 0 behind the last.  Every lane
+// Tile t of all adapters' tiles of 2^sh rows; behind the last e < 0, and index counts on
+// from 0.  Every lane
 // takes four adapters' counts; a scan over the lanes finds the tile's.  The
 // result is uniform.
 __device__ __forceinline__ Tile find_tile(const AdapterRows &o, int sh, int t) {
@@ -95,7 +96,10 @@ __device__ __forceinline__ Tile find_tile(const AdapterRows &o, int sh, int t) {
     const int incl = wave_inclusive_scan(sum), sincl = wave_inclusive_scan(sev);
     Tile r{-1, 0, 0, 0, 0, 0};
     const uint64_t has = __ballot(incl > t);
-    if (!has) return r;
+    if (!has) {
+        r.index = t - __builtin_amdgcn_readlane(incl, 63);
+        return r;
+    }
     const int l = __builtin_ctzll(has);
     int left = t - (incl - sum), before = sincl - sev, q = 0, first = at[0], last = at[1];
 #pragma unroll
@@ -962,6 +966,29 @@ __device__ __forceinline__ int tiles_before(const AdapterRows &o, int sh, int e)
     return __builtin_amdgcn_readlane(wave_inclusive_scan(n), 63);
 }
 
+// The n-th adapter without rows, -1 if there are fewer.
+__device__ __forceinline__ int empty_adapter(const AdapterRows &o, int n) {
+    const int lane = threadIdx.x & 63;
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = 4 * lane + i;
+        mine += e < o.count && offset_at(o, e + 1) <= offset_at(o, e);
+    }
+    const int incl = wave_inclusive_scan(mine);
+    const uint64_t has = __ballot(incl > n);
+    if (!has) return -1;
+    const int l = __builtin_ctzll(has);
+    int left = n - __builtin_amdgcn_readlane(incl - mine, l);
+    for (int e = 4 * l; e < min(4 * l + 4, o.count); ++e)
+        if (offset_at(o, e + 1) <= offset_at(o, e) && left-- == 0) return e;
+    return -1;
+}
+
+// What becomes of da and db.  kZero: workgroups behind the last tile write the zeros of
+// adapters without rows (else the join does).
+enum { kSet = 0, kAdd = 1, kZero = 2 };
+
 // The contraction runs over rows, 32 an instruction.  A lane loads 8 rows x 8
 // columns of q and turns them in registers: the operands of eight instructions,
 // the j-th of which has column 8 (lane % 16) + j.  M is the rank.  Four waves stand
@@ -971,14 +998,26 @@ __device__ __forceinline__ int tiles_before(const AdapterRows &o, int sh, int e)
 // p and what it writes; twice the waves with half the registers spill (75 us).
 template <int RB, int NR>
 __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const float *scale, int sh,
-                                      int slots, bool accumulate, const Outer &k, int block,
+                                      int slots, int mode, const Outer &k, int block,
                                       char *lds) {
     constexpr int TSH = tile_shift_of(RB), TM = 16 * RB, KR = kWaves / 4;
     floatx4 *sums = reinterpret_cast<floatx4 *>(lds);
     int *rows = reinterpret_cast<int *>(sums + 4 * NR * 8 * 64);
     const int share = block % k.shares, at_cb = block / k.shares % k.cb;
     const Tile t = find_tile(o, sh, block / k.shares / k.cb);
-    if (t.e < 0 || (t.tiles > 1 && t.several + t.index >= slots)) return;
+    if (t.e < 0) {
+        const int e = mode == kZero ? empty_adapter(o, t.index) : -1;
+        if (e < 0) return;
+        const int c0 = at_cb * 512, C = min(512, k.C - c0), n = C * rank / 4;
+        float *to = k.out + (int64_t)e * rank * k.C;
+        for (int i = threadIdx.x + 64 * kWaves * share; i < n; i += 64 * kWaves * k.shares) {
+            float *d = k.transposed ? to + (int64_t)c0 * rank + 4 * i
+                                    : to + (int64_t)(i / (C / 4)) * k.C + c0 + i % (C / 4) * 4;
+            *reinterpret_cast<floatx4 *>(d) = floatx4{};
+        }
+        return;
+    }
+    if (t.tiles > 1 && t.several + t.index >= slots) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cw = wave % 4, rw = wave / 4;
     const int col = (at_cb * 4 + cw) * 128 + 8 * m, qc = min(col, k.C - 8);
@@ -1092,7 +1131,7 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
             __syncthreads();
         }
         if ((one || rw == 0) && col < k.C) {
-            const bool whole = t.tiles == 1, add = whole && accumulate;
+            const bool whole = t.tiles == 1, add = whole && mode == kAdd;
             float *to = whole ? k.out + (int64_t)t.e * rank * k.C
                               : k.parts + (int64_t)(t.several + t.index) * rank * k.C;
 #pragma unroll
@@ -1127,23 +1166,23 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
 template <int RB, int NR>
 __global__ __launch_bounds__(64 * kWaves) void outer_kernel(AdapterRows o, int rank,
                                                                  const float *scale, int sh,
-                                                                 int slots, int accumulate,
+                                                                 int slots, int mode,
                                                                  Outer kb, Outer ka) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int b = blockIdx.x;
-    outer<RB, NR>(o, rank, scale, sh, slots, accumulate, b < kb.blocks ? kb : ka,
+    outer<RB, NR>(o, rank, scale, sh, slots, mode, b < kb.blocks ? kb : ka,
                   b < kb.blocks ? b : b - kb.blocks, lds);
 }
 
 // Of few rows: those and the blocks of dx in one launch.
 template <int NR, class Y>
 __global__ __launch_bounds__(64 * kWaves, NR == 1 ? 4 : 2) void back_kernel(
-    AdapterRows o, int rank, const float *scale, int sh, int slots, int accumulate, Outer kb,
+    AdapterRows o, int rank, const float *scale, int sh, int slots, int mode, Outer kb,
     Outer ka, Expand<Y> kx) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int b = blockIdx.x;
     if (b < kb.blocks + ka.blocks)
-        outer<1, NR>(o, rank, scale, sh, slots, accumulate, b < kb.blocks ? kb : ka,
+        outer<1, NR>(o, rank, scale, sh, slots, mode, b < kb.blocks ? kb : ka,
                      b < kb.blocks ? b : b - kb.blocks, lds);
     else
         expand<1, Y, true>(o, rank, kx, b - kb.blocks - ka.blocks, lds);
@@ -1346,7 +1385,8 @@ size_t outer_lds(int nr) { return (size_t)4 * nr * 8 * 64 * sizeof(floatx4) + 51
 // blocks a wave, 66 with one.
 constexpr int kOuterBlocks = 512;
 int size_outer(const AdapterRows &o, int rank, Outer &ka, Outer &kb) {
-    const int tiles = (int)tile_cap(o.rows, o.count, outer_shift(o.rows));
+    const int tiles = (int)std::max<int64_t>(tile_cap(o.rows, o.count, outer_shift(o.rows)),
+                                             o.count);  // of adapters without rows too
     const int blocks = tiles * (ka.cb + kb.cb);
     const int most = (rank + 15) / 16;
     // one rank block a wave where that makes no more workgroups than are at home at once,
@@ -1362,7 +1402,7 @@ int size_outer(const AdapterRows &o, int rank, Outer &ka, Outer &kb) {
     return nr;
 }
 
-hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool accumulate,
+hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, int mode,
                         Outer kb, Outer ka, hipStream_t s) {
     const int sh = outer_shift(o.rows), slots = (int)outer_slots(o.rows);
     const int nr = size_outer(o, rank, ka, kb);
@@ -1371,7 +1411,7 @@ hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool
         const size_t lds = outer_lds(nr());
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
         fn<<<(unsigned)(ka.blocks + kb.blocks), 64 * kWaves, lds, s>>>(o, rank, scale, sh, slots,
-                                                                       accumulate, kb, ka);
+                                                                       mode, kb, ka);
         return hipGetLastError();
     };
     if (o.blocks == 8)
@@ -1381,7 +1421,7 @@ hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, bool
 
 template <class Y>
 hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const AdapterBack &k,
-                        Outer kb, Outer ka, hipStream_t s) {
+                        int mode, Outer kb, Outer ka, hipStream_t s) {
     const int sh = outer_shift(o.rows), slots = (int)outer_slots(o.rows);
     const int rank = ad.rank, nr = size_outer(o, rank, ka, kb);
     const auto kx = make_expand<Y>(o, rank, ad.k, k.v, ad.a, ad.scale, k.base, k.dx);
@@ -1390,7 +1430,7 @@ hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const Adap
         const size_t lds = std::max(outer_lds(nr()), expand_lds<Y>(o, rank));
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
         fn<<<ka.blocks + kb.blocks + expand_blocks(kx), 64 * kWaves, lds, s>>>(
-            o, rank, ad.scale, sh, slots, k.accumulate, kb, ka, kx);
+            o, rank, ad.scale, sh, slots, mode, kb, ka, kx);
         return hipGetLastError();
     };
     return nr == 1 ? go(Int<1>()) : go(Int<2>());
@@ -1422,7 +1462,7 @@ int64_t expand_cap(int64_t rows, int64_t tiles, int N) {
     return (tiles + (rows + 63) / 64) * ((N / 64 + kExpandSpan - 1) / kExpandSpan);
 }
 int64_t outer_cap(int64_t rows, int count, int n, int k) {
-    return tile_cap(rows, count, outer_shift(rows)) * ((n + 511) / 512 + (k + 511) / 512);
+    return std::max<int64_t>(tile_cap(rows, count, outer_shift(rows)), count) * ((n + 511) / 512 + (k + 511) / 512);
 }
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }
@@ -1500,6 +1540,9 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
                                    const AdapterBack &k, hipStream_t s) {
     const Outer ka{k.v, k.x, k.pa, k.da, ad.k, 0, (ad.k + 511) / 512, 0, 1};
     const Outer kb{k.u, k.dy, k.pb, k.db, ad.n, 1, (ad.n + 511) / 512, 0, 1};
+    // a tile an adapter at most: nothing to join
+    const bool joins = o.rows == 0 || o.rows > (int64_t)1 << outer_shift(o.rows);
+    const int mode = k.accumulate ? kAdd : joins ? kSet : kZero;
     if (o.rows) {
         // v = B^T dy, and for db u = A x
         const int tiles = (int)tile_count(o);
@@ -1510,8 +1553,8 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
         if (k.dx && k.da && o.blocks == 1) {
             // few rows: one launch for the three products
             if (hipError_t e = k.dx_type == MOE_FP32
-                                   ? launch_short<float>(o, ad, k, kb, ka, s)
-                                   : launch_short<bf16_t>(o, ad, k, kb, ka, s))
+                                   ? launch_short<float>(o, ad, k, mode, kb, ka, s)
+                                   : launch_short<bf16_t>(o, ad, k, mode, kb, ka, s))
                 return e;
         } else {
             if (k.dx)
@@ -1519,11 +1562,11 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
                                                        k.base, k.dx, k.dx_type, s))
                     return e;
             if (k.da)
-                if (hipError_t e = launch_outer(o, ad.rank, ad.scale, k.accumulate, kb, ka, s))
+                if (hipError_t e = launch_outer(o, ad.rank, ad.scale, mode, kb, ka, s))
                     return e;
         }
     }
-    return k.da ? launch_join(o, ad.rank, k.accumulate, ka, kb, s) : hipSuccess;
+    return k.da && joins ? launch_join(o, ad.rank, k.accumulate, ka, kb, s) : hipSuccess;
 }
 
 }  // namespace moe

@@ -211,7 +211,9 @@ SHAPES = [  # rows, n, k, rank, count
     (700, 256, 256, 64, 7), (1100, 704, 64, 32, 2), (3000, 64, 128, 8, 3),
     # either side of where a workgroup sums over k itself
     (1, 128, 12288, 8, 2), (3, 64, 6208, 16, 2), (16, 192, 2048, 32, 1), (16, 128, 2112, 32, 3),
-    (90, 4096, 128, 16, 2), (200, 4160, 64, 24, 40), (1400, 1536, 128, 16, 7)]
+    (90, 4096, 128, 16, 2), (200, 4160, 64, 24, 40), (1400, 1536, 128, 16, 7),
+    # up to and beyond the rows from which on gradients are joined
+    (127, 576, 64, 8, 3), (128, 64, 1088, 24, 130), (128, 128, 64, 48, 1), (129, 64, 128, 8, 200)]
 
 
 @gpu
@@ -509,6 +511,27 @@ def test_gradients_of_many_rows(R, count):
         backward(p, None, dx, da, db)
         check_backward(p, None, dx, da, db)
         assert (da[count:] == 0).all() and (db[count:] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("R,used", [(1, [37]), (5, [0, 255]), (128, [254]), (40, [])])
+def test_gradients_of_idle_adapters(R, used):
+    """Zeros for every adapter without rows, wherever it lies; nothing where they add."""
+    ids = torch.tensor([used[i % len(used)] if used else -1 for i in range(R)],
+                       dtype=torch.int32, device="cuda")
+    p = Problem(15, R, 576, 64, 16, 256, ids)
+    for dtype in (BF16, F32):
+        dx, da, db = grads(p, dtype)
+        backward(p, None, dx, da, db)
+        check_backward(p, None, dx, da, db)
+        da2, db2 = torch.full_like(da, 9.0), torch.full_like(db, 9.0)
+        backward(p, None, None, da2, db2)
+        assert torch.equal(da, da2) and torch.equal(db, db2)
+        da2.fill_(3.0), db2.fill_(3.0)
+        backward(p, None, dx, da2, db2, accumulate=True)
+        idle = torch.ones(256, dtype=torch.bool, device="cuda")
+        idle[used] = False
+        assert (da2[idle] == 3).all() and (db2[idle] == 3).all()
 
 
 @gpu
