@@ -1253,11 +1253,13 @@ int64_t tall_from(const moe_adapters &ad, bool back) {
 int row_blocks(int64_t rows, const moe_adapters &ad, bool back) {
     return rows >= tall_from(ad, back) ? 8 : 1;
 }
+
 // Values of x and A that every workgroup of expand reads itself (own_sums) rather than a
 // launch before it, at most: y of 4096 columns, rank 16, with and without it, us in a
 // graph: one row of 4096 k 8.4 and 8.8 (called one by one 8.5 and 11.0), of 8192 k 11.4
 // and 9.8; 100 rows of 1024 k 7.7 and 9.5.
 constexpr int64_t kFewValues = 98304;
+
 int64_t tile_count(const AdapterRows &o) {
     return tile_cap(o.rows, o.count, tile_shift_of(o.blocks));
 }
@@ -1414,8 +1416,7 @@ hipError_t launch_outer(const AdapterRows &o, int rank, const float *scale, int 
                                                                        mode, kb, ka);
         return hipGetLastError();
     };
-    if (o.blocks == 8)
-        return nr == 1 ? go(Int<8>(), Int<1>()) : go(Int<8>(), Int<2>());
+    if (o.blocks == 8) return nr == 1 ? go(Int<8>(), Int<1>()) : go(Int<8>(), Int<2>());
     return nr == 1 ? go(Int<1>(), Int<1>()) : go(Int<1>(), Int<2>());
 }
 
@@ -1462,7 +1463,8 @@ int64_t expand_cap(int64_t rows, int64_t tiles, int N) {
     return (tiles + (rows + 63) / 64) * ((N / 64 + kExpandSpan - 1) / kExpandSpan);
 }
 int64_t outer_cap(int64_t rows, int count, int n, int k) {
-    return std::max<int64_t>(tile_cap(rows, count, outer_shift(rows)), count) * ((n + 511) / 512 + (k + 511) / 512);
+    return std::max<int64_t>(tile_cap(rows, count, outer_shift(rows)), count) *
+           ((n + 511) / 512 + (k + 511) / 512);
 }
 
 size_t up(size_t v) { return (v + 255) & ~size_t(255); }

@@ -236,15 +236,16 @@ def test_rows(shape, dtype):
 # tall tiles: from 18 * 2^20 values of (n + k) rows on, the gradient from 2^30 of
 # (n + k) (rank + 24) rows on, and 64 rows an adapter
 MANY = [(1536, 64, 64, 8, 24, False), (1537, 576, 320, 24, 24, True), (1663, 64, 448, 32, 1, True),
-        (2047, 128, 576, 64, 7, True), (2500, 704, 704, 128, 2, True), (3001, 64, 1024, 136, 4, True),
-        (4097, 128, 512, 120, 9, True), (9000, 192, 192, 48, 1, False),
+        (2047, 128, 576, 64, 7, True), (2500, 704, 704, 128, 2, True),
+        (3001, 64, 1024, 136, 4, True), (4097, 128, 512, 120, 9, True), (9000, 192, 192, 48, 1, False),
         (4600, 64, 7936, 8, 24, False), (4300, 6080, 2112, 16, 25, True),
         (3001, 320, 8000, 24, 24, True), (2403, 7872, 448, 32, 1, True),
         (2500, 64, 8192, 40, 5, False), (3100, 4096, 2112, 64, 7, True),
         (2800, 1344, 5440, 72, 3, False), (2600, 5696, 1728, 128, 2, True),
         (4097, 4160, 512, 120, 60, True), (9200, 192, 2048, 48, 1, False),
         (16500, 64, 1088, 64, 128, True), (2303, 4096, 4096, 16, 36, False),
-        (2304, 4096, 4096, 16, 36, False), (2304, 4096, 4096, 16, 37, False)]
+        (2304, 4096, 4096, 16, 36, False), (2304, 4096, 4096, 16, 37, False),
+        (70, 64, 1 << 19, 16, 1, False), (65, 1 << 19, 64, 24, 1, False)]
 
 
 def many(shape, seed=0):
