@@ -213,7 +213,8 @@ SHAPES = [  # rows, n, k, rank, count
     (1, 128, 12288, 8, 2), (3, 64, 6208, 16, 2), (16, 192, 2048, 32, 1), (16, 128, 2112, 32, 3),
     (90, 4096, 128, 16, 2), (200, 4160, 64, 24, 40), (1400, 1536, 128, 16, 7),
     # up to and beyond the rows from which on gradients are joined
-    (127, 576, 64, 8, 3), (128, 64, 1088, 24, 130), (128, 128, 64, 48, 1), (129, 64, 128, 8, 200)]
+    (127, 576, 64, 8, 3), (128, 64, 1088, 24, 130), (128, 128, 64, 48, 1), (129, 64, 128, 8, 200),
+    (255, 128, 64, 24, 2), (256, 64, 576, 72, 2), (256, 64, 64, 16, 1)]
 
 
 @gpu
@@ -515,7 +516,8 @@ def test_gradients_of_many_rows(R, count):
 
 
 @gpu
-@pytest.mark.parametrize("R,used", [(1, [37]), (5, [0, 255]), (128, [254]), (40, [])])
+@pytest.mark.parametrize("R,used", [(1, [37]), (5, [0, 255]), (128, [254]), (40, []), (256, [9]),
+                                    (300, [3, 77])])
 def test_gradients_of_idle_adapters(R, used):
     """Zeros for every adapter without rows, wherever it lies; nothing where they add."""
     ids = torch.tensor([used[i % len(used)] if used else -1 for i in range(R)],
