@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside a shared projection,
 //   y = base + scale (x A^T) B^T,
 // and their gradient.  Rows are ordered by adapter, as the dispatch orders
-// tokens by expert; a tile is up to 16 or 64 rows of one adapter, found on the
+// tokens by expert; a tile is up to 16 or 128 rows of one adapter, found on the
 // device from the adapters' offsets.
 //
 // The sums over K of x A^T ("shrink") go through memory in fp32: rank values a
@@ -79,9 +79,8 @@ __device__ __forceinline__ int offset_at(const AdapterRows &o, int e) {
 }
 
 // Tile t of all adapters' tiles of 2^sh rows; behind the last e < 0, and index counts on
-// from 0.  Every lane
-// takes four adapters' counts; a scan over the lanes finds the tile's.  The
-// result is uniform.
+// from 0.  Every lane takes four adapters' counts; a scan over the lanes finds the
+// tile's.  The result is uniform.
 __device__ __forceinline__ Tile find_tile(const AdapterRows &o, int sh, int t) {
     const int lane = threadIdx.x & 63, TM = 1 << sh;
     int at[5], n[4], sum = 0, sev = 0;
@@ -669,10 +668,10 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
 // of a row (lanes side by side on one row: the cache takes a lane's 16 bytes of a row
 // of its own as slowly as 64 of a shared one).
 //
-// Tall tiles: the waves have a row block each and the same columns.  B
-// comes in as whole lines, by all of them, and lies in LDS as operands
-// [j][chunk][n][8], two blocks of 64 columns in turn.  Short tiles: the waves have
-// columns of their own and take B's operands from memory.
+// Tall tiles: the waves have a row block each and the same columns.  B comes in as
+// whole lines, by all of them, and lies in LDS as operands [j][chunk][n][8], two blocks
+// of 64 columns in turn, two more on their way.  Short tiles: the waves have columns of
+// their own and take B's operands from memory.
 //
 // 16384 rows of rank 64: 74 us, 66 without the products; a linear copy of the base alone
 // takes 61 there.  Gradient of 8192 rows, rank 32, w turned: 40.
@@ -1276,17 +1275,6 @@ int64_t outer_slots(int64_t rows, int count) {
 
 template <int N>
 using Int = std::integral_constant<int, N>;
-// fn(row blocks of a tile, rank blocks of a wave) of this size.
-template <class F>
-hipError_t by_size(const AdapterRows &o, int rank, int most, F fn) {
-    auto go = [&](auto rb) {
-        return rank <= 16   ? fn(rb, Int<1>())
-               : rank <= most ? fn(rb, Int<2>())
-                              : fn(rb, Int<4>());
-    };
-    return o.blocks == 8 ? go(Int<8>()) : go(Int<1>());
-}
-
 // More than 64 KB of LDS are asked for.
 hipError_t allow_lds(const void *fn, size_t lds) {
     return lds > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -1305,8 +1293,7 @@ hipError_t launch_shrink(const AdapterRows &o, int rank, const float *scale, con
                                     : (size_t)shrink_waves(1) / 2 * nr() * 64 * sizeof(floatx4);
         const auto fn = shrink_kernel<rb(), nr(), TURNED>;
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
-        fn<<<(unsigned)(na + nb), 64 * shrink_waves(rb()), lds, s>>>(o, rank, scale, a, b,
-                                                                        na);
+        fn<<<(unsigned)(na + nb), 64 * shrink_waves(rb()), lds, s>>>(o, rank, scale, a, b, na);
         if (hipError_t e = hipGetLastError()) return e;
         if (rb() > 1 && std::max(a.out.splits, b.out.splits) > 1) {
             cut_kernel<8><<<(unsigned)(a.tiles + b.tiles), 512, 0, s>>>(o, rank, scale, a, b);
@@ -1314,9 +1301,17 @@ hipError_t launch_shrink(const AdapterRows &o, int rank, const float *scale, con
         }
         return hipSuccess;
     };
-    if (rank > 64 && o.blocks > 1)  // one pass over the rows
-        return go(Int<8>(), Int<8>());
-    return by_size(o, rank, TURNED && o.blocks == 1 ? kMaxRank : 32, go);
+    if (o.blocks == 8)  // one pass over the rows
+        return rank <= 16   ? go(Int<8>(), Int<1>())
+               : rank <= 32 ? go(Int<8>(), Int<2>())
+               : rank <= 64 ? go(Int<8>(), Int<4>())
+                            : go(Int<8>(), Int<8>());
+    if (rank <= 16) return go(Int<1>(), Int<1>());
+    // (a turned w of more needs its registers: 1000 rows of rank 64 27 us, so 21)
+    if constexpr (TURNED)
+        return go(Int<1>(), Int<2>());
+    else
+        return rank <= 32 ? go(Int<1>(), Int<2>()) : go(Int<1>(), Int<4>());
 }
 
 template <class Y>
