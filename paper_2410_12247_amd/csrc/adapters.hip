@@ -24,6 +24,7 @@ namespace {
 constexpr int kWaves = 8;  // of expand (tall tiles: a row block each; short: 64 columns) and
                            // of outer (four column blocks, two halves of the rows)
 constexpr int kExpandSpan = 8;  // blocks of 64 columns of expand's workgroups
+constexpr int kMostSplits = 8;  // shares of K
 
 // Row blocks of 16 of a tile (1 or 8) -> rows of it, as a power of two.
 constexpr int tile_shift_of(int RB) { return RB == 8 ? 7 : 4; }
@@ -248,7 +249,7 @@ struct Shrink {
 // The four waves (and `splits` workgroups) share K, each taking every so many-th 128
 // bytes of a row, and keep DEP steps of them in flight.  A turned w comes a value a
 // lane: a load has 16 rank values of four k, side by side where the rank is 16.
-// 64 rows of as many adapters, 6144 k, rank 32: 7.7 us, a launch's chain of latencies
+// 64 rows of as many adapters, 6144 k, rank 32: 7.4 us, a launch's chain of latencies
 // (offsets, order, rows) and 15 MB; both sums of the gradient of 997 rows 10 us (with
 // the adapter transposed by a launch before it 11.2 + 3.8).
 template <int NR, bool TURNED>
@@ -1448,14 +1449,15 @@ hipError_t launch_join(const AdapterRows &o, int rank, bool accumulate, const Ou
     return hipGetLastError();
 }
 
-// Shares of K that the sums of these rows are cut into: workgroups for every compute
-// unit at once, a step of 64 k for every wave.  together: sums in the same launch.
+// Shares of K that the sums of these rows are cut into: a workgroup for every compute
+// unit (twice that: 64 rows of as many adapters, 4096 x 4096, rank 64 22 us in place of 19),
+// two where tiles are tall, and a step of 64 k for every wave.  together: sums in the same
+// launch.
 int splits_of(int64_t rows, int count, int K, int rb, int together) {
     const int64_t tiles = std::max<int64_t>(tile_cap(rows, count, tile_shift_of(rb)), 1);
-    const int64_t want =
-        rb > 1 ? 512 / tiles / together : ((rows < 512 ? 512 : 256) + tiles - 1) / tiles;
+    const int64_t want = rb > 1 ? 512 / tiles / together : (256 + tiles - 1) / tiles;
     const int64_t most = std::max(1, K / 64 / 4);
-    return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)8}));
+    return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)kMostSplits}));
 }
 
 // Blocks of 512 threads at most that a launch of expand, or of outer over both
@@ -1478,7 +1480,7 @@ SumsSize sums_size(int64_t rows, int count, int rank, int rb) {
     const int sh = tile_shift_of(rb);
     const int64_t tiles = tile_cap(rows, count, sh);
     // no more than splits * tiles of any K
-    const int64_t sums = std::max(tiles, std::min<int64_t>(8 * tiles, rb == 1 ? 1024 : 512));
+    const int64_t sums = std::max(tiles, std::min<int64_t>(kMostSplits * tiles, 512));
     SumsSize z{up((size_t)sums * rank * sizeof(float) << sh), 0, 0};
     if (rb > 1) {
         z.e = up((size_t)tiles * ((rank / 8 * 3 + 3) / 4 * 4) * 16 << sh);
