@@ -652,7 +652,8 @@ size_t moe_adapter_workspace_bytes(int64_t rows, const moe_adapters *adapters);
  * y[r] = base[r] for the others.  x [rows][k] bf16; base and y [rows][n] of y_type
  * (MOE_BF16 or MOE_FP32).  base may be y itself (the projection's output; rows
  * without an adapter are then not touched and slot_row may be NULL), or NULL for
- * zeros.  A x is held in fp32. */
+ * zeros.  A x is held in fp32 and multiplied in its 24 bits, whatever y's type; so is
+ * B^T dy below. */
 moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const int32_t *offsets,
                             const int32_t *sorted_slot, const int32_t *slot_row,
                             const moe_bf16 *x, const void *base, void *y, int32_t y_type, void *ws,

@@ -30,6 +30,7 @@ constexpr int kMostSplits = 8;  // shares of K
 constexpr int tile_shift_of(int RB) { return RB == 8 ? 7 : 4; }
 // The waves of shrink.
 constexpr int shrink_waves(int RB) { return RB == 1 ? 4 : RB; }
+constexpr int kParts = 3;   // bf16 parts that hold fp32's 24 bits
 constexpr int kPitch = 17;  // operands of 16 rows and one: writes of different banks
 
 __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
@@ -128,13 +129,12 @@ __device__ __forceinline__ int row_at(const AdapterRows &o, int64_t place) {
     return (uint32_t)row < (uint64_t)o.rows ? row : -1;
 }
 
-// hi + mid (+ lo): the leading 8 bits by cutting, the last part rounded.
-template <int S>
-__device__ __forceinline__ void cut(float v, uint32_t (&part)[S]) {
+// hi + mid + lo: the leading 8 bits by cutting, the last part rounded.
+__device__ __forceinline__ void cut(float v, uint32_t (&part)[kParts]) {
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
+    for (int i = 0; i < kParts; ++i) {
         const uint32_t u = __float_as_uint(v);
-        if (i + 1 < S) {
+        if (i + 1 < kParts) {
             part[i] = u >> 16;
             v = (u & 0x7F800000u) == 0x7F800000u ? 0.f : v - __uint_as_float(u & 0xFFFF0000u);
         } else {
@@ -144,18 +144,17 @@ __device__ __forceinline__ void cut(float v, uint32_t (&part)[S]) {
     }
 }
 // Eight values' parts, two to a word.
-template <int S>
-__device__ __forceinline__ void cut8(const float (&v)[8], bf16x8 (&part)[S]) {
-    u32x4 w[S] = {};
+__device__ __forceinline__ void cut8(const float (&v)[8], bf16x8 (&part)[kParts]) {
+    u32x4 w[kParts] = {};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        uint32_t c[S];
-        cut<S>(v[j], c);
+        uint32_t c[kParts];
+        cut(v[j], c);
 #pragma unroll
-        for (int q = 0; q < S; ++q) w[q][j / 2] |= c[q] << (16 * (j & 1));
+        for (int q = 0; q < kParts; ++q) w[q][j / 2] |= c[q] << (16 * (j & 1));
     }
 #pragma unroll
-    for (int q = 0; q < S; ++q) part[q] = __builtin_bit_cast(bf16x8, w[q]);
+    for (int q = 0; q < kParts; ++q) part[q] = __builtin_bit_cast(bf16x8, w[q]);
 }
 
 // v[j] += the sum over splits of p[split * pitch + j * TM], four splits' loads at once.
@@ -175,24 +174,16 @@ __device__ __forceinline__ void sum_splits(float (&v)[8], const float *p, int pi
 }
 
 // Sums of tall tiles, scaled and cut once a row for the many workgroups behind: by the
-// workgroup that has all of them, or where K is split by a launch of its own.  e: S
+// workgroup that has all of them, or where K is split by a launch of its own.  e:
 // parts as operands of expand, [tile][row block][chunk][row][8] with the chunks of
-// Expand; q: three parts as operands of outer, [tile][part][rank][row].  16384 rows of
+// Expand; q: parts as operands of outer, [tile][part][rank][row].  16384 rows of
 // rank 64: 6.4 us, where every workgroup of expand cutting for itself cost 40.
 struct Cut {
-    int S;  // parts of e; 0: none
-    bool q;
+    bool e, q;
 };
 
-__device__ __forceinline__ int chunks_of(int rank, int S) { return (rank / 8 * S + 3) / 4 * 4; }
-
-template <int S>
-__device__ __forceinline__ void store_parts(const float (&v)[8], bf16x8 *e, int chunk0, int rc,
-                                            int kc, int row) {
-    bf16x8 part[S];
-    cut8<S>(v, part);
-#pragma unroll
-    for (int s = 0; s < S; ++s) e[(chunk0 + s * rc + kc) * 16 + row] = part[s];
+__host__ __device__ __forceinline__ int chunks_of(int rank) {
+    return (rank / 8 * kParts + 3) / 4 * 4;
 }
 
 // p: [split][rank][row], PITCH values a rank value.
@@ -201,10 +192,10 @@ __device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const f
                                          const Cut &k, const AdapterSums &u, const Tile &t,
                                          int tile, const float *p, int splits) {
     constexpr int TM = 16 * RB;
-    const int rc = rank / 8, chunks = k.S ? chunks_of(rank, k.S) : 0;
+    const int rc = rank / 8, chunks = chunks_of(rank);
     const float f = scale ? scale[t.e] : 1.f;
     bf16x8 *e = reinterpret_cast<bf16x8 *>(u.e) + (int64_t)tile * chunks * TM;
-    uint16_t *q = u.q + (int64_t)tile * 3 * rank * TM;
+    uint16_t *q = u.q + (int64_t)tile * kParts * rank * TM;
     for (int i = threadIdx.x; i < TM * rc; i += 512) {
         const int row = i % TM, kc = i / TM;
         float v[8] = {};
@@ -213,23 +204,28 @@ __device__ __forceinline__ void cut_tile(const AdapterRows &o, int rank, const f
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= f;
         }
-        if (k.S == 2) store_parts<2>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
-        if (k.S == 3) store_parts<3>(v, e, (row >> 4) * chunks, rc, kc, row & 15);
+        if (k.e) {
+            bf16x8 part[kParts];
+            cut8(v, part);
+#pragma unroll
+            for (int s = 0; s < kParts; ++s)
+                e[((row >> 4) * chunks + s * rc + kc) * 16 + (row & 15)] = part[s];
+        }
         if (k.q) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t c[3];
-                cut<3>(v[j], c);
+                uint32_t c[kParts];
+                cut(v[j], c);
 #pragma unroll
-                for (int s = 0; s < 3; ++s)
+                for (int s = 0; s < kParts; ++s)
                     q[((int64_t)s * rank + 8 * kc + j) * TM + row] = (uint16_t)c[s];
             }
         }
     }
     // the padding behind the last part
-    const int pad = chunks - rc * k.S;
+    const int pad = k.e ? chunks - rc * kParts : 0;
     for (int i = threadIdx.x; i < TM * pad; i += 512) {
-        const int row = i % TM, c = rc * k.S + i / TM;
+        const int row = i % TM, c = rc * kParts + i / TM;
         e[((row >> 4) * chunks + c) * 16 + (row & 15)] = bf16x8{};
     }
 }
@@ -602,14 +598,12 @@ __global__ __launch_bounds__(512) void cut_kernel(AdapterRows o, int rank, const
 }
 
 // A lane's four columns of a row, next to each other (the lanes of a group have 64
-// between them).  S: bf16 parts of u, two for bf16 outputs (2^-15 of a value at worst,
-// where the output's rounding is 2^-8), three for fp32.
+// between them).
 template <class Y>
 struct Four;
 template <>
 struct Four<bf16_t> {
     typedef u32x2 V;
-    static constexpr int S = 2;
     static __device__ __forceinline__ V add(V base, floatx4 a) {
         return V{pack2(__uint_as_float(base[0] << 16) + a[0],
                        __uint_as_float(base[0] & 0xFFFF0000u) + a[1]),
@@ -620,7 +614,6 @@ struct Four<bf16_t> {
 template <>
 struct Four<float> {
     typedef u32x4 V;
-    static constexpr int S = 3;
     static __device__ __forceinline__ V add(V base, floatx4 a) {
         return __builtin_bit_cast(u32x4, __builtin_bit_cast(floatx4, base) + a);
     }
@@ -660,7 +653,7 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
     }
 }
 
-// The contraction runs over S * rank positions: the S parts of u one behind the
+// The contraction runs over three times the rank's positions: u's parts one behind the
 // other, against B's columns as many times.  Chunk c (8 positions) is part
 // c / (rank / 8) of u; chunks are padded to whole instructions of four.  Where
 // rank is a multiple of 32 an operand of B serves all parts.  M is the rows, N the
@@ -683,7 +676,7 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
                                        int block, char *lds) {
     using P = Four<Y>;
     using V = typename P::V;
-    constexpr int S = P::S, TM = 16 * RB;
+    constexpr int TM = 16 * RB;
     constexpr bool SHARED = RB > 1;
     constexpr int TH = 64 * kWaves, WC = SHARED ? 1 : kWaves;
     const int tile = block / k.ranges;
@@ -696,7 +689,7 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
     if (t.e < 0) return;
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b0 = SHARED ? wave : 0;
-    const int rc = rank / 8, chunks = chunks_of(rank, S);
+    const int rc = rank / 8, chunks = chunks_of(rank);
     const bool whole = rank % 32 == 0;
     const int steps = whole ? rc / 4 : chunks / 4;  // of B's operands
     const bf16_t *we = k.w + (int64_t)t.e * k.N * rank;
@@ -727,13 +720,13 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
     auto product = [&](const bf16x8(&wv)[4], int st) {
         if (whole) {
 #pragma unroll
-            for (int q = 0; q < S; ++q) {
+            for (int q = 0; q < kParts; ++q) {
                 const bf16x8 uv = u[(b0 * chunks + q * rc + 4 * st + g) * 16 + m];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[j] = mfma(uv, wv[j], acc[j]);
             }
         } else {
-            const bool pad = 4 * st + g >= rc * S;  // zeros against u's zeros: B may hold inf
+            const bool pad = 4 * st + g >= rc * kParts;  // zeros against u's zeros: B may hold inf
             const bf16x8 uv = u[(b0 * chunks + 4 * st + g) * 16 + m];
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[j] = mfma(uv, pad ? bf16x8{} : wv[j], acc[j]);
@@ -883,20 +876,20 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
             pt = reinterpret_cast<const float *>(at);
         }
         const int splits = OWN > 0 ? kWaves : k.u.splits;
-        for (int i = threadIdx.x; i < TM * (chunks - rc * (S - 1)); i += TH) {
+        for (int i = threadIdx.x; i < TM * (chunks - rc * (kParts - 1)); i += TH) {
             const int row = i % TM, kc = i / TM;
-            bf16x8 part[S] = {};
+            bf16x8 part[kParts] = {};
             if (row < t.rows && kc < rc) {
                 float v[8] = {};
                 sum_splits<TM>(v, pt + 8 * kc * TM + row, rank * TM, splits);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= f;
-                cut8<S>(v, part);
+                cut8(v, part);
             }
             // chunks behind the last part's are the padding
 #pragma unroll
-            for (int q = 0; q < S; ++q)
-                if (kc < rc || q + 1 == S) u[(q * rc + kc) * 16 + row] = part[q];
+            for (int q = 0; q < kParts; ++q)
+                if (kc < rc || q + 1 == kParts) u[(q * rc + kc) * 16 + row] = part[q];
         }
         __syncthreads();
         while (c < c1) {
@@ -1096,7 +1089,7 @@ __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const floa
                                        !(none && rows[k0 + 8 * g + i] < 0)
                                    ? pv[b][i / 4][i % 4] * f
                                    : 0.f;
-                    cut8<3>(v, part);
+                    cut8(v, part);
                 } else {
                     // (a tile's rows behind its last are zeros; eights behind that: no tile's)
 #pragma unroll
@@ -1326,10 +1319,9 @@ Expand<Y> make_expand(const AdapterRows &o, int rank, int N, const AdapterSums &
     k.ranges = (N / 64 + k.span - 1) / k.span;
     return k;
 }
-template <class Y>
 size_t expand_lds(const AdapterRows &o, int rank) {
     const int rb = o.blocks;
-    const size_t u = (size_t)rb * ((rank / 8 * Four<Y>::S + 3) / 4 * 4) * 256;
+    const size_t u = (size_t)rb * chunks_of(rank) * 256;
     return rb > 1 ? u + (size_t)2 * 4 * (rank / 8) * kPitch * 16 : u;  // and B's two blocks
 }
 template <class Y>
@@ -1339,7 +1331,7 @@ unsigned expand_blocks(const Expand<Y> &k) {
 
 template <bool TURNED, class Y>
 hipError_t launch_expand(const AdapterRows &o, int rank, const Expand<Y> &k, hipStream_t s) {
-    const size_t lds = expand_lds<Y>(o, rank);
+    const size_t lds = expand_lds(o, rank);
     const auto fn = o.blocks == 8 ? expand_kernel<8, Y, TURNED>
                                                            : expand_kernel<1, Y, TURNED>;
     if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
@@ -1371,7 +1363,7 @@ hipError_t launch_few(const AdapterRows &o, const moe_adapters &ad, const bf16_t
     auto k = make_expand<Y>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y);
     k.x = x, k.a = ad.a, k.K = ad.k;
     auto go = [&](auto nr) {
-        const size_t lds = expand_lds<Y>(o, ad.rank) + OwnSums<nr()>::LDS;
+        const size_t lds = expand_lds(o, ad.rank) + OwnSums<nr()>::LDS;
         const auto fn = few_kernel<nr(), Y>;
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
         fn<<<expand_blocks(k), 64 * kWaves, lds, s>>>(o, ad.rank, k);
@@ -1431,7 +1423,7 @@ hipError_t launch_short(const AdapterRows &o, const moe_adapters &ad, const Adap
     const auto kx = make_expand<Y>(o, rank, ad.k, k.v, ad.a, ad.scale, k.base, k.dx);
     auto go = [&](auto nr) {
         const auto fn = back_kernel<nr(), Y>;
-        const size_t lds = std::max(outer_lds(nr()), expand_lds<Y>(o, rank));
+        const size_t lds = std::max(outer_lds(nr()), expand_lds(o, rank));
         if (hipError_t e = allow_lds((const void *)fn, lds)) return e;
         fn<<<ka.blocks + kb.blocks + expand_blocks(kx), 64 * kWaves, lds, s>>>(
             o, rank, ad.scale, sh, slots, mode, kb, ka, kx);
@@ -1483,8 +1475,8 @@ SumsSize sums_size(int64_t rows, int count, int rank, int rb) {
     const int64_t sums = std::max(tiles, std::min<int64_t>(kMostSplits * tiles, 512));
     SumsSize z{up((size_t)sums * rank * sizeof(float) << sh), 0, 0};
     if (rb > 1) {
-        z.e = up((size_t)tiles * ((rank / 8 * 3 + 3) / 4 * 4) * 16 << sh);
-        z.q = up((size_t)tiles * 3 * rank * sizeof(bf16_t) << sh);
+        z.e = up((size_t)tiles * chunks_of(rank) * 16 << sh);
+        z.q = up((size_t)tiles * kParts * rank * sizeof(bf16_t) << sh);
     }
     return z;
 }
@@ -1535,8 +1527,7 @@ hipError_t launch_adapter_rows(const AdapterRows &o, const moe_adapters &ad, con
     if (few_rows(o, ad))
         return y_type == MOE_FP32 ? launch_few<float>(o, ad, x, base, y, u, s)
                                   : launch_few<bf16_t>(o, ad, x, base, y, u, s);
-    const Cut cut{y_type == MOE_FP32 ? 3 : 2, false};
-    const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o), cut};
+    const Shrink ku{x, ad.a, u, ad.k, (int)tile_count(o), Cut{true, false}};
     if (hipError_t e = launch_shrink<false>(o, ad.rank, ad.scale, ku, Shrink{}, s)) return e;
     return launch_expand<false>(o, ad.rank, ad.n, u, ad.b, ad.scale, base, y, y_type, s);
 }
@@ -1551,9 +1542,9 @@ hipError_t launch_adapter_backward(const AdapterRows &o, const moe_adapters &ad,
     if (o.rows) {
         // v = B^T dy, and for db u = A x
         const int tiles = (int)tile_count(o);
-        const Cut cv{!k.dx ? 0 : k.dx_type == MOE_FP32 ? 3 : 2, k.da != nullptr};
+        const Cut cv{k.dx != nullptr, k.da != nullptr};
         const Shrink kv{k.dy, ad.b, k.v, ad.n, tiles, cv};
-        const Shrink ku = k.da ? Shrink{k.x, ad.a, k.u, ad.k, tiles, Cut{0, true}} : Shrink{};
+        const Shrink ku = k.da ? Shrink{k.x, ad.a, k.u, ad.k, tiles, Cut{false, true}} : Shrink{};
         if (hipError_t e = launch_shrink<true>(o, ad.rank, ad.scale, kv, ku, s)) return e;
         if (k.dx && k.da && o.blocks == 1) {
             // few rows: one launch for the three products

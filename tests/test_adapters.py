@@ -572,6 +572,79 @@ def test_gradients_are_difference_quotients():
         assert abs(q - (grad.double() * step).sum()) <= 2.0 ** -15 * grad.norm() * step.norm()
 
 
+def whole_numbers(seed, R, n, k, rank, count, turned):
+    """A problem of whole numbers whose every sum is below 2^24, so exact in fp32 in any
+    order.  The rank's values stand in pairs of nearly equal ones with weights 1 and -1:
+    their sums over k (of dy over n where turned) have 16 to 20 bits and outputs some ten."""
+    p = Problem(seed, R, n, k, rank, count, pick(seed, R, count, 0.2 if R > 1 else 0.0))
+    g = torch.Generator().manual_seed(seed + 1)
+
+    def ints(most, *s):
+        return torch.randint(-most, most + 1, s, generator=g)
+    K, N = (n, k) if turned else (k, n)
+    rows, long = ints(255, R, K), ints(min(127, int(2 ** 24 * 1.8 / (140 * K))), count, rank, K)
+    long[:, 1::2] = long[:, ::2]
+    at = torch.randint(0, K, (count, rank // 2, 3), generator=g)
+    long[:, 1::2].scatter_add_(2, at, ints(1, *at.shape))
+    pair, sign = torch.randint(0, rank // 2, (count, N, 1), generator=g), ints(1, count, N, 1)
+    wide = torch.zeros((count, N, rank), dtype=torch.int64)
+    wide.scatter_(2, 2 * pair, sign).scatter_(2, 2 * pair + 1, -sign)
+    assert int((rows.abs() @ long.abs().flatten(0, 1).t()).max()) < 2 ** 24
+    if turned:
+        p.dy.copy_(rows), p.b.copy_(long.transpose(1, 2)), p.a.copy_(wide.transpose(1, 2))
+    else:
+        p.x.copy_(rows), p.a.copy_(long), p.b.copy_(wide)
+    p.scale.copy_(2.0 ** ints(2, count))
+    return p, ints(256, R, N).double().cuda()
+
+
+# one workgroup's own sums; short tiles, of ranks that fill whole instructions and that do
+# not; tall ones
+WHOLE = [(1, 576, 1344, 16, 4), (16, 192, 2048, 32, 1), (40, 128, 4096, 32, 3),
+         (200, 320, 704, 24, 6), (300, 512, 704, 200, 3), (1100, 704, 576, 64, 2),
+         (2403, 7872, 448, 32, 1), (3100, 4096, 2112, 64, 7), (2600, 5696, 1728, 128, 2),
+         (2500, 512, 8192, 40, 5)]
+
+
+@gpu
+@pytest.mark.parametrize("shape", WHOLE, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_sums_keep_their_bits(shape, dtype):
+    """Where the rank's terms cancel, outputs are what is left, rounded once: A x is
+    held, and multiplied, in fp32's 24 bits whatever the output's type."""
+    p, base = whole_numbers(sum(shape), *shape, turned=False)
+    d = torch.zeros((p.R, p.n), dtype=F64, device="cuda")
+    most = 0.0
+    for e, at in p.rows_of():
+        u = p.x[at].double() @ p.a[e].double().t()
+        most = max(most, float(u.abs().max()))
+        d[at] = p.factor(e) * (u @ p.b[e].double().t())
+    assert most >= 2 ** 16  # more bits than two bf16 parts hold
+    assert torch.equal(forward(p, None, dtype), d.to(dtype))
+    assert torch.equal(forward(p, base.to(dtype), dtype), (d + base).to(dtype))
+
+
+@gpu
+@pytest.mark.parametrize("shape", WHOLE, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_gradient_sums_keep_their_bits(shape, dtype):
+    """The same of dy B in dx, beside the gradients of A and B and by itself."""
+    p, base = whole_numbers(sum(shape) + 1, *shape, turned=True)
+    d = torch.zeros((p.R, p.k), dtype=F64, device="cuda")
+    most = 0.0
+    for e, at in p.rows_of():
+        v = p.dy[at].double() @ p.b[e].double()
+        most = max(most, float(v.abs().max()))
+        d[at] = p.factor(e) * (v @ p.a[e].double())
+    assert most >= 2 ** 16
+    dx, da, db = grads(p, dtype)
+    backward(p, None, dx, da, db)
+    assert torch.equal(dx, d.to(dtype))
+    dx.fill_(9.0)
+    backward(p, base.to(dtype), dx, None, None)
+    assert torch.equal(dx, (d + base).to(dtype))
+
+
 # ---- streams, graphs, workspaces, a layer -------------------------------------
 
 
