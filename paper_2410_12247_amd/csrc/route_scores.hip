@@ -755,31 +755,58 @@ template <int I>
 __device__ __forceinline__ uint32_t row_lane(uint32_t v) {  // lane I of the row
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x150 + I, 0xF, 0xF, false);
 }
-// Sum of c over the row's first eight lanes with the same id.
-__device__ __forceinline__ float same_id_sum(int id, float c) {
-    float s = 0.f;
-    auto add = [&](uint32_t other, uint32_t value) {
-        s += (int)other == id ? __uint_as_float(value) : 0.f;
-    };
-    const uint32_t i = (uint32_t)id, v = __float_as_uint(c);
-    add(row_lane<0>(i), row_lane<0>(v));
-    add(row_lane<1>(i), row_lane<1>(v));
-    add(row_lane<2>(i), row_lane<2>(v));
-    add(row_lane<3>(i), row_lane<3>(v));
-    add(row_lane<4>(i), row_lane<4>(v));
-    add(row_lane<5>(i), row_lane<5>(v));
-    add(row_lane<6>(i), row_lane<6>(v));
-    add(row_lane<7>(i), row_lane<7>(v));
+template <int I>
+__device__ __forceinline__ double row_lane_f64(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)row_lane<I>((uint32_t)(b >> 32)) << 32 |
+                                          row_lane<I>((uint32_t)b));
+}
+// fn(I) for each of the row's first eight lanes.
+template <class F>
+__device__ __forceinline__ void each_slot(F fn) {
+    fn(std::integral_constant<int, 0>()), fn(std::integral_constant<int, 1>());
+    fn(std::integral_constant<int, 2>()), fn(std::integral_constant<int, 3>());
+    fn(std::integral_constant<int, 4>()), fn(std::integral_constant<int, 5>());
+    fn(std::integral_constant<int, 6>()), fn(std::integral_constant<int, 7>());
+}
+// Sum of v over those with the same id.
+__device__ __forceinline__ double same_id_sum(int id, double v) {
+    double s = 0.0;
+    each_slot([&](auto i) {
+        const double o = row_lane_f64<i()>(v);
+        const int o_id = (int)row_lane<i()>((uint32_t)id);
+        s += o_id == id ? o : 0.0;
+    });
+    return s;
+}
+// Whether the lane is the first of its id.
+__device__ __forceinline__ bool first_of_id(int id, int l) {
+    bool first = true;
+    each_slot([&](auto i) {
+        const int o = (int)row_lane<i()>((uint32_t)id);  // (by all lanes: none is off)
+        first &= i() >= l | o != id;
+    });
+    return first;
+}
+// Sum of p_i (g - g_i) over those i.
+__device__ __forceinline__ double weighted_gaps(double p, double g) {
+    double s = 0.0;
+    each_slot([&](auto i) { s = fma(row_lane_f64<i()>(p), g - row_lane_f64<i()>(g), s); });
     return s;
 }
 
 // dz of four tokens.  Lane j < k of a token works out the chosen expert j's part:
-//   softmax over all     dz_e = s_e (sum over j with id e of G_j - D), D = sum G_j s_j
-//   softmax, renormalised dz_j = p_j (G_j - sum G p)      p: softmax over the chosen
-//   sigmoid              dz_j = G_j s (1 - s)
-//   sigmoid, renormalised dz_j = q_j (1 - s_j) (G_j - sum G q)   q: s over their sum
-// with G = scale dw, in 64 bits; the other experts' -s_e D in fp32.  65536 tokens of 256
-// experts, sigmoid: 17 us, 6.1 TB/s (a wave a token, without the rows through LDS: 53).
+//   softmax over all      dz_e = s_e (U g_e + sum p_i (g_e - g_i)) over the chosen experts
+//                         i, g_i the sum of their G, U the other experts' share; at those
+//                         -s_e D, D = sum G_j s_j
+//   softmax, renormalised dz_j = p_j sum p_i (G_j - G_i)      p: softmax over the chosen
+//   sigmoid               dz_j = G_j s (1 - s)
+//   sigmoid, renormalised dz_j = q_j (1 - s_j) sum q_i (G_j - G_i)   q: s over their sum
+// with G = scale dw, in 64 bits: G - D and 1 - s, which the sums stand for, would lose
+// what is left of them where one expert has nearly all.  The other experts' -s_e D is
+// a product of fp32 values.
+// 65536 tokens of 256 experts, sigmoid: 17 us, 6.1 TB/s (a wave a token, without the rows
+// through LDS: 53).
 template <int NV, class Z, bool ALIGNED>
 __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
     Rules r, const Z *__restrict__ z, const int32_t *__restrict__ ids,
@@ -802,8 +829,13 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
     float *mine = q.v + lane * Q::PITCH;
     float s[NV];
     float zmax = 0.f;
-    double sum = 1.0;
+    double sum = 1.0, rest = 0.0;
     if (all) {
+        uint32_t chosen = 0;  // of the lane's experts
+        each_slot([&](auto i) {
+            const uint32_t at = row_lane<i()>((uint32_t)id) - (uint32_t)(l * r.per);
+            chosen |= at < (uint32_t)r.per ? 1u << at : 0u;
+        });
         tokens_in<16, NV, Z, ALIGNED>(r, z + t0 * r.E, n, q);
         wave_sync();
         tokens_get(r, q, n, -INFINITY, s);
@@ -815,27 +847,31 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
             nan |= s[i] != s[i];
         }
         zmax = max_f32<16>(zmax);
-        if (lanes_true<16>(nan)) zmax = NAN;
+        const bool bad = lanes_true<16>(nan) != 0 || zmax == INFINITY;
         if (zmax == -INFINITY) zmax = 0.f;  // every expert switched off: all s are 0
-        float total = 0.f;
+        double total = 0.0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(kLog2e * (s[i] - zmax));
-            total += s[i];
+            const double e = exp_near((double)s[i] - zmax);
+            total += e;
+            rest += chosen >> i & 1 ? 0.0 : e;
+            s[i] = (float)e;
         }
-        total = sum_f32<16>(total);
-        sum = total > 0.f ? (double)total : total == 0.f ? 1.0 : (double)NAN;
+        total = sum_f64<16>(total);
+        sum = bad ? (double)NAN : total > 0.0 ? total : 1.0;
+        rest = sum_f64<16>(rest) / sum;
     }
     const double p = chosen_weight<16>(r.sigmoid, r.renorm, there, zj, zmax, sum);
     const double D = sum_f64<16>(G * p);
     double c;
-    if (r.sigmoid) {
-        const double rest = 1.0 / (1.0 + exp((double)zj));  // 1 - s
-        c = r.renorm ? p * rest * (G - D) : G * p * rest;
+    if (all) {
+        const double g = same_id_sum(id, G);
+        c = p * fma(rest, g, weighted_gaps(first_of_id(id, l) ? p : 0.0, g));
     } else {
-        c = r.renorm ? p * (G - D) : G * p;
+        c = r.renorm ? p * weighted_gaps(p, G) : G * p;
+        if (r.sigmoid) c *= 1.0 / (1.0 + exp((double)zj));  // 1 - s
+        c = same_id_sum(id, there ? c : 0.0);
     }
-    const float add = same_id_sum(id, there ? (float)c : 0.f);
     const float f = all ? (float)(-D / sum) : 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) s[i] = all ? s[i] * f : 0.f;
@@ -848,12 +884,8 @@ __global__ __launch_bounds__(64 * kWaves) void scores_back_kernel(
         for (int i = 0; i < NV; ++i) mine[i] = s[i];
     }
     wave_sync();
-    if (there) {  // (lanes of one id write the same value)
-        const int at = Q::at(r, (lane >> 4) * r.E + id);
-        const float was = q.v[at];
-        wave_sync();
-        q.v[at] = was + add;
-    }
+    if (there)  // (lanes of one id write the same value)
+        q.v[Q::at(r, (lane >> 4) * r.E + id)] = (float)c;
     wave_sync();
     Z *dst = dz + t0 * r.E;
     constexpr int IT = (NV + 3) / 4;

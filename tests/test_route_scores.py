@@ -412,6 +412,67 @@ def test_gradient_of_odd_choices(sigmoid, renorm):
     assert (dz[0] == 0).all() and (dz[5] == 0).all()
 
 
+def exact_gradient(z, ids, dw, sigmoid, renorm, scale):
+    """dz and the sum of its terms' magnitudes without a difference of sums:
+    s_e sum_i s_i (g_e - g_i) over all experts, g the gradient of their weights; over
+    the chosen slots with s of those alone where renormalised (times 1 - s of a
+    sigmoid's logit); in the host's longest type."""
+    f = np.longdouble
+    z, g = z.astype(f), dw.astype(f) * f(scale)
+    dz, size = np.zeros(z.shape, f), np.zeros(z.shape, f)
+    for t in range(len(z)):
+        on = ids[t] >= 0
+        at = ids[t][on]
+        if not len(at):
+            continue
+        if not renorm:
+            gt = np.zeros(z.shape[1], f)
+            np.add.at(gt, at, g[t][on])
+        if sigmoid and not renorm:
+            dz[t] = gt / (1 + np.exp(-z[t])) / (1 + np.exp(z[t]))
+            size[t] = np.abs(dz[t])
+            continue
+        zt, gt = (z[t][at], g[t][on]) if renorm else (z[t], gt)
+        s = 1 / (1 + np.exp(-zt)) if sigmoid else np.exp(zt - zt.max())
+        s = s / s.sum()
+        terms = (gt[:, None] - gt) * s * s[:, None]
+        if sigmoid:
+            terms = terms / (1 + np.exp(zt))[:, None]
+        if renorm:
+            np.add.at(dz[t], at, terms.sum(1))
+            np.add.at(size[t], at, np.abs(terms).sum(1))
+        else:
+            dz[t], size[t] = terms.sum(1), np.abs(terms).sum(1)
+    return dz, size
+
+
+@gpu
+@pytest.mark.parametrize("sigmoid", [False, True], ids=["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [False, True], ids=["raw", "renorm"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradient_of_confident_tokens(sigmoid, renorm, dtype):
+    """One logit, or two, ahead of the others by up to 80: what is left of 1 - s there."""
+    for E, k in ((8, 1), (8, 2), (61, 3), (160, 6), (256, 8)):
+        z = make(E + k, 99, E, F32).cpu() * 0.5
+        gap = torch.arange(99) % 33 * 2.5
+        z[torch.arange(99), torch.arange(99) * 7 % E] += gap
+        z[66:, 5] = z[66:].amax(1)  # two of them
+        z = z.to(dtype).cuda()
+        ids, _ = run(z, None, k, sigmoid, 1, 1, False, renorm, 2.5)
+        ids[40:45, -1] = -1
+        if k > 2:
+            ids[45:50, -1] = ids[45:50, 0]  # one expert twice
+        dw = torch.randn((99, k), generator=torch.Generator().manual_seed(E)).cuda()
+        dz = back(z, ids, dw, sigmoid, renorm, 2.5).double().cpu().numpy()
+        want, size = exact_gradient(z.double().cpu().numpy(), ids.cpu().numpy(),
+                                    dw.double().cpu().numpy(), sigmoid, renorm, 2.5)
+        # terms in 64 bits (exponentials to 2^-37, sums of 256 of them), at most three
+        # roundings to fp32, one to bf16; below fp32's normal range half of its step
+        half = 3 * 2.0 ** -24 + (2.0 ** -8 if dtype == BF16 else 0)
+        step = 2.0 ** (-134 if dtype == BF16 else -149)
+        assert (np.abs(dz - want) <= half * np.abs(want) + 2.0 ** -35 * size + step).all(), (E, k)
+
+
 @gpu
 @pytest.mark.parametrize("sigmoid", [False, True], ids=["softmax", "sigmoid"])
 @pytest.mark.parametrize("renorm", [False, True], ids=["raw", "renorm"])
