@@ -659,7 +659,8 @@ moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const in
                             const moe_bf16 *x, const void *base, void *y, int32_t y_type, void *ws,
                             size_t ws_bytes, void *stream);
 
-/* Workspace of moe_adapter_backward.  Host-only; 0 for invalid arguments. */
+/* Workspace of moe_adapter_backward, no less than moe_adapter_rows': one serves both.
+ * Host-only; 0 for invalid arguments. */
 size_t moe_adapter_backward_bytes(int64_t rows, const moe_adapters *adapters);
 
 /* Its gradient from dy [rows][n] bf16, the gradient of y (base's is dy itself):

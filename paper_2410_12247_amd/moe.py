@@ -643,6 +643,7 @@ def adapter_workspace_bytes(rows: int, ad: Adapters) -> int:
 
 
 def adapter_backward_bytes(rows: int, ad: Adapters) -> int:
+    """No less than adapter_workspace_bytes: one workspace serves both."""
     return lib().moe_adapter_backward_bytes(rows, ctypes.byref(ad))
 
 

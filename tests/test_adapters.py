@@ -55,6 +55,19 @@ def test_workspaces():
         assert fn(4, None) == 0
 
 
+@pytest.mark.parametrize("rank", [8, 16, 32, 64, 128, 136, 256])
+def test_the_gradients_workspace_serves_both(rank):
+    """On either side of where either direction's tiles become tall."""
+    for n, k in ((64, 64), (64, 512), (1344, 64), (8192, 64), (4096, 4096)):
+        for count in (1, 8, 256):
+            ad = handle(count, rank, n, k)
+            edges = [-(-(18 << 20) // (n + k)), -(-(1 << 30) // ((n + k) * (rank + 24))),
+                     64 * count, 1, 300, 40000]
+            for rows in (r + d for r in edges for d in (-1, 0, 1) if r + d > 0):
+                both = moe.adapter_workspace_bytes(rows, ad), moe.adapter_backward_bytes(rows, ad)
+                assert 0 < both[0] <= both[1], (n, k, count, rows)
+
+
 def test_refusals():
     L = moe.lib()
     need = L.moe_adapter_workspace_bytes(4, ctypes.byref(handle()))
