@@ -628,8 +628,10 @@ moe_status moe_route_scores_backward(const moe_dims *dims, const moe_routing *ro
  * too.  Outputs overlap no input but base and dx_base as said below.  Results are
  * deterministic; their bits depend on rows, count and widths (which pick the tiles),
  * not on the other rows' adapters.  An infinity stays in the outputs that its formula
- * reaches, as an infinity or NaN.  Offsets outside [0, rows] are cut to it, and
- * entries of sorted_slot outside [0, rows) are passed over: their rows take no part.
+ * reaches, as an infinity or NaN.  Offsets ascend (where they do not, nothing outside the
+ * outputs is touched); those outside [0, rows] are cut to it.  Entries of sorted_slot
+ * outside [0, rows) are passed over.  A row whose place in slot_row has another entry, or
+ * lies in no adapter's range, is a row without an adapter.
  * Rows and widths that need 2^32 lanes in a launch (some 5 10^10 values of y) are
  * MOE_ERR_UNSUPPORTED. */
 

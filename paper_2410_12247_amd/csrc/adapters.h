@@ -10,7 +10,7 @@ constexpr int kRankAlign = 8;  // a 16-byte load of an adapter row
 
 // The rows of a launch, ordered by adapter (moe_permute's outputs): places
 // [offsets[e], offsets[e + 1]) belong to adapter e, place p is row order[p];
-// place[row] < 0 for a row of no adapter.
+// place[row] is row's, < 0 for a row of no adapter.
 struct AdapterRows {
     const int32_t *offsets, *order, *place;
     int64_t rows;

@@ -129,6 +129,13 @@ __device__ __forceinline__ int row_at(const AdapterRows &o, int64_t place) {
     return (uint32_t)row < (uint64_t)o.rows ? row : -1;
 }
 
+// Whether a row is that of a place of an adapter's (offsets that ascend).
+__device__ __forceinline__ bool has_place(const AdapterRows &o, int64_t row) {
+    const int p = o.place[row];
+    const bool in = p >= offset_at(o, 0) && p < offset_at(o, o.count);
+    return in && o.order[in ? p : 0] == row;
+}
+
 // hi + mid + lo: the leading 8 bits by cutting, the last part rounded.
 __device__ __forceinline__ void cut(float v, uint32_t (&part)[kParts]) {
 #pragma unroll
@@ -634,14 +641,14 @@ struct Expand {
     int K;
 };
 
-// Rows of no adapter: base's row (zeros without one), 64 rows a workgroup.
+// Rows of no adapter, or of no place: base's row (zeros without one), 64 rows a workgroup.
 template <class Y>
 __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> &k, int block,
                                           int c0, int c1) {
     constexpr int V = 16 / sizeof(Y);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t mine = (int64_t)block * 64 + lane;
-    uint64_t none = __ballot(mine < o.rows && o.place[min(mine, o.rows - 1)] < 0);
+    uint64_t none = __ballot(mine < o.rows && !has_place(o, min(mine, o.rows - 1)));
     for (int i = 0; none; ++i, none &= none - 1) {
         if (i % kWaves != wave) continue;
         const int64_t at = ((int64_t)block * 64 + __builtin_ctzll(none)) * k.N;

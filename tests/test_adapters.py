@@ -363,6 +363,56 @@ def test_bad_indices_are_passed_over():
     torch.cuda.synchronize()
 
 
+def whole_order(ids, count):
+    """offsets, sorted_slot, slot_row with the rows of no adapter behind the others."""
+    key = torch.where(ids < 0, count, ids)
+    slot = torch.argsort(key, stable=True)
+    off = torch.zeros(count + 1, dtype=torch.int32, device="cuda")
+    off[1:] = torch.bincount(key, minlength=count + 1)[:count].cumsum(0)
+    row = torch.empty_like(ids)
+    row[slot] = torch.arange(len(ids), dtype=torch.int32, device="cuda")
+    row[ids < 0] = -1
+    return off, slot.int(), row
+
+
+@gpu
+@pytest.mark.parametrize("R,n", [(1, 128), (100, 128), (700, 192), (5000, 5696)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_rows_out_of_order_are_rows_of_no_adapter(R, n, dtype):
+    """Bad entries of sorted_slot, and offsets that end early, late or fall: every
+    output is written, as for rows without an adapter where no place is theirs."""
+    p = Problem(18, R, n, 128, 16, 4)
+    p.ids[0] = 2
+    off, slot, row = whole_order(p.ids, 4)
+    used, ids = int(off[-1]), p.ids.clone()
+    bad = torch.arange(0, used, 7, device="cuda")
+    worse = slot.clone()
+    worse[bad] = torch.tensor([-1, R, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32,
+                              device="cuda").repeat(len(bad))[:len(bad)]
+    without = ids.clone()
+    without[slot[bad].long()] = -1
+    short, late = off.clone(), off.clone()
+    short[-1] = max(int(off[-2]), used - 3)
+    fewer = ids.clone()
+    fewer[slot[int(short[-1]):used].long()] = -1
+    late[0], late[-1] = -5, 2 ** 31 - 1  # the last adapter has the others' rows too
+    place = row.clone()
+    place[slot[used:].long()] = torch.arange(used, R, dtype=torch.int32, device="cuda")
+    for order, has in (((off, slot, row), ids), ((off, worse, row), without),
+                       ((short, slot, row), fewer),
+                       ((late, slot, place), torch.where(ids < 0, 3, ids)),
+                       ((off.flip(0).contiguous(), slot, row), torch.full_like(ids, -1))):
+        p.order, p.ids = order, has
+        for base, dx0 in ((p.normal(1, n, dtype), p.normal(2, 128, dtype)), (None, None)):
+            check_forward(p, forward(p, base, dtype), base)
+            dx, da, db = grads(p, dtype)
+            backward(p, dx0, dx, da, db)
+            check_backward(p, dx0, dx, da, db)
+            if base is not None:
+                forward(p, base, dtype, y=base, place=False)
+                check_forward(p, base, p.normal(1, n, dtype))
+
+
 @gpu
 def test_offsets_past_32_bits():
     """x and y of more than 4 GiB."""
