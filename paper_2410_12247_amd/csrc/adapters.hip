@@ -903,6 +903,10 @@ __device__ __forceinline__ void expand(const AdapterRows &o, int rank, const Exp
             clear();
             product(first, 0);
             for (int st = 1; st < steps; ++st) {
+                if (4 % rc == 0) {  // (rank 16: the same operands of B)
+                    product(first, st);
+                    continue;
+                }
                 bf16x8 wv[4];
                 load_w(wv, c, st);
                 product(wv, st);
