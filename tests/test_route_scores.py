@@ -312,6 +312,60 @@ def test_rules_over_many_tokens(E, k, G, top):
         assert torch.equal(w[:5000].view(torch.int32), w2.view(torch.int32))
 
 
+def compare(z, bias, k, at, **rules):
+    """run() over all tokens against 64 bits at some."""
+    ids, w = run(z, bias, k, **rules)
+    rid, rw = ref.route(z[at].double().cpu().numpy(),
+                        None if bias is None else bias.double().cpu().numpy(), k, **rules)
+    np.testing.assert_array_equal(ids[at].cpu().numpy(), rid)
+    np.testing.assert_allclose(w[at].cpu().numpy(), rw, rtol=2.0 ** -23, atol=2.0 ** -150)
+
+
+@gpu
+@pytest.mark.parametrize("sigmoid", [False, True], ids=["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k,G,top", [(256, 8, 8, 4), (256, 8, 1, 1), (160, 6, 8, 3),
+                                       (200, 3, 5, 2), (12, 4, 3, 2)])
+def test_biases_of_any_size(E, k, G, top, sigmoid):
+    """Finite biases on either side of 4: as a common offset, at one expert or at some
+    among small ones, and so large that scores vanish beside them."""
+    g = torch.Generator().manual_seed(E)
+    small = torch.randn(E, generator=g) * 0.1
+    some = small.clone()
+    some[::5], some[1::7], some[3] = -10.0, 20.0, 1e3
+    one = small.clone()
+    one[E // 3] = -10.0
+    biases = [small + c for c in (3.5, -3.5, 3.9, 4.1, -4.1, 20.0, -20.0)]
+    biases += [one, -one, some, -some, torch.full((E,), 1e30), torch.full((E,), -3e38)]
+    for T in (37, 16387):
+        z = make(E + T, T, E, F32, 0, sigmoid)
+        at = torch.arange(0, T, 37 if T < 100 else 1021).cuda()
+        at = torch.cat([torch.arange(30).cuda(), at, torch.arange(T - 3, T).cuda()])
+        for i, b in enumerate(biases):
+            compare(z.to(BF16) if i % 4 == 3 else z, b.cuda(), k, at, sigmoid=sigmoid, groups=G,
+                    top_groups=top, pair=i % 2 == 0, renorm=i % 3 == 0, scale=2.0)
+
+
+@gpu
+@pytest.mark.parametrize("T", [997, 16387])
+def test_what_fp32_does_not_decide(T):
+    """Softmax scores with a bias of their size, and logits of which the last chosen
+    lie far below the largest: many tokens, or all, are done in 64 bits."""
+    at = torch.arange(0, T, T // 60).cuda()
+    for E, k, G, top in ((256, 8, 8, 4), (256, 8, 1, 1), (160, 6, 8, 3)):
+        g = torch.Generator().manual_seed(E)
+        z = torch.randn((T, E), generator=g).cuda()
+        b = (torch.randn(E, generator=g) / E).cuda()
+        for pair in (False, True):
+            for renorm in (False, True):
+                rules = dict(sigmoid=False, groups=G, top_groups=top, pair=pair, renorm=renorm,
+                             scale=1.0)
+                compare(z * 0.3, b, k, at, **rules)
+                compare(z * 0.001, b, k, at, **rules)
+                compare(z * 8, None, k, at, **rules)
+                compare(z * 8, b, k, at, **rules)
+                compare(z * 8, None, k, at, **{**rules, "sigmoid": True})
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_any_address(dtype):
@@ -526,6 +580,35 @@ def test_gradient_of_many_tokens():
     assert (np.abs(dz[at].double().cpu().numpy() - want) <= 2.0 ** -20 * g).all()
     rest = torch.ones_like(dz, dtype=torch.bool).scatter_(1, ids.long(), False)
     assert (dz[rest] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("E,k,renorm", [(256, 8, False), (160, 6, False), (61, 3, False),
+                                        (256, 8, True)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_softmax_gradient_of_many_tokens(E, k, renorm, dtype):
+    T = 40003
+    z = make(52, T, E, dtype)
+    z[5 * 997] = -math.inf
+    z[6 * 997, E // 2:] = -math.inf
+    ids, _ = run(z, None, k, False, 1, 1, False, renorm, 1.5)
+    dw = torch.randn((T, k), generator=torch.Generator().manual_seed(7)).cuda()
+    dz = back(z, ids, dw, False, renorm, 1.5)
+    at = torch.cat([torch.arange(0, T, 997), torch.arange(T - 5, T)]).cuda()
+    want = ref.route_backward(z[at].double().cpu().numpy(), ids[at].cpu().numpy(),
+                              dw[at].double().cpu().numpy(), False, renorm, 1.5)
+    # of the definition's difference s (g - s g): 2^-50 of |G|; of the kernel's values at
+    # most three roundings to fp32, one to bf16
+    half = 3 * 2.0 ** -24 + (2.0 ** -8 if dtype == BF16 else 0)
+    g = 1.5 * dw[at].abs().amax(1, keepdim=True).double().cpu().numpy()
+    err = np.abs(dz[at].double().cpu().numpy() - want)
+    assert (err <= half * np.abs(want) + 2.0 ** -33 * g).all()
+    assert dz.isfinite().all()
+    if renorm:
+        rest = torch.ones_like(dz, dtype=torch.bool).scatter_(1, ids.clamp(min=0).long(), False)
+        assert (dz[rest] == 0).all()
+    dz2 = back(z[:5000], ids[:5000], dw[:5000], False, renorm, 1.5)
+    assert torch.equal(dz[:5000], dz2)
 
 
 @gpu
