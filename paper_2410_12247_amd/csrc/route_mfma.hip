@@ -427,15 +427,24 @@ bool mfma_router_selects_apart(const moe_dims &d, const float *logits) {
                           mfma_cost(d.tokens, 32, blocks_per_wave(eb)));
 }
 
-// One tile of a wave while the SIMDs take them at once, then more tokens and
-// experts per workgroup, which read fewer operands.
+// A tile a wave by itself while the SIMDs take them at once, or of one expert block;
+// else 2 x 2 waves of a tile, which read fewer operands; 8 waves of eight tiles where
+// their rounds of one workgroup a compute unit, each some 13 rounds of the others' tiles,
+// come out as fewer.  us of the three (bound by the chains of fp32 products: 16384 x 160
+// at H = 5120 is 27 GFLOP, 175 at the 154 TFLOP/s of a library's fp32 product):
+//   H = 5120   1 x 160 24 25 288    4096 x 160 75 67 300    8192 x 160 132 114 299
+//     16384 x 160 287 236 301   32768 x 160 847 520 595   16384 x 256 452 372 303
+//     65536 x 256 2744 1655 1210
+//   H = 6144   16384 x 16 51 66 352   65536 x 16 196 231 708   16384 x 32 86 67 353
 hipError_t launch_route_logits(const moe_dims &d, const bf16_t *x, const float *wr, float *z,
                                hipStream_t s) {
-    const int64_t simds = 4 * (int64_t)device_cu_count();
-    if (tile_waves(d) <= simds) return launch_mfma_logits<1, 1, 1, 1, 6>(d, x, wr, nullptr, z, s);
-    if (expert_blocks(d) <= 2 || tile_waves(d) <= 4 * simds)
-        return launch_mfma_logits<1, 1, 2, 2, 3>(d, x, wr, nullptr, z, s);
-    return launch_mfma_logits<2, 4, 4, 2, 3>(d, x, wr, nullptr, z, s);
+    const int64_t cus = device_cu_count(), simds = 4 * cus, tiles = tile_waves(d);
+    const int64_t large = (d.tokens + 127) / 128 * ((d.experts + 127) / 128);
+    if (tiles <= simds || expert_blocks(d) == 1)
+        return launch_mfma_logits<1, 1, 1, 1, 6>(d, x, wr, nullptr, z, s);
+    if ((large + cus - 1) / cus * 13 < (tiles + simds - 1) / simds)
+        return launch_mfma_logits<2, 4, 4, 2, 3>(d, x, wr, nullptr, z, s);
+    return launch_mfma_logits<1, 1, 2, 2, 3>(d, x, wr, nullptr, z, s);
 }
 
 extern "C" int32_t moe_router_shape_for_tests(const moe_dims *d, int32_t *blocks) {

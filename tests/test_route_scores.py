@@ -648,6 +648,23 @@ def test_route_logits_are_moe_routes(T, H, E):
 
 
 @gpu
+@pytest.mark.parametrize("T,H,E", [(16380, 64, 256), (16385, 64, 256), (33000, 128, 250),
+                                   (20000, 192, 16), (16384, 64, 17), (5000, 64, 100)])
+def test_route_logits_of_many_tokens(T, H, E):
+    """On either side of where tiles grow; the rows around stay as they were."""
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn((T, H), generator=g).to(BF16).cuda()
+    wr = (torch.randn((E, H), generator=g) * 0.05).cuda()
+    flat = torch.full(((T + 2) * E,), 7.0, device="cuda")
+    z = flat[E:-E].view(T, E)
+    moe.route_logits(moe.dims(T, H, 64, E, 1), x, wr, z)
+    want = x.double() @ wr.double().t()
+    size = x.double().abs() @ wr.double().abs().t()
+    assert ((z - want).abs() <= H * 2.0 ** -24 * size).all()  # a chain of H fp32 roundings
+    assert (flat[:E] == 7).all() and (flat[-E:] == 7).all()
+
+
+@gpu
 def test_other_stream_and_captured_graph():
     T, E, k = 333, 160, 6
     z = make(71, T, E, F32)
