@@ -592,8 +592,8 @@ moe_status moe_route_logits(const moe_dims *dims, const moe_bf16 *x, const float
  *                      ascending)
  *   topk_w[t][j] = scale * s[id_j], with dims->renormalize scale * s[id_j] / sum
  *                  of the chosen s
- * Choices and group values are compared in 64 bits, weights computed in 64 bits
- * and rounded to fp32; choices nearer to each other than 2^-50 may come in either
+ * Choices and group values are compared in 64 bits, weights computed in 64 bits (the
+ * softmax's sum over all experts to 2^-37) and rounded to fp32; choices nearer to each other than 2^-50 may come in either
  * order.  An expert is switched off by a logit of -inf, or by a choice of -inf or
  * NaN (its bias'); it is never chosen.  Where fewer than k are left, the last ids
  * are -1 with weight 0 (moe_permute and moe_combine pass over them).  A token with

@@ -7,8 +7,8 @@
 // The sums over K of x A^T ("shrink") go through memory in fp32: rank values a
 // row, where the rows themselves have thousands.  The products behind it take
 // them cut into bf16 parts (hi + mid + lo hold all 24 bits), so that the matrix
-// cores multiply bf16 by bf16 without a rounding.  All of it is bound by memory: the
-// matrix cores are busy 5 to 10% of the time.  Times below are of one call among
+// cores multiply bf16 by bf16 without a rounding.  Few rows are bound by latencies, many
+// by memory: the matrix cores are busy 1 to 13% of the time.  Times below are of one call among
 // others on inputs of their own (4096 x 4096, bf16 y, where nothing else is said).
 #include "adapters.h"
 
@@ -184,7 +184,7 @@ __device__ __forceinline__ void sum_splits(float (&v)[8], const float *p, int pi
 // workgroup that has all of them, or where K is split by a launch of its own.  e:
 // parts as operands of expand, [tile][row block][chunk][row][8] with the chunks of
 // Expand; q: parts as operands of outer, [tile][part][rank][row].  16384 rows of
-// rank 64: 6.4 us, where every workgroup of expand cutting for itself cost 40.
+// rank 64: 7.2 us, where every workgroup of expand cutting for itself cost 40.
 struct Cut {
     bool e, q;
 };
@@ -674,8 +674,9 @@ __device__ __forceinline__ void copy_rows(const AdapterRows &o, const Expand<Y> 
 // of 64 columns in turn, two more on their way.  Short tiles: the waves have columns of
 // their own and take B's operands from memory.
 //
-// 16384 rows of rank 64: 74 us, 66 without the products; a linear copy of the base alone
-// takes 61 there.  Gradient of 8192 rows, rank 32, w turned: 40.
+// 16384 rows of rank 64: 80 us (75 with two parts of u, 66 without the products); a
+// linear copy of the base alone takes 61 there.  Gradient of 8192 rows, rank 32, w turned:
+// 42.
 //
 // OWN: rank blocks of own_sums, 0 where the sums come from memory.
 template <int RB, class Y, bool TURNED, int OWN = 0>
@@ -998,8 +999,9 @@ enum { kSet = 0, kAdd = 1, kZero = 2 };
 // the j-th of which has column 8 (lane % 16) + j.  M is the rank.  Four waves stand
 // side by side, 128 columns each, and read the same of p; two such rows of waves take
 // steps of 32 rows in turn and join in LDS.  p in three parts: the sums are as exact
-// as fp32's.  8192 rows, rank 32, both: 36 us for 134 MB of x and dy, 4.8 TB/s with
-// p and what it writes; twice the waves with half the registers spill (75 us).
+// as fp32's.  8192 rows, rank 32, both: 38 us for 134 MB of x and dy, 4.7 TB/s with p and
+// what it writes; twice the waves with half the registers spill (75 us).  Every 16 NR rank
+// values read q anew.
 template <int RB, int NR>
 __device__ __forceinline__ void outer(const AdapterRows &o, int rank, const float *scale, int sh,
                                       int slots, int mode, const Outer &k, int block,
@@ -1243,9 +1245,11 @@ int64_t tile_cap(int64_t rows, int count, int sh) {
 // rows as whole lines, and take two launches more, some 12 us: worth it from so many
 // values of rows and outputs on, in the gradient the earlier the larger the rank, where
 // the adapters' mean rows fill half a tile and u's parts of a tile fit LDS.  us, short and
-// tall: rank 32, 4096 x 4096, 2100 rows 25.5 and 27.7, 3000 rows 37 and 29; 1024 x 2048, 4200
-// rows 19 and 26, 8200 rows 34 and 31.  The gradient: 4096 x 4096, rank 16, 3000 rows 47 and
-// 48, 6200 rows 72 and 67; rank 128, 1600 rows 117 and 107, 3000 rows 173 and 132.
+// tall: rank 32, 4096 x 4096, 1800 rows 29 and 31, 3000 rows 42 and 36 (2100 rows, where
+// short tiles just need a round more, 38 and 32); 1024 x 2048, 3000 rows 21 and 25, 6000
+// rows 33 and 34, 8200 rows 45 and 37.  The gradient: 4096 x 4096, rank 16, 3000 rows 56
+// and 59, 6200 rows 104 and 91; rank 128, 1600 rows 158 and 128, 3000 rows 222 and 151.
+// Ranks above 128 have short tiles only: rank 256, 8192 rows 344, the gradient 857.
 constexpr int64_t kTallValues = 18 << 20, kTallWork = 1 << 30;
 int64_t tall_from(const moe_adapters &ad, bool back) {
     if (ad.rank > 128) return std::numeric_limits<int64_t>::max();
@@ -1260,8 +1264,8 @@ int row_blocks(int64_t rows, const moe_adapters &ad, bool back) {
 
 // Values of x and A that every workgroup of expand reads itself (own_sums) rather than a
 // launch before it, at most: y of 4096 columns, rank 16, with and without it, us in a
-// graph: one row of 4096 k 8.4 and 8.8 (called one by one 8.5 and 11.0), of 8192 k 11.4
-// and 9.8; 100 rows of 1024 k 7.7 and 9.5.
+// graph: one row of 4096 k 8.4 and 8.9 (called one by one 8.5 and 11.0), of 8192 k 11.4
+// and 9.9; 100 rows of 1024 k 8.2 and 9.8.
 constexpr int64_t kFewValues = 98304;
 
 int64_t tile_count(const AdapterRows &o) {

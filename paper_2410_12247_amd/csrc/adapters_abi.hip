@@ -114,7 +114,8 @@ moe_status moe_adapter_rows(int64_t rows, const moe_adapters *adapters, const in
 size_t moe_adapter_backward_bytes(int64_t rows, const moe_adapters *adapters) {
     if (check_adapters("moe_adapter_backward_bytes", rows, adapters) != MOE_OK) return 0;
     // (the forward pass has tall tiles, which need more, from fewer rows on at small ranks)
-    return std::max<size_t>({back_ws(rows, adapters).total, sums_bytes(rows, adapters, false), 256});
+    return std::max<size_t>(
+        {back_ws(rows, adapters).total, sums_bytes(rows, adapters, false), 256});
 }
 
 moe_status moe_adapter_backward(int64_t rows, const moe_adapters *adapters,
